@@ -446,6 +446,161 @@ int ifvs_train_step(ifvs_index* ix, const float* queries, const ifvs_predicate* 
 int ifvs_get_conditioning(ifvs_index* ix, float* bank, float* W, uint32_t flags);
 
 /*
+ * Layers of a predicate encoder.  §2 takes w_z from a learned encoder of the
+ * predicate whose architecture the paper does not give; ifvs_search_batch
+ * takes the vectors that such an encoder makes and ifvs_train_grad returns
+ * dL/dw_z for it.  The calls below are the operators to build one from, each
+ * with its gradient: embedding lookup, norms around a block joined with its
+ * gate and residual, gated feed-forward block.
+ *
+ * Arrays are row-major device memory on the handle's device, contiguous, all
+ * of one element type per call; index arrays say their own.  Sums, norms and
+ * statistics are float32; every output is rounded once.  Sums run in a fixed
+ * order: equal calls give equal bits.  Outputs must not overlap inputs or
+ * each other.
+ *
+ * A handle holds the workspace, the order of the calls that use it, and an
+ * error word.  With a non-NULL stream a call only enqueues its work there
+ * (the legacy default stream is cudaStreamLegacy, (void*)1) and the handle's
+ * next call waits for it on the device, whatever that call's stream; with
+ * stream NULL it runs on a stream of the handle's own, a blocking one, and
+ * returns when its outputs are written.  A call whose workspace has to grow
+ * allocates (and waits for the device): run the largest shape once before a
+ * stream capture.  Errors that a kernel finds (a token id or offsets out of
+ * range, a bounded wait that ran out) are returned by the call itself when it
+ * waits, else by ifvs_layers_status.  A handle may be used by one thread at
+ * a time.
+ */
+typedef struct ifvs_layers ifvs_layers;
+
+/* Element types. */
+enum { IFVS_T_F32 = 0, IFVS_T_F16 = 1, IFVS_T_BF16 = 2 };
+/* Activations of the gated feed-forward block: x sigmoid(x), x Phi(x) with
+ * the normal distribution function Phi, max(x, 0). */
+enum { IFVS_ACT_SILU = 0, IFVS_ACT_GELU = 1, IFVS_ACT_RELU = 2 };
+
+#define IFVS_MAX_WIDTH 8192      /* largest row width D of the layers          */
+#define IFVS_MAX_HIDDEN 65536    /* largest hidden width F of ifvs_ffn         */
+
+/* ifvs_layers_create — a handle on `device` (free with ifvs_layers_free,
+ * which waits for the handle's work). */
+int ifvs_layers_create(ifvs_layers** out, int32_t device);
+void ifvs_layers_free(ifvs_layers* L);
+
+/* ifvs_layers_status — waits for the work enqueued through the handle,
+ * returns the error that its kernels found since the last status call or
+ * waiting call (IFVS_OK: none) and clears it. */
+int ifvs_layers_status(ifvs_layers* L);
+
+/*
+ * ifvs_embed — out[t] = scale table[ids[t]].
+ *   table  [V][D] of `type`;  ids [T] int32: 0..V-1, or -1 (padding): a row
+ *          of zeros
+ *   out    [T][D] of `type`
+ * An id outside -1..V-1 gives zeros and IFVS_ERR_ARG (as described above).
+ * Errors: IFVS_ERR_ARG (NULL, T < 0, V outside 1..2^31 - 1, D outside
+ * 1..IFVS_MAX_WIDTH, unknown type, an array not aligned to its elements,
+ * scale not finite).
+ */
+int ifvs_embed(ifvs_layers* L, const void* table, int64_t V, int32_t D, int32_t type, const int32_t* ids,
+               int64_t T, float scale, void* out, void* stream);
+
+/*
+ * ifvs_embed_grad — d_table[v] = scale sum over the tokens t with ids[t] = v
+ * of d_out[t]; zeros for ids that no token has.  The tokens are sorted by id
+ * and each id's rows summed in an order that depends on T alone.
+ *   d_out [T][D], d_table [V][D] of `type`; T < 2^31.  Padding adds nothing;
+ * other ids outside 0..V-1 add nothing and are reported.  Errors as
+ * ifvs_embed, plus IFVS_ERR_OOM.
+ */
+int ifvs_embed_grad(ifvs_layers* L, const void* d_out, const int32_t* ids, int64_t T, int64_t V, int32_t D,
+                    int32_t type, float scale, void* d_table, void* stream);
+
+/* What ifvs_norm_join and its gradient share. */
+typedef struct {
+    int64_t T;          /* tokens, 0 <= T < 2^31                              */
+    int32_t D;          /* width, 1..IFVS_MAX_WIDTH                           */
+    int32_t type;       /* IFVS_T_* of every array but offsets                */
+    int64_t n_seq;      /* sequences B >= 1 (rows of `gate`); B < 2^31        */
+    const int64_t* offsets; /* [B+1]: tokens [offsets[b], offsets[b+1]) are
+                           sequence b; offsets[0] = 0, offsets[B] = T, not
+                           decreasing (equal: an empty sequence).  NULL for
+                           B = 1: all tokens                                  */
+    const void* gate;   /* [B][D], or NULL: ones                              */
+    const void* w_post; /* [D] weight of the norm after the block             */
+    const void* w_pre;  /* [D] weight of the norm before the next block, or
+                           NULL: there is no such norm                        */
+    float res_scale;    /* scale of the residual                              */
+    float eps;          /* > 0, added to the mean square in both norms        */
+    void* stream;
+} ifvs_join_params;
+
+/*
+ * ifvs_norm_join — around one block of an encoder, in one pass:
+ *   x_out = res_scale x + gate_b * w_post * y / rms(y)
+ *   n_out = w_pre * x_out / rms(x_out),   rms(v) = sqrt(mean(v^2) + eps)
+ * for the tokens of sequence b: the norm after the block whose output is y,
+ * its gate, the residual x, the norm before the next block.
+ *   x, y, x_out, n_out [T][D].  n_out NULL iff w_pre NULL.  y NULL (with
+ *   gate, w_post and x_out NULL): only the norm n_out of x.
+ * n_out is computed from x_out before its rounding.  Offsets that break their
+ * rules give unspecified values in the tokens concerned and are reported;
+ * they make no access out of range.  Errors: IFVS_ERR_ARG.
+ */
+int ifvs_norm_join(ifvs_layers* L, const ifvs_join_params* p, const void* x, const void* y, void* x_out,
+                   void* n_out);
+
+/*
+ * ifvs_norm_join_grad — gradients of a loss through ifvs_norm_join.
+ *   x_out, y       the forward call's output and block output [T][D]
+ *   d_x_out, d_n   gradients of x_out and n_out [T][D]; either may be NULL
+ *                  (zero), not both; d_n needs w_pre
+ *   dx, dy         [T][D] out
+ *   d_gate         [B][D] out, or NULL; zeros for an empty sequence
+ *   d_w_post, d_w_pre  [D] out; d_w_pre NULL when d_n is
+ * With y NULL (the forward call had none; x_out is its x, d_x_out what x
+ * receives from elsewhere) only dx and d_w_pre are written, res_scale is
+ * taken as 1 and gate, w_post, dy, d_gate, d_w_post are NULL.
+ * Errors: IFVS_ERR_ARG, IFVS_ERR_OOM.
+ */
+int ifvs_norm_join_grad(ifvs_layers* L, const ifvs_join_params* p, const void* x_out, const void* y,
+                        const void* d_x_out, const void* d_n, void* dx, void* dy, void* d_gate, void* d_w_post,
+                        void* d_w_pre);
+
+typedef struct {
+    int64_t T;          /* tokens, 0 <= T < 2^31                              */
+    int32_t D;          /* width, a multiple of 8, 8..IFVS_MAX_WIDTH          */
+    int32_t F;          /* hidden width, a multiple of 8, 8..IFVS_MAX_HIDDEN  */
+    int32_t type;       /* IFVS_T_F16 or IFVS_T_BF16                          */
+    int32_t act;        /* IFVS_ACT_*                                         */
+    const void* w_in;   /* [2F][D]: the gate's rows, then the up projection's */
+    const void* w_out;  /* [D][F]                                             */
+    void* stream;
+} ifvs_ffn_params;
+
+/*
+ * ifvs_ffn — gated feed-forward block y = (act(x Wg^T) * (x Wu^T)) w_out^T,
+ * w_in = [Wg; Wu].
+ *   x, y [T][D].  Arrays must be aligned to 16 bytes.
+ * The hidden values act(g) * u are rounded to `type` between the two
+ * products (in IFVS_T_F16 values beyond 65504 become infinite).
+ * Errors: IFVS_ERR_ARG, IFVS_ERR_UNSUPPORTED (IFVS_T_F32; D or F not a
+ * multiple of 8), IFVS_ERR_OOM.
+ */
+int ifvs_ffn(ifvs_layers* L, const ifvs_ffn_params* p, const void* x, void* y);
+
+/*
+ * ifvs_ffn_grad — gradients of a loss through ifvs_ffn from dL/dy; the
+ * hidden values are computed again from x, nothing is kept between the calls.
+ *   dy, dx [T][D]; d_w_in [2F][D]; d_w_out [D][F]
+ * The hidden values and their gradients are rounded to `type` before the
+ * products that sum over tokens or over F.  T = 0 writes zeros to d_w_in and
+ * d_w_out.  Errors as ifvs_ffn.
+ */
+int ifvs_ffn_grad(ifvs_layers* L, const ifvs_ffn_params* p, const void* x, const void* dy, void* dx,
+                  void* d_w_in, void* d_w_out);
+
+/*
  * ifvs_stage_times — device time (ms, from CUDA events recorded on the
  * launching stream around each launch) and launch counts per stage,
  * accumulated over calls made with IFVS_F_STAGE_TIMING.  Those calls run every

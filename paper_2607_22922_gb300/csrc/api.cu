@@ -49,6 +49,8 @@ int cuda_fail(cudaError_t e, const char* what, int line) {
         if (rc_ != 0) return rc_; \
     } while (0)
 
+}  // namespace
+
 // Every device allocation of the library goes through device_malloc.
 // Failure injection for tests of the error path (no GPU fault involved):
 // while the environment variable IFVS_FAIL_ALLOC holds a number n >= 1,
@@ -56,7 +58,7 @@ int cuda_fail(cudaError_t e, const char* what, int line) {
 // value fails as if the device were out of memory (no cudaMalloc is called
 // for it); the count restarts whenever the variable's string changes (so
 // "1" and then "01" each fail the next allocation) or is unset.
-cudaError_t device_malloc(void** p, size_t bytes) {
+cudaError_t ifvs::device_malloc(void** p, size_t bytes) {
     static std::mutex mu;
     static std::string last;
     static long count = 0;
@@ -78,6 +80,8 @@ cudaError_t device_malloc(void** p, size_t bytes) {
     }
     return cudaMalloc(p, bytes);
 }
+
+namespace {
 
 // Timeout injection for tests of the scan's bounded waits (no GPU fault
 // involved): while the environment variable IFVS_TEST_STALL_COPIES is "1",
@@ -116,19 +120,6 @@ void release(DevBuf& b) {
     b.p = nullptr;
     b.cap = 0;
 }
-
-struct DeviceGuard {
-    int prev = -1;
-    bool ok = true;
-    explicit DeviceGuard(int dev) {
-        if (cudaGetDevice(&prev) != cudaSuccess) prev = -1;
-        if (prev != dev) ok = cudaSetDevice(dev) == cudaSuccess;
-    }
-    ~DeviceGuard() {
-        int cur = -1;
-        if (prev >= 0 && cudaGetDevice(&cur) == cudaSuccess && cur != prev) cudaSetDevice(prev);
-    }
-};
 
 int64_t round_up(int64_t a, int64_t b) { return (a + b - 1) / b * b; }
 

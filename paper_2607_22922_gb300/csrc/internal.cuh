@@ -498,5 +498,21 @@ struct IndexView {
 int index_view(const ifvs_index* ix, IndexView* out);
 // Sets the thread-local message of ifvs_last_error and returns `code`.
 int report_error(int code, const char* fmt, ...);
+// Every device allocation of the library (api.cu: injected failures)
+cudaError_t device_malloc(void** p, size_t bytes);
+
+// Makes a device current for its lifetime
+struct DeviceGuard {
+    int prev = -1;
+    bool ok = true;
+    explicit DeviceGuard(int dev) {
+        if (cudaGetDevice(&prev) != cudaSuccess) prev = -1;
+        if (prev != dev) ok = cudaSetDevice(dev) == cudaSuccess;
+    }
+    ~DeviceGuard() {
+        int cur = -1;
+        if (prev >= 0 && cudaGetDevice(&cur) == cudaSuccess && cur != prev) cudaSetDevice(prev);
+    }
+};
 
 }  // namespace ifvs

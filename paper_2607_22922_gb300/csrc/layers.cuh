@@ -1,0 +1,115 @@
+// Layers of a predicate encoder: what their kernels share.
+#pragma once
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include "internal.cuh"
+
+namespace ifvs {
+
+// Bits of the handle's error word
+constexpr int kErrId = 1;        // a token id outside -1..V-1
+constexpr int kErrOffsets = 2;   // offsets that break their rules
+constexpr int kErrWait = 4;      // a bounded wait ran out
+
+inline size_t elem_bytes(int type) { return type == IFVS_T_F32 ? 4 : 2; }
+
+// ---- element types --------------------------------------------------------
+__device__ __forceinline__ float to_f32(float v) { return v; }
+__device__ __forceinline__ float to_f32(__half v) { return __half2float(v); }
+__device__ __forceinline__ float to_f32(__nv_bfloat16 v) { return __bfloat162float(v); }
+template <class T>
+__device__ __forceinline__ T from_f32(float v);
+template <>
+__device__ __forceinline__ float from_f32<float>(float v) { return v; }
+template <>
+__device__ __forceinline__ __half from_f32<__half>(float v) { return __float2half_rn(v); }
+template <>
+__device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
+
+__device__ __forceinline__ float warp_sum(float v) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
+    return v;
+}
+
+// Calls f with a value of the element type that `type` names
+template <class Fn>
+inline cudaError_t with_type(int type, const Fn& f) {
+    if (type == IFVS_T_F32) return f(float());
+    if (type == IFVS_T_F16) return f(__half());
+    return f(__nv_bfloat16());
+}
+
+// ---- launchers --------------------------------------------------------------
+struct EmbedArgs {
+    const int32_t* ids;
+    int64_t T, V;
+    int D, type;
+    float scale;
+    int* err;
+    int num_sms;
+};
+cudaError_t launch_embed(const EmbedArgs& a, const void* table, void* out, cudaStream_t s);
+size_t embed_grad_bytes(const EmbedArgs& a);
+cudaError_t launch_embed_grad(const EmbedArgs& a, const void* d_out, void* d_table, uint8_t* work, cudaStream_t s);
+
+struct JoinArgs {
+    int64_t T, B;
+    int D, type;
+    const int64_t* offsets;      // null: B = 1
+    const void *gate, *w_post, *w_pre;
+    float rho, eps;
+    int* err;
+    int num_sms;
+};
+cudaError_t launch_norm_join(const JoinArgs& a, const void* x, const void* y, void* x_out, void* n_out,
+                             cudaStream_t s);
+struct JoinGrads {
+    const void *x_out, *y, *d_x_out, *d_n;
+    void *dx, *dy, *d_gate, *d_w_post, *d_w_pre;
+};
+size_t norm_join_grad_bytes(const JoinArgs& a);
+cudaError_t launch_norm_join_grad(const JoinArgs& a, const JoinGrads& g, uint8_t* work, cudaStream_t s);
+
+struct FfnArgs {
+    int64_t T;
+    int D, F, type, act;
+    const void *w_in, *w_out;
+    int* err;
+    int num_sms;
+};
+size_t ffn_bytes(const FfnArgs& a);
+cudaError_t launch_ffn(const FfnArgs& a, const void* x, void* y, uint8_t* work, cudaStream_t s);
+size_t ffn_grad_bytes(const FfnArgs& a);
+cudaError_t launch_ffn_grad(const FfnArgs& a, const void* x, const void* dy, void* dx, void* d_w_in, void* d_w_out,
+                            uint8_t* work, cudaStream_t s);
+
+// Reports offsets that break their rules; the whole grid (x) calls it.
+__device__ __forceinline__ void check_offsets(const int64_t* __restrict__ offsets, int64_t B, int64_t T, int* err) {
+    if (offsets == nullptr) return;
+    bool bad = false;
+    for (int64_t b = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; b < B; b += (int64_t)gridDim.x * blockDim.x) {
+        const int64_t lo = __ldg(offsets + b), hi = __ldg(offsets + b + 1);
+        bad |= hi < lo || (b == 0 && lo != 0) || (b == B - 1 && hi != T);
+    }
+    if (bad) *err = kErrOffsets;
+}
+
+// the sequence of token t: the last b with offsets[b] <= t, within 0..B-1
+// whatever the offsets hold
+__device__ __forceinline__ int64_t sequence_of(const int64_t* __restrict__ offsets, int64_t B, int64_t t) {
+    if (offsets == nullptr || B == 1) return 0;
+    int64_t lo = 0, hi = B;      // offsets[lo] <= t (assumed of 0), hi: beyond
+    while (hi - lo > 1) {
+        const int64_t m = (lo + hi) >> 1;
+        if (__ldg(offsets + m) <= t)
+            lo = m;
+        else
+            hi = m;
+    }
+    return lo;
+}
+
+}  // namespace ifvs

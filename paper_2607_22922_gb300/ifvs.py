@@ -22,6 +22,8 @@ IFVS_OP_EQ, IFVS_OP_RANGE, IFVS_OP_GE, IFVS_OP_LT, IFVS_OP_GT, IFVS_OP_LE = 0, 1
 IFVS_ATTR_I32, IFVS_ATTR_I16 = 0, 1
 IFVS_F_DEVICE_IO, IFVS_F_STAGE_TIMING, IFVS_F_PLAIN_PQ, IFVS_F_PLAIN_LOADS = 0x1, 0x2, 0x4, 0x8
 IFVS_MAX_K, IFVS_MAX_M, IFVS_MAX_ATTRS, IFVS_N_STAGES = 256, 128, 4, 9
+IFVS_T_F32, IFVS_T_F16, IFVS_T_BF16 = 0, 1, 2
+IFVS_ACT_SILU, IFVS_ACT_GELU, IFVS_ACT_RELU = 0, 1, 2
 STAGES = ("predicate", "filter", "condition", "lut", "scan", "merge", "rerank", "layout", "train")
 
 # ifvs_predicate: 104 bytes (n_clauses, reserved, 4 x {col, op, lo, hi})
@@ -41,6 +43,19 @@ class SearchParams(C.Structure):
                 ("stream", C.c_void_p)]
 
 
+class JoinParams(C.Structure):
+    _fields_ = [("T", C.c_int64), ("D", C.c_int32), ("type", C.c_int32), ("n_seq", C.c_int64),
+                ("offsets", C.c_void_p), ("gate", C.c_void_p), ("w_post", C.c_void_p),
+                ("w_pre", C.c_void_p), ("res_scale", C.c_float), ("eps", C.c_float),
+                ("stream", C.c_void_p)]
+
+
+class FfnParams(C.Structure):
+    _fields_ = [("T", C.c_int64), ("D", C.c_int32), ("F", C.c_int32), ("type", C.c_int32),
+                ("act", C.c_int32), ("w_in", C.c_void_p), ("w_out", C.c_void_p),
+                ("stream", C.c_void_p)]
+
+
 class TrainParams(C.Structure):
     _fields_ = [("tau", C.c_float), ("lam", C.c_float), ("lr", C.c_float), ("lr_wz", C.c_float),
                 ("n_pos", C.c_int32), ("n_neg", C.c_int32), ("flags", C.c_uint32),
@@ -52,7 +67,7 @@ def _load():
         raise ImportError("libifvs.so is not built (%s); run `python -c \"import __graft_entry__ "
                           "as g; g.build()\"` or `python -m paper_2607_22922_gb300.build`" % LIB_PATH)
     L = C.CDLL(LIB_PATH)
-    P, I32, I64, U32 = C.c_void_p, C.c_int32, C.c_int64, C.c_uint32
+    P, I32, I64, U32, F32 = C.c_void_p, C.c_int32, C.c_int64, C.c_uint32, C.c_float
     sig = {
         "ifvs_load_index": (C.c_int, [P, I32, P, I64, I32, I32, P, P, I32, P, I32, U32]),
         "ifvs_load_codebooks": (C.c_int, [P, P, I32, P, I64, I32, I32, P, P]),
@@ -68,6 +83,15 @@ def _load():
         "ifvs_train_grad": (C.c_int, [P, P, P, I64, P, P, P, P, P, P, P]),
         "ifvs_train_step": (C.c_int, [P, P, P, I64, P, P, P, P, P]),
         "ifvs_get_conditioning": (C.c_int, [P, P, P, U32]),
+        "ifvs_layers_create": (C.c_int, [P, I32]),
+        "ifvs_layers_free": (None, [P]),
+        "ifvs_layers_status": (C.c_int, [P]),
+        "ifvs_embed": (C.c_int, [P, P, I64, I32, I32, P, I64, F32, P, P]),
+        "ifvs_embed_grad": (C.c_int, [P, P, P, I64, I64, I32, I32, F32, P, P]),
+        "ifvs_norm_join": (C.c_int, [P, P, P, P, P, P]),
+        "ifvs_norm_join_grad": (C.c_int, [P] * 11),
+        "ifvs_ffn": (C.c_int, [P, P, P, P]),
+        "ifvs_ffn_grad": (C.c_int, [P] * 7),
         "ifvs_stage_times": (C.c_int, [P, P, P, I32]),
         "ifvs_canonical_predicate": (C.c_int, [P, P, I32, P, P, P]),
         "ifvs_index_info": (C.c_int, [P, P]),
@@ -380,6 +404,186 @@ def ifvs_get_conditioning(ix, B, Mr, W_shape):
     return bank, W
 
 
+# ---- layers of a predicate encoder: CUDA tensors only ----------------------
+
+_ACTS = {"silu": IFVS_ACT_SILU, "gelu": IFVS_ACT_GELU, "relu": IFVS_ACT_RELU}
+_TYPES = {}         # torch's element types -> IFVS_T_*, filled on first use
+_LEGACY_STREAM = 1  # cudaStreamLegacy: the default stream as a non-NULL handle
+
+
+def _type(a):
+    t = _TYPES.get(a.dtype)
+    if t is None:
+        name = str(a.dtype).replace("torch.", "")
+        if name not in ("float32", "float16", "bfloat16"):
+            raise TypeError("tensors must be float32, float16 or bfloat16, got %s" % name)
+        t = _TYPES[a.dtype] = {"float32": IFVS_T_F32, "float16": IFVS_T_F16,
+                               "bfloat16": IFVS_T_BF16}[name]
+    return t
+
+
+def _dev(a, shape, dtype, name):
+    """Address of a contiguous CUDA tensor of this shape and type (None -> NULL)."""
+    if a is None:
+        return None
+    if a.shape != shape or a.dtype != dtype:
+        raise ValueError("%s is %s %s, expected %s %s" % (name, tuple(a.shape), a.dtype, shape, dtype))
+    if not a.is_cuda or not a.is_contiguous():
+        raise ValueError("%s must be a contiguous CUDA tensor" % name)
+    return a.data_ptr() or 256      # a tensor without elements has no address; none is read
+
+
+def _stream(stream):
+    """A raw handle, a torch stream (its default stream is the legacy one) or
+    None (the handle's own stream; the call waits)."""
+    if stream is None or isinstance(stream, int):
+        return stream
+    return stream.cuda_stream or _LEGACY_STREAM
+
+
+def _like(a, *shape):
+    return a.new_empty(shape)
+
+
+def ifvs_layers_create(device=0):
+    h = C.c_void_p()
+    _check(_lib.ifvs_layers_create(C.byref(h), device))
+    return h
+
+
+def ifvs_layers_free(L):
+    _lib.ifvs_layers_free(L)
+
+
+def ifvs_layers_status(L):
+    _check(_lib.ifvs_layers_status(L))
+
+
+def _ids(ids):
+    if str(ids.dtype) != "torch.int32" or ids.dim() != 1:
+        raise ValueError("ids must be a vector of int32")
+    return int(ids.shape[0])
+
+
+def ifvs_embed(L, table, ids, scale=1.0, out=None, stream=None):
+    """out [T][D] = scale table[ids]; id -1 gives a row of zeros."""
+    (V, D), T = table.shape, _ids(ids)
+    out = _like(table, T, D) if out is None else out
+    dt = table.dtype
+    _check(_lib.ifvs_embed(L, _dev(table, (V, D), dt, "table"), V, D, _type(table),
+                           _dev(ids, (T,), ids.dtype, "ids"), T, scale, _dev(out, (T, D), dt, "out"),
+                           _stream(stream)))
+    return out
+
+
+def ifvs_embed_grad(L, d_out, ids, scale=1.0, V=None, d_table=None, stream=None):
+    """d_table [V][D]: per id, scale times the sum of its tokens' rows of d_out
+    (zeros for ids without tokens).  Give V or d_table."""
+    (T, D), dt = d_out.shape, d_out.dtype
+    d_table = _like(d_out, V, D) if d_table is None else d_table
+    V = int(d_table.shape[0])
+    _check(_lib.ifvs_embed_grad(L, _dev(d_out, (T, D), dt, "d_out"), _dev(ids, (_ids(ids),), ids.dtype, "ids"),
+                                _same_length(ids, T), V, D, _type(d_out), scale,
+                                _dev(d_table, (V, D), dt, "d_table"), _stream(stream)))
+    return d_table
+
+
+def _same_length(ids, T):
+    if ids.shape[0] != T:
+        raise ValueError("%d ids for %d tokens" % (ids.shape[0], T))
+    return int(T)
+
+
+def _join_params(x, gate, w_post, w_pre, offsets, res_scale, eps, stream):
+    (T, D), dt = x.shape, x.dtype
+    p = JoinParams()
+    p.T, p.D, p.type = T, D, _type(x)
+    B = 1
+    if offsets is not None:
+        if str(offsets.dtype) != "torch.int64" or offsets.dim() != 1 or offsets.shape[0] < 2:
+            raise ValueError("offsets must be a vector of B + 1 int64")
+        B = int(offsets.shape[0]) - 1
+        p.offsets = _dev(offsets, (B + 1,), offsets.dtype, "offsets")
+    p.n_seq = B
+    p.gate = _dev(gate, (B, D), dt, "gate")
+    p.w_post = _dev(w_post, (D,), dt, "w_post")
+    p.w_pre = _dev(w_pre, (D,), dt, "w_pre")
+    p.res_scale, p.eps = res_scale, eps
+    p.stream = _stream(stream)
+    return p, (T, D), (B, D), dt
+
+
+def ifvs_norm_join(L, x, y=None, gate=None, w_post=None, w_pre=None, offsets=None, res_scale=1.0,
+                   eps=1e-5, x_out=None, n_out=None, stream=None):
+    """x_out = res_scale x + gate * w_post * y / rms(y) and, with w_pre,
+    n_out = w_pre * x_out / rms(x_out); gate [B][D] by the sequences that
+    ``offsets`` delimits.  Without y only n_out, of x.  Returns (x_out, n_out)."""
+    p, td, _, dt = _join_params(x, gate, w_post, w_pre, offsets, res_scale, eps, stream)
+    if y is not None and x_out is None:
+        x_out = _like(x, *td)
+    if w_pre is not None and n_out is None:
+        n_out = _like(x, *td)
+    _check(_lib.ifvs_norm_join(L, C.byref(p), _dev(x, td, dt, "x"), _dev(y, td, dt, "y"),
+                               _dev(x_out, td, dt, "x_out"), _dev(n_out, td, dt, "n_out")))
+    return x_out, n_out
+
+
+def ifvs_norm_join_grad(L, x_out, y=None, gate=None, w_post=None, w_pre=None, d_x_out=None, d_n=None,
+                        offsets=None, res_scale=1.0, eps=1e-5, dx=None, dy=None, d_gate=None,
+                        d_w_post=None, d_w_pre=None, stream=None):
+    """Gradients through ifvs_norm_join from those of x_out and n_out (either
+    may be None).  Returns (dx, dy, d_gate, d_w_post, d_w_pre), None where the
+    forward call had no such input."""
+    p, td, bd, dt = _join_params(x_out, gate, w_post, w_pre, offsets, res_scale, eps, stream)
+    dx = _like(x_out, *td) if dx is None else dx
+    if y is not None:
+        dy = _like(x_out, *td) if dy is None else dy
+        d_w_post = _like(x_out, td[1]) if d_w_post is None else d_w_post
+        if gate is not None and d_gate is None:
+            d_gate = _like(x_out, *bd)
+    if d_n is not None and d_w_pre is None:
+        d_w_pre = _like(x_out, td[1])
+    d = td[1:]
+    _check(_lib.ifvs_norm_join_grad(
+        L, C.byref(p), _dev(x_out, td, dt, "x_out"), _dev(y, td, dt, "y"),
+        _dev(d_x_out, td, dt, "d_x_out"), _dev(d_n, td, dt, "d_n"), _dev(dx, td, dt, "dx"),
+        _dev(dy, td, dt, "dy"), _dev(d_gate, bd, dt, "d_gate"), _dev(d_w_post, d, dt, "d_w_post"),
+        _dev(d_w_pre, d, dt, "d_w_pre")))
+    return dx, dy, d_gate, d_w_post, d_w_pre
+
+
+def _ffn_params(x, w_in, w_out, act, stream):
+    (T, D), F, dt = x.shape, int(w_out.shape[1]), x.dtype
+    if act not in _ACTS:
+        raise ValueError("act must be one of %s" % sorted(_ACTS))
+    p = FfnParams()
+    p.T, p.D, p.F, p.type, p.act = T, D, F, _type(x), _ACTS[act]
+    p.w_in = _dev(w_in, (2 * F, D), dt, "w_in")
+    p.w_out = _dev(w_out, (D, F), dt, "w_out")
+    p.stream = _stream(stream)
+    return p, (T, D), F, dt
+
+
+def ifvs_ffn(L, x, w_in, w_out, act="silu", y=None, stream=None):
+    """y = (act(x Wg^T) * (x Wu^T)) w_out^T, w_in [2F][D] = [Wg; Wu], w_out [D][F]."""
+    p, td, _, dt = _ffn_params(x, w_in, w_out, act, stream)
+    y = _like(x, *td) if y is None else y
+    _check(_lib.ifvs_ffn(L, C.byref(p), _dev(x, td, dt, "x"), _dev(y, td, dt, "y")))
+    return y
+
+
+def ifvs_ffn_grad(L, x, w_in, w_out, dy, act="silu", dx=None, d_w_in=None, d_w_out=None, stream=None):
+    """Gradients (dx, d_w_in, d_w_out) through ifvs_ffn from dy."""
+    p, td, F, dt = _ffn_params(x, w_in, w_out, act, stream)
+    dx = _like(x, *td) if dx is None else dx
+    d_w_in = _like(x, 2 * F, td[1]) if d_w_in is None else d_w_in
+    d_w_out = _like(x, td[1], F) if d_w_out is None else d_w_out
+    _check(_lib.ifvs_ffn_grad(L, C.byref(p), _dev(x, td, dt, "x"), _dev(dy, td, dt, "dy"),
+                              _dev(dx, td, dt, "dx"), _dev(d_w_in, (2 * F, td[1]), dt, "d_w_in"),
+                              _dev(d_w_out, (td[1], F), dt, "d_w_out")))
+    return dx, d_w_in, d_w_out
+
+
 def ifvs_rerank(ix, queries, cand, k, flags=0):
     queries = _host(queries, np.float32)
     cand = _host(cand, np.int64)
@@ -484,6 +688,47 @@ class Index:
     def close(self):
         if getattr(self, "h", None):
             ifvs_free(self.h)
+            self.h = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+class Layers:
+    """Owns an ifvs_layers handle: the layers of a predicate encoder on one
+    device (freed on close / garbage collection)."""
+
+    def __init__(self, device=0):
+        self.h = ifvs_layers_create(device)
+
+    def embed(self, table, ids, scale=1.0, **kw):
+        return ifvs_embed(self.h, table, ids, scale, **kw)
+
+    def embed_grad(self, d_out, ids, scale=1.0, **kw):
+        return ifvs_embed_grad(self.h, d_out, ids, scale, **kw)
+
+    def norm_join(self, x, y=None, gate=None, w_post=None, w_pre=None, **kw):
+        return ifvs_norm_join(self.h, x, y, gate, w_post, w_pre, **kw)
+
+    def norm_join_grad(self, x_out, y=None, gate=None, w_post=None, w_pre=None, d_x_out=None, d_n=None, **kw):
+        return ifvs_norm_join_grad(self.h, x_out, y, gate, w_post, w_pre, d_x_out, d_n, **kw)
+
+    def ffn(self, x, w_in, w_out, **kw):
+        return ifvs_ffn(self.h, x, w_in, w_out, **kw)
+
+    def ffn_grad(self, x, w_in, w_out, dy, **kw):
+        return ifvs_ffn_grad(self.h, x, w_in, w_out, dy, **kw)
+
+    def status(self):
+        """Waits for the enqueued calls; raises what their kernels found."""
+        ifvs_layers_status(self.h)
+
+    def close(self):
+        if getattr(self, "h", None):
+            ifvs_layers_free(self.h)
             self.h = None
 
     def __del__(self):
