@@ -1,35 +1,525 @@
 // Embedding lookup with scaling and its gradient (ifvs_embed, ifvs_embed_grad).
+//
+// Lookup: out[t] = scale table[ids[t]], a copy of rows: bound by memory.
+//
+// Gradient: d_table[v] = scale (sum of d_out[t] over the tokens with id v).  The
+// tokens are sorted by id (stable, so a row's sum runs over its tokens in
+// order), and the sorted order is cut into parts of equal length, whatever ids
+// they hold: a few ids have most of the tokens.  A warp adds the rows of its
+// part for a slice of the columns, run by run: a run inside the part goes to its
+// row, the two that may reach beyond it are left as float32 partial sums, which
+// k_embed_join adds in the order of the parts.  Rows that no token names are
+// found by a search in the sorted ids and set to zero.  Every row is written
+// once, no order depends on timing.
 #include "layers.cuh"
 
 namespace ifvs {
 
 namespace {
 
-// out[t] = scale table[ids[t]]: a CTA per token
-template <class T>
-__global__ void k_embed(const T* __restrict__ table, EmbedArgs a, T* __restrict__ out) {
-    const int64_t t = blockIdx.x;
-    const int id = a.ids[t];
-    const bool ok = id >= 0 && id < a.V;
-    if (!ok && id != -1 && threadIdx.x == 0) *a.err = kErrId;
-    for (int d = threadIdx.x; d < a.D; d += blockDim.x)
-        out[t * a.D + d] = from_f32<T>(ok ? a.scale * to_f32(table[(int64_t)id * a.D + d]) : 0.f);
+// N consecutive elements as floats, in one access
+template <class T, int N>
+struct Pack {
+    static constexpr int kBytes = N * (int)sizeof(T);
+    using Word = std::conditional_t<kBytes == 16, uint4, std::conditional_t<kBytes == 4, uint32_t, uint16_t>>;
+    Word w;
+    __device__ __forceinline__ void load(const T* p) { w = __ldg(reinterpret_cast<const Word*>(p)); }
+    __device__ __forceinline__ void store(T* p) const { *reinterpret_cast<Word*>(p) = w; }
+    __device__ __forceinline__ float get(int i) const { return to_f32(reinterpret_cast<const T*>(&w)[i]); }
+    __device__ __forceinline__ void set(int i, float v) { reinterpret_cast<T*>(&w)[i] = from_f32<T>(v); }
+};
+
+inline bool vectors(const EmbedArgs& a, const void* p, const void* q) {
+    return a.D * elem_bytes(a.type) % 16 == 0 && ((uintptr_t)p | (uintptr_t)q) % 16 == 0;
 }
 
-// d_table[v]: a CTA per row of the table looks through all ids
-template <class T>
-__global__ void k_embed_grad(const T* __restrict__ d_out, EmbedArgs a, T* __restrict__ d_table) {
-    const int64_t v = blockIdx.x;
-    for (int d0 = 0; d0 < a.D; d0 += blockDim.x) {
-        const int d = d0 + threadIdx.x;
-        float sum = 0.f;
-        for (int64_t t = 0; t < a.T; ++t) {
-            const int id = __ldg(a.ids + t);
-            if (v == 0 && d == 0 && (id < -1 || id >= a.V)) *a.err = kErrId;
-            if (id == v && d < a.D) sum += to_f32(d_out[t * a.D + d]);
-        }
-        if (d < a.D) d_table[v * a.D + d] = from_f32<T>(a.scale * sum);
+// out[t] = scale table[ids[t]].  A thread copies kEmbedRows pieces of a row.
+constexpr int kEmbedPieces = 4;
+
+template <class T, int N>
+__global__ void __launch_bounds__(256)
+k_embed(const T* __restrict__ table, EmbedArgs a, T* __restrict__ out) {
+    const int per_row = a.D / N;
+    const int64_t n = a.T * per_row;
+    const int64_t first = (int64_t)blockIdx.x * (256 * kEmbedPieces) + threadIdx.x;
+    Pack<T, N> v[kEmbedPieces];
+    bool some[kEmbedPieces];
+#pragma unroll
+    for (int i = 0; i < kEmbedPieces; ++i) {
+        const int64_t at = first + i * 256;
+        some[i] = false;
+        if (at >= n) continue;
+        const int64_t t = n <= 0x7FFFFFFF ? (int64_t)((uint32_t)at / (uint32_t)per_row) : at / per_row;
+        const int col = (int)(at - t * per_row);
+        const int id = __ldg(a.ids + t);
+        some[i] = id >= 0 && id < a.V;
+        if (!some[i] && id != -1 && col == 0) *a.err = kErrId;
+        if (some[i]) v[i].load(table + (int64_t)id * a.D + col * N);
     }
+#pragma unroll
+    for (int i = 0; i < kEmbedPieces; ++i) {
+        const int64_t at = first + i * 256;
+        if (at >= n) continue;
+#pragma unroll
+        for (int j = 0; j < N; ++j) v[i].set(j, some[i] ? a.scale * v[i].get(j) : 0.f);
+        v[i].store(out + at * N);
+    }
+}
+
+// ---- sort by id ------------------------------------------------------------------
+// Least significant digit first, digits of equal width of at most 8 bits; the
+// key of a token without a row is V.
+constexpr int kBins = 256;
+constexpr int kSortRounds = 8;                       // keys per lane
+
+struct SortPlan {
+    int passes, bits;
+    __host__ __device__ uint32_t digit(uint32_t key, int pass) const {
+        return (key >> (pass * bits)) & ((1u << bits) - 1u);
+    }
+};
+SortPlan sort_plan(int64_t V) {
+    int bits = 1;
+    while ((1ll << bits) <= V) ++bits;               // keys 0..V
+    const int passes = (bits + 7) / 8;
+    return {passes, (bits + passes - 1) / passes};
+}
+
+struct Pairs {
+    uint32_t *key, *pos;
+};
+
+__device__ __forceinline__ uint32_t key_of(const EmbedArgs& a, int64_t i) {
+    const int id = __ldg(a.ids + i);
+    if (id >= 0 && id < a.V) return (uint32_t)id;
+    if (id != -1) *a.err = kErrId;
+    return (uint32_t)a.V;
+}
+
+// The keys of a warp's kSortRounds x 32 places from `first` (absent beyond n),
+// with their rank among the warp's earlier keys of the same digit; counts in
+// hist [kBins].
+struct WarpKeys {
+    uint32_t key[kSortRounds], pos[kSortRounds];
+    uint16_t rank[kSortRounds];
+};
+__device__ __forceinline__ void load_keys(WarpKeys& k, const EmbedArgs& a, Pairs in, int64_t first, int lane) {
+#pragma unroll
+    for (int j = 0; j < kSortRounds; ++j) {
+        const int64_t i = first + j * 32 + lane;
+        k.key[j] = k.pos[j] = 0;
+        if (i >= a.T) continue;
+        if (in.key) {
+            // written by this kernel's cluster or an earlier kernel: not through the read-only path
+            k.key[j] = __ldcg(in.key + i);
+            k.pos[j] = __ldcg(in.pos + i);
+        } else {
+            k.key[j] = key_of(a, i);
+            k.pos[j] = (uint32_t)i;
+        }
+    }
+}
+__device__ __forceinline__ void rank_keys(WarpKeys& k, const SortPlan& plan, int pass, int64_t left, int lane,
+                                          uint32_t* hist) {
+#pragma unroll
+    for (int j = 0; j < kSortRounds; ++j) {
+        const bool in = j * 32 + lane < left;
+        const uint32_t d = in ? plan.digit(k.key[j], pass) : kBins;
+        const uint32_t same = __match_any_sync(0xFFFFFFFFu, d);
+        const uint32_t before = in ? hist[d] : 0u;
+        k.rank[j] = (uint16_t)(before + __popc(same & ((1u << lane) - 1u)));
+        __syncwarp();
+        if (in && (same >> lane) == 1u) hist[d] = before + __popc(same);    // the last of its digit
+        __syncwarp();
+    }
+}
+
+// exclusive sums of 256 values, by the first 256 threads of a block (all of it calls)
+__device__ __forceinline__ uint32_t scan256(uint32_t v, uint32_t* warp_sums) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    uint32_t s = v;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const uint32_t u = __shfl_up_sync(0xFFFFFFFFu, s, o);
+        if (lane >= o) s += u;
+    }
+    if (lane == 31 && warp < 8) warp_sums[warp] = s;
+    __syncthreads();
+    uint32_t base = 0;
+    for (int i = 0; i < min(warp, 8); ++i) base += warp_sums[i];
+    return base + s - v;
+}
+
+// Up to kClusterTokens tokens: one cluster sorts them in one launch.  Each of its
+// CTAs owns a segment; the digits' counts meet through distributed shared memory.
+constexpr int kClusterWarps = 32;
+constexpr int kClusterSegment = kClusterWarps * 32 * kSortRounds;    // 8192 tokens per CTA
+constexpr int kClusterMax = 8;
+constexpr int64_t kClusterTokens = (int64_t)kClusterSegment * kClusterMax;
+
+__device__ __forceinline__ uint32_t cluster_size() {
+    uint32_t v;
+    asm("mov.u32 %0, %%cluster_nctaid.x;" : "=r"(v));
+    return v;
+}
+__device__ __forceinline__ void cluster_sync() {
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ uint32_t load_of(const uint32_t* p, uint32_t cta) {
+    uint32_t at, v;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"((uint32_t)__cvta_generic_to_shared(p)), "r"(cta));
+    asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(at) : "memory");
+    return v;
+}
+
+__global__ void __launch_bounds__(kClusterWarps * 32, 1)
+k_sort_cluster(EmbedArgs a, SortPlan plan, Pairs p0, Pairs p1) {
+    __shared__ uint32_t hist[kClusterWarps][kBins];
+    __shared__ uint32_t total[kBins], base[kBins], warp_sums[8];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const uint32_t cta = blockIdx.x, ctas = cluster_size();
+    const int64_t first = (int64_t)cta * kClusterSegment + warp * (32 * kSortRounds);
+    start_dependents();
+    for (int pass = 0; pass < plan.passes; ++pass) {
+        const Pairs in = pass == 0 ? Pairs{nullptr, nullptr} : (pass & 1 ? p0 : p1);
+        const Pairs out = pass & 1 ? p1 : p0;
+        for (int i = lane; i < kBins; i += 32) hist[warp][i] = 0;
+        WarpKeys k;
+        load_keys(k, a, in, first, lane);
+        __syncwarp();
+        rank_keys(k, plan, pass, a.T - first, lane, hist[warp]);
+        __syncthreads();
+        const int d = threadIdx.x;
+        if (d < kBins) {
+            uint32_t sum = 0;
+            for (int w = 0; w < kClusterWarps; ++w) {
+                const uint32_t n = hist[w][d];
+                hist[w][d] = sum;
+                sum += n;
+            }
+            total[d] = sum;
+        }
+        cluster_sync();
+        uint32_t all = 0, before = 0;
+        if (d < kBins)
+            for (uint32_t c = 0; c < ctas; ++c) {
+                const uint32_t n = load_of(&total[d], c);
+                before += c < cta ? n : 0u;
+                all += n;
+            }
+        const uint32_t start = scan256(all, warp_sums);
+        if (d < kBins) base[d] = start + before;
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < kSortRounds; ++j)
+            if (first + j * 32 + lane < a.T) {
+                const uint32_t g = plan.digit(k.key[j], pass), at = base[g] + hist[warp][g] + k.rank[j];
+                out.key[at] = k.key[j];
+                out.pos[at] = k.pos[j];
+            }
+        cluster_sync();      // the pairs are written, and every CTA has read the totals
+    }
+}
+
+// More tokens: per pass the digits' counts of every tile of kTileTokens, their
+// sums over the tiles before, and the scatter.
+constexpr int kTileWarps = 8;
+constexpr int kTileTokens = kTileWarps * 32 * kSortRounds;   // 2048
+
+// counts [kBins][tiles]
+__global__ void __launch_bounds__(kTileWarps * 32)
+k_sort_count(EmbedArgs a, SortPlan plan, int pass, Pairs in, uint32_t* __restrict__ counts, int tiles) {
+    __shared__ uint32_t hist[kBins];
+    hist[threadIdx.x] = 0;
+    __syncthreads();
+    start_dependents();
+    if (pass > 0) wait_before();
+    const int64_t first = (int64_t)blockIdx.x * kTileTokens;
+#pragma unroll
+    for (int j = 0; j < kSortRounds; ++j) {
+        const int64_t i = first + j * (kTileWarps * 32) + threadIdx.x;
+        if (i < a.T) atomicAdd(&hist[plan.digit(in.key ? __ldcg(in.key + i) : key_of(a, i), pass)], 1u);
+    }
+    __syncthreads();
+    counts[(int64_t)threadIdx.x * tiles + blockIdx.x] = hist[threadIdx.x];
+}
+
+// a warp per digit: exclusive sums over the tiles, and the digit's total
+__global__ void __launch_bounds__(256) k_sort_scan(uint32_t* __restrict__ counts, int tiles, uint32_t* __restrict__ totals) {
+    start_dependents();
+    wait_before();
+    const int lane = threadIdx.x & 31, d = blockIdx.x * 8 + (threadIdx.x >> 5);
+    uint32_t* c = counts + (int64_t)d * tiles;
+    uint32_t sum = 0;
+    for (int i0 = 0; i0 < tiles; i0 += 32) {
+        const int i = i0 + lane;
+        const uint32_t v = i < tiles ? __ldcg(c + i) : 0u;
+        uint32_t s = v;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const uint32_t u = __shfl_up_sync(0xFFFFFFFFu, s, o);
+            if (lane >= o) s += u;
+        }
+        if (i < tiles) c[i] = sum + s - v;
+        sum += __shfl_sync(0xFFFFFFFFu, s, 31);
+    }
+    if (lane == 0) totals[d] = sum;
+}
+
+__global__ void __launch_bounds__(kTileWarps * 32)
+k_sort_scatter(EmbedArgs a, SortPlan plan, int pass, Pairs in, Pairs out, const uint32_t* __restrict__ counts,
+               int tiles, const uint32_t* __restrict__ totals) {
+    __shared__ uint32_t hist[kTileWarps][kBins], warp_sums[8], base[kBins];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, d = threadIdx.x;
+    start_dependents();
+    for (int i = lane; i < kBins; i += 32) hist[warp][i] = 0;
+    const int64_t first = (int64_t)blockIdx.x * kTileTokens + warp * (32 * kSortRounds);
+    wait_before();
+    WarpKeys k;
+    load_keys(k, a, in, first, lane);
+    __syncwarp();
+    rank_keys(k, plan, pass, a.T - first, lane, hist[warp]);
+    const uint32_t start = scan256(__ldcg(totals + d), warp_sums);
+    base[d] = start + __ldcg(counts + (int64_t)d * tiles + blockIdx.x);
+    __syncthreads();
+    uint32_t sum = base[d];
+    for (int w = 0; w < kTileWarps; ++w) {
+        const uint32_t n = hist[w][d];
+        hist[w][d] = sum;
+        sum += n;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < kSortRounds; ++j)
+        if (first + j * 32 + lane < a.T) {
+            const uint32_t at = hist[warp][plan.digit(k.key[j], pass)] + k.rank[j];
+            out.key[at] = k.key[j];
+            out.pos[at] = k.pos[j];
+        }
+}
+
+// ---- sums by id --------------------------------------------------------------------
+struct SumPlan {
+    int part;            // tokens per part (a multiple of 32)
+    int64_t parts;
+    int slices;          // of the columns
+    int64_t sum_warps;   // parts x slices
+    int64_t zero_warps;  // of 32 rows of the table
+};
+
+// this lane's columns of slice s: NV vectors of N
+template <class T, int N, int NV>
+__device__ __forceinline__ int column(int s, int i, int lane) {
+    return ((s * NV + i) * 32 + lane) * N;
+}
+
+// Partial sums [parts][2][D]: of the run that reaches into the part from before
+// (0) and of the one that begins in it and goes on (1).
+template <class T, int N, int NV>
+__global__ void __launch_bounds__(256)
+k_embed_sum(const T* __restrict__ d_out, EmbedArgs a, SumPlan p, Pairs sorted, float* __restrict__ partial,
+            T* __restrict__ d_table) {
+    constexpr int AHEAD = 8;
+    const int lane = threadIdx.x & 31;
+    const int64_t job = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
+    start_dependents();
+    wait_before();
+    if (job >= p.sum_warps) {
+        // rows without tokens: a lane looks for its row, the warp clears
+        const int64_t v = (job - p.sum_warps) * 32 + lane;
+        bool absent = false;
+        if (job - p.sum_warps < p.zero_warps && v < a.V) {
+            int64_t lo = 0, hi = a.T;                    // the first place with a key >= v
+            while (lo < hi) {
+                const int64_t m = (lo + hi) >> 1;
+                if (__ldcg(sorted.key + m) < (uint32_t)v)
+                    lo = m + 1;
+                else
+                    hi = m;
+            }
+            absent = lo == a.T || __ldcg(sorted.key + lo) != (uint32_t)v;
+        }
+        uint32_t rows = __ballot_sync(0xFFFFFFFFu, absent);
+        Pack<T, N> zero;
+#pragma unroll
+        for (int j = 0; j < N; ++j) zero.set(j, 0.f);
+        for (; rows; rows &= rows - 1u) {
+            T* row = d_table + (v - lane + __ffs(rows) - 1) * a.D;
+            for (int c = lane * N; c < a.D; c += 32 * N) zero.store(row + c);
+        }
+        return;
+    }
+    const int64_t part = job / p.slices;
+    const int slice = (int)(job - part * p.slices);
+    const int64_t begin = part * p.part, end = min(a.T, begin + p.part);
+    float sum[NV][N];
+    int64_t run = -1;                                    // the run's key
+    bool head = false;
+    auto clear = [&] {
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+            for (int j = 0; j < N; ++j) sum[i][j] = 0.f;
+    };
+    auto flush = [&](bool goes_on) {
+        if (run < 0 || run >= a.V) return;
+        if (head || goes_on) {
+            float* to = partial + (part * 2 + (head ? 0 : 1)) * a.D;
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                const int c = column<T, N, NV>(slice, i, lane);
+#pragma unroll
+                for (int j = 0; j < N; ++j)
+                    if (c + j < a.D) to[c + j] = sum[i][j];
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                const int c = column<T, N, NV>(slice, i, lane);
+                Pack<T, N> v;
+#pragma unroll
+                for (int j = 0; j < N; ++j) v.set(j, a.scale * sum[i][j]);
+                if (c < a.D) v.store(d_table + run * a.D + c);
+            }
+        }
+    };
+    clear();
+    const int64_t before = begin > 0 ? (int64_t)__ldcg(sorted.key + begin - 1) : -1;
+    for (int64_t b = begin; b < end; b += 32) {
+        const bool in = b + lane < end;
+        const uint32_t key = in ? __ldcg(sorted.key + b + lane) : 0xFFFFFFFFu;
+        const uint32_t pos = in ? __ldcg(sorted.pos + b + lane) : 0u;
+        const int n = (int)min((int64_t)32, end - b);
+        for (int i0 = 0; i0 < n; i0 += AHEAD) {
+            Pack<T, N> v[AHEAD][NV];
+            uint32_t k[AHEAD];
+#pragma unroll
+            for (int u = 0; u < AHEAD; ++u) {
+                k[u] = __shfl_sync(0xFFFFFFFFu, key, i0 + u);
+                const T* row = d_out + (int64_t)__shfl_sync(0xFFFFFFFFu, pos, i0 + u) * a.D;
+                if (i0 + u < n && k[u] < a.V)
+#pragma unroll
+                    for (int i = 0; i < NV; ++i) {
+                        const int c = column<T, N, NV>(slice, i, lane);
+                        if (c < a.D) v[u][i].load(row + c);
+                    }
+            }
+#pragma unroll
+            for (int u = 0; u < AHEAD; ++u) {
+                if (i0 + u >= n || k[u] >= a.V) continue;
+                if ((int64_t)k[u] != run) {
+                    flush(false);
+                    clear();
+                    run = k[u];
+                    head = b + i0 + u == begin && before == run;
+                }
+#pragma unroll
+                for (int i = 0; i < NV; ++i)
+#pragma unroll
+                    for (int j = 0; j < N; ++j)
+                        if (column<T, N, NV>(slice, i, lane) < a.D) sum[i][j] += v[u][i].get(j);
+            }
+        }
+    }
+    flush(end < a.T && (int64_t)__ldcg(sorted.key + end) == run);
+}
+
+// Runs over several parts: a CTA per part in which one begins adds its partial sums
+template <class T>
+__global__ void __launch_bounds__(256)
+k_embed_join(EmbedArgs a, SumPlan p, Pairs sorted, const float* __restrict__ partial, T* __restrict__ d_table) {
+    __shared__ float part_sum[8][32];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    wait_before();
+    const int64_t part = blockIdx.x, begin = part * p.part, end = begin + p.part;
+    const uint32_t run = __ldcg(sorted.key + end - 1);      // parts but the last are whole
+    if (run >= a.V || __ldcg(sorted.key + end) != run) return;
+    if (__ldcg(sorted.key + begin) == run && begin > 0 && __ldcg(sorted.key + begin - 1) == run) return;
+    int64_t lo = end, hi = a.T;                              // the first place with a key > run
+    while (lo < hi) {
+        const int64_t m = (lo + hi) >> 1;
+        if (__ldcg(sorted.key + m) <= run)
+            lo = m + 1;
+        else
+            hi = m;
+    }
+    const int64_t last = (lo - 1) / p.part;
+    for (int c0 = 0; c0 < a.D; c0 += 32) {
+        const int c = c0 + lane;
+        float sum = 0.f;
+        if (c < a.D) {
+            if (warp == 0) sum = __ldcg(partial + (part * 2 + 1) * a.D + c);
+#pragma unroll 4
+            for (int64_t q = part + 1 + warp; q <= last; q += 8) sum += __ldcg(partial + q * 2 * a.D + c);
+        }
+        part_sum[warp][lane] = sum;
+        __syncthreads();
+        if (warp == 0 && c < a.D) {
+            for (int w = 1; w < 8; ++w) sum += part_sum[w][lane];
+            d_table[(int64_t)run * a.D + c] = from_f32<T>(a.scale * sum);
+        }
+        __syncthreads();
+    }
+}
+
+// Parts long enough that their partial sums are few against the rows, short
+// enough that every SM has 16 warps of them
+template <class T, int N, int NV>
+SumPlan sum_plan(const EmbedArgs& a) {
+    SumPlan p;
+    p.slices = (a.D + 32 * N * NV - 1) / (32 * N * NV);
+    p.part = 32;
+    while (p.part < 256 && a.T / (2 * p.part) * p.slices >= 16 * a.num_sms) p.part *= 2;
+    p.parts = (a.T + p.part - 1) / p.part;
+    p.sum_warps = p.parts * p.slices;
+    p.zero_warps = (a.V + 31) / 32;
+    return p;
+}
+
+size_t padded(size_t n) { return (n + 255) / 256 * 256; }
+int64_t sort_tiles(const EmbedArgs& a) { return (a.T + kTileTokens - 1) / kTileTokens; }
+
+cudaError_t sort_by_id(const EmbedArgs& a, Pairs p0, Pairs p1, uint32_t* counts, cudaStream_t s, Pairs* sorted) {
+    const SortPlan plan = sort_plan(a.V);
+    *sorted = plan.passes & 1 ? p0 : p1;
+    if (a.T <= kClusterTokens) {
+        int ctas = 1;
+        while ((int64_t)ctas * kClusterSegment < a.T) ctas *= 2;
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3((unsigned)ctas);
+        cfg.blockDim = dim3(kClusterWarps * 32);
+        cfg.stream = s;
+        cudaLaunchAttribute attr[1];
+        attr[0].id = cudaLaunchAttributeClusterDimension;
+        attr[0].val.clusterDim = {(unsigned)ctas, 1u, 1u};
+        cfg.attrs = attr;
+        cfg.numAttrs = 1;
+        return cudaLaunchKernelEx(&cfg, k_sort_cluster, a, plan, p0, p1);
+    }
+    const int tiles = (int)sort_tiles(a);
+    uint32_t* totals = counts + (int64_t)kBins * tiles;
+    cudaError_t e = cudaSuccess;
+    auto then = [&](cudaError_t r) { e = e == cudaSuccess ? r : e; };
+    for (int pass = 0; pass < plan.passes; ++pass) {
+        const Pairs in = pass == 0 ? Pairs{nullptr, nullptr} : (pass & 1 ? p0 : p1);
+        const Pairs out = pass & 1 ? p1 : p0;
+        then(launch_kernel(k_sort_count, dim3(tiles), dim3(kTileWarps * 32), 0, pass > 0, s, a, plan, pass, in, counts, tiles));
+        then(launch_kernel(k_sort_scan, dim3(kBins / 8), dim3(256), 0, true, s, counts, tiles, totals));
+        then(launch_kernel(k_sort_scatter, dim3(tiles), dim3(kTileWarps * 32), 0, true, s, a, plan, pass, in, out,
+                           (const uint32_t*)counts, tiles, (const uint32_t*)totals));
+    }
+    return e;
+}
+
+template <class T, int N, int NV>
+cudaError_t sum_by_id(const EmbedArgs& a, const void* d_out, Pairs sorted, float* partial, void* d_table, cudaStream_t s) {
+    const SumPlan p = sum_plan<T, N, NV>(a);
+    cudaError_t e = launch_kernel(k_embed_sum<T, N, NV>, dim3((unsigned)((p.sum_warps + p.zero_warps + 7) / 8)), dim3(256), 0,
+                                  true, s, (const T*)d_out, a, p, sorted, partial, (T*)d_table);
+    if (e == cudaSuccess && p.parts > 1)
+        e = launch_kernel(k_embed_join<T>, dim3((unsigned)(p.parts - 1)), dim3(256), 0, true, s, a, p, sorted,
+                          (const float*)partial, (T*)d_table);
+    return e;
 }
 
 }  // namespace
@@ -37,18 +527,42 @@ __global__ void k_embed_grad(const T* __restrict__ d_out, EmbedArgs a, T* __rest
 cudaError_t launch_embed(const EmbedArgs& a, const void* table, void* out, cudaStream_t s) {
     return with_type(a.type, [&](auto z) {
         using T = decltype(z);
-        k_embed<T><<<(unsigned)a.T, 128, 0, s>>>((const T*)table, a, (T*)out);
+        constexpr int N = 16 / (int)sizeof(T);
+        const bool vec = vectors(a, table, out);
+        const int64_t n = a.T * (a.D / (vec ? N : 1));
+        const unsigned grid = (unsigned)((n + 256 * kEmbedPieces - 1) / (256 * kEmbedPieces));
+        if (vec)
+            k_embed<T, N><<<grid, 256, 0, s>>>((const T*)table, a, (T*)out);
+        else
+            k_embed<T, 1><<<grid, 256, 0, s>>>((const T*)table, a, (T*)out);
         return cudaGetLastError();
     });
 }
 
-size_t embed_grad_bytes(const EmbedArgs&) { return 0; }
+// two sets of pairs, the tiles' counts, the partial sums of the shortest parts
+size_t embed_grad_bytes(const EmbedArgs& a) {
+    return 4 * padded((size_t)a.T * 4) + padded((size_t)(sort_tiles(a) + 1) * kBins * 4) +
+           (size_t)((a.T + 31) / 32) * 2 * a.D * 4;
+}
 
-cudaError_t launch_embed_grad(const EmbedArgs& a, const void* d_out, void* d_table, uint8_t*, cudaStream_t s) {
+cudaError_t launch_embed_grad(const EmbedArgs& a, const void* d_out, void* d_table, uint8_t* work, cudaStream_t s) {
+    if (a.T == 0) return cudaMemsetAsync(d_table, 0, (size_t)a.V * a.D * elem_bytes(a.type), s);
+    auto take = [&](size_t bytes) {
+        uint8_t* p = work;
+        work += padded(bytes);
+        return (uint32_t*)p;
+    };
+    const size_t n = (size_t)a.T * 4;
+    const Pairs p0{take(n), take(n)}, p1{take(n), take(n)};
+    uint32_t* counts = take((size_t)(sort_tiles(a) + 1) * kBins * 4);
+    float* partial = (float*)work;
+    Pairs sorted;
+    const cudaError_t e = sort_by_id(a, p0, p1, counts, s, &sorted);
+    if (e != cudaSuccess) return e;
     return with_type(a.type, [&](auto z) {
         using T = decltype(z);
-        k_embed_grad<T><<<(unsigned)a.V, 128, 0, s>>>((const T*)d_out, a, (T*)d_table);
-        return cudaGetLastError();
+        if (vectors(a, d_out, d_table)) return sum_by_id<T, 16 / (int)sizeof(T), 1>(a, d_out, sorted, partial, d_table, s);
+        return sum_by_id<T, 1, 8>(a, d_out, sorted, partial, d_table, s);
     });
 }
 
