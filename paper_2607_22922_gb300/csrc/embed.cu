@@ -25,6 +25,8 @@ struct Pack {
     Word w;
     __device__ __forceinline__ void load(const T* p) { w = __ldg(reinterpret_cast<const Word*>(p)); }
     __device__ __forceinline__ void store(T* p) const { *reinterpret_cast<Word*>(p) = w; }
+    // not to be read again soon
+    __device__ __forceinline__ void store_stream(T* p) const { __stcs(reinterpret_cast<Word*>(p), w); }
     __device__ __forceinline__ float get(int i) const { return to_f32(reinterpret_cast<const T*>(&w)[i]); }
     __device__ __forceinline__ void set(int i, float v) { reinterpret_cast<T*>(&w)[i] = from_f32<T>(v); }
 };
@@ -62,7 +64,7 @@ k_embed(const T* __restrict__ table, EmbedArgs a, T* __restrict__ out) {
         if (at >= n) continue;
 #pragma unroll
         for (int j = 0; j < N; ++j) v[i].set(j, some[i] ? a.scale * v[i].get(j) : 0.f);
-        v[i].store(out + at * N);
+        v[i].store_stream(out + at * N);     // the table's rows stay in L2
     }
 }
 
@@ -98,17 +100,17 @@ __device__ __forceinline__ uint32_t key_of(const EmbedArgs& a, int64_t i) {
 
 // The keys of a warp's kSortRounds x 32 places from `first` (absent beyond n),
 // with their rank among the warp's earlier keys of the same digit; counts in
-// hist [kBins].
+// hist [kBins].  Lanes of equal digits find each other by a ballot per bit.
 struct WarpKeys {
     uint32_t key[kSortRounds], pos[kSortRounds];
     uint16_t rank[kSortRounds];
 };
-__device__ __forceinline__ void load_keys(WarpKeys& k, const EmbedArgs& a, Pairs in, int64_t first, int lane) {
+__device__ __forceinline__ void load_keys(WarpKeys& k, const EmbedArgs& a, Pairs in, int64_t first, int64_t left, int lane) {
 #pragma unroll
     for (int j = 0; j < kSortRounds; ++j) {
         const int64_t i = first + j * 32 + lane;
         k.key[j] = k.pos[j] = 0;
-        if (i >= a.T) continue;
+        if (j * 32 + lane >= left) continue;
         if (in.key) {
             // written by this kernel's cluster or an earlier kernel: not through the read-only path
             k.key[j] = __ldcg(in.key + i);
@@ -123,9 +125,15 @@ __device__ __forceinline__ void rank_keys(WarpKeys& k, const SortPlan& plan, int
                                           uint32_t* hist) {
 #pragma unroll
     for (int j = 0; j < kSortRounds; ++j) {
+        if (j * 32 >= left) break;
         const bool in = j * 32 + lane < left;
-        const uint32_t d = in ? plan.digit(k.key[j], pass) : kBins;
-        const uint32_t same = __match_any_sync(0xFFFFFFFFu, d);
+        const uint32_t d = plan.digit(k.key[j], pass);
+        uint32_t same = __ballot_sync(0xFFFFFFFFu, in);
+        for (int b = 0; b < plan.bits; ++b) {
+            const bool bit = d >> b & 1u;
+            const uint32_t set = __ballot_sync(0xFFFFFFFFu, bit);
+            same &= bit ? set : ~set;
+        }
         const uint32_t before = in ? hist[d] : 0u;
         k.rank[j] = (uint16_t)(before + __popc(same & ((1u << lane) - 1u)));
         __syncwarp();
@@ -152,10 +160,9 @@ __device__ __forceinline__ uint32_t scan256(uint32_t v, uint32_t* warp_sums) {
 
 // Up to kClusterTokens tokens: one cluster sorts them in one launch.  Each of its
 // CTAs owns a segment; the digits' counts meet through distributed shared memory.
-constexpr int kClusterWarps = 32;
-constexpr int kClusterSegment = kClusterWarps * 32 * kSortRounds;    // 8192 tokens per CTA
+constexpr int kClusterWarps = 16;
 constexpr int kClusterMax = 8;
-constexpr int64_t kClusterTokens = (int64_t)kClusterSegment * kClusterMax;
+constexpr int64_t kClusterTokens = (int64_t)kClusterMax * kClusterWarps * 32 * kSortRounds;    // 32768
 
 __device__ __forceinline__ uint32_t cluster_size() {
     uint32_t v;
@@ -173,21 +180,22 @@ __device__ __forceinline__ uint32_t load_of(const uint32_t* p, uint32_t cta) {
 }
 
 __global__ void __launch_bounds__(kClusterWarps * 32, 1)
-k_sort_cluster(EmbedArgs a, SortPlan plan, Pairs p0, Pairs p1) {
+k_sort_cluster(EmbedArgs a, SortPlan plan, Pairs p0, Pairs p1, int rounds) {
     __shared__ uint32_t hist[kClusterWarps][kBins];
     __shared__ uint32_t total[kBins], base[kBins], warp_sums[8];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const uint32_t cta = blockIdx.x, ctas = cluster_size();
-    const int64_t first = (int64_t)cta * kClusterSegment + warp * (32 * kSortRounds);
+    const int64_t first = ((int64_t)cta * kClusterWarps + warp) * 32 * rounds;
+    const int64_t left = min(a.T - first, (int64_t)32 * rounds);
     start_dependents();
     for (int pass = 0; pass < plan.passes; ++pass) {
         const Pairs in = pass == 0 ? Pairs{nullptr, nullptr} : (pass & 1 ? p0 : p1);
         const Pairs out = pass & 1 ? p1 : p0;
         for (int i = lane; i < kBins; i += 32) hist[warp][i] = 0;
         WarpKeys k;
-        load_keys(k, a, in, first, lane);
+        load_keys(k, a, in, first, left, lane);
         __syncwarp();
-        rank_keys(k, plan, pass, a.T - first, lane, hist[warp]);
+        rank_keys(k, plan, pass, left, lane, hist[warp]);
         __syncthreads();
         const int d = threadIdx.x;
         if (d < kBins) {
@@ -212,7 +220,7 @@ k_sort_cluster(EmbedArgs a, SortPlan plan, Pairs p0, Pairs p1) {
         __syncthreads();
 #pragma unroll
         for (int j = 0; j < kSortRounds; ++j)
-            if (first + j * 32 + lane < a.T) {
+            if (j * 32 + lane < left) {
                 const uint32_t g = plan.digit(k.key[j], pass), at = base[g] + hist[warp][g] + k.rank[j];
                 out.key[at] = k.key[j];
                 out.pos[at] = k.pos[j];
@@ -276,9 +284,10 @@ k_sort_scatter(EmbedArgs a, SortPlan plan, int pass, Pairs in, Pairs out, const 
     const int64_t first = (int64_t)blockIdx.x * kTileTokens + warp * (32 * kSortRounds);
     wait_before();
     WarpKeys k;
-    load_keys(k, a, in, first, lane);
+    const int64_t left = a.T - first;
+    load_keys(k, a, in, first, left, lane);
     __syncwarp();
-    rank_keys(k, plan, pass, a.T - first, lane, hist[warp]);
+    rank_keys(k, plan, pass, left, lane, hist[warp]);
     const uint32_t start = scan256(__ldcg(totals + d), warp_sums);
     base[d] = start + __ldcg(counts + (int64_t)d * tiles + blockIdx.x);
     __syncthreads();
@@ -291,7 +300,7 @@ k_sort_scatter(EmbedArgs a, SortPlan plan, int pass, Pairs in, Pairs out, const 
     __syncthreads();
 #pragma unroll
     for (int j = 0; j < kSortRounds; ++j)
-        if (first + j * 32 + lane < a.T) {
+        if (j * 32 + lane < left) {
             const uint32_t at = hist[warp][plan.digit(k.key[j], pass)] + k.rank[j];
             out.key[at] = k.key[j];
             out.pos[at] = k.pos[j];
@@ -316,10 +325,10 @@ __device__ __forceinline__ int column(int s, int i, int lane) {
 // Partial sums [parts][2][D]: of the run that reaches into the part from before
 // (0) and of the one that begins in it and goes on (1).
 template <class T, int N, int NV>
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(256, NV == 1 ? 4 : 2)
 k_embed_sum(const T* __restrict__ d_out, EmbedArgs a, SumPlan p, Pairs sorted, float* __restrict__ partial,
             T* __restrict__ d_table) {
-    constexpr int AHEAD = 8;
+    constexpr int AHEAD = NV == 1 ? 8 : 4;               // rows in flight
     const int lane = threadIdx.x & 31;
     const int64_t job = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
     start_dependents();
@@ -395,18 +404,16 @@ k_embed_sum(const T* __restrict__ d_out, EmbedArgs a, SumPlan p, Pairs sorted, f
             uint32_t k[AHEAD];
 #pragma unroll
             for (int u = 0; u < AHEAD; ++u) {
+                // without conditions, so that all loads are issued before the first
+                // is used: places beyond the part read row 0, columns beyond D the last
                 k[u] = __shfl_sync(0xFFFFFFFFu, key, i0 + u);
                 const T* row = d_out + (int64_t)__shfl_sync(0xFFFFFFFFu, pos, i0 + u) * a.D;
-                if (i0 + u < n && k[u] < a.V)
 #pragma unroll
-                    for (int i = 0; i < NV; ++i) {
-                        const int c = column<T, N, NV>(slice, i, lane);
-                        if (c < a.D) v[u][i].load(row + c);
-                    }
+                for (int i = 0; i < NV; ++i) v[u][i].load(row + min(column<T, N, NV>(slice, i, lane), a.D - N));
             }
 #pragma unroll
             for (int u = 0; u < AHEAD; ++u) {
-                if (i0 + u >= n || k[u] >= a.V) continue;
+                if (k[u] >= a.V) continue;           // no row, or beyond the part
                 if ((int64_t)k[u] != run) {
                     flush(false);
                     clear();
@@ -416,49 +423,53 @@ k_embed_sum(const T* __restrict__ d_out, EmbedArgs a, SumPlan p, Pairs sorted, f
 #pragma unroll
                 for (int i = 0; i < NV; ++i)
 #pragma unroll
-                    for (int j = 0; j < N; ++j)
-                        if (column<T, N, NV>(slice, i, lane) < a.D) sum[i][j] += v[u][i].get(j);
+                    for (int j = 0; j < N; ++j) sum[i][j] += v[u][i].get(j);
             }
         }
     }
     flush(end < a.T && (int64_t)__ldcg(sorted.key + end) == run);
 }
 
-// Runs over several parts: a CTA per part in which one begins adds its partial sums
+// Runs over several parts: a CTA per part in which one begins (and 128 columns)
+// adds its partial sums, a warp every eighth part
 template <class T>
 __global__ void __launch_bounds__(256)
 k_embed_join(EmbedArgs a, SumPlan p, Pairs sorted, const float* __restrict__ partial, T* __restrict__ d_table) {
-    __shared__ float part_sum[8][32];
+    __shared__ float part_sum[8][128];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     wait_before();
     const int64_t part = blockIdx.x, begin = part * p.part, end = begin + p.part;
-    const uint32_t run = __ldcg(sorted.key + end - 1);      // parts but the last are whole
-    if (run >= a.V || __ldcg(sorted.key + end) != run) return;
-    if (__ldcg(sorted.key + begin) == run && begin > 0 && __ldcg(sorted.key + begin - 1) == run) return;
-    int64_t lo = end, hi = a.T;                              // the first place with a key > run
-    while (lo < hi) {
-        const int64_t m = (lo + hi) >> 1;
-        if (__ldcg(sorted.key + m) <= run)
-            lo = m + 1;
-        else
-            hi = m;
+    const uint32_t run = __ldcg(sorted.key + end - 1), next = __ldcg(sorted.key + end);    // parts but the last are whole
+    const uint32_t first = __ldcg(sorted.key + begin), before = __ldcg(sorted.key + max(begin - 1, (int64_t)0));
+    if (run >= a.V || next != run || (begin > 0 && first == run && before == run)) return;
+    // the parts that follow and begin with the run
+    int64_t more = 1;
+    for (;;) {
+        const int64_t q = part + 1 + more + threadIdx.x;
+        const int n = __syncthreads_count(q < p.parts && __ldcg(sorted.key + q * p.part) == run);
+        more += n;
+        if (n < 256) break;
     }
-    const int64_t last = (lo - 1) / p.part;
-    for (int c0 = 0; c0 < a.D; c0 += 32) {
-        const int c = c0 + lane;
-        float sum = 0.f;
-        if (c < a.D) {
-            if (warp == 0) sum = __ldcg(partial + (part * 2 + 1) * a.D + c);
+    const int c0 = blockIdx.y * 128;
+    float sum[4] = {0.f, 0.f, 0.f, 0.f};
+    auto add = [&](const float* from) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int c = c0 + j * 32 + lane;
+            if (c < a.D) sum[j] += __ldcg(from + c);
+        }
+    };
+    if (warp == 0) add(partial + (part * 2 + 1) * a.D);
 #pragma unroll 4
-            for (int64_t q = part + 1 + warp; q <= last; q += 8) sum += __ldcg(partial + q * 2 * a.D + c);
-        }
-        part_sum[warp][lane] = sum;
-        __syncthreads();
-        if (warp == 0 && c < a.D) {
-            for (int w = 1; w < 8; ++w) sum += part_sum[w][lane];
-            d_table[(int64_t)run * a.D + c] = from_f32<T>(a.scale * sum);
-        }
-        __syncthreads();
+    for (int64_t q = part + 1 + warp; q <= part + more; q += 8) add(partial + q * 2 * a.D);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) part_sum[warp][j * 32 + lane] = sum[j];
+    __syncthreads();
+    const int c = c0 + threadIdx.x;
+    if (threadIdx.x < 128 && c < a.D) {
+        float total = 0.f;
+        for (int w = 0; w < 8; ++w) total += part_sum[w][threadIdx.x];
+        d_table[(int64_t)run * a.D + c] = from_f32<T>(a.scale * total);
     }
 }
 
@@ -483,8 +494,11 @@ cudaError_t sort_by_id(const EmbedArgs& a, Pairs p0, Pairs p1, uint32_t* counts,
     const SortPlan plan = sort_plan(a.V);
     *sorted = plan.passes & 1 ? p0 : p1;
     if (a.T <= kClusterTokens) {
+        // the work of a pass is in its ranks: spread over the cluster's SMs, two
+        // rounds a warp at least
         int ctas = 1;
-        while ((int64_t)ctas * kClusterSegment < a.T) ctas *= 2;
+        while (ctas < kClusterMax && (int64_t)ctas * kClusterWarps * 64 < a.T) ctas *= 2;
+        const int rounds = (int)((a.T + ctas * kClusterWarps * 32 - 1) / (ctas * kClusterWarps * 32));
         cudaLaunchConfig_t cfg = {};
         cfg.gridDim = dim3((unsigned)ctas);
         cfg.blockDim = dim3(kClusterWarps * 32);
@@ -494,7 +508,7 @@ cudaError_t sort_by_id(const EmbedArgs& a, Pairs p0, Pairs p1, uint32_t* counts,
         attr[0].val.clusterDim = {(unsigned)ctas, 1u, 1u};
         cfg.attrs = attr;
         cfg.numAttrs = 1;
-        return cudaLaunchKernelEx(&cfg, k_sort_cluster, a, plan, p0, p1);
+        return cudaLaunchKernelEx(&cfg, k_sort_cluster, a, plan, p0, p1, rounds);
     }
     const int tiles = (int)sort_tiles(a);
     uint32_t* totals = counts + (int64_t)kBins * tiles;
@@ -517,7 +531,8 @@ cudaError_t sum_by_id(const EmbedArgs& a, const void* d_out, Pairs sorted, float
     cudaError_t e = launch_kernel(k_embed_sum<T, N, NV>, dim3((unsigned)((p.sum_warps + p.zero_warps + 7) / 8)), dim3(256), 0,
                                   true, s, (const T*)d_out, a, p, sorted, partial, (T*)d_table);
     if (e == cudaSuccess && p.parts > 1)
-        e = launch_kernel(k_embed_join<T>, dim3((unsigned)(p.parts - 1)), dim3(256), 0, true, s, a, p, sorted,
+        e = launch_kernel(k_embed_join<T>, dim3((unsigned)(p.parts - 1), (unsigned)((a.D + 127) / 128)), dim3(256), 0, true, s,
+                          a, p, sorted,
                           (const float*)partial, (T*)d_table);
     return e;
 }
