@@ -17,20 +17,6 @@ namespace ifvs {
 
 namespace {
 
-// N consecutive elements as floats, in one access
-template <class T, int N>
-struct Pack {
-    static constexpr int kBytes = N * (int)sizeof(T);
-    using Word = std::conditional_t<kBytes == 16, uint4, std::conditional_t<kBytes == 4, uint32_t, uint16_t>>;
-    Word w;
-    __device__ __forceinline__ void load(const T* p) { w = __ldg(reinterpret_cast<const Word*>(p)); }
-    __device__ __forceinline__ void store(T* p) const { *reinterpret_cast<Word*>(p) = w; }
-    // not to be read again soon
-    __device__ __forceinline__ void store_stream(T* p) const { __stcs(reinterpret_cast<Word*>(p), w); }
-    __device__ __forceinline__ float get(int i) const { return to_f32(reinterpret_cast<const T*>(&w)[i]); }
-    __device__ __forceinline__ void set(int i, float v) { reinterpret_cast<T*>(&w)[i] = from_f32<T>(v); }
-};
-
 inline bool vectors(const EmbedArgs& a, const void* p, const void* q) {
     return a.D * elem_bytes(a.type) % 16 == 0 && ((uintptr_t)p | (uintptr_t)q) % 16 == 0;
 }

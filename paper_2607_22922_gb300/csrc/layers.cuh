@@ -4,6 +4,8 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
+#include <type_traits>
+
 #include "internal.cuh"
 
 namespace ifvs {
@@ -33,6 +35,20 @@ __device__ __forceinline__ float warp_sum(float v) {
     for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
     return v;
 }
+
+// N consecutive elements as floats, in one access
+template <class T, int N>
+struct Pack {
+    static constexpr int kBytes = N * (int)sizeof(T);
+    using Word = std::conditional_t<kBytes == 16, uint4, std::conditional_t<kBytes == 4, uint32_t, uint16_t>>;
+    Word w;
+    __device__ __forceinline__ void load(const T* p) { w = __ldg(reinterpret_cast<const Word*>(p)); }
+    __device__ __forceinline__ void store(T* p) const { *reinterpret_cast<Word*>(p) = w; }
+    // not to be read again soon
+    __device__ __forceinline__ void store_stream(T* p) const { __stcs(reinterpret_cast<Word*>(p), w); }
+    __device__ __forceinline__ float get(int i) const { return to_f32(reinterpret_cast<const T*>(&w)[i]); }
+    __device__ __forceinline__ void set(int i, float v) { reinterpret_cast<T*>(&w)[i] = from_f32<T>(v); }
+};
 
 // Calls f with a value of the element type that `type` names
 template <class Fn>
