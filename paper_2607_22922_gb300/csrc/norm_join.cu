@@ -10,14 +10,18 @@
 //   d_w_post = sum of gate_b g u, d_w_pre = sum of d_n x' i over all tokens
 //
 // Both are bound by memory: two rows read and two written per token, four and
-// two.  A team of 1 to 16 warps holds a token's rows in registers, so that each
-// is read once whatever the norms need of it.  A team takes tokens that follow
-// each other: the sequence of the first is searched, the others' follow, and
-// the gradient keeps its sums over tokens in registers.  A sequence inside a
-// team's tokens has its gate's gradient written at once; one that reaches
-// beyond them leaves float32 partial sums that k_join_finish adds in order, as
-// it does with the norms' weights.  No result depends on timing.
+// two.  A team of 1 to 16 warps takes a token's rows through a ring of kStages
+// places in shared memory, filled ahead by bulk copies, or by 4-byte
+// asynchronous copies where rows do not begin on 16 bytes: each row is read
+// once from memory, whatever the norms need of it, and a team's loads go on
+// while it reduces.  A team takes tokens that follow each other: the sequence of
+// the first is searched, the others' follow, and the gradient keeps its sums
+// over tokens in registers.  A sequence inside a team's tokens has its gate's
+// gradient written at once; one that reaches beyond them leaves float32 partial
+// sums that k_join_finish adds in order, as it does with the norms' weights.  No
+// result depends on timing.
 #include "layers.cuh"
+#include "scan_common.cuh"
 
 namespace ifvs {
 
@@ -29,6 +33,12 @@ struct Team {
     int warps, warp, id;        // warps of the team, this one's place, the team's number in the CTA
     float4* slots;              // [2][all warps of the CTA]
     int turn, all;
+    __device__ __forceinline__ void sync() const {
+        if (warps == 1)
+            __syncwarp();
+        else
+            asm volatile("barrier.cta.sync %0, %1;" ::"r"(1 + id), "r"(warps * 32) : "memory");
+    }
     __device__ __forceinline__ float4 sum(float4 v) {
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) {
@@ -40,7 +50,7 @@ struct Team {
         float4* s = slots + turn * all + id * warps;
         turn ^= 1;
         if ((threadIdx.x & 31) == 0) s[warp] = v;
-        asm volatile("barrier.cta.sync %0, %1;" ::"r"(1 + id), "r"(warps * 32) : "memory");
+        sync();
         v = s[0];
         for (int w = 1; w < warps; ++w) {
             v.x += s[w].x;
@@ -69,28 +79,138 @@ struct Sequence {
     __device__ __forceinline__ int64_t begin() const { return offsets ? __ldg(offsets + b) : 0; }
 };
 
-template <class T, int N, int NV>
-struct Row {
-    Pack<T, N> v[NV];
-    // p: the row; columns beyond D read as zeros
-    __device__ __forceinline__ void load(const T* p, int col, int step, int D) {
+constexpr int kStages = 3;               // places of a ring (1: no copies ahead)
+
+// A team's ring of rows: A arrays per place (absent ones are null).  Bulk copies
+// (one thread, completion on an mbarrier) where rows begin on 16 bytes;
+// otherwise 4-byte copies by all lanes, from the 4-byte word that holds the
+// row's first element, so that a row lies `shift` bytes into its place.
+template <class T, int N, int A, int S = kStages>
+struct Rows {
+    static constexpr bool kBulk = N * sizeof(T) == 16;
+    const T* p[A];
+    uint8_t* ring;              // S x A x stride bytes
+    uint64_t* bars;             // S
+    volatile int* dead;
+    int* err;
+    int D, stride, place = 0;
+    uint32_t parity = 0;
+
+    static __host__ __device__ int stride_of(int D) { return (D * (int)sizeof(T) + 4 + 15) / 16 * 16; }
+    __device__ __forceinline__ uint8_t* at(int place_, int k) const { return ring + (place_ * A + k) * stride; }
+    __device__ __forceinline__ uint32_t shift(int k, int64_t t) const {
+        return kBulk ? 0u : (uint32_t)(reinterpret_cast<uintptr_t>(p[k] + t * D) & 3u);
+    }
+    // the whole team; its earlier reads of the place lie before a barrier of the team
+    __device__ __forceinline__ void fill(const Team& team, int place_, int64_t t) const {
+        const int lane = threadIdx.x & 31;
+        if constexpr (kBulk) {
+            if (team.warp == 0 && lane == 0) {
+                const uint32_t bar = (uint32_t)__cvta_generic_to_shared(bars + place_), bytes = D * sizeof(T);
+                int n = 0;
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            v[i].w = {};
-            if (col + i * step < D) v[i].load(p + col + i * step);
+                for (int k = 0; k < A; ++k) n += p[k] != nullptr;
+                mbar_arrive_expect_tx(bar, n * bytes);
+                const uint64_t once = policy_evict_first();
+#pragma unroll
+                for (int k = 0; k < A; ++k)
+                    if (p[k]) bulk_g2s((uint32_t)__cvta_generic_to_shared(at(place_, k)), p[k] + t * D, bytes, bar, once);
+            }
+        } else {
+#pragma unroll
+            for (int k = 0; k < A; ++k) {
+                if (!p[k]) continue;
+                const uint8_t* row = reinterpret_cast<const uint8_t*>(p[k] + t * D);
+                const uint32_t s = shift(k, t), end = s + D * sizeof(T);
+                const uint32_t dst = (uint32_t)__cvta_generic_to_shared(at(place_, k));
+                for (uint32_t w = (team.warp * 32 + lane) * 4; w < end; w += team.warps * 128) {
+                    if (w >= s && w + 4 <= end) {
+                        asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst + w), "l"(row - s + w) : "memory");
+                    } else {                // a word of which the row has one half: no byte beside the row is read
+                        const uint32_t h = w < s ? s : w;
+                        *reinterpret_cast<uint16_t*>(at(place_, k) + h) = __ldg(reinterpret_cast<const uint16_t*>(row - s + h));
+                    }
+                }
+            }
         }
     }
-    __device__ __forceinline__ float get(int i, int j) const { return v[i].get(j); }
+    __device__ __forceinline__ void close() const {      // after every fill, taken place or not
+        if constexpr (!kBulk) asm volatile("cp.async.commit_group;" ::: "memory");
+    }
+    // the place's rows are there, for the whole team.  A wait that runs out marks
+    // the CTA: later waits return at once, the team goes on and its results are
+    // reported as incomplete
+    __device__ __forceinline__ void wait(const Team& team) const {
+        if constexpr (kBulk) {
+            const uint32_t bar = (uint32_t)__cvta_generic_to_shared(bars + place);
+            if (!mbar_try_wait(bar, parity)) {
+                const long long t0 = clock64();
+                while (!mbar_try_wait(bar, parity) && !*dead)
+                    if (clock64() - t0 > kWaitCycles) {
+                        *dead = 1;
+                        *err = kErrWait;
+                    }
+            }
+        } else {
+            asm volatile("cp.async.wait_group %0;" ::"n"(S - 1) : "memory");
+            team.sync();
+        }
+    }
+    __device__ __forceinline__ Pack<T, N> get(int k, int64_t t, int col) const {
+        Pack<T, N> v;
+        const uint8_t* q = at(place, k) + shift(k, t) + col * sizeof(T);
+        v.w = *reinterpret_cast<const typename Pack<T, N>::Word*>(q);
+        return v;
+    }
+    // this place is read by the whole team: orders the reads before its next fill
+    __device__ __forceinline__ void leave(const Team& team, int64_t t, int64_t end) {
+        if constexpr (kBulk) fence_proxy_async_smem();
+        team.sync();
+        if (t + S < end) fill(team, place, t + S);
+        close();
+        if (++place == S) {
+            place = 0;
+            parity ^= 1u;
+        }
+    }
+    __device__ __forceinline__ void start(const Team& team, int64_t t0, int64_t t1) const {
+        for (int i = 0; i < S; ++i) {
+            if (t0 + i < t1) fill(team, i, t0 + i);
+            close();
+        }
+    }
+    // copies in flight after a wait that ran out: bounded
+    __device__ __forceinline__ void drain() const {
+        if constexpr (kBulk) {
+            if (!*dead) return;
+            for (int i = 0; i < S; ++i) {
+                const long long t0 = clock64();
+                while (!mbar_try_wait((uint32_t)__cvta_generic_to_shared(bars + i), parity ^ (i < place ? 1u : 0u)) &&
+                       clock64() - t0 < kWaitCycles) {
+                }
+            }
+        }
+    }
 };
 
 constexpr int kJoinThreads = 256;
+constexpr int kJoinColumns = 1024;       // columns a warp holds at most
+
+// Shared memory of a kernel whose `teams` teams have rings of A rows a place
+template <class T, int N, int A, int S = kStages>
+size_t ring_bytes(int teams, int D) {
+    return (size_t)teams * S * A * Rows<T, N, A>::stride_of(D);
+}
 
 // Tokens [chunk team, chunk (team + 1)) of team number `team`
 template <class T, int N, int NV>
-__global__ void __launch_bounds__(kJoinThreads, N * NV > 16 ? 3 : 4)
+__global__ void __launch_bounds__(kJoinThreads, 2)
 k_norm_join(JoinArgs a, int team_warps, int64_t chunk, const T* __restrict__ x, const T* __restrict__ y,
             T* __restrict__ xo, T* __restrict__ no) {
+    extern __shared__ __align__(16) uint8_t rings[];
     __shared__ float4 slots[2 * kJoinThreads / 32];
+    __shared__ __align__(8) uint64_t bars[kJoinThreads / 32 * kStages];
+    __shared__ int dead;
     check_offsets(a.offsets, a.B, a.T, a.err);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     Team team{team_warps, warp % team_warps, warp / team_warps, slots, 0, kJoinThreads / 32};
@@ -101,34 +221,49 @@ k_norm_join(JoinArgs a, int team_warps, int64_t chunk, const T* __restrict__ x, 
     const T* gate = (const T*)a.gate;
     const T* wp = (const T*)a.w_post;
     const T* wn = (const T*)a.w_pre;
+    Rows<T, N, 2> rows{{x, y}, rings + team.id * kStages * 2 * Rows<T, N, 2>::stride_of(a.D), bars + team.id * kStages,
+                       &dead, a.err, a.D, Rows<T, N, 2>::stride_of(a.D)};
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < kJoinThreads / 32 * kStages; ++i) mbar_init((uint32_t)__cvta_generic_to_shared(bars + i), 1);
+        dead = 0;
+        fence_mbar_init();
+    }
+    __syncthreads();
     if (t0 >= t1) return;
+    rows.start(team, t0, t1);
     Sequence seq{a.offsets, a.B, a.T, 0, 0};
     if (gate) seq.start(t0);
     for (int64_t t = t0; t < t1; ++t) {
-        Row<T, N, NV> rx, ry;
-        rx.load(x + t * a.D, col, step, a.D);
         float v[NV][N];
         float q = 0.f;
+        rows.wait(team);
         if (y) {
-            ry.load(y + t * a.D, col, step, a.D);
             if (gate && seq.moved(t)) seq.move(t);
 #pragma unroll
-            for (int i = 0; i < NV; ++i)
+            for (int i = 0; i < NV; ++i) {
+                const int c = col + i * step;
+                if (c >= a.D) continue;
+                const Pack<T, N> r = rows.get(1, t, c);
 #pragma unroll
-                for (int j = 0; j < N; ++j) q = fmaf(ry.get(i, j), ry.get(i, j), q);
+                for (int j = 0; j < N; ++j) {
+                    v[i][j] = r.get(j);
+                    q = fmaf(v[i][j], v[i][j], q);
+                }
+            }
             const float iy = rsqrtf(fmaf(team.sum(make_float4(q, 0.f, 0.f, 0.f)).x, inv_d, a.eps));
             q = 0.f;
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
                 const int c = col + i * step;
                 if (c >= a.D) continue;
+                const Pack<T, N> r = rows.get(0, t, c);
                 Pack<T, N> w, g, o;
                 w.load(wp + c);
                 if (gate) g.load(gate + seq.b * a.D + c);
 #pragma unroll
                 for (int j = 0; j < N; ++j) {
-                    const float post = w.get(j) * (ry.get(i, j) * iy);
-                    v[i][j] = fmaf(a.rho, rx.get(i, j), gate ? g.get(j) * post : post);
+                    const float post = w.get(j) * (v[i][j] * iy);
+                    v[i][j] = fmaf(a.rho, r.get(j), gate ? g.get(j) * post : post);
                     q = fmaf(v[i][j], v[i][j], q);
                     o.set(j, v[i][j]);
                 }
@@ -136,13 +271,18 @@ k_norm_join(JoinArgs a, int team_warps, int64_t chunk, const T* __restrict__ x, 
             }
         } else {
 #pragma unroll
-            for (int i = 0; i < NV; ++i)
+            for (int i = 0; i < NV; ++i) {
+                const int c = col + i * step;
+                if (c >= a.D) continue;
+                const Pack<T, N> r = rows.get(0, t, c);
 #pragma unroll
                 for (int j = 0; j < N; ++j) {
-                    v[i][j] = rx.get(i, j);
+                    v[i][j] = r.get(j);
                     q = fmaf(v[i][j], v[i][j], q);
                 }
+            }
         }
+        rows.leave(team, t, t1);
         if (!no) continue;
         const float ix = rsqrtf(fmaf(team.sum(make_float4(q, 0.f, 0.f, 0.f)).x, inv_d, a.eps));
 #pragma unroll
@@ -156,11 +296,14 @@ k_norm_join(JoinArgs a, int team_warps, int64_t chunk, const T* __restrict__ x, 
             o.store(no + t * a.D + c);
         }
     }
+    rows.drain();
 }
 
 // ---- gradient ------------------------------------------------------------------
-constexpr int kGradThreads = 512;
-constexpr int kGradWarps = kGradThreads / 32;
+// 16 warps of 16-bit rows, 8 of float32 rows: three places of four rows each fit
+// the shared memory at 512 columns a warp.  One row of float32 beyond 4096 takes
+// 16 warps, and a single place.
+constexpr int grad_warps(int type, int D) { return type == IFVS_T_F32 && D <= 8 * 512 ? 8 : 16; }
 constexpr int kGradColumns = 512;        // columns a warp holds at most
 
 struct GradPlan {
@@ -171,20 +314,32 @@ struct GradPlan {
     float* weights;      // [ctas][2][D]: d_w_post, d_w_pre
 };
 
-template <class T, int N, int NV>
-__global__ void __launch_bounds__(kGradThreads, 1) k_norm_join_grad(JoinArgs a, JoinGrads g, GradPlan p) {
-    __shared__ float4 slots[2 * kGradWarps];
-    extern __shared__ float sums[];          // [teams of the CTA][D]
+template <class T, int N, int NV, int WARPS, int S>
+__global__ void __launch_bounds__(WARPS * 32, 1) k_norm_join_grad(JoinArgs a, JoinGrads g, GradPlan p) {
+    using Ring = Rows<T, N, 4, S>;
+    __shared__ float4 slots[2 * WARPS];
+    __shared__ __align__(8) uint64_t bars[WARPS * S];
+    __shared__ int dead;
+    extern __shared__ __align__(16) uint8_t rings[];     // after the tokens: [teams of the CTA][D] sums
     check_offsets(a.offsets, a.B, a.T, a.err);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    Team team{p.team_warps, warp % p.team_warps, warp / p.team_warps, slots, 0, kGradWarps};
-    const int cta_teams = kGradWarps / p.team_warps;
+    Team team{p.team_warps, warp % p.team_warps, warp / p.team_warps, slots, 0, WARPS};
+    const int cta_teams = WARPS / p.team_warps;
     const int64_t number = (int64_t)blockIdx.x * cta_teams + team.id;
     const int64_t t0 = min(a.T, number * p.chunk), t1 = min(a.T, t0 + p.chunk);
     const int col = (team.warp * 32 + lane) * N, step = p.team_warps * 32 * N;
     const float inv_d = 1.f / (float)a.D;
     const T *x = (const T*)g.x_out, *y = (const T*)g.y, *dxo = (const T*)g.d_x_out, *dn = (const T*)g.d_n;
     const T *gate = (const T*)a.gate, *wp = (const T*)a.w_post, *wn = (const T*)a.w_pre;
+    Ring rows{{x, y, dxo, dn}, rings + team.id * S * 4 * Ring::stride_of(a.D), bars + team.id * S, &dead, a.err, a.D,
+              Ring::stride_of(a.D)};
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < WARPS * S; ++i) mbar_init((uint32_t)__cvta_generic_to_shared(bars + i), 1);
+        dead = 0;
+        fence_mbar_init();
+    }
+    __syncthreads();
+    rows.start(team, t0, t1);
     float s_gate[NV][N], s_post[NV][N], s_pre[NV][N];
 #pragma unroll
     for (int i = 0; i < NV; ++i)
@@ -216,59 +371,80 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_norm_join_grad(JoinArgs a, 
     if (t0 < t1 && gate) seq.start(t0);
     for (int64_t t = t0; t < t1; ++t) {
         const int64_t at = t * a.D;
-        Row<T, N, NV> rx, ry, rd, rn;
-        rx.load(x + at, col, step, a.D);
-        if (dn) rn.load(dn + at, col, step, a.D);
-        if (y) ry.load(y + at, col, step, a.D);
-        if (dxo) rd.load(dxo + at, col, step, a.D);
         if (gate && seq.moved(t)) {
             if (g.d_gate) flush();
             seq.move(t);
         }
+        rows.wait(team);
         float4 q = make_float4(0.f, 0.f, 0.f, 0.f);        // x'^2, z x', y^2
-        float v[NV][N];                                    // z, then g
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int c = col + i * step;
-            Pack<T, N> w;
-            w.w = {};
-            if (dn && c < a.D) w.load(wn + c);
+            if (c >= a.D) continue;
+            if (dn) {
+                const Pack<T, N> r = rows.get(0, t, c), n = rows.get(3, t, c);
+                Pack<T, N> w;
+                w.load(wn + c);
 #pragma unroll
-            for (int j = 0; j < N; ++j) {
-                v[i][j] = dn ? rn.get(i, j) * w.get(j) : 0.f;
-                q.x = fmaf(rx.get(i, j), rx.get(i, j), q.x);
-                q.y = fmaf(v[i][j], rx.get(i, j), q.y);
-                if (y) q.z = fmaf(ry.get(i, j), ry.get(i, j), q.z);
+                for (int j = 0; j < N; ++j) {
+                    q.x = fmaf(r.get(j), r.get(j), q.x);
+                    q.y = fmaf(n.get(j) * w.get(j), r.get(j), q.y);
+                }
+            }
+            if (y) {
+                const Pack<T, N> r = rows.get(1, t, c);
+#pragma unroll
+                for (int j = 0; j < N; ++j) q.z = fmaf(r.get(j), r.get(j), q.z);
             }
         }
         q = team.sum(q);
         const float ix = dn ? rsqrtf(fmaf(q.x, inv_d, a.eps)) : 0.f, iy = rsqrtf(fmaf(q.z, inv_d, a.eps));
         const float along = ix * ix * (q.y * inv_d);
+        float v[NV][N], u[NV][N];                          // du, u
         float m = 0.f;                                     // du u
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int c = col + i * step;
             if (c >= a.D) continue;
-            Pack<T, N> w, k, o;
-            if (y) w.load(wp + c);
-            if (gate) k.load(gate + seq.b * a.D + c);
+            if (dxo) {
+                const Pack<T, N> r = rows.get(2, t, c);
 #pragma unroll
-            for (int j = 0; j < N; ++j) {
-                const float xv = rx.get(i, j);
-                float gv = ix * (v[i][j] - xv * along);
-                if (dxo) gv += rd.get(i, j);
-                if (dn) s_pre[i][j] = fmaf(rn.get(i, j) * ix, xv, s_pre[i][j]);
-                o.set(j, a.rho * gv);
-                if (y) {
-                    const float gu = gv * (ry.get(i, j) * iy), gk = gate ? k.get(j) : 1.f;
-                    s_gate[i][j] += gu;
-                    s_post[i][j] = fmaf(gk, gu, s_post[i][j]);
-                    v[i][j] = gk * w.get(j) * gv;          // du
-                    m = fmaf(v[i][j], ry.get(i, j) * iy, m);
+                for (int j = 0; j < N; ++j) v[i][j] = r.get(j);
+            } else {
+#pragma unroll
+                for (int j = 0; j < N; ++j) v[i][j] = 0.f;
+            }
+            if (dn) {
+                const Pack<T, N> r = rows.get(0, t, c), n = rows.get(3, t, c);
+                Pack<T, N> w;
+                w.load(wn + c);
+#pragma unroll
+                for (int j = 0; j < N; ++j) {
+                    v[i][j] += ix * (n.get(j) * w.get(j) - r.get(j) * along);
+                    s_pre[i][j] = fmaf(n.get(j) * ix, r.get(j), s_pre[i][j]);
                 }
             }
+            Pack<T, N> o;
+#pragma unroll
+            for (int j = 0; j < N; ++j) o.set(j, a.rho * v[i][j]);
             o.store((T*)g.dx + at + c);
+            if (y) {
+                const Pack<T, N> r = rows.get(1, t, c);
+                Pack<T, N> w, k;
+                w.load(wp + c);
+                if (gate) k.load(gate + seq.b * a.D + c);
+#pragma unroll
+                for (int j = 0; j < N; ++j) {
+                    u[i][j] = r.get(j) * iy;
+                    const float gu = v[i][j] * u[i][j], gk = gate ? k.get(j) : 1.f;
+                    s_gate[i][j] += gu;
+                    s_post[i][j] = fmaf(gk, gu, s_post[i][j]);
+                    v[i][j] *= gk * w.get(j);
+                    m = fmaf(v[i][j], u[i][j], m);
+                }
+            }
         }
+        rows.leave(team, t, t1);
         if (!y) continue;
         m = team.sum(make_float4(m, 0.f, 0.f, 0.f)).x * inv_d;
 #pragma unroll
@@ -277,12 +453,14 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_norm_join_grad(JoinArgs a, 
             if (c >= a.D) continue;
             Pack<T, N> o;
 #pragma unroll
-            for (int j = 0; j < N; ++j) o.set(j, iy * (v[i][j] - (ry.get(i, j) * iy) * m));
+            for (int j = 0; j < N; ++j) o.set(j, iy * (v[i][j] - u[i][j] * m));
             o.store((T*)g.dy + at + c);
         }
     }
+    rows.drain();
     if (t0 < t1 && g.d_gate) flush();
     // the CTA's sums for the norms' weights, teams in order
+    float* sums = reinterpret_cast<float*>(rings);
     auto gather = [&](const float (&s)[NV][N], float* to) {
         __syncthreads();
 #pragma unroll
@@ -291,7 +469,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_norm_join_grad(JoinArgs a, 
             for (int j = 0; j < N; ++j)
                 if (col + i * step < a.D) sums[team.id * a.D + col + i * step + j] = s[i][j];
         __syncthreads();
-        for (int c = threadIdx.x; c < a.D; c += kGradThreads) {
+        for (int c = threadIdx.x; c < a.D; c += WARPS * 32) {
             float v = 0.f;
             for (int k = 0; k < cta_teams; ++k) v += sums[k * a.D + c];
             to[c] = v;
@@ -391,6 +569,8 @@ cudaError_t pick(int n, std::integer_sequence<int, NV...>, const Fn& f) {
      ...);
     return e;
 }
+template <int N>
+using Count = std::integral_constant<int, N>;
 template <int... NV>
 using Counts = std::integer_sequence<int, NV...>;
 
@@ -399,15 +579,18 @@ using Counts = std::integer_sequence<int, NV...>;
 cudaError_t launch_norm_join(const JoinArgs& a, const void* x, const void* y, void* x_out, void* n_out,
                              cudaStream_t s) {
     const int N = access_elems(a, x, y, x_out, n_out);
-    const Shape sh = team_shape(a.D, N, 1024);
+    const Shape sh = team_shape(a.D, N, kJoinColumns);
     auto go = [&](auto t, auto n, auto nv) {
         using T = decltype(t);
-        constexpr int E = n() * nv();
-        const int64_t cta_teams = kJoinThreads / 32 / sh.warps;
-        const int64_t want = (a.T + cta_teams - 1) / cta_teams, most = (int64_t)a.num_sms * (E > 16 ? 3 : 4);
+        const int cta_teams = kJoinThreads / 32 / sh.warps;
+        const size_t smem = ring_bytes<T, n(), 2>(cta_teams, a.D);
+        const cudaError_t e = cudaFuncSetAttribute(k_norm_join<T, n(), nv()>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        if (e != cudaSuccess) return e;
+        // as many CTAs as run at once; fewer tokens: one per team
+        const int64_t want = (a.T + cta_teams - 1) / cta_teams, most = (int64_t)a.num_sms * (smem > 110 * 1024 ? 1 : 2);
         const int64_t ctas = want < most ? want : most, chunk = (a.T + ctas * cta_teams - 1) / (ctas * cta_teams);
-        k_norm_join<T, n(), nv()><<<(unsigned)ctas, kJoinThreads, 0, s>>>(a, sh.warps, chunk, (const T*)x, (const T*)y,
-                                                                        (T*)x_out, (T*)n_out);
+        k_norm_join<T, n(), nv()><<<(unsigned)ctas, kJoinThreads, smem, s>>>(a, sh.warps, chunk, (const T*)x, (const T*)y,
+                                                                           (T*)x_out, (T*)n_out);
         return cudaGetLastError();
     };
     auto of16 = [&](auto t) {
@@ -423,10 +606,12 @@ cudaError_t launch_norm_join(const JoinArgs& a, const void* x, const void* y, vo
 }
 
 namespace {
-GradPlan grad_plan(const JoinArgs& a, int warps) {
+GradPlan grad_plan(const JoinArgs& a) {
     GradPlan p{};
-    p.team_warps = warps;
-    const int64_t cta_teams = kGradWarps / warps, want = (a.T + cta_teams - 1) / cta_teams;
+    p.team_warps = 1;
+    while (p.team_warps * kGradColumns < a.D) p.team_warps *= 2;
+    const int64_t cta_teams = grad_warps(a.type, a.D) / p.team_warps;
+    const int64_t want = (a.T + cta_teams - 1) / cta_teams;
     p.ctas = (int)(want < a.num_sms ? want : a.num_sms);
     p.teams = p.ctas * cta_teams;
     p.chunk = p.teams ? (a.T + p.teams - 1) / p.teams : 1;
@@ -434,26 +619,39 @@ GradPlan grad_plan(const JoinArgs& a, int warps) {
 }
 }  // namespace
 
-// the team's shape depends on the arrays' alignment: room for teams of one warp
 size_t norm_join_grad_bytes(const JoinArgs& a) {
-    int warps = 1;
-    while (warps * kGradColumns < a.D) warps *= 2;
-    const GradPlan p = grad_plan(a, warps);
+    const GradPlan p = grad_plan(a);
     return (size_t)(p.teams + p.ctas) * 2 * a.D * sizeof(float);
 }
 
 cudaError_t launch_norm_join_grad(const JoinArgs& a, const JoinGrads& g, uint8_t* work, cudaStream_t s) {
     const int N = access_elems(a, g.x_out, g.y, g.d_x_out, g.d_n, g.dx, g.dy, g.d_gate);
     const Shape sh = team_shape(a.D, N, kGradColumns);
-    GradPlan p = grad_plan(a, sh.warps);
+    GradPlan p = grad_plan(a);
     p.gates = (float*)work;
     p.weights = p.gates + p.teams * 2 * a.D;
     auto go = [&](auto t, auto n, auto nv) {
         using T = decltype(t);
-        const size_t smem = (size_t)(kGradWarps / sh.warps) * a.D * sizeof(float);     // at most 32 KB
-        if (a.T > 0)
-            k_norm_join_grad<T, n(), nv()><<<(unsigned)p.ctas, kGradThreads, smem, s>>>(a, g, p);
-        cudaError_t e = cudaGetLastError();
+        auto rows = [&](auto warps, auto places) {
+            const auto kernel = k_norm_join_grad<T, n(), nv(), warps(), places()>;
+            const int cta_teams = warps() / p.team_warps;
+            size_t smem = ring_bytes<T, n(), 4, places()>(cta_teams, a.D);
+            const size_t sums = (size_t)cta_teams * a.D * sizeof(float);
+            smem = smem > sums ? smem : sums;
+            const cudaError_t r = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+            if (r != cudaSuccess) return r;
+            kernel<<<(unsigned)p.ctas, warps() * 32, smem, s>>>(a, g, p);
+            return cudaGetLastError();
+        };
+        cudaError_t e = cudaSuccess;
+        if (a.T == 0) {
+        } else if constexpr (sizeof(T) == 2) {
+            e = rows(Count<16>(), Count<kStages>());
+        } else if (grad_warps(a.type, a.D) == 8) {
+            e = rows(Count<8>(), Count<kStages>());
+        } else if constexpr (n() * nv() == 16) {
+            e = rows(Count<16>(), Count<1>());
+        }
         if (e != cudaSuccess) return e;
         const int64_t teams = g.d_gate ? p.teams : 0, clears = g.d_gate && a.offsets ? (a.B + kClearRows - 1) / kClearRows : 0;
         GradPlan q = p;
