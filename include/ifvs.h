@@ -461,8 +461,8 @@ int ifvs_get_conditioning(ifvs_index* ix, float* bank, float* W, uint32_t flags)
  *
  * A handle holds the workspace, the order of the calls that use it, and an
  * error word.  With a non-NULL stream a call only enqueues its work there
- * (the legacy default stream is cudaStreamLegacy, (void*)1) and the handle's
- * next call waits for it on the device, whatever that call's stream; with
+ * (the legacy default stream is cudaStreamLegacy, (void*)1); calls that use
+ * the workspace wait for each other on the device, whatever their streams; with
  * stream NULL it runs on a stream of the handle's own, a blocking one, and
  * returns when its outputs are written.  A call whose workspace has to grow
  * allocates (and waits for the device): run the largest shape once before a
@@ -483,12 +483,11 @@ enum { IFVS_ACT_SILU = 0, IFVS_ACT_GELU = 1, IFVS_ACT_RELU = 2 };
 #define IFVS_MAX_HIDDEN 65536    /* largest hidden width F of ifvs_ffn         */
 
 /* ifvs_layers_create — a handle on `device` (free with ifvs_layers_free,
- * which waits for the handle's work). */
+ * which waits for the device). */
 int ifvs_layers_create(ifvs_layers** out, int32_t device);
 void ifvs_layers_free(ifvs_layers* L);
 
-/* ifvs_layers_status — waits for the work enqueued through the handle,
- * returns the error that its kernels found since the last status call or
+/* ifvs_layers_status — waits for the device, returns the error that its kernels found since the last status call or
  * waiting call (IFVS_OK: none) and clears it. */
 int ifvs_layers_status(ifvs_layers* L);
 

@@ -27,6 +27,7 @@ constexpr int kEmbedPieces = 4;
 template <class T, int N>
 __global__ void __launch_bounds__(256)
 k_embed(const T* __restrict__ table, EmbedArgs a, T* __restrict__ out) {
+    using F = typename Pack<T, N>::F;
     const int per_row = a.D / N;
     const int64_t n = a.T * per_row;
     const int64_t first = (int64_t)blockIdx.x * (256 * kEmbedPieces) + threadIdx.x;
@@ -49,7 +50,7 @@ k_embed(const T* __restrict__ table, EmbedArgs a, T* __restrict__ out) {
         const int64_t at = first + i * 256;
         if (at >= n) continue;
 #pragma unroll
-        for (int j = 0; j < N; ++j) v[i].set(j, some[i] ? a.scale * v[i].get(j) : 0.f);
+        for (int j = 0; j < Pack<T, N>::kF; ++j) v[i].set(j, some[i] ? mul_(both<F>(a.scale), v[i].get(j)) : both<F>(0.f));
         v[i].store_stream(out + at * N);     // the table's rows stay in L2
     }
 }
@@ -314,6 +315,8 @@ template <class T, int N, int NV>
 __global__ void __launch_bounds__(256, NV == 1 ? 4 : 2)
 k_embed_sum(const T* __restrict__ d_out, EmbedArgs a, SumPlan p, Pairs sorted, float* __restrict__ partial,
             T* __restrict__ d_table) {
+    using F = typename Pack<T, N>::F;
+    constexpr int kF = Pack<T, N>::kF;
     constexpr int AHEAD = NV == 1 ? 8 : 4;               // rows in flight
     const int lane = threadIdx.x & 31;
     const int64_t job = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
@@ -337,7 +340,7 @@ k_embed_sum(const T* __restrict__ d_out, EmbedArgs a, SumPlan p, Pairs sorted, f
         uint32_t rows = __ballot_sync(0xFFFFFFFFu, absent);
         Pack<T, N> zero;
 #pragma unroll
-        for (int j = 0; j < N; ++j) zero.set(j, 0.f);
+        for (int j = 0; j < kF; ++j) zero.set(j, both<F>(0.f));
         for (; rows; rows &= rows - 1u) {
             T* row = d_table + (v - lane + __ffs(rows) - 1) * a.D;
             for (int c = lane * N; c < a.D; c += 32 * N) zero.store(row + c);
@@ -347,14 +350,14 @@ k_embed_sum(const T* __restrict__ d_out, EmbedArgs a, SumPlan p, Pairs sorted, f
     const int64_t part = job / p.slices;
     const int slice = (int)(job - part * p.slices);
     const int64_t begin = part * p.part, end = min(a.T, begin + p.part);
-    float sum[NV][N];
+    F sum[NV][kF];
     int64_t run = -1;                                    // the run's key
     bool head = false;
     auto clear = [&] {
 #pragma unroll
         for (int i = 0; i < NV; ++i)
 #pragma unroll
-            for (int j = 0; j < N; ++j) sum[i][j] = 0.f;
+            for (int j = 0; j < kF; ++j) sum[i][j] = both<F>(0.f);
     };
     auto flush = [&](bool goes_on) {
         if (run < 0 || run >= a.V) return;
@@ -364,8 +367,8 @@ k_embed_sum(const T* __restrict__ d_out, EmbedArgs a, SumPlan p, Pairs sorted, f
             for (int i = 0; i < NV; ++i) {
                 const int c = column<T, N, NV>(slice, i, lane);
 #pragma unroll
-                for (int j = 0; j < N; ++j)
-                    if (c + j < a.D) to[c + j] = sum[i][j];
+                for (int j = 0; j < kF; ++j)
+                    if (c < a.D) *reinterpret_cast<F*>(to + c + j * (N / kF)) = sum[i][j];
             }
         } else {
 #pragma unroll
@@ -373,7 +376,7 @@ k_embed_sum(const T* __restrict__ d_out, EmbedArgs a, SumPlan p, Pairs sorted, f
                 const int c = column<T, N, NV>(slice, i, lane);
                 Pack<T, N> v;
 #pragma unroll
-                for (int j = 0; j < N; ++j) v.set(j, a.scale * sum[i][j]);
+                for (int j = 0; j < kF; ++j) v.set(j, mul_(both<F>(a.scale), sum[i][j]));
                 if (c < a.D) v.store(d_table + run * a.D + c);
             }
         }
@@ -409,7 +412,7 @@ k_embed_sum(const T* __restrict__ d_out, EmbedArgs a, SumPlan p, Pairs sorted, f
 #pragma unroll
                 for (int i = 0; i < NV; ++i)
 #pragma unroll
-                    for (int j = 0; j < N; ++j) sum[i][j] += v[u][i].get(j);
+                    for (int j = 0; j < kF; ++j) sum[i][j] = add_(sum[i][j], v[u][i].get(j));
             }
         }
     }

@@ -13,7 +13,7 @@ using namespace ifvs;
 struct ifvs_layers {
     int device = 0, num_sms = 0;
     cudaStream_t own = nullptr;
-    cudaEvent_t done = nullptr;     // after the last enqueued call
+    cudaEvent_t done = nullptr;     // after the last enqueued call that used the workspace
     uint8_t* work = nullptr;
     size_t work_bytes = 0;
     int* err_host = nullptr;        // the error word, page-locked
@@ -55,18 +55,21 @@ struct Call {
     ifvs_layers* L;
     DeviceGuard guard;
     cudaStream_t s;
-    bool waits, captured = false;
+    bool waits, ordered = false;
 
     Call(ifvs_layers* l, void* stream)
         : L(l), guard(l->device), s(stream ? (cudaStream_t)stream : l->own), waits(stream == nullptr) {}
 
+    // bytes: of workspace (0: the call has no place in the order of those that use it)
     int begin(size_t bytes) {
         if (!guard.ok) return report_error(IFVS_ERR_CUDA, "device %d cannot be made current", L->device);
+        if (bytes == 0) return 0;
         cudaStreamCaptureStatus st = cudaStreamCaptureStatusNone;
         if (!waits) CUDA_TRY(cudaStreamIsCapturing(s, &st));
-        captured = st != cudaStreamCaptureStatusNone;
+        // in a capture the order of the graph's launches is the caller's
+        ordered = st == cudaStreamCaptureStatusNone;
         if (bytes > L->work_bytes) {
-            if (captured) return report_error(IFVS_ERR_STATE, "the workspace would have to grow during a stream capture");
+            if (!ordered) return report_error(IFVS_ERR_STATE, "the workspace would have to grow during a stream capture");
             CUDA_TRY(cudaEventSynchronize(L->done));
             if (L->work) cudaFree(L->work);
             L->work = nullptr;
@@ -81,12 +84,11 @@ struct Call {
             L->work = (uint8_t*)p;
             L->work_bytes = bytes;
         }
-        // in a capture the order of the graph's launches is the caller's
-        if (!captured) CUDA_TRY(cudaStreamWaitEvent(s, L->done, 0));
+        if (ordered) CUDA_TRY(cudaStreamWaitEvent(s, L->done, 0));
         return 0;
     }
     int end() {
-        if (!captured) CUDA_TRY(cudaEventRecord(L->done, s));
+        if (ordered) CUDA_TRY(cudaEventRecord(L->done, s));
         if (!waits) return IFVS_OK;
         CUDA_TRY(cudaStreamSynchronize(s));
         return take_error(L);
@@ -209,10 +211,8 @@ int ifvs_layers_create(ifvs_layers** out, int32_t device) {
 void ifvs_layers_free(ifvs_layers* L) {
     if (!L) return;
     DeviceGuard guard(L->device);
-    if (L->done) {
-        cudaEventSynchronize(L->done);
-        cudaEventDestroy(L->done);
-    }
+    cudaDeviceSynchronize();        // kernels may still write the error word
+    if (L->done) cudaEventDestroy(L->done);
     if (L->work) cudaFree(L->work);
     if (L->own) cudaStreamDestroy(L->own);
     if (L->err_host) cudaFreeHost(L->err_host);
@@ -223,7 +223,7 @@ void ifvs_layers_free(ifvs_layers* L) {
 int ifvs_layers_status(ifvs_layers* L) {
     if (!L) return report_error(IFVS_ERR_ARG, "the handle is NULL");
     DeviceGuard guard(L->device);
-    CUDA_TRY(cudaEventSynchronize(L->done));
+    CUDA_TRY(cudaDeviceSynchronize());
     return take_error(L);
 }
 

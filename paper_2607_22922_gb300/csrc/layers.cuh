@@ -36,18 +36,83 @@ __device__ __forceinline__ float warp_sum(float v) {
     return v;
 }
 
-// N consecutive elements as floats, in one access
+// ---- pairs of floats: two float32 operations per instruction -----------------
+__device__ __forceinline__ uint64_t bits(float2 v) { return *reinterpret_cast<uint64_t*>(&v); }
+__device__ __forceinline__ float2 pair(uint64_t v) { return *reinterpret_cast<float2*>(&v); }
+__device__ __forceinline__ float2 fma_(float2 a, float2 b, float2 c) {
+    uint64_t d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(bits(a)), "l"(bits(b)), "l"(bits(c)));
+    return pair(d);
+}
+__device__ __forceinline__ float2 mul_(float2 a, float2 b) {
+    uint64_t d;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(bits(a)), "l"(bits(b)));
+    return pair(d);
+}
+__device__ __forceinline__ float2 add_(float2 a, float2 b) {
+    uint64_t d;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(bits(a)), "l"(bits(b)));
+    return pair(d);
+}
+__device__ __forceinline__ float fma_(float a, float b, float c) { return fmaf(a, b, c); }
+__device__ __forceinline__ float mul_(float a, float b) { return a * b; }
+__device__ __forceinline__ float add_(float a, float b) { return a + b; }
+__device__ __forceinline__ float total(float2 v) { return v.x + v.y; }
+__device__ __forceinline__ float total(float v) { return v; }
+template <class F>
+__device__ __forceinline__ F both(float v);
+template <>
+__device__ __forceinline__ float both<float>(float v) { return v; }
+template <>
+__device__ __forceinline__ float2 both<float2>(float v) { return make_float2(v, v); }
+
+// two 16-bit elements <-> a pair of floats
+__device__ __forceinline__ float2 unpack2(uint32_t w, __nv_bfloat16) {
+    return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u));
+}
+__device__ __forceinline__ float2 unpack2(uint32_t w, __half) { return __half22float2(*reinterpret_cast<__half2*>(&w)); }
+__device__ __forceinline__ uint32_t pack2(float2 v, __nv_bfloat16) {
+    uint32_t d;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(v.y), "f"(v.x));
+    return d;
+}
+__device__ __forceinline__ uint32_t pack2(float2 v, __half) {
+    uint32_t d;
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(v.y), "f"(v.x));
+    return d;
+}
+
+// N consecutive elements, in one access of 16, 4 or 2 bytes, as N / 2 pairs of
+// floats or (N = 1) one float
 template <class T, int N>
 struct Pack {
     static constexpr int kBytes = N * (int)sizeof(T);
     using Word = std::conditional_t<kBytes == 16, uint4, std::conditional_t<kBytes == 4, uint32_t, uint16_t>>;
+    using F = std::conditional_t<N == 1, float, float2>;
+    static constexpr int kF = N == 1 ? 1 : N / 2;
     Word w;
     __device__ __forceinline__ void load(const T* p) { w = __ldg(reinterpret_cast<const Word*>(p)); }
     __device__ __forceinline__ void store(T* p) const { *reinterpret_cast<Word*>(p) = w; }
     // not to be read again soon
     __device__ __forceinline__ void store_stream(T* p) const { __stcs(reinterpret_cast<Word*>(p), w); }
-    __device__ __forceinline__ float get(int i) const { return to_f32(reinterpret_cast<const T*>(&w)[i]); }
-    __device__ __forceinline__ void set(int i, float v) { reinterpret_cast<T*>(&w)[i] = from_f32<T>(v); }
+    __device__ __forceinline__ F get(int i) const {
+        if constexpr (N == 1) {
+            return to_f32(*reinterpret_cast<const T*>(&w));
+        } else if constexpr (sizeof(T) == 4) {
+            return reinterpret_cast<const float2*>(&w)[i];
+        } else {
+            return unpack2(reinterpret_cast<const uint32_t*>(&w)[i], T());
+        }
+    }
+    __device__ __forceinline__ void set(int i, F v) {
+        if constexpr (N == 1) {
+            *reinterpret_cast<T*>(&w) = from_f32<T>(v);
+        } else if constexpr (sizeof(T) == 4) {
+            reinterpret_cast<float2*>(&w)[i] = v;
+        } else {
+            reinterpret_cast<uint32_t*>(&w)[i] = pack2(v, T());
+        }
+    }
 };
 
 // Calls f with a value of the element type that `type` names

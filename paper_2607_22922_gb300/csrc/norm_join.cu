@@ -231,40 +231,56 @@ k_norm_join(JoinArgs a, int team_warps, int64_t chunk, const T* __restrict__ x, 
     __syncthreads();
     if (t0 >= t1) return;
     rows.start(team, t0, t1);
+    using F = typename Pack<T, N>::F;
+    constexpr int kF = Pack<T, N>::kF;
     Sequence seq{a.offsets, a.B, a.T, 0, 0};
+    F gw[NV][kF];                    // gate * w_post of the sequence
+    auto load_gate = [&] {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int c = col + i * step;
+            if (c >= a.D) continue;
+            Pack<T, N> w, g;
+            w.load(wp + c);
+            if (gate) g.load(gate + seq.b * a.D + c);
+#pragma unroll
+            for (int j = 0; j < kF; ++j) gw[i][j] = gate ? mul_(g.get(j), w.get(j)) : w.get(j);
+        }
+    };
     if (gate) seq.start(t0);
+    if (y) load_gate();
+    const F rho = both<F>(a.rho);
     for (int64_t t = t0; t < t1; ++t) {
-        float v[NV][N];
-        float q = 0.f;
+        F v[NV][kF], q = both<F>(0.f);
+        if (gate && seq.moved(t)) {
+            seq.move(t);
+            load_gate();
+        }
         rows.wait(team);
         if (y) {
-            if (gate && seq.moved(t)) seq.move(t);
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
                 const int c = col + i * step;
                 if (c >= a.D) continue;
                 const Pack<T, N> r = rows.get(1, t, c);
 #pragma unroll
-                for (int j = 0; j < N; ++j) {
+                for (int j = 0; j < kF; ++j) {
                     v[i][j] = r.get(j);
-                    q = fmaf(v[i][j], v[i][j], q);
+                    q = fma_(v[i][j], v[i][j], q);
                 }
             }
-            const float iy = rsqrtf(fmaf(team.sum(make_float4(q, 0.f, 0.f, 0.f)).x, inv_d, a.eps));
-            q = 0.f;
+            const F iy = both<F>(rsqrtf(fmaf(team.sum(make_float4(total(q), 0.f, 0.f, 0.f)).x, inv_d, a.eps)));
+            q = both<F>(0.f);
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
                 const int c = col + i * step;
                 if (c >= a.D) continue;
                 const Pack<T, N> r = rows.get(0, t, c);
-                Pack<T, N> w, g, o;
-                w.load(wp + c);
-                if (gate) g.load(gate + seq.b * a.D + c);
+                Pack<T, N> o;
 #pragma unroll
-                for (int j = 0; j < N; ++j) {
-                    const float post = w.get(j) * (v[i][j] * iy);
-                    v[i][j] = fmaf(a.rho, r.get(j), gate ? g.get(j) * post : post);
-                    q = fmaf(v[i][j], v[i][j], q);
+                for (int j = 0; j < kF; ++j) {
+                    v[i][j] = fma_(mul_(v[i][j], iy), gw[i][j], mul_(rho, r.get(j)));
+                    q = fma_(v[i][j], v[i][j], q);
                     o.set(j, v[i][j]);
                 }
                 o.store(xo + t * a.D + c);
@@ -276,15 +292,15 @@ k_norm_join(JoinArgs a, int team_warps, int64_t chunk, const T* __restrict__ x, 
                 if (c >= a.D) continue;
                 const Pack<T, N> r = rows.get(0, t, c);
 #pragma unroll
-                for (int j = 0; j < N; ++j) {
+                for (int j = 0; j < kF; ++j) {
                     v[i][j] = r.get(j);
-                    q = fmaf(v[i][j], v[i][j], q);
+                    q = fma_(v[i][j], v[i][j], q);
                 }
             }
         }
         rows.leave(team, t, t1);
         if (!no) continue;
-        const float ix = rsqrtf(fmaf(team.sum(make_float4(q, 0.f, 0.f, 0.f)).x, inv_d, a.eps));
+        const F ix = both<F>(rsqrtf(fmaf(team.sum(make_float4(total(q), 0.f, 0.f, 0.f)).x, inv_d, a.eps)));
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int c = col + i * step;
@@ -292,7 +308,7 @@ k_norm_join(JoinArgs a, int team_warps, int64_t chunk, const T* __restrict__ x, 
             Pack<T, N> w, o;
             w.load(wn + c);
 #pragma unroll
-            for (int j = 0; j < N; ++j) o.set(j, w.get(j) * (v[i][j] * ix));
+            for (int j = 0; j < kF; ++j) o.set(j, mul_(w.get(j), mul_(v[i][j], ix)));
             o.store(no + t * a.D + c);
         }
     }
@@ -340,43 +356,69 @@ __global__ void __launch_bounds__(WARPS * 32, 1) k_norm_join_grad(JoinArgs a, Jo
     }
     __syncthreads();
     rows.start(team, t0, t1);
-    float s_gate[NV][N], s_post[NV][N], s_pre[NV][N];
+    using F = typename Pack<T, N>::F;
+    constexpr int kF = Pack<T, N>::kF;
+    F s_gate[NV][kF], s_post[NV][kF], s_pre[NV][kF];
 #pragma unroll
     for (int i = 0; i < NV; ++i)
 #pragma unroll
-        for (int j = 0; j < N; ++j) s_gate[i][j] = s_post[i][j] = s_pre[i][j] = 0.f;
+        for (int j = 0; j < kF; ++j) s_gate[i][j] = s_post[i][j] = s_pre[i][j] = both<F>(0.f);
     Sequence seq{a.offsets, a.B, a.T, 0, 0};
-    // the sums of the tokens of seq.b among this team's
+    F gw[NV][kF];                                          // gate * w_post of the sequence
+    auto load_gate = [&] {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int c = col + i * step;
+            if (c >= a.D) continue;
+            Pack<T, N> w, k;
+            w.load(wp + c);
+            if (gate) k.load(gate + seq.b * a.D + c);
+#pragma unroll
+            for (int j = 0; j < kF; ++j) gw[i][j] = gate ? mul_(k.get(j), w.get(j)) : w.get(j);
+        }
+    };
+    // s_gate, the sum of g u over the tokens of seq.b among this team's, goes to
+    // its place and, times the gate, to s_post
     auto flush = [&] {
         const bool head = seq.begin() < t0, goes_on = seq.end > t1;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int c = col + i * step;
             if (c >= a.D) continue;
-            if (head || goes_on) {
-                float* to = p.gates + (number * 2 + (head ? 0 : 1)) * a.D + c;
+            if (g.d_gate) {
+                if (head || goes_on) {
+                    float* to = p.gates + (number * 2 + (head ? 0 : 1)) * a.D + c;
 #pragma unroll
-                for (int j = 0; j < N; ++j) to[j] = s_gate[i][j];
-            } else {
-                Pack<T, N> w, o;
-                w.load(wp + c);
+                    for (int j = 0; j < kF; ++j) *reinterpret_cast<F*>(to + j * (N / kF)) = s_gate[i][j];
+                } else {
+                    Pack<T, N> w, o;
+                    w.load(wp + c);
 #pragma unroll
-                for (int j = 0; j < N; ++j) o.set(j, w.get(j) * s_gate[i][j]);
-                o.store((T*)g.d_gate + seq.b * a.D + c);
+                    for (int j = 0; j < kF; ++j) o.set(j, mul_(w.get(j), s_gate[i][j]));
+                    o.store((T*)g.d_gate + seq.b * a.D + c);
+                }
             }
+            Pack<T, N> k;
+            if (gate) k.load(gate + seq.b * a.D + c);
 #pragma unroll
-            for (int j = 0; j < N; ++j) s_gate[i][j] = 0.f;
+            for (int j = 0; j < kF; ++j) {
+                s_post[i][j] = fma_(gate ? k.get(j) : both<F>(1.f), s_gate[i][j], s_post[i][j]);
+                s_gate[i][j] = both<F>(0.f);
+            }
         }
     };
     if (t0 < t1 && gate) seq.start(t0);
+    if (t0 < t1 && y) load_gate();
+    const F rho = both<F>(a.rho);
     for (int64_t t = t0; t < t1; ++t) {
         const int64_t at = t * a.D;
         if (gate && seq.moved(t)) {
-            if (g.d_gate) flush();
+            flush();
             seq.move(t);
+            load_gate();
         }
         rows.wait(team);
-        float4 q = make_float4(0.f, 0.f, 0.f, 0.f);        // x'^2, z x', y^2
+        F qx = both<F>(0.f), qz = both<F>(0.f), qy = both<F>(0.f);      // x'^2, z x', y^2
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int c = col + i * step;
@@ -386,22 +428,23 @@ __global__ void __launch_bounds__(WARPS * 32, 1) k_norm_join_grad(JoinArgs a, Jo
                 Pack<T, N> w;
                 w.load(wn + c);
 #pragma unroll
-                for (int j = 0; j < N; ++j) {
-                    q.x = fmaf(r.get(j), r.get(j), q.x);
-                    q.y = fmaf(n.get(j) * w.get(j), r.get(j), q.y);
+                for (int j = 0; j < kF; ++j) {
+                    const F x_ = r.get(j);
+                    qx = fma_(x_, x_, qx);
+                    qz = fma_(mul_(n.get(j), w.get(j)), x_, qz);
                 }
             }
             if (y) {
                 const Pack<T, N> r = rows.get(1, t, c);
 #pragma unroll
-                for (int j = 0; j < N; ++j) q.z = fmaf(r.get(j), r.get(j), q.z);
+                for (int j = 0; j < kF; ++j) qy = fma_(r.get(j), r.get(j), qy);
             }
         }
-        q = team.sum(q);
-        const float ix = dn ? rsqrtf(fmaf(q.x, inv_d, a.eps)) : 0.f, iy = rsqrtf(fmaf(q.z, inv_d, a.eps));
-        const float along = ix * ix * (q.y * inv_d);
-        float v[NV][N], u[NV][N];                          // du, u
-        float m = 0.f;                                     // du u
+        const float4 q = team.sum(make_float4(total(qx), total(qz), total(qy), 0.f));
+        const float ix_ = dn ? rsqrtf(fmaf(q.x, inv_d, a.eps)) : 0.f, iy_ = rsqrtf(fmaf(q.z, inv_d, a.eps));
+        const F ix = both<F>(ix_), along = both<F>(-ix_ * ix_ * ix_ * (q.y * inv_d)), iy = both<F>(iy_);
+        F v[NV][kF], m = both<F>(0.f);                     // du / rms(y); du u
+        Pack<T, N> ry[NV];
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int c = col + i * step;
@@ -409,65 +452,62 @@ __global__ void __launch_bounds__(WARPS * 32, 1) k_norm_join_grad(JoinArgs a, Jo
             if (dxo) {
                 const Pack<T, N> r = rows.get(2, t, c);
 #pragma unroll
-                for (int j = 0; j < N; ++j) v[i][j] = r.get(j);
+                for (int j = 0; j < kF; ++j) v[i][j] = r.get(j);
             } else {
 #pragma unroll
-                for (int j = 0; j < N; ++j) v[i][j] = 0.f;
+                for (int j = 0; j < kF; ++j) v[i][j] = both<F>(0.f);
             }
             if (dn) {
                 const Pack<T, N> r = rows.get(0, t, c), n = rows.get(3, t, c);
                 Pack<T, N> w;
                 w.load(wn + c);
 #pragma unroll
-                for (int j = 0; j < N; ++j) {
-                    v[i][j] += ix * (n.get(j) * w.get(j) - r.get(j) * along);
-                    s_pre[i][j] = fmaf(n.get(j) * ix, r.get(j), s_pre[i][j]);
+                for (int j = 0; j < kF; ++j) {
+                    const F x_ = r.get(j), n_ = mul_(n.get(j), ix);
+                    v[i][j] = fma_(x_, along, fma_(n_, w.get(j), v[i][j]));
+                    s_pre[i][j] = fma_(n_, x_, s_pre[i][j]);
                 }
             }
             Pack<T, N> o;
 #pragma unroll
-            for (int j = 0; j < N; ++j) o.set(j, a.rho * v[i][j]);
+            for (int j = 0; j < kF; ++j) o.set(j, mul_(rho, v[i][j]));
             o.store((T*)g.dx + at + c);
             if (y) {
-                const Pack<T, N> r = rows.get(1, t, c);
-                Pack<T, N> w, k;
-                w.load(wp + c);
-                if (gate) k.load(gate + seq.b * a.D + c);
+                ry[i] = rows.get(1, t, c);
 #pragma unroll
-                for (int j = 0; j < N; ++j) {
-                    u[i][j] = r.get(j) * iy;
-                    const float gu = v[i][j] * u[i][j], gk = gate ? k.get(j) : 1.f;
-                    s_gate[i][j] += gu;
-                    s_post[i][j] = fmaf(gk, gu, s_post[i][j]);
-                    v[i][j] *= gk * w.get(j);
-                    m = fmaf(v[i][j], u[i][j], m);
+                for (int j = 0; j < kF; ++j) {
+                    const F y_ = ry[i].get(j), gi = mul_(v[i][j], iy);
+                    s_gate[i][j] = fma_(gi, y_, s_gate[i][j]);
+                    v[i][j] = mul_(gi, gw[i][j]);
+                    m = fma_(v[i][j], y_, m);
                 }
             }
         }
         rows.leave(team, t, t1);
         if (!y) continue;
-        m = team.sum(make_float4(m, 0.f, 0.f, 0.f)).x * inv_d;
+        const F back = both<F>(-iy_ * iy_ * (team.sum(make_float4(total(m), 0.f, 0.f, 0.f)).x * inv_d));
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int c = col + i * step;
             if (c >= a.D) continue;
             Pack<T, N> o;
 #pragma unroll
-            for (int j = 0; j < N; ++j) o.set(j, iy * (v[i][j] - u[i][j] * m));
+            for (int j = 0; j < kF; ++j) o.set(j, fma_(ry[i].get(j), back, v[i][j]));
             o.store((T*)g.dy + at + c);
         }
     }
     rows.drain();
-    if (t0 < t1 && g.d_gate) flush();
+    if (t0 < t1 && y) flush();
     // the CTA's sums for the norms' weights, teams in order
     float* sums = reinterpret_cast<float*>(rings);
-    auto gather = [&](const float (&s)[NV][N], float* to) {
+    auto gather = [&](const F (&s)[NV][kF], float* to) {
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < NV; ++i)
 #pragma unroll
-            for (int j = 0; j < N; ++j)
-                if (col + i * step < a.D) sums[team.id * a.D + col + i * step + j] = s[i][j];
+            for (int j = 0; j < kF; ++j)
+                if (col + i * step < a.D)
+                    *reinterpret_cast<F*>(sums + team.id * a.D + col + i * step + j * (N / kF)) = s[i][j];
         __syncthreads();
         for (int c = threadIdx.x; c < a.D; c += WARPS * 32) {
             float v = 0.f;
@@ -479,57 +519,88 @@ __global__ void __launch_bounds__(WARPS * 32, 1) k_norm_join_grad(JoinArgs a, Jo
     if (dn) gather(s_pre, p.weights + ((int64_t)blockIdx.x * 2 + 1) * a.D);
 }
 
-// CTAs (32 columns each along y) of three kinds along x: 0 and 1 add the norms'
-// weights over the CTAs before; the next ones, one per team, add the partial sums
-// of a sequence that begins among the team's tokens and goes on; the rest clear
-// the gradients of empty sequences' gates.
+// CTAs (128 columns each along y) of three kinds along x: 0 and 1 add the norms'
+// weights over the CTAs before; the next ones, for eight teams each, add the
+// partial sums of sequences that begin among a team's tokens and go on (a warp
+// per team, or for long ones the CTA); the rest clear the gradients of empty
+// sequences' gates.
 constexpr int kClearRows = 256;
+constexpr int kWarpRows = 16;            // partial sums that a warp adds by itself
 
 template <class T>
 __global__ void __launch_bounds__(256) k_join_finish(JoinArgs a, JoinGrads g, GradPlan p) {
-    __shared__ float part[8][32];
+    __shared__ float part[8][128];
+    __shared__ int64_t long_last[8];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int c = blockIdx.y * 32 + lane;
+    const int c0 = blockIdx.y * 128;
     wait_before();
-    // sum over rows first + warp, first + warp + 8, ... <= last of p[row * stride + c]
-    auto column_sum = [&](const float* from, int64_t stride, int64_t first, int64_t last) {
-        float v = 0.f;
-        if (c < a.D)
+    // v[j] += sum over rows first, first + by, ... <= last of from[row * stride + c0 + 32 j + lane]
+    auto add_rows = [&](float (&v)[4], const float* from, int64_t stride, int64_t first, int64_t last, int by) {
 #pragma unroll 4
-            for (int64_t r = first + warp; r <= last; r += 8) v += __ldcg(from + r * stride + c);
-        part[warp][lane] = v;
-        __syncthreads();
-        v = 0.f;
-        for (int w = 0; w < 8; ++w) v += part[w][lane];
-        return v;
+        for (int64_t r = first; r <= last; r += by)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (c0 + j * 32 + lane < a.D) v[j] += __ldcg(from + r * stride + c0 + j * 32 + lane);
     };
+    // the same with rows spread over the CTA's warps: column threadIdx.x < 128
+    auto cta_rows = [&](const float* from, int64_t stride, int64_t first, int64_t last) {
+        float v[4] = {0.f, 0.f, 0.f, 0.f};
+        add_rows(v, from, stride, first + warp, last, 8);
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < 4; ++j) part[warp][j * 32 + lane] = v[j];
+        __syncthreads();
+        float sum = 0.f;
+        if (threadIdx.x < 128)
+            for (int w = 0; w < 8; ++w) sum += part[w][threadIdx.x];
+        return sum;
+    };
+    const int c = c0 + threadIdx.x;
     if (blockIdx.x < 2) {
         T* out = (T*)(blockIdx.x == 0 ? g.d_w_post : g.d_w_pre);
         if (!out) return;
-        const float v = column_sum(p.weights + blockIdx.x * a.D, 2 * a.D, 0, p.ctas - 1);
-        if (warp == 0 && c < a.D) out[c] = from_f32<T>(v);
+        const float v = cta_rows(p.weights + blockIdx.x * a.D, 2 * a.D, 0, p.ctas - 1);
+        if (threadIdx.x < 128 && c < a.D) out[c] = from_f32<T>(v);
         return;
     }
-    const int64_t k = (int64_t)blockIdx.x - 2;
-    if (k < p.teams) {
-        const int64_t t0 = k * p.chunk, t1 = t0 + p.chunk;
-        if (t1 >= a.T) return;
-        const int64_t b = sequence_of(a.offsets, a.B, t1 - 1);
-        const int64_t begin = a.offsets ? __ldg(a.offsets + b) : 0, end = a.offsets ? min(a.T, __ldg(a.offsets + b + 1)) : a.T;
-        if (begin < t0 || end <= t1) return;
-        const int64_t last = min(p.teams - 1, (end - 1) / p.chunk);
+    const int64_t group = (int64_t)blockIdx.x - 2, groups = (p.teams + 7) / 8;
+    const T* wp = (const T*)a.w_post;
+    if (group < groups) {
+        const int64_t k = group * 8 + warp, t0 = k * p.chunk, t1 = t0 + p.chunk;
+        int64_t last = -1, b = 0;
+        if (k < p.teams && t1 < a.T) {
+            b = sequence_of(a.offsets, a.B, t1 - 1);
+            const int64_t begin = a.offsets ? __ldg(a.offsets + b) : 0;
+            const int64_t end = a.offsets ? min(a.T, __ldg(a.offsets + b + 1)) : a.T;
+            if (begin >= t0 && end > t1) last = min(p.teams - 1, (end - 1) / p.chunk);
+        }
         // this team's second row, then the first row of those that follow
-        float v = column_sum(p.gates, 2 * a.D, k + 1, last);
-        if (warp == 0 && c < a.D) {
-            v = __ldcg(p.gates + (k * 2 + 1) * a.D + c) + v;
-            ((T*)g.d_gate)[b * a.D + c] = from_f32<T>(to_f32(((const T*)a.w_post)[c]) * v);
+        const bool alone = last - k <= kWarpRows;
+        if (lane == 0) long_last[warp] = alone ? -1 : last;
+        if (last >= 0 && alone) {
+            float v[4] = {0.f, 0.f, 0.f, 0.f};
+            add_rows(v, p.gates + a.D, 2 * a.D, k, k, 1);
+            add_rows(v, p.gates, 2 * a.D, k + 1, last, 1);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int e = c0 + j * 32 + lane;
+                if (e < a.D) ((T*)g.d_gate)[b * a.D + e] = from_f32<T>(to_f32(wp[e]) * v[j]);
+            }
+        }
+        __syncthreads();
+        for (int w = 0; w < 8; ++w) {
+            if (long_last[w] < 0) continue;
+            const int64_t kw = group * 8 + w, bw = sequence_of(a.offsets, a.B, kw * p.chunk + p.chunk - 1);
+            const float v = cta_rows(p.gates, 2 * a.D, kw + 1, long_last[w]);
+            if (threadIdx.x < 128 && c < a.D)
+                ((T*)g.d_gate)[bw * a.D + c] = from_f32<T>(to_f32(wp[c]) * (__ldcg(p.gates + (kw * 2 + 1) * a.D + c) + v));
         }
         return;
     }
-    if (c >= a.D) return;
-    const int64_t b0 = (k - p.teams) * kClearRows;
+    const int64_t b0 = (group - groups) * kClearRows;
     for (int64_t b = b0 + warp; b < min(a.B, b0 + kClearRows); b += 8)
-        if (__ldg(a.offsets + b) == __ldg(a.offsets + b + 1)) ((T*)g.d_gate)[b * a.D + c] = from_f32<T>(0.f);
+        if (__ldg(a.offsets + b) == __ldg(a.offsets + b + 1))
+            for (int e = c0 + lane; e < min(a.D, c0 + 128); e += 32) ((T*)g.d_gate)[b * a.D + e] = from_f32<T>(0.f);
 }
 
 // ---- host ------------------------------------------------------------------------
@@ -656,7 +727,7 @@ cudaError_t launch_norm_join_grad(const JoinArgs& a, const JoinGrads& g, uint8_t
         const int64_t teams = g.d_gate ? p.teams : 0, clears = g.d_gate && a.offsets ? (a.B + kClearRows - 1) / kClearRows : 0;
         GradPlan q = p;
         q.teams = teams;
-        return launch_kernel(k_join_finish<T>, dim3((unsigned)(2 + teams + clears), (unsigned)((a.D + 31) / 32)), dim3(256), 0,
+        return launch_kernel(k_join_finish<T>, dim3((unsigned)(2 + (teams + 7) / 8 + clears), (unsigned)((a.D + 127) / 128)), dim3(256), 0,
                              true, s, a, g, q);
     };
     auto of16 = [&](auto t) {
