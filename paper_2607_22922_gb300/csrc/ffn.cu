@@ -5,10 +5,11 @@
 //   dx = [dg du] W_in, dW_in = [dg du]^T x, dWo = dy^T h          (W_in = [Wg; Wu])
 //
 // k_hidden makes h with both projections in one accumulator tile (128 tokens x
-// 128 gate columns and the same 128 up columns), k_hidden_grad makes h, dg and
-// du from x and dy with three (g, u and dh all sum over D), so that nothing of
-// the hidden layer is kept from the forward call.  The other products are
-// k_product.  All are persistent: one CTA per SM takes tiles; a warp fills a
+// FT gate columns and the same FT up columns), k_hidden_grad makes h, dg and du
+// from x and dy with three (g, u and dh all sum over D), so that nothing of the
+// hidden layer is kept from the forward call.  k_products makes the other
+// products, those of the gradient in one launch.  All are persistent: a CTA, or
+// a pair of CTAs that share one MMA of 256 rows, takes tiles; a warp fills a
 // ring of operand stages by TMA, a warp issues the MMAs, the others turn
 // accumulators into 16-bit tiles in shared memory and store them by TMA.
 #include "umma.cuh"
@@ -17,11 +18,11 @@ namespace ifvs {
 
 namespace {
 
-constexpr uint32_t kRowTile = 128;                        // rows of an accumulator tile
-constexpr uint32_t kABytes = kRowTile * 128;              // a stage's A tile
-constexpr uint32_t kBBytes = 256 * 128;                   // a stage's B tile (up to 256 columns)
-constexpr uint32_t kStageBytes = kABytes + kBBytes;
+constexpr int kRows = 128;                                // rows of a CTA's accumulator tile
+constexpr uint32_t kABytes = kRows * 128;                 // a stage's A tile
 constexpr uint32_t kOutBytes = 32 * 128;                  // 32 rows x 64 columns of output
+constexpr int kMaxStages = 8;
+constexpr size_t kMaxSmem = 227 * 1024 - 512;             // beside the static shared memory
 
 // act(g) and act'(g)
 template <int ACT>
@@ -41,85 +42,86 @@ __device__ __forceinline__ void activation(float g, float& v, float& slope) {
 }
 
 // Barriers of a CTA: operand stages, accumulator slots, the last MMAs
-template <int S, int SLOTS>
+template <int S>
 struct Bars {
-    uint64_t full[S], empty[S], acc_full[SLOTS], acc_empty[SLOTS], drain;
+    uint64_t full[S], empty[S], acc_full[2], acc_empty[2], drain;
+    uint32_t tmem;
+    int dead;
 };
 
 // What every kernel here starts with; returns the TMEM base (512 columns).
-// Warps 0 .. EPI - 1: epilogue, EPI: TMA, EPI + 1: MMA.
-template <int EPI, int S, int SLOTS>
-__device__ __forceinline__ uint32_t setup(Bars<S, SLOTS>& b, uint32_t* tmem, int* dead) {
+// Warps 0 .. EPI - 1: epilogue, EPI: TMA, EPI + 1: MMA (of a pair the first CTA's).
+template <int CG, int EPI, int S>
+__device__ __forceinline__ uint32_t setup(Bars<S>& b) {
     if (threadIdx.x == 0) {
         for (int i = 0; i < S; ++i) {
             mbar_init(smem_addr(&b.full[i]), 1);
             mbar_init(smem_addr(&b.empty[i]), 1);
         }
-        for (int i = 0; i < SLOTS; ++i) {
+        for (int i = 0; i < 2; ++i) {
             mbar_init(smem_addr(&b.acc_full[i]), 1);
-            mbar_init(smem_addr(&b.acc_empty[i]), EPI);
+            mbar_init(smem_addr(&b.acc_empty[i]), EPI * CG);
         }
         mbar_init(smem_addr(&b.drain), 1);
-        *dead = 0;
+        b.dead = 0;
         fence_mbar_init();
     }
-    if (threadIdx.x / 32 == EPI + 1) {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_addr(tmem)) : "memory");
-        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
-    }
+    if (threadIdx.x / 32 == EPI + 1) tmem_alloc<CG>(smem_addr(&b.tmem), 512);
     fence_before_sync();
     __syncthreads();
+    if constexpr (CG == 2) pair_sync();      // the other CTA's barriers are there
     fence_after_sync();
-    return *tmem;
+    return b.tmem;
 }
 
 // The end of a kernel: with everything in order the roles have waited for
 // their own work; a dead CTA waits here for what it had in flight.
-template <int EPI, int S, int SLOTS>
-__device__ __forceinline__ void finish(Bars<S, SLOTS>& b, uint32_t tmem, const int* dead, int filled) {
+template <int CG, int EPI, int S>
+__device__ __forceinline__ void finish(Bars<S>& b, uint32_t tmem, int filled, bool issues) {
     __syncwarp();
     __syncthreads();
-    if (*(volatile const int*)dead) {
+    if (*(volatile int*)&b.dead) {
         auto bounded = [](uint32_t bar, uint32_t parity) {
             const long long t0 = clock64();
             while (!mbar_try_wait(bar, parity) && clock64() - t0 < kWaitCycles) {
             }
         };
-        if (threadIdx.x == EPI * 32)
+        if (threadIdx.x == EPI * 32 && issues)
             for (int i = max(0, filled - S); i < filled; ++i) bounded(smem_addr(&b.full[i % S]), (uint32_t)(i / S) & 1u);
-        if (threadIdx.x == EPI * 32 + 32) {
-            mma_commit(smem_addr(&b.drain));
+        if (threadIdx.x == EPI * 32 + 32 && issues) {
+            mma_commit<CG>(smem_addr(&b.drain));
             bounded(smem_addr(&b.drain), 0);
         }
+        __syncwarp();
         __syncthreads();
     }
-    if (threadIdx.x / 32 == EPI + 1)
-        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem));
+    if constexpr (CG == 2) pair_sync();      // nothing of the pair uses this CTA's memory any more
+    if (threadIdx.x / 32 == EPI + 1) tmem_free<CG>(tmem, 512);
 }
 
 // K-major tiles: `rows` rows from `row`; MN-major: `rows` columns from `row`.
 // k: the first of the stage's 64 along the sum.
-template <bool MN>
-__device__ __forceinline__ void load_tile(uint32_t dst, const CUtensorMap* map, int row, int rows, int k, uint32_t bar) {
-    if (MN) {
+template <int CG>
+__device__ __forceinline__ void load_tile(bool mn_major, uint32_t dst, const CUtensorMap* map, int row, int rows, int k,
+                                          uint32_t bar) {
+    if (mn_major) {
 #pragma unroll 1
-        for (int i = 0; i < rows; i += 64) tma_load(dst + (uint32_t)i * 128u, map, row + i, k, bar);
+        for (int i = 0; i < rows; i += 64) tma_load<CG>(dst + (uint32_t)i * 128u, map, row + i, k, bar);
     } else {
-        tma_load(dst, map, k, row, bar);
+        tma_load<CG>(dst, map, k, row, bar);
     }
 }
 
 // the four MMAs of a stage
-template <bool A_MN, bool B_MN>
-__device__ __forceinline__ void mma_stage(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, bool first) {
-    const uint64_t da = tile_desc(a, A_MN), db = tile_desc(b, B_MN);
+template <int CG>
+__device__ __forceinline__ void mma_stage(uint32_t d, uint32_t a, uint32_t b, bool a_mn, bool b_mn, uint32_t idesc, bool first) {
+    const uint64_t da = tile_desc(a, a_mn), db = tile_desc(b, b_mn), sa = desc_step(a_mn), sb = desc_step(b_mn);
 #pragma unroll
-    for (uint32_t i = 0; i < kStepK / 16; ++i)
-        mma_f16(d, da + i * desc_step(A_MN), db + i * desc_step(B_MN), idesc, !first || i > 0);
+    for (uint32_t i = 0; i < kStepK / 16; ++i) mma_f16<CG>(d, da + i * sa, db + i * sb, idesc, !first || i > 0);
 }
 
-// This warp's 32 rows x 64 columns of 16-bit output: `words` packed pairs go to
-// the staging tile (swizzled), a TMA store takes it.  BUFS tiles per warp.
+// This warp's 32 rows x 64 columns of 16-bit output: packed pairs go to the
+// staging tile (swizzled), a TMA store takes it.  BUFS tiles per warp.
 template <int BUFS>
 struct OutTile {
     uint32_t base;      // of this warp's staging tiles
@@ -147,8 +149,8 @@ struct OutTile {
 };
 
 struct Grid {
-    int m_tiles, n_tiles, k_steps;
-    int rows, cols;      // of the output
+    int m_tiles, n_tiles, k_steps;     // m_tiles of CG x 128 rows
+    int rows, cols;                    // of the output
 };
 
 __device__ __forceinline__ uint32_t dynamic_smem() {
@@ -156,23 +158,69 @@ __device__ __forceinline__ uint32_t dynamic_smem() {
     return (smem_addr(raw) + 1023u) & ~1023u;
 }
 
-// ---- C = A B^T in 16 bits ----------------------------------------------------------
-// A K-major [rows][K] or MN-major [K][rows]; B the same with `cols`.
-constexpr int kProductStages = 4;
+// stages that fit beside the staging tiles
+constexpr int stages_of(uint32_t stage_bytes, uint32_t out_bytes) {
+    const int n = (int)((kMaxSmem - 1024 - out_bytes) / stage_bytes);
+    return n < kMaxStages ? n : kMaxStages;
+}
+constexpr size_t smem_of(uint32_t stage_bytes, uint32_t out_bytes) {
+    return 1024 + (size_t)stages_of(stage_bytes, out_bytes) * stage_bytes + out_bytes;
+}
 
-template <bool A_MN, bool B_MN, int BN>
-__global__ void __launch_bounds__(192, 1)
-k_product(const __grid_constant__ CUtensorMap ma, const __grid_constant__ CUtensorMap mb,
-          const __grid_constant__ CUtensorMap mc, Grid g, bool f16, int* err) {
-    constexpr int EPI = 4, S = kProductStages;
-    __shared__ __align__(8) Bars<S, 2> bars;
-    __shared__ uint32_t tmem_slot;
-    __shared__ int dead;
-    const uint32_t ring = dynamic_smem(), out = ring + S * kStageBytes;
+// ---- products C = A B^T in 16 bits ---------------------------------------------------
+// A K-major [rows][K] or MN-major [K][rows]; B the same with `cols`.  Up to three
+// products in one launch, items (tiles, or parts of a tile's sum) in their order.
+struct Product {
+    CUtensorMap a, b, c;
+    Grid g;
+    int splits;          // parts of the sum; more than one: float32 parts in `parts`, added by k_join_parts
+    int items;           // tiles x splits
+    bool a_mn, b_mn;
+    float* parts;        // [splits][rows][cols]
+};
+struct Products {
+    Product p[3];
+    int n, items;
+};
+
+template <int CG, int BN>
+struct ProductShape {
+    static constexpr uint32_t kB = BN / CG * 128, kStage = kABytes + kB, kOut = 4 * 2 * kOutBytes;
+    static constexpr int kStages = stages_of(kStage, kOut);
+    static constexpr size_t kSmem = smem_of(kStage, kOut);
+};
+
+struct Item {
+    const Product* p;
+    int m, n, split, k0, k1;
+};
+__device__ __forceinline__ Item item_of(const Products& all, int i) {
+    int j = 0;
+    while (j + 1 < all.n && i >= all.p[j].items) i -= all.p[j++].items;
+    Item t;
+    t.p = &all.p[j];
+    const Grid& g = t.p->g;
+    const int tile = i / t.p->splits;
+    t.split = i - tile * t.p->splits;
+    const int2 mn = tile_of(tile, g.m_tiles, g.n_tiles);
+    t.m = mn.x;
+    t.n = mn.y;
+    t.k0 = (int)((int64_t)g.k_steps * t.split / t.p->splits);
+    t.k1 = (int)((int64_t)g.k_steps * (t.split + 1) / t.p->splits);
+    return t;
+}
+
+template <int CG, int BN>
+__global__ void __launch_bounds__(192, 1) k_products(const __grid_constant__ Products all, bool f16, int* err) {
+    using Sh = ProductShape<CG, BN>;
+    constexpr int EPI = 4, S = Sh::kStages;
+    __shared__ __align__(8) Bars<S> bars;
+    const uint32_t ring = dynamic_smem(), out = ring + S * Sh::kStage;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const uint32_t tmem = setup<EPI>(bars, &tmem_slot, &dead);
-    const Watch w{&dead, err};
-    const int tiles = g.m_tiles * g.n_tiles;
+    const int rank = CG == 2 ? (int)cluster_rank() : 0;
+    const uint32_t tmem = setup<CG, EPI>(bars);
+    const Watch w{&bars.dead, err};
+    const int first = blockIdx.x / CG, step = gridDim.x / CG;
     int filled = 0;
     wait_before();
 
@@ -180,58 +228,74 @@ k_product(const __grid_constant__ CUtensorMap ma, const __grid_constant__ CUtens
         if (lane == 0) {
             Ring<S> r;
             bool ok = true;
-            for (int t = blockIdx.x; t < tiles && ok; t += gridDim.x) {
-                const int2 mn = tile_of(t, g.m_tiles, g.n_tiles);
-                for (int k = 0; k < g.k_steps; ++k, r.next(), ++filled) {
+            for (int i = first; i < all.items && ok; i += step) {
+                const Item t = item_of(all, i);
+                const bool a_mn = t.p->a_mn, b_mn = t.p->b_mn;
+                const int row = (t.m * CG + rank) * kRows, col = t.n * BN + rank * (BN / CG);
+                for (int k = t.k0; k < t.k1; ++k, r.next(), ++filled) {
                     if (!(ok = w.wait(smem_addr(&bars.empty[r.at]), r.parity ^ 1u))) break;
-                    const uint32_t a = ring + r.at * kStageBytes, bar = smem_addr(&bars.full[r.at]);
-                    mbar_arrive_expect_tx(bar, kABytes + BN * 128);
-                    load_tile<A_MN>(a, &ma, mn.x * kRowTile, kRowTile, k * kStepK, bar);
-                    load_tile<B_MN>(a + kABytes, &mb, mn.y * BN, BN, k * kStepK, bar);
+                    const uint32_t a = ring + r.at * Sh::kStage, bar = smem_addr(&bars.full[r.at]);
+                    if (rank == 0) mbar_arrive_expect_tx(bar, CG * Sh::kStage);
+                    load_tile<CG>(a_mn, a, &t.p->a, row, kRows, k * kStepK, bar);
+                    load_tile<CG>(b_mn, a + kABytes, &t.p->b, col, BN / CG, k * kStepK, bar);
                 }
             }
             start_dependents();
         }
     } else if (warp == EPI + 1) {
-        if (lane == 0) {
-            const uint32_t idesc = mma_desc(BN, f16, A_MN, B_MN);
+        if (lane == 0 && rank == 0) {
             Ring<S> r;
             Ring<2> acc;
             bool ok = true;
-            for (int t = blockIdx.x; t < tiles && ok; t += gridDim.x, acc.next()) {
+            for (int i = first; i < all.items && ok; i += step, acc.next()) {
+                const Item t = item_of(all, i);
+                const bool a_mn = t.p->a_mn, b_mn = t.p->b_mn;
+                const uint32_t idesc = mma_desc(CG * kRows, BN, f16, a_mn, b_mn);
                 if (!(ok = w.wait(smem_addr(&bars.acc_empty[acc.at]), acc.parity ^ 1u))) break;
                 fence_after_sync();
-                for (int k = 0; k < g.k_steps; ++k, r.next()) {
+                for (int k = t.k0; k < t.k1; ++k, r.next()) {
                     if (!(ok = w.wait(smem_addr(&bars.full[r.at]), r.parity))) break;
                     fence_after_sync();
-                    const uint32_t a = ring + r.at * kStageBytes;
-                    mma_stage<A_MN, B_MN>(tmem + acc.at * 256, a, a + kABytes, idesc, k == 0);
-                    mma_commit(smem_addr(&bars.empty[r.at]));
+                    const uint32_t a = ring + r.at * Sh::kStage;
+                    mma_stage<CG>(tmem + acc.at * 256, a, a + kABytes, a_mn, b_mn, idesc, k == t.k0);
+                    mma_commit<CG>(smem_addr(&bars.empty[r.at]));
                 }
-                mma_commit(smem_addr(&bars.acc_full[acc.at]));
+                mma_commit<CG>(smem_addr(&bars.acc_full[acc.at]));
             }
         }
     } else {
         OutTile<2> o{out + (uint32_t)warp * 2 * kOutBytes};
         Ring<2> acc;
-        for (int t = blockIdx.x; t < tiles; t += gridDim.x, acc.next()) {
-            const int2 mn = tile_of(t, g.m_tiles, g.n_tiles);
-            const int row = mn.x * (int)kRowTile + warp * 32;
+        for (int i = first; i < all.items; i += step, acc.next()) {
+            const Item t = item_of(all, i);
+            const Grid& g = t.p->g;
+            const int row = (t.m * CG + rank) * kRows + warp * 32;
             if (!__all_sync(0xFFFFFFFFu, w.wait(smem_addr(&bars.acc_full[acc.at]), acc.parity))) break;
             fence_after_sync();
             const uint32_t tm = tmem + acc.at * 256 + ((uint32_t)warp << 21);
 #pragma unroll 1
             for (int c = 0; c < BN; c += 64) {
+                const int col = t.n * BN + c;
                 float v[2][32];
                 tmem_ld32(tm + c, v[0]);
                 tmem_ld32(tm + c + 32, v[1]);
-                o.begin(lane);
+                if (t.p->splits == 1) o.begin(lane);
                 tmem_wait(v[0]);
                 tmem_wait(v[1]);
                 if (c + 64 == BN) {
                     fence_before_sync();
                     __syncwarp();
-                    if (lane == 0) mbar_arrive(smem_addr(&bars.acc_empty[acc.at]));
+                    if (lane == 0) mbar_arrive<CG>(smem_addr(&bars.acc_empty[acc.at]));
+                }
+                if (t.p->splits > 1) {
+                    if (row + lane < g.rows) {
+                        float* to = t.p->parts + ((int64_t)t.split * g.rows + row + lane) * g.cols + col;
+#pragma unroll
+                        for (int j = 0; j < 64; j += 4)      // columns are a multiple of 8
+                            if (col + j < g.cols)
+                                *reinterpret_cast<float4*>(to + j) = *reinterpret_cast<float4*>(&v[j >> 5][j & 31]);
+                    }
+                    continue;
                 }
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
@@ -239,91 +303,132 @@ k_product(const __grid_constant__ CUtensorMap ma, const __grid_constant__ CUtens
                     o.put(lane, j, pack16(q[0], q[1], f16), pack16(q[2], q[3], f16), pack16(q[4], q[5], f16),
                           pack16(q[6], q[7], f16));
                 }
-                const int col = mn.y * BN + c;
-                o.store(lane, &mc, col, row, row < g.rows && col < g.cols);
+                o.store(lane, &t.p->c, col, row, row < g.rows && col < g.cols);
             }
         }
         if (lane == 0) tma_wait_all();
     }
-    finish<EPI>(bars, tmem, &dead, filled);
+    finish<CG, EPI>(bars, tmem, filled, rank == 0);
+}
+
+// C = the sum of the parts, in order; up to three products
+struct Parts {
+    const float* parts[3];
+    void* c[3];
+    int64_t n[3];        // values, a multiple of 8
+    int splits[3];
+};
+template <class T>
+__global__ void __launch_bounds__(256) k_join_parts(Parts p) {
+    wait_before();
+    const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
+    const int j = blockIdx.y;
+    if (i >= p.n[j]) return;
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+    for (int s = 0; s < p.splits[j]; ++s) {
+        const float4 q = __ldcg(reinterpret_cast<const float4*>(p.parts[j] + s * p.n[j] + i));
+        v.x += q.x;
+        v.y += q.y;
+        v.z += q.z;
+        v.w += q.w;
+    }
+    *reinterpret_cast<uint2*>((T*)p.c[j] + i) = make_uint2(pack2(make_float2(v.x, v.y), T()), pack2(make_float2(v.z, v.w), T()));
 }
 
 // ---- h = act(x Wg^T) * (x Wu^T) ------------------------------------------------------
-constexpr int kHiddenEpi = 8;
+// FT hidden columns per tile: gate rows and up rows of W_in side by side in B.  In
+// a pair the first CTA holds the gate's rows, the second the up projection's.
+template <int CG, int FT>
+struct HiddenShape {
+    static constexpr int kEpi = FT / 16;                 // a warp: 32 rows x 64 columns
+    static constexpr uint32_t kStage = kABytes + 2 * FT / CG * 128, kOut = kEpi * kOutBytes;
+    static constexpr int kStages = stages_of(kStage, kOut);
+    static constexpr size_t kSmem = smem_of(kStage, kOut);
+};
 
-template <int ACT>
-__global__ void __launch_bounds__(kHiddenEpi * 32 + 64, 1)
+template <int CG, int FT>
+__device__ __forceinline__ void load_projections(uint32_t dst, const CUtensorMap* mw, int f, int F, int k, int rank, uint32_t bar) {
+    if constexpr (CG == 1) {
+        tma_load<CG>(dst, mw, k, f, bar);
+        tma_load<CG>(dst + FT * 128, mw, k, F + f, bar);
+    } else {
+        tma_load<CG>(dst, mw, k, rank * F + f, bar);
+    }
+}
+
+template <int ACT, int CG, int FT>
+__global__ void __launch_bounds__(HiddenShape<CG, FT>::kEpi * 32 + 64, 1)
 k_hidden(const __grid_constant__ CUtensorMap mx, const __grid_constant__ CUtensorMap mw,
          const __grid_constant__ CUtensorMap mh, Grid g, bool f16, int* err) {
-    constexpr int EPI = kHiddenEpi, S = 4;
-    __shared__ __align__(8) Bars<S, 2> bars;
-    __shared__ uint32_t tmem_slot;
-    __shared__ int dead;
-    const uint32_t ring = dynamic_smem(), out = ring + S * kStageBytes;
+    using Sh = HiddenShape<CG, FT>;
+    constexpr int EPI = Sh::kEpi, S = Sh::kStages;
+    __shared__ __align__(8) Bars<S> bars;
+    const uint32_t ring = dynamic_smem(), out = ring + S * Sh::kStage;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const uint32_t tmem = setup<EPI>(bars, &tmem_slot, &dead);
-    const Watch w{&dead, err};
-    const int tiles = g.m_tiles * g.n_tiles;
+    const int rank = CG == 2 ? (int)cluster_rank() : 0;
+    const uint32_t tmem = setup<CG, EPI>(bars);
+    const Watch w{&bars.dead, err};
+    const int tiles = g.m_tiles * g.n_tiles, first = blockIdx.x / CG, step = gridDim.x / CG;
     int filled = 0;
 
     if (warp == EPI) {
         if (lane == 0) {
             Ring<S> r;
             bool ok = true;
-            for (int t = blockIdx.x; t < tiles && ok; t += gridDim.x) {
+            for (int t = first; t < tiles && ok; t += step) {
                 const int2 mn = tile_of(t, g.m_tiles, g.n_tiles);
                 for (int k = 0; k < g.k_steps; ++k, r.next(), ++filled) {
                     if (!(ok = w.wait(smem_addr(&bars.empty[r.at]), r.parity ^ 1u))) break;
-                    const uint32_t a = ring + r.at * kStageBytes, bar = smem_addr(&bars.full[r.at]);
-                    mbar_arrive_expect_tx(bar, kStageBytes);
-                    tma_load(a, &mx, k * kStepK, mn.x * kRowTile, bar);
-                    tma_load(a + kABytes, &mw, k * kStepK, mn.y * 128, bar);
-                    tma_load(a + kABytes + kBBytes / 2, &mw, k * kStepK, g.cols + mn.y * 128, bar);
+                    const uint32_t a = ring + r.at * Sh::kStage, bar = smem_addr(&bars.full[r.at]);
+                    if (rank == 0) mbar_arrive_expect_tx(bar, CG * Sh::kStage);
+                    tma_load<CG>(a, &mx, k * kStepK, (mn.x * CG + rank) * kRows, bar);
+                    load_projections<CG, FT>(a + kABytes, &mw, mn.y * FT, g.cols, k * kStepK, rank, bar);
                 }
             }
             start_dependents();
         }
     } else if (warp == EPI + 1) {
-        if (lane == 0) {
-            const uint32_t idesc = mma_desc(256, f16, false, false);
+        if (lane == 0 && rank == 0) {
+            const uint32_t idesc = mma_desc(CG * kRows, 2 * FT, f16, false, false);
             Ring<S> r;
             Ring<2> acc;
             bool ok = true;
-            for (int t = blockIdx.x; t < tiles && ok; t += gridDim.x, acc.next()) {
+            for (int t = first; t < tiles && ok; t += step, acc.next()) {
                 if (!(ok = w.wait(smem_addr(&bars.acc_empty[acc.at]), acc.parity ^ 1u))) break;
                 fence_after_sync();
                 for (int k = 0; k < g.k_steps; ++k, r.next()) {
                     if (!(ok = w.wait(smem_addr(&bars.full[r.at]), r.parity))) break;
                     fence_after_sync();
-                    const uint32_t a = ring + r.at * kStageBytes;
-                    mma_stage<false, false>(tmem + acc.at * 256, a, a + kABytes, idesc, k == 0);
-                    mma_commit(smem_addr(&bars.empty[r.at]));
+                    const uint32_t a = ring + r.at * Sh::kStage;
+                    mma_stage<CG>(tmem + acc.at * 256, a, a + kABytes, false, false, idesc, k == 0);
+                    mma_commit<CG>(smem_addr(&bars.empty[r.at]));
                 }
-                mma_commit(smem_addr(&bars.acc_full[acc.at]));
+                mma_commit<CG>(smem_addr(&bars.acc_full[acc.at]));
             }
         }
     } else {
         OutTile<1> o{out + (uint32_t)warp * kOutBytes};
-        const int quad = warp & 3, half = (warp >> 2) * 64;
+        const int quad = warp & 3, part = (warp >> 2) * 64;
         Ring<2> acc;
-        for (int t = blockIdx.x; t < tiles; t += gridDim.x, acc.next()) {
+        for (int t = first; t < tiles; t += step, acc.next()) {
             const int2 mn = tile_of(t, g.m_tiles, g.n_tiles);
-            const int row = mn.x * (int)kRowTile + quad * 32, col = mn.y * 128 + half;
+            const int row = (mn.x * CG + rank) * kRows + quad * 32, col = mn.y * FT + part;
             if (!__all_sync(0xFFFFFFFFu, w.wait(smem_addr(&bars.acc_full[acc.at]), acc.parity))) break;
             fence_after_sync();
-            const uint32_t tm = tmem + acc.at * 256 + half + ((uint32_t)quad << 21);
+            const uint32_t tm = tmem + acc.at * 256 + part + ((uint32_t)quad << 21);
             o.begin(lane);
 #pragma unroll 1
             for (int c = 0; c < 64; c += 32) {
                 float a[32], u[32];
                 tmem_ld32(tm + c, a);
-                tmem_ld32(tm + 128 + c, u);
+                tmem_ld32(tm + FT + c, u);
                 tmem_wait(a);
                 tmem_wait(u);
                 if (c == 32) {
                     fence_before_sync();
                     __syncwarp();
-                    if (lane == 0) mbar_arrive(smem_addr(&bars.acc_empty[acc.at]));
+                    if (lane == 0) mbar_arrive<CG>(smem_addr(&bars.acc_empty[acc.at]));
                 }
 #pragma unroll
                 for (int j = 0; j < 32; ++j) {
@@ -340,102 +445,110 @@ k_hidden(const __grid_constant__ CUtensorMap mx, const __grid_constant__ CUtenso
         }
         if (lane == 0) tma_wait_all();
     }
-    finish<EPI>(bars, tmem, &dead, filled);
+    finish<CG, EPI>(bars, tmem, filled, rank == 0);
 }
 
 // ---- h, dg, du from x and dy ---------------------------------------------------------
-// Per tile first dh = dy Wo (128 columns), then g and u (256).  TMEM: g | u at
-// columns 128 .. 383; dh in the first or the last 128 by turns, so that the next
-// tile's dh accumulates while this tile's values are read.
-constexpr int kGradStages = 3;
+// Per tile first dh = dy Wo (FT columns), then g and u (2 FT).  TMEM: g | u in
+// columns FT .. 3 FT - 1; dh in the first FT or from 3 FT by turns, so that the
+// next tile's dh accumulates while this tile's values are read.
+template <int CG, int FT>
+struct GradShape {
+    static constexpr int kEpi = FT / 16;
+    static constexpr uint32_t kStage = kABytes + 2 * FT / CG * 128, kOut = kEpi * 2 * kOutBytes;
+    static constexpr uint32_t kDhBytes = kABytes + FT / CG * 128;      // of a stage of dh
+    static constexpr int kStages = stages_of(kStage, kOut);
+    static constexpr size_t kSmem = smem_of(kStage, kOut);
+};
 
-template <int ACT>
-__global__ void __launch_bounds__(kHiddenEpi * 32 + 64, 1)
+template <int ACT, int CG, int FT>
+__global__ void __launch_bounds__(GradShape<CG, FT>::kEpi * 32 + 64, 1)
 k_hidden_grad(const __grid_constant__ CUtensorMap mx, const __grid_constant__ CUtensorMap mdy,
               const __grid_constant__ CUtensorMap mw, const __grid_constant__ CUtensorMap mwo,
               const __grid_constant__ CUtensorMap mh, const __grid_constant__ CUtensorMap mdg,
               const __grid_constant__ CUtensorMap mdu, Grid g, bool f16, int* err) {
-    constexpr int EPI = kHiddenEpi, S = kGradStages;
-    __shared__ __align__(8) Bars<S, 2> bars;     // slot 0: g | u, slot 1: dh (both places)
-    __shared__ uint32_t tmem_slot;
-    __shared__ int dead;
-    const uint32_t ring = dynamic_smem(), out = ring + S * kStageBytes;
+    using Sh = GradShape<CG, FT>;
+    constexpr int EPI = Sh::kEpi, S = Sh::kStages;
+    __shared__ __align__(8) Bars<S> bars;     // slot 0: g | u, slot 1: dh (both places)
+    const uint32_t ring = dynamic_smem(), out = ring + S * Sh::kStage;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const uint32_t tmem = setup<EPI>(bars, &tmem_slot, &dead);
-    const Watch w{&dead, err};
-    const int tiles = g.m_tiles * g.n_tiles;
+    const int rank = CG == 2 ? (int)cluster_rank() : 0;
+    const uint32_t tmem = setup<CG, EPI>(bars);
+    const Watch w{&bars.dead, err};
+    const int tiles = g.m_tiles * g.n_tiles, first = blockIdx.x / CG, step = gridDim.x / CG;
     int filled = 0;
 
     if (warp == EPI) {
         if (lane == 0) {
             Ring<S> r;
             bool ok = true;
-            for (int t = blockIdx.x; t < tiles && ok; t += gridDim.x) {
+            for (int t = first; t < tiles && ok; t += step) {
                 const int2 mn = tile_of(t, g.m_tiles, g.n_tiles);
+                const int row = (mn.x * CG + rank) * kRows;
                 for (int k = 0; k < 2 * g.k_steps; ++k, r.next(), ++filled) {
                     if (!(ok = w.wait(smem_addr(&bars.empty[r.at]), r.parity ^ 1u))) break;
-                    const uint32_t a = ring + r.at * kStageBytes, bar = smem_addr(&bars.full[r.at]);
+                    const uint32_t a = ring + r.at * Sh::kStage, bar = smem_addr(&bars.full[r.at]);
                     if (k < g.k_steps) {
-                        mbar_arrive_expect_tx(bar, kABytes + kBBytes / 2);
-                        tma_load(a, &mdy, k * kStepK, mn.x * kRowTile, bar);
-                        load_tile<true>(a + kABytes, &mwo, mn.y * 128, 128, k * kStepK, bar);
+                        if (rank == 0) mbar_arrive_expect_tx(bar, CG * Sh::kDhBytes);
+                        tma_load<CG>(a, &mdy, k * kStepK, row, bar);
+                        load_tile<CG>(true, a + kABytes, &mwo, mn.y * FT + rank * (FT / CG), FT / CG, k * kStepK, bar);
                     } else {
                         const int kk = (k - g.k_steps) * kStepK;
-                        mbar_arrive_expect_tx(bar, kStageBytes);
-                        tma_load(a, &mx, kk, mn.x * kRowTile, bar);
-                        tma_load(a + kABytes, &mw, kk, mn.y * 128, bar);
-                        tma_load(a + kABytes + kBBytes / 2, &mw, kk, g.cols + mn.y * 128, bar);
+                        if (rank == 0) mbar_arrive_expect_tx(bar, CG * Sh::kStage);
+                        tma_load<CG>(a, &mx, kk, row, bar);
+                        load_projections<CG, FT>(a + kABytes, &mw, mn.y * FT, g.cols, kk, rank, bar);
                     }
                 }
             }
             start_dependents();
         }
     } else if (warp == EPI + 1) {
-        if (lane == 0) {
-            const uint32_t id_gu = mma_desc(256, f16, false, false), id_dh = mma_desc(128, f16, false, true);
+        if (lane == 0 && rank == 0) {
+            const uint32_t id_gu = mma_desc(CG * kRows, 2 * FT, f16, false, false);
+            const uint32_t id_dh = mma_desc(CG * kRows, FT, f16, false, true);
             Ring<S> r;
             uint32_t parity = 0;
             int turn = 0;
             bool ok = true;
-            for (int t = blockIdx.x; t < tiles && ok; t += gridDim.x, ++turn, parity ^= 1u) {
+            for (int t = first; t < tiles && ok; t += step, ++turn, parity ^= 1u) {
                 // dh's place was read two tiles ago, before the g | u of the last tile
                 for (int k = 0; k < 2 * g.k_steps; ++k, r.next()) {
                     if (k == g.k_steps) {
-                        mma_commit(smem_addr(&bars.acc_full[1]));
+                        mma_commit<CG>(smem_addr(&bars.acc_full[1]));
                         if (!(ok = w.wait(smem_addr(&bars.acc_empty[0]), parity ^ 1u))) break;
                         fence_after_sync();
                     }
                     if (!(ok = w.wait(smem_addr(&bars.full[r.at]), r.parity))) break;
                     fence_after_sync();
-                    const uint32_t a = ring + r.at * kStageBytes;
+                    const uint32_t a = ring + r.at * Sh::kStage;
                     if (k < g.k_steps)
-                        mma_stage<false, true>(tmem + (turn & 1 ? 384 : 0), a, a + kABytes, id_dh, k == 0);
+                        mma_stage<CG>(tmem + (turn & 1 ? 3 * FT : 0), a, a + kABytes, false, true, id_dh, k == 0);
                     else
-                        mma_stage<false, false>(tmem + 128, a, a + kABytes, id_gu, k == g.k_steps);
-                    mma_commit(smem_addr(&bars.empty[r.at]));
+                        mma_stage<CG>(tmem + FT, a, a + kABytes, false, false, id_gu, k == g.k_steps);
+                    mma_commit<CG>(smem_addr(&bars.empty[r.at]));
                 }
-                mma_commit(smem_addr(&bars.acc_full[0]));
+                mma_commit<CG>(smem_addr(&bars.acc_full[0]));
             }
         }
     } else {
         OutTile<2> o{out + (uint32_t)warp * 2 * kOutBytes};
-        const int quad = warp & 3, half = (warp >> 2) * 64;
+        const int quad = warp & 3, part = (warp >> 2) * 64;
         uint32_t parity = 0;
         int turn = 0;
-        for (int t = blockIdx.x; t < tiles; t += gridDim.x, ++turn, parity ^= 1u) {
+        for (int t = first; t < tiles; t += step, ++turn, parity ^= 1u) {
             const int2 mn = tile_of(t, g.m_tiles, g.n_tiles);
-            const int row = mn.x * (int)kRowTile + quad * 32, col = mn.y * 128 + half;
+            const int row = (mn.x * CG + rank) * kRows + quad * 32, col = mn.y * FT + part;
             const bool in = row < g.rows && col < g.cols;
             // g | u come after dh in the order of the MMAs
             if (!__all_sync(0xFFFFFFFFu, w.wait(smem_addr(&bars.acc_full[0]), parity))) break;
             fence_after_sync();
-            const uint32_t tm = tmem + half + ((uint32_t)quad << 21), td = tm + (turn & 1 ? 384 : 0);
+            const uint32_t tm = tmem + part + ((uint32_t)quad << 21), td = tm + (turn & 1 ? 3 * FT : 0);
             uint32_t h[32], dg[32], du[32];
 #pragma unroll
             for (int c = 0; c < 64; c += 32) {
                 float a[32], u[32], d[32];
-                tmem_ld32(tm + 128 + c, a);
-                tmem_ld32(tm + 256 + c, u);
+                tmem_ld32(tm + FT + c, a);
+                tmem_ld32(tm + 2 * FT + c, u);
                 tmem_ld32(td + c, d);
                 tmem_wait(a);
                 tmem_wait(u);
@@ -443,7 +556,7 @@ k_hidden_grad(const __grid_constant__ CUtensorMap mx, const __grid_constant__ CU
                 if (c == 32) {
                     fence_before_sync();
                     __syncwarp();
-                    if (lane == 0) mbar_arrive(smem_addr(&bars.acc_empty[0]));
+                    if (lane == 0) mbar_arrive<CG>(smem_addr(&bars.acc_empty[0]));
                 }
 #pragma unroll
                 for (int j = 0; j < 32; j += 2) {
@@ -467,37 +580,95 @@ k_hidden_grad(const __grid_constant__ CUtensorMap mx, const __grid_constant__ CU
         }
         if (lane == 0) tma_wait_all();
     }
-    finish<EPI>(bars, tmem, &dead, filled);
+    finish<CG, EPI>(bars, tmem, filled, rank == 0);
+}
+
+// ---- a few tokens ----------------------------------------------------------------------
+// Up to kFewTokens tokens: the weights are read once and bound the call, and a
+// tile of 128 tokens would leave most SMs without one.  A row of weights (PAIR:
+// the gate's row and the up projection's) is spread over the lanes of one or
+// more warps, 16 bytes a lane and access, against every token's row.
+constexpr int kFewTokens = 16;
+
+template <class T>
+struct FewArgs {
+    const T *x, *w;      // x [tokens][K], w [rows][K] (PAIR: [2 rows][K])
+    T* out;              // [tokens][rows]
+    int tokens, rows, K;
+    int cta_rows;        // rows per CTA of 8 warps: 8 / cta_rows warps share one
+};
+
+template <class T, bool PAIR, int ACT, int TT>
+__global__ void __launch_bounds__(256) k_few(FewArgs<T> a) {
+    constexpr int NW = PAIR ? 2 : 1, AHEAD = 4;
+    __shared__ float sums[8][NW * TT];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int share = 8 / a.cta_rows, part = warp % share, row = blockIdx.x * a.cta_rows + warp / share;
+    const int chunks = a.K / 8;
+    const bool in = row < a.rows;
+    const T* w[NW];
+#pragma unroll
+    for (int r = 0; r < NW; ++r) w[r] = a.w + ((int64_t)r * a.rows + (in ? row : 0)) * a.K;
+    float2 acc[NW][TT];
+#pragma unroll
+    for (int r = 0; r < NW; ++r)
+#pragma unroll
+        for (int t = 0; t < TT; ++t) acc[r][t] = make_float2(0.f, 0.f);
+    bool waited = false;
+    if constexpr (PAIR) start_dependents();
+    for (int c0 = part * 32 + lane; c0 < chunks; c0 += share * 32 * AHEAD) {
+        Pack<T, 8> v[AHEAD][NW];
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k)
+#pragma unroll
+            for (int r = 0; r < NW; ++r) v[k][r].load(w[r] + (int64_t)min(c0 + k * share * 32, chunks - 1) * 8);
+        // the weights are on their way before the kernel that makes x has ended
+        if (!PAIR && !waited) wait_before();
+        waited = true;
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) {
+            const int c = c0 + k * share * 32;
+            if (c >= chunks) break;
+#pragma unroll
+            for (int t = 0; t < TT; ++t) {
+                Pack<T, 8> x;
+                x.w = __ldcg(reinterpret_cast<const uint4*>(a.x + (int64_t)min(t, a.tokens - 1) * a.K + c * 8));
+#pragma unroll
+                for (int r = 0; r < NW; ++r)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) acc[r][t] = fma_(v[k][r].get(j), x.get(j), acc[r][t]);
+            }
+        }
+    }
+    if (!PAIR && !waited) wait_before();
+#pragma unroll
+    for (int r = 0; r < NW; ++r)
+#pragma unroll
+        for (int t = 0; t < TT; ++t) {
+            const float s = warp_sum(total(acc[r][t]));
+            if (lane == 0) sums[warp][r * TT + t] = s;
+        }
+    __syncthreads();
+    if (part == 0 && in)
+        for (int t = lane; t < a.tokens; t += 32) {
+            float s[NW];
+#pragma unroll
+            for (int r = 0; r < NW; ++r) {
+                s[r] = 0.f;
+                for (int k = 0; k < share; ++k) s[r] += sums[warp + k][r * TT + t];
+            }
+            float v = s[0];
+            if constexpr (PAIR) {
+                float slope;
+                activation<ACT>(s[0], v, slope);
+                v *= s[1];
+            }
+            a.out[(int64_t)t * a.rows + row] = from_f32<T>(v);
+        }
 }
 
 // ---- host -------------------------------------------------------------------------
-constexpr size_t kProductSmem = 1024 + kProductStages * kStageBytes + 4 * 2 * kOutBytes;
-constexpr size_t kHiddenSmem = 1024 + 4 * kStageBytes + kHiddenEpi * kOutBytes;
-constexpr size_t kGradSmem = 1024 + kGradStages * kStageBytes + kHiddenEpi * 2 * kOutBytes;
-
-template <class K>
-cudaError_t allow_smem(K* kernel, size_t bytes) {
-    return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
-}
-
 int ceil_div(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
-
-// C [rows][cols] = A B^T over K
-template <bool A_MN, bool B_MN>
-cudaError_t product(const FfnArgs& a, int64_t rows, int64_t cols, int64_t K, const void* A, const void* B, void* C,
-                    cudaStream_t s) {
-    constexpr int BN = 256;
-    CUtensorMap ma, mb, mc;
-    cudaError_t e = A_MN ? make_map(&ma, a.type, A, K, rows, rows, 64) : make_map(&ma, a.type, A, rows, K, K, kRowTile);
-    if (e == cudaSuccess) e = B_MN ? make_map(&mb, a.type, B, K, cols, cols, 64) : make_map(&mb, a.type, B, cols, K, K, BN);
-    if (e == cudaSuccess) e = make_map(&mc, a.type, C, rows, cols, cols, 32);
-    if (e == cudaSuccess) e = allow_smem(k_product<A_MN, B_MN, BN>, kProductSmem);
-    if (e != cudaSuccess) return e;
-    const Grid g{ceil_div(rows, kRowTile), ceil_div(cols, BN), ceil_div(K, kStepK), (int)rows, (int)cols};
-    const int64_t tiles = (int64_t)g.m_tiles * g.n_tiles;
-    return launch_kernel(k_product<A_MN, B_MN, BN>, dim3((unsigned)(tiles < a.num_sms ? tiles : a.num_sms)), dim3(192),
-                         kProductSmem, true, s, ma, mb, mc, g, a.type == IFVS_T_F16, a.err);
-}
 
 // f(constant) for the activation
 template <class Fn>
@@ -505,6 +676,121 @@ cudaError_t with_act(int act, const Fn& f) {
     if (act == IFVS_ACT_SILU) return f(std::integral_constant<int, IFVS_ACT_SILU>());
     if (act == IFVS_ACT_GELU) return f(std::integral_constant<int, IFVS_ACT_GELU>());
     return f(std::integral_constant<int, IFVS_ACT_RELU>());
+}
+
+// A persistent launch: at most one CTA per SM, in clusters of CG
+template <int CG, class... P, class... A>
+cudaError_t launch_tiles(void (*kernel)(P...), int64_t items, int num_sms, int threads, size_t smem, bool chain,
+                         cudaStream_t s, const A&... args) {
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    if (e != cudaSuccess) return e;
+    const int64_t most = num_sms / CG;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)((items < most ? items : most) * CG));
+    cfg.blockDim = dim3((unsigned)threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = s;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim = {(unsigned)CG, 1u, 1u};
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = chain ? 2 : 1;
+    return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
+
+// Products of one launch, in the order they are added
+struct Plan {
+    const FfnArgs& a;
+    bool pairs;          // 256 x 256 tiles of CTA pairs; else 128 x 128
+    uint8_t* work;       // for parts of sums
+    Products all;
+    Parts parts;
+    int joined = 0;
+    cudaError_t e = cudaSuccess;
+    explicit Plan(const FfnArgs& a_, bool pairs_, uint8_t* work_) : a(a_), pairs(pairs_), work(work_) {
+        all.n = all.items = 0;
+    }
+
+    int rows_tile() const { return pairs ? 256 : 128; }
+    // C [rows][cols] = A B^T over K
+    void add(int64_t rows, int64_t cols, int64_t K, const void* A, bool a_mn, const void* B, bool b_mn, void* C) {
+        Product& p = all.p[all.n++];
+        auto then = [&](cudaError_t r) { e = e == cudaSuccess ? r : e; };
+        then(a_mn ? make_map(&p.a, a.type, A, K, rows, rows, 64) : make_map(&p.a, a.type, A, rows, K, K, kRows));
+        then(b_mn ? make_map(&p.b, a.type, B, K, cols, cols, 64) : make_map(&p.b, a.type, B, cols, K, K, 128));
+        then(make_map(&p.c, a.type, C, rows, cols, cols, 32));
+        p.g = Grid{ceil_div(rows, rows_tile()), ceil_div(cols, rows_tile()), ceil_div(K, kStepK), (int)rows, (int)cols};
+        p.a_mn = a_mn;
+        p.b_mn = b_mn;
+        p.splits = splits_of(a, rows, cols, K, pairs);
+        p.items = p.g.m_tiles * p.g.n_tiles * p.splits;
+        p.parts = nullptr;
+        all.items += p.items;
+        if (p.splits > 1) {
+            p.parts = (float*)work;
+            work += (size_t)p.splits * rows * cols * sizeof(float);
+            parts.parts[joined] = p.parts;
+            parts.c[joined] = C;
+            parts.n[joined] = rows * cols;
+            parts.splits[joined++] = p.splits;
+        }
+    }
+    // Parts of a tile's sum: where the tiles leave SMs without work, at least four
+    // stages each.  A sum of any length is cut below 2^16 stages, which bounds
+    // every wait for a tile.
+    static int splits_of(const FfnArgs& a, int64_t rows, int64_t cols, int64_t K, bool pairs) {
+        const int tile = pairs ? 256 : 128, steps = ceil_div(K, kStepK);
+        const int64_t tiles = (int64_t)ceil_div(rows, tile) * ceil_div(cols, tile), slots = a.num_sms / (pairs ? 2 : 1);
+        int64_t n = slots / tiles;
+        if (n > steps / 4) n = steps / 4;
+        if (n > 32) n = 32;
+        const int64_t least = ((int64_t)steps + 65535) / 65536;
+        return (int)(n > least ? n : (least > 1 ? least : 1));
+    }
+    static size_t part_bytes(const FfnArgs& a, int64_t rows, int64_t cols, int64_t K, bool pairs) {
+        const int n = splits_of(a, rows, cols, K, pairs);
+        return n > 1 ? (size_t)n * rows * cols * sizeof(float) : 0;
+    }
+    cudaError_t launch(bool chain, cudaStream_t s) {
+        if (e != cudaSuccess) return e;
+        const bool f16 = a.type == IFVS_T_F16;
+        e = pairs ? launch_tiles<2>(k_products<2, 256>, all.items, a.num_sms, 192, ProductShape<2, 256>::kSmem, chain, s, all,
+                                    f16, a.err)
+                  : launch_tiles<1>(k_products<1, 128>, all.items, a.num_sms, 192, ProductShape<1, 128>::kSmem, chain, s, all,
+                                    f16, a.err);
+        if (e != cudaSuccess || joined == 0) return e;
+        int64_t most = 0;
+        for (int j = 0; j < joined; ++j) most = parts.n[j] > most ? parts.n[j] : most;
+        const dim3 grid((unsigned)((most + 1023) / 1024), (unsigned)joined);
+        return f16 ? launch_kernel(k_join_parts<__half>, grid, dim3(256), 0, true, s, parts)
+                   : launch_kernel(k_join_parts<__nv_bfloat16>, grid, dim3(256), 0, true, s, parts);
+    }
+};
+
+// Pairs of CTAs where their tiles fill the device
+bool use_pairs(const FfnArgs& a, int64_t rows, int64_t cols) {
+    return (int64_t)ceil_div(rows, 256) * ceil_div(cols, 256) >= a.num_sms / 2;
+}
+
+template <class T, bool PAIR, int ACT>
+cudaError_t launch_few(const FfnArgs& a, const void* x, const void* w, void* out, int rows, int K, cudaStream_t s) {
+    FewArgs<T> f{(const T*)x, (const T*)w, (T*)out, (int)a.T, rows, K, 8};
+    while (f.cta_rows > 1 && ceil_div(rows, f.cta_rows) < 2 * a.num_sms) f.cta_rows /= 2;
+    const dim3 grid((unsigned)ceil_div(rows, f.cta_rows));
+    auto go = [&](auto tt) { return launch_kernel(k_few<T, PAIR, ACT, tt()>, grid, dim3(256), 0, !PAIR, s, f); };
+    if (a.T == 1) return go(std::integral_constant<int, 1>());
+    if (a.T == 2) return go(std::integral_constant<int, 2>());
+    if (a.T <= 4) return go(std::integral_constant<int, 4>());
+    if (a.T <= 8) return go(std::integral_constant<int, 8>());
+    return go(std::integral_constant<int, 16>());
+}
+
+template <class T>
+cudaError_t ffn_few(const FfnArgs& a, const void* x, void* y, void* h, cudaStream_t s) {
+    const cudaError_t e = with_act(a.act, [&](auto act) { return launch_few<T, true, act()>(a, x, a.w_in, h, a.F, a.D, s); });
+    return e != cudaSuccess ? e : launch_few<T, false, IFVS_ACT_RELU>(a, h, a.w_out, y, a.D, a.F, s);
 }
 
 }  // namespace
@@ -529,26 +815,44 @@ cudaError_t make_map(CUtensorMap* map, int type, const void* p, int64_t rows, in
     return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
 }
 
-size_t ffn_bytes(const FfnArgs& a) { return (size_t)a.T * a.F * 2; }
-size_t ffn_grad_bytes(const FfnArgs& a) { return (size_t)a.T * a.F * 6; }
+namespace {
+size_t padded(size_t n) { return (n + 255) / 256 * 256; }
+bool out_pairs(const FfnArgs& a) { return use_pairs(a, a.T, a.D); }
+bool grad_pairs(const FfnArgs& a) { return use_pairs(a, a.T, a.D) || use_pairs(a, 2 * (int64_t)a.F, a.D); }
+}  // namespace
+
+size_t ffn_bytes(const FfnArgs& a) {
+    return padded((size_t)a.T * a.F * 2) + (a.T > 0 ? Plan::part_bytes(a, a.T, a.D, a.F, out_pairs(a)) : 0);
+}
+size_t ffn_grad_bytes(const FfnArgs& a) {
+    if (a.T == 0) return 0;
+    const bool p = grad_pairs(a);
+    return padded((size_t)a.T * a.F * 2) + padded((size_t)a.T * a.F * 4) + Plan::part_bytes(a, a.T, a.D, 2 * (int64_t)a.F, p) +
+           Plan::part_bytes(a, 2 * (int64_t)a.F, a.D, a.T, p) + Plan::part_bytes(a, a.D, a.F, a.T, p);
+}
 
 cudaError_t launch_ffn(const FfnArgs& a, const void* x, void* y, uint8_t* work, cudaStream_t s) {
+    if (a.T <= kFewTokens)
+        return a.type == IFVS_T_F16 ? ffn_few<__half>(a, x, y, work, s) : ffn_few<__nv_bfloat16>(a, x, y, work, s);
     CUtensorMap mx, mw, mh;
-    cudaError_t e = make_map(&mx, a.type, x, a.T, a.D, a.D, kRowTile);
-    if (e == cudaSuccess) e = make_map(&mw, a.type, a.w_in, 2 * (int64_t)a.F, a.D, a.D, 128);
-    if (e == cudaSuccess) e = make_map(&mh, a.type, work, a.T, a.F, a.F, 32);
-    if (e != cudaSuccess) return e;
-    const Grid g{ceil_div(a.T, kRowTile), ceil_div(a.F, 128), ceil_div(a.D, kStepK), (int)a.T, a.F};
-    const int64_t tiles = (int64_t)g.m_tiles * g.n_tiles;
-    e = with_act(a.act, [&](auto act) {
-        const cudaError_t r = allow_smem(k_hidden<act()>, kHiddenSmem);
-        return r != cudaSuccess ? r
-                                : launch_kernel(k_hidden<act()>, dim3((unsigned)(tiles < a.num_sms ? tiles : a.num_sms)),
-                                                dim3(kHiddenEpi * 32 + 64), kHiddenSmem, false, s, mx, mw, mh, g,
-                                                a.type == IFVS_T_F16, a.err);
+    auto run = [&](auto act, auto cg, auto ft) {
+        using Sh = HiddenShape<cg(), ft()>;
+        cudaError_t e = make_map(&mx, a.type, x, a.T, a.D, a.D, kRows);
+        if (e == cudaSuccess) e = make_map(&mw, a.type, a.w_in, 2 * (int64_t)a.F, a.D, a.D, ft());
+        if (e == cudaSuccess) e = make_map(&mh, a.type, work, a.T, a.F, a.F, 32);
+        if (e != cudaSuccess) return e;
+        const Grid g{ceil_div(a.T, kRows * cg()), ceil_div(a.F, ft()), ceil_div(a.D, kStepK), (int)a.T, a.F};
+        return launch_tiles<cg()>(k_hidden<act(), cg(), ft()>, (int64_t)g.m_tiles * g.n_tiles, a.num_sms, Sh::kEpi * 32 + 64,
+                                  Sh::kSmem, false, s, mx, mw, mh, g, a.type == IFVS_T_F16, a.err);
+    };
+    const cudaError_t e = with_act(a.act, [&](auto act) {
+        return use_pairs(a, a.T, 2 * (int64_t)a.F) ? run(act, std::integral_constant<int, 2>(), std::integral_constant<int, 128>())
+                                                   : run(act, std::integral_constant<int, 1>(), std::integral_constant<int, 64>());
     });
     if (e != cudaSuccess) return e;
-    return product<false, false>(a, a.T, a.D, a.F, work, a.w_out, y, s);
+    Plan plan(a, out_pairs(a), work + padded((size_t)a.T * a.F * 2));
+    plan.add(a.T, a.D, a.F, work, false, a.w_out, false, y);
+    return plan.launch(true, s);
 }
 
 cudaError_t launch_ffn_grad(const FfnArgs& a, const void* x, const void* dy, void* dx, void* d_w_in, void* d_w_out,
@@ -558,30 +862,43 @@ cudaError_t launch_ffn_grad(const FfnArgs& a, const void* x, const void* dy, voi
         const cudaError_t e = cudaMemsetAsync(d_w_in, 0, (size_t)(2 * F * D) * 2, s);
         return e != cudaSuccess ? e : cudaMemsetAsync(d_w_out, 0, (size_t)(D * F) * 2, s);
     }
-    uint8_t *h = work, *dgu = work + (size_t)a.T * F * 2;
-    CUtensorMap mx, mdy, mw, mwo, mh, mdg, mdu;
-    cudaError_t e = make_map(&mx, a.type, x, a.T, D, D, kRowTile);
-    auto then = [&](cudaError_t r) { e = e == cudaSuccess ? r : e; };
-    then(make_map(&mdy, a.type, dy, a.T, D, D, kRowTile));
-    then(make_map(&mw, a.type, a.w_in, 2 * F, D, D, 128));
-    then(make_map(&mwo, a.type, a.w_out, D, F, F, 64));
-    then(make_map(&mh, a.type, h, a.T, F, F, 32));
-    then(make_map(&mdg, a.type, dgu, a.T, F, 2 * F, 32));
-    then(make_map(&mdu, a.type, dgu + F * 2, a.T, F, 2 * F, 32));
-    if (e != cudaSuccess) return e;
-    const Grid g{ceil_div(a.T, kRowTile), ceil_div(F, 128), ceil_div(D, kStepK), (int)a.T, a.F};
-    const int64_t tiles = (int64_t)g.m_tiles * g.n_tiles;
-    e = with_act(a.act, [&](auto act) {
-        const cudaError_t r = allow_smem(k_hidden_grad<act()>, kGradSmem);
-        return r != cudaSuccess ? r
-                                : launch_kernel(k_hidden_grad<act()>, dim3((unsigned)(tiles < a.num_sms ? tiles : a.num_sms)),
-                                                dim3(kHiddenEpi * 32 + 64), kGradSmem, false, s, mx, mdy, mw, mwo, mh, mdg,
-                                                mdu, g, a.type == IFVS_T_F16, a.err);
+    uint8_t *h = work, *dgu = work + padded((size_t)a.T * F * 2);
+    auto run = [&](auto act, auto cg, auto ft) {
+        using Sh = GradShape<cg(), ft()>;
+        CUtensorMap mx, mdy, mw, mwo, mh, mdg, mdu;
+        cudaError_t e = make_map(&mx, a.type, x, a.T, D, D, kRows);
+        auto then = [&](cudaError_t r) { e = e == cudaSuccess ? r : e; };
+        then(make_map(&mdy, a.type, dy, a.T, D, D, kRows));
+        then(make_map(&mw, a.type, a.w_in, 2 * F, D, D, ft()));
+        then(make_map(&mwo, a.type, a.w_out, D, F, F, 64));
+        then(make_map(&mh, a.type, h, a.T, F, F, 32));
+        then(make_map(&mdg, a.type, dgu, a.T, F, 2 * F, 32));
+        then(make_map(&mdu, a.type, dgu + F * 2, a.T, F, 2 * F, 32));
+        if (e != cudaSuccess) return e;
+        const Grid g{ceil_div(a.T, kRows * cg()), ceil_div(F, ft()), ceil_div(D, kStepK), (int)a.T, a.F};
+        return launch_tiles<cg()>(k_hidden_grad<act(), cg(), ft()>, (int64_t)g.m_tiles * g.n_tiles, a.num_sms,
+                                  Sh::kEpi * 32 + 64, Sh::kSmem, false, s, mx, mdy, mw, mwo, mh, mdg, mdu, g,
+                                  a.type == IFVS_T_F16, a.err);
+    };
+    const cudaError_t e = with_act(a.act, [&](auto act) {
+        return use_pairs(a, a.T, 2 * F) ? run(act, std::integral_constant<int, 2>(), std::integral_constant<int, 128>())
+                                        : run(act, std::integral_constant<int, 1>(), std::integral_constant<int, 64>());
     });
-    if (e == cudaSuccess) e = product<false, true>(a, a.T, D, 2 * F, dgu, a.w_in, dx, s);
-    if (e == cudaSuccess) e = product<true, true>(a, 2 * F, D, a.T, dgu, x, d_w_in, s);
-    if (e == cudaSuccess) e = product<true, true>(a, D, F, a.T, dy, h, d_w_out, s);
-    return e;
+    if (e != cudaSuccess) return e;
+    // the longest sums first
+    Plan plan(a, grad_pairs(a), dgu + padded((size_t)a.T * F * 4));
+    auto d_in = [&] { plan.add(2 * F, D, a.T, dgu, true, x, true, d_w_in); };
+    auto d_out = [&] { plan.add(D, F, a.T, dy, true, h, true, d_w_out); };
+    if (a.T >= 2 * F) {
+        d_in();
+        d_out();
+        plan.add(a.T, D, 2 * F, dgu, false, a.w_in, true, dx);
+    } else {
+        plan.add(a.T, D, 2 * F, dgu, false, a.w_in, true, dx);
+        d_in();
+        d_out();
+    }
+    return plan.launch(true, s);
 }
 
 }  // namespace ifvs

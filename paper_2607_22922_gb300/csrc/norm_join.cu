@@ -520,17 +520,18 @@ __global__ void __launch_bounds__(WARPS * 32, 1) k_norm_join_grad(JoinArgs a, Jo
 }
 
 // CTAs (128 columns each along y) of three kinds along x: 0 and 1 add the norms'
-// weights over the CTAs before; the next ones, for eight teams each, add the
+// weights over the CTAs before; the next ones, for 32 teams each, add the
 // partial sums of sequences that begin among a team's tokens and go on (a warp
 // per team, or for long ones the CTA); the rest clear the gradients of empty
 // sequences' gates.
-constexpr int kClearRows = 256;
+constexpr int kFinishWarps = 32;         // teams per CTA too
+constexpr int kClearRows = 1024;
 constexpr int kWarpRows = 16;            // partial sums that a warp adds by itself
 
 template <class T>
-__global__ void __launch_bounds__(256) k_join_finish(JoinArgs a, JoinGrads g, GradPlan p) {
-    __shared__ float part[8][128];
-    __shared__ int64_t long_last[8];
+__global__ void __launch_bounds__(kFinishWarps * 32) k_join_finish(JoinArgs a, JoinGrads g, GradPlan p) {
+    __shared__ float part[kFinishWarps][128];
+    __shared__ int64_t long_last[kFinishWarps];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int c0 = blockIdx.y * 128;
     wait_before();
@@ -545,14 +546,14 @@ __global__ void __launch_bounds__(256) k_join_finish(JoinArgs a, JoinGrads g, Gr
     // the same with rows spread over the CTA's warps: column threadIdx.x < 128
     auto cta_rows = [&](const float* from, int64_t stride, int64_t first, int64_t last) {
         float v[4] = {0.f, 0.f, 0.f, 0.f};
-        add_rows(v, from, stride, first + warp, last, 8);
+        add_rows(v, from, stride, first + warp, last, kFinishWarps);
         __syncthreads();
 #pragma unroll
         for (int j = 0; j < 4; ++j) part[warp][j * 32 + lane] = v[j];
         __syncthreads();
         float sum = 0.f;
         if (threadIdx.x < 128)
-            for (int w = 0; w < 8; ++w) sum += part[w][threadIdx.x];
+            for (int w = 0; w < kFinishWarps; ++w) sum += part[w][threadIdx.x];
         return sum;
     };
     const int c = c0 + threadIdx.x;
@@ -563,10 +564,10 @@ __global__ void __launch_bounds__(256) k_join_finish(JoinArgs a, JoinGrads g, Gr
         if (threadIdx.x < 128 && c < a.D) out[c] = from_f32<T>(v);
         return;
     }
-    const int64_t group = (int64_t)blockIdx.x - 2, groups = (p.teams + 7) / 8;
+    const int64_t group = (int64_t)blockIdx.x - 2, groups = (p.teams + kFinishWarps - 1) / kFinishWarps;
     const T* wp = (const T*)a.w_post;
     if (group < groups) {
-        const int64_t k = group * 8 + warp, t0 = k * p.chunk, t1 = t0 + p.chunk;
+        const int64_t k = group * kFinishWarps + warp, t0 = k * p.chunk, t1 = t0 + p.chunk;
         int64_t last = -1, b = 0;
         if (k < p.teams && t1 < a.T) {
             b = sequence_of(a.offsets, a.B, t1 - 1);
@@ -588,9 +589,9 @@ __global__ void __launch_bounds__(256) k_join_finish(JoinArgs a, JoinGrads g, Gr
             }
         }
         __syncthreads();
-        for (int w = 0; w < 8; ++w) {
+        for (int w = 0; w < kFinishWarps; ++w) {
             if (long_last[w] < 0) continue;
-            const int64_t kw = group * 8 + w, bw = sequence_of(a.offsets, a.B, kw * p.chunk + p.chunk - 1);
+            const int64_t kw = group * kFinishWarps + w, bw = sequence_of(a.offsets, a.B, kw * p.chunk + p.chunk - 1);
             const float v = cta_rows(p.gates, 2 * a.D, kw + 1, long_last[w]);
             if (threadIdx.x < 128 && c < a.D)
                 ((T*)g.d_gate)[bw * a.D + c] = from_f32<T>(to_f32(wp[c]) * (__ldcg(p.gates + (kw * 2 + 1) * a.D + c) + v));
@@ -598,7 +599,7 @@ __global__ void __launch_bounds__(256) k_join_finish(JoinArgs a, JoinGrads g, Gr
         return;
     }
     const int64_t b0 = (group - groups) * kClearRows;
-    for (int64_t b = b0 + warp; b < min(a.B, b0 + kClearRows); b += 8)
+    for (int64_t b = b0 + warp; b < min(a.B, b0 + kClearRows); b += kFinishWarps)
         if (__ldg(a.offsets + b) == __ldg(a.offsets + b + 1))
             for (int e = c0 + lane; e < min(a.D, c0 + 128); e += 32) ((T*)g.d_gate)[b * a.D + e] = from_f32<T>(0.f);
 }
@@ -727,8 +728,8 @@ cudaError_t launch_norm_join_grad(const JoinArgs& a, const JoinGrads& g, uint8_t
         const int64_t teams = g.d_gate ? p.teams : 0, clears = g.d_gate && a.offsets ? (a.B + kClearRows - 1) / kClearRows : 0;
         GradPlan q = p;
         q.teams = teams;
-        return launch_kernel(k_join_finish<T>, dim3((unsigned)(2 + (teams + 7) / 8 + clears), (unsigned)((a.D + 127) / 128)), dim3(256), 0,
-                             true, s, a, g, q);
+        return launch_kernel(k_join_finish<T>, dim3((unsigned)(2 + (teams + kFinishWarps - 1) / kFinishWarps + clears), (unsigned)((a.D + 127) / 128)),
+                             dim3(kFinishWarps * 32), 0, true, s, a, g, q);
     };
     auto of16 = [&](auto t) {
         using T = decltype(t);
