@@ -82,12 +82,12 @@ __device__ __forceinline__ uint32_t pack2(float2 v, __half) {
     return d;
 }
 
-// N consecutive elements, in one access of 16, 4 or 2 bytes, as N / 2 pairs of
+// N consecutive elements, in one access of 16, 8, 4 or 2 bytes, as N / 2 pairs of
 // floats or (N = 1) one float
 template <class T, int N>
 struct Pack {
     static constexpr int kBytes = N * (int)sizeof(T);
-    using Word = std::conditional_t<kBytes == 16, uint4, std::conditional_t<kBytes == 4, uint32_t, uint16_t>>;
+    using Word = std::conditional_t<kBytes == 16, uint4, std::conditional_t<kBytes == 8, uint2, std::conditional_t<kBytes == 4, uint32_t, uint16_t>>>;
     using F = std::conditional_t<N == 1, float, float2>;
     static constexpr int kF = N == 1 ? 1 : N / 2;
     Word w;

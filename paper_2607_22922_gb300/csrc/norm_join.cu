@@ -10,12 +10,12 @@
 //   d_w_post = sum of gate_b g u, d_w_pre = sum of d_n x' i over all tokens
 //
 // Both are bound by memory: two rows read and two written per token, four and
-// two.  A team of 1 to 16 warps takes a token's rows through a ring of kStages
-// places in shared memory, filled ahead by bulk copies, or by 4-byte
-// asynchronous copies where rows do not begin on 16 bytes: each row is read
-// once from memory, whatever the norms need of it, and a team's loads go on
-// while it reduces.  A team takes tokens that follow each other: the sequence of
-// the first is searched, the others' follow, and the gradient keeps its sums
+// two.  A team of 1 to 16 warps takes tokens that follow each other, through a ring
+// of kStages places in shared memory that bulk copies fill ahead: each row is
+// read once from memory, whatever the norms need of it, and a team's loads go on
+// while it reduces.  A place holds the bytes of a few tokens (they follow each
+// other in memory, so that rows need no alignment).  The sequence of a team's
+// first token is searched, the others' follow, and the gradient keeps its sums
 // over tokens in registers.  A sequence inside a team's tokens has its gate's
 // gradient written at once; one that reaches beyond them leaves float32 partial
 // sums that k_join_finish adds in order, as it does with the norms' weights.  No
@@ -31,7 +31,7 @@ namespace {
 // slots, so that a set is not written again before all have read it.
 struct Team {
     int warps, warp, id;        // warps of the team, this one's place, the team's number in the CTA
-    float4* slots;              // [2][all warps of the CTA]
+    float* slots;               // [2][all warps of the CTA][4], 16-byte aligned
     int turn, all;
     __device__ __forceinline__ void sync() const {
         if (warps == 1)
@@ -39,155 +39,198 @@ struct Team {
         else
             asm volatile("barrier.cta.sync %0, %1;" ::"r"(1 + id), "r"(warps * 32) : "memory");
     }
-    __device__ __forceinline__ float4 sum(float4 v) {
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) {
-            v.x += __shfl_xor_sync(0xFFFFFFFFu, v.x, o);
-            v.y += __shfl_xor_sync(0xFFFFFFFFu, v.y, o);
-            v.z += __shfl_xor_sync(0xFFFFFFFFu, v.z, o);
-        }
+    __device__ __forceinline__ float sum(float v) {
+        v = warp_sum(v);
         if (warps == 1) return v;
-        float4* s = slots + turn * all + id * warps;
+        float* s = slots + (turn * all + id * warps) * 4;
         turn ^= 1;
-        if ((threadIdx.x & 31) == 0) s[warp] = v;
+        if ((threadIdx.x & 31) == 0) s[warp * 4] = v;
         sync();
         v = s[0];
-        for (int w = 1; w < warps; ++w) {
-            v.x += s[w].x;
-            v.y += s[w].y;
-            v.z += s[w].z;
-        }
+        for (int w = 1; w < warps; ++w) v += s[w * 4];
         return v;
+    }
+    // three sums at once: lanes that differ in bit 0 share the first two, in bit 1
+    // those and the third, so that three more exchanges end all of them
+    __device__ __forceinline__ float3 sum3(float x, float y, float z) {
+        const int lane = threadIdx.x & 31;
+        const bool odd = lane & 1, third = lane & 2;
+        float v = (odd ? y : x) + __shfl_xor_sync(0xFFFFFFFFu, odd ? x : y, 1);
+        z += __shfl_xor_sync(0xFFFFFFFFu, z, 1);
+        v = (third ? z : v) + __shfl_xor_sync(0xFFFFFFFFu, third ? v : z, 2);
+#pragma unroll
+        for (int o = 4; o < 32; o <<= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
+        if (warps == 1)
+            return make_float3(__shfl_sync(0xFFFFFFFFu, v, 0), __shfl_sync(0xFFFFFFFFu, v, 1), __shfl_sync(0xFFFFFFFFu, v, 2));
+        float* s = slots + (turn * all + id * warps) * 4;
+        turn ^= 1;
+        if (lane < 4) s[warp * 4 + lane] = v;
+        sync();
+        float4 t = *reinterpret_cast<const float4*>(s);
+        for (int w = 1; w < warps; ++w) {
+            const float4 q = *reinterpret_cast<const float4*>(s + w * 4);
+            t.x += q.x;
+            t.y += q.y;
+            t.z += q.z;
+        }
+        return make_float3(t.x, t.y, t.z);
     }
 };
 
 // The sequence of a team's next token, given that of an earlier one
 struct Sequence {
     const int64_t* offsets;
-    int64_t B, T, b, end;       // offsets[b + 1]
-    __device__ __forceinline__ void start(int64_t t) {
-        b = sequence_of(offsets, B, t);
-        end = offsets ? __ldg(offsets + b + 1) : T;
+    int B, T, b, end;           // end: offsets[b + 1], within 0..T whatever the offsets hold
+    __device__ __forceinline__ int offset(int i) const { return (int)max((int64_t)0, min((int64_t)T, __ldg(offsets + i))); }
+    __device__ __forceinline__ void start(int t) {
+        b = (int)sequence_of(offsets, B, t);
+        end = offsets ? offset(b + 1) : T;
     }
     // whether the sequence changes at token t
-    __device__ __forceinline__ bool moved(int64_t t) const { return t >= end && b + 1 < B; }
-    __device__ __forceinline__ void move(int64_t t) {
+    __device__ __forceinline__ bool moved(int t) const { return t >= end && b + 1 < B; }
+    __device__ __forceinline__ void move(int t) {
         ++b;
-        end = __ldg(offsets + b + 1);
+        end = offset(b + 1);
         if (t >= end && b + 1 < B) start(t);     // past empty sequences
     }
-    __device__ __forceinline__ int64_t begin() const { return offsets ? __ldg(offsets + b) : 0; }
+    __device__ __forceinline__ int begin() const { return offsets ? offset(b) : 0; }
 };
 
 constexpr int kStages = 3;               // places of a ring (1: no copies ahead)
 
-// A team's ring of rows: A arrays per place (absent ones are null).  Bulk copies
-// (one thread, completion on an mbarrier) where rows begin on 16 bytes;
-// otherwise 4-byte copies by all lanes, from the 4-byte word that holds the
-// row's first element, so that a row lies `shift` bytes into its place.
+extern __shared__ __align__(16) uint8_t join_smem[];
+
+// tokens per place: about 1 KB of an array, at most 8
+__host__ __device__ constexpr int place_tokens(int row_bytes) {
+    return row_bytes >= 1024 ? 1 : (row_bytes <= 128 ? 8 : 1024 / row_bytes);
+}
+
+// A team's ring: per place the rows of `per` tokens of A arrays (absent ones are
+// null), from the 16-byte boundary before them to the one after.  Where that
+// boundary lies outside the array, the row's bytes beside it are copied by
+// plain loads: no byte outside an array is read.
 template <class T, int N, int A, int S = kStages>
 struct Rows {
-    static constexpr bool kBulk = N * sizeof(T) == 16;
     const T* p[A];
-    uint8_t* ring;              // S x A x stride bytes
-    uint64_t* bars;             // S
+    uint32_t ring;              // S x A x stride bytes of join_smem
+    uint32_t bars;              // address of S mbarriers
     volatile int* dead;
     int* err;
-    int D, stride, place = 0;
+    int T_, D;                  // tokens of the arrays, their width
+    int per, stride, place = 0;
     uint32_t parity = 0;
+    uint32_t off[A];            // of the current token's rows in the ring
 
-    static __host__ __device__ int stride_of(int D) { return (D * (int)sizeof(T) + 4 + 15) / 16 * 16; }
-    __device__ __forceinline__ uint8_t* at(int place_, int k) const { return ring + (place_ * A + k) * stride; }
-    __device__ __forceinline__ uint32_t shift(int k, int64_t t) const {
-        return kBulk ? 0u : (uint32_t)(reinterpret_cast<uintptr_t>(p[k] + t * D) & 3u);
+    static __host__ __device__ int stride_of(int D) {
+        return (place_tokens(D * (int)sizeof(T)) * D * (int)sizeof(T) + 32 + 15) / 16 * 16;
     }
-    // the whole team; its earlier reads of the place lie before a barrier of the team
-    __device__ __forceinline__ void fill(const Team& team, int place_, int64_t t) const {
+    __device__ __forceinline__ Rows(uint64_t* bars_, int* dead_, const JoinArgs& a, int team)
+        : ring(team * S * A * stride_of(a.D)),
+          bars((uint32_t)__cvta_generic_to_shared(bars_ + team * S)), dead(dead_), err(a.err), T_((int)a.T), D(a.D),
+          per(place_tokens(a.D * (int)sizeof(T))), stride(stride_of(a.D)) {}
+
+    // tokens [t, t + n); the team's earlier reads of the place lie before a barrier of the team
+    __device__ __forceinline__ void fill(const Team& team, int place_, int t, int n) const {
+        if (team.warp != 0) return;
         const int lane = threadIdx.x & 31;
-        if constexpr (kBulk) {
-            if (team.warp == 0 && lane == 0) {
-                const uint32_t bar = (uint32_t)__cvta_generic_to_shared(bars + place_), bytes = D * sizeof(T);
-                int n = 0;
+        const uint32_t to = (uint32_t)__cvta_generic_to_shared(join_smem) + ring + place_ * A * stride;
+        if constexpr (N * sizeof(T) == 16) {        // rows begin and end on 16 bytes
+            if (lane != 0) return;
+            const uint32_t len = n * D * (uint32_t)sizeof(T);
+            const int64_t at = (int64_t)t * D;
+            uint32_t arrays = 0;
 #pragma unroll
-                for (int k = 0; k < A; ++k) n += p[k] != nullptr;
-                mbar_arrive_expect_tx(bar, n * bytes);
-                const uint64_t once = policy_evict_first();
+            for (int k = 0; k < A; ++k) arrays += p[k] != nullptr;
+            mbar_arrive_expect_tx(bars + 8u * place_, arrays * len);
+            const uint64_t once = policy_evict_first();
 #pragma unroll
-                for (int k = 0; k < A; ++k)
-                    if (p[k]) bulk_g2s((uint32_t)__cvta_generic_to_shared(at(place_, k)), p[k] + t * D, bytes, bar, once);
-            }
-        } else {
+            for (int k = 0; k < A; ++k)
+                if (p[k]) bulk_g2s(to + k * stride, p[k] + at, len, bars + 8u * place_, once);
+            return;
+        }
+        const int64_t o = (int64_t)t * D * (int)sizeof(T), rest = (int64_t)(T_ - t - n) * D * (int)sizeof(T);
+        const uint32_t len = n * D * (uint32_t)sizeof(T), bar = bars + 8u * place_;
+        // of array k: bytes of the copy before and after the rows, and whether they lie in the array
+        auto copy = [&](int k, bool issue, uint64_t policy) -> uint32_t {
+            const uint8_t* lo = reinterpret_cast<const uint8_t*>(p[k]) + o;
+            const uint32_t before = (uint32_t)(reinterpret_cast<uintptr_t>(lo)) & 15u, after = (0u - before - len) & 15u;
+            const uint32_t skip = before > o ? 16u : 0u, cut = after > rest ? 16u : 0u;
+            const uint32_t all = before + len + after;
+            const uint32_t bytes = all > skip + cut ? all - skip - cut : 0u;
+            if (!issue) return bytes;
+            if (skip | cut)
+                for (uint32_t q = before + lane * 2; q < before + len; q += 64)
+                    if (q < skip || q >= skip + bytes)
+                        asm volatile("st.shared.u16 [%0], %1;" ::"r"(to + k * stride + q),
+                                     "h"(__ldg(reinterpret_cast<const uint16_t*>(lo - before + q)))
+                                     : "memory");
+            if (bytes && lane == 0)
+                bulk_g2s(to + k * stride + skip, lo - before + skip, bytes, bar, policy);
+            return bytes;
+        };
+        uint32_t all = 0;
 #pragma unroll
-            for (int k = 0; k < A; ++k) {
-                if (!p[k]) continue;
-                const uint8_t* row = reinterpret_cast<const uint8_t*>(p[k] + t * D);
-                const uint32_t s = shift(k, t), end = s + D * sizeof(T);
-                const uint32_t dst = (uint32_t)__cvta_generic_to_shared(at(place_, k));
-                for (uint32_t w = (team.warp * 32 + lane) * 4; w < end; w += team.warps * 128) {
-                    if (w >= s && w + 4 <= end) {
-                        asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst + w), "l"(row - s + w) : "memory");
-                    } else {                // a word of which the row has one half: no byte beside the row is read
-                        const uint32_t h = w < s ? s : w;
-                        *reinterpret_cast<uint16_t*>(at(place_, k) + h) = __ldg(reinterpret_cast<const uint16_t*>(row - s + h));
-                    }
+        for (int k = 0; k < A; ++k)
+            if (p[k]) all += copy(k, false, 0);
+        if (lane == 0) mbar_arrive_expect_tx(bar, all);
+        const uint64_t once = policy_evict_first();
+#pragma unroll
+        for (int k = 0; k < A; ++k)
+            if (p[k]) copy(k, true, once);
+    }
+    // fills the ring for tokens [t, end)
+    __device__ __forceinline__ void start(const Team& team, int t, int end) const {
+        for (int i = 0; i < S; ++i, t += per)
+            if (t < end) fill(team, i, t, min(per, end - t));
+        team.sync();
+    }
+    // The place's rows are there, for the whole team; t is its first token.  A wait
+    // that runs out marks the CTA: later waits return at once, the team goes on and
+    // its results are reported as incomplete.
+    __device__ __forceinline__ void enter(const Team& team, int t) {
+        const uint32_t bar = bars + 8u * place;
+        if (!mbar_try_wait(bar, parity)) {
+            const long long t0 = clock64();
+            while (!mbar_try_wait(bar, parity) && !*dead)
+                if (clock64() - t0 > kWaitCycles) {
+                    *dead = 1;
+                    *err = kErrWait;
                 }
-            }
+        }
+        if (S == 1) team.sync();         // plain loads of the fill just before
+#pragma unroll
+        for (int k = 0; k < A; ++k) {
+            off[k] = ring + (uint32_t)((place * A + k) * stride);
+            if (N * sizeof(T) != 16) off[k] += (uint32_t)reinterpret_cast<uintptr_t>(p[k] + (int64_t)t * D) & 15u;
         }
     }
-    __device__ __forceinline__ void close() const {      // after every fill, taken place or not
-        if constexpr (!kBulk) asm volatile("cp.async.commit_group;" ::: "memory");
-    }
-    // the place's rows are there, for the whole team.  A wait that runs out marks
-    // the CTA: later waits return at once, the team goes on and its results are
-    // reported as incomplete
-    __device__ __forceinline__ void wait(const Team& team) const {
-        if constexpr (kBulk) {
-            const uint32_t bar = (uint32_t)__cvta_generic_to_shared(bars + place);
-            if (!mbar_try_wait(bar, parity)) {
-                const long long t0 = clock64();
-                while (!mbar_try_wait(bar, parity) && !*dead)
-                    if (clock64() - t0 > kWaitCycles) {
-                        *dead = 1;
-                        *err = kErrWait;
-                    }
-            }
-        } else {
-            asm volatile("cp.async.wait_group %0;" ::"n"(S - 1) : "memory");
-            team.sync();
-        }
-    }
-    __device__ __forceinline__ Pack<T, N> get(int k, int64_t t, int col) const {
+    __device__ __forceinline__ Pack<T, N> get(int k, int col) const {
         Pack<T, N> v;
-        const uint8_t* q = at(place, k) + shift(k, t) + col * sizeof(T);
-        v.w = *reinterpret_cast<const typename Pack<T, N>::Word*>(q);
+        v.w = *reinterpret_cast<const typename Pack<T, N>::Word*>(join_smem + off[k] + col * (uint32_t)sizeof(T));
         return v;
     }
-    // this place is read by the whole team: orders the reads before its next fill
-    __device__ __forceinline__ void leave(const Team& team, int64_t t, int64_t end) {
-        if constexpr (kBulk) fence_proxy_async_smem();
+    __device__ __forceinline__ void next() {
+#pragma unroll
+        for (int k = 0; k < A; ++k) off[k] += D * sizeof(T);
+    }
+    // the place that begins with token t is read by the whole team: fills it with what comes S places later
+    __device__ __forceinline__ void leave(const Team& team, int t, int end) {
+        fence_proxy_async_smem();
         team.sync();
-        if (t + S < end) fill(team, place, t + S);
-        close();
+        const int f = t + S * per;
+        if (f < end) fill(team, place, f, min(per, end - f));
         if (++place == S) {
             place = 0;
             parity ^= 1u;
         }
     }
-    __device__ __forceinline__ void start(const Team& team, int64_t t0, int64_t t1) const {
-        for (int i = 0; i < S; ++i) {
-            if (t0 + i < t1) fill(team, i, t0 + i);
-            close();
-        }
-    }
     // copies in flight after a wait that ran out: bounded
     __device__ __forceinline__ void drain() const {
-        if constexpr (kBulk) {
-            if (!*dead) return;
-            for (int i = 0; i < S; ++i) {
-                const long long t0 = clock64();
-                while (!mbar_try_wait((uint32_t)__cvta_generic_to_shared(bars + i), parity ^ (i < place ? 1u : 0u)) &&
-                       clock64() - t0 < kWaitCycles) {
-                }
+        if (!*dead) return;
+        for (int i = 0; i < S; ++i) {
+            const long long t0 = clock64();
+            while (!mbar_try_wait(bars + 8u * i, parity ^ (i < place ? 1u : 0u)) &&
+                   clock64() - t0 < kWaitCycles) {
             }
         }
     }
@@ -199,7 +242,7 @@ constexpr int kJoinColumns = 1024;       // columns a warp holds at most
 // Shared memory of a kernel whose `teams` teams have rings of A rows a place
 template <class T, int N, int A, int S = kStages>
 size_t ring_bytes(int teams, int D) {
-    return (size_t)teams * S * A * Rows<T, N, A>::stride_of(D);
+    return (size_t)teams * S * A * Rows<T, N, A, S>::stride_of(D);
 }
 
 // Tokens [chunk team, chunk (team + 1)) of team number `team`
@@ -207,22 +250,22 @@ template <class T, int N, int NV>
 __global__ void __launch_bounds__(kJoinThreads, 2)
 k_norm_join(JoinArgs a, int team_warps, int64_t chunk, const T* __restrict__ x, const T* __restrict__ y,
             T* __restrict__ xo, T* __restrict__ no) {
-    extern __shared__ __align__(16) uint8_t rings[];
-    __shared__ float4 slots[2 * kJoinThreads / 32];
+    __shared__ __align__(16) float slots[2 * kJoinThreads / 32 * 4];
     __shared__ __align__(8) uint64_t bars[kJoinThreads / 32 * kStages];
     __shared__ int dead;
     check_offsets(a.offsets, a.B, a.T, a.err);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     Team team{team_warps, warp % team_warps, warp / team_warps, slots, 0, kJoinThreads / 32};
     const int64_t number = (int64_t)blockIdx.x * (kJoinThreads / 32 / team_warps) + team.id;
-    const int64_t t0 = number * chunk, t1 = min(a.T, t0 + chunk);
+    const int t0 = (int)min(a.T, number * chunk), t1 = (int)min(a.T, number * chunk + chunk);
     const int col = (team.warp * 32 + lane) * N, step = team_warps * 32 * N;
     const float inv_d = 1.f / (float)a.D;
     const T* gate = (const T*)a.gate;
     const T* wp = (const T*)a.w_post;
     const T* wn = (const T*)a.w_pre;
-    Rows<T, N, 2> rows{{x, y}, rings + team.id * kStages * 2 * Rows<T, N, 2>::stride_of(a.D), bars + team.id * kStages,
-                       &dead, a.err, a.D, Rows<T, N, 2>::stride_of(a.D)};
+    Rows<T, N, 2> rows(bars, &dead, a, team.id);
+    rows.p[0] = x;
+    rows.p[1] = y;
     if (threadIdx.x == 0) {
         for (int i = 0; i < kJoinThreads / 32 * kStages; ++i) mbar_init((uint32_t)__cvta_generic_to_shared(bars + i), 1);
         dead = 0;
@@ -233,7 +276,7 @@ k_norm_join(JoinArgs a, int team_warps, int64_t chunk, const T* __restrict__ x, 
     rows.start(team, t0, t1);
     using F = typename Pack<T, N>::F;
     constexpr int kF = Pack<T, N>::kF;
-    Sequence seq{a.offsets, a.B, a.T, 0, 0};
+    Sequence seq{a.offsets, (int)a.B, (int)a.T, 0, 0};
     F gw[NV][kF];                    // gate * w_post of the sequence
     auto load_gate = [&] {
 #pragma unroll
@@ -242,7 +285,7 @@ k_norm_join(JoinArgs a, int team_warps, int64_t chunk, const T* __restrict__ x, 
             if (c >= a.D) continue;
             Pack<T, N> w, g;
             w.load(wp + c);
-            if (gate) g.load(gate + seq.b * a.D + c);
+            if (gate) g.load(gate + (int64_t)seq.b * a.D + c);
 #pragma unroll
             for (int j = 0; j < kF; ++j) gw[i][j] = gate ? mul_(g.get(j), w.get(j)) : w.get(j);
         }
@@ -250,32 +293,33 @@ k_norm_join(JoinArgs a, int team_warps, int64_t chunk, const T* __restrict__ x, 
     if (gate) seq.start(t0);
     if (y) load_gate();
     const F rho = both<F>(a.rho);
-    for (int64_t t = t0; t < t1; ++t) {
+    int first = t0;                                        // token of the place
+    for (int t = t0; t < t1; ++t) {
         F v[NV][kF], q = both<F>(0.f);
         if (gate && seq.moved(t)) {
             seq.move(t);
             load_gate();
         }
-        rows.wait(team);
+        if (t == first) rows.enter(team, t);
         if (y) {
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
                 const int c = col + i * step;
                 if (c >= a.D) continue;
-                const Pack<T, N> r = rows.get(1, t, c);
+                const Pack<T, N> r = rows.get(1, c);
 #pragma unroll
                 for (int j = 0; j < kF; ++j) {
                     v[i][j] = r.get(j);
                     q = fma_(v[i][j], v[i][j], q);
                 }
             }
-            const F iy = both<F>(rsqrtf(fmaf(team.sum(make_float4(total(q), 0.f, 0.f, 0.f)).x, inv_d, a.eps)));
+            const F iy = both<F>(rsqrtf(fmaf(team.sum(total(q)), inv_d, a.eps)));
             q = both<F>(0.f);
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
                 const int c = col + i * step;
                 if (c >= a.D) continue;
-                const Pack<T, N> r = rows.get(0, t, c);
+                const Pack<T, N> r = rows.get(0, c);
                 Pack<T, N> o;
 #pragma unroll
                 for (int j = 0; j < kF; ++j) {
@@ -283,14 +327,14 @@ k_norm_join(JoinArgs a, int team_warps, int64_t chunk, const T* __restrict__ x, 
                     q = fma_(v[i][j], v[i][j], q);
                     o.set(j, v[i][j]);
                 }
-                o.store(xo + t * a.D + c);
+                o.store(xo + (int64_t)t * a.D + c);
             }
         } else {
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
                 const int c = col + i * step;
                 if (c >= a.D) continue;
-                const Pack<T, N> r = rows.get(0, t, c);
+                const Pack<T, N> r = rows.get(0, c);
 #pragma unroll
                 for (int j = 0; j < kF; ++j) {
                     v[i][j] = r.get(j);
@@ -298,9 +342,13 @@ k_norm_join(JoinArgs a, int team_warps, int64_t chunk, const T* __restrict__ x, 
                 }
             }
         }
-        rows.leave(team, t, t1);
+        rows.next();
+        if (t + 1 == first + rows.per || t + 1 == t1) {
+            rows.leave(team, first, t1);
+            first = t + 1;
+        }
         if (!no) continue;
-        const F ix = both<F>(rsqrtf(fmaf(team.sum(make_float4(total(q), 0.f, 0.f, 0.f)).x, inv_d, a.eps)));
+        const F ix = both<F>(rsqrtf(fmaf(team.sum(total(q)), inv_d, a.eps)));
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int c = col + i * step;
@@ -309,18 +357,19 @@ k_norm_join(JoinArgs a, int team_warps, int64_t chunk, const T* __restrict__ x, 
             w.load(wn + c);
 #pragma unroll
             for (int j = 0; j < kF; ++j) o.set(j, mul_(w.get(j), mul_(v[i][j], ix)));
-            o.store(no + t * a.D + c);
+            o.store(no + (int64_t)t * a.D + c);
         }
     }
     rows.drain();
 }
 
 // ---- gradient ------------------------------------------------------------------
-// 16 warps of 16-bit rows, 8 of float32 rows: three places of four rows each fit
-// the shared memory at 512 columns a warp.  One row of float32 beyond 4096 takes
-// 16 warps, and a single place.
-constexpr int grad_warps(int type, int D) { return type == IFVS_T_F32 && D <= 8 * 512 ? 8 : 16; }
-constexpr int kGradColumns = 512;        // columns a warp holds at most
+// 16 warps a CTA; three places of four rows each in shared memory at 512 columns
+// of 16 bits a warp (more warps per token repeat its sums and waits: 410 us with
+// 256 columns, 360 with 512, 131101 tokens x 1024), 256 of float32.  Float32
+// rows beyond 4096 take 512 and a single place.
+constexpr int kGradWarps = 16;
+constexpr int grad_columns(int type, int D) { return type == IFVS_T_F32 && D <= kGradWarps * 256 ? 256 : 512; }
 
 struct GradPlan {
     int team_warps, ctas;
@@ -328,27 +377,32 @@ struct GradPlan {
     float* gates;        // [teams][2][D]: sums of the sequence that reaches into the team's tokens from
                          // before, and of the one that begins in them and goes on
     float* weights;      // [ctas][2][D]: d_w_post, d_w_pre
+    int2* open;          // [teams]: the sequence that begins in the team's tokens and goes on (-1: none), its end
 };
 
-template <class T, int N, int NV, int WARPS, int S>
-__global__ void __launch_bounds__(WARPS * 32, 1) k_norm_join_grad(JoinArgs a, JoinGrads g, GradPlan p) {
+// ALL: y, d_x_out, d_n and the gate are there
+template <class T, int N, int NV, int S, bool ALL>
+__global__ void __launch_bounds__(kGradWarps * 32, 1) k_norm_join_grad(JoinArgs a, JoinGrads g, GradPlan p) {
     using Ring = Rows<T, N, 4, S>;
-    __shared__ float4 slots[2 * WARPS];
+    constexpr int WARPS = kGradWarps;
+    __shared__ __align__(16) float slots[2 * WARPS * 4];
     __shared__ __align__(8) uint64_t bars[WARPS * S];
     __shared__ int dead;
-    extern __shared__ __align__(16) uint8_t rings[];     // after the tokens: [teams of the CTA][D] sums
     check_offsets(a.offsets, a.B, a.T, a.err);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     Team team{p.team_warps, warp % p.team_warps, warp / p.team_warps, slots, 0, WARPS};
     const int cta_teams = WARPS / p.team_warps;
     const int64_t number = (int64_t)blockIdx.x * cta_teams + team.id;
-    const int64_t t0 = min(a.T, number * p.chunk), t1 = min(a.T, t0 + p.chunk);
+    const int t0 = (int)min(a.T, number * p.chunk), t1 = (int)min(a.T, number * p.chunk + p.chunk);
     const int col = (team.warp * 32 + lane) * N, step = p.team_warps * 32 * N;
     const float inv_d = 1.f / (float)a.D;
     const T *x = (const T*)g.x_out, *y = (const T*)g.y, *dxo = (const T*)g.d_x_out, *dn = (const T*)g.d_n;
     const T *gate = (const T*)a.gate, *wp = (const T*)a.w_post, *wn = (const T*)a.w_pre;
-    Ring rows{{x, y, dxo, dn}, rings + team.id * S * 4 * Ring::stride_of(a.D), bars + team.id * S, &dead, a.err, a.D,
-              Ring::stride_of(a.D)};
+    Ring rows(bars, &dead, a, team.id);
+    rows.p[0] = x;
+    rows.p[1] = y;
+    rows.p[2] = dxo;
+    rows.p[3] = dn;
     if (threadIdx.x == 0) {
         for (int i = 0; i < WARPS * S; ++i) mbar_init((uint32_t)__cvta_generic_to_shared(bars + i), 1);
         dead = 0;
@@ -363,7 +417,7 @@ __global__ void __launch_bounds__(WARPS * 32, 1) k_norm_join_grad(JoinArgs a, Jo
     for (int i = 0; i < NV; ++i)
 #pragma unroll
         for (int j = 0; j < kF; ++j) s_gate[i][j] = s_post[i][j] = s_pre[i][j] = both<F>(0.f);
-    Sequence seq{a.offsets, a.B, a.T, 0, 0};
+    Sequence seq{a.offsets, (int)a.B, (int)a.T, 0, 0};
     F gw[NV][kF];                                          // gate * w_post of the sequence
     auto load_gate = [&] {
 #pragma unroll
@@ -372,15 +426,17 @@ __global__ void __launch_bounds__(WARPS * 32, 1) k_norm_join_grad(JoinArgs a, Jo
             if (c >= a.D) continue;
             Pack<T, N> w, k;
             w.load(wp + c);
-            if (gate) k.load(gate + seq.b * a.D + c);
+            if (ALL || gate) k.load(gate + (int64_t)seq.b * a.D + c);
 #pragma unroll
-            for (int j = 0; j < kF; ++j) gw[i][j] = gate ? mul_(k.get(j), w.get(j)) : w.get(j);
+            for (int j = 0; j < kF; ++j) gw[i][j] = ALL || gate ? mul_(k.get(j), w.get(j)) : w.get(j);
         }
     };
     // s_gate, the sum of g u over the tokens of seq.b among this team's, goes to
     // its place and, times the gate, to s_post
+    int2 open = make_int2(-1, 0);
     auto flush = [&] {
         const bool head = seq.begin() < t0, goes_on = seq.end > t1;
+        if (goes_on && !head) open = make_int2(seq.b, seq.end);
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int c = col + i * step;
@@ -395,36 +451,37 @@ __global__ void __launch_bounds__(WARPS * 32, 1) k_norm_join_grad(JoinArgs a, Jo
                     w.load(wp + c);
 #pragma unroll
                     for (int j = 0; j < kF; ++j) o.set(j, mul_(w.get(j), s_gate[i][j]));
-                    o.store((T*)g.d_gate + seq.b * a.D + c);
+                    o.store((T*)g.d_gate + (int64_t)seq.b * a.D + c);
                 }
             }
             Pack<T, N> k;
-            if (gate) k.load(gate + seq.b * a.D + c);
+            if (ALL || gate) k.load(gate + (int64_t)seq.b * a.D + c);
 #pragma unroll
             for (int j = 0; j < kF; ++j) {
-                s_post[i][j] = fma_(gate ? k.get(j) : both<F>(1.f), s_gate[i][j], s_post[i][j]);
+                s_post[i][j] = fma_(ALL || gate ? k.get(j) : both<F>(1.f), s_gate[i][j], s_post[i][j]);
                 s_gate[i][j] = both<F>(0.f);
             }
         }
     };
-    if (t0 < t1 && gate) seq.start(t0);
-    if (t0 < t1 && y) load_gate();
+    if (t0 < t1 && (ALL || gate)) seq.start(t0);
+    if (t0 < t1 && (ALL || y)) load_gate();
     const F rho = both<F>(a.rho);
-    for (int64_t t = t0; t < t1; ++t) {
-        const int64_t at = t * a.D;
-        if (gate && seq.moved(t)) {
+    int first = t0;                                        // token of the place
+    for (int t = t0; t < t1; ++t) {
+        const int64_t at = (int64_t)t * a.D;
+        if ((ALL || gate) && seq.moved(t)) {
             flush();
             seq.move(t);
             load_gate();
         }
-        rows.wait(team);
+        if (t == first) rows.enter(team, t);
         F qx = both<F>(0.f), qz = both<F>(0.f), qy = both<F>(0.f);      // x'^2, z x', y^2
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int c = col + i * step;
             if (c >= a.D) continue;
-            if (dn) {
-                const Pack<T, N> r = rows.get(0, t, c), n = rows.get(3, t, c);
+            if (ALL || dn) {
+                const Pack<T, N> r = rows.get(0, c), n = rows.get(3, c);
                 Pack<T, N> w;
                 w.load(wn + c);
 #pragma unroll
@@ -434,14 +491,14 @@ __global__ void __launch_bounds__(WARPS * 32, 1) k_norm_join_grad(JoinArgs a, Jo
                     qz = fma_(mul_(n.get(j), w.get(j)), x_, qz);
                 }
             }
-            if (y) {
-                const Pack<T, N> r = rows.get(1, t, c);
+            if (ALL || y) {
+                const Pack<T, N> r = rows.get(1, c);
 #pragma unroll
                 for (int j = 0; j < kF; ++j) qy = fma_(r.get(j), r.get(j), qy);
             }
         }
-        const float4 q = team.sum(make_float4(total(qx), total(qz), total(qy), 0.f));
-        const float ix_ = dn ? rsqrtf(fmaf(q.x, inv_d, a.eps)) : 0.f, iy_ = rsqrtf(fmaf(q.z, inv_d, a.eps));
+        const float3 q = team.sum3(total(qx), total(qz), total(qy));
+        const float ix_ = ALL || dn ? rsqrtf(fmaf(q.x, inv_d, a.eps)) : 0.f, iy_ = rsqrtf(fmaf(q.z, inv_d, a.eps));
         const F ix = both<F>(ix_), along = both<F>(-ix_ * ix_ * ix_ * (q.y * inv_d)), iy = both<F>(iy_);
         F v[NV][kF], m = both<F>(0.f);                     // du / rms(y); du u
         Pack<T, N> ry[NV];
@@ -449,16 +506,16 @@ __global__ void __launch_bounds__(WARPS * 32, 1) k_norm_join_grad(JoinArgs a, Jo
         for (int i = 0; i < NV; ++i) {
             const int c = col + i * step;
             if (c >= a.D) continue;
-            if (dxo) {
-                const Pack<T, N> r = rows.get(2, t, c);
+            if (ALL || dxo) {
+                const Pack<T, N> r = rows.get(2, c);
 #pragma unroll
                 for (int j = 0; j < kF; ++j) v[i][j] = r.get(j);
             } else {
 #pragma unroll
                 for (int j = 0; j < kF; ++j) v[i][j] = both<F>(0.f);
             }
-            if (dn) {
-                const Pack<T, N> r = rows.get(0, t, c), n = rows.get(3, t, c);
+            if (ALL || dn) {
+                const Pack<T, N> r = rows.get(0, c), n = rows.get(3, c);
                 Pack<T, N> w;
                 w.load(wn + c);
 #pragma unroll
@@ -472,8 +529,8 @@ __global__ void __launch_bounds__(WARPS * 32, 1) k_norm_join_grad(JoinArgs a, Jo
 #pragma unroll
             for (int j = 0; j < kF; ++j) o.set(j, mul_(rho, v[i][j]));
             o.store((T*)g.dx + at + c);
-            if (y) {
-                ry[i] = rows.get(1, t, c);
+            if (ALL || y) {
+                ry[i] = rows.get(1, c);
 #pragma unroll
                 for (int j = 0; j < kF; ++j) {
                     const F y_ = ry[i].get(j), gi = mul_(v[i][j], iy);
@@ -483,9 +540,13 @@ __global__ void __launch_bounds__(WARPS * 32, 1) k_norm_join_grad(JoinArgs a, Jo
                 }
             }
         }
-        rows.leave(team, t, t1);
-        if (!y) continue;
-        const F back = both<F>(-iy_ * iy_ * (team.sum(make_float4(total(m), 0.f, 0.f, 0.f)).x * inv_d));
+        rows.next();
+        if (t + 1 == first + rows.per || t + 1 == t1) {
+            rows.leave(team, first, t1);
+            first = t + 1;
+        }
+        if (!ALL && !y) continue;
+        const F back = both<F>(-iy_ * iy_ * (team.sum(total(m)) * inv_d));
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int c = col + i * step;
@@ -497,9 +558,10 @@ __global__ void __launch_bounds__(WARPS * 32, 1) k_norm_join_grad(JoinArgs a, Jo
         }
     }
     rows.drain();
-    if (t0 < t1 && y) flush();
+    if (t0 < t1 && (ALL || y)) flush();
+    if (g.d_gate && team.warp == 0 && lane == 0) p.open[number] = open;
     // the CTA's sums for the norms' weights, teams in order
-    float* sums = reinterpret_cast<float*>(rings);
+    float* sums = reinterpret_cast<float*>(join_smem);     // [teams of the CTA][D]
     auto gather = [&](const F (&s)[NV][kF], float* to) {
         __syncthreads();
 #pragma unroll
@@ -515,8 +577,8 @@ __global__ void __launch_bounds__(WARPS * 32, 1) k_norm_join_grad(JoinArgs a, Jo
             to[c] = v;
         }
     };
-    if (y) gather(s_post, p.weights + (int64_t)blockIdx.x * 2 * a.D);
-    if (dn) gather(s_pre, p.weights + ((int64_t)blockIdx.x * 2 + 1) * a.D);
+    if (ALL || y) gather(s_post, p.weights + (int64_t)blockIdx.x * 2 * a.D);
+    if (ALL || dn) gather(s_pre, p.weights + ((int64_t)blockIdx.x * 2 + 1) * a.D);
 }
 
 // CTAs (128 columns each along y) of three kinds along x: 0 and 1 add the norms'
@@ -531,7 +593,7 @@ constexpr int kWarpRows = 16;            // partial sums that a warp adds by its
 template <class T>
 __global__ void __launch_bounds__(kFinishWarps * 32) k_join_finish(JoinArgs a, JoinGrads g, GradPlan p) {
     __shared__ float part[kFinishWarps][128];
-    __shared__ int64_t long_last[kFinishWarps];
+    __shared__ int2 long_run[kFinishWarps];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int c0 = blockIdx.y * 128;
     wait_before();
@@ -567,17 +629,13 @@ __global__ void __launch_bounds__(kFinishWarps * 32) k_join_finish(JoinArgs a, J
     const int64_t group = (int64_t)blockIdx.x - 2, groups = (p.teams + kFinishWarps - 1) / kFinishWarps;
     const T* wp = (const T*)a.w_post;
     if (group < groups) {
-        const int64_t k = group * kFinishWarps + warp, t0 = k * p.chunk, t1 = t0 + p.chunk;
-        int64_t last = -1, b = 0;
-        if (k < p.teams && t1 < a.T) {
-            b = sequence_of(a.offsets, a.B, t1 - 1);
-            const int64_t begin = a.offsets ? __ldg(a.offsets + b) : 0;
-            const int64_t end = a.offsets ? min(a.T, __ldg(a.offsets + b + 1)) : a.T;
-            if (begin >= t0 && end > t1) last = min(p.teams - 1, (end - 1) / p.chunk);
-        }
+        const int64_t k = group * kFinishWarps + warp;
+        int2 open = k < p.teams ? __ldcg(p.open + k) : make_int2(-1, 0);
+        open.y = (int)min(p.teams - 1, (int64_t)((open.y - 1) / (int)p.chunk));       // the last team with tokens of it
+        const int64_t b = open.x, last = open.x < 0 ? -1 : open.y;
         // this team's second row, then the first row of those that follow
         const bool alone = last - k <= kWarpRows;
-        if (lane == 0) long_last[warp] = alone ? -1 : last;
+        if (lane == 0) long_run[warp] = alone ? make_int2(-1, 0) : open;
         if (last >= 0 && alone) {
             float v[4] = {0.f, 0.f, 0.f, 0.f};
             add_rows(v, p.gates + a.D, 2 * a.D, k, k, 1);
@@ -590,9 +648,9 @@ __global__ void __launch_bounds__(kFinishWarps * 32) k_join_finish(JoinArgs a, J
         }
         __syncthreads();
         for (int w = 0; w < kFinishWarps; ++w) {
-            if (long_last[w] < 0) continue;
-            const int64_t kw = group * kFinishWarps + w, bw = sequence_of(a.offsets, a.B, kw * p.chunk + p.chunk - 1);
-            const float v = cta_rows(p.gates, 2 * a.D, kw + 1, long_last[w]);
+            if (long_run[w].x < 0) continue;
+            const int64_t kw = group * kFinishWarps + w, bw = long_run[w].x;
+            const float v = cta_rows(p.gates, 2 * a.D, kw + 1, long_run[w].y);
             if (threadIdx.x < 128 && c < a.D)
                 ((T*)g.d_gate)[bw * a.D + c] = from_f32<T>(to_f32(wp[c]) * (__ldcg(p.gates + (kw * 2 + 1) * a.D + c) + v));
         }
@@ -606,8 +664,8 @@ __global__ void __launch_bounds__(kFinishWarps * 32) k_join_finish(JoinArgs a, J
 
 // ---- host ------------------------------------------------------------------------
 
-// Elements per access: 16 bytes where every row of every array begins on 16,
-// 4 bytes for even widths of the 16-bit types
+// Elements per access: of 16, 8 or 4 bytes where every row of every array begins on
+// a multiple of that, else one
 template <class... P>
 int access_elems(const JoinArgs& a, P... arrays) {
     uintptr_t all = (uintptr_t)a.gate | (uintptr_t)a.w_post | (uintptr_t)a.w_pre;
@@ -615,7 +673,7 @@ int access_elems(const JoinArgs& a, P... arrays) {
     for (uintptr_t p : each) all |= p;
     const int e = (int)elem_bytes(a.type);
     all |= (uintptr_t)(a.D * e);
-    return all % 16 == 0 ? 16 / e : (all % 4 == 0 ? 4 / e : 1);
+    return all % 16 == 0 ? 16 / e : (all % 8 == 0 ? 8 / e : (all % 4 == 0 ? 4 / e : 1));
 }
 
 // Warps per team and accesses per lane for rows of D, N elements an access, at
@@ -651,7 +709,9 @@ using Counts = std::integer_sequence<int, NV...>;
 cudaError_t launch_norm_join(const JoinArgs& a, const void* x, const void* y, void* x_out, void* n_out,
                              cudaStream_t s) {
     const int N = access_elems(a, x, y, x_out, n_out);
-    const Shape sh = team_shape(a.D, N, kJoinColumns);
+    // short accesses take twice the registers: half the columns a warp, up to the CTA's warps
+    const bool whole = N * elem_bytes(a.type) == 16 || a.D > 8 * kJoinColumns / 2;
+    const Shape sh = team_shape(a.D, N, whole ? kJoinColumns : kJoinColumns / 2);
     auto go = [&](auto t, auto n, auto nv) {
         using T = decltype(t);
         const int cta_teams = kJoinThreads / 32 / sh.warps;
@@ -668,21 +728,23 @@ cudaError_t launch_norm_join(const JoinArgs& a, const void* x, const void* y, vo
     auto of16 = [&](auto t) {
         using T = decltype(t);
         if (N == 8) return pick<T, 8>(sh.accesses, Counts<1, 2, 4>(), go);
+        if (N == 4) return pick<T, 4>(sh.accesses, Counts<1, 4, 8>(), go);
         if (N == 2) return pick<T, 2>(sh.accesses, Counts<2, 8, 16>(), go);
         return pick<T, 1>(sh.accesses, Counts<4, 16, 32>(), go);
     };
     if (a.type == IFVS_T_F16) return of16(__half());
     if (a.type == IFVS_T_BF16) return of16(__nv_bfloat16());
-    return N == 4 ? pick<float, 4>(sh.accesses, Counts<1, 2, 4, 8>(), go)
-                  : pick<float, 1>(sh.accesses, Counts<4, 16, 32>(), go);
+    if (N == 4) return pick<float, 4>(sh.accesses, Counts<1, 2, 4, 8>(), go);
+    if (N == 2) return pick<float, 2>(sh.accesses, Counts<2, 8, 16>(), go);
+    return pick<float, 1>(sh.accesses, Counts<4, 16, 32>(), go);
 }
 
 namespace {
 GradPlan grad_plan(const JoinArgs& a) {
     GradPlan p{};
     p.team_warps = 1;
-    while (p.team_warps * kGradColumns < a.D) p.team_warps *= 2;
-    const int64_t cta_teams = grad_warps(a.type, a.D) / p.team_warps;
+    while (p.team_warps * grad_columns(a.type, a.D) < a.D) p.team_warps *= 2;
+    const int64_t cta_teams = kGradWarps / p.team_warps;
     const int64_t want = (a.T + cta_teams - 1) / cta_teams;
     p.ctas = (int)(want < a.num_sms ? want : a.num_sms);
     p.teams = p.ctas * cta_teams;
@@ -693,36 +755,36 @@ GradPlan grad_plan(const JoinArgs& a) {
 
 size_t norm_join_grad_bytes(const JoinArgs& a) {
     const GradPlan p = grad_plan(a);
-    return (size_t)(p.teams + p.ctas) * 2 * a.D * sizeof(float);
+    return (size_t)p.teams * sizeof(int2) + (size_t)(p.teams + p.ctas) * 2 * a.D * sizeof(float);
 }
 
 cudaError_t launch_norm_join_grad(const JoinArgs& a, const JoinGrads& g, uint8_t* work, cudaStream_t s) {
     const int N = access_elems(a, g.x_out, g.y, g.d_x_out, g.d_n, g.dx, g.dy, g.d_gate);
-    const Shape sh = team_shape(a.D, N, kGradColumns);
+    const Shape sh = team_shape(a.D, N, grad_columns(a.type, a.D));
     GradPlan p = grad_plan(a);
-    p.gates = (float*)work;
+    p.open = (int2*)work;
+    p.gates = (float*)(p.open + p.teams);
     p.weights = p.gates + p.teams * 2 * a.D;
     auto go = [&](auto t, auto n, auto nv) {
         using T = decltype(t);
-        auto rows = [&](auto warps, auto places) {
-            const auto kernel = k_norm_join_grad<T, n(), nv(), warps(), places()>;
-            const int cta_teams = warps() / p.team_warps;
+        auto rows = [&](auto places) {
+            const bool all = g.y && g.d_x_out && g.d_n && a.gate;
+            const auto kernel = all ? k_norm_join_grad<T, n(), nv(), places(), true> : k_norm_join_grad<T, n(), nv(), places(), false>;
+            const int cta_teams = kGradWarps / p.team_warps;
             size_t smem = ring_bytes<T, n(), 4, places()>(cta_teams, a.D);
             const size_t sums = (size_t)cta_teams * a.D * sizeof(float);
             smem = smem > sums ? smem : sums;
             const cudaError_t r = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
             if (r != cudaSuccess) return r;
-            kernel<<<(unsigned)p.ctas, warps() * 32, smem, s>>>(a, g, p);
+            kernel<<<(unsigned)p.ctas, kGradWarps * 32, smem, s>>>(a, g, p);
             return cudaGetLastError();
         };
         cudaError_t e = cudaSuccess;
-        if (a.T == 0) {
-        } else if constexpr (sizeof(T) == 2) {
-            e = rows(Count<16>(), Count<kStages>());
-        } else if (grad_warps(a.type, a.D) == 8) {
-            e = rows(Count<8>(), Count<kStages>());
-        } else if constexpr (n() * nv() == 16) {
-            e = rows(Count<16>(), Count<1>());
+        if (a.T > 0) {
+            if constexpr (sizeof(T) == 4 && n() * nv() == 16)
+                e = rows(Count<1>());
+            else
+                e = rows(Count<kStages>());
         }
         if (e != cudaSuccess) return e;
         const int64_t teams = g.d_gate ? p.teams : 0, clears = g.d_gate && a.offsets ? (a.B + kClearRows - 1) / kClearRows : 0;
@@ -734,8 +796,9 @@ cudaError_t launch_norm_join_grad(const JoinArgs& a, const JoinGrads& g, uint8_t
     auto of16 = [&](auto t) {
         using T = decltype(t);
         if (N == 8) return pick<T, 8>(sh.accesses, Counts<1, 2>(), go);
-        if (N == 2) return pick<T, 2>(sh.accesses, Counts<2, 8>(), go);
-        return pick<T, 1>(sh.accesses, Counts<4, 16>(), go);
+        if (N == 4) return pick<T, 4>(sh.accesses, Counts<1, 2, 4>(), go);
+        if (N == 2) return pick<T, 2>(sh.accesses, Counts<2, 4, 8>(), go);
+        return pick<T, 1>(sh.accesses, Counts<4, 8, 16>(), go);
     };
     if (a.T == 0 && g.d_gate) {     // no team: the gates' gradients are all zeros
         const cudaError_t e = cudaMemsetAsync(g.d_gate, 0, (size_t)a.B * a.D * elem_bytes(a.type), s);
@@ -743,7 +806,9 @@ cudaError_t launch_norm_join_grad(const JoinArgs& a, const JoinGrads& g, uint8_t
     }
     if (a.type == IFVS_T_F16) return of16(__half());
     if (a.type == IFVS_T_BF16) return of16(__nv_bfloat16());
-    return N == 4 ? pick<float, 4>(sh.accesses, Counts<1, 2, 4>(), go) : pick<float, 1>(sh.accesses, Counts<4, 16>(), go);
+    if (N == 4) return pick<float, 4>(sh.accesses, Counts<1, 2, 4>(), go);
+    if (N == 2) return pick<float, 2>(sh.accesses, Counts<2, 4, 8>(), go);
+    return pick<float, 1>(sh.accesses, Counts<4, 8, 16>(), go);
 }
 
 }  // namespace ifvs
