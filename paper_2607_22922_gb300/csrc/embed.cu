@@ -12,6 +12,7 @@
 // found by a search in the sorted ids and set to zero.  Every row is written
 // once, no order depends on timing.
 #include "layers.cuh"
+#include "scan_common.cuh"
 
 namespace ifvs {
 
@@ -178,30 +179,36 @@ k_sort_cluster(EmbedArgs a, SortPlan plan, Pairs p0, Pairs p1, int rounds) {
     for (int pass = 0; pass < plan.passes; ++pass) {
         const Pairs in = pass == 0 ? Pairs{nullptr, nullptr} : (pass & 1 ? p0 : p1);
         const Pairs out = pass & 1 ? p1 : p0;
-        for (int i = lane; i < kBins; i += 32) hist[warp][i] = 0;
+        for (int i = lane; i < (1 << plan.bits); i += 32) hist[warp][i] = 0;
         WarpKeys k;
         load_keys(k, a, in, first, left, lane);
         __syncwarp();
         rank_keys(k, plan, pass, left, lane, hist[warp]);
         __syncthreads();
-        const int d = threadIdx.x;
-        if (d < kBins) {
-            uint32_t sum = 0;
+        const int d = threadIdx.x, bins = 1 << plan.bits;
+        if (d < bins) {
+            uint32_t n[kClusterWarps], sum = 0;
+#pragma unroll
+            for (int w = 0; w < kClusterWarps; ++w) n[w] = hist[w][d];
+#pragma unroll
             for (int w = 0; w < kClusterWarps; ++w) {
-                const uint32_t n = hist[w][d];
                 hist[w][d] = sum;
-                sum += n;
+                sum += n[w];
             }
             total[d] = sum;
         }
         cluster_sync();
         uint32_t all = 0, before = 0;
-        if (d < kBins)
-            for (uint32_t c = 0; c < ctas; ++c) {
-                const uint32_t n = load_of(&total[d], c);
-                before += c < cta ? n : 0u;
-                all += n;
+        if (d < bins) {
+            uint32_t n[kClusterMax];
+#pragma unroll
+            for (uint32_t c = 0; c < kClusterMax; ++c) n[c] = c < ctas ? load_of(&total[d], c) : 0u;
+#pragma unroll
+            for (uint32_t c = 0; c < kClusterMax; ++c) {
+                before += c < cta ? n[c] : 0u;
+                all += n[c];
             }
+        }
         const uint32_t start = scan256(all, warp_sums);
         if (d < kBins) base[d] = start + before;
         __syncthreads();
@@ -278,11 +285,13 @@ k_sort_scatter(EmbedArgs a, SortPlan plan, int pass, Pairs in, Pairs out, const 
     const uint32_t start = scan256(__ldcg(totals + d), warp_sums);
     base[d] = start + __ldcg(counts + (int64_t)d * tiles + blockIdx.x);
     __syncthreads();
-    uint32_t sum = base[d];
+    uint32_t n[kTileWarps], sum = base[d];
+#pragma unroll
+    for (int w = 0; w < kTileWarps; ++w) n[w] = hist[w][d];
+#pragma unroll
     for (int w = 0; w < kTileWarps; ++w) {
-        const uint32_t n = hist[w][d];
         hist[w][d] = sum;
-        sum += n;
+        sum += n[w];
     }
     __syncthreads();
 #pragma unroll
@@ -298,125 +307,224 @@ k_sort_scatter(EmbedArgs a, SortPlan plan, int pass, Pairs in, Pairs out, const 
 struct SumPlan {
     int part;            // tokens per part (a multiple of 32)
     int64_t parts;
-    int slices;          // of the columns
+    int slices, width;   // of the columns, columns per slice
     int64_t sum_warps;   // parts x slices
     int64_t zero_warps;  // of 32 rows of the table
 };
 
-// this lane's columns of slice s: NV vectors of N
-template <class T, int N, int NV>
-__device__ __forceinline__ int column(int s, int i, int lane) {
-    return ((s * NV + i) * 32 + lane) * N;
+// Clears the rows that no token names: a lane looks for its row of the 32 from
+// v0 in the sorted ids, the warp clears.
+template <class T, int N>
+__device__ __forceinline__ void clear_absent(const EmbedArgs& a, Pairs sorted, int64_t v0, T* __restrict__ d_table) {
+    const int lane = threadIdx.x & 31;
+    const int64_t v = v0 + lane;
+    bool absent = false;
+    if (v < a.V) {
+        int64_t lo = 0, hi = a.T;                    // the first place with a key >= v
+        while (lo < hi) {
+            const int64_t m = (lo + hi) >> 1;
+            if (__ldcg(sorted.key + m) < (uint32_t)v)
+                lo = m + 1;
+            else
+                hi = m;
+        }
+        absent = lo == a.T || __ldcg(sorted.key + lo) != (uint32_t)v;
+    }
+    uint32_t rows = __ballot_sync(0xFFFFFFFFu, absent);
+    Pack<T, N> zero;
+#pragma unroll
+    for (int j = 0; j < Pack<T, N>::kF; ++j) zero.set(j, both<typename Pack<T, N>::F>(0.f));
+    for (; rows; rows &= rows - 1u) {
+        T* row = d_table + (v0 + __ffs(rows) - 1) * a.D;
+        for (int c = lane * N; c < a.D; c += 32 * N) zero.store(row + c);
+    }
 }
 
+// One warp's sums over its part: NV accesses of N columns from `col`, 32 N apart,
+// below `limit`.
 // Partial sums [parts][2][D]: of the run that reaches into the part from before
 // (0) and of the one that begins in it and goes on (1).
 template <class T, int N, int NV>
-__global__ void __launch_bounds__(256, NV == 1 ? 4 : 2)
+struct RunSums {
+    using F = typename Pack<T, N>::F;
+    static constexpr int kF = Pack<T, N>::kF;
+    F sum[NV][kF];
+    int64_t run = -1, part, before;     // the run's key; the key before the part
+    bool head = false;
+    int col, limit;
+
+    __device__ __forceinline__ void clear() {
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+            for (int j = 0; j < kF; ++j) sum[i][j] = both<F>(0.f);
+    }
+    __device__ __forceinline__ void flush(const EmbedArgs& a, bool goes_on, float* partial, T* d_table) {
+        if (run < 0 || run >= a.V) return;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int c = col + i * 32 * N;
+            if (c >= limit) continue;
+            if (head || goes_on) {
+                float* to = partial + (part * 2 + (head ? 0 : 1)) * a.D + c;
+#pragma unroll
+                for (int j = 0; j < kF; ++j) *reinterpret_cast<F*>(to + j * (N / kF)) = sum[i][j];
+            } else {
+                Pack<T, N> v;
+#pragma unroll
+                for (int j = 0; j < kF; ++j) v.set(j, mul_(both<F>(a.scale), sum[i][j]));
+                v.store(d_table + run * a.D + c);
+            }
+        }
+    }
+    // the next token's row; first: it is the part's first token
+    __device__ __forceinline__ void add(const EmbedArgs& a, uint32_t key, bool first, const Pack<T, N> (&v)[NV], float* partial,
+                                        T* d_table) {
+        if (key >= a.V) return;          // no row, or beyond the part
+        if ((int64_t)key != run) {
+            flush(a, false, partial, d_table);
+            clear();
+            run = key;
+            head = first && before == run;
+        }
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+            for (int j = 0; j < kF; ++j) sum[i][j] = add_(sum[i][j], v[i].get(j));
+    }
+};
+
+// Rows on 16 bytes: a warp has kHalf rows (of its slice) on their way into each
+// of two halves of its shared memory, a bulk copy per lane and row, while it adds
+// those of the other.  Measured at 400009 rows of 768 bytes: loads into registers,
+// 8 in flight a warp, 87 us; the same as a ring of 8, 179 us (a use waits for
+// the loads after its own too).
+constexpr int kHalf = 16;
+constexpr int kSumWarps = 4;
+constexpr int kSliceBytes = 512;
+
+template <class T>
+__global__ void __launch_bounds__(kSumWarps * 32)
+k_embed_sum_rows(const T* __restrict__ d_out, EmbedArgs a, SumPlan p, Pairs sorted, float* __restrict__ partial,
+                 T* __restrict__ d_table) {
+    constexpr int N = 16 / (int)sizeof(T);
+    extern __shared__ __align__(16) uint8_t halves[];        // [kSumWarps][2][kHalf][kSliceBytes]
+    __shared__ __align__(8) uint64_t bars[kSumWarps][2];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int64_t job = (int64_t)blockIdx.x * kSumWarps + warp;
+    start_dependents();
+    if (lane < 2) mbar_init((uint32_t)__cvta_generic_to_shared(&bars[warp][lane]), 1);
+    fence_mbar_init();
+    __syncwarp();
+    wait_before();
+    if (job >= p.sum_warps) {
+        if (job - p.sum_warps < p.zero_warps) clear_absent<T, N>(a, sorted, (job - p.sum_warps) * 32, d_table);
+        return;
+    }
+    const int64_t part = job / p.slices, begin = part * p.part, end = min(a.T, begin + p.part);
+    const int c0 = (int)(job - part * p.slices) * p.width;
+    RunSums<T, N, 1> r;
+    r.part = part;
+    r.before = begin > 0 ? (int64_t)__ldcg(sorted.key + begin - 1) : -1;
+    r.col = c0 + lane * N;
+    r.limit = min(a.D, c0 + p.width);
+    r.clear();
+    const uint32_t bytes = (uint32_t)(r.limit - c0) * (uint32_t)sizeof(T);
+    uint8_t* mine = halves + warp * (2 * kHalf * kSliceBytes);
+    const uint32_t mine_at = (uint32_t)__cvta_generic_to_shared(mine), bar = (uint32_t)__cvta_generic_to_shared(bars[warp]);
+    const uint64_t once = policy_evict_first();
+    auto keys_at = [&](int64_t b) { return b + lane < end ? __ldcg(sorted.key + b + lane) : 0xFFFFFFFFu; };
+    auto places_at = [&](int64_t b) { return b + lane < end ? __ldcg(sorted.pos + b + lane) : 0u; };
+    // the rows of half h of the 32 tokens whose keys and places these are
+    auto fetch = [&](int h, uint32_t key, uint32_t pos) {
+        const bool mine_too = lane / kHalf == h && key < a.V;
+        const uint32_t rows = __popc(__ballot_sync(0xFFFFFFFFu, mine_too));
+        if (lane == 0) mbar_arrive_expect_tx(bar + 8 * h, rows * bytes);
+        __syncwarp();
+        if (mine_too)
+            bulk_g2s(mine_at + lane * kSliceBytes, d_out + (int64_t)pos * a.D + c0, bytes, bar + 8 * h, once);
+    };
+    uint32_t key = keys_at(begin), pos = places_at(begin), next_key = keys_at(begin + 32), next_pos = places_at(begin + 32);
+    fetch(0, key, pos);
+    fetch(1, key, pos);
+    bool late = false;
+    uint32_t parity = 0;
+    for (int64_t b = begin; b < end; b += 32, parity ^= 1u) {
+#pragma unroll 1
+        for (int h = 0; h < 2; ++h) {
+            // a wait that runs out: the sums go on with what is there and are reported
+            if (!late && !mbar_wait_warp(bar + 8 * h, parity)) {
+                late = true;
+                if (lane == 0) *a.err = kErrWait;
+            }
+#pragma unroll 1
+            for (int i0 = 0; i0 < kHalf; i0 += 8) {
+                Pack<T, N> v[8][1];
+#pragma unroll
+                for (int u = 0; u < 8; ++u)
+                    v[u][0].w = *reinterpret_cast<const uint4*>(mine + (h * kHalf + i0 + u) * kSliceBytes + lane * 16);
+#pragma unroll
+                for (int u = 0; u < 8; ++u) {
+                    const int i = h * kHalf + i0 + u;
+                    r.add(a, __shfl_sync(0xFFFFFFFFu, key, i), b + i == begin, v[u], partial, d_table);
+                }
+            }
+            fence_proxy_async_smem();
+            __syncwarp();
+            if (b + 32 < end) fetch(h, next_key, next_pos);
+        }
+        key = next_key;
+        pos = next_pos;
+        next_key = keys_at(b + 64);
+        next_pos = places_at(b + 64);
+    }
+    r.flush(a, end < a.T && (int64_t)__ldcg(sorted.key + end) == r.run, partial, d_table);
+    if (late)                            // copies in flight: bounded
+        for (int h = 0; h < 2; ++h) mbar_wait_warp(bar + 8 * h, parity ^ 1u);
+}
+
+// Rows of any alignment: element loads into registers, kAhead rows at a time
+template <class T>
+__global__ void __launch_bounds__(256, 2)
 k_embed_sum(const T* __restrict__ d_out, EmbedArgs a, SumPlan p, Pairs sorted, float* __restrict__ partial,
             T* __restrict__ d_table) {
-    using F = typename Pack<T, N>::F;
-    constexpr int kF = Pack<T, N>::kF;
-    constexpr int AHEAD = NV == 1 ? 8 : 4;               // rows in flight
+    constexpr int NV = 8, kAhead = 4;
     const int lane = threadIdx.x & 31;
     const int64_t job = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
     start_dependents();
     wait_before();
     if (job >= p.sum_warps) {
-        // rows without tokens: a lane looks for its row, the warp clears
-        const int64_t v = (job - p.sum_warps) * 32 + lane;
-        bool absent = false;
-        if (job - p.sum_warps < p.zero_warps && v < a.V) {
-            int64_t lo = 0, hi = a.T;                    // the first place with a key >= v
-            while (lo < hi) {
-                const int64_t m = (lo + hi) >> 1;
-                if (__ldcg(sorted.key + m) < (uint32_t)v)
-                    lo = m + 1;
-                else
-                    hi = m;
-            }
-            absent = lo == a.T || __ldcg(sorted.key + lo) != (uint32_t)v;
-        }
-        uint32_t rows = __ballot_sync(0xFFFFFFFFu, absent);
-        Pack<T, N> zero;
-#pragma unroll
-        for (int j = 0; j < kF; ++j) zero.set(j, both<F>(0.f));
-        for (; rows; rows &= rows - 1u) {
-            T* row = d_table + (v - lane + __ffs(rows) - 1) * a.D;
-            for (int c = lane * N; c < a.D; c += 32 * N) zero.store(row + c);
-        }
+        if (job - p.sum_warps < p.zero_warps) clear_absent<T, 1>(a, sorted, (job - p.sum_warps) * 32, d_table);
         return;
     }
-    const int64_t part = job / p.slices;
-    const int slice = (int)(job - part * p.slices);
-    const int64_t begin = part * p.part, end = min(a.T, begin + p.part);
-    F sum[NV][kF];
-    int64_t run = -1;                                    // the run's key
-    bool head = false;
-    auto clear = [&] {
-#pragma unroll
-        for (int i = 0; i < NV; ++i)
-#pragma unroll
-            for (int j = 0; j < kF; ++j) sum[i][j] = both<F>(0.f);
-    };
-    auto flush = [&](bool goes_on) {
-        if (run < 0 || run >= a.V) return;
-        if (head || goes_on) {
-            float* to = partial + (part * 2 + (head ? 0 : 1)) * a.D;
-#pragma unroll
-            for (int i = 0; i < NV; ++i) {
-                const int c = column<T, N, NV>(slice, i, lane);
-#pragma unroll
-                for (int j = 0; j < kF; ++j)
-                    if (c < a.D) *reinterpret_cast<F*>(to + c + j * (N / kF)) = sum[i][j];
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < NV; ++i) {
-                const int c = column<T, N, NV>(slice, i, lane);
-                Pack<T, N> v;
-#pragma unroll
-                for (int j = 0; j < kF; ++j) v.set(j, mul_(both<F>(a.scale), sum[i][j]));
-                if (c < a.D) v.store(d_table + run * a.D + c);
-            }
-        }
-    };
-    clear();
-    const int64_t before = begin > 0 ? (int64_t)__ldcg(sorted.key + begin - 1) : -1;
+    const int64_t part = job / p.slices, begin = part * p.part, end = min(a.T, begin + p.part);
+    RunSums<T, 1, NV> r;
+    r.part = part;
+    r.before = begin > 0 ? (int64_t)__ldcg(sorted.key + begin - 1) : -1;
+    r.col = (int)(job - part * p.slices) * p.width + lane;
+    r.limit = a.D;
+    r.clear();
     for (int64_t b = begin; b < end; b += 32) {
         const bool in = b + lane < end;
         const uint32_t key = in ? __ldcg(sorted.key + b + lane) : 0xFFFFFFFFu;
         const uint32_t pos = in ? __ldcg(sorted.pos + b + lane) : 0u;
         const int n = (int)min((int64_t)32, end - b);
-        for (int i0 = 0; i0 < n; i0 += AHEAD) {
-            Pack<T, N> v[AHEAD][NV];
-            uint32_t k[AHEAD];
+        for (int i0 = 0; i0 < n; i0 += kAhead) {
+            Pack<T, 1> v[kAhead][NV];
+            // without conditions, so that all loads are issued before the first is
+            // used: places beyond the part read row 0, columns beyond D the last
 #pragma unroll
-            for (int u = 0; u < AHEAD; ++u) {
-                // without conditions, so that all loads are issued before the first
-                // is used: places beyond the part read row 0, columns beyond D the last
-                k[u] = __shfl_sync(0xFFFFFFFFu, key, i0 + u);
+            for (int u = 0; u < kAhead; ++u) {
                 const T* row = d_out + (int64_t)__shfl_sync(0xFFFFFFFFu, pos, i0 + u) * a.D;
 #pragma unroll
-                for (int i = 0; i < NV; ++i) v[u][i].load(row + min(column<T, N, NV>(slice, i, lane), a.D - N));
+                for (int i = 0; i < NV; ++i) v[u][i].load(row + min(r.col + i * 32, a.D - 1));
             }
 #pragma unroll
-            for (int u = 0; u < AHEAD; ++u) {
-                if (k[u] >= a.V) continue;           // no row, or beyond the part
-                if ((int64_t)k[u] != run) {
-                    flush(false);
-                    clear();
-                    run = k[u];
-                    head = b + i0 + u == begin && before == run;
-                }
-#pragma unroll
-                for (int i = 0; i < NV; ++i)
-#pragma unroll
-                    for (int j = 0; j < kF; ++j) sum[i][j] = add_(sum[i][j], v[u][i].get(j));
-            }
+            for (int u = 0; u < kAhead; ++u)
+                r.add(a, __shfl_sync(0xFFFFFFFFu, key, i0 + u), b + i0 + u == begin, v[u], partial, d_table);
         }
     }
-    flush(end < a.T && (int64_t)__ldcg(sorted.key + end) == run);
+    r.flush(a, end < a.T && (int64_t)__ldcg(sorted.key + end) == r.run, partial, d_table);
 }
 
 // Runs over several parts: a CTA per part in which one begins (and 128 columns)
@@ -463,13 +571,13 @@ k_embed_join(EmbedArgs a, SumPlan p, Pairs sorted, const float* __restrict__ par
 }
 
 // Parts long enough that their partial sums are few against the rows, short
-// enough that every SM has 16 warps of them
-template <class T, int N, int NV>
-SumPlan sum_plan(const EmbedArgs& a) {
+// enough that every SM has `warps` of them
+SumPlan sum_plan(const EmbedArgs& a, int most_columns, int multiple, int warps) {
     SumPlan p;
-    p.slices = (a.D + 32 * N * NV - 1) / (32 * N * NV);
+    p.slices = (a.D + most_columns - 1) / most_columns;
+    p.width = ((a.D + p.slices - 1) / p.slices + multiple - 1) / multiple * multiple;
     p.part = 32;
-    while (p.part < 256 && a.T / (2 * p.part) * p.slices >= 16 * a.num_sms) p.part *= 2;
+    while (p.part < 256 && a.T / (2 * p.part) * p.slices >= (int64_t)warps * a.num_sms) p.part *= 2;
     p.parts = (a.T + p.part - 1) / p.part;
     p.sum_warps = p.parts * p.slices;
     p.zero_warps = (a.V + 31) / 32;
@@ -514,15 +622,26 @@ cudaError_t sort_by_id(const EmbedArgs& a, Pairs p0, Pairs p1, uint32_t* counts,
     return e;
 }
 
-template <class T, int N, int NV>
+template <class T>
 cudaError_t sum_by_id(const EmbedArgs& a, const void* d_out, Pairs sorted, float* partial, void* d_table, cudaStream_t s) {
-    const SumPlan p = sum_plan<T, N, NV>(a);
-    cudaError_t e = launch_kernel(k_embed_sum<T, N, NV>, dim3((unsigned)((p.sum_warps + p.zero_warps + 7) / 8)), dim3(256), 0,
-                                  true, s, (const T*)d_out, a, p, sorted, partial, (T*)d_table);
+    const bool rows = vectors(a, d_out, d_table);
+    constexpr int N = 16 / (int)sizeof(T);
+    const SumPlan p = rows ? sum_plan(a, kSliceBytes / (int)sizeof(T), N, 32) : sum_plan(a, 256, 256, 16);
+    const int64_t warps = p.sum_warps + p.zero_warps;
+    cudaError_t e;
+    if (rows) {
+        const size_t smem = (size_t)kSumWarps * 2 * kHalf * kSliceBytes;
+        e = cudaFuncSetAttribute(k_embed_sum_rows<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        if (e == cudaSuccess)
+            e = launch_kernel(k_embed_sum_rows<T>, dim3((unsigned)((warps + kSumWarps - 1) / kSumWarps)), dim3(kSumWarps * 32),
+                              smem, true, s, (const T*)d_out, a, p, sorted, partial, (T*)d_table);
+    } else {
+        e = launch_kernel(k_embed_sum<T>, dim3((unsigned)((warps + 7) / 8)), dim3(256), 0, true, s, (const T*)d_out, a, p, sorted,
+                          partial, (T*)d_table);
+    }
     if (e == cudaSuccess && p.parts > 1)
         e = launch_kernel(k_embed_join<T>, dim3((unsigned)(p.parts - 1), (unsigned)((a.D + 127) / 128)), dim3(256), 0, true, s,
-                          a, p, sorted,
-                          (const float*)partial, (T*)d_table);
+                          a, p, sorted, (const float*)partial, (T*)d_table);
     return e;
 }
 
@@ -565,8 +684,7 @@ cudaError_t launch_embed_grad(const EmbedArgs& a, const void* d_out, void* d_tab
     if (e != cudaSuccess) return e;
     return with_type(a.type, [&](auto z) {
         using T = decltype(z);
-        if (vectors(a, d_out, d_table)) return sum_by_id<T, 16 / (int)sizeof(T), 1>(a, d_out, sorted, partial, d_table, s);
-        return sum_by_id<T, 1, 8>(a, d_out, sorted, partial, d_table, s);
+        return sum_by_id<T>(a, d_out, sorted, partial, d_table, s);
     });
 }
 
