@@ -60,7 +60,7 @@ k_embed(const T* __restrict__ table, EmbedArgs a, T* __restrict__ out) {
 // Least significant digit first, digits of equal width of at most 8 bits; the
 // key of a token without a row is V.
 constexpr int kBins = 256;
-constexpr int kSortRounds = 8;                       // keys per lane
+constexpr int kSortRounds = 8;                       // keys per lane, at most
 
 struct SortPlan {
     int passes, bits;
@@ -86,16 +86,18 @@ __device__ __forceinline__ uint32_t key_of(const EmbedArgs& a, int64_t i) {
     return (uint32_t)a.V;
 }
 
-// The keys of a warp's kSortRounds x 32 places from `first` (absent beyond n),
+// The keys of a warp's R x 32 places from `first` (absent beyond n),
 // with their rank among the warp's earlier keys of the same digit; counts in
 // hist [kBins].  Lanes of equal digits find each other by a ballot per bit.
+template <int R>
 struct WarpKeys {
-    uint32_t key[kSortRounds], pos[kSortRounds];
-    uint16_t rank[kSortRounds];
+    uint32_t key[R], pos[R];
+    uint16_t rank[R];
 };
-__device__ __forceinline__ void load_keys(WarpKeys& k, const EmbedArgs& a, Pairs in, int64_t first, int64_t left, int lane) {
+template <int R>
+__device__ __forceinline__ void load_keys(WarpKeys<R>& k, const EmbedArgs& a, Pairs in, int64_t first, int64_t left, int lane) {
 #pragma unroll
-    for (int j = 0; j < kSortRounds; ++j) {
+    for (int j = 0; j < R; ++j) {
         const int64_t i = first + j * 32 + lane;
         k.key[j] = k.pos[j] = 0;
         if (j * 32 + lane >= left) continue;
@@ -109,10 +111,11 @@ __device__ __forceinline__ void load_keys(WarpKeys& k, const EmbedArgs& a, Pairs
         }
     }
 }
-__device__ __forceinline__ void rank_keys(WarpKeys& k, const SortPlan& plan, int pass, int64_t left, int lane,
+template <int R>
+__device__ __forceinline__ void rank_keys(WarpKeys<R>& k, const SortPlan& plan, int pass, int64_t left, int lane,
                                           uint32_t* hist) {
 #pragma unroll
-    for (int j = 0; j < kSortRounds; ++j) {
+    for (int j = 0; j < R; ++j) {
         if (j * 32 >= left) break;
         const bool in = j * 32 + lane < left;
         const uint32_t d = plan.digit(k.key[j], pass);
@@ -180,7 +183,7 @@ k_sort_cluster(EmbedArgs a, SortPlan plan, Pairs p0, Pairs p1, int rounds) {
         const Pairs in = pass == 0 ? Pairs{nullptr, nullptr} : (pass & 1 ? p0 : p1);
         const Pairs out = pass & 1 ? p1 : p0;
         for (int i = lane; i < (1 << plan.bits); i += 32) hist[warp][i] = 0;
-        WarpKeys k;
+        WarpKeys<kSortRounds> k;
         load_keys(k, a, in, first, left, lane);
         __syncwarp();
         rank_keys(k, plan, pass, left, lane, hist[warp]);
@@ -226,7 +229,8 @@ k_sort_cluster(EmbedArgs a, SortPlan plan, Pairs p0, Pairs p1, int rounds) {
 // More tokens: per pass the digits' counts of every tile of kTileTokens, their
 // sums over the tiles before, and the scatter.
 constexpr int kTileWarps = 8;
-constexpr int kTileTokens = kTileWarps * 32 * kSortRounds;   // 2048
+constexpr int kTileRounds = 4;
+constexpr int kTileTokens = kTileWarps * 32 * kTileRounds;   // 1024: more CTAs, each a chain of latencies
 
 // counts [kBins][tiles]
 __global__ void __launch_bounds__(kTileWarps * 32)
@@ -238,7 +242,7 @@ k_sort_count(EmbedArgs a, SortPlan plan, int pass, Pairs in, uint32_t* __restric
     if (pass > 0) wait_before();
     const int64_t first = (int64_t)blockIdx.x * kTileTokens;
 #pragma unroll
-    for (int j = 0; j < kSortRounds; ++j) {
+    for (int j = 0; j < kTileRounds; ++j) {
         const int64_t i = first + j * (kTileWarps * 32) + threadIdx.x;
         if (i < a.T) atomicAdd(&hist[plan.digit(in.key ? __ldcg(in.key + i) : key_of(a, i), pass)], 1u);
     }
@@ -275,9 +279,9 @@ k_sort_scatter(EmbedArgs a, SortPlan plan, int pass, Pairs in, Pairs out, const 
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, d = threadIdx.x;
     start_dependents();
     for (int i = lane; i < kBins; i += 32) hist[warp][i] = 0;
-    const int64_t first = (int64_t)blockIdx.x * kTileTokens + warp * (32 * kSortRounds);
+    const int64_t first = (int64_t)blockIdx.x * kTileTokens + warp * (32 * kTileRounds);
     wait_before();
-    WarpKeys k;
+    WarpKeys<kTileRounds> k;
     const int64_t left = a.T - first;
     load_keys(k, a, in, first, left, lane);
     __syncwarp();
@@ -295,7 +299,7 @@ k_sort_scatter(EmbedArgs a, SortPlan plan, int pass, Pairs in, Pairs out, const 
     }
     __syncthreads();
 #pragma unroll
-    for (int j = 0; j < kSortRounds; ++j)
+    for (int j = 0; j < kTileRounds; ++j)
         if (j * 32 + lane < left) {
             const uint32_t at = hist[warp][plan.digit(k.key[j], pass)] + k.rank[j];
             out.key[at] = k.key[j];
@@ -344,23 +348,26 @@ __device__ __forceinline__ void clear_absent(const EmbedArgs& a, Pairs sorted, i
 // below `limit`.
 // Partial sums [parts][2][D]: of the run that reaches into the part from before
 // (0) and of the one that begins in it and goes on (1).
+constexpr uint32_t kNoKey = 0xFFFFFFFFu;
+
 template <class T, int N, int NV>
 struct RunSums {
     using F = typename Pack<T, N>::F;
     static constexpr int kF = Pack<T, N>::kF;
     F sum[NV][kF];
-    int64_t run = -1, part, before;     // the run's key; the key before the part
+    int64_t part;
+    uint32_t run = kNoKey, last;        // the run's key; the key before the next token
     bool head = false;
     int col, limit;
 
-    __device__ __forceinline__ void clear() {
-#pragma unroll
-        for (int i = 0; i < NV; ++i)
-#pragma unroll
-            for (int j = 0; j < kF; ++j) sum[i][j] = both<F>(0.f);
+    __device__ __forceinline__ void start(const EmbedArgs& a, Pairs sorted, int64_t part_, int64_t begin, int col_, int limit_) {
+        part = part_;
+        col = col_;
+        limit = limit_;
+        last = begin > 0 ? __ldcg(sorted.key + begin - 1) : kNoKey;
     }
     __device__ __forceinline__ void flush(const EmbedArgs& a, bool goes_on, float* partial, T* d_table) {
-        if (run < 0 || run >= a.V) return;
+        if (run == kNoKey) return;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int c = col + i * 32 * N;
@@ -373,42 +380,54 @@ struct RunSums {
                 Pack<T, N> v;
 #pragma unroll
                 for (int j = 0; j < kF; ++j) v.set(j, mul_(both<F>(a.scale), sum[i][j]));
-                v.store(d_table + run * a.D + c);
+                v.store(d_table + (int64_t)run * a.D + c);
             }
         }
     }
-    // the next token's row; first: it is the part's first token
-    __device__ __forceinline__ void add(const EmbedArgs& a, uint32_t key, bool first, const Pack<T, N> (&v)[NV], float* partial,
-                                        T* d_table) {
-        if (key >= a.V) return;          // no row, or beyond the part
-        if ((int64_t)key != run) {
+    // Of 32 tokens with these keys (sorted; kNoKey beyond the part): which begin a
+    // run of this part (bit per token), and how many have a row.
+    __device__ __forceinline__ uint32_t starts(const EmbedArgs& a, uint32_t key, bool first, int* rows) {
+        const int lane = threadIdx.x & 31;
+        uint32_t prev = __shfl_up_sync(0xFFFFFFFFu, key, 1);
+        if (lane == 0) prev = first ? kNoKey : last;
+        const uint32_t some = __ballot_sync(0xFFFFFFFFu, key < a.V);
+        *rows = __popc(some);
+        return __ballot_sync(0xFFFFFFFFu, key != prev) & some;
+    }
+    // the row of token i of the 32
+    __device__ __forceinline__ void add(const EmbedArgs& a, uint32_t starts, uint32_t key, int i, bool first,
+                                        const Pack<T, N> (&v)[NV], float* partial, T* d_table) {
+        if (starts >> i & 1u) {
             flush(a, false, partial, d_table);
-            clear();
-            run = key;
-            head = first && before == run;
+            run = __shfl_sync(0xFFFFFFFFu, key, i);
+            head = first && i == 0 && last == run;
+#pragma unroll
+            for (int k = 0; k < NV; ++k)
+#pragma unroll
+                for (int j = 0; j < kF; ++j) sum[k][j] = v[k].get(j);
+        } else {
+#pragma unroll
+            for (int k = 0; k < NV; ++k)
+#pragma unroll
+                for (int j = 0; j < kF; ++j) sum[k][j] = add_(sum[k][j], v[k].get(j));
         }
-#pragma unroll
-        for (int i = 0; i < NV; ++i)
-#pragma unroll
-            for (int j = 0; j < kF; ++j) sum[i][j] = add_(sum[i][j], v[i].get(j));
     }
 };
 
-// Rows on 16 bytes: a warp has kHalf rows (of its slice) on their way into each
+// Rows on 16 bytes: a warp has 16 / NV rows (of its slice) on their way into each
 // of two halves of its shared memory, a bulk copy per lane and row, while it adds
 // those of the other.  Measured at 400009 rows of 768 bytes: loads into registers,
 // 8 in flight a warp, 87 us; the same as a ring of 8, 179 us (a use waits for
 // the loads after its own too).
-constexpr int kHalf = 16;
 constexpr int kSumWarps = 4;
-constexpr int kSliceBytes = 512;
+constexpr int kSliceBytes = 512;         // per NV
 
-template <class T>
+template <class T, int NV>
 __global__ void __launch_bounds__(kSumWarps * 32)
 k_embed_sum_rows(const T* __restrict__ d_out, EmbedArgs a, SumPlan p, Pairs sorted, float* __restrict__ partial,
                  T* __restrict__ d_table) {
-    constexpr int N = 16 / (int)sizeof(T);
-    extern __shared__ __align__(16) uint8_t halves[];        // [kSumWarps][2][kHalf][kSliceBytes]
+    constexpr int N = 16 / (int)sizeof(T), HALF = 16 / NV, GROUPS = 32 / HALF, ROW = kSliceBytes * NV;
+    extern __shared__ __align__(16) uint8_t halves[];        // [kSumWarps][2][HALF][ROW]
     __shared__ __align__(8) uint64_t bars[kSumWarps][2];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int64_t job = (int64_t)blockIdx.x * kSumWarps + warp;
@@ -423,62 +442,74 @@ k_embed_sum_rows(const T* __restrict__ d_out, EmbedArgs a, SumPlan p, Pairs sort
     }
     const int64_t part = job / p.slices, begin = part * p.part, end = min(a.T, begin + p.part);
     const int c0 = (int)(job - part * p.slices) * p.width;
-    RunSums<T, N, 1> r;
-    r.part = part;
-    r.before = begin > 0 ? (int64_t)__ldcg(sorted.key + begin - 1) : -1;
-    r.col = c0 + lane * N;
-    r.limit = min(a.D, c0 + p.width);
-    r.clear();
+    RunSums<T, N, NV> r;
+    r.start(a, sorted, part, begin, c0 + lane * N, min(a.D, c0 + p.width));
     const uint32_t bytes = (uint32_t)(r.limit - c0) * (uint32_t)sizeof(T);
-    uint8_t* mine = halves + warp * (2 * kHalf * kSliceBytes);
+    uint8_t* mine = halves + warp * (2 * HALF * ROW);
     const uint32_t mine_at = (uint32_t)__cvta_generic_to_shared(mine), bar = (uint32_t)__cvta_generic_to_shared(bars[warp]);
     const uint64_t once = policy_evict_first();
-    auto keys_at = [&](int64_t b) { return b + lane < end ? __ldcg(sorted.key + b + lane) : 0xFFFFFFFFu; };
+    auto keys_at = [&](int64_t b) { return b + lane < end ? __ldcg(sorted.key + b + lane) : kNoKey; };
     auto places_at = [&](int64_t b) { return b + lane < end ? __ldcg(sorted.pos + b + lane) : 0u; };
-    // the rows of half h of the 32 tokens whose keys and places these are
-    auto fetch = [&](int h, uint32_t key, uint32_t pos) {
-        const bool mine_too = lane / kHalf == h && key < a.V;
-        const uint32_t rows = __popc(__ballot_sync(0xFFFFFFFFu, mine_too));
-        if (lane == 0) mbar_arrive_expect_tx(bar + 8 * h, rows * bytes);
+    // the rows of group g of the 32 tokens whose keys and places these are, to half g & 1
+    auto fetch = [&](int g, uint32_t key, uint32_t pos) {
+        const bool its = lane / HALF == g && key < a.V;
+        const uint32_t rows = __popc(__ballot_sync(0xFFFFFFFFu, its)), to = bar + 8 * (g & 1);
+        if (lane == 0) mbar_arrive_expect_tx(to, rows * bytes);
         __syncwarp();
-        if (mine_too)
-            bulk_g2s(mine_at + lane * kSliceBytes, d_out + (int64_t)pos * a.D + c0, bytes, bar + 8 * h, once);
+        if (its) bulk_g2s(mine_at + lane % (2 * HALF) * ROW, d_out + (int64_t)pos * a.D + c0, bytes, to, once);
     };
     uint32_t key = keys_at(begin), pos = places_at(begin), next_key = keys_at(begin + 32), next_pos = places_at(begin + 32);
     fetch(0, key, pos);
     fetch(1, key, pos);
     bool late = false;
     uint32_t parity = 0;
-    for (int64_t b = begin; b < end; b += 32, parity ^= 1u) {
+    for (int64_t b = begin; b < end; b += 32) {
+        int rows;
+        const uint32_t starts = r.starts(a, key, b == begin, &rows);
 #pragma unroll 1
-        for (int h = 0; h < 2; ++h) {
+        for (int g = 0; g < GROUPS; ++g) {
             // a wait that runs out: the sums go on with what is there and are reported
-            if (!late && !mbar_wait_warp(bar + 8 * h, parity)) {
+            if (!late && !mbar_wait_warp(bar + 8 * (g & 1), parity)) {
                 late = true;
                 if (lane == 0) *a.err = kErrWait;
             }
+            parity ^= (uint32_t)g & 1u;
+            auto row = [&](Pack<T, N>(&v)[NV], int i) {
+#pragma unroll
+                for (int k = 0; k < NV; ++k)
+                    v[k].w = *reinterpret_cast<const uint4*>(mine + i % (2 * HALF) * ROW + (k * 32 + lane) * 16);
+            };
 #pragma unroll 1
-            for (int i0 = 0; i0 < kHalf; i0 += 8) {
-                Pack<T, N> v[8][1];
+            for (int i0 = g * HALF; i0 < min(rows, (g + 1) * HALF); i0 += 8) {
+                if (i0 + 8 <= rows) {
+                    Pack<T, N> v[8][NV];
 #pragma unroll
-                for (int u = 0; u < 8; ++u)
-                    v[u][0].w = *reinterpret_cast<const uint4*>(mine + (h * kHalf + i0 + u) * kSliceBytes + lane * 16);
+                    for (int u = 0; u < 8; ++u) row(v[u], i0 + u);
 #pragma unroll
-                for (int u = 0; u < 8; ++u) {
-                    const int i = h * kHalf + i0 + u;
-                    r.add(a, __shfl_sync(0xFFFFFFFFu, key, i), b + i == begin, v[u], partial, d_table);
+                    for (int u = 0; u < 8; ++u) r.add(a, starts, key, i0 + u, b == begin, v[u], partial, d_table);
+                } else {
+#pragma unroll 1
+                    for (int i = i0; i < rows; ++i) {
+                        Pack<T, N> v[NV];
+                        row(v, i);
+                        r.add(a, starts, key, i, b == begin, v, partial, d_table);
+                    }
                 }
             }
             fence_proxy_async_smem();
             __syncwarp();
-            if (b + 32 < end) fetch(h, next_key, next_pos);
+            if (g + 2 < GROUPS)
+                fetch(g + 2, key, pos);
+            else if (b + 32 < end)
+                fetch(g + 2 - GROUPS, next_key, next_pos);
         }
+        r.last = __shfl_sync(0xFFFFFFFFu, key, 31);
         key = next_key;
         pos = next_pos;
         next_key = keys_at(b + 64);
         next_pos = places_at(b + 64);
     }
-    r.flush(a, end < a.T && (int64_t)__ldcg(sorted.key + end) == r.run, partial, d_table);
+    r.flush(a, end < a.T && __ldcg(sorted.key + end) == r.run, partial, d_table);
     if (late)                            // copies in flight: bounded
         for (int h = 0; h < 2; ++h) mbar_wait_warp(bar + 8 * h, parity ^ 1u);
 }
@@ -499,20 +530,17 @@ k_embed_sum(const T* __restrict__ d_out, EmbedArgs a, SumPlan p, Pairs sorted, f
     }
     const int64_t part = job / p.slices, begin = part * p.part, end = min(a.T, begin + p.part);
     RunSums<T, 1, NV> r;
-    r.part = part;
-    r.before = begin > 0 ? (int64_t)__ldcg(sorted.key + begin - 1) : -1;
-    r.col = (int)(job - part * p.slices) * p.width + lane;
-    r.limit = a.D;
-    r.clear();
+    r.start(a, sorted, part, begin, (int)(job - part * p.slices) * p.width + lane, a.D);
     for (int64_t b = begin; b < end; b += 32) {
         const bool in = b + lane < end;
-        const uint32_t key = in ? __ldcg(sorted.key + b + lane) : 0xFFFFFFFFu;
+        const uint32_t key = in ? __ldcg(sorted.key + b + lane) : kNoKey;
         const uint32_t pos = in ? __ldcg(sorted.pos + b + lane) : 0u;
-        const int n = (int)min((int64_t)32, end - b);
-        for (int i0 = 0; i0 < n; i0 += kAhead) {
+        int rows;
+        const uint32_t starts = r.starts(a, key, b == begin, &rows);
+        for (int i0 = 0; i0 < rows; i0 += kAhead) {
             Pack<T, 1> v[kAhead][NV];
             // without conditions, so that all loads are issued before the first is
-            // used: places beyond the part read row 0, columns beyond D the last
+            // used: places without a row read another, columns beyond D the last
 #pragma unroll
             for (int u = 0; u < kAhead; ++u) {
                 const T* row = d_out + (int64_t)__shfl_sync(0xFFFFFFFFu, pos, i0 + u) * a.D;
@@ -521,34 +549,25 @@ k_embed_sum(const T* __restrict__ d_out, EmbedArgs a, SumPlan p, Pairs sorted, f
             }
 #pragma unroll
             for (int u = 0; u < kAhead; ++u)
-                r.add(a, __shfl_sync(0xFFFFFFFFu, key, i0 + u), b + i0 + u == begin, v[u], partial, d_table);
+                if (i0 + u < rows) r.add(a, starts, key, i0 + u, b == begin, v[u], partial, d_table);
         }
+        r.last = __shfl_sync(0xFFFFFFFFu, key, 31);
     }
-    r.flush(a, end < a.T && (int64_t)__ldcg(sorted.key + end) == r.run, partial, d_table);
+    r.flush(a, end < a.T && __ldcg(sorted.key + end) == r.run, partial, d_table);
 }
 
-// Runs over several parts: a CTA per part in which one begins (and 128 columns)
-// adds its partial sums, a warp every eighth part
+// Runs over several parts: a warp per part in which one begins (and 128 columns)
+// adds its partial sums; the CTA together those of long runs.
+constexpr int kWarpParts = 16;           // parts that a warp adds by itself
+
 template <class T>
 __global__ void __launch_bounds__(256)
 k_embed_join(EmbedArgs a, SumPlan p, Pairs sorted, const float* __restrict__ partial, T* __restrict__ d_table) {
     __shared__ float part_sum[8][128];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    __shared__ uint32_t long_run[8];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c0 = blockIdx.y * 128;
     wait_before();
-    const int64_t part = blockIdx.x, begin = part * p.part, end = begin + p.part;
-    const uint32_t run = __ldcg(sorted.key + end - 1), next = __ldcg(sorted.key + end);    // parts but the last are whole
-    const uint32_t first = __ldcg(sorted.key + begin), before = __ldcg(sorted.key + max(begin - 1, (int64_t)0));
-    if (run >= a.V || next != run || (begin > 0 && first == run && before == run)) return;
-    // the parts that follow and begin with the run
-    int64_t more = 1;
-    for (;;) {
-        const int64_t q = part + 1 + more + threadIdx.x;
-        const int n = __syncthreads_count(q < p.parts && __ldcg(sorted.key + q * p.part) == run);
-        more += n;
-        if (n < 256) break;
-    }
-    const int c0 = blockIdx.y * 128;
-    float sum[4] = {0.f, 0.f, 0.f, 0.f};
+    float sum[4];
     auto add = [&](const float* from) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
@@ -556,17 +575,61 @@ k_embed_join(EmbedArgs a, SumPlan p, Pairs sorted, const float* __restrict__ par
             if (c < a.D) sum[j] += __ldcg(from + c);
         }
     };
-    if (warp == 0) add(partial + (part * 2 + 1) * a.D);
-#pragma unroll 4
-    for (int64_t q = part + 1 + warp; q <= part + more; q += 8) add(partial + q * 2 * a.D);
+    auto key_at = [&](int64_t i) { return __ldcg(sorted.key + i); };
+    const int64_t part = (int64_t)blockIdx.x * 8 + warp;
+    uint32_t its = kNoKey;               // the run that begins in this part and goes on
+    if (part + 1 < p.parts) {            // parts but the last are whole
+        const int64_t begin = part * p.part, end = begin + p.part;
+        const uint32_t run = key_at(end - 1), next = key_at(end), first = key_at(begin), before = key_at(max(begin - 1, (int64_t)0));
+        if (run < a.V && next == run && !(begin > 0 && first == run && before == run)) its = run;
+    }
+    // the parts after the next that begin with the run
+    int more = 1;
+    if (its != kNoKey) {
+        const int64_t q = part + 2 + lane;
+        more += __popc(__ballot_sync(0xFFFFFFFFu, q < p.parts && key_at(q * p.part) == its));
+    }
+    const bool alone = more <= kWarpParts;
+    if (lane == 0) long_run[warp] = alone ? kNoKey : its;
+    if (its != kNoKey && alone) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) part_sum[warp][j * 32 + lane] = sum[j];
+        for (int j = 0; j < 4; ++j) sum[j] = 0.f;
+        add(partial + (part * 2 + 1) * a.D);
+#pragma unroll 4
+        for (int64_t q = part + 1; q <= part + more; ++q) add(partial + q * 2 * a.D);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int c = c0 + j * 32 + lane;
+            if (c < a.D) d_table[(int64_t)its * a.D + c] = from_f32<T>(a.scale * sum[j]);
+        }
+    }
     __syncthreads();
-    const int c = c0 + threadIdx.x;
-    if (threadIdx.x < 128 && c < a.D) {
-        float total = 0.f;
-        for (int w = 0; w < 8; ++w) total += part_sum[w][threadIdx.x];
-        d_table[(int64_t)run * a.D + c] = from_f32<T>(a.scale * total);
+    for (int w = 0; w < 8; ++w) {
+        const uint32_t run = long_run[w];
+        if (run == kNoKey) continue;
+        const int64_t k = (int64_t)blockIdx.x * 8 + w;
+        int64_t many = 1;
+        for (;;) {
+            const int64_t q = k + 1 + many + threadIdx.x;
+            const int n = __syncthreads_count(q < p.parts && key_at(q * p.part) == run);
+            many += n;
+            if (n < 256) break;
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) sum[j] = 0.f;
+        if (warp == 0) add(partial + (k * 2 + 1) * a.D);
+#pragma unroll 4
+        for (int64_t q = k + 1 + warp; q <= k + many; q += 8) add(partial + q * 2 * a.D);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) part_sum[warp][j * 32 + lane] = sum[j];
+        __syncthreads();
+        const int c = c0 + threadIdx.x;
+        if (threadIdx.x < 128 && c < a.D) {
+            float all = 0.f;
+            for (int v = 0; v < 8; ++v) all += part_sum[v][threadIdx.x];
+            d_table[(int64_t)run * a.D + c] = from_f32<T>(a.scale * all);
+        }
+        __syncthreads();
     }
 }
 
@@ -624,23 +687,24 @@ cudaError_t sort_by_id(const EmbedArgs& a, Pairs p0, Pairs p1, uint32_t* counts,
 
 template <class T>
 cudaError_t sum_by_id(const EmbedArgs& a, const void* d_out, Pairs sorted, float* partial, void* d_table, cudaStream_t s) {
-    const bool rows = vectors(a, d_out, d_table);
+    const bool rows = vectors(a, d_out, d_table), wide = a.D * sizeof(T) > kSliceBytes;
     constexpr int N = 16 / (int)sizeof(T);
-    const SumPlan p = rows ? sum_plan(a, kSliceBytes / (int)sizeof(T), N, 32) : sum_plan(a, 256, 256, 16);
+    const SumPlan p = rows ? sum_plan(a, kSliceBytes * (wide ? 2 : 1) / (int)sizeof(T), N, 16) : sum_plan(a, 256, 256, 16);
     const int64_t warps = p.sum_warps + p.zero_warps;
     cudaError_t e;
     if (rows) {
-        const size_t smem = (size_t)kSumWarps * 2 * kHalf * kSliceBytes;
-        e = cudaFuncSetAttribute(k_embed_sum_rows<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        const size_t smem = (size_t)kSumWarps * 2 * 16 * kSliceBytes;
+        const auto kernel = wide ? k_embed_sum_rows<T, 2> : k_embed_sum_rows<T, 1>;
+        e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
         if (e == cudaSuccess)
-            e = launch_kernel(k_embed_sum_rows<T>, dim3((unsigned)((warps + kSumWarps - 1) / kSumWarps)), dim3(kSumWarps * 32),
-                              smem, true, s, (const T*)d_out, a, p, sorted, partial, (T*)d_table);
+            e = launch_kernel(kernel, dim3((unsigned)((warps + kSumWarps - 1) / kSumWarps)), dim3(kSumWarps * 32), smem, true, s,
+                              (const T*)d_out, a, p, sorted, partial, (T*)d_table);
     } else {
         e = launch_kernel(k_embed_sum<T>, dim3((unsigned)((warps + 7) / 8)), dim3(256), 0, true, s, (const T*)d_out, a, p, sorted,
                           partial, (T*)d_table);
     }
     if (e == cudaSuccess && p.parts > 1)
-        e = launch_kernel(k_embed_join<T>, dim3((unsigned)(p.parts - 1), (unsigned)((a.D + 127) / 128)), dim3(256), 0, true, s,
+        e = launch_kernel(k_embed_join<T>, dim3((unsigned)((p.parts + 7) / 8), (unsigned)((a.D + 127) / 128)), dim3(256), 0, true, s,
                           a, p, sorted, (const float*)partial, (T*)d_table);
     return e;
 }
