@@ -57,9 +57,10 @@ k_embed(const T* __restrict__ table, EmbedArgs a, T* __restrict__ out) {
 }
 
 // ---- sort by id ------------------------------------------------------------------
-// Least significant digit first, digits of equal width of at most 8 bits; the
-// key of a token without a row is V.
-constexpr int kBins = 256;
+// Least significant digit first, digits of equal width of at most 9 bits (tables
+// below 2^18 rows in two passes; a pass costs three launches); the key of a
+// token without a row is V.
+constexpr int kDigitBits = 9, kBins = 1 << kDigitBits;
 constexpr int kSortRounds = 8;                       // keys per lane, at most
 
 struct SortPlan {
@@ -71,7 +72,7 @@ struct SortPlan {
 SortPlan sort_plan(int64_t V) {
     int bits = 1;
     while ((1ll << bits) <= V) ++bits;               // keys 0..V
-    const int passes = (bits + 7) / 8;
+    const int passes = (bits + kDigitBits - 1) / kDigitBits;
     return {passes, (bits + passes - 1) / passes};
 }
 
@@ -133,27 +134,44 @@ __device__ __forceinline__ void rank_keys(WarpKeys<R>& k, const SortPlan& plan, 
     }
 }
 
-// exclusive sums of 256 values, by the first 256 threads of a block (all of it calls)
-__device__ __forceinline__ uint32_t scan256(uint32_t v, uint32_t* warp_sums) {
+// Exclusive sums of kBins values, two neighbours for each of the first kBins / 2
+// threads (the whole block calls): the sum before the first of the two.
+constexpr int kScanThreads = kBins / 2;
+__device__ __forceinline__ uint32_t scan_bins(uint32_t v0, uint32_t v1, uint32_t* warp_sums) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const uint32_t v = v0 + v1;
     uint32_t s = v;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
         const uint32_t u = __shfl_up_sync(0xFFFFFFFFu, s, o);
         if (lane >= o) s += u;
     }
-    if (lane == 31 && warp < 8) warp_sums[warp] = s;
+    if (lane == 31 && warp < kScanThreads / 32) warp_sums[warp] = s;
     __syncthreads();
     uint32_t base = 0;
-    for (int i = 0; i < min(warp, 8); ++i) base += warp_sums[i];
+    for (int i = 0; i < min(warp, kScanThreads / 32); ++i) base += warp_sums[i];
     return base + s - v;
 }
 
-// Up to kClusterTokens tokens: one cluster sorts them in one launch.  Each of its
+// In each bin of a block's W histograms the counts of the warps before, from
+// `start`; returns the bin's total
+template <int W>
+__device__ __forceinline__ uint32_t stack_counts(uint32_t (*hist)[kBins], int bin, uint32_t start) {
+    uint32_t n[W], sum = start;
+#pragma unroll
+    for (int w = 0; w < W; ++w) n[w] = hist[w][bin];
+#pragma unroll
+    for (int w = 0; w < W; ++w) {
+        hist[w][bin] = sum;
+        sum += n[w];
+    }
+    return sum - start;
+}
+
+// Up to 65536 tokens: one cluster sorts them in one launch.  Each of its
 // CTAs owns a segment; the digits' counts meet through distributed shared memory.
-constexpr int kClusterWarps = 16;
 constexpr int kClusterMax = 8;
-constexpr int64_t kClusterTokens = (int64_t)kClusterMax * kClusterWarps * 32 * kSortRounds;    // 32768
+constexpr int64_t cluster_tokens(int warps) { return (int64_t)kClusterMax * warps * 32 * kSortRounds; }   // 65536 at 32
 
 __device__ __forceinline__ uint32_t cluster_size() {
     uint32_t v;
@@ -170,50 +188,45 @@ __device__ __forceinline__ uint32_t load_of(const uint32_t* p, uint32_t cta) {
     return v;
 }
 
-__global__ void __launch_bounds__(kClusterWarps * 32, 1)
+// W warps a CTA: 16 where they suffice (17408 tokens: 25 us for the whole gradient, 28 with 32)
+template <int W>
+__global__ void __launch_bounds__(W * 32, 1)
 k_sort_cluster(EmbedArgs a, SortPlan plan, Pairs p0, Pairs p1, int rounds) {
-    __shared__ uint32_t hist[kClusterWarps][kBins];
-    __shared__ uint32_t total[kBins], base[kBins], warp_sums[8];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    extern __shared__ uint32_t sort_smem[];
+    uint32_t(*hist)[kBins] = reinterpret_cast<uint32_t(*)[kBins]>(sort_smem);      // [W]
+    __shared__ uint32_t total[kBins], base[kBins], warp_sums[kScanThreads / 32];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, bins = 1 << plan.bits;
     const uint32_t cta = blockIdx.x, ctas = cluster_size();
-    const int64_t first = ((int64_t)cta * kClusterWarps + warp) * 32 * rounds;
+    const int64_t first = ((int64_t)cta * W + warp) * 32 * rounds;
     const int64_t left = min(a.T - first, (int64_t)32 * rounds);
     start_dependents();
     for (int pass = 0; pass < plan.passes; ++pass) {
         const Pairs in = pass == 0 ? Pairs{nullptr, nullptr} : (pass & 1 ? p0 : p1);
         const Pairs out = pass & 1 ? p1 : p0;
-        for (int i = lane; i < (1 << plan.bits); i += 32) hist[warp][i] = 0;
+        for (int i = lane; i < bins; i += 32) hist[warp][i] = 0;
         WarpKeys<kSortRounds> k;
         load_keys(k, a, in, first, left, lane);
         __syncwarp();
         rank_keys(k, plan, pass, left, lane, hist[warp]);
         __syncthreads();
-        const int d = threadIdx.x, bins = 1 << plan.bits;
-        if (d < bins) {
-            uint32_t n[kClusterWarps], sum = 0;
-#pragma unroll
-            for (int w = 0; w < kClusterWarps; ++w) n[w] = hist[w][d];
-#pragma unroll
-            for (int w = 0; w < kClusterWarps; ++w) {
-                hist[w][d] = sum;
-                sum += n[w];
-            }
-            total[d] = sum;
-        }
+        for (int d = threadIdx.x; d < kBins; d += W * 32) total[d] = d < bins ? stack_counts<W>(hist, d, 0) : 0u;
         cluster_sync();
-        uint32_t all = 0, before = 0;
-        if (d < bins) {
-            uint32_t n[kClusterMax];
+        uint32_t all[2] = {0, 0}, before[2] = {0, 0};
+        const int d0 = threadIdx.x * 2;
+        if (d0 < bins)
 #pragma unroll
-            for (uint32_t c = 0; c < kClusterMax; ++c) n[c] = c < ctas ? load_of(&total[d], c) : 0u;
+            for (uint32_t c = 0; c < kClusterMax; ++c)
 #pragma unroll
-            for (uint32_t c = 0; c < kClusterMax; ++c) {
-                before += c < cta ? n[c] : 0u;
-                all += n[c];
-            }
+                for (int j = 0; j < 2; ++j) {
+                    const uint32_t n = c < ctas ? load_of(&total[d0 + j], c) : 0u;
+                    before[j] += c < cta ? n : 0u;
+                    all[j] += n;
+                }
+        const uint32_t start = scan_bins(all[0], all[1], warp_sums);
+        if (d0 < bins) {
+            base[d0] = start + before[0];
+            base[d0 + 1] = start + all[0] + before[1];
         }
-        const uint32_t start = scan256(all, warp_sums);
-        if (d < kBins) base[d] = start + before;
         __syncthreads();
 #pragma unroll
         for (int j = 0; j < kSortRounds; ++j)
@@ -236,7 +249,7 @@ constexpr int kTileTokens = kTileWarps * 32 * kTileRounds;   // 1024: more CTAs,
 __global__ void __launch_bounds__(kTileWarps * 32)
 k_sort_count(EmbedArgs a, SortPlan plan, int pass, Pairs in, uint32_t* __restrict__ counts, int tiles) {
     __shared__ uint32_t hist[kBins];
-    hist[threadIdx.x] = 0;
+    for (int d = threadIdx.x; d < kBins; d += kTileWarps * 32) hist[d] = 0;
     __syncthreads();
     start_dependents();
     if (pass > 0) wait_before();
@@ -247,14 +260,16 @@ k_sort_count(EmbedArgs a, SortPlan plan, int pass, Pairs in, uint32_t* __restric
         if (i < a.T) atomicAdd(&hist[plan.digit(in.key ? __ldcg(in.key + i) : key_of(a, i), pass)], 1u);
     }
     __syncthreads();
-    counts[(int64_t)threadIdx.x * tiles + blockIdx.x] = hist[threadIdx.x];
+    for (int d = threadIdx.x; d < 1 << plan.bits; d += kTileWarps * 32) counts[(int64_t)d * tiles + blockIdx.x] = hist[d];
 }
 
 // a warp per digit: exclusive sums over the tiles, and the digit's total
-__global__ void __launch_bounds__(256) k_sort_scan(uint32_t* __restrict__ counts, int tiles, uint32_t* __restrict__ totals) {
+__global__ void __launch_bounds__(256)
+k_sort_scan(uint32_t* __restrict__ counts, int bins, int tiles, uint32_t* __restrict__ totals) {
     start_dependents();
     wait_before();
     const int lane = threadIdx.x & 31, d = blockIdx.x * 8 + (threadIdx.x >> 5);
+    if (d >= bins) return;
     uint32_t* c = counts + (int64_t)d * tiles;
     uint32_t sum = 0;
     for (int i0 = 0; i0 < tiles; i0 += 32) {
@@ -275,27 +290,29 @@ __global__ void __launch_bounds__(256) k_sort_scan(uint32_t* __restrict__ counts
 __global__ void __launch_bounds__(kTileWarps * 32)
 k_sort_scatter(EmbedArgs a, SortPlan plan, int pass, Pairs in, Pairs out, const uint32_t* __restrict__ counts,
                int tiles, const uint32_t* __restrict__ totals) {
-    __shared__ uint32_t hist[kTileWarps][kBins], warp_sums[8], base[kBins];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, d = threadIdx.x;
+    __shared__ uint32_t hist[kTileWarps][kBins], warp_sums[kScanThreads / 32];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, bins = 1 << plan.bits;
     start_dependents();
-    for (int i = lane; i < kBins; i += 32) hist[warp][i] = 0;
+    for (int i = lane; i < bins; i += 32) hist[warp][i] = 0;
     const int64_t first = (int64_t)blockIdx.x * kTileTokens + warp * (32 * kTileRounds);
     wait_before();
+    const int d0 = threadIdx.x * 2;
+    uint32_t all[2] = {0, 0}, before[2] = {0, 0};
+    if (d0 < bins)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            all[j] = __ldcg(totals + d0 + j);
+            before[j] = __ldcg(counts + (int64_t)(d0 + j) * tiles + blockIdx.x);
+        }
     WarpKeys<kTileRounds> k;
     const int64_t left = a.T - first;
     load_keys(k, a, in, first, left, lane);
     __syncwarp();
     rank_keys(k, plan, pass, left, lane, hist[warp]);
-    const uint32_t start = scan256(__ldcg(totals + d), warp_sums);
-    base[d] = start + __ldcg(counts + (int64_t)d * tiles + blockIdx.x);
-    __syncthreads();
-    uint32_t n[kTileWarps], sum = base[d];
-#pragma unroll
-    for (int w = 0; w < kTileWarps; ++w) n[w] = hist[w][d];
-#pragma unroll
-    for (int w = 0; w < kTileWarps; ++w) {
-        hist[w][d] = sum;
-        sum += n[w];
+    const uint32_t start = scan_bins(all[0], all[1], warp_sums);     // with a barrier: every warp has ranked
+    if (d0 < bins) {
+        stack_counts<kTileWarps>(hist, d0, start + before[0]);
+        stack_counts<kTileWarps>(hist, d0 + 1, start + all[0] + before[1]);
     }
     __syncthreads();
 #pragma unroll
@@ -558,7 +575,7 @@ k_embed_sum(const T* __restrict__ d_out, EmbedArgs a, SumPlan p, Pairs sorted, f
 
 // Runs over several parts: a warp per part in which one begins (and 128 columns)
 // adds its partial sums; the CTA together those of long runs.
-constexpr int kWarpParts = 16;           // parts that a warp adds by itself
+constexpr int kWarpParts = 8;            // parts that a warp adds by itself (17408 tokens: 28 us; 31 with 32)
 
 template <class T>
 __global__ void __launch_bounds__(256)
@@ -595,7 +612,7 @@ k_embed_join(EmbedArgs a, SumPlan p, Pairs sorted, const float* __restrict__ par
 #pragma unroll
         for (int j = 0; j < 4; ++j) sum[j] = 0.f;
         add(partial + (part * 2 + 1) * a.D);
-#pragma unroll 4
+#pragma unroll 8
         for (int64_t q = part + 1; q <= part + more; ++q) add(partial + q * 2 * a.D);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
@@ -653,23 +670,28 @@ int64_t sort_tiles(const EmbedArgs& a) { return (a.T + kTileTokens - 1) / kTileT
 cudaError_t sort_by_id(const EmbedArgs& a, Pairs p0, Pairs p1, uint32_t* counts, cudaStream_t s, Pairs* sorted) {
     const SortPlan plan = sort_plan(a.V);
     *sorted = plan.passes & 1 ? p0 : p1;
-    if (a.T <= kClusterTokens) {
-        // the work of a pass is in its ranks: spread over the cluster's SMs, two
-        // rounds a warp at least
+    auto in_cluster = [&](auto warps) {
+        const auto kernel = k_sort_cluster<warps()>;
+        // the work of a pass is in its ranks: spread over the cluster's SMs
         int ctas = 1;
-        while (ctas < kClusterMax && (int64_t)ctas * kClusterWarps * 64 < a.T) ctas *= 2;
-        const int rounds = (int)((a.T + ctas * kClusterWarps * 32 - 1) / (ctas * kClusterWarps * 32));
+        while (ctas < kClusterMax && (int64_t)ctas * warps() * 64 < a.T) ctas *= 2;
+        const int rounds = (int)((a.T + ctas * warps() * 32 - 1) / (ctas * warps() * 32));
         cudaLaunchConfig_t cfg = {};
         cfg.gridDim = dim3((unsigned)ctas);
-        cfg.blockDim = dim3(kClusterWarps * 32);
+        cfg.blockDim = dim3(warps() * 32);
+        cfg.dynamicSmemBytes = sizeof(uint32_t) * warps() * kBins;
+        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)cfg.dynamicSmemBytes);
+        if (e != cudaSuccess) return e;
         cfg.stream = s;
         cudaLaunchAttribute attr[1];
         attr[0].id = cudaLaunchAttributeClusterDimension;
         attr[0].val.clusterDim = {(unsigned)ctas, 1u, 1u};
         cfg.attrs = attr;
         cfg.numAttrs = 1;
-        return cudaLaunchKernelEx(&cfg, k_sort_cluster, a, plan, p0, p1, rounds);
-    }
+        return cudaLaunchKernelEx(&cfg, kernel, a, plan, p0, p1, rounds);
+    };
+    if (a.T <= cluster_tokens(16)) return in_cluster(std::integral_constant<int, 16>());
+    if (a.T <= cluster_tokens(32)) return in_cluster(std::integral_constant<int, 32>());
     const int tiles = (int)sort_tiles(a);
     uint32_t* totals = counts + (int64_t)kBins * tiles;
     cudaError_t e = cudaSuccess;
@@ -678,7 +700,8 @@ cudaError_t sort_by_id(const EmbedArgs& a, Pairs p0, Pairs p1, uint32_t* counts,
         const Pairs in = pass == 0 ? Pairs{nullptr, nullptr} : (pass & 1 ? p0 : p1);
         const Pairs out = pass & 1 ? p1 : p0;
         then(launch_kernel(k_sort_count, dim3(tiles), dim3(kTileWarps * 32), 0, pass > 0, s, a, plan, pass, in, counts, tiles));
-        then(launch_kernel(k_sort_scan, dim3(kBins / 8), dim3(256), 0, true, s, counts, tiles, totals));
+        then(launch_kernel(k_sort_scan, dim3((unsigned)(((1 << plan.bits) + 7) / 8)), dim3(256), 0, true, s, counts, 1 << plan.bits, tiles,
+                           totals));
         then(launch_kernel(k_sort_scatter, dim3(tiles), dim3(kTileWarps * 32), 0, true, s, a, plan, pass, in, out,
                            (const uint32_t*)counts, tiles, (const uint32_t*)totals));
     }

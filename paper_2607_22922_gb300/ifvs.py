@@ -9,6 +9,7 @@ memory.  No computation of the query path happens in Python: if
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import os
 
 import numpy as np
@@ -408,6 +409,7 @@ def ifvs_get_conditioning(ix, B, Mr, W_shape):
 
 _ACTS = {"silu": IFVS_ACT_SILU, "gelu": IFVS_ACT_GELU, "relu": IFVS_ACT_RELU}
 _TYPES = {}         # torch's element types -> IFVS_T_*, filled on first use
+_INTS = {}          # and its integer types -> their names
 _LEGACY_STREAM = 1  # cudaStreamLegacy: the default stream as a non-NULL handle
 
 
@@ -420,6 +422,14 @@ def _type(a):
         t = _TYPES[a.dtype] = {"float32": IFVS_T_F32, "float16": IFVS_T_F16,
                                "bfloat16": IFVS_T_BF16}[name]
     return t
+
+
+def _is_vector(a, name):
+    """Whether ``a`` is a vector of this integer type."""
+    t = _INTS.get(a.dtype)
+    if t is None:
+        t = _INTS[a.dtype] = str(a.dtype).replace("torch.", "")
+    return t == name and a.dim() == 1
 
 
 def _dev(a, shape, dtype, name):
@@ -460,7 +470,7 @@ def ifvs_layers_status(L):
 
 
 def _ids(ids):
-    if str(ids.dtype) != "torch.int32" or ids.dim() != 1:
+    if not _is_vector(ids, "int32"):
         raise ValueError("ids must be a vector of int32")
     return int(ids.shape[0])
 
@@ -496,20 +506,14 @@ def _same_length(ids, T):
 
 def _join_params(x, gate, w_post, w_pre, offsets, res_scale, eps, stream):
     (T, D), dt = x.shape, x.dtype
-    p = JoinParams()
-    p.T, p.D, p.type = T, D, _type(x)
-    B = 1
+    B, at = 1, None
     if offsets is not None:
-        if str(offsets.dtype) != "torch.int64" or offsets.dim() != 1 or offsets.shape[0] < 2:
+        if not _is_vector(offsets, "int64") or offsets.shape[0] < 2:
             raise ValueError("offsets must be a vector of B + 1 int64")
-        B = int(offsets.shape[0]) - 1
-        p.offsets = _dev(offsets, (B + 1,), offsets.dtype, "offsets")
-    p.n_seq = B
-    p.gate = _dev(gate, (B, D), dt, "gate")
-    p.w_post = _dev(w_post, (D,), dt, "w_post")
-    p.w_pre = _dev(w_pre, (D,), dt, "w_pre")
-    p.res_scale, p.eps = res_scale, eps
-    p.stream = _stream(stream)
+        B = offsets.shape[0] - 1
+        at = _dev(offsets, (B + 1,), offsets.dtype, "offsets")
+    p = JoinParams(T, D, _type(x), B, at, _dev(gate, (B, D), dt, "gate"), _dev(w_post, (D,), dt, "w_post"),
+                   _dev(w_pre, (D,), dt, "w_pre"), res_scale, eps, _stream(stream))
     return p, (T, D), (B, D), dt
 
 
@@ -553,14 +557,11 @@ def ifvs_norm_join_grad(L, x_out, y=None, gate=None, w_post=None, w_pre=None, d_
 
 
 def _ffn_params(x, w_in, w_out, act, stream):
-    (T, D), F, dt = x.shape, int(w_out.shape[1]), x.dtype
+    (T, D), F, dt = x.shape, w_out.shape[1], x.dtype
     if act not in _ACTS:
         raise ValueError("act must be one of %s" % sorted(_ACTS))
-    p = FfnParams()
-    p.T, p.D, p.F, p.type, p.act = T, D, F, _type(x), _ACTS[act]
-    p.w_in = _dev(w_in, (2 * F, D), dt, "w_in")
-    p.w_out = _dev(w_out, (D, F), dt, "w_out")
-    p.stream = _stream(stream)
+    p = FfnParams(T, D, F, _type(x), _ACTS[act], _dev(w_in, (2 * F, D), dt, "w_in"),
+                  _dev(w_out, (D, F), dt, "w_out"), _stream(stream))
     return p, (T, D), F, dt
 
 
@@ -703,24 +704,13 @@ class Layers:
 
     def __init__(self, device=0):
         self.h = ifvs_layers_create(device)
-
-    def embed(self, table, ids, scale=1.0, **kw):
-        return ifvs_embed(self.h, table, ids, scale, **kw)
-
-    def embed_grad(self, d_out, ids, scale=1.0, **kw):
-        return ifvs_embed_grad(self.h, d_out, ids, scale, **kw)
-
-    def norm_join(self, x, y=None, gate=None, w_post=None, w_pre=None, **kw):
-        return ifvs_norm_join(self.h, x, y, gate, w_post, w_pre, **kw)
-
-    def norm_join_grad(self, x_out, y=None, gate=None, w_post=None, w_pre=None, d_x_out=None, d_n=None, **kw):
-        return ifvs_norm_join_grad(self.h, x_out, y, gate, w_post, w_pre, d_x_out, d_n, **kw)
-
-    def ffn(self, x, w_in, w_out, **kw):
-        return ifvs_ffn(self.h, x, w_in, w_out, **kw)
-
-    def ffn_grad(self, x, w_in, w_out, dy, **kw):
-        return ifvs_ffn_grad(self.h, x, w_in, w_out, dy, **kw)
+        # the functions above with this handle as their first argument
+        self.embed = functools.partial(ifvs_embed, self.h)
+        self.embed_grad = functools.partial(ifvs_embed_grad, self.h)
+        self.norm_join = functools.partial(ifvs_norm_join, self.h)
+        self.norm_join_grad = functools.partial(ifvs_norm_join_grad, self.h)
+        self.ffn = functools.partial(ifvs_ffn, self.h)
+        self.ffn_grad = functools.partial(ifvs_ffn_grad, self.h)
 
     def status(self):
         """Waits for the enqueued calls; raises what their kernels found."""
@@ -729,6 +719,7 @@ class Layers:
     def close(self):
         if getattr(self, "h", None):
             ifvs_layers_free(self.h)
+            self.h.value = None      # the bound functions refuse it from here on
             self.h = None
 
     def __del__(self):
