@@ -35,9 +35,18 @@ __device__ __forceinline__ void activation(float g, float& v, float& slope) {
         v = g * p;
         slope = p * (1.f + g * (1.f - p));
     } else {
-        const float p = 0.5f * erfcf(-0.70710678f * g);
+        // Phi by Abramowitz and Stegun 7.1.26: erfc(x) = (a1 t + .. + a5 t^5) e^(-x^2),
+        // t = 1 / (1 + p x), within 1.5e-7; here x = |g| / sqrt(2), so that the
+        // exponential serves the density too
+        const float e = __expf(-0.5f * g * g), t = __fdividef(1.f, fmaf(0.3275911f * 0.70710678f, fabsf(g), 1.f));
+        float q = fmaf(t, 1.061405429f, -1.453152027f);
+        q = fmaf(t, q, 1.421413741f);
+        q = fmaf(t, q, -0.284496736f);
+        q = fmaf(t, q, 0.254829592f);
+        q *= 0.5f * t * e;
+        const float p = g < 0.f ? q : 1.f - q;
         v = g * p;
-        slope = p + g * 0.39894228f * __expf(-0.5f * g * g);
+        slope = fmaf(0.39894228f * g, e, p);
     }
 }
 
@@ -86,9 +95,9 @@ __device__ __forceinline__ void finish(Bars<S>& b, uint32_t tmem, int filled, bo
             while (!mbar_try_wait(bar, parity) && clock64() - t0 < kWaitCycles) {
             }
         };
-        if (threadIdx.x == EPI * 32 && issues)
+        if (threadIdx.x / 32 == EPI && issues)       // `filled` is the elected thread's
             for (int i = max(0, filled - S); i < filled; ++i) bounded(smem_addr(&b.full[i % S]), (uint32_t)(i / S) & 1u);
-        if (threadIdx.x == EPI * 32 + 32 && issues) {
+        if (threadIdx.x / 32 == EPI + 1 && issues && elect_one()) {
             mma_commit<CG>(smem_addr(&b.drain));
             bounded(smem_addr(&b.drain), 0);
         }
@@ -112,13 +121,20 @@ __device__ __forceinline__ void load_tile(bool mn_major, uint32_t dst, const CUt
     }
 }
 
-// the four MMAs of a stage
-template <int CG>
-__device__ __forceinline__ void mma_stage(uint32_t d, uint32_t a, uint32_t b, bool a_mn, bool b_mn, uint32_t idesc, bool first) {
-    const uint64_t da = tile_desc(a, a_mn), db = tile_desc(b, b_mn), sa = desc_step(a_mn), sb = desc_step(b_mn);
+// The operands' descriptors at the ring's first stage; a stage further on differs
+// in the address alone
+struct Operands {
+    uint64_t a, b, step_a, step_b;
+    __device__ __forceinline__ Operands(uint32_t at_a, uint32_t at_b, bool a_mn, bool b_mn)
+        : a(tile_desc(at_a, a_mn)), b(tile_desc(at_b, b_mn)), step_a(desc_step(a_mn)), step_b(desc_step(b_mn)) {}
+    // the four MMAs of the stage `offset` bytes into the ring
+    template <int CG>
+    __device__ __forceinline__ void mma(uint32_t d, uint32_t offset, uint32_t idesc, bool first) const {
+        const uint64_t da = a + (offset >> 4), db = b + (offset >> 4);
 #pragma unroll
-    for (uint32_t i = 0; i < kStepK / 16; ++i) mma_f16<CG>(d, da + i * sa, db + i * sb, idesc, !first || i > 0);
-}
+        for (uint32_t i = 0; i < kStepK / 16; ++i) mma_f16<CG>(d, da + i * step_a, db + i * step_b, idesc, !first || i > 0);
+    }
+};
 
 // This warp's 32 rows x 64 columns of 16-bit output: packed pairs go to the
 // staging tile (swizzled), a TMA store takes it.  BUFS tiles per warp.
@@ -225,7 +241,7 @@ __global__ void __launch_bounds__(192, 1) k_products(const __grid_constant__ Pro
     wait_before();
 
     if (warp == EPI) {
-        if (lane == 0) {
+        if (elect_one()) {
             Ring<S> r;
             bool ok = true;
             for (int i = first; i < all.items && ok; i += step) {
@@ -243,7 +259,7 @@ __global__ void __launch_bounds__(192, 1) k_products(const __grid_constant__ Pro
             start_dependents();
         }
     } else if (warp == EPI + 1) {
-        if (lane == 0 && rank == 0) {
+        if (rank == 0 && elect_one()) {
             Ring<S> r;
             Ring<2> acc;
             bool ok = true;
@@ -253,11 +269,11 @@ __global__ void __launch_bounds__(192, 1) k_products(const __grid_constant__ Pro
                 const uint32_t idesc = mma_desc(CG * kRows, BN, f16, a_mn, b_mn);
                 if (!(ok = w.wait(smem_addr(&bars.acc_empty[acc.at]), acc.parity ^ 1u))) break;
                 fence_after_sync();
+                const Operands o(ring, ring + kABytes, a_mn, b_mn);
                 for (int k = t.k0; k < t.k1; ++k, r.next()) {
                     if (!(ok = w.wait(smem_addr(&bars.full[r.at]), r.parity))) break;
                     fence_after_sync();
-                    const uint32_t a = ring + r.at * Sh::kStage;
-                    mma_stage<CG>(tmem + acc.at * 256, a, a + kABytes, a_mn, b_mn, idesc, k == t.k0);
+                    o.mma<CG>(tmem + acc.at * 256, r.at * Sh::kStage, idesc, k == t.k0);
                     mma_commit<CG>(smem_addr(&bars.empty[r.at]));
                 }
                 mma_commit<CG>(smem_addr(&bars.acc_full[acc.at]));
@@ -373,7 +389,7 @@ k_hidden(const __grid_constant__ CUtensorMap mx, const __grid_constant__ CUtenso
     int filled = 0;
 
     if (warp == EPI) {
-        if (lane == 0) {
+        if (elect_one()) {
             Ring<S> r;
             bool ok = true;
             for (int t = first; t < tiles && ok; t += step) {
@@ -389,8 +405,9 @@ k_hidden(const __grid_constant__ CUtensorMap mx, const __grid_constant__ CUtenso
             start_dependents();
         }
     } else if (warp == EPI + 1) {
-        if (lane == 0 && rank == 0) {
+        if (rank == 0 && elect_one()) {
             const uint32_t idesc = mma_desc(CG * kRows, 2 * FT, f16, false, false);
+            const Operands o(ring, ring + kABytes, false, false);
             Ring<S> r;
             Ring<2> acc;
             bool ok = true;
@@ -400,8 +417,7 @@ k_hidden(const __grid_constant__ CUtensorMap mx, const __grid_constant__ CUtenso
                 for (int k = 0; k < g.k_steps; ++k, r.next()) {
                     if (!(ok = w.wait(smem_addr(&bars.full[r.at]), r.parity))) break;
                     fence_after_sync();
-                    const uint32_t a = ring + r.at * Sh::kStage;
-                    mma_stage<CG>(tmem + acc.at * 256, a, a + kABytes, false, false, idesc, k == 0);
+                    o.mma<CG>(tmem + acc.at * 256, r.at * Sh::kStage, idesc, k == 0);
                     mma_commit<CG>(smem_addr(&bars.empty[r.at]));
                 }
                 mma_commit<CG>(smem_addr(&bars.acc_full[acc.at]));
@@ -479,7 +495,7 @@ k_hidden_grad(const __grid_constant__ CUtensorMap mx, const __grid_constant__ CU
     int filled = 0;
 
     if (warp == EPI) {
-        if (lane == 0) {
+        if (elect_one()) {
             Ring<S> r;
             bool ok = true;
             for (int t = first; t < tiles && ok; t += step) {
@@ -503,9 +519,10 @@ k_hidden_grad(const __grid_constant__ CUtensorMap mx, const __grid_constant__ CU
             start_dependents();
         }
     } else if (warp == EPI + 1) {
-        if (lane == 0 && rank == 0) {
+        if (rank == 0 && elect_one()) {
             const uint32_t id_gu = mma_desc(CG * kRows, 2 * FT, f16, false, false);
             const uint32_t id_dh = mma_desc(CG * kRows, FT, f16, false, true);
+            const Operands of_gu(ring, ring + kABytes, false, false), of_dh(ring, ring + kABytes, false, true);
             Ring<S> r;
             uint32_t parity = 0;
             int turn = 0;
@@ -520,11 +537,10 @@ k_hidden_grad(const __grid_constant__ CUtensorMap mx, const __grid_constant__ CU
                     }
                     if (!(ok = w.wait(smem_addr(&bars.full[r.at]), r.parity))) break;
                     fence_after_sync();
-                    const uint32_t a = ring + r.at * Sh::kStage;
                     if (k < g.k_steps)
-                        mma_stage<CG>(tmem + (turn & 1 ? 3 * FT : 0), a, a + kABytes, false, true, id_dh, k == 0);
+                        of_dh.mma<CG>(tmem + (turn & 1 ? 3 * FT : 0), r.at * Sh::kStage, id_dh, k == 0);
                     else
-                        mma_stage<CG>(tmem + FT, a, a + kABytes, false, false, id_gu, k == g.k_steps);
+                        of_gu.mma<CG>(tmem + FT, r.at * Sh::kStage, id_gu, k == g.k_steps);
                     mma_commit<CG>(smem_addr(&bars.empty[r.at]));
                 }
                 mma_commit<CG>(smem_addr(&bars.acc_full[0]));
