@@ -115,21 +115,28 @@ __device__ __forceinline__ void load_keys(WarpKeys<R>& k, const EmbedArgs& a, Pa
 template <int R>
 __device__ __forceinline__ void rank_keys(WarpKeys<R>& k, const SortPlan& plan, int pass, int64_t left, int lane,
                                           uint32_t* hist) {
+    uint32_t same[R];
+#pragma unroll
+    for (int j = 0; j < R; ++j) same[j] = __ballot_sync(0xFFFFFFFFu, j * 32 + lane < left);
+    // bit by bit over all rounds: the ballots of a bit do not wait for each other
+    for (int b = 0; b < plan.bits; ++b) {
+        const int at = pass * plan.bits + b;
+#pragma unroll
+        for (int j = 0; j < R; ++j) {
+            const bool bit = k.key[j] >> at & 1u;
+            const uint32_t set = __ballot_sync(0xFFFFFFFFu, bit);
+            same[j] &= bit ? set : ~set;
+        }
+    }
 #pragma unroll
     for (int j = 0; j < R; ++j) {
         if (j * 32 >= left) break;
         const bool in = j * 32 + lane < left;
         const uint32_t d = plan.digit(k.key[j], pass);
-        uint32_t same = __ballot_sync(0xFFFFFFFFu, in);
-        for (int b = 0; b < plan.bits; ++b) {
-            const bool bit = d >> b & 1u;
-            const uint32_t set = __ballot_sync(0xFFFFFFFFu, bit);
-            same &= bit ? set : ~set;
-        }
         const uint32_t before = in ? hist[d] : 0u;
-        k.rank[j] = (uint16_t)(before + __popc(same & ((1u << lane) - 1u)));
+        k.rank[j] = (uint16_t)(before + __popc(same[j] & ((1u << lane) - 1u)));
         __syncwarp();
-        if (in && (same >> lane) == 1u) hist[d] = before + __popc(same);    // the last of its digit
+        if (in && (same[j] >> lane) == 1u) hist[d] = before + __popc(same[j]);    // the last of its digit
         __syncwarp();
     }
 }
@@ -168,8 +175,10 @@ __device__ __forceinline__ uint32_t stack_counts(uint32_t (*hist)[kBins], int bi
     return sum - start;
 }
 
-// Up to 65536 tokens: one cluster sorts them in one launch.  Each of its
-// CTAs owns a segment; the digits' counts meet through distributed shared memory.
+// Up to 65536 tokens: one cluster sorts them in one launch.  Each of its CTAs owns
+// a segment of the order, in shared memory between the passes; the digits'
+// counts and the pairs pass through distributed shared memory (through global
+// memory a pass of 17408 tokens took 7 us instead of 5).
 constexpr int kClusterMax = 8;
 constexpr int64_t cluster_tokens(int warps) { return (int64_t)kClusterMax * warps * 32 * kSortRounds; }   // 65536 at 32
 
@@ -181,61 +190,92 @@ __device__ __forceinline__ uint32_t cluster_size() {
 __device__ __forceinline__ void cluster_sync() {
     asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
-__device__ __forceinline__ uint32_t load_of(const uint32_t* p, uint32_t cta) {
-    uint32_t at, v;
+// two neighbours at this CTA's address p, from another CTA
+__device__ __forceinline__ uint2 load_of(const uint32_t* p, uint32_t cta) {
+    uint32_t at;
+    uint2 v;
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"((uint32_t)__cvta_generic_to_shared(p)), "r"(cta));
-    asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(at) : "memory");
+    asm volatile("ld.shared::cluster.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(at) : "memory");
     return v;
 }
+__device__ __forceinline__ void store_to(uint32_t at, uint32_t cta, uint32_t a, uint32_t b) {
+    uint32_t q;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(q) : "r"(at), "r"(cta));
+    asm volatile("st.shared::cluster.v2.u32 [%0], {%1, %2};" ::"r"(q), "r"(a), "r"(b) : "memory");
+}
 
-// W warps a CTA: 16 where they suffice (17408 tokens: 25 us for the whole gradient, 28 with 32)
+// W warps a CTA, 16 where they suffice.  magic: 2^32 / segment, rounded up.
+constexpr size_t cluster_smem(int warps, int rounds) {
+    return sizeof(uint32_t) * warps * kBins + 2 * sizeof(uint2) * warps * 32 * rounds;
+}
 template <int W>
 __global__ void __launch_bounds__(W * 32, 1)
-k_sort_cluster(EmbedArgs a, SortPlan plan, Pairs p0, Pairs p1, int rounds) {
-    extern __shared__ uint32_t sort_smem[];
+k_sort_cluster(EmbedArgs a, SortPlan plan, Pairs out, int rounds, uint32_t magic) {
+    extern __shared__ __align__(16) uint32_t sort_smem[];
     uint32_t(*hist)[kBins] = reinterpret_cast<uint32_t(*)[kBins]>(sort_smem);      // [W]
-    __shared__ uint32_t total[kBins], base[kBins], warp_sums[kScanThreads / 32];
+    const int segment = W * 32 * rounds;
+    uint2* held = reinterpret_cast<uint2*>(sort_smem + W * kBins);                  // [2][segment] keys and positions
+    __shared__ __align__(8) uint32_t total[kBins];
+    __shared__ uint32_t base[kBins], warp_sums[kScanThreads / 32];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, bins = 1 << plan.bits;
     const uint32_t cta = blockIdx.x, ctas = cluster_size();
-    const int64_t first = ((int64_t)cta * W + warp) * 32 * rounds;
+    const int64_t first = (int64_t)cta * segment + warp * 32 * rounds;
     const int64_t left = min(a.T - first, (int64_t)32 * rounds);
     start_dependents();
     for (int pass = 0; pass < plan.passes; ++pass) {
-        const Pairs in = pass == 0 ? Pairs{nullptr, nullptr} : (pass & 1 ? p0 : p1);
-        const Pairs out = pass & 1 ? p1 : p0;
         for (int i = lane; i < bins; i += 32) hist[warp][i] = 0;
         WarpKeys<kSortRounds> k;
-        load_keys(k, a, in, first, left, lane);
+        if (pass == 0) {
+            load_keys(k, a, Pairs{nullptr, nullptr}, first, left, lane);
+        } else {
+#pragma unroll
+            for (int j = 0; j < kSortRounds; ++j) {
+                uint2 v = make_uint2(0, 0);
+                if (j * 32 + lane < left) v = held[(pass & 1) * segment + (warp * rounds + j) * 32 + lane];
+                k.key[j] = v.x;
+                k.pos[j] = v.y;
+            }
+        }
         __syncwarp();
         rank_keys(k, plan, pass, left, lane, hist[warp]);
         __syncthreads();
-        for (int d = threadIdx.x; d < kBins; d += W * 32) total[d] = d < bins ? stack_counts<W>(hist, d, 0) : 0u;
+        for (int d = threadIdx.x; d < bins; d += W * 32) total[d] = stack_counts<W>(hist, d, 0);
         cluster_sync();
         uint32_t all[2] = {0, 0}, before[2] = {0, 0};
         const int d0 = threadIdx.x * 2;
-        if (d0 < bins)
+        if (d0 < bins) {
+            uint2 n[kClusterMax];        // all loads are issued before the first is used
 #pragma unroll
-            for (uint32_t c = 0; c < kClusterMax; ++c)
+            for (uint32_t c = 0; c < kClusterMax; ++c) n[c] = load_of(&total[d0], min(c, ctas - 1u));
 #pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    const uint32_t n = c < ctas ? load_of(&total[d0 + j], c) : 0u;
-                    before[j] += c < cta ? n : 0u;
-                    all[j] += n;
-                }
+            for (uint32_t c = 0; c < kClusterMax; ++c) {
+                before[0] += c < cta ? n[c].x : 0u;
+                before[1] += c < cta ? n[c].y : 0u;
+                all[0] += c < ctas ? n[c].x : 0u;
+                all[1] += c < ctas ? n[c].y : 0u;
+            }
+        }
         const uint32_t start = scan_bins(all[0], all[1], warp_sums);
         if (d0 < bins) {
             base[d0] = start + before[0];
             base[d0 + 1] = start + all[0] + before[1];
         }
         __syncthreads();
+        const bool last = pass + 1 == plan.passes;
+        const uint32_t to = (uint32_t)__cvta_generic_to_shared(held) + ((pass + 1) & 1) * segment * 8u;
 #pragma unroll
         for (int j = 0; j < kSortRounds; ++j)
             if (j * 32 + lane < left) {
                 const uint32_t g = plan.digit(k.key[j], pass), at = base[g] + hist[warp][g] + k.rank[j];
-                out.key[at] = k.key[j];
-                out.pos[at] = k.pos[j];
+                if (last) {
+                    out.key[at] = k.key[j];
+                    out.pos[at] = k.pos[j];
+                } else {
+                    const uint32_t c = __umulhi(at, magic);
+                    store_to(to + (at - c * segment) * 8u, c, k.key[j], k.pos[j]);
+                }
             }
-        cluster_sync();      // the pairs are written, and every CTA has read the totals
+        cluster_sync();      // the pairs are there, and every CTA has read the totals
     }
 }
 
@@ -592,6 +632,24 @@ k_embed_join(EmbedArgs a, SumPlan p, Pairs sorted, const float* __restrict__ par
             if (c < a.D) sum[j] += __ldcg(from + c);
         }
     };
+    // the first partial sums of parts first, first + by, ... <= last
+    auto add_parts = [&](int64_t first, int64_t last, int by) {
+        for (int64_t r = first; r <= last; r += 8 * by) {
+            float q[8][4];               // eight parts' loads are issued before the first is added
+#pragma unroll
+            for (int u = 0; u < 8; ++u)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    q[u][j] = 0.f;
+                    if (r + u * by <= last && c0 + j * 32 + lane < a.D)
+                        q[u][j] = __ldcg(partial + (r + u * by) * 2 * a.D + c0 + j * 32 + lane);
+                }
+#pragma unroll
+            for (int u = 0; u < 8; ++u)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) sum[j] += q[u][j];
+        }
+    };
     auto key_at = [&](int64_t i) { return __ldcg(sorted.key + i); };
     const int64_t part = (int64_t)blockIdx.x * 8 + warp;
     uint32_t its = kNoKey;               // the run that begins in this part and goes on
@@ -612,8 +670,7 @@ k_embed_join(EmbedArgs a, SumPlan p, Pairs sorted, const float* __restrict__ par
 #pragma unroll
         for (int j = 0; j < 4; ++j) sum[j] = 0.f;
         add(partial + (part * 2 + 1) * a.D);
-#pragma unroll 8
-        for (int64_t q = part + 1; q <= part + more; ++q) add(partial + q * 2 * a.D);
+        add_parts(part + 1, part + more, 1);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             const int c = c0 + j * 32 + lane;
@@ -635,8 +692,7 @@ k_embed_join(EmbedArgs a, SumPlan p, Pairs sorted, const float* __restrict__ par
 #pragma unroll
         for (int j = 0; j < 4; ++j) sum[j] = 0.f;
         if (warp == 0) add(partial + (k * 2 + 1) * a.D);
-#pragma unroll 4
-        for (int64_t q = k + 1 + warp; q <= k + many; q += 8) add(partial + q * 2 * a.D);
+        add_parts(k + 1 + warp, k + many, 8);
 #pragma unroll
         for (int j = 0; j < 4; ++j) part_sum[warp][j * 32 + lane] = sum[j];
         __syncthreads();
@@ -669,7 +725,7 @@ int64_t sort_tiles(const EmbedArgs& a) { return (a.T + kTileTokens - 1) / kTileT
 
 cudaError_t sort_by_id(const EmbedArgs& a, Pairs p0, Pairs p1, uint32_t* counts, cudaStream_t s, Pairs* sorted) {
     const SortPlan plan = sort_plan(a.V);
-    *sorted = plan.passes & 1 ? p0 : p1;
+    *sorted = p0;
     auto in_cluster = [&](auto warps) {
         const auto kernel = k_sort_cluster<warps()>;
         // the work of a pass is in its ranks: spread over the cluster's SMs
@@ -679,8 +735,8 @@ cudaError_t sort_by_id(const EmbedArgs& a, Pairs p0, Pairs p1, uint32_t* counts,
         cudaLaunchConfig_t cfg = {};
         cfg.gridDim = dim3((unsigned)ctas);
         cfg.blockDim = dim3(warps() * 32);
-        cfg.dynamicSmemBytes = sizeof(uint32_t) * warps() * kBins;
-        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)cfg.dynamicSmemBytes);
+        cfg.dynamicSmemBytes = cluster_smem(warps(), rounds);
+        const cudaError_t e = allow_smem(kernel, cfg.dynamicSmemBytes);
         if (e != cudaSuccess) return e;
         cfg.stream = s;
         cudaLaunchAttribute attr[1];
@@ -688,10 +744,12 @@ cudaError_t sort_by_id(const EmbedArgs& a, Pairs p0, Pairs p1, uint32_t* counts,
         attr[0].val.clusterDim = {(unsigned)ctas, 1u, 1u};
         cfg.attrs = attr;
         cfg.numAttrs = 1;
-        return cudaLaunchKernelEx(&cfg, kernel, a, plan, p0, p1, rounds);
+        const uint32_t magic = (uint32_t)((1ull << 32) / (unsigned)(warps() * 32 * rounds) + 1);
+        return cudaLaunchKernelEx(&cfg, kernel, a, plan, p0, rounds, magic);
     };
     if (a.T <= cluster_tokens(16)) return in_cluster(std::integral_constant<int, 16>());
     if (a.T <= cluster_tokens(32)) return in_cluster(std::integral_constant<int, 32>());
+    *sorted = plan.passes & 1 ? p0 : p1;
     const int tiles = (int)sort_tiles(a);
     uint32_t* totals = counts + (int64_t)kBins * tiles;
     cudaError_t e = cudaSuccess;
@@ -718,7 +776,7 @@ cudaError_t sum_by_id(const EmbedArgs& a, const void* d_out, Pairs sorted, float
     if (rows) {
         const size_t smem = (size_t)kSumWarps * 2 * 16 * kSliceBytes;
         const auto kernel = wide ? k_embed_sum_rows<T, 2> : k_embed_sum_rows<T, 1>;
-        e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        e = allow_smem(kernel, smem);
         if (e == cudaSuccess)
             e = launch_kernel(kernel, dim3((unsigned)((warps + kSumWarps - 1) / kSumWarps)), dim3(kSumWarps * 32), smem, true, s,
                               (const T*)d_out, a, p, sorted, partial, (T*)d_table);

@@ -341,7 +341,7 @@ __global__ void __launch_bounds__(256) k_join_parts(Parts p) {
     const int j = blockIdx.y;
     if (i >= p.n[j]) return;
     float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
+#pragma unroll 8
     for (int s = 0; s < p.splits[j]; ++s) {
         const float4 q = __ldcg(reinterpret_cast<const float4*>(p.parts[j] + s * p.n[j] + i));
         v.x += q.x;
@@ -698,7 +698,7 @@ cudaError_t with_act(int act, const Fn& f) {
 template <int CG, class... P, class... A>
 cudaError_t launch_tiles(void (*kernel)(P...), int64_t items, int num_sms, int threads, size_t smem, bool chain,
                          cudaStream_t s, const A&... args) {
-    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    cudaError_t e = allow_smem(kernel, smem);
     if (e != cudaSuccess) return e;
     const int64_t most = num_sms / CG;
     cudaLaunchConfig_t cfg = {};

@@ -123,6 +123,13 @@ inline cudaError_t with_type(int type, const Fn& f) {
     return f(__nv_bfloat16());
 }
 
+// Dynamic shared memory beyond the 48 KB that a kernel may have unasked
+template <class K>
+inline cudaError_t allow_smem(K* kernel, size_t bytes) {
+    return bytes <= 48 * 1024 ? cudaSuccess
+                              : cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+}
+
 // ---- launchers --------------------------------------------------------------
 struct EmbedArgs {
     const int32_t* ids;

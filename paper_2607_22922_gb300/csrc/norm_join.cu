@@ -587,7 +587,7 @@ __global__ void __launch_bounds__(kGradWarps * 32, 1) k_norm_join_grad(JoinArgs 
 // per team, or for long ones the CTA); the rest clear the gradients of empty
 // sequences' gates.
 constexpr int kFinishWarps = 32;         // teams per CTA too
-constexpr int kClearRows = 1024;
+constexpr int kClearRows = kFinishWarps * 32;
 constexpr int kWarpRows = 16;            // partial sums that a warp adds by itself
 
 template <class T>
@@ -599,11 +599,21 @@ __global__ void __launch_bounds__(kFinishWarps * 32) k_join_finish(JoinArgs a, J
     wait_before();
     // v[j] += sum over rows first, first + by, ... <= last of from[row * stride + c0 + 32 j + lane]
     auto add_rows = [&](float (&v)[4], const float* from, int64_t stride, int64_t first, int64_t last, int by) {
-#pragma unroll 4
-        for (int64_t r = first; r <= last; r += by)
+        for (int64_t r = first; r <= last; r += 8 * by) {
+            float q[8][4];               // eight rows' loads are issued before the first is added
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-                if (c0 + j * 32 + lane < a.D) v[j] += __ldcg(from + r * stride + c0 + j * 32 + lane);
+            for (int u = 0; u < 8; ++u)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    q[u][j] = 0.f;
+                    if (r + u * by <= last && c0 + j * 32 + lane < a.D)
+                        q[u][j] = __ldcg(from + (r + u * by) * stride + c0 + j * 32 + lane);
+                }
+#pragma unroll
+            for (int u = 0; u < 8; ++u)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) v[j] += q[u][j];
+        }
     };
     // the same with rows spread over the CTA's warps: column threadIdx.x < 128
     auto cta_rows = [&](const float* from, int64_t stride, int64_t first, int64_t last) {
@@ -656,10 +666,11 @@ __global__ void __launch_bounds__(kFinishWarps * 32) k_join_finish(JoinArgs a, J
         }
         return;
     }
-    const int64_t b0 = (group - groups) * kClearRows;
-    for (int64_t b = b0 + warp; b < min(a.B, b0 + kClearRows); b += kFinishWarps)
-        if (__ldg(a.offsets + b) == __ldg(a.offsets + b + 1))
-            for (int e = c0 + lane; e < min(a.D, c0 + 128); e += 32) ((T*)g.d_gate)[b * a.D + e] = from_f32<T>(0.f);
+    const int64_t b0 = (group - groups) * kClearRows + warp * 32;
+    uint32_t empty = __ballot_sync(0xFFFFFFFFu, b0 + lane < a.B && __ldg(a.offsets + b0 + lane) == __ldg(a.offsets + b0 + lane + 1));
+    for (; empty; empty &= empty - 1u)
+        for (int e = c0 + lane; e < min(a.D, c0 + 128); e += 32)
+            ((T*)g.d_gate)[(b0 + __ffs(empty) - 1) * a.D + e] = from_f32<T>(0.f);
 }
 
 // ---- host ------------------------------------------------------------------------
@@ -716,7 +727,7 @@ cudaError_t launch_norm_join(const JoinArgs& a, const void* x, const void* y, vo
         using T = decltype(t);
         const int cta_teams = kJoinThreads / 32 / sh.warps;
         const size_t smem = ring_bytes<T, n(), 2>(cta_teams, a.D);
-        const cudaError_t e = cudaFuncSetAttribute(k_norm_join<T, n(), nv()>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        const cudaError_t e = allow_smem(k_norm_join<T, n(), nv()>, smem);
         if (e != cudaSuccess) return e;
         // as many CTAs as run at once; fewer tokens: one per team
         const int64_t want = (a.T + cta_teams - 1) / cta_teams, most = (int64_t)a.num_sms * (smem > 110 * 1024 ? 1 : 2);
@@ -774,7 +785,7 @@ cudaError_t launch_norm_join_grad(const JoinArgs& a, const JoinGrads& g, uint8_t
             size_t smem = ring_bytes<T, n(), 4, places()>(cta_teams, a.D);
             const size_t sums = (size_t)cta_teams * a.D * sizeof(float);
             smem = smem > sums ? smem : sums;
-            const cudaError_t r = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+            const cudaError_t r = allow_smem(kernel, smem);
             if (r != cudaSuccess) return r;
             kernel<<<(unsigned)p.ctas, kGradWarps * 32, smem, s>>>(a, g, p);
             return cudaGetLastError();
