@@ -115,6 +115,17 @@ struct Pack {
     }
 };
 
+// One thread of a converged warp, always the same.  Where it is asked for this
+// way the compiler knows that one thread runs the branch; under `lane == 0` it
+// issues every MMA and TMA instruction in a loop over the warp's active
+// threads: 513 clocks per 4 MMAs of 128 columns with their wait and commit
+// instead of 257, which is what the tensor pipe takes.
+__device__ __forceinline__ bool elect_one() {
+    uint32_t ok;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xFFFFFFFF;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(ok));
+    return ok != 0u;
+}
+
 // Calls f with a value of the element type that `type` names
 template <class Fn>
 inline cudaError_t with_type(int type, const Fn& f) {
@@ -123,10 +134,11 @@ inline cudaError_t with_type(int type, const Fn& f) {
     return f(__nv_bfloat16());
 }
 
-// Dynamic shared memory beyond the 48 KB that a kernel may have unasked
+// Dynamic shared memory beyond the 48 KB, static included (at most 17 KB in these
+// kernels), that a kernel may have unasked
 template <class K>
 inline cudaError_t allow_smem(K* kernel, size_t bytes) {
-    return bytes <= 48 * 1024 ? cudaSuccess
+    return bytes <= 31 * 1024 ? cudaSuccess
                               : cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
 }
 

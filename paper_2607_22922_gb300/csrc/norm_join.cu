@@ -135,7 +135,7 @@ struct Rows {
         const int lane = threadIdx.x & 31;
         const uint32_t to = (uint32_t)__cvta_generic_to_shared(join_smem) + ring + place_ * A * stride;
         if constexpr (N * sizeof(T) == 16) {        // rows begin and end on 16 bytes
-            if (lane != 0) return;
+            if (!elect_one()) return;
             const uint32_t len = n * D * (uint32_t)sizeof(T);
             const int64_t at = (int64_t)t * D;
             uint32_t arrays = 0;
@@ -164,7 +164,7 @@ struct Rows {
                         asm volatile("st.shared.u16 [%0], %1;" ::"r"(to + k * stride + q),
                                      "h"(__ldg(reinterpret_cast<const uint16_t*>(lo - before + q)))
                                      : "memory");
-            if (bytes && lane == 0)
+            if (bytes && elect_one())
                 bulk_g2s(to + k * stride + skip, lo - before + skip, bytes, bar, policy);
             return bytes;
         };
@@ -172,7 +172,7 @@ struct Rows {
 #pragma unroll
         for (int k = 0; k < A; ++k)
             if (p[k]) all += copy(k, false, 0);
-        if (lane == 0) mbar_arrive_expect_tx(bar, all);
+        if (elect_one()) mbar_arrive_expect_tx(bar, all);
         const uint64_t once = policy_evict_first();
 #pragma unroll
         for (int k = 0; k < A; ++k)

@@ -86,17 +86,6 @@ __device__ __forceinline__ void tmem_free(uint32_t base, uint32_t columns) {
         asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(base), "r"(columns));
 }
 
-// One thread of a converged warp, always the same.  Where it is asked for this
-// way the compiler knows that one thread runs the branch; under `lane == 0` it
-// issues every MMA and TMA instruction in a loop over the warp's active
-// threads: 513 clocks per 4 MMAs of 128 columns with their wait and commit
-// instead of 257, which is what the tensor pipe takes.
-__device__ __forceinline__ bool elect_one() {
-    uint32_t ok;
-    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xFFFFFFFF;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(ok));
-    return ok != 0u;
-}
-
 // ---- pairs of CTAs --------------------------------------------------------------
 __device__ __forceinline__ uint32_t cluster_rank() {
     uint32_t r;
