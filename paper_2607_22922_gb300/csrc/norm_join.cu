@@ -39,9 +39,13 @@ struct Team {
         else
             asm volatile("barrier.cta.sync %0, %1;" ::"r"(1 + id), "r"(warps * 32) : "memory");
     }
+    // both sums hold a barrier of the team
     __device__ __forceinline__ float sum(float v) {
         v = warp_sum(v);
-        if (warps == 1) return v;
+        if (warps == 1) {
+            __syncwarp();
+            return v;
+        }
         float* s = slots + (turn * all + id * warps) * 4;
         turn ^= 1;
         if ((threadIdx.x & 31) == 0) s[warp * 4] = v;
@@ -213,10 +217,11 @@ struct Rows {
 #pragma unroll
         for (int k = 0; k < A; ++k) off[k] += D * sizeof(T);
     }
-    // the place that begins with token t is read by the whole team: fills it with what comes S places later
+    // This thread has read the place (before a barrier of the team, then leave).
+    __device__ __forceinline__ void done() const { fence_proxy_async_smem(); }
+    // The place that begins with token t is read by the whole team: fills it with
+    // what comes S places later.
     __device__ __forceinline__ void leave(const Team& team, int t, int end) {
-        fence_proxy_async_smem();
-        team.sync();
         const int f = t + S * per;
         if (f < end) fill(team, place, f, min(per, end - f));
         if (++place == S) {
@@ -343,12 +348,15 @@ k_norm_join(JoinArgs a, int team_warps, int64_t chunk, const T* __restrict__ x, 
             }
         }
         rows.next();
-        if (t + 1 == first + rows.per || t + 1 == t1) {
+        const bool last = t + 1 == first + rows.per || t + 1 == t1;      // of the place
+        if (last) rows.done();
+        const float square = team.sum(total(q));           // with a barrier
+        if (last) {
             rows.leave(team, first, t1);
             first = t + 1;
         }
         if (!no) continue;
-        const F ix = both<F>(rsqrtf(fmaf(team.sum(total(q)), inv_d, a.eps)));
+        const F ix = both<F>(rsqrtf(fmaf(square, inv_d, a.eps)));
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int c = col + i * step;
@@ -541,12 +549,15 @@ __global__ void __launch_bounds__(kGradWarps * 32, 1) k_norm_join_grad(JoinArgs 
             }
         }
         rows.next();
-        if (t + 1 == first + rows.per || t + 1 == t1) {
+        const bool last = t + 1 == first + rows.per || t + 1 == t1;      // of the place
+        if (last) rows.done();
+        const float along_u = team.sum(total(m));          // with a barrier
+        if (last) {
             rows.leave(team, first, t1);
             first = t + 1;
         }
         if (!ALL && !y) continue;
-        const F back = both<F>(-iy_ * iy_ * (team.sum(total(m)) * inv_d));
+        const F back = both<F>(-iy_ * iy_ * (along_u * inv_d));
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int c = col + i * step;
