@@ -11,7 +11,7 @@
 //
 // Both are bound by memory: two rows read and two written per token, four and
 // two.  A team of 1 to 16 warps takes tokens that follow each other, through a ring
-// of kStages places in shared memory that bulk copies fill ahead: each row is
+// of two places in shared memory that bulk copies fill ahead: each row is
 // read once from memory, whatever the norms need of it, and a team's loads go on
 // while it reduces.  A place holds the bytes of a few tokens (they follow each
 // other in memory, so that rows need no alignment).  The sequence of a team's
@@ -100,7 +100,7 @@ struct Sequence {
     __device__ __forceinline__ int begin() const { return offsets ? offset(b) : 0; }
 };
 
-constexpr int kStages = 3;               // places of a ring (1: no copies ahead)
+constexpr int kStages = 2;               // places of a ring (1: no copies ahead)
 
 extern __shared__ __align__(16) uint8_t join_smem[];
 
@@ -242,7 +242,10 @@ struct Rows {
 };
 
 constexpr int kJoinThreads = 256;
-constexpr int kJoinColumns = 1024;       // columns a warp holds at most
+// columns a warp holds at most.  163847 tokens x 960, bfloat16: 226 us with 512 and
+// three CTAs an SM, 235 with 1024 and two.
+constexpr int join_columns(int D) { return D <= kJoinThreads / 32 * 512 ? 512 : 1024; }
+constexpr int join_ctas(int columns) { return columns > 512 ? 2 : 3; }       // per SM, by registers
 
 // Shared memory of a kernel whose `teams` teams have rings of A rows a place
 template <class T, int N, int A, int S = kStages>
@@ -252,7 +255,7 @@ size_t ring_bytes(int teams, int D) {
 
 // Tokens [chunk team, chunk (team + 1)) of team number `team`
 template <class T, int N, int NV>
-__global__ void __launch_bounds__(kJoinThreads, 2)
+__global__ void __launch_bounds__(kJoinThreads, join_ctas(32 * N * NV))
 k_norm_join(JoinArgs a, int team_warps, int64_t chunk, const T* __restrict__ x, const T* __restrict__ y,
             T* __restrict__ xo, T* __restrict__ no) {
     __shared__ __align__(16) float slots[2 * kJoinThreads / 32 * 4];
@@ -372,11 +375,12 @@ k_norm_join(JoinArgs a, int team_warps, int64_t chunk, const T* __restrict__ x, 
 }
 
 // ---- gradient ------------------------------------------------------------------
-// 16 warps a CTA; three places of four rows each in shared memory at 512 columns
-// of 16 bits a warp (more warps per token repeat its sums and waits: 410 us with
+// 16 warps a CTA; two places of four rows each in shared memory at 512 columns of
+// 16 bits a warp (more warps per token repeat its sums and waits: 410 us with
 // 256 columns, 360 with 512, 131101 tokens x 1024), 256 of float32.  Float32
 // rows beyond 4096 take 512 and a single place.
 constexpr int kGradWarps = 16;
+constexpr int kGradStages = kStages;     // 293 us, 331 with 3 (131101 tokens x 1024): what is left is L1 for the weights
 constexpr int grad_columns(int type, int D) { return type == IFVS_T_F32 && D <= kGradWarps * 256 ? 256 : 512; }
 
 struct GradPlan {
@@ -731,9 +735,7 @@ using Counts = std::integer_sequence<int, NV...>;
 cudaError_t launch_norm_join(const JoinArgs& a, const void* x, const void* y, void* x_out, void* n_out,
                              cudaStream_t s) {
     const int N = access_elems(a, x, y, x_out, n_out);
-    // short accesses take twice the registers: half the columns a warp, up to the CTA's warps
-    const bool whole = N * elem_bytes(a.type) == 16 || a.D > 8 * kJoinColumns / 2;
-    const Shape sh = team_shape(a.D, N, whole ? kJoinColumns : kJoinColumns / 2);
+    const Shape sh = team_shape(a.D, N, join_columns(a.D));
     auto go = [&](auto t, auto n, auto nv) {
         using T = decltype(t);
         const int cta_teams = kJoinThreads / 32 / sh.warps;
@@ -741,7 +743,8 @@ cudaError_t launch_norm_join(const JoinArgs& a, const void* x, const void* y, vo
         const cudaError_t e = allow_smem(k_norm_join<T, n(), nv()>, smem);
         if (e != cudaSuccess) return e;
         // as many CTAs as run at once; fewer tokens: one per team
-        const int64_t want = (a.T + cta_teams - 1) / cta_teams, most = (int64_t)a.num_sms * (smem > 110 * 1024 ? 1 : 2);
+        const int64_t want = (a.T + cta_teams - 1) / cta_teams, by_smem = 226 * 1024 / ((int64_t)smem + 2048);
+        const int64_t regs = join_ctas(32 * n() * nv()), most = a.num_sms * (by_smem < regs ? by_smem : regs);
         const int64_t ctas = want < most ? want : most, chunk = (a.T + ctas * cta_teams - 1) / (ctas * cta_teams);
         k_norm_join<T, n(), nv()><<<(unsigned)ctas, kJoinThreads, smem, s>>>(a, sh.warps, chunk, (const T*)x, (const T*)y,
                                                                            (T*)x_out, (T*)n_out);
@@ -806,7 +809,7 @@ cudaError_t launch_norm_join_grad(const JoinArgs& a, const JoinGrads& g, uint8_t
             if constexpr (sizeof(T) == 4 && n() * nv() == 16)
                 e = rows(Count<1>());
             else
-                e = rows(Count<kStages>());
+                e = rows(Count<kGradStages>());
         }
         if (e != cudaSuccess) return e;
         const int64_t teams = g.d_gate ? p.teams : 0, clears = g.d_gate && a.offsets ? (a.B + kClearRows - 1) / kClearRows : 0;
