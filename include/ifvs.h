@@ -466,7 +466,9 @@ int ifvs_get_conditioning(ifvs_index* ix, float* bank, float* W, uint32_t flags)
  * stream NULL it runs on a stream of the handle's own, a blocking one, and
  * returns when its outputs are written.  A call whose workspace has to grow
  * allocates (and waits for the device): run the largest shape once before a
- * stream capture.  Errors that a kernel finds (a token id or offsets out of
+ * stream capture.  A captured graph keeps the workspace that it was captured
+ * with, until the handle is freed; its replays and other calls that use the
+ * workspace are ordered by the caller.  Errors that a kernel finds (a token id or offsets out of
  * range, a bounded wait that ran out) are returned by the call itself when it
  * waits, else by ifvs_layers_status.  A handle may be used by one thread at
  * a time.

@@ -10,12 +10,22 @@
 
 using namespace ifvs;
 
+namespace {
+// A workspace that a captured graph may still use
+struct Retired {
+    uint8_t* p;
+    Retired* next;
+};
+}  // namespace
+
 struct ifvs_layers {
     int device = 0, num_sms = 0;
     cudaStream_t own = nullptr;
     cudaEvent_t done = nullptr;     // after the last enqueued call that used the workspace
     uint8_t* work = nullptr;
     size_t work_bytes = 0;
+    bool work_captured = false;     // a captured graph holds its address
+    Retired* retired = nullptr;
     int* err_host = nullptr;        // the error word, page-locked
     int* err = nullptr;             // its device address
 };
@@ -71,9 +81,16 @@ struct Call {
         if (bytes > L->work_bytes) {
             if (!ordered) return report_error(IFVS_ERR_STATE, "the workspace would have to grow during a stream capture");
             CUDA_TRY(cudaEventSynchronize(L->done));
-            if (L->work) cudaFree(L->work);
+            if (L->work && L->work_captured) {
+                Retired* r = new (std::nothrow) Retired{L->work, L->retired};
+                if (!r) return report_error(IFVS_ERR_OOM, "out of host memory");
+                L->retired = r;
+            } else if (L->work) {
+                cudaFree(L->work);
+            }
             L->work = nullptr;
             L->work_bytes = 0;
+            L->work_captured = false;
             void* p = nullptr;
             const cudaError_t e = device_malloc(&p, bytes);
             if (e != cudaSuccess) {
@@ -84,7 +101,10 @@ struct Call {
             L->work = (uint8_t*)p;
             L->work_bytes = bytes;
         }
-        if (ordered) CUDA_TRY(cudaStreamWaitEvent(s, L->done, 0));
+        if (ordered)
+            CUDA_TRY(cudaStreamWaitEvent(s, L->done, 0));
+        else
+            L->work_captured = true;
         return 0;
     }
     int end() {
@@ -214,6 +234,11 @@ void ifvs_layers_free(ifvs_layers* L) {
     cudaDeviceSynchronize();        // kernels may still write the error word
     if (L->done) cudaEventDestroy(L->done);
     if (L->work) cudaFree(L->work);
+    while (Retired* r = L->retired) {
+        L->retired = r->next;
+        cudaFree(r->p);
+        delete r;
+    }
     if (L->own) cudaStreamDestroy(L->own);
     if (L->err_host) cudaFreeHost(L->err_host);
     cudaGetLastError();

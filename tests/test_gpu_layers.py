@@ -412,6 +412,43 @@ def test_calls_in_a_graph(layers):
     assert torch.equal(y, layers.ffn(*a)) and torch.equal(dx, layers.ffn_grad(*a, dy)[0])
 
 
+def test_a_captured_workspace_outlives_its_growth(ifvs):
+    L = ifvs.Layers()
+    d_out, ids = _rand(14)(900, 40), _ids("hot", 900, 64, 14)
+    out = torch.empty(64, 40, device="cuda")
+    want = L.embed_grad(d_out, ids, V=64)
+    s, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=s):
+        L.embed_grad(d_out, ids, d_table=out, stream=s)
+        with pytest.raises(ifvs.IfvsError) as e:     # nothing grows in a capture
+            L.embed_grad(torch.empty(300_000, 40, device="cuda"), torch.empty(300_000, dtype=torch.int32, device="cuda"),
+                         d_table=out, stream=s)
+        assert e.value.code == ifvs.IFVS_ERR_STATE
+    L.embed_grad(_rand(15)(300_000, 40), _ids("any", 300_000, 64, 15), V=64)       # grows
+    for _ in range(3):
+        out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want)
+    del graph
+    L.close()
+
+
+@pytest.mark.parametrize("act,type_", [("silu", "f16"), ("gelu", "bf16"), ("gelu", "f16"), ("relu", "bf16")])
+def test_ffn_pairs_of_ctas(layers, act, type_):
+    """Tiles of 256 tokens in the hidden layer, of 128 in the products."""
+    a, dy = _ffn_inputs(12_001, 136, 392, type_, 16)
+    ref.within(layers.ffn(*a, act=act), *ref.ffn(*a, act))
+    _check(layers.ffn_grad(*a, dy, act=act), ref.ffn_grad(*a, dy, act))
+
+
+@pytest.mark.parametrize("T,V", [(33_000, 5000), (65_537, 600_000), (65_536, 511), (8_193, 512)])
+def test_embed_grad_around_the_sorts_limits(layers, T, V):
+    """One cluster of 16 or 32 warps a CTA, tiles beyond; one, two and three digits."""
+    d_out, ids = _rand(T)(T, 12), _ids("hot", T, V, V)
+    ref.within(layers.embed_grad(d_out, ids, V=V), *ref.embed_grad(d_out, ids, 1.0, V))
+
+
 def test_failed_workspace_leaves_the_handle_usable(ifvs):
     L = ifvs.Layers()
     a, dy = _ffn_inputs(40, 64, 136, "bf16", 7)
