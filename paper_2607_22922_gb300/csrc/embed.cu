@@ -22,36 +22,46 @@ inline bool vectors(const EmbedArgs& a, const void* p, const void* q) {
     return a.D * elem_bytes(a.type) % 16 == 0 && ((uintptr_t)p | (uintptr_t)q) % 16 == 0;
 }
 
-// out[t] = scale table[ids[t]].  A thread copies kEmbedRows pieces of a row.
+// out[t] = scale table[ids[t]].  A thread copies kEmbedPieces pieces of a row, 256
+// pieces apart: that is `rows` rows and `pieces` pieces further, so that one
+// division per thread places all (a division per piece kept the SMs' issue slots
+// 68 % busy).
 constexpr int kEmbedPieces = 4;
 
 template <class T, int N>
 __global__ void __launch_bounds__(256)
-k_embed(const T* __restrict__ table, EmbedArgs a, T* __restrict__ out) {
+k_embed(const T* __restrict__ table, EmbedArgs a, int per_row, int rows, int pieces, T* __restrict__ out) {
     using F = typename Pack<T, N>::F;
-    const int per_row = a.D / N;
-    const int64_t n = a.T * per_row;
     const int64_t first = (int64_t)blockIdx.x * (256 * kEmbedPieces) + threadIdx.x;
+    int64_t t = first <= 0xFFFFFFFFll ? (int64_t)((uint32_t)first / (uint32_t)per_row) : first / per_row;
+    int col = (int)(first - t * per_row);
     Pack<T, N> v[kEmbedPieces];
-    bool some[kEmbedPieces];
+    int id[kEmbedPieces];
 #pragma unroll
     for (int i = 0; i < kEmbedPieces; ++i) {
-        const int64_t at = first + i * 256;
-        some[i] = false;
-        if (at >= n) continue;
-        const int64_t t = n <= 0x7FFFFFFF ? (int64_t)((uint32_t)at / (uint32_t)per_row) : at / per_row;
-        const int col = (int)(at - t * per_row);
-        const int id = __ldg(a.ids + t);
-        some[i] = id >= 0 && id < a.V;
-        if (!some[i] && id != -1 && col == 0) *a.err = kErrId;
-        if (some[i]) v[i].load(table + (int64_t)id * a.D + col * N);
+        id[i] = -1;
+        if (t < a.T) {
+            id[i] = __ldg(a.ids + t);
+            if (id[i] < -1 || id[i] >= a.V) {
+                if (col == 0) *a.err = kErrId;
+                id[i] = -1;
+            }
+            if (id[i] >= 0) v[i].load(table + (int64_t)id[i] * a.D + col * N);
+        }
+        col += pieces;
+        t += rows;
+        if (col >= per_row) {
+            col -= per_row;
+            ++t;
+        }
     }
+    const int64_t n = a.T * per_row;
 #pragma unroll
     for (int i = 0; i < kEmbedPieces; ++i) {
         const int64_t at = first + i * 256;
         if (at >= n) continue;
 #pragma unroll
-        for (int j = 0; j < Pack<T, N>::kF; ++j) v[i].set(j, some[i] ? mul_(both<F>(a.scale), v[i].get(j)) : both<F>(0.f));
+        for (int j = 0; j < Pack<T, N>::kF; ++j) v[i].set(j, id[i] >= 0 ? mul_(both<F>(a.scale), v[i].get(j)) : both<F>(0.f));
         v[i].store_stream(out + at * N);     // the table's rows stay in L2
     }
 }
@@ -797,12 +807,13 @@ cudaError_t launch_embed(const EmbedArgs& a, const void* table, void* out, cudaS
         using T = decltype(z);
         constexpr int N = 16 / (int)sizeof(T);
         const bool vec = vectors(a, table, out);
-        const int64_t n = a.T * (a.D / (vec ? N : 1));
+        const int per_row = a.D / (vec ? N : 1), rows = 256 / per_row, pieces = 256 % per_row;
+        const int64_t n = a.T * per_row;
         const unsigned grid = (unsigned)((n + 256 * kEmbedPieces - 1) / (256 * kEmbedPieces));
         if (vec)
-            k_embed<T, N><<<grid, 256, 0, s>>>((const T*)table, a, (T*)out);
+            k_embed<T, N><<<grid, 256, 0, s>>>((const T*)table, a, per_row, rows, pieces, (T*)out);
         else
-            k_embed<T, 1><<<grid, 256, 0, s>>>((const T*)table, a, (T*)out);
+            k_embed<T, 1><<<grid, 256, 0, s>>>((const T*)table, a, per_row, rows, pieces, (T*)out);
         return cudaGetLastError();
     });
 }
