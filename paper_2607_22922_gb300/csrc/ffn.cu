@@ -184,6 +184,9 @@ constexpr size_t smem_of(uint32_t stage_bytes, uint32_t out_bytes) {
 }
 
 // ---- products C = A B^T in 16 bits ---------------------------------------------------
+// Bound by the tensor pipe and, in a long run, by power: the gradient's three
+// products at 16411 x 1024 x 4096 (687 GFLOP) 380 us, 1.81 PFLOP/s, the pipe 96.5 %
+// active at 1.64 GHz.
 // A K-major [rows][K] or MN-major [K][rows]; B the same with `cols`.  Up to three
 // products in one launch, items (tiles, or parts of a tile's sum) in their order.
 struct Product {
@@ -353,6 +356,8 @@ __global__ void __launch_bounds__(256) k_join_parts(Parts p) {
 }
 
 // ---- h = act(x Wg^T) * (x Wu^T) ------------------------------------------------------
+// Bound by the tensor pipe: 17408 x 960 x 2560 (171 GFLOP) 90 us, 1.90 PFLOP/s, the
+// pipe 89 % active.
 // FT hidden columns per tile: gate rows and up rows of W_in side by side in B.  In
 // a pair the first CTA holds the gate's rows, the second the up projection's.
 template <int CG, int FT>
@@ -467,7 +472,10 @@ k_hidden(const __grid_constant__ CUtensorMap mx, const __grid_constant__ CUtenso
 // ---- h, dg, du from x and dy ---------------------------------------------------------
 // Per tile first dh = dy Wo (FT columns), then g and u (2 FT).  TMEM: g | u in
 // columns FT .. 3 FT - 1; dh in the first FT or from 3 FT by turns, so that the
-// next tile's dh accumulates while this tile's values are read.
+// next tile's dh accumulates while this tile's values are read.  Bound by shared
+// memory: per 64 of the sum 56 KB come in by TMA and are read by the MMAs, 112 KB
+// in the 768 clocks that the MMAs take, at 128 bytes a clock.  16411 x 1024 x 4096
+// (413 GFLOP) 267 us, 1.55 PFLOP/s, the tensor pipe 68 % active.
 template <int CG, int FT>
 struct GradShape {
     static constexpr int kEpi = FT / 16;
@@ -601,10 +609,12 @@ k_hidden_grad(const __grid_constant__ CUtensorMap mx, const __grid_constant__ CU
 
 // ---- a few tokens ----------------------------------------------------------------------
 // Up to kFewTokens tokens: the weights are read once and bound the call, and a
-// tile of 128 tokens would leave most SMs without one.  A row of weights (PAIR:
+// tile of 128 tokens would leave most SMs without one (960 x 2560, here against
+// the tensor cores: 1 token 7.9 us against 14.9, 4 tokens 9.1 against 15.1, 8
+// tokens 17.5 against 14.5).  A row of weights (PAIR:
 // the gate's row and the up projection's) is spread over the lanes of one or
 // more warps, 16 bytes a lane and access, against every token's row.
-constexpr int kFewTokens = 16;
+constexpr int kFewTokens = 4;
 
 template <class T>
 struct FewArgs {
@@ -648,7 +658,11 @@ __global__ void __launch_bounds__(256) k_few(FewArgs<T> a) {
 #pragma unroll
             for (int t = 0; t < TT; ++t) {
                 Pack<T, 8> x;
-                x.w = __ldcg(reinterpret_cast<const uint4*>(a.x + (int64_t)min(t, a.tokens - 1) * a.K + c * 8));
+                const T* from = a.x + (int64_t)min(t, a.tokens - 1) * a.K + c * 8;
+                if constexpr (PAIR)
+                    x.load(from);
+                else             // written by the kernel before, which this one may have started beside
+                    x.w = __ldcg(reinterpret_cast<const uint4*>(from));
 #pragma unroll
                 for (int r = 0; r < NW; ++r)
 #pragma unroll
@@ -785,9 +799,12 @@ struct Plan {
     }
 };
 
-// Pairs of CTAs where their tiles fill the device
-bool use_pairs(const FfnArgs& a, int64_t rows, int64_t cols) {
-    return (int64_t)ceil_div(rows, 256) * ceil_div(cols, 256) >= a.num_sms / 2;
+// Pairs of CTAs where their tiles fill the device, or half of it where each sums
+// over 1024 or more.  Forward pass, pairs against single CTAs: 8192 tokens x 960 x
+// 2560 76 us against 93; 2048 x 1536 x 5120 67 against 81; 1024 x 1536 x 5120 (24
+// tiles of the output) 57 against 45; 4096 x 128 x 344 11.8 against 11.1.
+bool use_pairs(const FfnArgs& a, int64_t rows, int64_t cols, int64_t K) {
+    return (int64_t)ceil_div(rows, 256) * ceil_div(cols, 256) >= a.num_sms / (K >= 1024 ? 4 : 2);
 }
 
 template <class T, bool PAIR, int ACT>
@@ -798,9 +815,7 @@ cudaError_t launch_few(const FfnArgs& a, const void* x, const void* w, void* out
     auto go = [&](auto tt) { return launch_kernel(k_few<T, PAIR, ACT, tt()>, grid, dim3(256), 0, !PAIR, s, f); };
     if (a.T == 1) return go(std::integral_constant<int, 1>());
     if (a.T == 2) return go(std::integral_constant<int, 2>());
-    if (a.T <= 4) return go(std::integral_constant<int, 4>());
-    if (a.T <= 8) return go(std::integral_constant<int, 8>());
-    return go(std::integral_constant<int, 16>());
+    return go(std::integral_constant<int, kFewTokens>());
 }
 
 template <class T>
@@ -833,8 +848,14 @@ cudaError_t make_map(CUtensorMap* map, int type, const void* p, int64_t rows, in
 
 namespace {
 size_t padded(size_t n) { return (n + 255) / 256 * 256; }
-bool out_pairs(const FfnArgs& a) { return use_pairs(a, a.T, a.D); }
-bool grad_pairs(const FfnArgs& a) { return use_pairs(a, a.T, a.D) || use_pairs(a, 2 * (int64_t)a.F, a.D); }
+bool hidden_pairs(const FfnArgs& a) { return use_pairs(a, a.T, 2 * (int64_t)a.F, a.D); }
+bool out_pairs(const FfnArgs& a) { return use_pairs(a, a.T, a.D, a.F); }
+// The gradient's products together.  The weights' sum over the tokens: few tokens
+// are over before a pair has started (960 x 2560, pairs against single CTAs: 128
+// tokens 35 us against 30, 512 42 against 39, 4096 116 against 149).
+bool grad_pairs(const FfnArgs& a) {
+    return a.T > 512 && (use_pairs(a, a.T, a.D, 2 * (int64_t)a.F) || use_pairs(a, 2 * (int64_t)a.F, a.D, a.T));
+}
 }  // namespace
 
 size_t ffn_bytes(const FfnArgs& a) {
@@ -862,7 +883,7 @@ cudaError_t launch_ffn(const FfnArgs& a, const void* x, void* y, uint8_t* work, 
                                   Sh::kSmem, false, s, mx, mw, mh, g, a.type == IFVS_T_F16, a.err);
     };
     const cudaError_t e = with_act(a.act, [&](auto act) {
-        return use_pairs(a, a.T, 2 * (int64_t)a.F) ? run(act, std::integral_constant<int, 2>(), std::integral_constant<int, 128>())
+        return hidden_pairs(a) ? run(act, std::integral_constant<int, 2>(), std::integral_constant<int, 128>())
                                                    : run(act, std::integral_constant<int, 1>(), std::integral_constant<int, 64>());
     });
     if (e != cudaSuccess) return e;
@@ -897,7 +918,7 @@ cudaError_t launch_ffn_grad(const FfnArgs& a, const void* x, const void* dy, voi
                                   a.type == IFVS_T_F16, a.err);
     };
     const cudaError_t e = with_act(a.act, [&](auto act) {
-        return use_pairs(a, a.T, 2 * F) ? run(act, std::integral_constant<int, 2>(), std::integral_constant<int, 128>())
+        return hidden_pairs(a) ? run(act, std::integral_constant<int, 2>(), std::integral_constant<int, 128>())
                                         : run(act, std::integral_constant<int, 1>(), std::integral_constant<int, 64>());
     });
     if (e != cudaSuccess) return e;
