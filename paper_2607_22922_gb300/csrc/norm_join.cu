@@ -22,6 +22,7 @@
 // result depends on timing.  Measured: 163847 tokens x 960 of bfloat16 227 us,
 // 5.6 TB/s; the gradient of 131101 x 1024 292 us, 5.5 TB/s.
 #include "layers.cuh"
+#include "places.h"
 #include "scan_common.cuh"
 
 namespace ifvs {
@@ -185,8 +186,8 @@ struct Rows {
     }
     // fills the ring for tokens [t, end)
     __device__ __forceinline__ void start(const Team& team, int t, int end) const {
-        for (int i = 0; i < S; ++i, t += per)
-            if (t < end) fill(team, i, t, min(per, end - t));
+        for (int i = 0; i < S; ++i)
+            if (const int n = place_count(t, end, per, i)) fill(team, i, t + i * per, n);
         team.sync();
     }
     // The place's rows are there, for the whole team; t is its first token.  A wait
@@ -223,8 +224,7 @@ struct Rows {
     // The place that begins with token t is read by the whole team: fills it with
     // what comes S places later.
     __device__ __forceinline__ void leave(const Team& team, int t, int end) {
-        const int f = t + S * per;
-        if (f < end) fill(team, place, f, min(per, end - f));
+        if (const int n = place_count(t, end, per, S)) fill(team, place, t + S * per, n);
         if (++place == S) {
             place = 0;
             parity ^= 1u;
@@ -352,7 +352,7 @@ k_norm_join(JoinArgs a, int team_warps, int64_t chunk, const T* __restrict__ x, 
             }
         }
         rows.next();
-        const bool last = t + 1 == first + rows.per || t + 1 == t1;      // of the place
+        const bool last = ends_place(t, first, t1, rows.per);
         if (last) rows.done();
         const float square = team.sum(total(q));           // with a barrier
         if (last) {
@@ -554,7 +554,7 @@ __global__ void __launch_bounds__(kGradWarps * 32, 1) k_norm_join_grad(JoinArgs 
             }
         }
         rows.next();
-        const bool last = t + 1 == first + rows.per || t + 1 == t1;      // of the place
+        const bool last = ends_place(t, first, t1, rows.per);
         if (last) rows.done();
         const float along_u = team.sum(total(m));          // with a barrier
         if (last) {

@@ -1,0 +1,68 @@
+"""The encoder's layers at the limits of their ranges and in their steady state,
+against float64 with the bounds of tests/layers_util.py."""
+import pytest
+
+import layers_util as ref
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+TYPES = {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}
+EPS = 1e-5
+
+
+@pytest.fixture(scope="module")
+def ifvs():
+    from paper_2607_22922_gb300 import build
+    build.build()
+    from paper_2607_22922_gb300 import ifvs as mod
+    return mod
+
+
+@pytest.fixture(scope="module")
+def layers(ifvs):
+    L = ifvs.Layers()
+    yield L
+    L.close()
+
+
+def _rand(seed):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    return lambda *shape: torch.randn(*shape, generator=g, device="cuda")
+
+
+def _check(got, want):
+    for a, w in zip(got, want):
+        assert (a is None) == (w is None)
+        if a is not None:
+            ref.within(a, *w)
+
+
+def test_norm_join_of_as_many_tokens_as_there_can_be(layers):
+    """T = 2^31 - 1: the last places of the rings end at the largest int.  A
+    token's outputs depend on its row and its sequence's gate alone, so the
+    first, some middle and the last tokens are compared."""
+    T, D, dt = 2**31 - 1, 1, torch.float16
+    if torch.cuda.mem_get_info()[0] < 60 << 30:
+        pytest.skip("needs 60 GB of device memory")
+    g = torch.Generator(device="cuda")
+    g.manual_seed(31)
+
+    def rows():
+        return torch.empty(T, D, dtype=dt, device="cuda").normal_(generator=g)
+
+    x, y, dxo, dn = rows(), rows(), rows(), rows()
+    cut = T - 21
+    off = torch.tensor([0, cut, T], dtype=torch.int64, device="cuda")
+    gate = torch.tensor([[0.5], [-1.5]], dtype=dt, device="cuda")
+    w_post, w_pre = torch.full((1,), 1.25, dtype=dt, device="cuda"), torch.full((1,), 0.75, dtype=dt, device="cuda")
+    kw = dict(offsets=off, res_scale=0.7, eps=EPS)
+    xo, no = layers.norm_join(x, y, gate, w_post, w_pre, **kw)
+    dx, dy, _, _, _ = layers.norm_join_grad(x, y, gate, w_post, w_pre, dxo, dn, **kw)
+    for lo, hi in ((0, 100), (T // 2, T // 2 + 100), (T - 100, T)):
+        s = slice(lo, hi)
+        here = torch.tensor([0, min(max(cut - lo, 0), hi - lo), hi - lo], dtype=torch.int64, device="cuda")
+        a = (x[s], y[s], gate, w_post, w_pre)
+        _check((xo[s], no[s]), ref.norm_join(*a, here, 0.7, EPS))
+        _check((dx[s], dy[s]), ref.norm_join_grad(*a, dxo[s], dn[s], here, 0.7, EPS)[:2])
