@@ -459,8 +459,8 @@ int ifvs_get_conditioning(ifvs_index* ix, float* bank, float* W, uint32_t flags)
  * order: equal calls give equal bits.  Outputs must not overlap inputs or
  * each other.
  *
- * A handle holds the workspace, the order of the calls that use it, and an
- * error word.  With a non-NULL stream a call only enqueues its work there
+ * A handle holds the workspace, the order of the calls that use it, and a
+ * word per error.  With a non-NULL stream a call only enqueues its work there
  * (the legacy default stream is cudaStreamLegacy, (void*)1); calls that use
  * the workspace wait for each other on the device, whatever their streams; with
  * stream NULL it runs on a stream of the handle's own, a blocking one, and
@@ -489,8 +489,9 @@ enum { IFVS_ACT_SILU = 0, IFVS_ACT_GELU = 1, IFVS_ACT_RELU = 2 };
 int ifvs_layers_create(ifvs_layers** out, int32_t device);
 void ifvs_layers_free(ifvs_layers* L);
 
-/* ifvs_layers_status — waits for the device, returns the error that its kernels found since the last status call or
- * waiting call (IFVS_OK: none) and clears it. */
+/* ifvs_layers_status — waits for the device, returns the error that its
+ * kernels found since the last status call or waiting call (IFVS_OK: none) and
+ * clears it.  Of several the first of: a wait that ran out, an id, offsets. */
 int ifvs_layers_status(ifvs_layers* L);
 
 /*

@@ -46,7 +46,7 @@ k_embed(const T* __restrict__ table, EmbedArgs a, int per_row, int rows, int pie
         if (t < a.T) {
             id[i] = __ldg(a.ids + t);
             if (id[i] < -1 || id[i] >= a.V) {
-                if (col == 0) *a.err = kErrId;
+                if (col == 0) a.err[kErrId] = 1;
                 id[i] = -1;
             }
             if (id[i] >= 0) v[i].load(table + (int64_t)id[i] * a.D + col * N);
@@ -96,7 +96,7 @@ struct Pairs {
 __device__ __forceinline__ uint32_t key_of(const EmbedArgs& a, int64_t i) {
     const int id = __ldg(a.ids + i);
     if (id >= 0 && id < a.V) return (uint32_t)id;
-    if (id != -1) *a.err = kErrId;
+    if (id != -1) a.err[kErrId] = 1;
     return (uint32_t)a.V;
 }
 
@@ -541,7 +541,7 @@ k_embed_sum_rows(const T* __restrict__ d_out, EmbedArgs a, SumPlan p, Pairs sort
             // a wait that runs out: the sums go on with what is there and are reported
             if (!late && !mbar_wait_warp(bar + 8 * (g & 1), parity)) {
                 late = true;
-                if (lane == 0) *a.err = kErrWait;
+                if (lane == 0) a.err[kErrWait] = 1;
             }
             parity ^= (uint32_t)g & 1u;
             auto row = [&](Pack<T, N>(&v)[NV], int i) {

@@ -26,8 +26,8 @@ struct ifvs_layers {
     size_t work_bytes = 0;
     bool work_captured = false;     // a captured graph holds its address
     Retired* retired = nullptr;
-    int* err_host = nullptr;        // the error word, page-locked
-    int* err = nullptr;             // its device address
+    int* err_host = nullptr;        // the error words, page-locked
+    int* err = nullptr;             // their device address
 };
 
 namespace {
@@ -50,13 +50,14 @@ int fail(cudaError_t e, const char* what, int line) {
         if (rc_ != 0) return rc_; \
     } while (0)
 
-// what the kernels found since the last look
+// What the kernels found since the last look, the gravest first.  A word is read
+// and cleared in one step: kernels of other streams may still store.
 int take_error(ifvs_layers* L) {
-    const int e = *reinterpret_cast<volatile int*>(L->err_host);
-    *L->err_host = 0;
-    if (e & kErrWait) return report_error(IFVS_ERR_TIMEOUT, "a bounded wait inside a kernel ran out");
-    if (e & kErrId) return report_error(IFVS_ERR_ARG, "a token id is outside -1..V-1");
-    if (e & kErrOffsets) return report_error(IFVS_ERR_ARG, "offsets must start at 0, end at T and not decrease");
+    int e[kErrWords];
+    for (int i = 0; i < kErrWords; ++i) e[i] = __atomic_exchange_n(L->err_host + i, 0, __ATOMIC_ACQ_REL);
+    if (e[kErrWait]) return report_error(IFVS_ERR_TIMEOUT, "a bounded wait inside a kernel ran out");
+    if (e[kErrId]) return report_error(IFVS_ERR_ARG, "a token id is outside -1..V-1");
+    if (e[kErrOffsets]) return report_error(IFVS_ERR_ARG, "offsets must start at 0, end at T and not decrease");
     return IFVS_OK;
 }
 
@@ -213,10 +214,10 @@ int ifvs_layers_create(ifvs_layers** out, int32_t device) {
     // blocking: ordered after the caller's work on the legacy default stream
     if (e == cudaSuccess) e = cudaStreamCreateWithFlags(&L->own, cudaStreamDefault);
     if (e == cudaSuccess) e = cudaEventCreateWithFlags(&L->done, cudaEventDisableTiming);
-    if (e == cudaSuccess) e = cudaHostAlloc(&h, sizeof(int), cudaHostAllocMapped | cudaHostAllocPortable);
+    if (e == cudaSuccess) e = cudaHostAlloc(&h, kErrWords * sizeof(int), cudaHostAllocMapped | cudaHostAllocPortable);
     if (e == cudaSuccess) {
         L->err_host = (int*)h;
-        *L->err_host = 0;
+        memset(h, 0, kErrWords * sizeof(int));
         e = cudaHostGetDevicePointer(&d, h, 0);
         L->err = (int*)d;
     }
@@ -231,7 +232,7 @@ int ifvs_layers_create(ifvs_layers** out, int32_t device) {
 void ifvs_layers_free(ifvs_layers* L) {
     if (!L) return;
     DeviceGuard guard(L->device);
-    cudaDeviceSynchronize();        // kernels may still write the error word
+    cudaDeviceSynchronize();        // kernels may still write the error words
     if (L->done) cudaEventDestroy(L->done);
     if (L->work) cudaFree(L->work);
     while (Retired* r = L->retired) {

@@ -10,10 +10,12 @@
 
 namespace ifvs {
 
-// Bits of the handle's error word
-constexpr int kErrId = 1;        // a token id outside -1..V-1
-constexpr int kErrOffsets = 2;   // offsets that break their rules
-constexpr int kErrWait = 4;      // a bounded wait ran out
+// The handle's error words: one per error, so that a kernel's plain store of 1
+// takes back no other
+constexpr int kErrId = 0;        // a token id outside -1..V-1
+constexpr int kErrOffsets = 1;   // offsets that break their rules
+constexpr int kErrWait = 2;      // a bounded wait ran out
+constexpr int kErrWords = 3;
 
 inline size_t elem_bytes(int type) { return type == IFVS_T_F32 ? 4 : 2; }
 
@@ -194,7 +196,7 @@ __device__ __forceinline__ void check_offsets(const int64_t* __restrict__ offset
         const int64_t lo = __ldg(offsets + b), hi = __ldg(offsets + b + 1);
         bad |= hi < lo || (b == 0 && lo != 0) || (b == B - 1 && hi != T);
     }
-    if (bad) *err = kErrOffsets;
+    if (bad) err[kErrOffsets] = 1;
 }
 
 // the sequence of token t: the last b with offsets[b] <= t, within 0..B-1

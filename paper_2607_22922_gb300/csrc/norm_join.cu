@@ -200,7 +200,7 @@ struct Rows {
             while (!mbar_try_wait(bar, parity) && !*dead)
                 if (clock64() - t0 > kWaitCycles) {
                     *dead = 1;
-                    *err = kErrWait;
+                    err[kErrWait] = 1;
                 }
         }
         if (S == 1) team.sync();         // plain loads of the fill just before

@@ -175,7 +175,7 @@ __device__ __forceinline__ void mbar_arrive(uint32_t bar) {
 
 // ---- bounded waits ----------------------------------------------------------------
 // A wait that runs out marks the CTA dead (every other wait then returns at
-// once) and the handle's error word; the roles leave their loops, and the
+// once) and the handle's error words; the roles leave their loops, and the
 // kernel waits, bounded again, for its copies and MMAs before it returns.
 struct Watch {
     volatile int* dead;     // shared memory
@@ -188,7 +188,7 @@ struct Watch {
             if (*dead) return false;
             if (clock64() - t0 > kWaitCycles) {
                 *dead = 1;
-                *err = kErrWait;
+                err[kErrWait] = 1;
                 return false;
             }
         }
