@@ -72,11 +72,12 @@ typedef enum {
  * IFVS_FAIL_ALLOC holds a number n >= 1, the n-th device allocation since
  * the variable took its current string fails without calling cudaMalloc.
  *
- * Kernels never wait without a bound.  The sorted-copy scan waits for its
- * bulk-copied code tiles for at most about half a second per tile; when a
- * wait runs out the search returns IFVS_ERR_TIMEOUT and the device stays
+ * Kernels never wait without a bound.  The sorted-copy scan and the encoder's
+ * layers wait for bulk-copied tiles for at most about half a second each; when a
+ * wait runs out the call returns IFVS_ERR_TIMEOUT and the device stays
  * usable.  For tests of that path, while the environment variable
- * IFVS_TEST_STALL_COPIES is "1" every such wait runs out. */
+ * IFVS_TEST_STALL_COPIES is "1" every such wait runs out (of a layers' handle,
+ * if the variable was set, to whatever value, when the handle was created). */
 
 /* Clause operators (Listing 1 uses = and >; all are intervals on integers):
  *   EQ    a == lo        RANGE lo <= a < hi     GE  a >= lo

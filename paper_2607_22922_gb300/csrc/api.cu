@@ -81,17 +81,17 @@ cudaError_t ifvs::device_malloc(void** p, size_t bytes) {
     return cudaMalloc(p, bytes);
 }
 
-namespace {
-
-// Timeout injection for tests of the scan's bounded waits (no GPU fault
-// involved): while the environment variable IFVS_TEST_STALL_COPIES is "1",
-// the bulk-copy barriers of the sorted-copy scan expect 16 bytes more than
-// their copies deliver, so every wait on them runs out after its bound and
-// the search returns IFVS_ERR_TIMEOUT with the context intact.
-bool stall_copies_for_tests() {
+// Timeout injection for tests of the bounded waits (no GPU fault involved):
+// while the environment variable IFVS_TEST_STALL_COPIES is "1", the bulk-copy
+// barriers of the sorted-copy scan and of the encoder's layers expect 16 bytes
+// more than their copies deliver, so every wait on them runs out after its bound
+// and the call returns IFVS_ERR_TIMEOUT with the context intact.
+bool ifvs::stall_copies_for_tests() {
     const char* v = getenv("IFVS_TEST_STALL_COPIES");
     return v != nullptr && v[0] == '1' && v[1] == '\0';
 }
+
+namespace {
 
 struct DevBuf {
     void* p = nullptr;

@@ -500,6 +500,8 @@ int index_view(const ifvs_index* ix, IndexView* out);
 int report_error(int code, const char* fmt, ...);
 // Every device allocation of the library (api.cu: injected failures)
 cudaError_t device_malloc(void** p, size_t bytes);
+// whether barriers are to expect more than their copies deliver (api.cu)
+bool stall_copies_for_tests();
 
 // Makes a device current for its lifetime
 struct DeviceGuard {

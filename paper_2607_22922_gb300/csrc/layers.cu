@@ -2,11 +2,13 @@
 // with them in include/ifvs.h): the handle, argument checks, workspace and
 // stream order.
 #include <math.h>
+#include <stdlib.h>
 #include <string.h>
 
 #include <new>
 
 #include "layers.cuh"
+#include "scan_common.cuh"
 
 using namespace ifvs;
 
@@ -25,6 +27,7 @@ struct ifvs_layers {
     uint8_t* work = nullptr;
     size_t work_bytes = 0;
     bool work_captured = false;     // a captured graph holds its address
+    bool may_stall = false;         // waits may be made to run out
     Retired* retired = nullptr;
     int* err_host = nullptr;        // the error words, page-locked
     int* err = nullptr;             // their device address
@@ -118,6 +121,14 @@ struct Call {
 
 bool aligned(const void* p, size_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
 
+// Waits run out after half a second; those that a test makes run out, after 32 ms.
+// Looking for the test's variable takes 0.5 us: only handles that were created
+// while it was there do, in every call.
+Waits waits_of(const ifvs_layers* L) {
+    if (L->may_stall && stall_copies_for_tests()) return {L->err, 16u, 1ll << 26};
+    return {L->err, 0u, kWaitCycles};
+}
+
 int check_type(int type) {
     if (type != IFVS_T_F32 && type != IFVS_T_F16 && type != IFVS_T_BF16)
         return report_error(IFVS_ERR_ARG, "unknown element type %d", type);
@@ -171,7 +182,7 @@ int join_check(const ifvs_layers* L, const ifvs_join_params* p, bool block, Join
     else if (p->w_post || p->gate)
         return report_error(IFVS_ERR_ARG, "w_post and gate must be NULL without y");
     *a = JoinArgs{p->T, p->n_seq, p->D, p->type, p->n_seq == 1 ? nullptr : p->offsets, p->gate, p->w_post, p->w_pre,
-                  block ? p->res_scale : 1.f, p->eps, L->err, L->num_sms};
+                  block ? p->res_scale : 1.f, p->eps, waits_of(L), L->num_sms};
     return 0;
 }
 
@@ -209,6 +220,7 @@ int ifvs_layers_create(ifvs_layers** out, int32_t device) {
     ifvs_layers* L = new (std::nothrow) ifvs_layers;
     if (!L) return report_error(IFVS_ERR_OOM, "out of host memory");
     L->device = device;
+    L->may_stall = getenv("IFVS_TEST_STALL_COPIES") != nullptr;
     void *h = nullptr, *d = nullptr;
     cudaError_t e = cudaDeviceGetAttribute(&L->num_sms, cudaDevAttrMultiProcessorCount, device);
     // blocking: ordered after the caller's work on the legacy default stream

@@ -144,6 +144,13 @@ inline cudaError_t allow_smem(K* kernel, size_t bytes) {
                               : cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
 }
 
+// What a kernel's waits for its copies go by
+struct Waits {
+    int* err;               // the error words
+    uint32_t extra;         // bytes that barriers expect beyond the copies' (0 but in tests)
+    long long cycles;       // a wait's bound
+};
+
 // ---- launchers --------------------------------------------------------------
 struct EmbedArgs {
     const int32_t* ids;
@@ -163,7 +170,7 @@ struct JoinArgs {
     const int64_t* offsets;      // null: B = 1
     const void *gate, *w_post, *w_pre;
     float rho, eps;
-    int* err;
+    Waits waits;
     int num_sms;
 };
 cudaError_t launch_norm_join(const JoinArgs& a, const void* x, const void* y, void* x_out, void* n_out,

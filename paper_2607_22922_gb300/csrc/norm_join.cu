@@ -111,6 +111,24 @@ __host__ __device__ constexpr int place_tokens(int row_bytes) {
     return row_bytes >= 1024 ? 1 : (row_bytes <= 128 ? 8 : 1024 / row_bytes);
 }
 
+// After a wait that ran out: waits for the copies of place number `at`, which
+// begins with token t, and of the places filled after it, once more and bounded
+// together.  Out of line: inside the token loop it costs the gradient registers
+// (131101 tokens x 1024: 297 us, 287 so).
+template <int S>
+__device__ __noinline__ void drain_places(uint32_t bars, int at, uint32_t parity, int t, int end, int per, long long cycles) {
+    const long long t0 = clock64();
+    for (int i = 0; i < S; ++i) {
+        if (place_count(t, end, per, i))
+            while (!mbar_try_wait(bars + 8u * at, parity) && clock64() - t0 < cycles) {
+            }
+        if (++at == S) {
+            at = 0;
+            parity ^= 1u;
+        }
+    }
+}
+
 // A team's ring: per place the rows of `per` tokens of A arrays (absent ones are
 // null), from the 16-byte boundary before them to the one after.  Where that
 // boundary lies outside the array, the row's bytes beside it are copied by
@@ -119,9 +137,8 @@ template <class T, int N, int A, int S = kStages>
 struct Rows {
     const T* p[A];
     uint32_t ring;              // S x A x stride bytes of join_smem
-    uint32_t bars;              // address of S mbarriers
-    volatile int* dead;
-    int* err;
+    uint32_t bars;              // address of S mbarriers and two 32-bit words: a wait for a place ran out, by turns
+    Waits waits;
     int T_, D;                  // tokens of the arrays, their width
     int per, stride, place = 0;
     uint32_t parity = 0;
@@ -130,9 +147,9 @@ struct Rows {
     static __host__ __device__ int stride_of(int D) {
         return (place_tokens(D * (int)sizeof(T)) * D * (int)sizeof(T) + 32 + 15) / 16 * 16;
     }
-    __device__ __forceinline__ Rows(uint64_t* bars_, int* dead_, const JoinArgs& a, int team)
+    __device__ __forceinline__ Rows(uint64_t* bars_, const JoinArgs& a, int team)
         : ring(team * S * A * stride_of(a.D)),
-          bars((uint32_t)__cvta_generic_to_shared(bars_ + team * S)), dead(dead_), err(a.err), T_((int)a.T), D(a.D),
+          bars((uint32_t)__cvta_generic_to_shared(bars_ + team * (S + 1))), waits(a.waits), T_((int)a.T), D(a.D),
           per(place_tokens(a.D * (int)sizeof(T))), stride(stride_of(a.D)) {}
 
     // tokens [t, t + n); the team's earlier reads of the place lie before a barrier of the team
@@ -147,7 +164,7 @@ struct Rows {
             uint32_t arrays = 0;
 #pragma unroll
             for (int k = 0; k < A; ++k) arrays += p[k] != nullptr;
-            mbar_arrive_expect_tx(bars + 8u * place_, arrays * len);
+            mbar_arrive_expect_tx(bars + 8u * place_, arrays * len + waits.extra);
             const uint64_t once = policy_evict_first();
 #pragma unroll
             for (int k = 0; k < A; ++k)
@@ -178,7 +195,7 @@ struct Rows {
 #pragma unroll
         for (int k = 0; k < A; ++k)
             if (p[k]) all += copy(k, false, 0);
-        if (elect_one()) mbar_arrive_expect_tx(bar, all);
+        if (elect_one()) mbar_arrive_expect_tx(bar, all + waits.extra);
         const uint64_t once = policy_evict_first();
 #pragma unroll
         for (int k = 0; k < A; ++k)
@@ -190,17 +207,22 @@ struct Rows {
             if (const int n = place_count(t, end, per, i)) fill(team, i, t + i * per, n);
         team.sync();
     }
+    // the word of the current place: another one than that of the place before
+    __device__ __forceinline__ uint32_t late() const {
+        static_assert(S <= 2, "places take turns");
+        return bars + 8u * S + 4u * (S == 2 ? (uint32_t)place : parity);
+    }
     // The place's rows are there, for the whole team; t is its first token.  A wait
-    // that runs out marks the CTA: later waits return at once, the team goes on and
-    // its results are reported as incomplete.
+    // that runs out is reported and ends the team's work where it leaves the place.
     __device__ __forceinline__ void enter(const Team& team, int t) {
         const uint32_t bar = bars + 8u * place;
         if (!mbar_try_wait(bar, parity)) {
             const long long t0 = clock64();
-            while (!mbar_try_wait(bar, parity) && !*dead)
-                if (clock64() - t0 > kWaitCycles) {
-                    *dead = 1;
-                    err[kErrWait] = 1;
+            while (!mbar_try_wait(bar, parity))
+                if (clock64() - t0 > waits.cycles) {
+                    asm volatile("st.shared.u32 [%0], %1;" ::"r"(late()), "r"(1) : "memory");
+                    waits.err[kErrWait] = 1;
+                    break;
                 }
         }
         if (S == 1) team.sync();         // plain loads of the fill just before
@@ -222,25 +244,36 @@ struct Rows {
     // This thread has read the place (before a barrier of the team, then leave).
     __device__ __forceinline__ void done() const { fence_proxy_async_smem(); }
     // The place that begins with token t is read by the whole team: fills it with
-    // what comes S places later.
-    __device__ __forceinline__ void leave(const Team& team, int t, int end) {
+    // what comes S places later.  False, for the whole team alike, where a wait for
+    // the place ran out: no barrier is armed again and no copy issued, and the team
+    // goes to drain.  (Between the word's stores, in enter, and this look at it lies
+    // a barrier of the team; before it can be stored again lie those of the next
+    // place, which has the other word.)
+    __device__ __forceinline__ bool leave(const Team& team, int t, int end) {
+        uint32_t ran_out;
+        asm volatile("ld.shared.u32 %0, [%1];" : "=r"(ran_out) : "r"(late()) : "memory");
+        if (ran_out) return false;
         if (const int n = place_count(t, end, per, S)) fill(team, place, t + S * per, n);
         if (++place == S) {
             place = 0;
             parity ^= 1u;
         }
+        return true;
     }
-    // copies in flight after a wait that ran out: bounded
-    __device__ __forceinline__ void drain() const {
-        if (!*dead) return;
-        for (int i = 0; i < S; ++i) {
-            const long long t0 = clock64();
-            while (!mbar_try_wait(bars + 8u * i, parity ^ (i < place ? 1u : 0u)) &&
-                   clock64() - t0 < kWaitCycles) {
-            }
-        }
+    __device__ __forceinline__ void drain(int t, int end) const {
+        drain_places<S>(bars, place, parity, t, end, per, waits.cycles);
     }
 };
+
+// one thread: the barriers and words of `teams` teams
+template <int S>
+__device__ __forceinline__ void init_bars(uint64_t* bars, int teams) {
+    for (int i = 0; i < teams; ++i, bars += S + 1) {
+        for (int k = 0; k < S; ++k) mbar_init((uint32_t)__cvta_generic_to_shared(bars + k), 1);
+        bars[S] = 0;
+    }
+    fence_mbar_init();
+}
 
 constexpr int kJoinThreads = 256;
 // columns a warp holds at most.  163847 tokens x 960, bfloat16: 226 us with 512 and
@@ -260,9 +293,8 @@ __global__ void __launch_bounds__(kJoinThreads, join_ctas(32 * N * NV))
 k_norm_join(JoinArgs a, int team_warps, int64_t chunk, const T* __restrict__ x, const T* __restrict__ y,
             T* __restrict__ xo, T* __restrict__ no) {
     __shared__ __align__(16) float slots[2 * kJoinThreads / 32 * 4];
-    __shared__ __align__(8) uint64_t bars[kJoinThreads / 32 * kStages];
-    __shared__ int dead;
-    check_offsets(a.offsets, a.B, a.T, a.err);
+    __shared__ __align__(8) uint64_t bars[kJoinThreads / 32 * (kStages + 1)];
+    check_offsets(a.offsets, a.B, a.T, a.waits.err);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     Team team{team_warps, warp % team_warps, warp / team_warps, slots, 0, kJoinThreads / 32};
     const int64_t number = (int64_t)blockIdx.x * (kJoinThreads / 32 / team_warps) + team.id;
@@ -272,14 +304,10 @@ k_norm_join(JoinArgs a, int team_warps, int64_t chunk, const T* __restrict__ x, 
     const T* gate = (const T*)a.gate;
     const T* wp = (const T*)a.w_post;
     const T* wn = (const T*)a.w_pre;
-    Rows<T, N, 2> rows(bars, &dead, a, team.id);
+    Rows<T, N, 2> rows(bars, a, team.id);
     rows.p[0] = x;
     rows.p[1] = y;
-    if (threadIdx.x == 0) {
-        for (int i = 0; i < kJoinThreads / 32 * kStages; ++i) mbar_init((uint32_t)__cvta_generic_to_shared(bars + i), 1);
-        dead = 0;
-        fence_mbar_init();
-    }
+    if (threadIdx.x == 0) init_bars<kStages>(bars, kJoinThreads / 32);
     __syncthreads();
     if (t0 >= t1) return;
     rows.start(team, t0, t1);
@@ -356,7 +384,10 @@ k_norm_join(JoinArgs a, int team_warps, int64_t chunk, const T* __restrict__ x, 
         if (last) rows.done();
         const float square = team.sum(total(q));           // with a barrier
         if (last) {
-            rows.leave(team, first, t1);
+            if (!rows.leave(team, first, t1)) {
+                rows.drain(first, t1);
+                break;
+            }
             first = t + 1;
         }
         if (!no) continue;
@@ -372,7 +403,6 @@ k_norm_join(JoinArgs a, int team_warps, int64_t chunk, const T* __restrict__ x, 
             o.store(no + (int64_t)t * a.D + c);
         }
     }
-    rows.drain();
 }
 
 // ---- gradient ------------------------------------------------------------------
@@ -399,9 +429,8 @@ __global__ void __launch_bounds__(kGradWarps * 32, 1) k_norm_join_grad(JoinArgs 
     using Ring = Rows<T, N, 4, S>;
     constexpr int WARPS = kGradWarps;
     __shared__ __align__(16) float slots[2 * WARPS * 4];
-    __shared__ __align__(8) uint64_t bars[WARPS * S];
-    __shared__ int dead;
-    check_offsets(a.offsets, a.B, a.T, a.err);
+    __shared__ __align__(8) uint64_t bars[WARPS * (S + 1)];
+    check_offsets(a.offsets, a.B, a.T, a.waits.err);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     Team team{p.team_warps, warp % p.team_warps, warp / p.team_warps, slots, 0, WARPS};
     const int cta_teams = WARPS / p.team_warps;
@@ -411,16 +440,12 @@ __global__ void __launch_bounds__(kGradWarps * 32, 1) k_norm_join_grad(JoinArgs 
     const float inv_d = 1.f / (float)a.D;
     const T *x = (const T*)g.x_out, *y = (const T*)g.y, *dxo = (const T*)g.d_x_out, *dn = (const T*)g.d_n;
     const T *gate = (const T*)a.gate, *wp = (const T*)a.w_post, *wn = (const T*)a.w_pre;
-    Ring rows(bars, &dead, a, team.id);
+    Ring rows(bars, a, team.id);
     rows.p[0] = x;
     rows.p[1] = y;
     rows.p[2] = dxo;
     rows.p[3] = dn;
-    if (threadIdx.x == 0) {
-        for (int i = 0; i < WARPS * S; ++i) mbar_init((uint32_t)__cvta_generic_to_shared(bars + i), 1);
-        dead = 0;
-        fence_mbar_init();
-    }
+    if (threadIdx.x == 0) init_bars<S>(bars, WARPS);
     __syncthreads();
     rows.start(team, t0, t1);
     using F = typename Pack<T, N>::F;
@@ -558,7 +583,10 @@ __global__ void __launch_bounds__(kGradWarps * 32, 1) k_norm_join_grad(JoinArgs 
         if (last) rows.done();
         const float along_u = team.sum(total(m));          // with a barrier
         if (last) {
-            rows.leave(team, first, t1);
+            if (!rows.leave(team, first, t1)) {
+                rows.drain(first, t1);
+                break;
+            }
             first = t + 1;
         }
         if (!ALL && !y) continue;
@@ -573,7 +601,6 @@ __global__ void __launch_bounds__(kGradWarps * 32, 1) k_norm_join_grad(JoinArgs 
             o.store((T*)g.dy + at + c);
         }
     }
-    rows.drain();
     if (t0 < t1 && (ALL || y)) flush();
     if (g.d_gate && team.warp == 0 && lane == 0) p.open[number] = open;
     // the CTA's sums for the norms' weights, teams in order

@@ -17,7 +17,8 @@ def ifvs():
 
 
 @pytest.fixture
-def layers(ifvs):
+def layers(ifvs, monkeypatch):
+    monkeypatch.setenv("IFVS_TEST_STALL_COPIES", "0")      # a handle that looks at it
     L = ifvs.Layers()
     yield L
     L.close()
@@ -51,3 +52,56 @@ def test_a_later_error_does_not_hide_an_earlier_one(ifvs, layers):
     with pytest.raises(ifvs.IfvsError) as e:
         layers.status()
     assert "offsets" in str(e.value)
+
+
+# ---- waits that run out.  While IFVS_TEST_STALL_COPIES is 1 the barriers expect
+# more bytes than the copies deliver: every wait runs out after its bound, the call
+# reports it, and the same call is right again once it is 0.
+
+def _same(a, b):
+    for p, q in zip(a, b):
+        assert (p is None and q is None) or torch.equal(p, q)
+
+
+def _runs_out(ifvs, monkeypatch, call):
+    want = call()
+    monkeypatch.setenv("IFVS_TEST_STALL_COPIES", "1")
+    for _ in range(2):
+        with pytest.raises(ifvs.IfvsError) as e:
+            call()
+        assert e.value.code == ifvs.IFVS_ERR_TIMEOUT
+    monkeypatch.setenv("IFVS_TEST_STALL_COPIES", "0")
+    _same(want, call())
+
+
+def _join_args(T, D, dtype, seed=1):
+    r = _rand(seed)
+    off = torch.tensor([0, T // 3, T // 3, T], dtype=torch.int64, device="cuda")
+    v = [r(T, D).to(dtype), r(T, D).to(dtype), r(3, D).to(dtype), r(D).to(dtype), r(D).to(dtype)]
+    return v, [r(T, D).to(dtype), r(T, D).to(dtype)], off
+
+
+# rows on 16 bytes and between them, one warp a team and many, few tokens a team and
+# many, a ring of one place (float32 rows beyond 4096 in the gradient)
+@pytest.mark.parametrize("T,D,dtype", [(1, 64, torch.float32), (5, 128, torch.bfloat16), (20_000, 96, torch.float16),
+                                       (20_000, 97, torch.bfloat16), (3_000, 1030, torch.bfloat16), (700, 8192, torch.float32)])
+def test_norm_join_wait_runs_out(ifvs, layers, monkeypatch, T, D, dtype):
+    v, d, off = _join_args(T, D, dtype)
+    _runs_out(ifvs, monkeypatch, lambda: layers.norm_join(*v, offsets=off, eps=EPS))
+    _runs_out(ifvs, monkeypatch, lambda: layers.norm_join(v[0], w_pre=v[4], eps=EPS))
+    _runs_out(ifvs, monkeypatch, lambda: layers.norm_join_grad(*v, *d, offsets=off, eps=EPS))
+    _runs_out(ifvs, monkeypatch, lambda: layers.norm_join_grad(v[0], w_pre=v[4], d_n=d[1], eps=EPS))
+
+
+def test_a_bad_argument_does_not_hide_a_wait_that_ran_out(ifvs, layers, monkeypatch):
+    v, _, off = _join_args(50, 64, torch.float32)
+    s = torch.cuda.current_stream()
+    monkeypatch.setenv("IFVS_TEST_STALL_COPIES", "1")
+    layers.norm_join(*v, offsets=off, eps=EPS, stream=s)
+    monkeypatch.setenv("IFVS_TEST_STALL_COPIES", "0")
+    _bad_offsets(layers, s)
+    _bad_id(layers, s)
+    with pytest.raises(ifvs.IfvsError) as e:
+        layers.status()
+    assert e.value.code == ifvs.IFVS_ERR_TIMEOUT
+    layers.status()
