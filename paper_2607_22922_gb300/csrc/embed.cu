@@ -46,7 +46,7 @@ k_embed(const T* __restrict__ table, EmbedArgs a, int per_row, int rows, int pie
         if (t < a.T) {
             id[i] = __ldg(a.ids + t);
             if (id[i] < -1 || id[i] >= a.V) {
-                if (col == 0) a.err[kErrId] = 1;
+                if (col == 0) a.waits.err[kErrId] = 1;
                 id[i] = -1;
             }
             if (id[i] >= 0) v[i].load(table + (int64_t)id[i] * a.D + col * N);
@@ -96,7 +96,7 @@ struct Pairs {
 __device__ __forceinline__ uint32_t key_of(const EmbedArgs& a, int64_t i) {
     const int id = __ldg(a.ids + i);
     if (id >= 0 && id < a.V) return (uint32_t)id;
-    if (id != -1) a.err[kErrId] = 1;
+    if (id != -1) a.waits.err[kErrId] = 1;
     return (uint32_t)a.V;
 }
 
@@ -524,24 +524,27 @@ k_embed_sum_rows(const T* __restrict__ d_out, EmbedArgs a, SumPlan p, Pairs sort
     auto fetch = [&](int g, uint32_t key, uint32_t pos) {
         const bool its = lane / HALF == g && key < a.V;
         const uint32_t rows = __popc(__ballot_sync(0xFFFFFFFFu, its)), to = bar + 8 * (g & 1);
-        if (lane == 0) mbar_arrive_expect_tx(to, rows * bytes);
+        if (lane == 0) mbar_arrive_expect_tx(to, rows * bytes + a.waits.extra);
         __syncwarp();
         if (its) bulk_g2s(mine_at + lane % (2 * HALF) * ROW, d_out + (int64_t)pos * a.D + c0, bytes, to, once);
     };
     uint32_t key = keys_at(begin), pos = places_at(begin), next_key = keys_at(begin + 32), next_pos = places_at(begin + 32);
     fetch(0, key, pos);
     fetch(1, key, pos);
-    bool late = false;
     uint32_t parity = 0;
     for (int64_t b = begin; b < end; b += 32) {
         int rows;
         const uint32_t starts = r.starts(a, key, b == begin, &rows);
 #pragma unroll 1
         for (int g = 0; g < GROUPS; ++g) {
-            // a wait that runs out: the sums go on with what is there and are reported
-            if (!late && !mbar_wait_warp(bar + 8 * (g & 1), parity)) {
-                late = true;
-                if (lane == 0) a.err[kErrWait] = 1;
+            // a wait that runs out is reported and ends the warp's work: no barrier is
+            // armed again; the copies of this half and of the other, if it has been
+            // armed, are waited for once more, bounded
+            if (!mbar_wait_warp(bar + 8 * (g & 1), parity, a.waits.cycles)) {
+                if (lane == 0) a.waits.err[kErrWait] = 1;
+                mbar_wait_warp(bar + 8 * (g & 1), parity, a.waits.cycles);
+                if (g + 1 < GROUPS || b + 32 < end) mbar_wait_warp(bar + 8 * (~g & 1), parity ^ ((uint32_t)g & 1u), a.waits.cycles);
+                return;
             }
             parity ^= (uint32_t)g & 1u;
             auto row = [&](Pack<T, N>(&v)[NV], int i) {
@@ -580,8 +583,6 @@ k_embed_sum_rows(const T* __restrict__ d_out, EmbedArgs a, SumPlan p, Pairs sort
         next_pos = places_at(b + 64);
     }
     r.flush(a, end < a.T && __ldcg(sorted.key + end) == r.run, partial, d_table);
-    if (late)                            // copies in flight: bounded
-        for (int h = 0; h < 2; ++h) mbar_wait_warp(bar + 8 * h, parity ^ 1u);
 }
 
 // Rows of any alignment: element loads into registers, kAhead rows at a time

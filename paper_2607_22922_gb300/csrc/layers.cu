@@ -159,7 +159,7 @@ int embed_check(const ifvs_layers* L, const int32_t* ids, int64_t T, int64_t V, 
     if (V < 1 || V > 0x7FFFFFFFLL) return report_error(IFVS_ERR_ARG, "V = %lld outside 1..2^31 - 1", (long long)V);
     if (!isfinite(scale)) return report_error(IFVS_ERR_ARG, "scale is not finite");
     if (T > 0) TRY(check_array(ids, 4, "ids"));
-    *a = EmbedArgs{ids, T, V, D, type, scale, L->err, L->num_sms};
+    *a = EmbedArgs{ids, T, V, D, type, scale, waits_of(L), L->num_sms};
     return 0;
 }
 

@@ -157,7 +157,7 @@ struct EmbedArgs {
     int64_t T, V;
     int D, type;
     float scale;
-    int* err;
+    Waits waits;
     int num_sms;
 };
 cudaError_t launch_embed(const EmbedArgs& a, const void* table, void* out, cudaStream_t s);

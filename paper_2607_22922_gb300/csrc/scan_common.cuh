@@ -696,14 +696,14 @@ __device__ __forceinline__ bool mbar_try_wait(uint32_t bar, uint32_t parity) {
 }
 
 // Waits, with every lane of the warp, until the barrier's phase of parity
-// `parity` has completed; false (for the whole warp) when kWaitCycles pass
+// `parity` has completed; false (for the whole warp) when `cycles` pass
 // first.
-__device__ __forceinline__ bool mbar_wait_warp(uint32_t bar, uint32_t parity) {
+__device__ __forceinline__ bool mbar_wait_warp(uint32_t bar, uint32_t parity, long long cycles = kWaitCycles) {
     const long long t0 = clock64();
     for (;;) {
         const bool ok = mbar_try_wait(bar, parity);
         if (__all_sync(0xFFFFFFFFu, ok)) return true;
-        if (__any_sync(0xFFFFFFFFu, clock64() - t0 > kWaitCycles)) return false;
+        if (__any_sync(0xFFFFFFFFu, clock64() - t0 > cycles)) return false;
     }
 }
 

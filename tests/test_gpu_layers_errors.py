@@ -105,3 +105,14 @@ def test_a_bad_argument_does_not_hide_a_wait_that_ran_out(ifvs, layers, monkeypa
         layers.status()
     assert e.value.code == ifvs.IFVS_ERR_TIMEOUT
     layers.status()
+
+
+# rows of one slice and of several, tokens of one part and of many, padding
+@pytest.mark.parametrize("T,D,V,dtype", [(1, 8, 3, torch.float32), (31, 128, 3, torch.bfloat16), (5_000, 64, 700, torch.float32),
+                                         (90_001, 960, 400, torch.float16), (400_000, 256, 9_000, torch.bfloat16)])
+def test_embed_grad_wait_runs_out(ifvs, layers, monkeypatch, T, D, V, dtype):
+    r = _rand(T)
+    d_out = r(T, D).to(dtype)
+    ids = torch.randint(-1, V, (T,), dtype=torch.int32, device="cuda", generator=torch.Generator("cuda").manual_seed(T))
+    ids[0] = V - 1
+    _runs_out(ifvs, monkeypatch, lambda: (layers.embed_grad(d_out, ids, V=V),))
