@@ -84,15 +84,16 @@ __device__ __forceinline__ uint32_t setup(Bars<S>& b) {
 }
 
 // The end of a kernel: with everything in order the roles have waited for
-// their own work; a dead CTA waits here for what it had in flight.
+// their own work; a dead CTA waits here, bounded, for what it had in flight: a
+// warp for all of its copies, a thread for its MMAs.
 template <int CG, int EPI, int S>
-__device__ __forceinline__ void finish(Bars<S>& b, uint32_t tmem, int filled, bool issues) {
+__device__ __forceinline__ void finish(Bars<S>& b, uint32_t tmem, int filled, bool issues, const Waits& waits) {
     __syncwarp();
     __syncthreads();
     if (*(volatile int*)&b.dead) {
-        auto bounded = [](uint32_t bar, uint32_t parity) {
-            const long long t0 = clock64();
-            while (!mbar_try_wait(bar, parity) && clock64() - t0 < kWaitCycles) {
+        const long long t0 = clock64();
+        auto bounded = [&](uint32_t bar, uint32_t parity) {
+            while (!mbar_try_wait(bar, parity) && clock64() - t0 < waits.cycles) {
             }
         };
         if (threadIdx.x / 32 == EPI && issues)       // `filled` is the elected thread's
@@ -230,7 +231,7 @@ __device__ __forceinline__ Item item_of(const Products& all, int i) {
 }
 
 template <int CG, int BN>
-__global__ void __launch_bounds__(192, 1) k_products(const __grid_constant__ Products all, bool f16, int* err) {
+__global__ void __launch_bounds__(192, 1) k_products(const __grid_constant__ Products all, bool f16, Waits waits) {
     using Sh = ProductShape<CG, BN>;
     constexpr int EPI = 4, S = Sh::kStages;
     __shared__ __align__(8) Bars<S> bars;
@@ -238,7 +239,7 @@ __global__ void __launch_bounds__(192, 1) k_products(const __grid_constant__ Pro
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int rank = CG == 2 ? (int)cluster_rank() : 0;
     const uint32_t tmem = setup<CG, EPI>(bars);
-    const Watch w{&bars.dead, err};
+    const Watch w{&bars.dead, waits};
     const int first = blockIdx.x / CG, step = gridDim.x / CG;
     int filled = 0;
     wait_before();
@@ -254,7 +255,7 @@ __global__ void __launch_bounds__(192, 1) k_products(const __grid_constant__ Pro
                 for (int k = t.k0; k < t.k1; ++k, r.next(), ++filled) {
                     if (!(ok = w.wait(smem_addr(&bars.empty[r.at]), r.parity ^ 1u))) break;
                     const uint32_t a = ring + r.at * Sh::kStage, bar = smem_addr(&bars.full[r.at]);
-                    if (rank == 0) mbar_arrive_expect_tx(bar, CG * Sh::kStage);
+                    if (rank == 0) mbar_arrive_expect_tx(bar, CG * Sh::kStage + waits.extra);
                     load_tile<CG>(a_mn, a, &t.p->a, row, kRows, k * kStepK, bar);
                     load_tile<CG>(b_mn, a + kABytes, &t.p->b, col, BN / CG, k * kStepK, bar);
                 }
@@ -279,7 +280,7 @@ __global__ void __launch_bounds__(192, 1) k_products(const __grid_constant__ Pro
                     o.mma<CG>(tmem + acc.at * 256, r.at * Sh::kStage, idesc, k == t.k0);
                     mma_commit<CG>(smem_addr(&bars.empty[r.at]));
                 }
-                mma_commit<CG>(smem_addr(&bars.acc_full[acc.at]));
+                if (ok) mma_commit<CG>(smem_addr(&bars.acc_full[acc.at]));
             }
         }
     } else {
@@ -327,7 +328,7 @@ __global__ void __launch_bounds__(192, 1) k_products(const __grid_constant__ Pro
         }
         if (lane == 0) tma_wait_all();
     }
-    finish<CG, EPI>(bars, tmem, filled, rank == 0);
+    finish<CG, EPI>(bars, tmem, filled, rank == 0, waits);
 }
 
 // C = the sum of the parts, in order; up to three products
@@ -381,7 +382,7 @@ __device__ __forceinline__ void load_projections(uint32_t dst, const CUtensorMap
 template <int ACT, int CG, int FT>
 __global__ void __launch_bounds__(HiddenShape<CG, FT>::kEpi * 32 + 64, 1)
 k_hidden(const __grid_constant__ CUtensorMap mx, const __grid_constant__ CUtensorMap mw,
-         const __grid_constant__ CUtensorMap mh, Grid g, bool f16, int* err) {
+         const __grid_constant__ CUtensorMap mh, Grid g, bool f16, Waits waits) {
     using Sh = HiddenShape<CG, FT>;
     constexpr int EPI = Sh::kEpi, S = Sh::kStages;
     __shared__ __align__(8) Bars<S> bars;
@@ -389,7 +390,7 @@ k_hidden(const __grid_constant__ CUtensorMap mx, const __grid_constant__ CUtenso
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int rank = CG == 2 ? (int)cluster_rank() : 0;
     const uint32_t tmem = setup<CG, EPI>(bars);
-    const Watch w{&bars.dead, err};
+    const Watch w{&bars.dead, waits};
     const int tiles = g.m_tiles * g.n_tiles, first = blockIdx.x / CG, step = gridDim.x / CG;
     int filled = 0;
 
@@ -402,7 +403,7 @@ k_hidden(const __grid_constant__ CUtensorMap mx, const __grid_constant__ CUtenso
                 for (int k = 0; k < g.k_steps; ++k, r.next(), ++filled) {
                     if (!(ok = w.wait(smem_addr(&bars.empty[r.at]), r.parity ^ 1u))) break;
                     const uint32_t a = ring + r.at * Sh::kStage, bar = smem_addr(&bars.full[r.at]);
-                    if (rank == 0) mbar_arrive_expect_tx(bar, CG * Sh::kStage);
+                    if (rank == 0) mbar_arrive_expect_tx(bar, CG * Sh::kStage + waits.extra);
                     tma_load<CG>(a, &mx, k * kStepK, (mn.x * CG + rank) * kRows, bar);
                     load_projections<CG, FT>(a + kABytes, &mw, mn.y * FT, g.cols, k * kStepK, rank, bar);
                 }
@@ -425,7 +426,7 @@ k_hidden(const __grid_constant__ CUtensorMap mx, const __grid_constant__ CUtenso
                     o.mma<CG>(tmem + acc.at * 256, r.at * Sh::kStage, idesc, k == 0);
                     mma_commit<CG>(smem_addr(&bars.empty[r.at]));
                 }
-                mma_commit<CG>(smem_addr(&bars.acc_full[acc.at]));
+                if (ok) mma_commit<CG>(smem_addr(&bars.acc_full[acc.at]));
             }
         }
     } else {
@@ -466,7 +467,7 @@ k_hidden(const __grid_constant__ CUtensorMap mx, const __grid_constant__ CUtenso
         }
         if (lane == 0) tma_wait_all();
     }
-    finish<CG, EPI>(bars, tmem, filled, rank == 0);
+    finish<CG, EPI>(bars, tmem, filled, rank == 0, waits);
 }
 
 // ---- h, dg, du from x and dy ---------------------------------------------------------
@@ -490,7 +491,7 @@ __global__ void __launch_bounds__(GradShape<CG, FT>::kEpi * 32 + 64, 1)
 k_hidden_grad(const __grid_constant__ CUtensorMap mx, const __grid_constant__ CUtensorMap mdy,
               const __grid_constant__ CUtensorMap mw, const __grid_constant__ CUtensorMap mwo,
               const __grid_constant__ CUtensorMap mh, const __grid_constant__ CUtensorMap mdg,
-              const __grid_constant__ CUtensorMap mdu, Grid g, bool f16, int* err) {
+              const __grid_constant__ CUtensorMap mdu, Grid g, bool f16, Waits waits) {
     using Sh = GradShape<CG, FT>;
     constexpr int EPI = Sh::kEpi, S = Sh::kStages;
     __shared__ __align__(8) Bars<S> bars;     // slot 0: g | u, slot 1: dh (both places)
@@ -498,7 +499,7 @@ k_hidden_grad(const __grid_constant__ CUtensorMap mx, const __grid_constant__ CU
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int rank = CG == 2 ? (int)cluster_rank() : 0;
     const uint32_t tmem = setup<CG, EPI>(bars);
-    const Watch w{&bars.dead, err};
+    const Watch w{&bars.dead, waits};
     const int tiles = g.m_tiles * g.n_tiles, first = blockIdx.x / CG, step = gridDim.x / CG;
     int filled = 0;
 
@@ -513,12 +514,12 @@ k_hidden_grad(const __grid_constant__ CUtensorMap mx, const __grid_constant__ CU
                     if (!(ok = w.wait(smem_addr(&bars.empty[r.at]), r.parity ^ 1u))) break;
                     const uint32_t a = ring + r.at * Sh::kStage, bar = smem_addr(&bars.full[r.at]);
                     if (k < g.k_steps) {
-                        if (rank == 0) mbar_arrive_expect_tx(bar, CG * Sh::kDhBytes);
+                        if (rank == 0) mbar_arrive_expect_tx(bar, CG * Sh::kDhBytes + waits.extra);
                         tma_load<CG>(a, &mdy, k * kStepK, row, bar);
                         load_tile<CG>(true, a + kABytes, &mwo, mn.y * FT + rank * (FT / CG), FT / CG, k * kStepK, bar);
                     } else {
                         const int kk = (k - g.k_steps) * kStepK;
-                        if (rank == 0) mbar_arrive_expect_tx(bar, CG * Sh::kStage);
+                        if (rank == 0) mbar_arrive_expect_tx(bar, CG * Sh::kStage + waits.extra);
                         tma_load<CG>(a, &mx, kk, row, bar);
                         load_projections<CG, FT>(a + kABytes, &mw, mn.y * FT, g.cols, kk, rank, bar);
                     }
@@ -551,7 +552,7 @@ k_hidden_grad(const __grid_constant__ CUtensorMap mx, const __grid_constant__ CU
                         of_gu.mma<CG>(tmem + FT, r.at * Sh::kStage, id_gu, k == g.k_steps);
                     mma_commit<CG>(smem_addr(&bars.empty[r.at]));
                 }
-                mma_commit<CG>(smem_addr(&bars.acc_full[0]));
+                if (ok) mma_commit<CG>(smem_addr(&bars.acc_full[0]));
             }
         }
     } else {
@@ -604,7 +605,7 @@ k_hidden_grad(const __grid_constant__ CUtensorMap mx, const __grid_constant__ CU
         }
         if (lane == 0) tma_wait_all();
     }
-    finish<CG, EPI>(bars, tmem, filled, rank == 0);
+    finish<CG, EPI>(bars, tmem, filled, rank == 0, waits);
 }
 
 // ---- a few tokens ----------------------------------------------------------------------
@@ -787,9 +788,9 @@ struct Plan {
         if (e != cudaSuccess) return e;
         const bool f16 = a.type == IFVS_T_F16;
         e = pairs ? launch_tiles<2>(k_products<2, 256>, all.items, a.num_sms, 192, ProductShape<2, 256>::kSmem, chain, s, all,
-                                    f16, a.err)
+                                    f16, a.waits)
                   : launch_tiles<1>(k_products<1, 128>, all.items, a.num_sms, 192, ProductShape<1, 128>::kSmem, chain, s, all,
-                                    f16, a.err);
+                                    f16, a.waits);
         if (e != cudaSuccess || joined == 0) return e;
         int64_t most = 0;
         for (int j = 0; j < joined; ++j) most = parts.n[j] > most ? parts.n[j] : most;
@@ -880,7 +881,7 @@ cudaError_t launch_ffn(const FfnArgs& a, const void* x, void* y, uint8_t* work, 
         if (e != cudaSuccess) return e;
         const Grid g{ceil_div(a.T, kRows * cg()), ceil_div(a.F, ft()), ceil_div(a.D, kStepK), (int)a.T, a.F};
         return launch_tiles<cg()>(k_hidden<act(), cg(), ft()>, (int64_t)g.m_tiles * g.n_tiles, a.num_sms, Sh::kEpi * 32 + 64,
-                                  Sh::kSmem, false, s, mx, mw, mh, g, a.type == IFVS_T_F16, a.err);
+                                  Sh::kSmem, false, s, mx, mw, mh, g, a.type == IFVS_T_F16, a.waits);
     };
     const cudaError_t e = with_act(a.act, [&](auto act) {
         return hidden_pairs(a) ? run(act, std::integral_constant<int, 2>(), std::integral_constant<int, 128>())
@@ -915,7 +916,7 @@ cudaError_t launch_ffn_grad(const FfnArgs& a, const void* x, const void* dy, voi
         const Grid g{ceil_div(a.T, kRows * cg()), ceil_div(F, ft()), ceil_div(D, kStepK), (int)a.T, a.F};
         return launch_tiles<cg()>(k_hidden_grad<act(), cg(), ft()>, (int64_t)g.m_tiles * g.n_tiles, a.num_sms,
                                   Sh::kEpi * 32 + 64, Sh::kSmem, false, s, mx, mdy, mw, mwo, mh, mdg, mdu, g,
-                                  a.type == IFVS_T_F16, a.err);
+                                  a.type == IFVS_T_F16, a.waits);
     };
     const cudaError_t e = with_act(a.act, [&](auto act) {
         return hidden_pairs(a) ? run(act, std::integral_constant<int, 2>(), std::integral_constant<int, 128>())

@@ -199,7 +199,7 @@ int ffn_check(const ifvs_layers* L, const ifvs_ffn_params* p, FfnArgs* a) {
         return report_error(IFVS_ERR_UNSUPPORTED, "D = %d and F = %d must be multiples of 8", p->D, p->F);
     TRY(check_array(p->w_in, 16, "w_in"));
     TRY(check_array(p->w_out, 16, "w_out"));
-    *a = FfnArgs{p->T, p->D, p->F, p->type, p->act, p->w_in, p->w_out, L->err, L->num_sms};
+    *a = FfnArgs{p->T, p->D, p->F, p->type, p->act, p->w_in, p->w_out, waits_of(L), L->num_sms};
     return 0;
 }
 

@@ -186,7 +186,7 @@ struct FfnArgs {
     int64_t T;
     int D, F, type, act;
     const void *w_in, *w_out;
-    int* err;
+    Waits waits;
     int num_sms;
 };
 size_t ffn_bytes(const FfnArgs& a);

@@ -179,16 +179,16 @@ __device__ __forceinline__ void mbar_arrive(uint32_t bar) {
 // kernel waits, bounded again, for its copies and MMAs before it returns.
 struct Watch {
     volatile int* dead;     // shared memory
-    int* err;
+    Waits by;
     __device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity) const {
         if (mbar_try_wait(bar, parity)) return true;
         const long long t0 = clock64();
         for (;;) {
             if (mbar_try_wait(bar, parity)) return true;
             if (*dead) return false;
-            if (clock64() - t0 > kWaitCycles) {
+            if (clock64() - t0 > by.cycles) {
                 *dead = 1;
-                err[kErrWait] = 1;
+                by.err[kErrWait] = 1;
                 return false;
             }
         }

@@ -116,3 +116,13 @@ def test_embed_grad_wait_runs_out(ifvs, layers, monkeypatch, T, D, V, dtype):
     ids = torch.randint(-1, V, (T,), dtype=torch.int32, device="cuda", generator=torch.Generator("cuda").manual_seed(T))
     ids[0] = V - 1
     _runs_out(ifvs, monkeypatch, lambda: (layers.embed_grad(d_out, ids, V=V),))
+
+
+# single CTAs and pairs, sums whole and in parts, few tiles and many
+@pytest.mark.parametrize("T,D,F,act,dtype", [(5, 64, 72, "silu", torch.float16), (129, 960, 264, "gelu", torch.bfloat16),
+                                             (3_000, 128, 344, "relu", torch.float16), (12_001, 136, 392, "silu", torch.bfloat16)])
+def test_ffn_wait_runs_out(ifvs, layers, monkeypatch, T, D, F, act, dtype):
+    r = _rand(T)
+    x, dy, w_in, w_out = (r(*s).to(dtype) for s in ((T, D), (T, D), (2 * F, D), (D, F)))
+    _runs_out(ifvs, monkeypatch, lambda: (layers.ffn(x, w_in, w_out, act=act),))
+    _runs_out(ifvs, monkeypatch, lambda: layers.ffn_grad(x, w_in, w_out, dy, act=act))
