@@ -759,25 +759,28 @@ cudaError_t sort_by_id(const EmbedArgs& a, Pairs p0, Pairs p1, uint32_t* counts,
         cfg.attrs = attr;
         cfg.numAttrs = 1;
         const uint32_t magic = (uint32_t)((1ull << 32) / (unsigned)(warps() * 32 * rounds) + 1);
-        return cudaLaunchKernelEx(&cfg, kernel, a, plan, p0, rounds, magic);
+        const cudaError_t n = next_launch();
+        return n != cudaSuccess ? n : cudaLaunchKernelEx(&cfg, kernel, a, plan, p0, rounds, magic);
     };
     if (a.T <= cluster_tokens(16)) return in_cluster(std::integral_constant<int, 16>());
     if (a.T <= cluster_tokens(32)) return in_cluster(std::integral_constant<int, 32>());
     *sorted = plan.passes & 1 ? p0 : p1;
     const int tiles = (int)sort_tiles(a);
     uint32_t* totals = counts + (int64_t)kBins * tiles;
-    cudaError_t e = cudaSuccess;
-    auto then = [&](cudaError_t r) { e = e == cudaSuccess ? r : e; };
+    // No launch after one that failed: the scatter writes where the counts say.
     for (int pass = 0; pass < plan.passes; ++pass) {
         const Pairs in = pass == 0 ? Pairs{nullptr, nullptr} : (pass & 1 ? p0 : p1);
         const Pairs out = pass & 1 ? p1 : p0;
-        then(launch_kernel(k_sort_count, dim3(tiles), dim3(kTileWarps * 32), 0, pass > 0, s, a, plan, pass, in, counts, tiles));
-        then(launch_kernel(k_sort_scan, dim3((unsigned)(((1 << plan.bits) + 7) / 8)), dim3(256), 0, true, s, counts, 1 << plan.bits, tiles,
-                           totals));
-        then(launch_kernel(k_sort_scatter, dim3(tiles), dim3(kTileWarps * 32), 0, true, s, a, plan, pass, in, out,
-                           (const uint32_t*)counts, tiles, (const uint32_t*)totals));
+        cudaError_t e = launch_next(k_sort_count, dim3(tiles), dim3(kTileWarps * 32), 0, pass > 0, s, a, plan, pass, in, counts, tiles);
+        if (e == cudaSuccess)
+            e = launch_next(k_sort_scan, dim3((unsigned)(((1 << plan.bits) + 7) / 8)), dim3(256), 0, true, s, counts, 1 << plan.bits,
+                            tiles, totals);
+        if (e == cudaSuccess)
+            e = launch_next(k_sort_scatter, dim3(tiles), dim3(kTileWarps * 32), 0, true, s, a, plan, pass, in, out,
+                            (const uint32_t*)counts, tiles, (const uint32_t*)totals);
+        if (e != cudaSuccess) return e;
     }
-    return e;
+    return cudaSuccess;
 }
 
 template <class T>
@@ -792,14 +795,14 @@ cudaError_t sum_by_id(const EmbedArgs& a, const void* d_out, Pairs sorted, float
         const auto kernel = wide ? k_embed_sum_rows<T, 2> : k_embed_sum_rows<T, 1>;
         e = allow_smem(kernel, smem);
         if (e == cudaSuccess)
-            e = launch_kernel(kernel, dim3((unsigned)((warps + kSumWarps - 1) / kSumWarps)), dim3(kSumWarps * 32), smem, true, s,
+            e = launch_next(kernel, dim3((unsigned)((warps + kSumWarps - 1) / kSumWarps)), dim3(kSumWarps * 32), smem, true, s,
                               (const T*)d_out, a, p, sorted, partial, (T*)d_table);
     } else {
-        e = launch_kernel(k_embed_sum<T>, dim3((unsigned)((warps + 7) / 8)), dim3(256), 0, true, s, (const T*)d_out, a, p, sorted,
+        e = launch_next(k_embed_sum<T>, dim3((unsigned)((warps + 7) / 8)), dim3(256), 0, true, s, (const T*)d_out, a, p, sorted,
                           partial, (T*)d_table);
     }
     if (e == cudaSuccess && p.parts > 1)
-        e = launch_kernel(k_embed_join<T>, dim3((unsigned)((p.parts + 7) / 8), (unsigned)((a.D + 127) / 128)), dim3(256), 0, true, s,
+        e = launch_next(k_embed_join<T>, dim3((unsigned)((p.parts + 7) / 8), (unsigned)((a.D + 127) / 128)), dim3(256), 0, true, s,
                           a, p, sorted, (const float*)partial, (T*)d_table);
     return e;
 }
@@ -814,6 +817,8 @@ cudaError_t launch_embed(const EmbedArgs& a, const void* table, void* out, cudaS
         const int per_row = a.D / (vec ? N : 1), rows = 256 / per_row, pieces = 256 % per_row;
         const int64_t n = a.T * per_row;
         const unsigned grid = (unsigned)((n + 256 * kEmbedPieces - 1) / (256 * kEmbedPieces));
+        const cudaError_t e = next_launch();
+        if (e != cudaSuccess) return e;
         if (vec)
             k_embed<T, N><<<grid, 256, 0, s>>>((const T*)table, a, per_row, rows, pieces, (T*)out);
         else

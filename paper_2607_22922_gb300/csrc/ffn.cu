@@ -728,7 +728,8 @@ cudaError_t launch_tiles(void (*kernel)(P...), int64_t items, int num_sms, int t
     attr[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = chain ? 2 : 1;
-    return cudaLaunchKernelEx(&cfg, kernel, args...);
+    e = next_launch();
+    return e != cudaSuccess ? e : cudaLaunchKernelEx(&cfg, kernel, args...);
 }
 
 // Products of one launch, in the order they are added
@@ -795,8 +796,8 @@ struct Plan {
         int64_t most = 0;
         for (int j = 0; j < joined; ++j) most = parts.n[j] > most ? parts.n[j] : most;
         const dim3 grid((unsigned)((most + 1023) / 1024), (unsigned)joined);
-        return f16 ? launch_kernel(k_join_parts<__half>, grid, dim3(256), 0, true, s, parts)
-                   : launch_kernel(k_join_parts<__nv_bfloat16>, grid, dim3(256), 0, true, s, parts);
+        return f16 ? launch_next(k_join_parts<__half>, grid, dim3(256), 0, true, s, parts)
+                   : launch_next(k_join_parts<__nv_bfloat16>, grid, dim3(256), 0, true, s, parts);
     }
 };
 
@@ -813,7 +814,7 @@ cudaError_t launch_few(const FfnArgs& a, const void* x, const void* w, void* out
     FewArgs<T> f{(const T*)x, (const T*)w, (T*)out, (int)a.T, rows, K, 8};
     while (f.cta_rows > 1 && ceil_div(rows, f.cta_rows) < 2 * a.num_sms) f.cta_rows /= 2;
     const dim3 grid((unsigned)ceil_div(rows, f.cta_rows));
-    auto go = [&](auto tt) { return launch_kernel(k_few<T, PAIR, ACT, tt()>, grid, dim3(256), 0, !PAIR, s, f); };
+    auto go = [&](auto tt) { return launch_next(k_few<T, PAIR, ACT, tt()>, grid, dim3(256), 0, !PAIR, s, f); };
     if (a.T == 1) return go(std::integral_constant<int, 1>());
     if (a.T == 2) return go(std::integral_constant<int, 2>());
     return go(std::integral_constant<int, kFewTokens>());

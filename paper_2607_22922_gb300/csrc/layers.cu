@@ -12,6 +12,8 @@
 
 using namespace ifvs;
 
+thread_local int ifvs::launches_to_failure = 0;
+
 namespace {
 // A workspace that a captured graph may still use
 struct Retired {
@@ -28,6 +30,7 @@ struct ifvs_layers {
     size_t work_bytes = 0;
     bool work_captured = false;     // a captured graph holds its address
     bool may_stall = false;         // waits may be made to run out
+    bool may_fail = false;          // launches may be made to fail
     Retired* retired = nullptr;
     int* err_host = nullptr;        // the error words, page-locked
     int* err = nullptr;             // their device address
@@ -77,6 +80,8 @@ struct Call {
     // bytes: of workspace (0: the call has no place in the order of those that use it)
     int begin(size_t bytes) {
         if (!guard.ok) return report_error(IFVS_ERR_CUDA, "device %d cannot be made current", L->device);
+        const char* n = L->may_fail ? getenv("IFVS_FAIL_LAUNCH") : nullptr;
+        launches_to_failure = n ? atoi(n) : 0;
         if (bytes == 0) return 0;
         cudaStreamCaptureStatus st = cudaStreamCaptureStatusNone;
         if (!waits) CUDA_TRY(cudaStreamIsCapturing(s, &st));
@@ -221,6 +226,7 @@ int ifvs_layers_create(ifvs_layers** out, int32_t device) {
     if (!L) return report_error(IFVS_ERR_OOM, "out of host memory");
     L->device = device;
     L->may_stall = getenv("IFVS_TEST_STALL_COPIES") != nullptr;
+    L->may_fail = getenv("IFVS_FAIL_LAUNCH") != nullptr;
     void *h = nullptr, *d = nullptr;
     cudaError_t e = cudaDeviceGetAttribute(&L->num_sms, cudaDevAttrMultiProcessorCount, device);
     // blocking: ordered after the caller's work on the legacy default stream

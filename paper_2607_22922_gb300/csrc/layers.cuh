@@ -151,6 +151,20 @@ struct Waits {
     long long cycles;       // a wait's bound
 };
 
+// Failure injection for tests of calls that fail on their way: the launch that the
+// calling thread's count reaches 0 at is not made and fails (layers.cu sets the
+// count; 0: none does).
+extern thread_local int launches_to_failure;
+inline cudaError_t next_launch() {
+    return launches_to_failure > 0 && --launches_to_failure == 0 ? cudaErrorLaunchOutOfResources : cudaSuccess;
+}
+// launch_kernel, as one of a call's launches
+template <class K, class... A>
+inline cudaError_t launch_next(K* kernel, dim3 grid, dim3 block, size_t smem, bool chain, cudaStream_t s, A... args) {
+    const cudaError_t e = next_launch();
+    return e != cudaSuccess ? e : launch_kernel(kernel, grid, block, smem, chain, s, args...);
+}
+
 // ---- launchers --------------------------------------------------------------
 struct EmbedArgs {
     const int32_t* ids;

@@ -768,7 +768,8 @@ cudaError_t launch_norm_join(const JoinArgs& a, const void* x, const void* y, vo
         using T = decltype(t);
         const int cta_teams = kJoinThreads / 32 / sh.warps;
         const size_t smem = ring_bytes<T, n(), 2>(cta_teams, a.D);
-        const cudaError_t e = allow_smem(k_norm_join<T, n(), nv()>, smem);
+        cudaError_t e = allow_smem(k_norm_join<T, n(), nv()>, smem);
+        if (e == cudaSuccess) e = next_launch();
         if (e != cudaSuccess) return e;
         // as many CTAs as run at once; fewer tokens: one per team
         const int64_t want = (a.T + cta_teams - 1) / cta_teams, by_smem = 226 * 1024 / ((int64_t)smem + 2048);
@@ -829,8 +830,7 @@ cudaError_t launch_norm_join_grad(const JoinArgs& a, const JoinGrads& g, uint8_t
             smem = smem > sums ? smem : sums;
             const cudaError_t r = allow_smem(kernel, smem);
             if (r != cudaSuccess) return r;
-            kernel<<<(unsigned)p.ctas, kGradWarps * 32, smem, s>>>(a, g, p);
-            return cudaGetLastError();
+            return launch_next(kernel, dim3((unsigned)p.ctas), dim3(kGradWarps * 32), smem, false, s, a, g, p);
         };
         cudaError_t e = cudaSuccess;
         if (a.T > 0) {
@@ -843,7 +843,7 @@ cudaError_t launch_norm_join_grad(const JoinArgs& a, const JoinGrads& g, uint8_t
         const int64_t teams = g.d_gate ? p.teams : 0, clears = g.d_gate && a.offsets ? (a.B + kClearRows - 1) / kClearRows : 0;
         GradPlan q = p;
         q.teams = teams;
-        return launch_kernel(k_join_finish<T>, dim3((unsigned)(2 + (teams + kFinishWarps - 1) / kFinishWarps + clears), (unsigned)((a.D + 127) / 128)),
+        return launch_next(k_join_finish<T>, dim3((unsigned)(2 + (teams + kFinishWarps - 1) / kFinishWarps + clears), (unsigned)((a.D + 127) / 128)),
                              dim3(kFinishWarps * 32), 0, true, s, a, g, q);
     };
     auto of16 = [&](auto t) {

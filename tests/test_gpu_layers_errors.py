@@ -18,7 +18,8 @@ def ifvs():
 
 @pytest.fixture
 def layers(ifvs, monkeypatch):
-    monkeypatch.setenv("IFVS_TEST_STALL_COPIES", "0")      # a handle that looks at it
+    monkeypatch.setenv("IFVS_TEST_STALL_COPIES", "0")      # a handle that looks at them
+    monkeypatch.setenv("IFVS_FAIL_LAUNCH", "0")
     L = ifvs.Layers()
     yield L
     L.close()
@@ -126,3 +127,46 @@ def test_ffn_wait_runs_out(ifvs, layers, monkeypatch, T, D, F, act, dtype):
     x, dy, w_in, w_out = (r(*s).to(dtype) for s in ((T, D), (T, D), (2 * F, D), (D, F)))
     _runs_out(ifvs, monkeypatch, lambda: (layers.ffn(x, w_in, w_out, act=act),))
     _runs_out(ifvs, monkeypatch, lambda: layers.ffn_grad(x, w_in, w_out, dy, act=act))
+
+
+# ---- calls that fail between their launches.  While IFVS_FAIL_LAUNCH is n the n-th
+# launch of a call is not made and fails.
+
+def _calls(layers):
+    v, d, off = _join_args(3_000, 64, torch.float32)
+    r = _rand(7)
+    x, dy, w_in, w_out = (r(*s).to(torch.bfloat16) for s in ((40, 64), (40, 64), (272, 64), (64, 136)))
+    x1 = x[:1].clone()
+    grads = {}
+    for T, V in ((30_000, 500), (90_000, 600)):      # one cluster's sort; two passes of three launches
+        ids = torch.randint(-1, V, (T,), dtype=torch.int32, device="cuda", generator=torch.Generator("cuda").manual_seed(T))
+        rows = r(T, 20)
+        grads["embed_grad %d" % T] = lambda s, ids=ids, rows=rows, V=V: (layers.embed_grad(rows, ids, V=V, stream=s),)
+    return {**grads,
+            "norm_join": lambda s: layers.norm_join(*v, offsets=off, eps=EPS, stream=s),
+            "norm_join_grad": lambda s: layers.norm_join_grad(*v, *d, offsets=off, eps=EPS, stream=s),
+            "ffn, one token": lambda s: (layers.ffn(x1, w_in, w_out, stream=s),),
+            "ffn": lambda s: (layers.ffn(x, w_in, w_out, stream=s),),
+            "ffn_grad": lambda s: layers.ffn_grad(x, w_in, w_out, dy, stream=s)}
+
+
+LAUNCHES = {"embed_grad 30000": 3, "embed_grad 90000": 8, "norm_join": 1, "norm_join_grad": 2, "ffn, one token": 2, "ffn": 2,
+            "ffn_grad": 2}
+
+
+@pytest.mark.parametrize("name", sorted(LAUNCHES))
+def test_no_launch_follows_one_that_failed(ifvs, layers, monkeypatch, name):
+    """A kernel whose input was not made would go by what the workspace holds from
+    earlier calls: the sort's scatter writes where the counts say."""
+    call = _calls(layers)[name]
+    want = call(None)
+    for n in range(1, LAUNCHES[name] + 1):
+        monkeypatch.setenv("IFVS_FAIL_LAUNCH", str(n))
+        with pytest.raises(ifvs.IfvsError) as e:
+            call(None)
+        assert e.value.code == ifvs.IFVS_ERR_CUDA
+        monkeypatch.setenv("IFVS_FAIL_LAUNCH", "0")
+        torch.cuda.synchronize()
+        _same(want, call(None))
+    monkeypatch.setenv("IFVS_FAIL_LAUNCH", str(LAUNCHES[name] + 1))
+    _same(want, call(None))
