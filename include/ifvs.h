@@ -471,7 +471,9 @@ int ifvs_get_conditioning(ifvs_index* ix, float* bank, float* W, uint32_t flags)
  * with, until the handle is freed; its replays and other calls that use the
  * workspace are ordered by the caller.  Errors that a kernel finds (a token id
  * or offsets out of range, a bounded wait that ran out) are returned by the call
- * itself when it waits, else by ifvs_layers_status.  (For tests: while
+ * itself when it waits, else by ifvs_layers_status.  A call that fails between
+ * its launches keeps its place in the order: what it had enqueued is waited for
+ * by the calls after it and, with stream NULL, by itself.  (For tests: while
  * IFVS_FAIL_LAUNCH holds n >= 1, the n-th launch of every call fails, of handles
  * created while the variable was set.)  A handle may be used by one thread at a
  * time.

@@ -116,11 +116,15 @@ struct Call {
             L->work_captured = true;
         return 0;
     }
-    int end() {
-        if (ordered) CUDA_TRY(cudaEventRecord(L->done, s));
-        if (!waits) return IFVS_OK;
-        CUDA_TRY(cudaStreamSynchronize(s));
-        return take_error(L);
+    // launched: of the call's launches.  Kernels enqueued before one that failed use
+    // the workspace and the arrays like those of a whole call.
+    int end(cudaError_t launched) {
+        const int rc = launched == cudaSuccess ? IFVS_OK : fail(launched, "a launch", __LINE__);
+        cudaError_t e = ordered ? cudaEventRecord(L->done, s) : cudaSuccess;
+        if (e == cudaSuccess && waits) e = cudaStreamSynchronize(s);
+        if (rc != IFVS_OK) return rc;
+        if (e != cudaSuccess) return fail(e, "the call's end", __LINE__);
+        return waits ? take_error(L) : IFVS_OK;
     }
 };
 
@@ -279,8 +283,7 @@ int ifvs_embed(ifvs_layers* L, const void* table, int64_t V, int32_t D, int32_t 
     if (T > 0) TRY(check_array(out, elem_bytes(type), "out"));
     Call c(L, stream);
     TRY(c.begin(0));
-    if (T > 0) CUDA_TRY(launch_embed(a, table, out, c.s));
-    return c.end();
+    return c.end(T > 0 ? launch_embed(a, table, out, c.s) : cudaSuccess);
 }
 
 int ifvs_embed_grad(ifvs_layers* L, const void* d_out, const int32_t* ids, int64_t T, int64_t V, int32_t D, int32_t type,
@@ -291,8 +294,7 @@ int ifvs_embed_grad(ifvs_layers* L, const void* d_out, const int32_t* ids, int64
     TRY(check_array(d_table, elem_bytes(type), "d_table"));
     Call c(L, stream);
     TRY(c.begin(embed_grad_bytes(a)));
-    CUDA_TRY(launch_embed_grad(a, d_out, d_table, L->work, c.s));
-    return c.end();
+    return c.end(launch_embed_grad(a, d_out, d_table, L->work, c.s));
 }
 
 int ifvs_norm_join(ifvs_layers* L, const ifvs_join_params* p, const void* x, const void* y, void* x_out, void* n_out) {
@@ -308,8 +310,7 @@ int ifvs_norm_join(ifvs_layers* L, const ifvs_join_params* p, const void* x, con
     TRY(check_array(x, e, "x"));
     Call c(L, p->stream);
     TRY(c.begin(0));
-    if (a.T > 0) CUDA_TRY(launch_norm_join(a, x, y, x_out, n_out, c.s));
-    return c.end();
+    return c.end(a.T > 0 ? launch_norm_join(a, x, y, x_out, n_out, c.s) : cudaSuccess);
 }
 
 int ifvs_norm_join_grad(ifvs_layers* L, const ifvs_join_params* p, const void* x_out, const void* y, const void* d_x_out,
@@ -335,8 +336,7 @@ int ifvs_norm_join_grad(ifvs_layers* L, const ifvs_join_params* p, const void* x
     Call c(L, p->stream);
     TRY(c.begin(norm_join_grad_bytes(a)));
     const JoinGrads g{x_out, y, d_x_out, d_n, dx, dy, d_gate, d_w_post, d_w_pre};
-    CUDA_TRY(launch_norm_join_grad(a, g, L->work, c.s));
-    return c.end();
+    return c.end(launch_norm_join_grad(a, g, L->work, c.s));
 }
 
 int ifvs_ffn(ifvs_layers* L, const ifvs_ffn_params* p, const void* x, void* y) {
@@ -348,8 +348,7 @@ int ifvs_ffn(ifvs_layers* L, const ifvs_ffn_params* p, const void* x, void* y) {
     }
     Call c(L, p->stream);
     TRY(c.begin(ffn_bytes(a)));
-    if (a.T > 0) CUDA_TRY(launch_ffn(a, x, y, L->work, c.s));
-    return c.end();
+    return c.end(a.T > 0 ? launch_ffn(a, x, y, L->work, c.s) : cudaSuccess);
 }
 
 int ifvs_ffn_grad(ifvs_layers* L, const ifvs_ffn_params* p, const void* x, const void* dy, void* dx, void* d_w_in,
@@ -365,8 +364,7 @@ int ifvs_ffn_grad(ifvs_layers* L, const ifvs_ffn_params* p, const void* x, const
     TRY(check_array(d_w_out, 16, "d_w_out"));
     Call c(L, p->stream);
     TRY(c.begin(ffn_grad_bytes(a)));
-    CUDA_TRY(launch_ffn_grad(a, x, dy, dx, d_w_in, d_w_out, L->work, c.s));
-    return c.end();
+    return c.end(launch_ffn_grad(a, x, dy, dx, d_w_in, d_w_out, L->work, c.s));
 }
 
 }  // extern "C"

@@ -170,3 +170,43 @@ def test_no_launch_follows_one_that_failed(ifvs, layers, monkeypatch, name):
         _same(want, call(None))
     monkeypatch.setenv("IFVS_FAIL_LAUNCH", str(LAUNCHES[name] + 1))
     _same(want, call(None))
+
+
+@pytest.mark.parametrize("name", sorted(LAUNCHES))
+def test_a_call_that_fails_on_its_way_keeps_its_place(ifvs, layers, monkeypatch, name):
+    """What such a call had enqueued (behind 50 ms of other work here) is waited for
+    by the next call that uses the workspace, on another stream, and by the call
+    itself where it has no stream."""
+    call = _calls(layers)[name]
+    want = call(None)
+    made = LAUNCHES[name]
+    for n in range(1, made + 1):
+        first, second = torch.cuda.Stream(), torch.cuda.Stream()
+        torch.cuda.synchronize()
+        for s in (first, None):
+            here = first if s is first else torch.cuda.default_stream()
+            with torch.cuda.stream(here):
+                torch.cuda._sleep(100_000_000)
+                slept = torch.cuda.Event()
+                slept.record(here)
+                monkeypatch.setenv("IFVS_FAIL_LAUNCH", str(n))
+                with pytest.raises(ifvs.IfvsError) as e:
+                    call(s)
+                monkeypatch.setenv("IFVS_FAIL_LAUNCH", "0")
+            assert e.value.code == ifvs.IFVS_ERR_CUDA
+            if s is None:
+                assert n == 1 or slept.query()
+            else:
+                assert not slept.query()
+                with torch.cuda.stream(second):
+                    got = call(second)
+                    done = torch.cuda.Event()
+                    done.record(second)
+                done.synchronize()
+                # calls without workspace have no place in the order
+                assert slept.query() or name == "norm_join"
+                _same(want, got)
+            torch.cuda.synchronize()
+    monkeypatch.setenv("IFVS_FAIL_LAUNCH", str(made + 1))
+    _same(want, call(None))
+    layers.status()
