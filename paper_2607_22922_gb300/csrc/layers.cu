@@ -190,7 +190,7 @@ int join_check(const ifvs_layers* L, const ifvs_join_params* p, bool block, Join
         TRY(check_array(p->w_post, e, "w_post"));
     else if (p->w_post || p->gate)
         return report_error(IFVS_ERR_ARG, "w_post and gate must be NULL without y");
-    *a = JoinArgs{p->T, p->n_seq, p->D, p->type, p->n_seq == 1 ? nullptr : p->offsets, p->gate, p->w_post, p->w_pre,
+    *a = JoinArgs{p->T, p->n_seq, p->D, p->type, p->n_seq == 1 ? nullptr : p->offsets, p->offsets, p->gate, p->w_post, p->w_pre,
                   block ? p->res_scale : 1.f, p->eps, waits_of(L), L->num_sms};
     return 0;
 }
@@ -310,7 +310,7 @@ int ifvs_norm_join(ifvs_layers* L, const ifvs_join_params* p, const void* x, con
     TRY(check_array(x, e, "x"));
     Call c(L, p->stream);
     TRY(c.begin(0));
-    return c.end(a.T > 0 ? launch_norm_join(a, x, y, x_out, n_out, c.s) : cudaSuccess);
+    return c.end(launch_norm_join(a, x, y, x_out, n_out, c.s));
 }
 
 int ifvs_norm_join_grad(ifvs_layers* L, const ifvs_join_params* p, const void* x_out, const void* y, const void* d_x_out,

@@ -182,6 +182,7 @@ struct JoinArgs {
     int64_t T, B;
     int D, type;
     const int64_t* offsets;      // null: B = 1
+    const int64_t* given;        // the caller's, of any B: to be checked, or null
     const void *gate, *w_post, *w_pre;
     float rho, eps;
     Waits waits;

@@ -287,6 +287,9 @@ size_t ring_bytes(int teams, int D) {
     return (size_t)teams * S * A * Rows<T, N, A, S>::stride_of(D);
 }
 
+// Without tokens: what the other kernels look at on their way
+__global__ void __launch_bounds__(256) k_check_offsets(JoinArgs a) { check_offsets(a.given, a.B, a.T, a.waits.err); }
+
 // Tokens [chunk team, chunk (team + 1)) of team number `team`
 template <class T, int N, int NV>
 __global__ void __launch_bounds__(kJoinThreads, join_ctas(32 * N * NV))
@@ -294,7 +297,7 @@ k_norm_join(JoinArgs a, int team_warps, int64_t chunk, const T* __restrict__ x, 
             T* __restrict__ xo, T* __restrict__ no) {
     __shared__ __align__(16) float slots[2 * kJoinThreads / 32 * 4];
     __shared__ __align__(8) uint64_t bars[kJoinThreads / 32 * (kStages + 1)];
-    check_offsets(a.offsets, a.B, a.T, a.waits.err);
+    check_offsets(a.given, a.B, a.T, a.waits.err);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     Team team{team_warps, warp % team_warps, warp / team_warps, slots, 0, kJoinThreads / 32};
     const int64_t number = (int64_t)blockIdx.x * (kJoinThreads / 32 / team_warps) + team.id;
@@ -430,7 +433,7 @@ __global__ void __launch_bounds__(kGradWarps * 32, 1) k_norm_join_grad(JoinArgs 
     constexpr int WARPS = kGradWarps;
     __shared__ __align__(16) float slots[2 * WARPS * 4];
     __shared__ __align__(8) uint64_t bars[WARPS * (S + 1)];
-    check_offsets(a.offsets, a.B, a.T, a.waits.err);
+    check_offsets(a.given, a.B, a.T, a.waits.err);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     Team team{p.team_warps, warp % p.team_warps, warp / p.team_warps, slots, 0, WARPS};
     const int cta_teams = WARPS / p.team_warps;
@@ -718,6 +721,12 @@ __global__ void __launch_bounds__(kFinishWarps * 32) k_join_finish(JoinArgs a, J
 
 // ---- host ------------------------------------------------------------------------
 
+cudaError_t check_without_tokens(const JoinArgs& a, cudaStream_t s) {
+    if (!a.given) return cudaSuccess;
+    const int64_t want = (a.B + 255) / 256, most = 8 * a.num_sms;
+    return launch_next(k_check_offsets, dim3((unsigned)(want < most ? want : most)), dim3(256), 0, false, s, a);
+}
+
 // Elements per access: of 16, 8 or 4 bytes where every row of every array begins on
 // a multiple of that, else one
 template <class... P>
@@ -762,6 +771,7 @@ using Counts = std::integer_sequence<int, NV...>;
 
 cudaError_t launch_norm_join(const JoinArgs& a, const void* x, const void* y, void* x_out, void* n_out,
                              cudaStream_t s) {
+    if (a.T == 0) return check_without_tokens(a, s);
     const int N = access_elems(a, x, y, x_out, n_out);
     const Shape sh = team_shape(a.D, N, join_columns(a.D));
     auto go = [&](auto t, auto n, auto nv) {
@@ -853,8 +863,9 @@ cudaError_t launch_norm_join_grad(const JoinArgs& a, const JoinGrads& g, uint8_t
         if (N == 2) return pick<T, 2>(sh.accesses, Counts<2, 4, 8>(), go);
         return pick<T, 1>(sh.accesses, Counts<4, 8, 16>(), go);
     };
-    if (a.T == 0 && g.d_gate) {     // no team: the gates' gradients are all zeros
-        const cudaError_t e = cudaMemsetAsync(g.d_gate, 0, (size_t)a.B * a.D * elem_bytes(a.type), s);
+    if (a.T == 0) {                 // no team: the gates' gradients are all zeros
+        cudaError_t e = check_without_tokens(a, s);
+        if (e == cudaSuccess && g.d_gate) e = cudaMemsetAsync(g.d_gate, 0, (size_t)a.B * a.D * elem_bytes(a.type), s);
         if (e != cudaSuccess) return e;
     }
     if (a.type == IFVS_T_F16) return of16(__half());

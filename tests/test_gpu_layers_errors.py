@@ -210,3 +210,22 @@ def test_a_call_that_fails_on_its_way_keeps_its_place(ifvs, layers, monkeypatch,
     monkeypatch.setenv("IFVS_FAIL_LAUNCH", str(made + 1))
     _same(want, call(None))
     layers.status()
+
+
+# ---- offsets that break their rules are reported whatever their number
+
+@pytest.mark.parametrize("T,bad", [(50, [5, 40]), (50, [0, 49]), (50, [0, 51]), (50, [-1, 50]), (50, [50, 0]), (0, [0, 1]),
+                                   (0, [-1, 0]), (0, [0, 0, 5]), (0, [0, 3, 0])])
+def test_offsets_of_one_sequence_and_of_no_tokens_are_checked(ifvs, layers, T, bad):
+    x, w = torch.ones(T, 24, device="cuda"), torch.ones(24, device="cuda")
+    gate, good = torch.ones(len(bad) - 1, 24, device="cuda"), [0] * (len(bad) - 1) + [T]
+    for offsets in (bad, good):
+        off = torch.tensor(offsets, dtype=torch.int64, device="cuda")
+        for call in (lambda: layers.norm_join(x, x, gate, w, w, offsets=off),
+                     lambda: layers.norm_join_grad(x, x, gate, w, w, x, x, offsets=off)):
+            if offsets is good:
+                call()
+                continue
+            with pytest.raises(ifvs.IfvsError) as e:
+                call()
+            assert e.value.code == ifvs.IFVS_ERR_ARG and "offsets" in str(e.value)
