@@ -28,8 +28,8 @@ constexpr size_t kMaxSmem = 227 * 1024 - 512;             // beside the static s
 template <int ACT>
 __device__ __forceinline__ void activation(float g, float& v, float& slope) {
     if (ACT == IFVS_ACT_RELU) {
-        v = g > 0.f ? g : 0.f;
-        slope = g > 0.f ? 1.f : 0.f;
+        v = g <= 0.f ? 0.f : g;              // a NaN passes
+        slope = g > 0.f ? 1.f : v;
     } else if (ACT == IFVS_ACT_SILU) {
         const float p = __fdividef(1.f, 1.f + __expf(-g));
         v = g * p;

@@ -66,3 +66,21 @@ def test_norm_join_of_as_many_tokens_as_there_can_be(layers):
         a = (x[s], y[s], gate, w_post, w_pre)
         _check((xo[s], no[s]), ref.norm_join(*a, here, 0.7, EPS))
         _check((dx[s], dy[s]), ref.norm_join_grad(*a, dxo[s], dn[s], here, 0.7, EPS)[:2])
+
+
+@pytest.mark.parametrize("act", ["silu", "gelu", "relu"])
+@pytest.mark.parametrize("T", [1, 4, 7, 200])
+def test_ffn_passes_a_nan_gate_on(layers, act, T):
+    """A NaN weight of one gate column reaches every output that the column's hidden
+    values do: all of y and dx, its own rows of d_w_in and column of d_w_out."""
+    D, F, bad = 64, 72, 5
+    r = _rand(T)
+    x, dy, w_in, w_out = (r(*s).bfloat16() for s in ((T, D), (T, D), (2 * F, D), (D, F)))
+    w_in[bad, 3] = float("nan")
+    assert layers.ffn(x, w_in, w_out, act=act).isnan().all()
+    dx, d_w_in, d_w_out = layers.ffn_grad(x, w_in, w_out, dy, act=act)
+    assert dx.isnan().all()
+    rows, cols = d_w_in.isnan().all(1), d_w_out.isnan().all(0)
+    assert rows[bad] and rows[F + bad] and cols[bad]
+    others = [i for i in range(F) if i != bad]
+    assert not d_w_in[others].isnan().any() and not d_w_in[F:][others].isnan().any() and not d_w_out[:, others].isnan().any()
