@@ -540,7 +540,9 @@ __global__ void __launch_bounds__(kGradWarps * 32, 1) k_norm_join_grad(JoinArgs 
         }
         const float3 q = team.sum3(total(qx), total(qz), total(qy));
         const float ix_ = ALL || dn ? rsqrtf(fmaf(q.x, inv_d, a.eps)) : 0.f, iy_ = rsqrtf(fmaf(q.z, inv_d, a.eps));
-        const F ix = both<F>(ix_), along = both<F>(-ix_ * ix_ * ix_ * (q.y * inv_d)), iy = both<F>(iy_);
+        // the mean first: of a row of zeros it is 0, and the cube of its 1 / rms may
+        // lie beyond float32 (from eps = 2e-26 down)
+        const F ix = both<F>(ix_), along = both<F>(-(q.y * inv_d * ix_) * ix_ * ix_), iy = both<F>(iy_);
         F v[NV][kF], m = both<F>(0.f);                     // du / rms(y); du u
         Pack<T, N> ry[NV];
 #pragma unroll
@@ -593,7 +595,7 @@ __global__ void __launch_bounds__(kGradWarps * 32, 1) k_norm_join_grad(JoinArgs 
             first = t + 1;
         }
         if (!ALL && !y) continue;
-        const F back = both<F>(-iy_ * iy_ * (along_u * inv_d));
+        const F back = both<F>(-(along_u * inv_d * iy_) * iy_);
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int c = col + i * step;

@@ -84,3 +84,20 @@ def test_ffn_passes_a_nan_gate_on(layers, act, T):
     assert rows[bad] and rows[F + bad] and cols[bad]
     others = [i for i in range(F) if i != bad]
     assert not d_w_in[others].isnan().any() and not d_w_in[F:][others].isnan().any() and not d_w_out[:, others].isnan().any()
+
+
+@pytest.mark.parametrize("eps", [1e-12, 1e-30, 1e-37])
+@pytest.mark.parametrize("type_", ["f32", "bf16"])
+def test_norm_join_rows_of_zeros_with_a_small_eps(layers, type_, eps):
+    """1 / rms of such a row is eps^(-1/2), whose powers leave float32."""
+    r, dt = _rand(9), TYPES[type_]
+    T, D = 24, 72
+    off = torch.tensor([0, 10, 24], dtype=torch.int64, device="cuda")
+    x, y, dxo, dn = (r(T, D).to(dt) for _ in range(4))
+    x[3:9], y[5:12] = 0, 0
+    dn *= 2.0 ** -30                    # times 1 / rms within the types' range
+    dxo *= 2.0 ** -30
+    a = (x, y, (1 + 0.3 * r(2, D)).to(dt), (1 + 0.1 * r(D)).to(dt), (1 + 0.1 * r(D)).to(dt))
+    kw = dict(offsets=off, res_scale=0.7, eps=eps)
+    _check(layers.norm_join(*a, **kw), ref.norm_join(*a, off, 0.7, eps))
+    _check(layers.norm_join_grad(*a, dxo, dn, **kw), ref.norm_join_grad(*a, dxo, dn, off, 0.7, eps))
