@@ -432,14 +432,23 @@ def _is_vector(a, name):
     return t == name and a.dim() == 1
 
 
-def _dev(a, shape, dtype, name):
-    """Address of a contiguous CUDA tensor of this shape and type (None -> NULL)."""
+def _on(L, a, name):
+    """The number of a tensor's device, which has to be the handle's."""
+    at = a.get_device()
+    if at != L.device:
+        raise ValueError("%s is on %s, the handle on cuda:%d" % (name, a.device, L.device))
+    return at
+
+
+def _dev(a, shape, dtype, name, at):
+    """Address of a contiguous tensor of this shape and type on CUDA device
+    ``at`` (None -> NULL)."""
     if a is None:
         return None
     if a.shape != shape or a.dtype != dtype:
         raise ValueError("%s is %s %s, expected %s %s" % (name, tuple(a.shape), a.dtype, shape, dtype))
-    if not a.is_cuda or not a.is_contiguous():
-        raise ValueError("%s must be a contiguous CUDA tensor" % name)
+    if a.get_device() != at or at < 0 or not a.is_contiguous():
+        raise ValueError("%s must be a contiguous tensor on cuda:%d" % (name, max(at, 0)))
     return a.data_ptr() or 256      # a tensor without elements has no address; none is read
 
 
@@ -455,9 +464,14 @@ def _like(a, *shape):
     return a.new_empty(shape)
 
 
+class _LayersHandle(C.c_void_p):
+    device = None       # its number
+
+
 def ifvs_layers_create(device=0):
-    h = C.c_void_p()
+    h = _LayersHandle()
     _check(_lib.ifvs_layers_create(C.byref(h), device))
+    h.device = device
     return h
 
 
@@ -477,11 +491,11 @@ def _ids(ids):
 
 def ifvs_embed(L, table, ids, scale=1.0, out=None, stream=None):
     """out [T][D] = scale table[ids]; id -1 gives a row of zeros."""
-    (V, D), T = table.shape, _ids(ids)
+    (V, D), T, at = table.shape, _ids(ids), _on(L, table, "table")
     out = _like(table, T, D) if out is None else out
     dt = table.dtype
-    _check(_lib.ifvs_embed(L, _dev(table, (V, D), dt, "table"), V, D, _type(table),
-                           _dev(ids, (T,), ids.dtype, "ids"), T, scale, _dev(out, (T, D), dt, "out"),
+    _check(_lib.ifvs_embed(L, _dev(table, (V, D), dt, "table", at), V, D, _type(table),
+                           _dev(ids, (T,), ids.dtype, "ids", at), T, scale, _dev(out, (T, D), dt, "out", at),
                            _stream(stream)))
     return out
 
@@ -489,12 +503,12 @@ def ifvs_embed(L, table, ids, scale=1.0, out=None, stream=None):
 def ifvs_embed_grad(L, d_out, ids, scale=1.0, V=None, d_table=None, stream=None):
     """d_table [V][D]: per id, scale times the sum of its tokens' rows of d_out
     (zeros for ids without tokens).  Give V or d_table."""
-    (T, D), dt = d_out.shape, d_out.dtype
+    (T, D), dt, at = d_out.shape, d_out.dtype, _on(L, d_out, "d_out")
     d_table = _like(d_out, V, D) if d_table is None else d_table
     V = int(d_table.shape[0])
-    _check(_lib.ifvs_embed_grad(L, _dev(d_out, (T, D), dt, "d_out"), _dev(ids, (_ids(ids),), ids.dtype, "ids"),
-                                _same_length(ids, T), V, D, _type(d_out), scale,
-                                _dev(d_table, (V, D), dt, "d_table"), _stream(stream)))
+    _check(_lib.ifvs_embed_grad(L, _dev(d_out, (T, D), dt, "d_out", at),
+                                _dev(ids, (_ids(ids),), ids.dtype, "ids", at), _same_length(ids, T), V, D, _type(d_out), scale,
+                                _dev(d_table, (V, D), dt, "d_table", at), _stream(stream)))
     return d_table
 
 
@@ -505,15 +519,15 @@ def _same_length(ids, T):
 
 
 def _join_params(x, gate, w_post, w_pre, offsets, res_scale, eps, stream):
-    (T, D), dt = x.shape, x.dtype
-    B, at = 1, None
+    (T, D), dt, at = x.shape, x.dtype, x.get_device()
+    B, off = 1, None
     if offsets is not None:
         if not _is_vector(offsets, "int64") or offsets.shape[0] < 2:
             raise ValueError("offsets must be a vector of B + 1 int64")
         B = offsets.shape[0] - 1
-        at = _dev(offsets, (B + 1,), offsets.dtype, "offsets")
-    p = JoinParams(T, D, _type(x), B, at, _dev(gate, (B, D), dt, "gate"), _dev(w_post, (D,), dt, "w_post"),
-                   _dev(w_pre, (D,), dt, "w_pre"), res_scale, eps, _stream(stream))
+        off = _dev(offsets, (B + 1,), offsets.dtype, "offsets", at)
+    p = JoinParams(T, D, _type(x), B, off, _dev(gate, (B, D), dt, "gate", at),
+                   _dev(w_post, (D,), dt, "w_post", at), _dev(w_pre, (D,), dt, "w_pre", at), res_scale, eps, _stream(stream))
     return p, (T, D), (B, D), dt
 
 
@@ -522,13 +536,14 @@ def ifvs_norm_join(L, x, y=None, gate=None, w_post=None, w_pre=None, offsets=Non
     """x_out = res_scale x + gate * w_post * y / rms(y) and, with w_pre,
     n_out = w_pre * x_out / rms(x_out); gate [B][D] by the sequences that
     ``offsets`` delimits.  Without y only n_out, of x.  Returns (x_out, n_out)."""
+    at = _on(L, x, "x")
     p, td, _, dt = _join_params(x, gate, w_post, w_pre, offsets, res_scale, eps, stream)
     if y is not None and x_out is None:
         x_out = _like(x, *td)
     if w_pre is not None and n_out is None:
         n_out = _like(x, *td)
-    _check(_lib.ifvs_norm_join(L, C.byref(p), _dev(x, td, dt, "x"), _dev(y, td, dt, "y"),
-                               _dev(x_out, td, dt, "x_out"), _dev(n_out, td, dt, "n_out")))
+    _check(_lib.ifvs_norm_join(L, C.byref(p), _dev(x, td, dt, "x", at), _dev(y, td, dt, "y", at),
+                               _dev(x_out, td, dt, "x_out", at), _dev(n_out, td, dt, "n_out", at)))
     return x_out, n_out
 
 
@@ -538,6 +553,7 @@ def ifvs_norm_join_grad(L, x_out, y=None, gate=None, w_post=None, w_pre=None, d_
     """Gradients through ifvs_norm_join from those of x_out and n_out (either
     may be None).  Returns (dx, dy, d_gate, d_w_post, d_w_pre), None where the
     forward call had no such input."""
+    at = _on(L, x_out, "x_out")
     p, td, bd, dt = _join_params(x_out, gate, w_post, w_pre, offsets, res_scale, eps, stream)
     dx = _like(x_out, *td) if dx is None else dx
     if y is not None:
@@ -549,39 +565,41 @@ def ifvs_norm_join_grad(L, x_out, y=None, gate=None, w_post=None, w_pre=None, d_
         d_w_pre = _like(x_out, td[1])
     d = td[1:]
     _check(_lib.ifvs_norm_join_grad(
-        L, C.byref(p), _dev(x_out, td, dt, "x_out"), _dev(y, td, dt, "y"),
-        _dev(d_x_out, td, dt, "d_x_out"), _dev(d_n, td, dt, "d_n"), _dev(dx, td, dt, "dx"),
-        _dev(dy, td, dt, "dy"), _dev(d_gate, bd, dt, "d_gate"), _dev(d_w_post, d, dt, "d_w_post"),
-        _dev(d_w_pre, d, dt, "d_w_pre")))
+        L, C.byref(p), _dev(x_out, td, dt, "x_out", at), _dev(y, td, dt, "y", at),
+        _dev(d_x_out, td, dt, "d_x_out", at), _dev(d_n, td, dt, "d_n", at), _dev(dx, td, dt, "dx", at),
+        _dev(dy, td, dt, "dy", at), _dev(d_gate, bd, dt, "d_gate", at), _dev(d_w_post, d, dt, "d_w_post", at),
+        _dev(d_w_pre, d, dt, "d_w_pre", at)))
     return dx, dy, d_gate, d_w_post, d_w_pre
 
 
 def _ffn_params(x, w_in, w_out, act, stream):
-    (T, D), F, dt = x.shape, w_out.shape[1], x.dtype
+    (T, D), F, dt, at = x.shape, w_out.shape[1], x.dtype, x.get_device()
     if act not in _ACTS:
         raise ValueError("act must be one of %s" % sorted(_ACTS))
-    p = FfnParams(T, D, F, _type(x), _ACTS[act], _dev(w_in, (2 * F, D), dt, "w_in"),
-                  _dev(w_out, (D, F), dt, "w_out"), _stream(stream))
+    p = FfnParams(T, D, F, _type(x), _ACTS[act], _dev(w_in, (2 * F, D), dt, "w_in", at),
+                  _dev(w_out, (D, F), dt, "w_out", at), _stream(stream))
     return p, (T, D), F, dt
 
 
 def ifvs_ffn(L, x, w_in, w_out, act="silu", y=None, stream=None):
     """y = (act(x Wg^T) * (x Wu^T)) w_out^T, w_in [2F][D] = [Wg; Wu], w_out [D][F]."""
+    at = _on(L, x, "x")
     p, td, _, dt = _ffn_params(x, w_in, w_out, act, stream)
     y = _like(x, *td) if y is None else y
-    _check(_lib.ifvs_ffn(L, C.byref(p), _dev(x, td, dt, "x"), _dev(y, td, dt, "y")))
+    _check(_lib.ifvs_ffn(L, C.byref(p), _dev(x, td, dt, "x", at), _dev(y, td, dt, "y", at)))
     return y
 
 
 def ifvs_ffn_grad(L, x, w_in, w_out, dy, act="silu", dx=None, d_w_in=None, d_w_out=None, stream=None):
     """Gradients (dx, d_w_in, d_w_out) through ifvs_ffn from dy."""
+    at = _on(L, x, "x")
     p, td, F, dt = _ffn_params(x, w_in, w_out, act, stream)
     dx = _like(x, *td) if dx is None else dx
     d_w_in = _like(x, 2 * F, td[1]) if d_w_in is None else d_w_in
     d_w_out = _like(x, td[1], F) if d_w_out is None else d_w_out
-    _check(_lib.ifvs_ffn_grad(L, C.byref(p), _dev(x, td, dt, "x"), _dev(dy, td, dt, "dy"),
-                              _dev(dx, td, dt, "dx"), _dev(d_w_in, (2 * F, td[1]), dt, "d_w_in"),
-                              _dev(d_w_out, (td[1], F), dt, "d_w_out")))
+    _check(_lib.ifvs_ffn_grad(L, C.byref(p), _dev(x, td, dt, "x", at), _dev(dy, td, dt, "dy", at),
+                              _dev(dx, td, dt, "dx", at), _dev(d_w_in, (2 * F, td[1]), dt, "d_w_in", at),
+                              _dev(d_w_out, (td[1], F), dt, "d_w_out", at)))
     return dx, d_w_in, d_w_out
 
 
