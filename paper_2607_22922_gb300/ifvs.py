@@ -406,6 +406,13 @@ def ifvs_get_conditioning(ix, B, Mr, W_shape):
 
 
 # ---- layers of a predicate encoder: CUDA tensors only ----------------------
+#
+# Streams.  A call with a stream (a torch stream or a raw handle) is enqueued
+# there: its inputs have to be ready in that stream's order, and to stay alive
+# until its work is done, which for tensors of another stream is the caller's to
+# see to (Tensor.record_stream).  Outputs that the call makes are that stream's
+# memory.  A call without one runs after everything that torch's current stream
+# has been given so far, and has written its outputs when it returns.
 
 _ACTS = {"silu": IFVS_ACT_SILU, "gelu": IFVS_ACT_GELU, "relu": IFVS_ACT_RELU}
 _TYPES = {}         # torch's element types -> IFVS_T_*, filled on first use
@@ -432,11 +439,20 @@ def _is_vector(a, name):
     return t == name and a.dim() == 1
 
 
-def _on(L, a, name):
-    """The number of a tensor's device, which has to be the handle's."""
+def _on(L, a, name, stream):
+    """The number of a tensor's device, which has to be the handle's.  For a call
+    without a stream, waits for torch's current one: the handle's own stream is
+    ordered after the default stream alone."""
     at = a.get_device()
     if at != L.device:
         raise ValueError("%s is on %s, the handle on cuda:%d" % (name, a.device, L.device))
+    if not stream:
+        import torch
+        here = torch.cuda.current_stream(at)
+        if here.cuda_stream:
+            if torch.cuda.is_current_stream_capturing():
+                raise ValueError("a call in a capture needs the captured stream")
+            here.synchronize()
     return at
 
 
@@ -447,8 +463,8 @@ def _dev(a, shape, dtype, name, at):
         return None
     if a.shape != shape or a.dtype != dtype:
         raise ValueError("%s is %s %s, expected %s %s" % (name, tuple(a.shape), a.dtype, shape, dtype))
-    if a.get_device() != at or at < 0 or not a.is_contiguous():
-        raise ValueError("%s must be a contiguous tensor on cuda:%d" % (name, max(at, 0)))
+    if a.get_device() != at or not a.is_contiguous():
+        raise ValueError("%s must be a contiguous tensor on cuda:%d" % (name, at))
     return a.data_ptr() or 256      # a tensor without elements has no address; none is read
 
 
@@ -460,7 +476,17 @@ def _stream(stream):
     return stream.cuda_stream or _LEGACY_STREAM
 
 
-def _like(a, *shape):
+def _like(a, stream, *shape):
+    """An output: memory of the stream that the call runs on."""
+    if stream:
+        import torch
+        raw = stream if isinstance(stream, int) else stream.cuda_stream
+        raw = 0 if raw == _LEGACY_STREAM else raw
+        if raw != torch.cuda.current_stream(a.device).cuda_stream:
+            if isinstance(stream, int):
+                stream = torch.cuda.ExternalStream(raw, a.device) if raw else torch.cuda.default_stream(a.device)
+            with torch.cuda.stream(stream):
+                return a.new_empty(shape)
     return a.new_empty(shape)
 
 
@@ -491,8 +517,8 @@ def _ids(ids):
 
 def ifvs_embed(L, table, ids, scale=1.0, out=None, stream=None):
     """out [T][D] = scale table[ids]; id -1 gives a row of zeros."""
-    (V, D), T, at = table.shape, _ids(ids), _on(L, table, "table")
-    out = _like(table, T, D) if out is None else out
+    (V, D), T, at = table.shape, _ids(ids), _on(L, table, "table", stream)
+    out = _like(table, stream, T, D) if out is None else out
     dt = table.dtype
     _check(_lib.ifvs_embed(L, _dev(table, (V, D), dt, "table", at), V, D, _type(table),
                            _dev(ids, (T,), ids.dtype, "ids", at), T, scale, _dev(out, (T, D), dt, "out", at),
@@ -503,8 +529,8 @@ def ifvs_embed(L, table, ids, scale=1.0, out=None, stream=None):
 def ifvs_embed_grad(L, d_out, ids, scale=1.0, V=None, d_table=None, stream=None):
     """d_table [V][D]: per id, scale times the sum of its tokens' rows of d_out
     (zeros for ids without tokens).  Give V or d_table."""
-    (T, D), dt, at = d_out.shape, d_out.dtype, _on(L, d_out, "d_out")
-    d_table = _like(d_out, V, D) if d_table is None else d_table
+    (T, D), dt, at = d_out.shape, d_out.dtype, _on(L, d_out, "d_out", stream)
+    d_table = _like(d_out, stream, V, D) if d_table is None else d_table
     V = int(d_table.shape[0])
     _check(_lib.ifvs_embed_grad(L, _dev(d_out, (T, D), dt, "d_out", at),
                                 _dev(ids, (_ids(ids),), ids.dtype, "ids", at), _same_length(ids, T), V, D, _type(d_out), scale,
@@ -518,8 +544,8 @@ def _same_length(ids, T):
     return int(T)
 
 
-def _join_params(x, gate, w_post, w_pre, offsets, res_scale, eps, stream):
-    (T, D), dt, at = x.shape, x.dtype, x.get_device()
+def _join_params(x, gate, w_post, w_pre, offsets, res_scale, eps, stream, at=None):
+    (T, D), dt, at = x.shape, x.dtype, x.get_device() if at is None else at
     B, off = 1, None
     if offsets is not None:
         if not _is_vector(offsets, "int64") or offsets.shape[0] < 2:
@@ -536,12 +562,12 @@ def ifvs_norm_join(L, x, y=None, gate=None, w_post=None, w_pre=None, offsets=Non
     """x_out = res_scale x + gate * w_post * y / rms(y) and, with w_pre,
     n_out = w_pre * x_out / rms(x_out); gate [B][D] by the sequences that
     ``offsets`` delimits.  Without y only n_out, of x.  Returns (x_out, n_out)."""
-    at = _on(L, x, "x")
-    p, td, _, dt = _join_params(x, gate, w_post, w_pre, offsets, res_scale, eps, stream)
+    at = _on(L, x, "x", stream)
+    p, td, _, dt = _join_params(x, gate, w_post, w_pre, offsets, res_scale, eps, stream, at)
     if y is not None and x_out is None:
-        x_out = _like(x, *td)
+        x_out = _like(x, stream, *td)
     if w_pre is not None and n_out is None:
-        n_out = _like(x, *td)
+        n_out = _like(x, stream, *td)
     _check(_lib.ifvs_norm_join(L, C.byref(p), _dev(x, td, dt, "x", at), _dev(y, td, dt, "y", at),
                                _dev(x_out, td, dt, "x_out", at), _dev(n_out, td, dt, "n_out", at)))
     return x_out, n_out
@@ -553,16 +579,16 @@ def ifvs_norm_join_grad(L, x_out, y=None, gate=None, w_post=None, w_pre=None, d_
     """Gradients through ifvs_norm_join from those of x_out and n_out (either
     may be None).  Returns (dx, dy, d_gate, d_w_post, d_w_pre), None where the
     forward call had no such input."""
-    at = _on(L, x_out, "x_out")
-    p, td, bd, dt = _join_params(x_out, gate, w_post, w_pre, offsets, res_scale, eps, stream)
-    dx = _like(x_out, *td) if dx is None else dx
+    at = _on(L, x_out, "x_out", stream)
+    p, td, bd, dt = _join_params(x_out, gate, w_post, w_pre, offsets, res_scale, eps, stream, at)
+    dx = _like(x_out, stream, *td) if dx is None else dx
     if y is not None:
-        dy = _like(x_out, *td) if dy is None else dy
-        d_w_post = _like(x_out, td[1]) if d_w_post is None else d_w_post
+        dy = _like(x_out, stream, *td) if dy is None else dy
+        d_w_post = _like(x_out, stream, td[1]) if d_w_post is None else d_w_post
         if gate is not None and d_gate is None:
-            d_gate = _like(x_out, *bd)
+            d_gate = _like(x_out, stream, *bd)
     if d_n is not None and d_w_pre is None:
-        d_w_pre = _like(x_out, td[1])
+        d_w_pre = _like(x_out, stream, td[1])
     d = td[1:]
     _check(_lib.ifvs_norm_join_grad(
         L, C.byref(p), _dev(x_out, td, dt, "x_out", at), _dev(y, td, dt, "y", at),
@@ -572,8 +598,8 @@ def ifvs_norm_join_grad(L, x_out, y=None, gate=None, w_post=None, w_pre=None, d_
     return dx, dy, d_gate, d_w_post, d_w_pre
 
 
-def _ffn_params(x, w_in, w_out, act, stream):
-    (T, D), F, dt, at = x.shape, w_out.shape[1], x.dtype, x.get_device()
+def _ffn_params(x, w_in, w_out, act, stream, at=None):
+    (T, D), F, dt, at = x.shape, w_out.shape[1], x.dtype, x.get_device() if at is None else at
     if act not in _ACTS:
         raise ValueError("act must be one of %s" % sorted(_ACTS))
     p = FfnParams(T, D, F, _type(x), _ACTS[act], _dev(w_in, (2 * F, D), dt, "w_in", at),
@@ -583,20 +609,20 @@ def _ffn_params(x, w_in, w_out, act, stream):
 
 def ifvs_ffn(L, x, w_in, w_out, act="silu", y=None, stream=None):
     """y = (act(x Wg^T) * (x Wu^T)) w_out^T, w_in [2F][D] = [Wg; Wu], w_out [D][F]."""
-    at = _on(L, x, "x")
-    p, td, _, dt = _ffn_params(x, w_in, w_out, act, stream)
-    y = _like(x, *td) if y is None else y
+    at = _on(L, x, "x", stream)
+    p, td, _, dt = _ffn_params(x, w_in, w_out, act, stream, at)
+    y = _like(x, stream, *td) if y is None else y
     _check(_lib.ifvs_ffn(L, C.byref(p), _dev(x, td, dt, "x", at), _dev(y, td, dt, "y", at)))
     return y
 
 
 def ifvs_ffn_grad(L, x, w_in, w_out, dy, act="silu", dx=None, d_w_in=None, d_w_out=None, stream=None):
     """Gradients (dx, d_w_in, d_w_out) through ifvs_ffn from dy."""
-    at = _on(L, x, "x")
-    p, td, F, dt = _ffn_params(x, w_in, w_out, act, stream)
-    dx = _like(x, *td) if dx is None else dx
-    d_w_in = _like(x, 2 * F, td[1]) if d_w_in is None else d_w_in
-    d_w_out = _like(x, td[1], F) if d_w_out is None else d_w_out
+    at = _on(L, x, "x", stream)
+    p, td, F, dt = _ffn_params(x, w_in, w_out, act, stream, at)
+    dx = _like(x, stream, *td) if dx is None else dx
+    d_w_in = _like(x, stream, 2 * F, td[1]) if d_w_in is None else d_w_in
+    d_w_out = _like(x, stream, td[1], F) if d_w_out is None else d_w_out
     _check(_lib.ifvs_ffn_grad(L, C.byref(p), _dev(x, td, dt, "x", at), _dev(dy, td, dt, "dy", at),
                               _dev(dx, td, dt, "dx", at), _dev(d_w_in, (2 * F, td[1]), dt, "d_w_in", at),
                               _dev(d_w_out, (td[1], F), dt, "d_w_out", at)))
@@ -718,7 +744,9 @@ class Index:
 
 class Layers:
     """Owns an ifvs_layers handle: the layers of a predicate encoder on one
-    device (freed on close / garbage collection)."""
+    device (freed on close / garbage collection).  With ``stream`` a call is
+    enqueued there (inputs ready in its order and kept until its work is done);
+    without, it follows torch's current stream and waits for its outputs."""
 
     def __init__(self, device=0):
         self.h = ifvs_layers_create(device)
