@@ -101,3 +101,87 @@ def test_norm_join_rows_of_zeros_with_a_small_eps(layers, type_, eps):
     kw = dict(offsets=off, res_scale=0.7, eps=eps)
     _check(layers.norm_join(*a, **kw), ref.norm_join(*a, off, 0.7, eps))
     _check(layers.norm_join_grad(*a, dxo, dn, **kw), ref.norm_join_grad(*a, dxo, dn, off, 0.7, eps))
+
+
+# ---- the steady state: sizes at which every team, warp and CTA has work for many
+# rounds of its ring, by the launch rules (asserted here for the device at hand)
+
+def _sms():
+    return torch.cuda.get_device_properties(0).multi_processor_count
+
+
+def _places(T, D, type_, teams):
+    """Places of its ring that a team fills."""
+    row = D * TYPES[type_].itemsize
+    per = 1 if row >= 1024 else (8 if row <= 128 else 1024 // row)
+    return -(-T // teams) // per
+
+
+def _cuts(T, B, seed):
+    """Offsets of B sequences: empty ones, single tokens, one of a third of all tokens."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    cuts = torch.randint(T // 3, T + 1, (B + 1,), generator=g, device="cuda").sort().values
+    cuts[1:7] = torch.tensor([0, 1, 2, 2, T // 3 - 1, T // 3], device="cuda")
+    cuts[0], cuts[B] = 0, T
+    return cuts
+
+
+@pytest.mark.parametrize("type_", sorted(TYPES))
+@pytest.mark.parametrize("T,D", [(160_003, 40), (140_001, 97), (60_001, 320), (40_003, 1030), (9_001, 5001)])
+def test_norm_join_in_its_steady_state(layers, type_, T, D):
+    warps = 1
+    while warps * (512 if D <= 4096 else 1024) < D:
+        warps *= 2
+    assert _places(T, D, type_, 3 * 8 // warps * _sms()) >= 4
+    r, dt, off = _rand(D), TYPES[type_], _cuts(T, 1500, D)
+    x, y, dxo, dn = ((s * r(T, D)).to(dt) for s in (1.5, 0.5, 1.0, 1.0))
+    a = (x, y, (1 + 0.3 * r(1500, D)).to(dt), (1 + 0.1 * r(D)).to(dt), (1 + 0.1 * r(D)).to(dt))
+    kw = dict(offsets=off, res_scale=0.7, eps=EPS)
+    _check(layers.norm_join(*a, **kw), ref.norm_join(*a, off, 0.7, EPS))
+    _check(layers.norm_join_grad(*a, dxo, dn, **kw), ref.norm_join_grad(*a, dxo, dn, off, 0.7, EPS))
+
+
+@pytest.mark.parametrize("T,D,V,type_", [(400_003, 40, 3_000, "bf16"), (700_001, 64, 50_000, "f32"), (400_003, 520, 9_000, "bf16"),
+                                         (700_001, 33, 500, "f16"), (300_007, 260, 2, "f32"), (400_003, 300, 70_000, "f16")])
+def test_embed_grad_in_its_steady_state(layers, T, D, V, type_):
+    """Parts of more than 32 tokens of the sorted order, aligned rows and others."""
+    assert T // 64 >= 16 * _sms()
+    g = torch.Generator(device="cuda")
+    g.manual_seed(T + D)
+    ids = torch.randint(0, V, (T,), generator=g, device="cuda")
+    ids = torch.where(torch.rand(T, generator=g, device="cuda") < 0.5, ids % min(V, 12), ids)
+    ids[torch.rand(T, generator=g, device="cuda") < 0.03] = -1
+    ids = ids.int()
+    d_out = _rand(D)(T, D).to(TYPES[type_])
+    ref.within(layers.embed_grad(d_out, ids, 1.5, V=V), *ref.embed_grad(d_out, ids, 1.5, V))
+
+
+def _pairs(rows, cols, K):
+    return -(-rows // 256) * -(-cols // 256) >= _sms() // (4 if K >= 1024 else 2)
+
+
+# tokens, width, hidden width, whether the output product and the gradient's products
+# go to pairs of CTAs on the measured device; several tiles of both operands each
+@pytest.mark.parametrize("T,D,F,out,grad", [(5_003, 520, 1032, True, True), (9_001, 264, 776, False, True),
+                                            (10_001, 264, 776, True, True), (1_100, 776, 1288, False, True),
+                                            (300, 520, 1032, False, False), (2_500, 1544, 2056, True, True)])
+@pytest.mark.parametrize("act,type_", [("silu", "bf16"), ("gelu", "f16")])
+def test_ffn_of_several_tiles(layers, T, D, F, out, grad, act, type_):
+    if _sms() == 152:
+        assert _pairs(T, D, F) == out
+        assert (T > 512 and (_pairs(T, D, 2 * F) or _pairs(2 * F, D, T))) == grad
+    r, dt = _rand(T + D), TYPES[type_]
+    x, dy = r(T, D).to(dt), r(T, D).to(dt)
+    w_in, w_out = (r(2 * F, D) / D ** 0.5).to(dt), (r(D, F) / F ** 0.5).to(dt)
+    ref.within(layers.ffn(x, w_in, w_out, act=act), *ref.ffn(x, w_in, w_out, act))
+    _check(layers.ffn_grad(x, w_in, w_out, dy, act=act), ref.ffn_grad(x, w_in, w_out, dy, act))
+
+
+@pytest.mark.parametrize("T,D,F", [(3, 8192, 72), (130, 8192, 64), (3, 64, 65536), (130, 64, 65536), (1, 8192, 8192), (130, 8192, 8192)])
+def test_ffn_of_the_largest_widths(layers, T, D, F):
+    r, dt = _rand(T + D), torch.bfloat16
+    x, dy = r(T, D).to(dt), r(T, D).to(dt)
+    w_in, w_out = (r(2 * F, D) / D ** 0.5).to(dt), (r(D, F) / F ** 0.5).to(dt)
+    ref.within(layers.ffn(x, w_in, w_out), *ref.ffn(x, w_in, w_out, "silu"))
+    _check(layers.ffn_grad(x, w_in, w_out, dy), ref.ffn_grad(x, w_in, w_out, dy, "silu"))
