@@ -457,8 +457,10 @@ int ifvs_get_conditioning(ifvs_index* ix, float* bank, float* W, uint32_t flags)
  * Arrays are row-major device memory on the handle's device, contiguous, all
  * of one element type per call; index arrays say their own.  Sums, norms and
  * statistics are float32; every output is rounded once.  Sums run in a fixed
- * order: equal calls give equal bits.  Outputs must not overlap inputs or
- * each other.
+ * order, which depends on the arguments, on whether the arrays begin on 16 bytes
+ * (8 and 4 for the norms), and on the number of SMs, never on timing: equal
+ * calls on equally aligned arrays give equal bits on one model of device.
+ * Outputs must not overlap inputs or each other.
  *
  * A handle holds the workspace, the order of the calls that use it, and a
  * word per error.  With a non-NULL stream a call only enqueues its work there
@@ -514,8 +516,10 @@ int ifvs_embed(ifvs_layers* L, const void* table, int64_t V, int32_t D, int32_t 
 
 /*
  * ifvs_embed_grad — d_table[v] = scale sum over the tokens t with ids[t] = v
- * of d_out[t]; zeros for ids that no token has.  The tokens are sorted by id
- * and each id's rows summed in an order that depends on T alone.
+ * of d_out[t]; zeros for ids that no token has.  The tokens are sorted by id,
+ * those of one id stay in their order, and the sorted rows are summed in parts of
+ * equal length whose length depends on T, D, the type, the alignment and the
+ * number of SMs; where an id's rows are cut depends on the ids before it.
  *   d_out [T][D], d_table [V][D] of `type`; T < 2^31.  Padding adds nothing;
  * other ids outside 0..V-1 add nothing and are reported.  Errors as
  * ifvs_embed, plus IFVS_ERR_OOM.

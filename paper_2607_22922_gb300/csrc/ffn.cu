@@ -7,7 +7,11 @@
 // k_hidden makes h with both projections in one accumulator tile (128 tokens x
 // FT gate columns and the same FT up columns), k_hidden_grad makes h, dg and du
 // from x and dy with three (g, u and dh all sum over D), so that nothing of the
-// hidden layer is kept from the forward call.  k_products makes the other
+// hidden layer is kept from the forward call.  h, dg and du are rounded to the
+// arrays' type between the products, because the tensor cores multiply 16-bit
+// operands (and k_few keeps to it): against float64 y and the gradients are off by
+// 0.0022 to 0.0024 of their norm in bfloat16, where rounding the outputs alone
+// takes 0.0017 (float16 0.0003 and 0.0002).  k_products makes the other
 // products, those of the gradient in one launch.  All are persistent: a CTA, or
 // a pair of CTAs that share one MMA of 256 rows, takes tiles; a warp fills a
 // ring of operand stages by TMA, a warp issues the MMAs, the others turn
@@ -186,8 +190,8 @@ constexpr size_t smem_of(uint32_t stage_bytes, uint32_t out_bytes) {
 
 // ---- products C = A B^T in 16 bits ---------------------------------------------------
 // Bound by the tensor pipe and, in a long run, by power: the gradient's three
-// products at 16411 x 1024 x 4096 (687 GFLOP) 380 us, 1.81 PFLOP/s, the pipe 96.5 %
-// active at 1.64 GHz.
+// products at 16411 x 1024 x 4096 (688 GFLOP) 372 us, 1.85 PFLOP/s, the pipe 96.4 %
+// active at 1.69 GHz.
 // A K-major [rows][K] or MN-major [K][rows]; B the same with `cols`.  Up to three
 // products in one launch, items (tiles, or parts of a tile's sum) in their order.
 struct Product {
@@ -357,8 +361,8 @@ __global__ void __launch_bounds__(256) k_join_parts(Parts p) {
 }
 
 // ---- h = act(x Wg^T) * (x Wu^T) ------------------------------------------------------
-// Bound by the tensor pipe: 17408 x 960 x 2560 (171 GFLOP) 90 us, 1.90 PFLOP/s, the
-// pipe 89 % active.
+// Bound by the tensor pipe: 17408 x 960 x 2560 (171 GFLOP) 92 us, 1.86 PFLOP/s, the
+// pipe 87 % active.
 // FT hidden columns per tile: gate rows and up rows of W_in side by side in B.  In
 // a pair the first CTA holds the gate's rows, the second the up projection's.
 template <int CG, int FT>
@@ -473,10 +477,11 @@ k_hidden(const __grid_constant__ CUtensorMap mx, const __grid_constant__ CUtenso
 // ---- h, dg, du from x and dy ---------------------------------------------------------
 // Per tile first dh = dy Wo (FT columns), then g and u (2 FT).  TMEM: g | u in
 // columns FT .. 3 FT - 1; dh in the first FT or from 3 FT by turns, so that the
-// next tile's dh accumulates while this tile's values are read.  Bound by shared
-// memory: per 64 of the sum 56 KB come in by TMA and are read by the MMAs, 112 KB
-// in the 768 clocks that the MMAs take, at 128 bytes a clock.  16411 x 1024 x 4096
-// (413 GFLOP) 267 us, 1.55 PFLOP/s, the tensor pipe 68 % active.
+// next tile's dh accumulates while this tile's values are read.  16411 x 1024 x 4096
+// (413 GFLOP) 267 us, 1.55 PFLOP/s, the tensor pipe 68 % active.  Shared memory
+// allows 86 %: per 64 of the sum 56 KB come in by TMA and are read by the MMAs, 112
+// KB or 896 clocks at 128 bytes each, against 768 clocks of MMAs.  What holds the
+// rest has not been measured; g | u are read before the next tile's may begin.
 template <int CG, int FT>
 struct GradShape {
     static constexpr int kEpi = FT / 16;
@@ -494,7 +499,7 @@ k_hidden_grad(const __grid_constant__ CUtensorMap mx, const __grid_constant__ CU
               const __grid_constant__ CUtensorMap mdu, Grid g, bool f16, Waits waits) {
     using Sh = GradShape<CG, FT>;
     constexpr int EPI = Sh::kEpi, S = Sh::kStages;
-    __shared__ __align__(8) Bars<S> bars;     // slot 0: g | u, slot 1: dh (both places)
+    __shared__ __align__(8) Bars<S> bars;     // of the accumulators' barriers the first pair alone
     const uint32_t ring = dynamic_smem(), out = ring + S * Sh::kStage;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int rank = CG == 2 ? (int)cluster_rank() : 0;
@@ -540,7 +545,6 @@ k_hidden_grad(const __grid_constant__ CUtensorMap mx, const __grid_constant__ CU
                 // dh's place was read two tiles ago, before the g | u of the last tile
                 for (int k = 0; k < 2 * g.k_steps; ++k, r.next()) {
                     if (k == g.k_steps) {
-                        mma_commit<CG>(smem_addr(&bars.acc_full[1]));
                         if (!(ok = w.wait(smem_addr(&bars.acc_empty[0]), parity ^ 1u))) break;
                         fence_after_sync();
                     }
@@ -610,9 +614,12 @@ k_hidden_grad(const __grid_constant__ CUtensorMap mx, const __grid_constant__ CU
 
 // ---- a few tokens ----------------------------------------------------------------------
 // Up to kFewTokens tokens: the weights are read once and bound the call, and a
-// tile of 128 tokens would leave most SMs without one (960 x 2560, here against
-// the tensor cores: 1 token 7.9 us against 14.9, 4 tokens 9.1 against 15.1, 8
-// tokens 17.5 against 14.5).  A row of weights (PAIR:
+// tile of 128 tokens would leave most SMs without one.  Both kernels' GPU time,
+// weights from memory, here against the tensor cores: 960 x 2560 1 token 8.0 us
+// against 15.4, 2 tokens 8.7 against 15.0, 4 tokens 9.4 against 15.1; 128 x 344 3.6,
+// 4.0 and 4.3 against 8.7.  Compiled for 8 tokens, 5 to 8 take 20 us against 15.3
+// at 960 x 2560 and 7.4 against 8.7 at 128 x 344 (for 16: 35 and 9).  A row of
+// weights (PAIR:
 // the gate's row and the up projection's) is spread over the lanes of one or
 // more warps, 16 bytes a lane and access, against every token's row.
 constexpr int kFewTokens = 4;

@@ -20,7 +20,10 @@
 // gradient written at once; one that reaches beyond them leaves float32 partial
 // sums that k_join_finish adds in order, as it does with the norms' weights.  No
 // result depends on timing.  Measured: 163847 tokens x 960 of bfloat16 227 us,
-// 5.6 TB/s; the gradient of 131101 x 1024 292 us, 5.5 TB/s.
+// 5.6 TB/s; the gradient of 131101 x 1024 289 us, 5.6 TB/s.  Rows that do not begin
+// on 16 bytes go by 8, 4 or 2: 100003 x 960, 964, 962 and 961 of bfloat16 141, 168,
+// 237 and 463 us (more accesses a row; of two elements and of one, with spilled
+// registers), the gradient of 100003 x 1024 and 1023 242 and 713.
 #include "layers.cuh"
 #include "places.h"
 #include "scan_common.cuh"
@@ -276,8 +279,10 @@ __device__ __forceinline__ void init_bars(uint64_t* bars, int teams) {
 }
 
 constexpr int kJoinThreads = 256;
-// columns a warp holds at most.  163847 tokens x 960, bfloat16: 226 us with 512 and
-// three CTAs an SM, 235 with 1024 and two.
+// Columns a warp holds at most: 512 and three CTAs an SM, 1024 and two where 512 a
+// warp need more warps than a CTA has.  512 against 1024, 100003 tokens of bfloat16:
+// 960 columns 141 us and 144, 964 168 and 163, 962 237 and 281, 961 463 and 511;
+// 50003 of float32: 960 133 and 146, 961 248 and 478.
 constexpr int join_columns(int D) { return D <= kJoinThreads / 32 * 512 ? 512 : 1024; }
 constexpr int join_ctas(int columns) { return columns > 512 ? 2 : 3; }       // per SM, by registers
 
