@@ -47,34 +47,29 @@ def listed():
         dict(kind="linear", name="linear-batch", t=17_408, d_in=960, d_out=2560, act="gelu", bias=True,
              residual=True, type="bf16"),
         # a training batch of a narrow encoder
-        dict(kind="linear_grad", name="linear_grad-narrow", t=2_051, d_in=128, d_out=344, act="silu", bias=True, type="f16"),
+        dict(kind="linear_grad", name="linear_grad-narrow", t=2_051, d_in=128, d_out=344, act="silu", bias=True,
+             type="f16"),
         # a training batch of a wide encoder: the largest case
         dict(kind="linear_grad", name="linear_grad-wide", t=16_411, d_in=1024, d_out=4096, act="gelu", bias=True,
              type="bf16"),
         # serving: one query's token and the 17 tokens of its predicate
-        dict(kind="attend", name="attend-predicate", b=1, q_min=1, q_max=1, k_min=17, k_max=17, heads=4,
-             kv_heads=4, dh=32, ids=False, lse=False,
-             fused=False, type="bf16"),
+        dict(kind="attend", name="attend-predicate", b=1, q_min=1, q_max=1, k_min=17, k_max=17,
+             heads=4, kv_heads=4, dh=32, ids=False, lse=False, fused=False, type="bf16"),
         # training: 1024 queries of 120 subspace tokens, predicates of 0 to 65 tokens, padding among them
-        dict(kind="attend", name="attend-batch", b=1024, q_min=120, q_max=120, k_min=0, k_max=65, heads=8,
-             kv_heads=2, dh=64, ids=True, lse=True,
-             fused=True, type="bf16"),
+        dict(kind="attend", name="attend-batch", b=1024, q_min=120, q_max=120, k_min=0, k_max=65,
+             heads=8, kv_heads=2, dh=64, ids=True, lse=True, fused=True, type="bf16"),
         # serving: one token for each of 8 workloads that took about 16 000 tokens to describe
-        dict(kind="attend", name="attend-states", b=8, q_min=1, q_max=1, k_min=16_001, k_max=16_801, heads=8,
-             kv_heads=8, dh=64, ids=False,
-             lse=False, fused=False, type="f16"),
+        dict(kind="attend", name="attend-states", b=8, q_min=1, q_max=1, k_min=16_001, k_max=16_801,
+             heads=8, kv_heads=8, dh=64, ids=False, lse=False, fused=False, type="f16"),
         # every token of a batch attends to the tokens of 1024 predicates
-        dict(kind="attend", name="attend-workload", b=1, q_min=4_099, q_max=4_099, k_min=17_403,
-             k_max=17_403, heads=8, kv_heads=8, dh=128,
-             ids=False, lse=False, fused=False, type="bf16"),
+        dict(kind="attend", name="attend-workload", b=1, q_min=4_099, q_max=4_099, k_min=17_403, k_max=17_403,
+             heads=8, kv_heads=8, dh=128, ids=False, lse=False, fused=False, type="bf16"),
         # training as above, with 64 subspace tokens
         dict(kind="attend_grad", name="attend_grad-batch", b=1000, q_min=60, q_max=68, k_min=1, k_max=65,
-             heads=8, kv_heads=2, dh=64, ids=True,
-             lse=True, fused=True, type="f16"),
+             heads=8, kv_heads=2, dh=64, ids=True, lse=True, fused=True, type="f16"),
         # four workloads, long on both sides
-        dict(kind="attend_grad", name="attend_grad-workload", b=4, q_min=1_301, q_max=1_701, k_min=3_500,
-             k_max=5_003, heads=8, kv_heads=8, dh=64,
-             ids=False, lse=True, fused=False, type="bf16"),
+        dict(kind="attend_grad", name="attend_grad-workload", b=4, q_min=1_301, q_max=1_701, k_min=3_500, k_max=5_003,
+             heads=8, kv_heads=8, dh=64, ids=False, lse=True, fused=False, type="bf16"),
         # the joined tokens of a small training batch
         dict(kind="dropout", name="dropout-batch", t=17_393, d=100, p=0.1, residual=True, type="f32"),
         # the gradient over the tokens of 10^4 queries
