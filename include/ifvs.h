@@ -452,7 +452,8 @@ int ifvs_get_conditioning(ifvs_index* ix, float* bank, float* W, uint32_t flags)
  * takes the vectors that such an encoder makes and ifvs_train_grad returns
  * dL/dw_z for it.  The calls below are the operators to build one from, each
  * with its gradient: embedding lookup, norms around a block joined with its
- * gate and residual, gated feed-forward block.
+ * gate and residual, gated feed-forward block, linear layer, cross attention,
+ * dropout.
  *
  * Arrays are row-major device memory on the handle's device, contiguous, all
  * of one element type per call; index arrays say their own.  Sums, norms and
@@ -484,12 +485,15 @@ typedef struct ifvs_layers ifvs_layers;
 
 /* Element types. */
 enum { IFVS_T_F32 = 0, IFVS_T_F16 = 1, IFVS_T_BF16 = 2 };
-/* Activations of the gated feed-forward block: x sigmoid(x), x Phi(x) with
- * the normal distribution function Phi, max(x, 0). */
-enum { IFVS_ACT_SILU = 0, IFVS_ACT_GELU = 1, IFVS_ACT_RELU = 2 };
+/* Activations of the gated feed-forward block and the linear layer: x sigmoid(x), x Phi(x) with
+ * the normal distribution function Phi, max(x, 0); of the linear layer also
+ * none: x. */
+enum { IFVS_ACT_SILU = 0, IFVS_ACT_GELU = 1, IFVS_ACT_RELU = 2, IFVS_ACT_NONE = 3 };
 
 #define IFVS_MAX_WIDTH 8192      /* largest row width D of the layers          */
-#define IFVS_MAX_HIDDEN 65536    /* largest hidden width F of ifvs_ffn         */
+#define IFVS_MAX_HIDDEN 65536    /* largest hidden width F of ifvs_ffn, largest
+                                    widths of ifvs_linear                      */
+#define IFVS_MAX_ELEMENTS (1ll << 40)   /* largest n of ifvs_dropout           */
 
 /* ifvs_layers_create — a handle on `device` (free with ifvs_layers_free,
  * which waits for the device). */
@@ -610,6 +614,54 @@ int ifvs_ffn(ifvs_layers* L, const ifvs_ffn_params* p, const void* x, void* y);
  */
 int ifvs_ffn_grad(ifvs_layers* L, const ifvs_ffn_params* p, const void* x, const void* dy, void* dx,
                   void* d_w_in, void* d_w_out);
+
+typedef struct {
+    int64_t T;          /* tokens, 0 <= T < 2^31                              */
+    int32_t D_in;       /* widths, multiples of 8, 8..IFVS_MAX_HIDDEN         */
+    int32_t D_out;
+    int32_t type;       /* IFVS_T_F16 or IFVS_T_BF16                          */
+    int32_t act;        /* IFVS_ACT_*                                         */
+    const void* w;      /* [D_out][D_in]                                      */
+    const void* bias;   /* [D_out], or NULL: none                             */
+    void* stream;
+} ifvs_linear_params;
+
+/*
+ * ifvs_linear — y = act(x w^T + bias) + residual, in one product with the rest in its
+ * epilogue.
+ *   x [T][D_in]; y [T][D_out]; residual [T][D_out], or NULL: none.  Arrays must be
+ *   aligned to 16 bytes.
+ * Nothing is rounded before y.  Errors: IFVS_ERR_ARG, IFVS_ERR_UNSUPPORTED
+ * (IFVS_T_F32; a width that is not a multiple of 8), IFVS_ERR_OOM.
+ */
+int ifvs_linear(ifvs_layers* L, const ifvs_linear_params* p, const void* x, const void* residual, void* y);
+
+/*
+ * ifvs_linear_grad — gradients of a loss through ifvs_linear from dL/dy (which is the
+ * residual's own); x w^T + bias is computed again, nothing is kept between the calls.
+ *   dy [T][D_out]; dx [T][D_in]; d_w [D_out][D_in]; d_bias [D_out], NULL iff bias is
+ * dz = dy act'(x w^T + bias) is rounded to `type` before it is summed over the tokens or
+ * over D_out (without an activation it is dy).  T = 0 writes zeros to d_w and d_bias.
+ * Errors as ifvs_linear.
+ */
+int ifvs_linear_grad(ifvs_layers* L, const ifvs_linear_params* p, const void* x, const void* dy, void* dx,
+                     void* d_w, void* d_bias);
+
+/*
+ * ifvs_dropout — out[i] = residual[i] + (word_i >= p 2^32 ? x[i] / (1 - p) : 0), i < n.
+ *   x, residual (or NULL: zeros), out: n elements of `type`, 0 <= n <= IFVS_MAX_ELEMENTS
+ *   p       0 <= p < 1; p 2^32 is rounded to a whole number, at most 2^32 - 1
+ *   word_i  word i mod 4 of Philox4x32-10 with counter (i / 4, step + *more_steps), 64
+ *           bits each, and key `seed`
+ *   more_steps  one int64 in device memory, read when the call runs (so that the replays
+ *           of a captured graph can differ), or NULL: 0
+ * The mask is stored nowhere: the gradient of x is the same call (same p, seed and steps,
+ * no residual) on the gradient of out.  Calls need a seed or step of their own to be
+ * independent.  A dropped x may be anything, NaN included.  Uses no workspace.  Errors:
+ * IFVS_ERR_ARG (n, p, unknown type, an array not aligned to its elements).
+ */
+int ifvs_dropout(ifvs_layers* L, const void* x, const void* residual, int64_t n, int32_t type, double p,
+                 uint64_t seed, uint64_t step, const int64_t* more_steps, void* out, void* stream);
 
 /*
  * ifvs_stage_times — device time (ms, from CUDA events recorded on the

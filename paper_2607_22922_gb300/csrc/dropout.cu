@@ -1,0 +1,90 @@
+// Dropout whose mask is never stored (ifvs_dropout): element i keeps its value iff the
+// random word i of (seed, step) is at least p 2^32, so that the backward pass, the
+// same call on the gradient, finds the same elements.
+#include "layers.cuh"
+#include "philox.h"
+
+namespace ifvs {
+
+namespace {
+
+struct DropArgs {
+    const void *x, *residual;
+    void* out;
+    int64_t n;
+    uint64_t seed, step;
+    const int64_t* more_steps;
+    uint32_t below;      // words below it drop their element
+    float scale;
+};
+
+// A thread takes CH chunks of 16 bytes of x, a grid's width apart.  WIDE: all arrays
+// begin on 16 bytes; else elements come one by one.
+template <class T, bool RES, bool WIDE, int CH>
+__global__ void __launch_bounds__(256) k_dropout(DropArgs a) {
+    constexpr int E = 16 / (int)sizeof(T);
+    using P = Pack<T, E>;
+    const T *x = (const T*)a.x, *res = (const T*)a.residual;
+    T* out = (T*)a.out;
+    const int64_t first = ((int64_t)blockIdx.x * CH * 256 + threadIdx.x) * E;
+    P v[CH], r[CH];
+    auto at = [&](int c) { return first + (int64_t)c * 256 * E; };
+    if constexpr (WIDE) {
+#pragma unroll
+        for (int c = 0; c < CH; ++c)
+            if (at(c) + E <= a.n) {
+                v[c].load(x + at(c));
+                if constexpr (RES) r[c].load(res + at(c));
+            }
+    }
+    const uint64_t step = a.step + (a.more_steps ? (uint64_t)__ldg(a.more_steps) : 0u);
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+        const int64_t i = at(c);
+        if (i >= a.n) return;
+        uint32_t w[E];
+#pragma unroll
+        for (int j = 0; j < E; j += 4) {
+            const Words q = philox((uint64_t)(i + j) / 4, step, a.seed);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) w[j + k] = q.w[k];
+        }
+        // one rounding; what is dropped may be anything
+        auto one = [&](float value, float base, uint32_t word) {
+            return word < a.below ? base : (RES ? fmaf(value, a.scale, base) : value * a.scale);
+        };
+        if (WIDE && i + E <= a.n) {
+#pragma unroll
+            for (int j = 0; j < E / 2; ++j) {
+                const float2 p = v[c].get(j), q = RES ? r[c].get(j) : make_float2(0.f, 0.f);
+                v[c].set(j, make_float2(one(p.x, q.x, w[2 * j]), one(p.y, q.y, w[2 * j + 1])));
+            }
+            v[c].store(out + i);
+        } else {
+#pragma unroll
+            for (int j = 0; j < E; ++j)
+                if (i + j < a.n) out[i + j] = from_f32<T>(one(to_f32(x[i + j]), RES ? to_f32(res[i + j]) : 0.f, w[j]));
+        }
+    }
+}
+
+bool wide(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+
+}  // namespace
+
+cudaError_t launch_dropout(const void* x, const void* residual, int64_t n, int type, uint32_t below, float scale, uint64_t seed,
+                           uint64_t step, const int64_t* more_steps, void* out, cudaStream_t s) {
+    const DropArgs a{x, residual, out, n, seed, step, more_steps, below, scale};
+    return with_type(type, [&](auto t) {
+        using T = decltype(t);
+        constexpr int CH = 2;
+        constexpr int64_t kPer = 256 * CH * (16 / (int64_t)sizeof(T));
+        const dim3 grid((unsigned)((n + kPer - 1) / kPer));
+        const bool w = wide(x) && wide(out) && wide(residual);
+        auto go = [&](auto res, auto wd) { return launch_next(k_dropout<T, res(), wd(), CH>, grid, dim3(256), 0, false, s, a); };
+        if (residual) return w ? go(std::true_type(), std::true_type()) : go(std::true_type(), std::false_type());
+        return w ? go(std::false_type(), std::true_type()) : go(std::false_type(), std::false_type());
+    });
+}
+
+}  // namespace ifvs

@@ -212,6 +212,23 @@ int ffn_check(const ifvs_layers* L, const ifvs_ffn_params* p, FfnArgs* a) {
     return 0;
 }
 
+int linear_check(const ifvs_layers* L, const ifvs_linear_params* p, LinearArgs* a) {
+    if (!L || !p) return report_error(IFVS_ERR_ARG, "the handle or params is NULL");
+    TRY(check_type(p->type));
+    TRY(check_tokens(p->T));
+    for (const int d : {p->D_in, p->D_out})
+        if (d < 1 || d > IFVS_MAX_HIDDEN) return report_error(IFVS_ERR_ARG, "a width of %d is outside 1..%d", d, IFVS_MAX_HIDDEN);
+    if (p->act != IFVS_ACT_NONE && p->act != IFVS_ACT_SILU && p->act != IFVS_ACT_GELU && p->act != IFVS_ACT_RELU)
+        return report_error(IFVS_ERR_ARG, "unknown activation %d", p->act);
+    if (p->type == IFVS_T_F32) return report_error(IFVS_ERR_UNSUPPORTED, "the linear layer takes 16-bit types only");
+    if (p->D_in % 8 || p->D_out % 8)
+        return report_error(IFVS_ERR_UNSUPPORTED, "D_in = %d and D_out = %d must be multiples of 8", p->D_in, p->D_out);
+    TRY(check_array(p->w, 16, "w"));
+    TRY(check_optional(p->bias, 16, "bias"));
+    *a = LinearArgs{p->T, p->D_in, p->D_out, p->type, p->act, p->w, p->bias, waits_of(L), L->num_sms};
+    return 0;
+}
+
 }  // namespace
 
 extern "C" {
@@ -365,6 +382,58 @@ int ifvs_ffn_grad(ifvs_layers* L, const ifvs_ffn_params* p, const void* x, const
     Call c(L, p->stream);
     TRY(c.begin(ffn_grad_bytes(a)));
     return c.end(launch_ffn_grad(a, x, dy, dx, d_w_in, d_w_out, L->work, c.s));
+}
+
+int ifvs_linear(ifvs_layers* L, const ifvs_linear_params* p, const void* x, const void* residual, void* y) {
+    LinearArgs a;
+    TRY(linear_check(L, p, &a));
+    if (a.T > 0) {
+        TRY(check_array(x, 16, "x"));
+        TRY(check_array(y, 16, "y"));
+    }
+    TRY(check_optional(residual, 16, "residual"));
+    Call c(L, p->stream);
+    TRY(c.begin(linear_bytes(a)));
+    return c.end(a.T > 0 ? launch_linear(a, x, residual, y, L->work, c.s) : cudaSuccess);
+}
+
+int ifvs_linear_grad(ifvs_layers* L, const ifvs_linear_params* p, const void* x, const void* dy, void* dx, void* d_w,
+                     void* d_bias) {
+    LinearArgs a;
+    TRY(linear_check(L, p, &a));
+    if (a.T > 0) {
+        TRY(check_array(x, 16, "x"));
+        TRY(check_array(dy, 16, "dy"));
+        TRY(check_array(dx, 16, "dx"));
+    }
+    TRY(check_array(d_w, 16, "d_w"));
+    if ((d_bias == nullptr) != (a.bias == nullptr)) return report_error(IFVS_ERR_ARG, "bias and d_bias go together");
+    TRY(check_optional(d_bias, 16, "d_bias"));
+    Call c(L, p->stream);
+    TRY(c.begin(linear_grad_bytes(a)));
+    return c.end(launch_linear_grad(a, x, dy, dx, d_w, d_bias, L->work, c.s));
+}
+
+int ifvs_dropout(ifvs_layers* L, const void* x, const void* residual, int64_t n, int32_t type, double p, uint64_t seed,
+                 uint64_t step, const int64_t* more_steps, void* out, void* stream) {
+    if (!L) return report_error(IFVS_ERR_ARG, "the handle is NULL");
+    TRY(check_type(type));
+    if (n < 0 || n > IFVS_MAX_ELEMENTS)
+        return report_error(IFVS_ERR_ARG, "n = %lld outside 0..2^40", (long long)n);
+    if (!(p >= 0.0 && p < 1.0)) return report_error(IFVS_ERR_ARG, "p = %g outside [0, 1)", p);
+    const size_t e = elem_bytes(type);
+    TRY(check_optional(residual, e, "residual"));
+    TRY(check_optional(more_steps, 8, "more_steps"));
+    if (n > 0) {
+        TRY(check_array(x, e, "x"));
+        TRY(check_array(out, e, "out"));
+    }
+    const double below = nearbyint(ldexp(p, 32));
+    Call c(L, stream);
+    TRY(c.begin(0));
+    return c.end(n > 0 ? launch_dropout(x, residual, n, type, below < 4294967295.0 ? (uint32_t)below : 0xFFFFFFFFu,
+                                        (float)(1.0 / (1.0 - p)), seed, step, more_steps, out, c.s)
+                       : cudaSuccess);
 }
 
 }  // extern "C"

@@ -210,6 +210,22 @@ size_t ffn_grad_bytes(const FfnArgs& a);
 cudaError_t launch_ffn_grad(const FfnArgs& a, const void* x, const void* dy, void* dx, void* d_w_in, void* d_w_out,
                             uint8_t* work, cudaStream_t s);
 
+struct LinearArgs {
+    int64_t T;
+    int D_in, D_out, type, act;
+    const void *w, *bias;        // bias: or null
+    Waits waits;
+    int num_sms;
+};
+size_t linear_bytes(const LinearArgs& a);
+cudaError_t launch_linear(const LinearArgs& a, const void* x, const void* residual, void* y, uint8_t* work, cudaStream_t s);
+size_t linear_grad_bytes(const LinearArgs& a);
+cudaError_t launch_linear_grad(const LinearArgs& a, const void* x, const void* dy, void* dx, void* d_w, void* d_bias,
+                               uint8_t* work, cudaStream_t s);
+
+cudaError_t launch_dropout(const void* x, const void* residual, int64_t n, int type, uint32_t below, float scale, uint64_t seed,
+                           uint64_t step, const int64_t* more_steps, void* out, cudaStream_t s);
+
 // Reports offsets that break their rules; the whole grid (x) calls it.
 __device__ __forceinline__ void check_offsets(const int64_t* __restrict__ offsets, int64_t B, int64_t T, int* err) {
     if (offsets == nullptr) return;

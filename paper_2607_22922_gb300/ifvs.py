@@ -24,7 +24,7 @@ IFVS_ATTR_I32, IFVS_ATTR_I16 = 0, 1
 IFVS_F_DEVICE_IO, IFVS_F_STAGE_TIMING, IFVS_F_PLAIN_PQ, IFVS_F_PLAIN_LOADS = 0x1, 0x2, 0x4, 0x8
 IFVS_MAX_K, IFVS_MAX_M, IFVS_MAX_ATTRS, IFVS_N_STAGES = 256, 128, 4, 9
 IFVS_T_F32, IFVS_T_F16, IFVS_T_BF16 = 0, 1, 2
-IFVS_ACT_SILU, IFVS_ACT_GELU, IFVS_ACT_RELU = 0, 1, 2
+IFVS_ACT_SILU, IFVS_ACT_GELU, IFVS_ACT_RELU, IFVS_ACT_NONE = 0, 1, 2, 3
 STAGES = ("predicate", "filter", "condition", "lut", "scan", "merge", "rerank", "layout", "train")
 
 # ifvs_predicate: 104 bytes (n_clauses, reserved, 4 x {col, op, lo, hi})
@@ -57,6 +57,11 @@ class FfnParams(C.Structure):
                 ("stream", C.c_void_p)]
 
 
+class LinearParams(C.Structure):
+    _fields_ = [("T", C.c_int64), ("D_in", C.c_int32), ("D_out", C.c_int32), ("type", C.c_int32),
+                ("act", C.c_int32), ("w", C.c_void_p), ("bias", C.c_void_p), ("stream", C.c_void_p)]
+
+
 class TrainParams(C.Structure):
     _fields_ = [("tau", C.c_float), ("lam", C.c_float), ("lr", C.c_float), ("lr_wz", C.c_float),
                 ("n_pos", C.c_int32), ("n_neg", C.c_int32), ("flags", C.c_uint32),
@@ -69,6 +74,7 @@ def _load():
                           "as g; g.build()\"` or `python -m paper_2607_22922_gb300.build`" % LIB_PATH)
     L = C.CDLL(LIB_PATH)
     P, I32, I64, U32, F32 = C.c_void_p, C.c_int32, C.c_int64, C.c_uint32, C.c_float
+    U64, F64 = C.c_uint64, C.c_double
     sig = {
         "ifvs_load_index": (C.c_int, [P, I32, P, I64, I32, I32, P, P, I32, P, I32, U32]),
         "ifvs_load_codebooks": (C.c_int, [P, P, I32, P, I64, I32, I32, P, P]),
@@ -93,6 +99,9 @@ def _load():
         "ifvs_norm_join_grad": (C.c_int, [P] * 11),
         "ifvs_ffn": (C.c_int, [P, P, P, P]),
         "ifvs_ffn_grad": (C.c_int, [P] * 7),
+        "ifvs_linear": (C.c_int, [P] * 5),
+        "ifvs_linear_grad": (C.c_int, [P] * 7),
+        "ifvs_dropout": (C.c_int, [P, P, P, I64, I32, F64, U64, U64, P, P, P]),
         "ifvs_stage_times": (C.c_int, [P, P, P, I32]),
         "ifvs_canonical_predicate": (C.c_int, [P, P, I32, P, P, P]),
         "ifvs_index_info": (C.c_int, [P, P]),
@@ -415,8 +424,10 @@ def ifvs_get_conditioning(ix, B, Mr, W_shape):
 # has been given so far, and has written its outputs when it returns.
 
 _ACTS = {"silu": IFVS_ACT_SILU, "gelu": IFVS_ACT_GELU, "relu": IFVS_ACT_RELU}
+_ANY_ACT = dict(_ACTS, none=IFVS_ACT_NONE)      # of the linear layer
 _TYPES = {}         # torch's element types -> IFVS_T_*, filled on first use
 _INTS = {}          # and its integer types -> their names
+_MASK64 = 2**64 - 1
 _LEGACY_STREAM = 1  # cudaStreamLegacy: the default stream as a non-NULL handle
 
 
@@ -629,6 +640,58 @@ def ifvs_ffn_grad(L, x, w_in, w_out, dy, act="silu", dx=None, d_w_in=None, d_w_o
     return dx, d_w_in, d_w_out
 
 
+def _linear_params(x, w, bias, act, stream, at):
+    (T, D_in), D_out, dt = x.shape, w.shape[0], x.dtype
+    if act not in _ANY_ACT:
+        raise ValueError("act must be one of %s" % sorted(_ANY_ACT))
+    p = LinearParams(T, D_in, D_out, _type(x), _ANY_ACT[act], _dev(w, (D_out, D_in), dt, "w", at),
+                     _dev(bias, (D_out,), dt, "bias", at), _stream(stream))
+    return p, (T, D_in), (T, D_out), dt
+
+
+def ifvs_linear(L, x, w, bias=None, act="none", residual=None, y=None, stream=None):
+    """y = act(x w^T + bias) + residual, w [D_out][D_in]."""
+    at = _on(L, x, "x", stream)
+    p, ti, to, dt = _linear_params(x, w, bias, act, stream, at)
+    y = _like(x, stream, *to) if y is None else y
+    _check(_lib.ifvs_linear(L, C.byref(p), _dev(x, ti, dt, "x", at), _dev(residual, to, dt, "residual", at),
+                            _dev(y, to, dt, "y", at)))
+    return y
+
+
+def ifvs_linear_grad(L, x, w, dy, bias=None, act="none", dx=None, d_w=None, d_bias=None, stream=None):
+    """Gradients (dx, d_w, d_bias) through ifvs_linear from dy, which is the
+    residual's own; d_bias None without a bias."""
+    at = _on(L, x, "x", stream)
+    p, ti, to, dt = _linear_params(x, w, bias, act, stream, at)
+    dx = _like(x, stream, *ti) if dx is None else dx
+    d_w = _like(x, stream, to[1], ti[1]) if d_w is None else d_w
+    if bias is not None and d_bias is None:
+        d_bias = _like(x, stream, to[1])
+    _check(_lib.ifvs_linear_grad(L, C.byref(p), _dev(x, ti, dt, "x", at), _dev(dy, to, dt, "dy", at),
+                                 _dev(dx, ti, dt, "dx", at), _dev(d_w, (to[1], ti[1]), dt, "d_w", at),
+                                 _dev(d_bias, to[1:], dt, "d_bias", at)))
+    return dx, d_w, d_bias
+
+
+def ifvs_dropout(L, x, p, seed, step=0, residual=None, out=None, stream=None):
+    """out = residual + (x / (1 - p) where its random word is at least p 2^32, else
+    0), for a tensor of any shape; the words are those of (seed, step).  Of a
+    gradient the same call without the residual.  step: a number, or a tensor of one
+    int64 on the device that is read when the call runs; seed and number mod 2^64."""
+    at = _on(L, x, "x", stream)
+    more = None
+    if not isinstance(step, int):
+        if not _is_vector(step, "int64"):
+            raise ValueError("step must be an int or a vector of one int64")
+        more, step = _dev(step, (1,), step.dtype, "step", at), 0
+    out = _like(x, stream, *x.shape) if out is None else out
+    _check(_lib.ifvs_dropout(L, _dev(x, x.shape, x.dtype, "x", at), _dev(residual, x.shape, x.dtype, "residual", at),
+                             x.numel(), _type(x), p, seed & _MASK64, step & _MASK64, more,
+                             _dev(out, x.shape, x.dtype, "out", at), _stream(stream)))
+    return out
+
+
 def ifvs_rerank(ix, queries, cand, k, flags=0):
     queries = _host(queries, np.float32)
     cand = _host(cand, np.int64)
@@ -757,6 +820,9 @@ class Layers:
         self.norm_join_grad = functools.partial(ifvs_norm_join_grad, self.h)
         self.ffn = functools.partial(ifvs_ffn, self.h)
         self.ffn_grad = functools.partial(ifvs_ffn_grad, self.h)
+        self.linear = functools.partial(ifvs_linear, self.h)
+        self.linear_grad = functools.partial(ifvs_linear_grad, self.h)
+        self.dropout = functools.partial(ifvs_dropout, self.h)
 
     def status(self):
         """Waits for the enqueued calls; raises what their kernels found."""
