@@ -647,6 +647,58 @@ int ifvs_linear(ifvs_layers* L, const ifvs_linear_params* p, const void* x, cons
 int ifvs_linear_grad(ifvs_layers* L, const ifvs_linear_params* p, const void* x, const void* dy, void* dx,
                      void* d_w, void* d_bias);
 
+#define IFVS_MAX_HEAD 128        /* largest head dimension of ifvs_attend       */
+
+/* What ifvs_attend and its gradient share.  Rows of q and of what has its shape are
+ * tokens: `heads` times dh elements, head h in elements h dh .. h dh + dh - 1; rows of
+ * k and v the same with kv_heads.  ld_*: elements from one row to the next, a
+ * multiple of 8, at least a row's; 0: rows without gaps.  (So that k and v can be halves
+ * of one projection's output, and their gradients halves of its gradient.) */
+typedef struct {
+    int64_t Tq, Tk;     /* queries and keys, 0 <= T < 2^31                    */
+    int32_t heads;      /* heads dh <= IFVS_MAX_WIDTH                         */
+    int32_t kv_heads;   /* divides heads: heads / kv_heads heads share one    */
+    int32_t dh;         /* head dimension, a multiple of 8, 8..IFVS_MAX_HEAD  */
+    int32_t type;       /* IFVS_T_F16 or IFVS_T_BF16                          */
+    int64_t n_seq;      /* sequences B >= 1, < 2^31                           */
+    const int64_t* q_offsets;  /* [B+1]: queries [q_offsets[b], q_offsets[b+1])
+                           attend to the keys of sequence b, which             */
+    const int64_t* kv_offsets; /* [B+1] delimits; both as in ifvs_join_params
+                           (NULL: B = 1, all tokens; equal: none)             */
+    const int32_t* kv_ids;     /* [Tk]: a key with a negative id is padding,
+                           which no query sees; NULL: no padding              */
+    float scale;        /* > 0, finite                                        */
+    int64_t ld_q, ld_k, ld_v, ld_out, ld_d_out, ld_dq, ld_dk, ld_dv;
+    void* stream;
+} ifvs_attend_params;
+
+/*
+ * ifvs_attend — attention of queries to the keys of their sequence:
+ *   p = softmax over the keys of scale q k, out = sum of p v
+ *   q, out [Tq][heads][dh]; k, v [Tk][kv_heads][dh]
+ *   lse    [Tq][heads] float32 out, or NULL: log of the sum over the keys of
+ *          exp(scale q k), which the gradient takes
+ * A query without keys (an empty sequence, or padding alone) has out = 0 and
+ * lse = -infinity.  Keys and values of padding may be anything, NaN included.  Arrays
+ * of `type` must be aligned to 16 bytes.  exp(scale q k - running maximum) is rounded to
+ * `type` before its product with v (in IFVS_T_F16 what is below 2^-25 vanishes).
+ * Errors: IFVS_ERR_ARG, IFVS_ERR_UNSUPPORTED (IFVS_T_F32; dh not a multiple of 8),
+ * IFVS_ERR_OOM; offsets that break their rules as for ifvs_norm_join.
+ */
+int ifvs_attend(ifvs_layers* L, const ifvs_attend_params* p, const void* q, const void* k, const void* v,
+                void* out, float* lse);
+
+/*
+ * ifvs_attend_grad — gradients of a loss through ifvs_attend from d_out.
+ *   out, lse   the forward call's; where all of a sequence's keys fit one tile they
+ *              are computed again instead
+ *   d_out, dq as q; dk, dv as k: for heads that share keys their sum
+ * Zeros for queries without keys, keys without queries and padding.  p and its gradient
+ * are rounded to `type` before the products that sum them.  Errors as ifvs_attend.
+ */
+int ifvs_attend_grad(ifvs_layers* L, const ifvs_attend_params* p, const void* q, const void* k, const void* v,
+                     const void* out, const float* lse, const void* d_out, void* dq, void* dk, void* dv);
+
 /*
  * ifvs_dropout — out[i] = residual[i] + (word_i >= p 2^32 ? x[i] / (1 - p) : 0), i < n.
  *   x, residual (or NULL: zeros), out: n elements of `type`, 0 <= n <= IFVS_MAX_ELEMENTS

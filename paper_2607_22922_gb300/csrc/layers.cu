@@ -7,6 +7,7 @@
 
 #include <new>
 
+#include "attend.cuh"
 #include "layers.cuh"
 #include "scan_common.cuh"
 
@@ -229,6 +230,49 @@ int linear_check(const ifvs_layers* L, const ifvs_linear_params* p, LinearArgs* 
     return 0;
 }
 
+// a row length, or 0 for `least`
+int check_ld(int64_t ld, int64_t least, const char* name, int64_t* out) {
+    if (ld != 0 && (ld < least || ld % 8)) return report_error(IFVS_ERR_ARG, "%s = %lld: at least %lld and a multiple of 8, or 0", name, (long long)ld, (long long)least);
+    *out = ld ? ld : least;
+    return 0;
+}
+
+int attend_check(const ifvs_layers* L, const ifvs_attend_params* p, const void* q, const void* k, const void* v, AttendArgs* a) {
+    if (!L || !p) return report_error(IFVS_ERR_ARG, "the handle or params is NULL");
+    TRY(check_type(p->type));
+    TRY(check_tokens(p->Tq));
+    TRY(check_tokens(p->Tk));
+    if (p->dh < 1 || p->dh > IFVS_MAX_HEAD) return report_error(IFVS_ERR_ARG, "dh = %d outside 1..%d", p->dh, IFVS_MAX_HEAD);
+    if (p->heads < 1 || p->kv_heads < 1 || p->heads % p->kv_heads)
+        return report_error(IFVS_ERR_ARG, "kv_heads = %d must divide heads = %d", p->kv_heads, p->heads);
+    if ((int64_t)p->heads * p->dh > IFVS_MAX_WIDTH)
+        return report_error(IFVS_ERR_ARG, "%d heads of %d are wider than %d", p->heads, p->dh, IFVS_MAX_WIDTH);
+    if (p->n_seq < 1 || p->n_seq > 0x7FFFFFFFLL)
+        return report_error(IFVS_ERR_ARG, "n_seq = %lld outside 1..2^31 - 1", (long long)p->n_seq);
+    if (p->n_seq != 1 && (!p->q_offsets || !p->kv_offsets))
+        return report_error(IFVS_ERR_ARG, "offsets are NULL with n_seq = %lld", (long long)p->n_seq);
+    TRY(check_optional(p->q_offsets, 8, "q_offsets"));
+    TRY(check_optional(p->kv_offsets, 8, "kv_offsets"));
+    TRY(check_optional(p->kv_ids, 4, "kv_ids"));
+    if (!(p->scale > 0.f) || !isfinite(p->scale)) return report_error(IFVS_ERR_ARG, "scale must be positive and finite");
+    if (p->type == IFVS_T_F32) return report_error(IFVS_ERR_UNSUPPORTED, "attention takes 16-bit types only");
+    if (p->dh % 8) return report_error(IFVS_ERR_UNSUPPORTED, "dh = %d must be a multiple of 8", p->dh);
+    const int64_t q_row = (int64_t)p->heads * p->dh, k_row = (int64_t)p->kv_heads * p->dh;
+    *a = AttendArgs{p->Tq, p->Tk, p->n_seq, p->heads, p->kv_heads, p->heads / p->kv_heads, p->dh, p->type, p->q_offsets,
+                    p->kv_offsets, p->kv_ids, p->scale, q, k, v, 0, 0, 0, waits_of(L), L->num_sms};
+    if (a->Tq * a->group / kTileRows + a->B > 0x7FFFFFFFLL || a->Tk / kTileKeys + a->B > 0x7FFFFFFFLL)
+        return report_error(IFVS_ERR_ARG, "more than 2^31 - 1 tiles");
+    TRY(check_ld(p->ld_q, q_row, "ld_q", &a->ld_q));
+    TRY(check_ld(p->ld_k, k_row, "ld_k", &a->ld_k));
+    TRY(check_ld(p->ld_v, k_row, "ld_v", &a->ld_v));
+    if (p->Tq > 0) TRY(check_array(q, 16, "q"));
+    if (p->Tk > 0) {
+        TRY(check_array(k, 16, "k"));
+        TRY(check_array(v, 16, "v"));
+    }
+    return 0;
+}
+
 }  // namespace
 
 extern "C" {
@@ -412,6 +456,44 @@ int ifvs_linear_grad(ifvs_layers* L, const ifvs_linear_params* p, const void* x,
     Call c(L, p->stream);
     TRY(c.begin(linear_grad_bytes(a)));
     return c.end(launch_linear_grad(a, x, dy, dx, d_w, d_bias, L->work, c.s));
+}
+
+int ifvs_attend(ifvs_layers* L, const ifvs_attend_params* p, const void* q, const void* k, const void* v, void* out, float* lse) {
+    AttendArgs a;
+    TRY(attend_check(L, p, q, k, v, &a));
+    AttendOut o{out, 0, lse};
+    TRY(check_ld(p->ld_out, (int64_t)a.heads * a.dh, "ld_out", &o.ld));
+    if (a.Tq > 0) TRY(check_array(out, 16, "out"));
+    TRY(check_optional(lse, 4, "lse"));
+    Call c(L, p->stream);
+    TRY(c.begin(attend_bytes(a)));
+    return c.end(launch_attend(a, o, L->work, c.s));
+}
+
+int ifvs_attend_grad(ifvs_layers* L, const ifvs_attend_params* p, const void* q, const void* k, const void* v, const void* out,
+                     const float* lse, const void* d_out, void* dq, void* dk, void* dv) {
+    AttendArgs a;
+    TRY(attend_check(L, p, q, k, v, &a));
+    AttendGrads g{out, d_out, lse, 0, 0, dq, dk, dv, 0, 0, 0};
+    const int64_t q_row = (int64_t)a.heads * a.dh, k_row = (int64_t)a.kv_heads * a.dh;
+    TRY(check_ld(p->ld_out, q_row, "ld_out", &g.ld_out));
+    TRY(check_ld(p->ld_d_out, q_row, "ld_d_out", &g.ld_d_out));
+    TRY(check_ld(p->ld_dq, q_row, "ld_dq", &g.ld_dq));
+    TRY(check_ld(p->ld_dk, k_row, "ld_dk", &g.ld_dk));
+    TRY(check_ld(p->ld_dv, k_row, "ld_dv", &g.ld_dv));
+    if (a.Tq > 0) {
+        TRY(check_array(out, 16, "out"));
+        TRY(check_array(lse, 4, "lse"));
+        TRY(check_array(d_out, 16, "d_out"));
+        TRY(check_array(dq, 16, "dq"));
+    }
+    if (a.Tk > 0) {
+        TRY(check_array(dk, 16, "dk"));
+        TRY(check_array(dv, 16, "dv"));
+    }
+    Call c(L, p->stream);
+    TRY(c.begin(attend_grad_bytes(a)));
+    return c.end(launch_attend_grad(a, g, L->work, c.s));
 }
 
 int ifvs_dropout(ifvs_layers* L, const void* x, const void* residual, int64_t n, int32_t type, double p, uint64_t seed,

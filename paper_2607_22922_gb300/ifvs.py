@@ -62,6 +62,14 @@ class LinearParams(C.Structure):
                 ("act", C.c_int32), ("w", C.c_void_p), ("bias", C.c_void_p), ("stream", C.c_void_p)]
 
 
+class AttendParams(C.Structure):
+    _fields_ = [("Tq", C.c_int64), ("Tk", C.c_int64), ("heads", C.c_int32), ("kv_heads", C.c_int32),
+                ("dh", C.c_int32), ("type", C.c_int32), ("n_seq", C.c_int64), ("q_offsets", C.c_void_p),
+                ("kv_offsets", C.c_void_p), ("kv_ids", C.c_void_p), ("scale", C.c_float)] + [
+                    ("ld_" + n, C.c_int64) for n in ("q", "k", "v", "out", "d_out", "dq", "dk", "dv")] + [
+                        ("stream", C.c_void_p)]
+
+
 class TrainParams(C.Structure):
     _fields_ = [("tau", C.c_float), ("lam", C.c_float), ("lr", C.c_float), ("lr_wz", C.c_float),
                 ("n_pos", C.c_int32), ("n_neg", C.c_int32), ("flags", C.c_uint32),
@@ -101,6 +109,8 @@ def _load():
         "ifvs_ffn_grad": (C.c_int, [P] * 7),
         "ifvs_linear": (C.c_int, [P] * 5),
         "ifvs_linear_grad": (C.c_int, [P] * 7),
+        "ifvs_attend": (C.c_int, [P] * 7),
+        "ifvs_attend_grad": (C.c_int, [P] * 11),
         "ifvs_dropout": (C.c_int, [P, P, P, I64, I32, F64, U64, U64, P, P, P]),
         "ifvs_stage_times": (C.c_int, [P, P, P, I32]),
         "ifvs_canonical_predicate": (C.c_int, [P, P, I32, P, P, P]),
@@ -487,8 +497,9 @@ def _stream(stream):
     return stream.cuda_stream or _LEGACY_STREAM
 
 
-def _like(a, stream, *shape):
+def _like(a, stream, *shape, dtype=None):
     """An output: memory of the stream that the call runs on."""
+    dtype = a.dtype if dtype is None else dtype
     if stream:
         import torch
         raw = stream if isinstance(stream, int) else stream.cuda_stream
@@ -497,8 +508,8 @@ def _like(a, stream, *shape):
             if isinstance(stream, int):
                 stream = torch.cuda.ExternalStream(raw, a.device) if raw else torch.cuda.default_stream(a.device)
             with torch.cuda.stream(stream):
-                return a.new_empty(shape)
-    return a.new_empty(shape)
+                return a.new_empty(shape, dtype=dtype)
+    return a.new_empty(shape, dtype=dtype)
 
 
 class _LayersHandle(C.c_void_p):
@@ -674,6 +685,93 @@ def ifvs_linear_grad(L, x, w, dy, bias=None, act="none", dx=None, d_w=None, d_bi
     return dx, d_w, d_bias
 
 
+def _heads(a, shape, dtype, name, at):
+    """Address and row stride of a tensor [tokens][heads][dh] whose rows may have gaps."""
+    if a.shape != shape or a.dtype != dtype:
+        raise ValueError("%s is %s %s, expected %s %s" % (name, tuple(a.shape), a.dtype, shape, dtype))
+    if a.get_device() != at:
+        raise ValueError("%s must be a tensor on cuda:%d" % (name, at))
+    (T, H, d), ld = shape, 0
+    if not a.is_contiguous():
+        s = a.stride()
+        if s[2] != 1 or (H > 1 and s[1] != d) or (T > 1 and (s[0] < H * d or s[0] % 8)):
+            raise ValueError("%s must hold a token's heads without gaps, its rows a multiple of 8 elements apart" % name)
+        ld = s[0] if T > 1 else 0
+    return a.data_ptr() or 256, ld
+
+
+def _offsets(a, name, at):
+    if a is None:
+        return 1, None
+    if not _is_vector(a, "int64") or a.shape[0] < 2:
+        raise ValueError("%s must be a vector of B + 1 int64" % name)
+    return a.shape[0] - 1, _dev(a, (a.shape[0],), a.dtype, name, at)
+
+
+def _attend_params(q, k, v, q_offsets, kv_offsets, kv_ids, scale, stream, at):
+    """The params and the addresses of q, k and v"""
+    if q.dim() != 3 or k.dim() != 3:
+        raise ValueError("q, k and v must be [tokens][heads][dh]")
+    (Tq, H, d), (Tk, Hk, _), dt = q.shape, k.shape, q.dtype
+    (B, qo), (Bk, ko) = _offsets(q_offsets, "q_offsets", at), _offsets(kv_offsets, "kv_offsets", at)
+    if B != Bk:
+        raise ValueError("q_offsets delimit %d sequences, kv_offsets %d" % (B, Bk))
+    p = AttendParams(Tq, Tk, H, Hk, d, _type(q), B, qo, ko)
+    if kv_ids is not None:
+        if _ids(kv_ids) != Tk:
+            raise ValueError("%d kv_ids for %d keys" % (kv_ids.shape[0], Tk))
+        p.kv_ids = _dev(kv_ids, (Tk,), kv_ids.dtype, "kv_ids", at)
+    p.scale = d ** -0.5 if scale is None else scale
+    p.stream = _stream(stream)
+    shapes = (Tq, H, d), (Tk, Hk, d)
+    ptr = [0, 0, 0]
+    ptr[0], p.ld_q = _heads(q, shapes[0], dt, "q", at)
+    ptr[1], p.ld_k = _heads(k, shapes[1], dt, "k", at)
+    ptr[2], p.ld_v = _heads(v, shapes[1], dt, "v", at)
+    return p, ptr, shapes, dt
+
+
+def _lse(lse, shape, at):
+    import torch
+    return _dev(lse, shape, torch.float32, "lse", at)
+
+
+def ifvs_attend(L, q, k, v, q_offsets=None, kv_offsets=None, kv_ids=None, scale=None, out=None, lse=None, stream=None):
+    """out = softmax(scale q k) v for queries [Tq][heads][dh] and the keys and values
+    [Tk][kv_heads][dh] of their sequence, which the offsets delimit; keys whose id is
+    negative are padding.  scale: dh^-1/2 by default.  Rows may have gaps (k and v
+    halves of one tensor).  lse: True or a tensor [Tq][heads] of float32 for the
+    logarithm of the softmax's sum, which the gradient takes.  Returns (out, lse)."""
+    at = _on(L, q, "q", stream)
+    p, ptr, (sq, _), dt = _attend_params(q, k, v, q_offsets, kv_offsets, kv_ids, scale, stream, at)
+    out = _like(q, stream, *sq) if out is None else out
+    if lse is True:
+        import torch
+        lse = _like(q, stream, *sq[:2], dtype=torch.float32)
+    to, p.ld_out = _heads(out, sq, dt, "out", at)
+    _check(_lib.ifvs_attend(L, C.byref(p), *ptr, to, _lse(lse, sq[:2], at)))
+    return out, lse
+
+
+def ifvs_attend_grad(L, q, k, v, out, lse, d_out, q_offsets=None, kv_offsets=None, kv_ids=None, scale=None, dq=None,
+                     dk=None, dv=None, stream=None):
+    """Gradients (dq, dk, dv) through ifvs_attend from d_out; out and lse as the forward
+    call with the same arguments returned them."""
+    at = _on(L, q, "q", stream)
+    p, ptr, (sq, sk), dt = _attend_params(q, k, v, q_offsets, kv_offsets, kv_ids, scale, stream, at)
+    dq = _like(q, stream, *sq) if dq is None else dq
+    dk = _like(q, stream, *sk) if dk is None else dk
+    dv = _like(q, stream, *sk) if dv is None else dv
+    o, p.ld_out = _heads(out, sq, dt, "out", at)
+    do, p.ld_d_out = _heads(d_out, sq, dt, "d_out", at)
+    to = [0, 0, 0]
+    to[0], p.ld_dq = _heads(dq, sq, dt, "dq", at)
+    to[1], p.ld_dk = _heads(dk, sk, dt, "dk", at)
+    to[2], p.ld_dv = _heads(dv, sk, dt, "dv", at)
+    _check(_lib.ifvs_attend_grad(L, C.byref(p), *ptr, o, _lse(lse, sq[:2], at), do, *to))
+    return dq, dk, dv
+
+
 def ifvs_dropout(L, x, p, seed, step=0, residual=None, out=None, stream=None):
     """out = residual + (x / (1 - p) where its random word is at least p 2^32, else
     0), for a tensor of any shape; the words are those of (seed, step).  Of a
@@ -822,6 +920,8 @@ class Layers:
         self.ffn_grad = functools.partial(ifvs_ffn_grad, self.h)
         self.linear = functools.partial(ifvs_linear, self.h)
         self.linear_grad = functools.partial(ifvs_linear_grad, self.h)
+        self.attend = functools.partial(ifvs_attend, self.h)
+        self.attend_grad = functools.partial(ifvs_attend_grad, self.h)
         self.dropout = functools.partial(ifvs_dropout, self.h)
 
     def status(self):

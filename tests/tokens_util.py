@@ -79,6 +79,10 @@ def dropout(x, p, seed, step, residual):
 
 # ---- attention over packed sequences
 
+# The base-2 exponential (ex2.approx.ftz) flushes results below float32's normal range,
+# 2^-126, to zero: a probability may be off by that much whatever its relative error.
+FLUSH = 2.0 ** -126
+
 def _sequences(Tq, Tk, q_offsets, kv_offsets, ids):
     """(queries' slice, keys' indices) of every sequence"""
     qo = [0, Tq] if q_offsets is None else q_offsets.tolist()
@@ -124,7 +128,7 @@ def attend(q, k, v, q_offsets=None, kv_offsets=None, ids=None, scale=None):
         o = torch.einsum("hqk,khd->qhd", p, vv)
         size = torch.einsum("hqk,khd->qhd", p, vv.abs())
         # a p below the type's normal range rounds absolutely: 2^-25 of the largest in float16
-        tiny = (2.0 ** -25 if dt == torch.float16 else 0.0) * torch.einsum("hqk,khd->qhd", torch.ones_like(p), vv.abs())
+        tiny = (2.0 ** -25 if dt == torch.float16 else FLUSH) * torch.einsum("hqk,khd->qhd", torch.ones_like(p), vv.abs())
         e = (rel[..., 0].t()[:, :, None] + r + 4 * U * (len(keys) + 8)) * size + tiny
         out[here], eo[here] = o, rounded(o, e, dt)
         lse[here], el[here] = l[..., 0].t(), e_lse[..., 0].t()
@@ -139,7 +143,7 @@ def attend_grad(q, k, v, d_out, q_offsets=None, kv_offsets=None, ids=None, scale
     scale = 1 / math.sqrt(d) if scale is None else scale
     group = H // Hk
     r = 2.0 ** -11 if dt == torch.float16 else 2.0 ** -8
-    least = 2.0 ** -25 if dt == torch.float16 else 0.0
+    least = 2.0 ** -25 if dt == torch.float16 else FLUSH
     value = [torch.zeros(t.shape, dtype=torch.float64, device=t.device) for t in (q, k, v)]
     bound = [torch.zeros_like(t) for t in value]
     heads = lambda t: t.double().repeat_interleave(group, 1)  # noqa: E731
@@ -163,7 +167,7 @@ def attend_grad(q, k, v, d_out, q_offsets=None, kv_offsets=None, ids=None, scale
         x = dp - delta
         ex = e_delta + (d + 8) * U * dp_size + 4 * U * (dp.abs() + delta.abs())
         ds = p * x
-        eds = p * (rel + 4 * U) * x.abs() + (p + ep) * ex + r * (ds.abs() + (p + ep) * ex) + least
+        eds = (p * (rel + 4 * U) + FLUSH) * x.abs() + (p + ep) * ex + r * (ds.abs() + (p + ep) * ex) + least
 
         def put(i, at, val, err):
             value[i][at], bound[i][at] = val, rounded(val, err, dt)
