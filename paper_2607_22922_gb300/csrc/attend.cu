@@ -6,7 +6,7 @@
 // One pass over the keys: a running maximum m and sum l of exp(s - m) in float32, the
 // output rescaled where m grows.  exp(s - m), at most 1, is rounded to the arrays' type
 // because the tensor cores multiply 16-bit operands; l sums the unrounded values.
-#include "attend.cuh"
+#include "attend_tc.cuh"
 
 namespace ifvs {
 
@@ -229,46 +229,59 @@ __global__ void __launch_bounds__(256) k_attend_join(AttendArgs a, AttendOut o, 
     if (o.lse && lane == 0) o.lse[row] = l == 0.f ? -INFINITY : (top + log2f(l)) * kLn2;
 }
 
-// Parts of the keys, where the rows leave SMs without a CTA: at least two tiles of the
-// average sequence each.
-int splits_of(const AttendArgs& a) {
-    const int64_t ctas = ((a.Tq * a.group + kTileRows - 1) / kTileRows > a.B ? (a.Tq * a.group + kTileRows - 1) / kTileRows : a.B) * a.kv_heads;
-    const int64_t tiles = a.Tk / a.B / kTileKeys;
-    int64_t n = ctas > 0 ? 3 * a.num_sms / ctas : 1;
+// How a call runs
+struct Plan {
+    bool tc;             // tiles of the tensor cores
+    int pack, splits;
+};
+Plan plan_of(const AttendArgs& a) {
+    Plan p;
+    p.pack = tc_pack(a);
+    p.tc = a.Tq * p.pack / a.B >= 128 && a.Tk / a.B >= 256;
+    // Parts of the keys, where the rows leave SMs without a CTA: at least two tiles of the
+    // average sequence each.
+    const int group = p.tc ? p.pack : a.group, rows = p.tc ? 256 : kTileRows, keys = p.tc ? 128 : kTileKeys;
+    const int64_t row_tiles = (a.Tq * group + rows - 1) / rows;
+    const int64_t ctas = (row_tiles > a.B ? row_tiles : a.B) * (a.heads / group), tiles = a.Tk / a.B / keys;
+    int64_t n = (p.tc ? 1 : 3) * a.num_sms / ctas;
     if (n > tiles / 2) n = tiles / 2;
     if (n > 64) n = 64;
-    return (int)(n < 1 ? 1 : n);
+    p.splits = (int)(n < 1 ? 1 : n);
+    return p;
 }
 
 template <class T, int DH>
-cudaError_t run(const AttendArgs& a, const AttendOut& o, uint8_t* work, cudaStream_t s) {
-    const int splits = splits_of(a);
-    float *part_out = nullptr, *part_lse = nullptr;
-    if (splits > 1) {
-        part_out = (float*)work;
-        part_lse = (float*)(work + padded((size_t)splits * a.Tq * a.heads * a.dh * 4));
-    }
+cudaError_t run(const AttendArgs& a, const AttendOut& o, int splits, float* part_out, float* part_lse, cudaStream_t s) {
     constexpr size_t smem = WarpTiles<T, DH>::kSmem;
-    cudaError_t e = allow_smem(k_attend<T, DH>, smem);
+    const cudaError_t e = allow_smem(k_attend<T, DH>, smem);
     if (e != cudaSuccess) return e;
     const dim3 grid((unsigned)slots(a.Tq, a.B, a.group, kTileRows), (unsigned)a.kv_heads, (unsigned)splits);
-    e = launch_next(k_attend<T, DH>, grid, dim3(128), smem, false, s, a, o, splits, part_out, part_lse);
-    if (e != cudaSuccess || splits == 1 || a.Tq == 0) return e;
-    return launch_next(k_attend_join<T>, dim3((unsigned)((a.Tq * a.heads + 7) / 8)), dim3(256), 0, true, s, a, o, splits,
-                       (const float*)part_out, (const float*)part_lse);
+    return launch_next(k_attend<T, DH>, grid, dim3(128), smem, false, s, a, o, splits, part_out, part_lse);
 }
 
 }  // namespace
 
 size_t attend_bytes(const AttendArgs& a) {
-    const int splits = splits_of(a);
+    const int splits = plan_of(a).splits;
     return splits == 1 ? 0 : padded((size_t)splits * a.Tq * a.heads * a.dh * 4) + padded((size_t)splits * a.Tq * a.heads * 4);
 }
 
 cudaError_t launch_attend(const AttendArgs& a, const AttendOut& o, uint8_t* work, cudaStream_t s) {
+    const Plan p = plan_of(a);
+    float *part_out = nullptr, *part_lse = nullptr;
+    if (p.splits > 1) {
+        part_out = (float*)work;
+        part_lse = (float*)(work + padded((size_t)p.splits * a.Tq * a.heads * a.dh * 4));
+    }
     auto go = [&](auto t) {
         using T = decltype(t);
-        return a.dh <= 32 ? run<T, 32>(a, o, work, s) : a.dh <= 64 ? run<T, 64>(a, o, work, s) : run<T, 128>(a, o, work, s);
+        const cudaError_t e = p.tc           ? launch_attend_tc(a, o, p.pack, p.splits, part_out, part_lse, s)
+                              : a.dh <= 32 ? run<T, 32>(a, o, p.splits, part_out, part_lse, s)
+                              : a.dh <= 64 ? run<T, 64>(a, o, p.splits, part_out, part_lse, s)
+                                           : run<T, 128>(a, o, p.splits, part_out, part_lse, s);
+        if (e != cudaSuccess || p.splits == 1 || a.Tq == 0) return e;
+        return launch_next(k_attend_join<T>, dim3((unsigned)((a.Tq * a.heads + 7) / 8)), dim3(256), 0, true, s, a, o, p.splits,
+                           (const float*)part_out, (const float*)part_lse);
     };
     return a.type == IFVS_T_F16 ? go(__half()) : go(__nv_bfloat16());
 }

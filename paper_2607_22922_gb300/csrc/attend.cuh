@@ -175,8 +175,6 @@ __device__ __forceinline__ void load_rows(const Rows<DH>& to, int rows, int dh, 
     }
 }
 
-inline size_t padded(size_t n) { return (n + 255) / 256 * 256; }
-
 // ---- launchers --------------------------------------------------------------------------
 size_t attend_bytes(const AttendArgs& a);
 cudaError_t launch_attend(const AttendArgs& a, const AttendOut& o, uint8_t* work, cudaStream_t s);

@@ -737,7 +737,6 @@ SumPlan sum_plan(const EmbedArgs& a, int most_columns, int multiple, int warps) 
     return p;
 }
 
-size_t padded(size_t n) { return (n + 255) / 256 * 256; }
 int64_t sort_tiles(const EmbedArgs& a) { return (a.T + kTileTokens - 1) / kTileTokens; }
 
 cudaError_t sort_by_id(const EmbedArgs& a, Pairs p0, Pairs p1, uint32_t* counts, cudaStream_t s, Pairs* sorted) {

@@ -17,6 +17,7 @@ constexpr int kErrOffsets = 1;   // offsets that break their rules
 constexpr int kErrWait = 2;      // a bounded wait ran out
 constexpr int kErrWords = 3;
 
+inline size_t padded(size_t n) { return (n + 255) / 256 * 256; }
 inline size_t elem_bytes(int type) { return type == IFVS_T_F32 ? 4 : 2; }
 
 // ---- element types --------------------------------------------------------

@@ -181,7 +181,6 @@ constexpr size_t smem_of(uint32_t stage_bytes, uint32_t out_bytes) {
 // ---- host -------------------------------------------------------------------------
 inline int ceil_div(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
 
-inline size_t padded(size_t n) { return (n + 255) / 256 * 256; }
 
 // f(constant) for the activation
 template <class Fn>
