@@ -7,7 +7,7 @@
 // tensor cores multiply 16-bit operands; sums are float32, in a fixed order.  Where a
 // sequence's keys are one tile, lse and delta come from the tile itself, else from the
 // forward call's lse and (rounded) output.
-#include "attend.cuh"
+#include "attend_tc.cuh"
 
 namespace ifvs {
 
@@ -403,46 +403,61 @@ __global__ void __launch_bounds__(128) k_attend_rows(AttendArgs a, AttendGrads g
                     [&](int i) { return at.dq + token(warp * 16 + i) * g.ld_dq + head(warp * 16 + i); });
 }
 
-// Parts of the rows, where the tiles of keys leave SMs without a CTA
-int splits_of(const AttendArgs& a) {
-    const int64_t tiles = a.Tk / kTileKeys > a.B ? a.Tk / kTileKeys : a.B, ctas = tiles * a.kv_heads;
-    const int64_t row_tiles = a.Tq * a.group / a.B / kTileRows;
-    int64_t n = 3 * a.num_sms / ctas;
+// How a call runs
+struct Plan {
+    bool tc;             // tiles of the tensor cores
+    int pack, splits;
+    size_t delta_bytes;
+};
+Plan plan_of(const AttendArgs& a) {
+    Plan p;
+    p.pack = tc_pack(a);
+    p.tc = a.Tq * p.pack / a.B >= 128 && a.Tk / a.B >= 256;
+    p.delta_bytes = p.tc ? padded((size_t)a.Tq * a.heads * 4) : 0;
+    // Parts of the rows, where the tiles of keys leave SMs without a CTA
+    const int keys = p.tc ? 128 : kTileKeys, rows = p.tc ? 128 : kTileRows;
+    const int64_t tiles = a.Tk / keys > a.B ? a.Tk / keys : a.B, ctas = tiles * a.kv_heads;
+    const int64_t row_tiles = a.Tq * a.group / a.B / rows;
+    int64_t n = (p.tc ? 1 : 3) * a.num_sms / ctas;
     if (n > row_tiles / 2) n = row_tiles / 2;
     if (n > 64) n = 64;
-    return (int)(n < 1 ? 1 : n);
+    p.splits = (int)(n < 1 ? 1 : n);
+    return p;
 }
 
 template <class T, int DH>
-cudaError_t run(const AttendArgs& a, const AttendGrads& g, uint8_t* work, cudaStream_t s) {
-    const int splits = splits_of(a);
-    float* part_dk = splits > 1 ? (float*)work : nullptr;
-    float* part_dv = splits > 1 ? part_dk + (size_t)splits * a.Tk * a.kv_heads * a.dh : nullptr;
+cudaError_t run(const AttendArgs& a, const AttendGrads& g, int splits, float* part_dk, float* part_dv, cudaStream_t s) {
     cudaError_t e = allow_smem(k_attend_keys<T, DH>, KeyTiles<T, DH>::kSmem);
     if (e == cudaSuccess) e = allow_smem(k_attend_rows<T, DH>, RowTiles<T, DH>::kSmem);
     if (e != cudaSuccess) return e;
     e = launch_next(k_attend_keys<T, DH>, dim3((unsigned)slots(a.Tk, a.B, 1, kTileKeys), (unsigned)a.kv_heads, (unsigned)splits), dim3(128),
                     KeyTiles<T, DH>::kSmem, false, s, a, g, splits, part_dk, part_dv);
-    if (e != cudaSuccess) return e;
-    if (a.Tk > kTileKeys && a.Tq > 0)
-        e = launch_next(k_attend_rows<T, DH>, dim3((unsigned)slots(a.Tq, a.B, a.group, kTileRows), (unsigned)a.kv_heads), dim3(128),
-                        RowTiles<T, DH>::kSmem, false, s, a, g);
-    if (e != cudaSuccess || splits == 1 || a.Tk == 0) return e;
-    return launch_next(k_attend_keys_join<T>, dim3((unsigned)((a.Tk * a.kv_heads * a.dh + 1023) / 1024), 2u), dim3(256), 0, false, s, a, g,
-                       splits, (const float*)part_dk, (const float*)part_dv);
+    if (e != cudaSuccess || a.Tk <= kTileKeys || a.Tq == 0) return e;
+    return launch_next(k_attend_rows<T, DH>, dim3((unsigned)slots(a.Tq, a.B, a.group, kTileRows), (unsigned)a.kv_heads), dim3(128),
+                       RowTiles<T, DH>::kSmem, false, s, a, g);
 }
 
 }  // namespace
 
 size_t attend_grad_bytes(const AttendArgs& a) {
-    const int splits = splits_of(a);
-    return splits == 1 ? 0 : (size_t)splits * a.Tk * a.kv_heads * a.dh * 8;
+    const Plan p = plan_of(a);
+    return p.delta_bytes + (p.splits == 1 ? 0 : (size_t)p.splits * a.Tk * a.kv_heads * a.dh * 8);
 }
 
 cudaError_t launch_attend_grad(const AttendArgs& a, const AttendGrads& g, uint8_t* work, cudaStream_t s) {
+    const Plan p = plan_of(a);
+    float* delta = (float*)work;
+    float* part_dk = p.splits > 1 ? (float*)(work + p.delta_bytes) : nullptr;
+    float* part_dv = p.splits > 1 ? part_dk + (size_t)p.splits * a.Tk * a.kv_heads * a.dh : nullptr;
     auto go = [&](auto t) {
         using T = decltype(t);
-        return a.dh <= 32 ? run<T, 32>(a, g, work, s) : a.dh <= 64 ? run<T, 64>(a, g, work, s) : run<T, 128>(a, g, work, s);
+        const cudaError_t e = p.tc           ? launch_attend_grad_tc(a, g, p.pack, p.splits, delta, part_dk, part_dv, s)
+                              : a.dh <= 32 ? run<T, 32>(a, g, p.splits, part_dk, part_dv, s)
+                              : a.dh <= 64 ? run<T, 64>(a, g, p.splits, part_dk, part_dv, s)
+                                           : run<T, 128>(a, g, p.splits, part_dk, part_dv, s);
+        if (e != cudaSuccess || p.splits == 1 || a.Tk == 0) return e;
+        return launch_next(k_attend_keys_join<T>, dim3((unsigned)((a.Tk * a.kv_heads * a.dh + 1023) / 1024), 2u), dim3(256), 0, false, s,
+                           a, g, p.splits, (const float*)part_dk, (const float*)part_dv);
     };
     return a.type == IFVS_T_F16 ? go(__half()) : go(__nv_bfloat16());
 }

@@ -56,5 +56,8 @@ inline int tc_pack(const AttendArgs& a) { return (a.group & (a.group - 1)) == 0 
 
 cudaError_t launch_attend_tc(const AttendArgs& a, const AttendOut& o, int pack, int splits, float* part_out, float* part_lse,
                              cudaStream_t s);
+// delta: [Tq][heads] floats of workspace
+cudaError_t launch_attend_grad_tc(const AttendArgs& a, const AttendGrads& g, int pack, int splits, float* delta, float* part_dk,
+                                  float* part_dv, cudaStream_t s);
 
 }  // namespace ifvs
