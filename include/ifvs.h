@@ -652,7 +652,7 @@ int ifvs_linear_grad(ifvs_layers* L, const ifvs_linear_params* p, const void* x,
 /* What ifvs_attend and its gradient share.  Rows of q and of what has its shape are
  * tokens: `heads` times dh elements, head h in elements h dh .. h dh + dh - 1; rows of
  * k and v the same with kv_heads.  ld_*: elements from one row to the next, a
- * multiple of 8, at least a row's; 0: rows without gaps.  (So that k and v can be halves
+ * multiple of 8, at least a row's, below 2^31; 0: rows without gaps.  (So that k and v can be halves
  * of one projection's output, and their gradients halves of its gradient.) */
 typedef struct {
     int64_t Tq, Tk;     /* queries and keys, 0 <= T < 2^31                    */

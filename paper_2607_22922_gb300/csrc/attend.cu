@@ -13,189 +13,250 @@ namespace ifvs {
 namespace {
 
 // ---- tiles of warps: any lengths ---------------------------------------------------------
-// A CTA takes 64 rows of one group and the keys of one split, 64 at a time; each of its 4
-// warps holds 16 rows' output in registers.
+// A CTA of 4 warps takes up to 2^log_rows rows of one group and the keys of one split.  Up to 128
+// keys stay in shared memory, and the warps go through tiles of 16 rows by themselves, the
+// next tile's queries on their way; more keys pass 64 at a time, for 64 rows at a time.
+constexpr int kWarps = 4, kResident = 128;
+
 template <class T, int DH>
 struct WarpTiles {
-    Rows<DH> q, k[2], v[2];
-    static constexpr uint32_t kRowsBytes = Rows<DH>::kLd * 2;
-    static constexpr size_t kSmem = (kTileRows + 4 * kTileKeys) * kRowsBytes;
+    static constexpr uint32_t kRowBytes = Rows<DH>::kLd * 2;
+    static constexpr size_t kSmem = (2 * kResident + kWarps * 32) * kRowBytes;
+    Rows<DH> k, v, q;        // kResident rows of keys and values; this warp's two tiles of queries
+    __device__ __forceinline__ explicit WarpTiles(const void* smem) {
+        k.at = smem32(smem);
+        v.at = k.at + kResident * kRowBytes;
+        q.at = v.at + (kResident + (threadIdx.x >> 5) * 32) * kRowBytes;
+    }
 };
 
+// A warp's 16 rows on their way through the keys
 template <class T, int DH>
-__global__ void __launch_bounds__(128) k_attend(AttendArgs a, AttendOut o, int splits, float* part_out, float* part_lse) {
-    extern __shared__ __align__(16) uint8_t raw[];
-    __shared__ uint32_t valid_bits[2][2];
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, hk = blockIdx.y, split = blockIdx.z;
-    check_offsets(a.q_offsets, a.B, a.Tq, a.waits.err);
-    check_offsets(a.kv_offsets, a.B, a.Tk, a.waits.err);
-    const Slot slot = slot_of(a.q_offsets, a.B, a.Tq, a.group, kTileRows, blockIdx.x);
-    const Span qs = span_of(a.q_offsets, slot.b, a.B, a.Tq), ks = span_of(a.kv_offsets, slot.b, a.B, a.Tk);
-    const int64_t row0 = slot.tile * kTileRows, left = qs.len * a.group - row0;
-    if (slot.tile < 0 || left <= 0) return;
-    const int rows = left < kTileRows ? (int)left : kTileRows;
-    const RowOf at(row0, a.group);
-    // this split's keys, whole tiles
-    const int64_t tiles = (ks.len + kTileKeys - 1) / kTileKeys;
-    const int64_t t0 = tiles * split / splits, t1 = tiles * (split + 1) / splits;
-
-    WarpTiles<T, DH> sm;
-    sm.q.at = smem32(raw);
-    for (int i = 0; i < 2; ++i) {
-        sm.k[i].at = sm.q.at + (kTileRows + 2 * i * kTileKeys) * sm.kRowsBytes;
-        sm.v[i].at = sm.k[i].at + kTileKeys * sm.kRowsBytes;
+struct Running {
+    float acc[DH / 8][4], m[2], l[2];
+    uint32_t q[DH / 16][4];
+    __device__ __forceinline__ void begin(const Rows<DH>& from, int row) {
+#pragma unroll
+        for (int d = 0; d < DH / 16; ++d) from.a(q[d], row, d * 16);
+#pragma unroll
+        for (int j = 0; j < DH / 8; ++j)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) acc[j][i] = 0.f;
+        m[0] = m[1] = -INFINITY;
+        l[0] = l[1] = 0.f;
     }
-    const T *q = (const T*)a.q + (int64_t)hk * a.group * a.dh, *k = (const T*)a.k + (int64_t)hk * a.dh,
-            *v = (const T*)a.v + (int64_t)hk * a.dh;
-    load_rows<DH, T>(sm.q, kTileRows, a.dh, a.q, [&](int i) {
-        return i < rows ? q + (qs.at + at.token_of(i)) * a.ld_q + (int64_t)at.head_of(i) * a.dh : nullptr;
-    });
-    auto key_in = [&](int64_t key) { return key < ks.len && (a.kv_ids == nullptr || __ldg(a.kv_ids + ks.at + key) >= 0); };
-    auto load_keys = [&](int64_t tile, int stage) {
-        const int64_t key0 = tile * kTileKeys;
-        load_rows<DH, T>(sm.k[stage], kTileKeys, a.dh, a.q, [&](int i) { return key_in(key0 + i) ? k + (ks.at + key0 + i) * a.ld_k : nullptr; });
-        load_rows<DH, T>(sm.v[stage], kTileKeys, a.dh, a.q, [&](int i) { return key_in(key0 + i) ? v + (ks.at + key0 + i) * a.ld_v : nullptr; });
-        if (warp < 2) {
-            const uint32_t bits = __ballot_sync(0xFFFFFFFFu, key_in(key0 + warp * 32 + lane));
-            if (lane == 0) valid_bits[stage][warp] = bits;
+    // up to 64 keys from row `at` of k and v, `blocks` of 16; bias: 0, or -infinity for a key
+    // that does not count, where its score's sum begins.  first: nothing came before.
+    __device__ __forceinline__ void step(const Rows<DH>& k, const Rows<DH>& v, int at, int blocks, const float* bias, float c, bool first) {
+        const int lane = threadIdx.x & 31;
+        float2 s[kTileKeys / 8][2];
+#pragma unroll
+        for (int j = 0; j < kTileKeys / 16; ++j) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+                s[2 * j + i][0] = s[2 * j + i][1] = *reinterpret_cast<const float2*>(bias + at + (2 * j + i) * 8 + (lane & 3) * 2);
+            if (j < blocks)
+#pragma unroll
+                for (int d = 0; d < DH / 16; ++d) {
+                    uint32_t b[4];
+                    k.b_t(b, at + j * 16, d * 16);
+                    mma16816<T>(reinterpret_cast<float(&)[4]>(s[2 * j]), q[d], b[0], b[1]);
+                    mma16816<T>(reinterpret_cast<float(&)[4]>(s[2 * j + 1]), q[d], b[2], b[3]);
+                }
         }
-    };
-    if (t0 < t1) load_keys(t0, 0);
-    copies_done();
-
-    float acc[DH / 8][4], m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
 #pragma unroll
-    for (int j = 0; j < DH / 8; ++j)
+        for (int r = 0; r < 2; ++r) {
+            float top = fmaxf(s[0][r].x, s[0][r].y);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) acc[j][i] = 0.f;
-    uint32_t qf[DH / 16][4];
-    const float c = a.scale * kLog2e;
-    const bool active = warp * 16 < rows;
-    for (int64_t t = t0; t < t1; ++t) {
-        const int stage = (int)(t - t0) & 1;
-        if (t + 1 < t1) load_keys(t + 1, stage ^ 1);
-        copies_done();
-        wait_copies<1>();
-        __syncthreads();
-        if (active) {
-            if (t == t0)
-#pragma unroll
-                for (int d = 0; d < DH / 16; ++d) sm.q.a(qf[d], warp * 16, d * 16);
-            float s[kTileKeys / 8][4];
+            for (int j = 1; j < kTileKeys / 8; ++j) top = fmaxf(top, fmaxf(s[j][r].x, s[j][r].y));
+            top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
+            top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
+            top = fmaxf(m[r], top * c);
+            const float base = top == -INFINITY ? 0.f : top;
+            const float2 c2 = make_float2(c, c), b2 = make_float2(-base, -base);
+            float2 sum = make_float2(0.f, 0.f);
 #pragma unroll
             for (int j = 0; j < kTileKeys / 8; ++j)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) s[j][i] = 0.f;
-#pragma unroll
-            for (int d = 0; d < DH / 16; ++d)
-#pragma unroll
-                for (int j = 0; j < kTileKeys / 16; ++j) {
-                    uint32_t b[4];
-                    sm.k[stage].b_t(b, j * 16, d * 16);
-                    mma16816<T>(s[2 * j], qf[d], b[0], b[1]);
-                    mma16816<T>(s[2 * j + 1], qf[d], b[2], b[3]);
+                if (j / 2 < blocks) {
+                    float2 e = fma_(s[j][r], c2, b2);
+                    e.x = ex2(e.x);
+                    e.y = ex2(e.y);
+                    s[j][r] = e;
+                    sum = add_(sum, e);
                 }
-            const uint32_t lo = valid_bits[stage][0], hi = valid_bits[stage][1];
-            if ((lo & hi) != 0xFFFFFFFFu)
-#pragma unroll
-                for (int j = 0; j < kTileKeys / 8; ++j)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int key = j * 8 + (lane & 3) * 2 + (i & 1);
-                        if (!(((key < 32 ? lo : hi) >> (key & 31)) & 1u)) s[j][i] = -INFINITY;
-                    }
-#pragma unroll
-            for (int r = 0; r < 2; ++r) {
-                float top = -INFINITY;
-#pragma unroll
-                for (int j = 0; j < kTileKeys / 8; ++j) top = fmaxf(top, fmaxf(s[j][2 * r], s[j][2 * r + 1]));
-                top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
-                top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
-                top = fmaxf(m[r], top * c);
-                const float base = top == -INFINITY ? 0.f : top, shrink = ex2(m[r] - base);
-                m[r] = top;
-                float sum = 0.f;
-#pragma unroll
-                for (int j = 0; j < kTileKeys / 8; ++j)
-#pragma unroll
-                    for (int i = 2 * r; i < 2 * r + 2; ++i) {
-                        s[j][i] = ex2(fmaf(s[j][i], c, -base));
-                        sum += s[j][i];
-                    }
-                l[r] = l[r] * shrink + sum;
+            if (first) {
+                l[r] = total(sum);
+            } else {
+                const float shrink = ex2(m[r] - base);
+                l[r] = l[r] * shrink + total(sum);
 #pragma unroll
                 for (int j = 0; j < DH / 8; ++j) {
                     acc[j][2 * r] *= shrink;
                     acc[j][2 * r + 1] *= shrink;
                 }
             }
+            m[r] = top;
+        }
 #pragma unroll
-            for (int j = 0; j < kTileKeys / 16; ++j) {
+        for (int j = 0; j < kTileKeys / 16; ++j)
+            if (j < blocks) {
                 uint32_t p[4];
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    p[i] = pack2(make_float2(s[2 * j + (i >> 1)][(i & 1) * 2], s[2 * j + (i >> 1)][(i & 1) * 2 + 1]), T());
+                for (int i = 0; i < 4; ++i) p[i] = pack2(s[2 * j + (i >> 1)][i & 1], T());
 #pragma unroll
                 for (int d = 0; d < DH / 16; ++d) {
                     uint32_t b[4];
-                    sm.v[stage].b(b, j * 16, d * 16);
+                    v.b(b, at + j * 16, d * 16);
                     mma16816<T>(acc[2 * d], p, b[0], b[1]);
                     mma16816<T>(acc[2 * d + 1], p, b[2], b[3]);
                 }
             }
-        }
-        __syncthreads();
     }
-    wait_copies<0>();
-    __syncthreads();
-    if (!active) return;
-    float inv[2], ln[2];
-#pragma unroll
-    for (int r = 0; r < 2; ++r) {
-        l[r] += __shfl_xor_sync(0xFFFFFFFFu, l[r], 1);
-        l[r] += __shfl_xor_sync(0xFFFFFFFFu, l[r], 2);
-        inv[r] = l[r] == 0.f ? 0.f : 1.f / l[r];          // 0: no key
-        ln[r] = l[r] == 0.f ? -INFINITY : m[r] + log2f(l[r]);
-    }
-    const int g = lane >> 2, two = (lane & 3) * 2;
-    if (splits > 1) {
+    // 1 / l and the base-2 logarithm of the sum, of rows lane / 4 and + 8
+    __device__ __forceinline__ void close(float (&inv)[2], float (&ln)[2]) {
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
-            const int i = warp * 16 + g + 8 * r;
-            if (i >= rows) continue;
-            const int64_t to = ((int64_t)split * a.Tq + qs.at + at.token_of(i)) * a.heads + hk * a.group + at.head_of(i);
+            l[r] += __shfl_xor_sync(0xFFFFFFFFu, l[r], 1);
+            l[r] += __shfl_xor_sync(0xFFFFFFFFu, l[r], 2);
+            inv[r] = l[r] == 0.f ? 0.f : 1.f / l[r];          // 0: no key
+            ln[r] = l[r] == 0.f ? -INFINITY : m[r] + log2f(l[r]);
+        }
+    }
+};
+
+template <class T, int DH>
+__global__ void __launch_bounds__(kWarps * 32, DH == 128 ? 2 : 4)
+k_attend(AttendArgs a, AttendOut o, int log_rows, int splits, float* part_out, float* part_lse) {
+    extern __shared__ __align__(16) uint8_t raw[];
+    __shared__ __align__(8) float bias[kResident];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, hk = blockIdx.y, split = blockIdx.z;
+    check_offsets(a.q_offsets, a.B, a.Tq, a.waits.err);
+    check_offsets(a.kv_offsets, a.B, a.Tk, a.waits.err);
+    const Slot slot = slot_of(a.q_offsets, a.B, a.Tq, a.group, log_rows, blockIdx.x);
+    const Span qs = span_of(a.q_offsets, slot.b, a.B, a.Tq), ks = span_of(a.kv_offsets, slot.b, a.B, a.Tk);
+    const int64_t row0 = slot.tile << log_rows, left = qs.len * a.group - row0;
+    if (slot.tile < 0 || left <= 0) return;
+    const int rows = left < 1 << log_rows ? (int)left : 1 << log_rows;
+    const RowOf ro(row0, a.group);
+    // this split's keys, whole tiles
+    const int64_t tiles = (ks.len + kTileKeys - 1) / kTileKeys;
+    const int64_t t0 = tiles * split / splits, t1 = tiles * (split + 1) / splits;
+    const WarpTiles<T, DH> sm(raw);
+    const T *k = (const T*)a.k + (int64_t)hk * a.dh, *v = (const T*)a.v + (int64_t)hk * a.dh;
+    const RowsAt<const T> q((const T*)a.q + (int64_t)hk * a.group * a.dh, qs.at + ro.token, a.ld_q, a.dh);
+    const RowsAt<T> out((T*)o.out + (int64_t)hk * a.group * a.dh, qs.at + ro.token, o.ld, a.dh);
+    // a row's place in arrays [Tq][heads]
+    auto head_row = [&](int i) {
+        const int2 r = ro.at(i);
+        return (qs.at + ro.token + r.x) * a.heads + hk * a.group + r.y;
+    };
+    auto key_in = [&](int64_t key) { return key < ks.len && (a.kv_ids == nullptr || __ldg(a.kv_ids + ks.at + key) >= 0); };
+    // n keys from key0 on to row `to`, and the bias of up to 64 or all
+    auto load_keys = [&](int64_t key0, int n, int to) {
+        const Rows<DH> dk{sm.k.addr(to, 0)}, dv{sm.v.addr(to, 0)};
+        load_rows<DH, T>(dk, n, a.dh, a.q, [&](int i) { return key_in(key0 + i) ? k + (ks.at + key0 + i) * a.ld_k : nullptr; });
+        load_rows<DH, T>(dv, n, a.dh, a.q, [&](int i) { return key_in(key0 + i) ? v + (ks.at + key0 + i) * a.ld_v : nullptr; });
+        for (int i = threadIdx.x; i < (n + 63) / 64 * 64; i += kWarps * 32) bias[to + i] = i < n && key_in(key0 + i) ? 0.f : -INFINITY;
+    };
+    // this warp's 16 rows from `row` on, to its buffer `to`
+    auto load_queries = [&](int row, int to) {
+        constexpr int C = DH / 8;
+#pragma unroll 4
+        for (int i = lane; i < 16 * C; i += 32) {
+            const int r = row + i / C, d = i % C * 8;
+            const bool in = r < rows && d < a.dh;
+            copy16(sm.q.addr(to * 16 + i / C, d), in ? (const void*)(q(ro.at(r)) + d) : a.q, in);
+        }
+    };
+    const float c = a.scale * kLog2e;
+    const int g = lane >> 2, two = (lane & 3) * 2;
+    Running<T, DH> run;
+    // writes the 16 rows from `row` on, through this warp's buffer `by`
+    auto put = [&](int row, int by) {
+        float inv[2], ln[2];
+        run.close(inv, ln);
+        if (splits > 1) {
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+                const int i = row + g + 8 * r;
+                if (i >= rows) continue;
+                const int64_t to = (int64_t)split * a.Tq * a.heads + head_row(i);
+#pragma unroll
+                for (int j = 0; j < DH / 8; ++j)
+                    if (j * 8 < a.dh)
+                        *reinterpret_cast<float2*>(part_out + to * a.dh + j * 8 + two) =
+                            make_float2(run.acc[j][2 * r] * inv[r], run.acc[j][2 * r + 1] * inv[r]);
+                if ((lane & 3) == 0) part_lse[to] = ln[r];
+            }
+            return;
+        }
+        __syncwarp();
+#pragma unroll
+        for (int r = 0; r < 2; ++r)
 #pragma unroll
             for (int j = 0; j < DH / 8; ++j)
-                if (j * 8 < a.dh)
-                    *reinterpret_cast<float2*>(part_out + to * a.dh + j * 8 + two) =
-                        make_float2(acc[j][2 * r] * inv[r], acc[j][2 * r + 1] * inv[r]);
-            if ((lane & 3) == 0) part_lse[to] = ln[r];
+                asm volatile("st.shared.b32 [%0], %1;" ::"r"(sm.q.addr(by * 16 + g + 8 * r, j * 8 + two)),
+                             "r"(pack2(make_float2(run.acc[j][2 * r] * inv[r], run.acc[j][2 * r + 1] * inv[r]), T()))
+                             : "memory");
+        __syncwarp();
+        constexpr int C = DH / 8;
+#pragma unroll 4
+        for (int i = lane; i < 16 * C; i += 32) {
+            const int r = row + i / C, d = i % C * 8;
+            if (r >= rows || d >= a.dh) continue;
+            uint4 w;
+            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+                         : "=r"(w.x), "=r"(w.y), "=r"(w.z), "=r"(w.w)
+                         : "r"(sm.q.addr(by * 16 + i / C, d))
+                         : "memory");
+            __stcs(reinterpret_cast<uint4*>(out(ro.at(r)) + d), w);
+        }
+        if (o.lse && (lane & 3) == 0)
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+                const int i = row + g + 8 * r;
+                if (i < rows) o.lse[head_row(i)] = ln[r] * kLn2;
+            }
+        __syncwarp();
+    };
+
+    const int64_t key0 = t0 * kTileKeys, key1 = t1 * kTileKeys < ks.len ? t1 * kTileKeys : ks.len;
+    if (key1 - key0 <= kResident) {
+        const int n = key1 > key0 ? (int)(key1 - key0) : 0, blocks = (n + 15) / 16;
+        load_keys(key0, blocks * 16, 0);
+        load_queries(warp * 16, 0);
+        copies_done();
+        wait_copies<0>();
+        __syncthreads();
+        int by = 0;
+        for (int row = warp * 16; row < rows; row += kWarps * 16, by ^= 1) {
+            if (row + kWarps * 16 < rows) load_queries(row + kWarps * 16, by ^ 1);
+            copies_done();
+            wait_copies<1>();
+            __syncwarp();
+            run.begin(sm.q, by * 16);
+            for (int at = 0; at < blocks; at += 4) run.step(sm.k, sm.v, at * 16, min(blocks - at, 4), bias, c, at == 0);
+            put(row, by);
         }
         return;
     }
-    // through this warp's rows of the query tile, so that rows are written 16 bytes a lane
-#pragma unroll
-    for (int r = 0; r < 2; ++r)
-#pragma unroll
-        for (int j = 0; j < DH / 8; ++j)
-            asm volatile("st.shared.b32 [%0], %1;" ::"r"(sm.q.addr(warp * 16 + g + 8 * r, j * 8 + two)),
-                         "r"(pack2(make_float2(acc[j][2 * r] * inv[r], acc[j][2 * r + 1] * inv[r]), T()))
-                         : "memory");
-    __syncwarp();
-    T* out = (T*)o.out + (int64_t)hk * a.group * a.dh;
-    for (int i = lane; i < 16 * (DH / 8); i += 32) {
-        const int r = warp * 16 + i / (DH / 8), d = i % (DH / 8) * 8;
-        if (r >= rows || d >= a.dh) continue;
-        uint4 w;
-        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w.x), "=r"(w.y), "=r"(w.z), "=r"(w.w) : "r"(sm.q.addr(r, d)) : "memory");
-        *reinterpret_cast<uint4*>(out + (qs.at + at.token_of(r)) * o.ld + (int64_t)at.head_of(r) * a.dh + d) = w;
-    }
-    if (o.lse && (lane & 3) == 0)
-#pragma unroll
-        for (int r = 0; r < 2; ++r) {
-            const int i = warp * 16 + g + 8 * r;
-            if (i < rows) o.lse[(qs.at + at.token_of(i)) * a.heads + hk * a.group + at.head_of(i)] = ln[r] * kLn2;
+    for (int row0 = 0; row0 < rows; row0 += kWarps * 16) {
+        const int row = row0 + warp * 16;
+        load_queries(row, 0);
+        load_keys(key0, kTileKeys, 0);
+        copies_done();
+        for (int64_t t = t0; t < t1; ++t) {
+            const int stage = (int)(t - t0) & 1;
+            if (t + 1 < t1) load_keys((t + 1) * kTileKeys, kTileKeys, (stage ^ 1) * kTileKeys);
+            copies_done();
+            wait_copies<1>();
+            __syncthreads();
+            if (t == t0) run.begin(sm.q, 0);
+            if (row < rows) run.step(sm.k, sm.v, stage * kTileKeys, 4, bias, c, t == t0);
+            __syncthreads();
         }
+        if (row < rows) put(row, 0);
+    }
 }
 
 // Joins the splits of every row, in order: a warp per (token, head).
@@ -232,18 +293,24 @@ __global__ void __launch_bounds__(256) k_attend_join(AttendArgs a, AttendOut o, 
 // How a call runs
 struct Plan {
     bool tc;             // tiles of the tensor cores
-    int pack, splits;
+    int pack, log_rows, splits;
 };
 Plan plan_of(const AttendArgs& a) {
     Plan p;
     p.pack = tc_pack(a);
     p.tc = a.Tq * p.pack / a.B >= 128 && a.Tk / a.B >= 256;
+    const int group = p.tc ? p.pack : a.group, keys = p.tc ? 128 : kTileKeys;
+    auto ctas = [&](int log) {
+        const int64_t tiles = (a.Tq * group >> log) + 1;
+        return (tiles > a.B ? tiles : a.B) * (a.heads / group);
+    };
+    // Rows of a CTA: more use the keys in shared memory again, as long as the SMs have work
+    p.log_rows = p.tc ? 8 : 9;
+    while (!p.tc && p.log_rows > 6 && ctas(p.log_rows) < 4 * a.num_sms) --p.log_rows;
     // Parts of the keys, where the rows leave SMs without a CTA: at least two tiles of the
     // average sequence each.
-    const int group = p.tc ? p.pack : a.group, rows = p.tc ? 256 : kTileRows, keys = p.tc ? 128 : kTileKeys;
-    const int64_t row_tiles = (a.Tq * group + rows - 1) / rows;
-    const int64_t ctas = (row_tiles > a.B ? row_tiles : a.B) * (a.heads / group), tiles = a.Tk / a.B / keys;
-    int64_t n = (p.tc ? 1 : 3) * a.num_sms / ctas;
+    const int64_t tiles = a.Tk / a.B / keys;
+    int64_t n = (p.tc ? 1 : 3) * a.num_sms / ctas(p.log_rows);
     if (n > tiles / 2) n = tiles / 2;
     if (n > 64) n = 64;
     p.splits = (int)(n < 1 ? 1 : n);
@@ -251,12 +318,12 @@ Plan plan_of(const AttendArgs& a) {
 }
 
 template <class T, int DH>
-cudaError_t run(const AttendArgs& a, const AttendOut& o, int splits, float* part_out, float* part_lse, cudaStream_t s) {
+cudaError_t run(const AttendArgs& a, const AttendOut& o, const Plan& p, float* part_out, float* part_lse, cudaStream_t s) {
     constexpr size_t smem = WarpTiles<T, DH>::kSmem;
     const cudaError_t e = allow_smem(k_attend<T, DH>, smem);
     if (e != cudaSuccess) return e;
-    const dim3 grid((unsigned)slots(a.Tq, a.B, a.group, kTileRows), (unsigned)a.kv_heads, (unsigned)splits);
-    return launch_next(k_attend<T, DH>, grid, dim3(128), smem, false, s, a, o, splits, part_out, part_lse);
+    const dim3 grid((unsigned)slots(a.Tq, a.B, a.group, p.log_rows), (unsigned)a.kv_heads, (unsigned)p.splits);
+    return launch_next(k_attend<T, DH>, grid, dim3(kWarps * 32), smem, false, s, a, o, p.log_rows, p.splits, part_out, part_lse);
 }
 
 }  // namespace
@@ -276,9 +343,9 @@ cudaError_t launch_attend(const AttendArgs& a, const AttendOut& o, uint8_t* work
     auto go = [&](auto t) {
         using T = decltype(t);
         const cudaError_t e = p.tc           ? launch_attend_tc(a, o, p.pack, p.splits, part_out, part_lse, s)
-                              : a.dh <= 32 ? run<T, 32>(a, o, p.splits, part_out, part_lse, s)
-                              : a.dh <= 64 ? run<T, 64>(a, o, p.splits, part_out, part_lse, s)
-                                           : run<T, 128>(a, o, p.splits, part_out, part_lse, s);
+                              : a.dh <= 32 ? run<T, 32>(a, o, p, part_out, part_lse, s)
+                              : a.dh <= 64 ? run<T, 64>(a, o, p, part_out, part_lse, s)
+                                           : run<T, 128>(a, o, p, part_out, part_lse, s);
         if (e != cudaSuccess || p.splits == 1 || a.Tq == 0) return e;
         return launch_next(k_attend_join<T>, dim3((unsigned)((a.Tq * a.heads + 7) / 8)), dim3(256), 0, true, s, a, o, p.splits,
                            (const float*)part_out, (const float*)part_lse);

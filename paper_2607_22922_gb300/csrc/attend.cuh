@@ -52,37 +52,54 @@ __device__ __forceinline__ Span span_of(const int64_t* __restrict__ offsets, int
     return {lo, hi > lo ? hi - lo : 0};
 }
 
-// Tiles of `per` rows (`group` a token) of all sequences, without their lengths on the
-// host: sequence b has the slots from tokens-before(b) group / per + b on, one more at
+// Tiles of 2^log rows (`group` a token) of all sequences, without their lengths on the
+// host: sequence b has the slots from tokens-before(b) group / 2^log + b on, one more at
 // least than its full tiles, so that slots(T, ...) of them hold every tile and one per
 // sequence.  A warp finds a slot's sequence by 32 probes at a time.
 struct Slot {
     int64_t b, tile;
 };
-__device__ __forceinline__ int64_t first_slot(const int64_t* offsets, int64_t b, int64_t B, int64_t T, int group, int per) {
-    return place(offsets, b, B, T) * group / per + b;
+__device__ __forceinline__ int64_t first_slot(const int64_t* offsets, int64_t b, int64_t B, int64_t T, int group, int log) {
+    return ((place(offsets, b, B, T) * group) >> log) + b;
 }
-__device__ __forceinline__ Slot slot_of(const int64_t* __restrict__ offsets, int64_t B, int64_t T, int group, int per, int64_t slot) {
+__device__ __forceinline__ Slot slot_of(const int64_t* __restrict__ offsets, int64_t B, int64_t T, int group, int log, int64_t slot) {
     const int lane = threadIdx.x & 31;
-    int64_t lo = 0, n = B;       // the sequence is in lo .. lo + n - 1
+    uint32_t lo = 0, n = (uint32_t)B;       // the sequence is in lo .. lo + n - 1
     while (n > 1) {
-        const int64_t step = (n + 31) / 32, i = lane * step;
-        const bool before = i < n && (lane == 0 || first_slot(offsets, lo + i, B, T, group, per) <= slot);
-        const int last = 31 - __clz((int)__ballot_sync(0xFFFFFFFFu, before));
-        lo += last * step;
-        n = n - last * step < step ? n - last * step : step;
+        const uint32_t step = (n + 31) / 32, i = lane * step;
+        const bool before = i < n && (lane == 0 || first_slot(offsets, lo + i, B, T, group, log) <= slot);
+        const uint32_t last = (31 - __clz((int)__ballot_sync(0xFFFFFFFFu, before))) * step;
+        lo += last;
+        n = n - last < step ? n - last : step;
     }
-    return {lo, slot - first_slot(offsets, lo, B, T, group, per)};
+    return {lo, slot - first_slot(offsets, lo, B, T, group, log)};
 }
-inline int64_t slots(int64_t T, int64_t B, int group, int per) { return T * group / per + B; }
+inline int64_t slots(int64_t T, int64_t B, int group, int log) { return ((T * group) >> log) + B; }
 
-// A row of a group's matrix: its token and head
+// Rows of a group's matrix from row `first` on: row i is token `token` + at(i).x, head
+// at(i).y of the group.  Division by the group's size is a product with its inverse: exact
+// below 2^22, and rows here are counted within a tile.
 struct RowOf {
-    int64_t token;      // of the tile's first row
-    int sub, group;
-    __device__ __forceinline__ RowOf(int64_t first, int group_) : token(first / group_), sub((int)(first % group_)), group(group_) {}
-    __device__ __forceinline__ int64_t token_of(int i) const { return token + (group == 1 ? i : (sub + i) / group); }
-    __device__ __forceinline__ int head_of(int i) const { return group == 1 ? 0 : (sub + i) % group; }
+    int64_t token;
+    uint32_t sub, group, inverse;
+    __device__ __forceinline__ RowOf(int64_t first, int group_)
+        : group((uint32_t)group_), inverse(0xFFFFFFFFu / (uint32_t)group_ + 1u) {
+        // a division of 64 bits takes a hundred instructions
+        token = first >> 32 ? first / group_ : (int64_t)((uint32_t)first / group);
+        sub = (uint32_t)(first - token * group_);
+    }
+    __device__ __forceinline__ int2 at(int i) const {
+        const uint32_t x = sub + (uint32_t)i, t = group == 1 ? x : __umulhi(x, inverse);
+        return make_int2((int)t, (int)(x - t * group));
+    }
+};
+// Where such rows lie: `ld` elements from token to token, dh from head to head
+template <class T>
+struct RowsAt {
+    T* first;        // of the tile's first token, the group's first head
+    int ld, dh;
+    __device__ __forceinline__ RowsAt(T* p, int64_t token, int64_t ld_, int dh_) : first(p + token * ld_), ld((int)ld_), dh(dh_) {}
+    __device__ __forceinline__ T* operator()(int2 at) const { return first + (int64_t)at.x * ld + at.y * dh; }
 };
 
 __device__ __forceinline__ float ex2(float x) {
@@ -160,7 +177,7 @@ struct Rows {
     }
 };
 
-constexpr int kTileRows = 64, kTileKeys = 64;
+constexpr int kTileRows = 64, kTileKeys = 64, kTileLog = 6;
 
 // Copies rows of a tile into shared memory: row(i) is row i's address, or null for zeros;
 // dims dh .. DH - 1 are zeros.  any: an address of global memory, not read.

@@ -13,93 +13,137 @@ namespace ifvs {
 
 namespace {
 
-// The two scores of a warp's 16 rows and the tile's keys: a = rows of `qa` times keys
-// `kb`, accumulated over DH.
+using Scores = float2[kTileKeys / 8][2];       // of rows lane / 4 and + 8, keys 8 j + lane % 4 * 2 and the next
+using Operands = uint32_t[kTileKeys / 16][4];    // 16 rows x 64 keys as operand A
+
+// A warp's 16 rows from `row` on times the tile's keys, over DH; `blocks` of 16 keys.  bias:
+// where a key's sums begin, or null: 0
 template <class T, int DH>
-__device__ __forceinline__ void scores(float (&s)[kTileKeys / 8][4], const Rows<DH>& q, int row, const Rows<DH>& k) {
+__device__ __forceinline__ void scores(Scores& s, const Rows<DH>& q, int row, const Rows<DH>& k, int blocks, const float* bias) {
 #pragma unroll
     for (int j = 0; j < kTileKeys / 8; ++j)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) s[j][i] = 0.f;
+        s[j][0] = s[j][1] = bias ? *reinterpret_cast<const float2*>(bias + j * 8 + (threadIdx.x & 3) * 2) : make_float2(0.f, 0.f);
 #pragma unroll
     for (int d = 0; d < DH / 16; ++d) {
         uint32_t f[4];
         q.a(f, row, d * 16);
 #pragma unroll
-        for (int j = 0; j < kTileKeys / 16; ++j) {
-            uint32_t b[4];
-            k.b_t(b, j * 16, d * 16);
-            mma16816<T>(s[2 * j], f, b[0], b[1]);
-            mma16816<T>(s[2 * j + 1], f, b[2], b[3]);
-        }
+        for (int j = 0; j < kTileKeys / 16; ++j)
+            if (j < blocks) {
+                uint32_t b[4];
+                k.b_t(b, j * 16, d * 16);
+                mma16816<T>(reinterpret_cast<float(&)[4]>(s[2 * j]), f, b[0], b[1]);
+                mma16816<T>(reinterpret_cast<float(&)[4]>(s[2 * j + 1]), f, b[2], b[3]);
+            }
     }
 }
 
-__device__ __forceinline__ bool bit(uint32_t lo, uint32_t hi, int key) { return ((key < 32 ? lo : hi) >> (key & 31)) & 1u; }
+__device__ __forceinline__ float2 both2(float v) { return make_float2(v, v); }
 
-// p and ds of a warp's rows from the scores s and dp, in their places.  lse2: base-2
-// log-sum-exp, -infinity for a row that does not count.
-template <class T>
-__device__ __forceinline__ void slopes(float (&s)[kTileKeys / 8][4], float (&dp)[kTileKeys / 8][4], const float (&lse2)[2],
-                                       const float (&delta)[2], float c, uint32_t lo, uint32_t hi) {
-    const int two = (threadIdx.x & 3) * 2;
+// p and ds of a warp's rows from the scores s and dp, in their places.  lse2: base 2,
+// infinite for a row without keys.
+__device__ __forceinline__ void slopes(Scores& s, Scores& dp, const float (&lse2)[2], const float (&delta)[2], float c, int blocks) {
 #pragma unroll
     for (int j = 0; j < kTileKeys / 8; ++j)
+        if (j / 2 < blocks)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const bool in = bit(lo, hi, j * 8 + two + (i & 1)) && lse2[i >> 1] != -INFINITY;
-            const float p = in ? ex2(fmaf(s[j][i], c, -lse2[i >> 1])) : 0.f;
-            dp[j][i] = in ? p * (dp[j][i] - delta[i >> 1]) : 0.f;
-            s[j][i] = p;
-        }
+            for (int r = 0; r < 2; ++r) {
+                float2 e = fma_(s[j][r], both2(c), both2(-lse2[r]));
+                e.x = ex2(e.x);
+                e.y = ex2(e.y);
+                s[j][r] = e;
+                dp[j][r] = mul_(e, add_(dp[j][r], both2(-delta[r])));
+            }
 }
-
-// acc += x y: x [16 rows][64 keys] in registers, y the keys' rows
-template <class T, int DH>
-__device__ __forceinline__ void times_keys(float (&acc)[DH / 8][4], const float (&x)[kTileKeys / 8][4], const Rows<DH>& y) {
+// The same where the tile has all of the rows' keys
+__device__ __forceinline__ void slopes_alone(Scores& s, Scores& dp, float c, int blocks) {
 #pragma unroll
-    for (int j = 0; j < kTileKeys / 16; ++j) {
-        uint32_t f[4];
+    for (int r = 0; r < 2; ++r) {
+        float top = fmaxf(s[0][r].x, s[0][r].y);
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            f[i] = pack2(make_float2(x[2 * j + (i >> 1)][(i & 1) * 2], x[2 * j + (i >> 1)][(i & 1) * 2 + 1]), T());
+        for (int j = 1; j < kTileKeys / 8; ++j) top = fmaxf(top, fmaxf(s[j][r].x, s[j][r].y));
+        top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
+        top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2)) * c;
+        const float base = top == -INFINITY ? 0.f : top;
+        float2 l2 = both2(0.f), sum2 = l2;
 #pragma unroll
-        for (int d = 0; d < DH / 16; ++d) {
-            uint32_t b[4];
-            y.b(b, j * 16, d * 16);
-            mma16816<T>(acc[2 * d], f, b[0], b[1]);
-            mma16816<T>(acc[2 * d + 1], f, b[2], b[3]);
+        for (int j = 0; j < kTileKeys / 8; ++j)
+            if (j / 2 < blocks) {
+                float2 e = fma_(s[j][r], both2(c), both2(-base));
+                e.x = ex2(e.x);
+                e.y = ex2(e.y);
+                s[j][r] = e;
+                l2 = add_(l2, e);
+                sum2 = fma_(e, dp[j][r], sum2);
+            }
+        float l = total(l2), sum = total(sum2);
+#pragma unroll
+        for (int x = 1; x <= 2; x <<= 1) {
+            l += __shfl_xor_sync(0xFFFFFFFFu, l, x);
+            sum += __shfl_xor_sync(0xFFFFFFFFu, sum, x);
         }
+        const float inv = l == 0.f ? 0.f : 1.f / l, delta = sum * inv;
+#pragma unroll
+        for (int j = 0; j < kTileKeys / 8; ++j)
+            if (j / 2 < blocks) {
+                s[j][r] = mul_(s[j][r], both2(inv));
+                dp[j][r] = mul_(s[j][r], add_(dp[j][r], both2(-delta)));
+            }
     }
 }
 
-// acc += x^T y: 16 of x's columns (keys) from `key`, x [64 rows][64 keys] and y [64 rows] in
-// shared memory
+template <class T>
+__device__ __forceinline__ void to_operands(Operands& f, const Scores& x) {
+#pragma unroll
+    for (int j = 0; j < kTileKeys / 16; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            f[j][i] = pack2(x[2 * j + (i >> 1)][i & 1], T());
+}
+
+// acc += x y: y the keys' rows
 template <class T, int DH>
-__device__ __forceinline__ void transposed_times(float (&acc)[DH / 8][4], const Rows<kTileKeys>& x, int key, const Rows<DH>& y) {
+__device__ __forceinline__ void times_keys(float (&acc)[DH / 8][4], const Operands& x, const Rows<DH>& y, int blocks) {
+#pragma unroll
+    for (int j = 0; j < kTileKeys / 16; ++j)
+        if (j < blocks)
+#pragma unroll
+            for (int d = 0; d < DH / 16; ++d) {
+                uint32_t b[4];
+                y.b(b, j * 16, d * 16);
+                mma16816<T>(acc[2 * d], x[j], b[0], b[1]);
+                mma16816<T>(acc[2 * d + 1], x[j], b[2], b[3]);
+            }
+}
+
+// acc += x^T y, its columns 16 d0 .. 16 d1 - 1: 16 of x's columns (keys) from `key`, x [64
+// rows][64 keys] and y [64 rows] in shared memory
+template <class T, int DH>
+__device__ __forceinline__ void transposed_times(float (&acc)[DH / 8][4], const Rows<kTileKeys>& x, int key, const Rows<DH>& y, int d0,
+                                                 int d1) {
 #pragma unroll
     for (int r = 0; r < kTileRows / 16; ++r) {
         uint32_t f[4];
         x.a_t(f, r * 16, key);
 #pragma unroll
-        for (int d = 0; d < DH / 16; ++d) {
-            uint32_t b[4];
-            y.b(b, r * 16, d * 16);
-            mma16816<T>(acc[2 * d], f, b[0], b[1]);
-            mma16816<T>(acc[2 * d + 1], f, b[2], b[3]);
-        }
+        for (int d = 0; d < DH / 16; ++d)
+            if (d >= d0 && d < d1) {
+                uint32_t b[4];
+                y.b(b, r * 16, d * 16);
+                mma16816<T>(acc[2 * d], f, b[0], b[1]);
+                mma16816<T>(acc[2 * d + 1], f, b[2], b[3]);
+            }
     }
 }
 
-template <class T>
-__device__ __forceinline__ void put_scores(const Rows<kTileKeys>& to, int row, const float (&x)[kTileKeys / 8][4]) {
+__device__ __forceinline__ void put_scores(const Rows<kTileKeys>& to, int row, const Operands& x) {
     const int lane = threadIdx.x & 31;
 #pragma unroll
-    for (int r = 0; r < 2; ++r)
+    for (int j = 0; j < kTileKeys / 16; ++j)
 #pragma unroll
-        for (int j = 0; j < kTileKeys / 8; ++j)
-            asm volatile("st.shared.b32 [%0], %1;" ::"r"(to.addr(row + (lane >> 2) + 8 * r, j * 8 + (lane & 3) * 2)),
-                         "r"(pack2(make_float2(x[j][2 * r], x[j][2 * r + 1]), T()))
+        for (int i = 0; i < 4; ++i)
+            asm volatile("st.shared.b32 [%0], %1;" ::"r"(to.addr(row + (lane >> 2) + 8 * (i & 1), j * 16 + (i >> 1) * 8 + (lane & 3) * 2)),
+                         "r"(x[j][i])
                          : "memory");
 }
 
@@ -134,24 +178,28 @@ __device__ __forceinline__ void row_terms(float (&lse2)[2], float (&delta)[2], c
     for (int r = 0; r < 2; ++r) {
         const int i = (lane >> 2) + 8 * r;
         delta[r] = __shfl_sync(0xFFFFFFFFu, v, i * 2);
-        lse2[r] = row + i < rows ? lse(row + i) * kLog2e : -INFINITY;
+        const float l = row + i < rows ? lse(row + i) : -INFINITY;
+        lse2[r] = l == -INFINITY ? INFINITY : l * kLog2e;
     }
 }
 
-// Stores a warp's 16 rows from registers, scaled
-template <class T, int DH, class Row>
-__device__ __forceinline__ void put_rows(const float (&acc)[DH / 8][4], float scale, int rows, int dh, const Row& to) {
+// Stores a warp's 16 rows from registers, scaled; columns 16 d0 .. 16 d1 - 1.  to(i): row i
+// of them.  counts(i): false for a row of zeros.
+template <class T, int DH, class Row, class Counts>
+__device__ __forceinline__ void put_rows(const float (&acc)[DH / 8][4], float scale, int rows, int dh, int d0, int d1, const Row& to,
+                                         const Counts& counts) {
     const int lane = threadIdx.x & 31;
 #pragma unroll
     for (int r = 0; r < 2; ++r) {
         const int i = (lane >> 2) + 8 * r;
         if (i >= rows) continue;
-        T* p = to(i);
+        T* p = to(i) + (lane & 3) * 2;
+        const bool in = counts(i);
 #pragma unroll
         for (int j = 0; j < DH / 8; ++j)
-            if (j * 8 < dh)
-                *reinterpret_cast<uint32_t*>(p + j * 8 + (lane & 3) * 2) =
-                    pack2(make_float2(acc[j][2 * r] * scale, acc[j][2 * r + 1] * scale), T());
+            if (j * 8 < dh && j / 2 >= d0 && j / 2 < d1)
+                *reinterpret_cast<uint32_t*>(p + j * 8) =
+                    in ? pack2(make_float2(acc[j][2 * r] * scale, acc[j][2 * r + 1] * scale), T()) : 0u;
     }
 }
 
@@ -174,141 +222,144 @@ struct Arrays {
 };
 
 // ---- dk and dv, and dq of sequences whose keys are one tile ---------------------------------
-// A CTA takes 64 keys and one part of the rows of their group, 64 at a time: each of its 4
-// warps makes p and ds of 16 rows, then adds 16 keys' sums over the 64 rows.
+// A CTA takes 64 keys and one part of the rows of their group, 64 at a time with the next
+// on their way: each of its 4 warps makes p and ds of 16 rows, then adds 16 keys' sums over
+// the 64 rows (a share of the columns for fewer keys).  Blocks of 16 keys behind the last are
+// left out.
 template <class T, int DH>
 struct KeyTiles {
-    Rows<DH> k, v, q, d_out;
+    Rows<DH> k, v, q[2], d_out[2];
     Rows<kTileKeys> p, ds;
     static constexpr uint32_t kBytes = Rows<DH>::kLd * 2 * 64;
-    static constexpr size_t kSmem = 4 * kBytes + 2 * kTileRows * Rows<kTileKeys>::kLd * 2;
+    static constexpr size_t kSmem = 6 * kBytes + 2 * kTileRows * Rows<kTileKeys>::kLd * 2;
 };
 
 template <class T, int DH>
-__global__ void __launch_bounds__(128) k_attend_keys(AttendArgs a, AttendGrads g, int splits, float* part_dk, float* part_dv) {
+__global__ void __launch_bounds__(128, DH == 128 ? 2 : 3) k_attend_keys(AttendArgs a, AttendGrads g, int splits, float* part_dk, float* part_dv) {
     extern __shared__ __align__(16) uint8_t raw[];
+    __shared__ __align__(8) float bias[kTileKeys];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, hk = blockIdx.y, split = blockIdx.z;
     check_offsets(a.q_offsets, a.B, a.Tq, a.waits.err);
     check_offsets(a.kv_offsets, a.B, a.Tk, a.waits.err);
-    const Slot slot = slot_of(a.kv_offsets, a.B, a.Tk, 1, kTileKeys, blockIdx.x);
+    const Slot slot = slot_of(a.kv_offsets, a.B, a.Tk, 1, kTileLog, blockIdx.x);
     const Span qs = span_of(a.q_offsets, slot.b, a.B, a.Tq), ks = span_of(a.kv_offsets, slot.b, a.B, a.Tk);
     const int64_t key0 = slot.tile * kTileKeys;
     // without keys the first tile still writes dq
     if (slot.tile < 0 || (key0 >= ks.len && slot.tile > 0)) return;
     const bool alone = ks.len <= kTileKeys;
-    const int keys = ks.len - key0 < kTileKeys ? (int)(ks.len - key0) : kTileKeys;
+    const int keys = ks.len - key0 < kTileKeys ? (int)(ks.len - key0) : kTileKeys, blocks = (keys + 15) / 16;
     const Arrays<T> at(a, g, hk);
+    const int64_t n_rows = qs.len * a.group, tiles = (n_rows + kTileRows - 1) / kTileRows;
+    const int64_t t0 = tiles * split / splits, t1 = tiles * (split + 1) / splits;
 
     KeyTiles<T, DH> sm;
-    sm.k.at = smem32(raw);
-    sm.v.at = sm.k.at + sm.kBytes;
-    sm.q.at = sm.v.at + sm.kBytes;
-    sm.d_out.at = sm.q.at + sm.kBytes;
-    sm.p.at = sm.d_out.at + sm.kBytes;
+    const uint32_t base = smem32(raw);
+    sm.k.at = base;
+    sm.v.at = base + sm.kBytes;
+    auto q_of = [&](int stage) { return Rows<DH>{base + (2 + 2 * stage) * sm.kBytes}; };
+    auto do_of = [&](int stage) { return Rows<DH>{base + (3 + 2 * stage) * sm.kBytes}; };
+    sm.p.at = base + 6 * sm.kBytes;
     sm.ds.at = sm.p.at + kTileRows * Rows<kTileKeys>::kLd * 2;
+    auto load_queries = [&](int64_t t, int stage) {
+        const int64_t row0 = t * kTileRows;
+        const int rows = n_rows - row0 < kTileRows ? (int)(n_rows - row0) : kTileRows;
+        const RowOf ro(row0, a.group);
+        const RowsAt<const T> q(at.q, qs.at + ro.token, a.ld_q, a.dh), d_out(at.d_out, qs.at + ro.token, g.ld_d_out, a.dh);
+        load_rows<DH, T>(q_of(stage), kTileRows, a.dh, a.q, [&](int i) { return i < rows ? q(ro.at(i)) : nullptr; });
+        load_rows<DH, T>(do_of(stage), kTileRows, a.dh, a.q, [&](int i) { return i < rows ? d_out(ro.at(i)) : nullptr; });
+    };
     auto key_in = [&](int i) { return i < keys && (a.kv_ids == nullptr || __ldg(a.kv_ids + ks.at + key0 + i) >= 0); };
-    load_rows<DH, T>(sm.k, kTileKeys, a.dh, a.q, [&](int i) { return key_in(i) ? at.k + (ks.at + key0 + i) * a.ld_k : nullptr; });
-    load_rows<DH, T>(sm.v, kTileKeys, a.dh, a.q, [&](int i) { return key_in(i) ? at.v + (ks.at + key0 + i) * a.ld_v : nullptr; });
-    const uint32_t lo = __ballot_sync(0xFFFFFFFFu, key_in(lane)), hi = __ballot_sync(0xFFFFFFFFu, key_in(32 + lane));
+    if (t0 < t1) load_queries(t0, 0);
+    load_rows<DH, T>(sm.k, blocks * 16, a.dh, a.q, [&](int i) { return key_in(i) ? at.k + (ks.at + key0 + i) * a.ld_k : nullptr; });
+    load_rows<DH, T>(sm.v, blocks * 16, a.dh, a.q, [&](int i) { return key_in(i) ? at.v + (ks.at + key0 + i) * a.ld_v : nullptr; });
+    copies_done();
+    if (threadIdx.x < kTileKeys) bias[threadIdx.x] = key_in(threadIdx.x) ? 0.f : -INFINITY;
     const float c = a.scale * kLog2e;
+    // this warp's share of dk and dv: 16 keys, columns 16 d0 .. 16 d1 - 1
+    const int shares = blocks == 1 ? 4 : blocks == 2 ? 2 : 1, block = warp / shares, d0 = warp % shares * (DH / 16) / shares,
+              d1 = (warp % shares + 1) * (DH / 16) / shares;
 
     float dk[DH / 8][4], dv[DH / 8][4];
 #pragma unroll
     for (int j = 0; j < DH / 8; ++j)
 #pragma unroll
         for (int i = 0; i < 4; ++i) dk[j][i] = dv[j][i] = 0.f;
-    const int64_t n_rows = qs.len * a.group, tiles = (n_rows + kTileRows - 1) / kTileRows;
-    const int64_t t0 = tiles * split / splits, t1 = tiles * (split + 1) / splits;
     for (int64_t t = t0; t < t1; ++t) {
+        const int stage = (int)(t - t0) & 1;
         const int64_t row0 = t * kTileRows;
         const int rows = n_rows - row0 < kTileRows ? (int)(n_rows - row0) : kTileRows;
         const RowOf ro(row0, a.group);
-        auto token = [&](int i) { return qs.at + ro.token_of(i); };
-        auto head = [&](int i) { return (int64_t)ro.head_of(i) * a.dh; };
-        load_rows<DH, T>(sm.q, kTileRows, a.dh, a.q, [&](int i) { return i < rows ? at.q + token(i) * a.ld_q + head(i) : nullptr; });
-        load_rows<DH, T>(sm.d_out, kTileRows, a.dh, a.q,
-                         [&](int i) { return i < rows ? at.d_out + token(i) * g.ld_d_out + head(i) : nullptr; });
+        const Rows<DH> sq = q_of(stage), sdo = do_of(stage);
+        if (t + 1 < t1) load_queries(t + 1, stage ^ 1);
         copies_done();
-        wait_copies<0>();
+        wait_copies<1>();
         __syncthreads();
-        {
-            float s[kTileKeys / 8][4], dp[kTileKeys / 8][4];
-            scores<T>(s, sm.q, warp * 16, sm.k);
-            scores<T>(dp, sm.d_out, warp * 16, sm.v);
-            float lse2[2], delta[2];
-            if (alone) {
-#pragma unroll
-                for (int r = 0; r < 2; ++r) {
-                    float top = -INFINITY;
-#pragma unroll
-                    for (int j = 0; j < kTileKeys / 8; ++j)
-#pragma unroll
-                        for (int i = 2 * r; i < 2 * r + 2; ++i)
-                            if (bit(lo, hi, j * 8 + (lane & 3) * 2 + (i & 1))) top = fmaxf(top, s[j][i]);
-                    top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
-                    top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2)) * c;
-                    const float base = top == -INFINITY ? 0.f : top;
-                    float l = 0.f, sum = 0.f;
-#pragma unroll
-                    for (int j = 0; j < kTileKeys / 8; ++j)
-#pragma unroll
-                        for (int i = 2 * r; i < 2 * r + 2; ++i)
-                            if (bit(lo, hi, j * 8 + (lane & 3) * 2 + (i & 1))) {
-                                const float e = ex2(fmaf(s[j][i], c, -base));
-                                l += e;
-                                sum = fmaf(e, dp[j][i], sum);
-                            }
-#pragma unroll
-                    for (int x = 1; x <= 2; x <<= 1) {
-                        l += __shfl_xor_sync(0xFFFFFFFFu, l, x);
-                        sum += __shfl_xor_sync(0xFFFFFFFFu, sum, x);
-                    }
-                    const bool in = warp * 16 + (lane >> 2) + 8 * r < rows && l != 0.f;
-                    lse2[r] = in ? base + log2f(l) : -INFINITY;
-                    delta[r] = in ? sum / l : 0.f;
+        if (warp * 16 < rows) {
+            Operands f;
+            {
+                Scores s, dp;
+                scores<T>(s, sq, warp * 16, sm.k, blocks, bias);
+                scores<T>(dp, sdo, warp * 16, sm.v, blocks, nullptr);
+                if (alone) {
+                    slopes_alone(s, dp, c, blocks);
+                } else {
+                    float lse2[2], delta[2];
+                    const RowsAt<const T> out(at.out, qs.at + ro.token, g.ld_out, a.dh);
+                    row_terms<T>(lse2, delta, sdo, warp * 16, rows, a.dh, [&](int i) { return i < rows ? out(ro.at(i)) : nullptr; },
+                                 [&](int i) {
+                                     const int2 r = ro.at(i);
+                                     return __ldg(g.lse + (qs.at + ro.token + r.x) * a.heads + hk * a.group + r.y);
+                                 });
+                    slopes(s, dp, lse2, delta, c, blocks);
                 }
-            } else {
-                row_terms<T>(lse2, delta, sm.d_out, warp * 16, rows, a.dh,
-                             [&](int i) { return i < rows ? at.out + token(i) * g.ld_out + head(i) : nullptr; },
-                             [&](int i) { return __ldg(g.lse + token(i) * a.heads + hk * a.group + ro.head_of(i)); });
+                to_operands<T>(f, s);
+                put_scores(sm.p, warp * 16, f);
+                to_operands<T>(f, dp);
+                put_scores(sm.ds, warp * 16, f);
             }
-            slopes<T>(s, dp, lse2, delta, c, lo, hi);
-            put_scores<T>(sm.p, warp * 16, s);
-            put_scores<T>(sm.ds, warp * 16, dp);
             if (alone) {
                 float dq[DH / 8][4];
 #pragma unroll
                 for (int j = 0; j < DH / 8; ++j)
 #pragma unroll
                     for (int i = 0; i < 4; ++i) dq[j][i] = 0.f;
-                times_keys<T, DH>(dq, dp, sm.k);
-                put_rows<T, DH>(dq, a.scale, rows - warp * 16, a.dh,
-                                [&](int i) { return at.dq + token(warp * 16 + i) * g.ld_dq + head(warp * 16 + i); });
+                times_keys<T, DH>(dq, f, sm.k, blocks);
+                const RowsAt<T> to(at.dq, qs.at + ro.token, g.ld_dq, a.dh);
+                put_rows<T, DH>(dq, a.scale, rows - warp * 16, a.dh, 0, DH / 16, [&](int i) { return to(ro.at(warp * 16 + i)); },
+                                [](int) { return true; });
             }
+        } else {                 // rows of zeros
+            const Operands f = {};
+            put_scores(sm.p, warp * 16, f);
+            put_scores(sm.ds, warp * 16, f);
         }
         __syncthreads();
-        transposed_times<T, DH>(dv, sm.p, warp * 16, sm.d_out);
-        transposed_times<T, DH>(dk, sm.ds, warp * 16, sm.q);
+        if (block < blocks) {
+            transposed_times<T, DH>(dv, sm.p, block * 16, sdo, d0, d1);
+            transposed_times<T, DH>(dk, sm.ds, block * 16, sq, d0, d1);
+        }
         __syncthreads();
     }
-    copies_done();
     wait_copies<0>();
-    const int mine = keys - warp * 16;
+    const int mine = keys - block * 16;
     if (splits == 1) {
-        put_rows<T, DH>(dk, a.scale, mine, a.dh, [&](int i) { return at.dk + (ks.at + key0 + warp * 16 + i) * g.ld_dk; });
-        put_rows<T, DH>(dv, 1.f, mine, a.dh, [&](int i) { return at.dv + (ks.at + key0 + warp * 16 + i) * g.ld_dv; });
+        auto counts = [&](int i) { return bias[block * 16 + i] == 0.f; };
+        put_rows<T, DH>(dk, a.scale, mine, a.dh, d0, d1, [&](int i) { return at.dk + (ks.at + key0 + block * 16 + i) * g.ld_dk; }, counts);
+        put_rows<T, DH>(dv, 1.f, mine, a.dh, d0, d1, [&](int i) { return at.dv + (ks.at + key0 + block * 16 + i) * g.ld_dv; }, counts);
         return;
     }
 #pragma unroll
     for (int r = 0; r < 2; ++r) {
         const int i = (lane >> 2) + 8 * r;
         if (i >= mine) continue;
-        const int64_t to = (((int64_t)split * a.Tk + ks.at + key0 + warp * 16 + i) * a.kv_heads + hk) * a.dh + (lane & 3) * 2;
+        const int64_t to = (((int64_t)split * a.Tk + ks.at + key0 + block * 16 + i) * a.kv_heads + hk) * a.dh + (lane & 3) * 2;
+        const bool in = bias[block * 16 + i] == 0.f;
 #pragma unroll
         for (int j = 0; j < DH / 8; ++j)
-            if (j * 8 < a.dh) {
-                *reinterpret_cast<float2*>(part_dk + to + j * 8) = make_float2(dk[j][2 * r] * a.scale, dk[j][2 * r + 1] * a.scale);
-                *reinterpret_cast<float2*>(part_dv + to + j * 8) = make_float2(dv[j][2 * r], dv[j][2 * r + 1]);
+            if (j * 8 < a.dh && j / 2 >= d0 && j / 2 < d1) {
+                *reinterpret_cast<float2*>(part_dk + to + j * 8) =
+                    in ? make_float2(dk[j][2 * r] * a.scale, dk[j][2 * r + 1] * a.scale) : both2(0.f);
+                *reinterpret_cast<float2*>(part_dv + to + j * 8) = in ? make_float2(dv[j][2 * r], dv[j][2 * r + 1]) : both2(0.f);
             }
     }
 }
@@ -335,72 +386,81 @@ __global__ void __launch_bounds__(256) k_attend_keys_join(AttendArgs a, AttendGr
 }
 
 // ---- dq of sequences with more keys than a tile ----------------------------------------------
+// A CTA takes slots of 64 rows by turns, since most may have nothing to do.
 template <class T, int DH>
 struct RowTiles {
-    Rows<DH> q, d_out, k[2], v[2];
     static constexpr uint32_t kBytes = Rows<DH>::kLd * 2 * 64;
     static constexpr size_t kSmem = 6 * kBytes;
 };
 
 template <class T, int DH>
-__global__ void __launch_bounds__(128) k_attend_rows(AttendArgs a, AttendGrads g) {
+__global__ void __launch_bounds__(128, DH == 128 ? 2 : 3) k_attend_rows(AttendArgs a, AttendGrads g, int64_t n_slots) {
     extern __shared__ __align__(16) uint8_t raw[];
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, hk = blockIdx.y;
-    const Slot slot = slot_of(a.q_offsets, a.B, a.Tq, a.group, kTileRows, blockIdx.x);
-    const Span qs = span_of(a.q_offsets, slot.b, a.B, a.Tq), ks = span_of(a.kv_offsets, slot.b, a.B, a.Tk);
-    const int64_t row0 = slot.tile * kTileRows, left = qs.len * a.group - row0;
-    if (slot.tile < 0 || left <= 0 || ks.len <= kTileKeys) return;
-    const int rows = left < kTileRows ? (int)left : kTileRows;
-    const RowOf ro(row0, a.group);
+    __shared__ __align__(8) float bias[2][kTileKeys];
+    const int warp = threadIdx.x >> 5, hk = blockIdx.y;
+    const uint32_t base = smem32(raw);
+    constexpr uint32_t kBytes = RowTiles<T, DH>::kBytes;
+    const Rows<DH> sq{base}, sdo{base + kBytes};
+    auto k_of = [&](int stage) { return Rows<DH>{base + (2 + 2 * stage) * kBytes}; };
+    auto v_of = [&](int stage) { return Rows<DH>{base + (3 + 2 * stage) * kBytes}; };
     const Arrays<T> at(a, g, hk);
-    auto token = [&](int i) { return qs.at + ro.token_of(i); };
-    auto head = [&](int i) { return (int64_t)ro.head_of(i) * a.dh; };
-    RowTiles<T, DH> sm;
-    sm.q.at = smem32(raw);
-    sm.d_out.at = sm.q.at + sm.kBytes;
-    for (int i = 0; i < 2; ++i) {
-        sm.k[i].at = sm.q.at + (2 + 2 * i) * sm.kBytes;
-        sm.v[i].at = sm.k[i].at + sm.kBytes;
-    }
-    load_rows<DH, T>(sm.q, kTileRows, a.dh, a.q, [&](int i) { return i < rows ? at.q + token(i) * a.ld_q + head(i) : nullptr; });
-    load_rows<DH, T>(sm.d_out, kTileRows, a.dh, a.q,
-                     [&](int i) { return i < rows ? at.d_out + token(i) * g.ld_d_out + head(i) : nullptr; });
-    auto key_in = [&](int64_t key) { return key < ks.len && (a.kv_ids == nullptr || __ldg(a.kv_ids + ks.at + key) >= 0); };
-    auto load_keys = [&](int64_t tile, int stage) {
-        const int64_t key0 = tile * kTileKeys;
-        load_rows<DH, T>(sm.k[stage], kTileKeys, a.dh, a.q, [&](int i) { return key_in(key0 + i) ? at.k + (ks.at + key0 + i) * a.ld_k : nullptr; });
-        load_rows<DH, T>(sm.v[stage], kTileKeys, a.dh, a.q, [&](int i) { return key_in(key0 + i) ? at.v + (ks.at + key0 + i) * a.ld_v : nullptr; });
-    };
-    const int64_t tiles = (ks.len + kTileKeys - 1) / kTileKeys;
-    load_keys(0, 0);
-    copies_done();
-    float dq[DH / 8][4], lse2[2] = {}, delta[2] = {};
-#pragma unroll
-    for (int j = 0; j < DH / 8; ++j)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) dq[j][i] = 0.f;
     const float c = a.scale * kLog2e;
-    for (int64_t t = 0; t < tiles; ++t) {
-        const int stage = (int)t & 1;
-        if (t + 1 < tiles) load_keys(t + 1, stage ^ 1);
+    for (int64_t n = blockIdx.x; n < n_slots; n += gridDim.x) {
+        const Slot slot = slot_of(a.q_offsets, a.B, a.Tq, a.group, kTileLog, n);
+        const Span qs = span_of(a.q_offsets, slot.b, a.B, a.Tq), ks = span_of(a.kv_offsets, slot.b, a.B, a.Tk);
+        const int64_t row0 = slot.tile * kTileRows, left = qs.len * a.group - row0;
+        if (slot.tile < 0 || left <= 0 || ks.len <= kTileKeys) continue;
+        const int rows = left < kTileRows ? (int)left : kTileRows;
+        const RowOf ro(row0, a.group);
+        const RowsAt<const T> q(at.q, qs.at + ro.token, a.ld_q, a.dh), d_out(at.d_out, qs.at + ro.token, g.ld_d_out, a.dh),
+            out(at.out, qs.at + ro.token, g.ld_out, a.dh);
+        load_rows<DH, T>(sq, kTileRows, a.dh, a.q, [&](int i) { return i < rows ? q(ro.at(i)) : nullptr; });
+        load_rows<DH, T>(sdo, kTileRows, a.dh, a.q, [&](int i) { return i < rows ? d_out(ro.at(i)) : nullptr; });
+        auto key_in = [&](int64_t key) { return key < ks.len && (a.kv_ids == nullptr || __ldg(a.kv_ids + ks.at + key) >= 0); };
+        auto load_keys = [&](int64_t tile, int stage) {
+            const int64_t key0 = tile * kTileKeys;
+            load_rows<DH, T>(k_of(stage), kTileKeys, a.dh, a.q,
+                             [&](int i) { return key_in(key0 + i) ? at.k + (ks.at + key0 + i) * a.ld_k : nullptr; });
+            load_rows<DH, T>(v_of(stage), kTileKeys, a.dh, a.q,
+                             [&](int i) { return key_in(key0 + i) ? at.v + (ks.at + key0 + i) * a.ld_v : nullptr; });
+            if (threadIdx.x < kTileKeys) bias[stage][threadIdx.x] = key_in(key0 + threadIdx.x) ? 0.f : -INFINITY;
+        };
+        const int64_t tiles = (ks.len + kTileKeys - 1) / kTileKeys;
+        load_keys(0, 0);
         copies_done();
-        wait_copies<1>();
-        __syncthreads();
-        if (t == 0)
-            row_terms<T>(lse2, delta, sm.d_out, warp * 16, rows, a.dh,
-                         [&](int i) { return i < rows ? at.out + token(i) * g.ld_out + head(i) : nullptr; },
-                         [&](int i) { return __ldg(g.lse + token(i) * a.heads + hk * a.group + ro.head_of(i)); });
-        const uint32_t lo = __ballot_sync(0xFFFFFFFFu, key_in(t * kTileKeys + lane)),
-                       hi = __ballot_sync(0xFFFFFFFFu, key_in(t * kTileKeys + 32 + lane));
-        float s[kTileKeys / 8][4], dp[kTileKeys / 8][4];
-        scores<T>(s, sm.q, warp * 16, sm.k[stage]);
-        scores<T>(dp, sm.d_out, warp * 16, sm.v[stage]);
-        slopes<T>(s, dp, lse2, delta, c, lo, hi);
-        times_keys<T, DH>(dq, dp, sm.k[stage]);
-        __syncthreads();
+        float dq[DH / 8][4], lse2[2] = {}, delta[2] = {};
+#pragma unroll
+        for (int j = 0; j < DH / 8; ++j)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) dq[j][i] = 0.f;
+        for (int64_t t = 0; t < tiles; ++t) {
+            const int stage = (int)t & 1;
+            if (t + 1 < tiles) load_keys(t + 1, stage ^ 1);
+            copies_done();
+            const int blocks = ks.len - t * kTileKeys < kTileKeys ? (int)(ks.len - t * kTileKeys + 15) / 16 : 4;
+            wait_copies<1>();
+            __syncthreads();
+            if (t == 0)
+                row_terms<T>(lse2, delta, sdo, warp * 16, rows, a.dh, [&](int i) { return i < rows ? out(ro.at(i)) : nullptr; },
+                             [&](int i) {
+                                 const int2 r = ro.at(i);
+                                 return __ldg(g.lse + (qs.at + ro.token + r.x) * a.heads + hk * a.group + r.y);
+                             });
+            if (warp * 16 < rows) {
+                Operands f;
+                Scores s, dp;
+                scores<T>(s, sq, warp * 16, k_of(stage), blocks, bias[stage]);
+                scores<T>(dp, sdo, warp * 16, v_of(stage), blocks, nullptr);
+                slopes(s, dp, lse2, delta, c, blocks);
+                to_operands<T>(f, dp);
+                times_keys<T, DH>(dq, f, k_of(stage), blocks);
+            }
+            __syncthreads();
+        }
+        const RowsAt<T> to(at.dq, qs.at + ro.token, g.ld_dq, a.dh);
+        put_rows<T, DH>(dq, a.scale, rows - warp * 16, a.dh, 0, DH / 16, [&](int i) { return to(ro.at(warp * 16 + i)); },
+                        [](int) { return true; });
     }
-    put_rows<T, DH>(dq, a.scale, rows - warp * 16, a.dh,
-                    [&](int i) { return at.dq + token(warp * 16 + i) * g.ld_dq + head(warp * 16 + i); });
 }
 
 // How a call runs
@@ -430,11 +490,12 @@ cudaError_t run(const AttendArgs& a, const AttendGrads& g, int splits, float* pa
     cudaError_t e = allow_smem(k_attend_keys<T, DH>, KeyTiles<T, DH>::kSmem);
     if (e == cudaSuccess) e = allow_smem(k_attend_rows<T, DH>, RowTiles<T, DH>::kSmem);
     if (e != cudaSuccess) return e;
-    e = launch_next(k_attend_keys<T, DH>, dim3((unsigned)slots(a.Tk, a.B, 1, kTileKeys), (unsigned)a.kv_heads, (unsigned)splits), dim3(128),
+    e = launch_next(k_attend_keys<T, DH>, dim3((unsigned)slots(a.Tk, a.B, 1, kTileLog), (unsigned)a.kv_heads, (unsigned)splits), dim3(128),
                     KeyTiles<T, DH>::kSmem, false, s, a, g, splits, part_dk, part_dv);
     if (e != cudaSuccess || a.Tk <= kTileKeys || a.Tq == 0) return e;
-    return launch_next(k_attend_rows<T, DH>, dim3((unsigned)slots(a.Tq, a.B, a.group, kTileRows), (unsigned)a.kv_heads), dim3(128),
-                       RowTiles<T, DH>::kSmem, false, s, a, g);
+    const int64_t n = slots(a.Tq, a.B, a.group, kTileLog), most = (3 * a.num_sms + a.kv_heads - 1) / a.kv_heads;
+    return launch_next(k_attend_rows<T, DH>, dim3((unsigned)(n < most ? n : most), (unsigned)a.kv_heads), dim3(128),
+                       RowTiles<T, DH>::kSmem, false, s, a, g, n);
 }
 
 }  // namespace

@@ -167,7 +167,7 @@ k_keys_tc(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtens
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, hk = blockIdx.y, split = blockIdx.z;
     check_offsets(a.q_offsets, a.B, a.Tq, a.waits.err);
     check_offsets(a.kv_offsets, a.B, a.Tk, a.waits.err);
-    const Slot slot = slot_of(a.kv_offsets, a.B, a.Tk, 1, 128, blockIdx.x);
+    const Slot slot = slot_of(a.kv_offsets, a.B, a.Tk, 1, 7, blockIdx.x);
     const Span qs = span_of(a.q_offsets, slot.b, a.B, a.Tq), ks = span_of(a.kv_offsets, slot.b, a.B, a.Tk);
     const int64_t key0 = slot.tile * 128;
     if (slot.tile < 0 || key0 >= ks.len) return;
@@ -381,7 +381,7 @@ k_rows_tc(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtens
     constexpr bool kF16 = std::is_same_v<T, __half>;
     __shared__ __align__(16) GradBars<S> bars;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, h0 = blockIdx.y * pack, hk = h0 / a.group;
-    const Slot slot = slot_of(a.q_offsets, a.B, a.Tq, pack, 128, blockIdx.x);
+    const Slot slot = slot_of(a.q_offsets, a.B, a.Tq, pack, 7, blockIdx.x);
     const Span qs = span_of(a.q_offsets, slot.b, a.B, a.Tq), ks = span_of(a.kv_offsets, slot.b, a.B, a.Tk);
     const int64_t row0 = slot.tile * 128, left = qs.len * pack - row0;
     if (slot.tile < 0 || left <= 0) return;
@@ -563,10 +563,10 @@ cudaError_t run(const AttendArgs& a, const AttendGrads& g, int pack, int splits,
     if (e != cudaSuccess) return e;
     e = launch_next(k_attend_delta<T>, dim3((unsigned)((a.Tq * a.heads + 63) / 64)), dim3(256), 0, false, s, a, g, delta);
     if (e != cudaSuccess) return e;
-    e = launch_next(k_keys_tc<T, DH>, dim3((unsigned)slots(a.Tk, a.B, 1, 128), (unsigned)a.kv_heads, (unsigned)splits), dim3(kThreads),
+    e = launch_next(k_keys_tc<T, DH>, dim3((unsigned)slots(a.Tk, a.B, 1, 7), (unsigned)a.kv_heads, (unsigned)splits), dim3(kThreads),
                     GradShape<DH>::kSmem, false, s, mq, mdo, mk, mv, a, g, pack, splits, (const float*)delta, part_dk, part_dv);
     if (e != cudaSuccess) return e;
-    return launch_next(k_rows_tc<T, DH>, dim3((unsigned)slots(a.Tq, a.B, pack, 128), (unsigned)(a.heads / pack)), dim3(kThreads),
+    return launch_next(k_rows_tc<T, DH>, dim3((unsigned)slots(a.Tq, a.B, pack, 7), (unsigned)(a.heads / pack)), dim3(kThreads),
                        GradShape<DH>::kSmem, false, s, mq, mdo, mk, mv, a, g, pack, (const float*)delta);
 }
 

@@ -53,7 +53,7 @@ k_attend_tc(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUte
     const int h0 = blockIdx.y * pack, hk = h0 / a.group;
     check_offsets(a.q_offsets, a.B, a.Tq, a.waits.err);
     check_offsets(a.kv_offsets, a.B, a.Tk, a.waits.err);
-    const Slot slot = slot_of(a.q_offsets, a.B, a.Tq, pack, 256, blockIdx.x);
+    const Slot slot = slot_of(a.q_offsets, a.B, a.Tq, pack, 8, blockIdx.x);
     const Span qs = span_of(a.q_offsets, slot.b, a.B, a.Tq), ks = span_of(a.kv_offsets, slot.b, a.B, a.Tk);
     const int64_t row0 = slot.tile * 256, left = qs.len * pack - row0;
     if (slot.tile < 0 || left <= 0) return;
@@ -336,7 +336,7 @@ cudaError_t run(const AttendArgs& a, const AttendOut& o, int pack, int splits, f
     if (e == cudaSuccess) e = make_head_map(&mv, a.type, a.v, a.Tk, a.kv_heads, a.dh, a.ld_v, 1, 128);
     if (e == cudaSuccess) e = allow_smem(k_attend_tc<T, DH>, TcShapes<DH>::kSmem);
     if (e != cudaSuccess) return e;
-    const dim3 grid((unsigned)slots(a.Tq, a.B, pack, 256), (unsigned)(a.heads / pack), (unsigned)splits);
+    const dim3 grid((unsigned)slots(a.Tq, a.B, pack, 8), (unsigned)(a.heads / pack), (unsigned)splits);
     return launch_next(k_attend_tc<T, DH>, grid, dim3(kThreads), TcShapes<DH>::kSmem, false, s, mq, mk, mv, a, o, pack, splits,
                        part_out, part_lse);
 }

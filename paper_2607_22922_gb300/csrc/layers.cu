@@ -232,7 +232,8 @@ int linear_check(const ifvs_layers* L, const ifvs_linear_params* p, LinearArgs* 
 
 // a row length, or 0 for `least`
 int check_ld(int64_t ld, int64_t least, const char* name, int64_t* out) {
-    if (ld != 0 && (ld < least || ld % 8)) return report_error(IFVS_ERR_ARG, "%s = %lld: at least %lld and a multiple of 8, or 0", name, (long long)ld, (long long)least);
+    if (ld != 0 && (ld < least || ld % 8 || ld > 0x7FFFFFFFLL))
+        return report_error(IFVS_ERR_ARG, "%s = %lld: %lld..2^31 - 1 and a multiple of 8, or 0", name, (long long)ld, (long long)least);
     *out = ld ? ld : least;
     return 0;
 }
