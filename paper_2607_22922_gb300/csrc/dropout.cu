@@ -12,7 +12,8 @@ struct DropArgs {
     const void *x, *residual;
     void* out;
     int64_t n;
-    uint64_t seed, step;
+    RoundKeys keys;
+    uint64_t step;
     const int64_t* more_steps;
     uint32_t below;      // words below it drop their element
     float scale;
@@ -21,7 +22,7 @@ struct DropArgs {
 // A thread takes CH chunks of 16 bytes of x, a grid's width apart.  WIDE: all arrays
 // begin on 16 bytes; else elements come one by one.
 template <class T, bool RES, bool WIDE, int CH>
-__global__ void __launch_bounds__(256) k_dropout(DropArgs a) {
+__global__ void __launch_bounds__(256) k_dropout(const __grid_constant__ DropArgs a) {
     constexpr int E = 16 / (int)sizeof(T);
     using P = Pack<T, E>;
     const T *x = (const T*)a.x, *res = (const T*)a.residual;
@@ -37,6 +38,10 @@ __global__ void __launch_bounds__(256) k_dropout(DropArgs a) {
                 if constexpr (RES) r[c].load(res + at(c));
             }
     }
+    // a CTA's blocks of four words are a power of two and begin at a multiple of it: their
+    // numbers' high halves are one, and so are the products with it
+    const uint64_t block0 = (uint64_t)blockIdx.x * (CH * 256 * E / 4);
+    const uint32_t low = (uint32_t)block0 + threadIdx.x * (E / 4), high = (uint32_t)(block0 >> 32);
     const uint64_t step = a.step + (a.more_steps ? (uint64_t)__ldg(a.more_steps) : 0u);
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
@@ -45,13 +50,24 @@ __global__ void __launch_bounds__(256) k_dropout(DropArgs a) {
         uint32_t w[E];
 #pragma unroll
         for (int j = 0; j < E; j += 4) {
-            const Words q = philox((uint64_t)(i + j) / 4, step, a.seed);
+            const Words q = philox(low + (uint32_t)(c * 256 * E + j) / 4, high, step, a.keys);
 #pragma unroll
             for (int k = 0; k < 4; ++k) w[j + k] = q.w[k];
         }
         // one rounding; what is dropped may be anything
         auto one = [&](float value, float base, uint32_t word) {
-            return word < a.below ? base : (RES ? fmaf(value, a.scale, base) : value * a.scale);
+            // predicated, not selected: comparisons, selections and the generator's exclusive
+            // ors share a pipe
+            float y = base;
+            if constexpr (RES)
+                asm("{\n\t.reg .pred p;\n\tsetp.ge.u32 p, %1, %2;\n\t@p fma.rn.f32 %0, %3, %4, %0;\n\t}"
+                    : "+f"(y)
+                    : "r"(word), "r"(a.below), "f"(value), "f"(a.scale));
+            else
+                asm("{\n\t.reg .pred p;\n\tsetp.ge.u32 p, %1, %2;\n\t@p mul.rn.f32 %0, %3, %4;\n\t}"
+                    : "+f"(y)
+                    : "r"(word), "r"(a.below), "f"(value), "f"(a.scale));
+            return y;
         };
         if (WIDE && i + E <= a.n) {
 #pragma unroll
@@ -74,7 +90,7 @@ bool wide(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
 cudaError_t launch_dropout(const void* x, const void* residual, int64_t n, int type, uint32_t below, float scale, uint64_t seed,
                            uint64_t step, const int64_t* more_steps, void* out, cudaStream_t s) {
-    const DropArgs a{x, residual, out, n, seed, step, more_steps, below, scale};
+    const DropArgs a{x, residual, out, n, round_keys(seed), step, more_steps, below, scale};
     return with_type(type, [&](auto t) {
         using T = decltype(t);
         constexpr int CH = 2;

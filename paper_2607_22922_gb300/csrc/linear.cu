@@ -7,7 +7,7 @@
 // k_linear accumulates a tile of z in TMEM and makes y (or, from dy, dz) of it, so
 // that z is never stored: the gradient computes it again.  dz is rounded to the
 // arrays' type, because the next products multiply 16-bit operands; without an
-// activation it is dy itself.  dx and dW are one launch of k_products.
+// activation it is dy itself.  dx, dW and db are one launch of k_products.
 #include "few.cuh"
 #include "products.cuh"
 
@@ -30,19 +30,64 @@ __device__ __forceinline__ uint4 bias_of(const Epilogue& e, int col, int cols) {
     return e.bias && col < cols ? __ldg(reinterpret_cast<const uint4*>((const uint16_t*)e.bias + col)) : make_uint4(0, 0, 0, 0);
 }
 
+__device__ __forceinline__ float rcp(float x) {
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ float2 pair_ex2(float2 x) {
+    float2 y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y.x) : "f"(x.x));
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y.y) : "f"(x.y));
+    return y;
+}
+
+// act and act' of two values, two float32 operations per instruction: the epilogue of 17408 x
+// 960 -> 2560 with GELU takes 16 instructions a value one by one, 10 so.
+template <int ACT>
+__device__ __forceinline__ void activations(float2 g, float2& v, float2& slope) {
+    auto both2 = [](float c) { return make_float2(c, c); };
+    if constexpr (ACT == IFVS_ACT_SILU) {
+        const float2 e = pair_ex2(mul_(g, both2(-1.44269504f))), d = add_(e, both2(1.f)), p = make_float2(rcp(d.x), rcp(d.y));
+        v = mul_(g, p);
+        slope = fma_(v, fma_(p, both2(-1.f), both2(1.f)), p);
+    } else if constexpr (ACT == IFVS_ACT_GELU) {
+        // Phi by Abramowitz and Stegun 7.1.26, as in activation()
+        const float2 e = pair_ex2(mul_(mul_(g, g), both2(-0.5f * 1.44269504f)));
+        const float2 d = fma_(make_float2(fabsf(g.x), fabsf(g.y)), both2(0.3275911f * 0.70710678f), both2(1.f));
+        const float2 t = make_float2(rcp(d.x), rcp(d.y));
+        float2 q = fma_(t, both2(1.061405429f), both2(-1.453152027f));
+        q = fma_(t, q, both2(1.421413741f));
+        q = fma_(t, q, both2(-0.284496736f));
+        q = fma_(t, q, both2(0.254829592f));
+        // Phi(|g|) - 1/2 = 1/2 - q t e / 2, with the sign of g
+        q = fma_(mul_(mul_(t, e), both2(-0.5f)), q, both2(0.5f));
+        const float2 p = add_(make_float2(copysignf(q.x, g.x), copysignf(q.y, g.y)), both2(0.5f));
+        v = mul_(g, p);
+        slope = fma_(mul_(g, both2(0.39894228f)), e, p);
+    } else {
+        activation<ACT>(g.x, v.x, slope.x);
+        activation<ACT>(g.y, v.y, slope.y);
+    }
+}
+
 template <int ACT, int MODE>
-__device__ __forceinline__ float finish_one(float z, float other) {
-    float v, slope;
-    activation<ACT>(z, v, slope);
-    return MODE == kSlope ? slope * other : v + other;
+__device__ __forceinline__ float2 finish_two(float2 z, float2 other) {
+    float2 v, slope;
+    activations<ACT>(z, v, slope);
+    return MODE == kSlope ? mul_(slope, other) : add_(v, other);
 }
 
 // ---- tiles -------------------------------------------------------------------------
-// BN columns of the output per tile; 8 epilogue warps, each 32 rows x BN / 2 columns.
+// BN columns of the output per tile; 8 epilogue warps, each 32 rows x BN / 2 columns, 32
+// columns at a time.  A warp's two buffers of 32 x 32 hold the residual (or dy), brought by
+// TMA, then the output in its place.  More room there would take a stage of the ring: with
+// five instead of six 17408 x 960 -> 2560 takes 101 us instead of 94.
+constexpr uint32_t kChunkBytes = 32 * 64;
 template <int CG, int BN>
 struct LinearShape {
     static constexpr int kEpi = 8;
-    static constexpr uint32_t kStage = kABytes + BN / CG * 128, kOut = kEpi * kOutBytes;
+    static constexpr uint32_t kStage = kABytes + BN / CG * 128, kOut = kEpi * 2 * kChunkBytes;
     static constexpr int kStages = stages_of(kStage, kOut);
     static constexpr size_t kSmem = smem_of(kStage, kOut);
 };
@@ -50,13 +95,17 @@ struct LinearShape {
 template <int ACT, int MODE, int CG, int BN>
 __global__ void __launch_bounds__(LinearShape<CG, BN>::kEpi * 32 + 64, 1)
 k_linear(const __grid_constant__ CUtensorMap mx, const __grid_constant__ CUtensorMap mw,
-         const __grid_constant__ CUtensorMap my, Grid g, int splits, float* parts, Epilogue e, Waits waits) {
+         const __grid_constant__ CUtensorMap my, const __grid_constant__ CUtensorMap mo, Grid g, int splits, float* parts, Epilogue e,
+         Waits waits) {
     using Sh = LinearShape<CG, BN>;
     constexpr int EPI = Sh::kEpi, S = Sh::kStages;
     __shared__ __align__(8) Bars<S> bars;
+    __shared__ __align__(8) uint64_t other_full[EPI][2];
     const uint32_t ring = dynamic_smem(), out = ring + S * Sh::kStage;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int rank = CG == 2 ? (int)cluster_rank() : 0;
+    if (threadIdx.x == 0)
+        for (int i = 0; i < 2 * EPI; ++i) mbar_init(smem_addr(&other_full[0][0] + i), 1);
     const uint32_t tmem = setup<CG, EPI>(bars);
     const Watch w{&bars.dead, waits};
     const int items = g.m_tiles * g.n_tiles * splits, first = blockIdx.x / CG, step = gridDim.x / CG;
@@ -101,35 +150,39 @@ k_linear(const __grid_constant__ CUtensorMap mx, const __grid_constant__ CUtenso
             }
         }
     } else {
-        OutTile<1> o{out + (uint32_t)warp * kOutBytes};
+        const uint32_t mine = out + (uint32_t)warp * 2 * kChunkBytes;
         const int quad = warp & 3, part = (warp >> 2) * (BN / 2);
+        auto row_of = [&](int2 mn) { return (mn.x * CG + rank) * kRows + quad * 32; };
+        const bool fetches = e.other && splits == 1;
+        // into buffer n mod 2, once its last store has been read
+        int asked = 0, taken = 0;
+        auto fetch = [&](int2 mn, int c) {
+            if (lane == 0) {
+                tma_wait_read<0>();
+                const uint32_t bar = smem_addr(&other_full[warp][asked & 1]);
+                mbar_arrive_expect_tx(bar, kChunkBytes + waits.extra);
+                tma_load<1>(mine + (asked & 1) * kChunkBytes, &mo, mn.y * BN + part + c, row_of(mn), bar);
+            }
+            ++asked;
+        };
+        if (fetches && first < items) fetch(tile_of(first, g.m_tiles, g.n_tiles), 0);
         Ring<2> acc;
-        for (int i = first; i < items; i += step, acc.next()) {
+        bool ok = true;
+        int turn = 0;
+        for (int i = first; i < items && ok; i += step, acc.next()) {
             const int2 mn = tile_of(i / splits, g.m_tiles, g.n_tiles);
-            const int row = (mn.x * CG + rank) * kRows + quad * 32, col0 = mn.y * BN + part;
-            // this lane's row of the residual or of dy, 32 columns ahead of their use
-            uint4 ahead[4];
-            auto fetch = [&](int col) {
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    ahead[j] = e.other && row + lane < g.rows && col + 8 * j < g.cols
-                                   ? __ldg(reinterpret_cast<const uint4*>((const uint16_t*)e.other +
-                                                                          (int64_t)(row + lane) * g.cols + col + 8 * j))
-                                   : make_uint4(0, 0, 0, 0);
-            };
-            if (splits == 1) fetch(col0);
-            if (!__all_sync(0xFFFFFFFFu, w.wait(smem_addr(&bars.acc_full[acc.at]), acc.parity))) break;
+            const int row = row_of(mn), col0 = mn.y * BN + part;
+            if (!(ok = __all_sync(0xFFFFFFFFu, w.wait(smem_addr(&bars.acc_full[acc.at]), acc.parity)))) break;
             fence_after_sync();
             const uint32_t tm = tmem + acc.at * 256 + part + ((uint32_t)quad << 21);
 #pragma unroll 1
-            for (int c = 0; c < BN / 2; c += 32) {
+            for (int c = 0; c < BN / 2; c += 32, turn ^= 1) {
                 const int col = col0 + c;
                 float z[32];
                 tmem_ld32(tm + c, z);
-                uint4 other[4];
+                uint4 b[4];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) other[j] = ahead[j];
-                if (splits == 1 && c + 32 < BN / 2) fetch(col + 32);
+                for (int j = 0; j < 4; ++j) b[j] = bias_of(e, col + 8 * j, g.cols);
                 tmem_wait(z);
                 if (c + 32 == BN / 2) {
                     fence_before_sync();
@@ -145,24 +198,60 @@ k_linear(const __grid_constant__ CUtensorMap mx, const __grid_constant__ CUtenso
                     }
                     continue;
                 }
-                if ((c & 32) == 0) o.begin(lane);
+                float2 v[16];
+#pragma unroll
+                for (int j = 0; j < 16; ++j) {
+                    const uint32_t bw = reinterpret_cast<const uint32_t*>(&b[j / 4])[j & 3];
+                    float2 slope;
+                    activations<ACT>(add_(make_float2(z[2 * j], z[2 * j + 1]), unpack16(bw, e.f16)), v[j], slope);
+                    if (MODE == kSlope) v[j] = slope;
+                }
+                if (fetches) {
+                    if (c + 32 < BN / 2)
+                        fetch(mn, c + 32);
+                    else if (i + step < items)
+                        fetch(tile_of(i + step, g.m_tiles, g.n_tiles), 0);
+                    ok = __all_sync(0xFFFFFFFFu, w.wait(smem_addr(&other_full[warp][taken & 1]), (uint32_t)(taken >> 1) & 1u));
+                    if (!ok) break;
+                    ++taken;
+                } else {
+                    if (lane == 0) tma_wait_read<1>();
+                    __syncwarp();
+                }
+                const uint32_t at = mine + turn * kChunkBytes + lane * 64, key = (lane >> 1) & 3;
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    const uint4 b = bias_of(e, col + 8 * j, g.cols);
-                    const uint32_t bw[4] = {b.x, b.y, b.z, b.w}, ow[4] = {other[j].x, other[j].y, other[j].z, other[j].w};
+                    const uint32_t to = at + ((j ^ key) << 4);
                     uint32_t q[4];
+                    if (fetches) asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(q[0]), "=r"(q[1]), "=r"(q[2]), "=r"(q[3]) : "r"(to) : "memory");
 #pragma unroll
                     for (int k = 0; k < 4; ++k) {
-                        const float2 bf = unpack16(bw[k], e.f16), of = unpack16(ow[k], e.f16);
-                        q[k] = pack16(finish_one<ACT, MODE>(z[8 * j + 2 * k] + bf.x, of.x),
-                                      finish_one<ACT, MODE>(z[8 * j + 2 * k + 1] + bf.y, of.y), e.f16);
+                        float2 r = v[4 * j + k];
+                        if (fetches) {
+                            const float2 other = unpack16(q[k], e.f16);
+                            r = MODE == kSlope ? mul_(r, other) : add_(r, other);
+                        }
+                        q[k] = pack16(r.x, r.y, e.f16);
                     }
-                    o.put(lane, (c & 32) / 8 + j, q[0], q[1], q[2], q[3]);
+                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to), "r"(q[0]), "r"(q[1]), "r"(q[2]), "r"(q[3]) : "memory");
                 }
-                if (c & 32) o.store(lane, &my, col - 32, row, row < g.rows && col - 32 < g.cols);
+                fence_proxy_async_smem();
+                __syncwarp();
+                if (lane == 0) {
+                    if (row < g.rows && col < g.cols) tma_store(&my, col, row, mine + turn * kChunkBytes);
+                    tma_commit();
+                }
             }
         }
         if (lane == 0) tma_wait_all();
+        // a wait ran out: what is on its way has to land before the CTA ends
+        if (*(volatile int*)&bars.dead) {
+            const long long begun = clock64();
+            for (; taken < asked; ++taken)
+                while (!mbar_try_wait(smem_addr(&other_full[warp][taken & 1]), (uint32_t)(taken >> 1) & 1u) &&
+                       clock64() - begun < waits.cycles) {
+                }
+        }
     }
     finish<CG, EPI>(bars, tmem, filled, rank == 0, waits);
 }
@@ -190,7 +279,7 @@ __global__ void __launch_bounds__(256) k_linear_join(const float* parts, int spl
         float2 b = make_float2(0.f, 0.f), o = b;
         if (e.bias) b = unpack2(__ldg((const uint32_t*)e.bias + (col >> 1) + k), T());
         if (e.other) o = unpack2(__ldg((const uint32_t*)e.other + (i >> 1) + k), T());
-        w[k] = pack2(make_float2(finish_one<ACT, MODE>(z[2 * k] + b.x, o.x), finish_one<ACT, MODE>(z[2 * k + 1] + b.y, o.y)), T());
+        w[k] = pack2(finish_two<ACT, MODE>(add_(make_float2(z[2 * k], z[2 * k + 1]), b), o), T());
     }
     *reinterpret_cast<uint2*>(out + i) = q;
 }
@@ -209,68 +298,9 @@ struct LinearOf {
     }
 };
 
-// ---- the bias's gradient: sums over the tokens -------------------------------------------
-// A CTA adds the rows of its part for 256 columns, 8 a lane; its 8 warps take rows by
-// turns and are added in order, and so are the parts.
-constexpr int kBiasCols = 256, kBiasAhead = 4;
-template <class T>
-__global__ void __launch_bounds__(256) k_bias_parts(const T* __restrict__ dz, int64_t rows, int cols, int n_parts, float* parts,
-                                                    T* out) {
-    __shared__ float sums[8][kBiasCols];
-    wait_before();
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, col = blockIdx.x * kBiasCols + lane * 8;
-    const int64_t r0 = rows * blockIdx.y / n_parts, r1 = rows * (blockIdx.y + 1) / n_parts;
-    float2 acc[4] = {};
-    if (col < cols)
-        for (int64_t r = r0 + warp; r < r1; r += 8 * kBiasAhead) {
-            Pack<T, 8> v[kBiasAhead];
-#pragma unroll
-            for (int k = 0; k < kBiasAhead; ++k)       // dz may be the work of the kernel before
-                v[k].w = r + 8 * k < r1 ? __ldcg(reinterpret_cast<const uint4*>(dz + (r + 8 * k) * cols + col)) : make_uint4(0, 0, 0, 0);
-#pragma unroll
-            for (int k = 0; k < kBiasAhead; ++k)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) acc[j] = add_(acc[j], v[k].get(j));
-        }
-#pragma unroll
-    for (int j = 0; j < 4; ++j) *reinterpret_cast<float2*>(&sums[warp][lane * 8 + 2 * j]) = acc[j];
-    __syncthreads();
-    const int c = blockIdx.x * kBiasCols + threadIdx.x;
-    if (c >= cols) return;
-    float s = 0.f;
-#pragma unroll
-    for (int k = 0; k < 8; ++k) s += sums[k][threadIdx.x];
-    if (n_parts == 1)
-        out[c] = from_f32<T>(s);
-    else
-        parts[(int64_t)blockIdx.y * cols + c] = s;
-}
-template <class T>
-__global__ void __launch_bounds__(256) k_bias_join(const float* parts, int n_parts, int cols, T* out) {
-    __shared__ float sums[8][33];
-    wait_before();
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = blockIdx.x * 32 + lane;
-    float s = 0.f;
-    if (c < cols)
-#pragma unroll 8
-        for (int p = warp; p < n_parts; p += 8) s += __ldcg(parts + (int64_t)p * cols + c);
-    sums[warp][lane] = s;
-    __syncthreads();
-    if (warp || c >= cols) return;
-    s = 0.f;
-#pragma unroll
-    for (int k = 0; k < 8; ++k) s += sums[k][lane];
-    out[c] = from_f32<T>(s);
-}
-
 // ---- host -------------------------------------------------------------------------------
 TileArgs tile_args(const LinearArgs& a) { return {a.type, a.num_sms, a.waits}; }
 bool linear_pairs(const LinearArgs& a) { return use_pairs(tile_args(a), a.T, a.D_out, a.D_in); }
-int bias_parts(const LinearArgs& a) {
-    const int64_t wanted = 4 * a.num_sms / ceil_div(a.D_out, kBiasCols), most = ceil_div(a.T, 64);
-    const int64_t n = wanted < most ? wanted : most;
-    return (int)(n < 1 ? 1 : n);
-}
 size_t z_part_bytes(const LinearArgs& a) { return padded(Plan::part_bytes(tile_args(a), a.T, a.D_out, a.D_in, linear_pairs(a))); }
 // the gradient's two products together
 bool grad_pairs(const LinearArgs& a) {
@@ -291,14 +321,16 @@ cudaError_t run_tiles(const LinearArgs& a, const void* x, const void* other, voi
     const int splits = Plan::splits_of(tile_args(a), a.T, a.D_out, a.D_in, pairs);
     auto run = [&](auto cg, auto bn) {
         using Sh = LinearShape<cg(), bn()>;
-        CUtensorMap mx, mw, my;
+        CUtensorMap mx, mw, my, mo;
         cudaError_t r = make_map(&mx, a.type, x, a.T, a.D_in, a.D_in, kRows);
         if (r == cudaSuccess) r = make_map(&mw, a.type, a.w, a.D_out, a.D_in, a.D_in, bn() / cg());
-        if (r == cudaSuccess) r = make_map(&my, a.type, out, a.T, a.D_out, a.D_out, 32);
+        if (r == cudaSuccess) r = make_map(&my, a.type, out, a.T, a.D_out, a.D_out, 32, 32);
+        mo = my;
+        if (r == cudaSuccess && other) r = make_map(&mo, a.type, other, a.T, a.D_out, a.D_out, 32, 32);
         if (r != cudaSuccess) return r;
         const Grid g{ceil_div(a.T, kRows * cg()), ceil_div(a.D_out, bn()), ceil_div(a.D_in, kStepK), (int)a.T, a.D_out};
         return launch_tiles<cg()>(k_linear<ACT, MODE, cg(), bn()>, (int64_t)g.m_tiles * g.n_tiles * splits, a.num_sms,
-                                  Sh::kEpi * 32 + 64, Sh::kSmem, false, s, mx, mw, my, g, splits, parts, e, a.waits);
+                                  Sh::kEpi * 32 + 64, Sh::kSmem, false, s, mx, mw, my, mo, g, splits, parts, e, a.waits);
     };
     const cudaError_t r = pairs ? run(std::integral_constant<int, 2>(), std::integral_constant<int, 256>())
                                 : run(std::integral_constant<int, 1>(), std::integral_constant<int, 128>());
@@ -311,16 +343,6 @@ cudaError_t run_tiles(const LinearArgs& a, const void* x, const void* other, voi
                                a.D_out, e, (__nv_bfloat16*)out);
 }
 
-template <class T>
-cudaError_t run_bias(const LinearArgs& a, const void* dz, void* d_bias, float* parts, bool chain, cudaStream_t s) {
-    const int n = bias_parts(a);
-    const dim3 grid((unsigned)ceil_div(a.D_out, kBiasCols), (unsigned)n);
-    const cudaError_t r = launch_next(k_bias_parts<T>, grid, dim3(256), 0, chain, s, (const T*)dz, a.T, a.D_out, n, parts, (T*)d_bias);
-    if (r != cudaSuccess || n == 1) return r;
-    return launch_next(k_bias_join<T>, dim3((unsigned)ceil_div(a.D_out, 32)), dim3(256), 0, true, s, (const float*)parts, n, a.D_out,
-                       (T*)d_bias);
-}
-
 }  // namespace
 
 size_t linear_bytes(const LinearArgs& a) { return a.T <= kFewTokens ? 0 : z_part_bytes(a); }
@@ -328,8 +350,7 @@ size_t linear_grad_bytes(const LinearArgs& a) {
     if (a.T == 0) return 0;
     const bool p = grad_pairs(a), act = a.act != IFVS_ACT_NONE;
     return (act ? padded((size_t)a.T * a.D_out * 2) + z_part_bytes(a) : 0) +
-           (a.bias ? padded((size_t)bias_parts(a) * a.D_out * 4) : 0) +
-           padded(Plan::part_bytes(tile_args(a), a.T, a.D_in, a.D_out, p)) +
+           (a.bias ? Plan::sums_bytes(tile_args(a), a.D_out) : 0) + Plan::part_bytes(tile_args(a), a.T, a.D_in, a.D_out, p) +
            Plan::part_bytes(tile_args(a), a.D_out, a.D_in, a.T, p);
 }
 
@@ -364,19 +385,13 @@ cudaError_t launch_linear_grad(const LinearArgs& a, const void* x, const void* d
         dz = to;
         chain = true;
     }
-    if (d_bias) {
-        const cudaError_t e = a.type == IFVS_T_F16 ? run_bias<__half>(a, dz, d_bias, (float*)work, chain, s)
-                                                   : run_bias<__nv_bfloat16>(a, dz, d_bias, (float*)work, chain, s);
-        if (e != cudaSuccess) return e;
-        work += padded((size_t)bias_parts(a) * a.D_out * 4);
-        chain = true;
-    }
     // the longer sums first
     Plan plan(tile_args(a), grad_pairs(a), work);
     auto weights = [&] { plan.add(a.D_out, a.D_in, a.T, dz, true, x, true, d_w); };
     if (a.T >= a.D_out) weights();
     plan.add(a.T, a.D_in, a.D_out, dz, false, a.w, true, dx);
     if (a.T < a.D_out) weights();
+    if (d_bias) plan.add_sums(dz, a.T, a.D_out, d_bias);
     return plan.launch(chain, s);
 }
 

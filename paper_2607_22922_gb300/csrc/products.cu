@@ -35,6 +35,51 @@ __device__ __forceinline__ Item item_of(const Products& all, int i) {
     return t;
 }
 
+// The epilogue's four warps' share of the row sums: they take rows by turns, 8 columns a lane,
+// and are added in order through `scratch` (4 KB of shared memory).
+template <class T>
+__device__ __forceinline__ void add_rows(const RowSums& r, uint32_t scratch) {
+    const int cta = blockIdx.x, part = cta % r.n_parts, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (cta / r.n_parts >= r.n_phases) return;
+    const int64_t r0 = r.rows * part / r.n_parts, r1 = r.rows * (part + 1) / r.n_parts;
+    constexpr int AHEAD = 8;
+#pragma unroll 1
+    for (int c0 = cta / r.n_parts * 256; c0 < r.cols; c0 += r.n_phases * 256) {
+        const int col = c0 + lane * 8;
+        float2 acc[4] = {};
+        if (col < r.cols)
+#pragma unroll 1
+            for (int64_t row = r0 + warp; row < r1; row += 4 * AHEAD) {
+                Pack<T, 8> v[AHEAD];
+#pragma unroll
+                for (int k = 0; k < AHEAD; ++k)       // may be the work of the kernel before
+                    v[k].w = row + 4 * k < r1 ? __ldcg(reinterpret_cast<const uint4*>((const T*)r.from + (row + 4 * k) * r.cols + col))
+                                              : make_uint4(0, 0, 0, 0);
+#pragma unroll
+                for (int k = 0; k < AHEAD; ++k)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) acc[j] = add_(acc[j], v[k].get(j));
+            }
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            asm volatile("st.shared.v2.f32 [%0], {%1, %2};" ::"r"(scratch + (warp * 256 + lane * 8 + 2 * j) * 4), "f"(acc[j].x), "f"(acc[j].y)
+                         : "memory");
+        asm volatile("bar.sync 1, 128;" ::: "memory");
+        const int t = threadIdx.x * 2;
+        if (c0 + t < r.cols) {
+            float2 s = make_float2(0.f, 0.f);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                float2 v;
+                asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(scratch + (k * 256 + t) * 4) : "memory");
+                s = add_(s, v);
+            }
+            *reinterpret_cast<float2*>(r.parts + (int64_t)part * r.cols + c0 + t) = s;
+        }
+        asm volatile("bar.sync 1, 128;" ::: "memory");
+    }
+}
+
 template <int CG, int BN>
 __global__ void __launch_bounds__(192, 1) k_products(const __grid_constant__ Products all, bool f16, Waits waits) {
     using Sh = ProductShape<CG, BN>;
@@ -89,6 +134,12 @@ __global__ void __launch_bounds__(192, 1) k_products(const __grid_constant__ Pro
             }
         }
     } else {
+        if (all.sums.from) {
+            if (f16)
+                add_rows<__half>(all.sums, out);
+            else
+                add_rows<__nv_bfloat16>(all.sums, out);
+        }
         OutTile<2> o{out + (uint32_t)warp * 2 * kOutBytes};
         Ring<2> acc;
         for (int i = first; i < all.items; i += step, acc.next()) {
@@ -137,27 +188,39 @@ __global__ void __launch_bounds__(192, 1) k_products(const __grid_constant__ Pro
 }
 
 template <class T>
-__global__ void __launch_bounds__(256) k_join_parts(Parts p) {
+__global__ void __launch_bounds__(256) k_join_parts(const __grid_constant__ Parts p) {
     wait_before();
-    const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
     const int j = blockIdx.y;
-    if (i >= p.n[j]) return;
+    // the row sums are few values of many parts: eight lanes share four of them
+    const bool shared = j == p.sums;
+    const int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x, i = (shared ? t / 8 : t) * 4;
+    const int first = shared ? (int)(t & 7) : 0, step = shared ? 8 : 1;
     float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+    const int splits = i < p.n[j] ? p.splits[j] : 0;
 #pragma unroll 8
-    for (int s = 0; s < p.splits[j]; ++s) {
+    for (int s = first; s < splits; s += step) {
         const float4 q = __ldcg(reinterpret_cast<const float4*>(p.parts[j] + s * p.n[j] + i));
         v.x += q.x;
         v.y += q.y;
         v.z += q.z;
         v.w += q.w;
     }
+    if (shared)
+#pragma unroll
+        for (int x = 1; x < 8; x <<= 1) {
+            v.x += __shfl_xor_sync(0xFFFFFFFFu, v.x, x);
+            v.y += __shfl_xor_sync(0xFFFFFFFFu, v.y, x);
+            v.z += __shfl_xor_sync(0xFFFFFFFFu, v.z, x);
+            v.w += __shfl_xor_sync(0xFFFFFFFFu, v.w, x);
+        }
+    if (i >= p.n[j] || first > 0) return;
     *reinterpret_cast<uint2*>((T*)p.c[j] + i) = make_uint2(pack2(make_float2(v.x, v.y), T()), pack2(make_float2(v.z, v.w), T()));
 }
 
 }  // namespace
 
 cudaError_t make_map(CUtensorMap* map, int type, const void* p, int64_t rows, int64_t cols, int64_t stride,
-                     int box_rows) {
+                     int box_rows, int box_cols) {
     static const auto encode = [] {
         void* fn = nullptr;
         cudaDriverEntryPointQueryResult r;
@@ -168,10 +231,10 @@ cudaError_t make_map(CUtensorMap* map, int type, const void* p, int64_t rows, in
     }();
     if (!encode) return cudaErrorNotSupported;
     const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)stride * 2};
-    const cuuint32_t box[2] = {64, (cuuint32_t)box_rows}, step[2] = {1, 1};
+    const cuuint32_t box[2] = {(cuuint32_t)box_cols, (cuuint32_t)box_rows}, step[2] = {1, 1};
     const CUresult r = encode(map, type == IFVS_T_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16,
                               2, const_cast<void*>(p), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                              box_cols == 64 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
 }
@@ -185,7 +248,10 @@ cudaError_t Plan::launch(bool chain, cudaStream_t s) {
                                 f16, a.waits);
     if (e != cudaSuccess || joined == 0) return e;
     int64_t most = 0;
-    for (int j = 0; j < joined; ++j) most = parts.n[j] > most ? parts.n[j] : most;
+    for (int j = 0; j < joined; ++j) {
+        const int64_t n = j == parts.sums ? parts.n[j] * 8 : parts.n[j];
+        most = n > most ? n : most;
+    }
     const dim3 grid((unsigned)((most + 1023) / 1024), (unsigned)joined);
     return f16 ? launch_next(k_join_parts<__half>, grid, dim3(256), 0, true, s, parts)
                : launch_next(k_join_parts<__nv_bfloat16>, grid, dim3(256), 0, true, s, parts);

@@ -16,17 +16,28 @@ struct Product {
     bool a_mn, b_mn;
     float* parts;        // [splits][rows][cols]
 };
+// Sums over the rows of a matrix (a bias's gradient), made by the warps that would wait for
+// the first tile: CTA c adds part c mod n_parts of the rows in every n_phases-th block of 256
+// columns from c / n_parts on.
+struct RowSums {
+    const void* from;    // [rows][cols], or null: none
+    int64_t rows;
+    int cols, n_parts, n_phases;
+    float* parts;        // [n_parts][cols]
+};
 struct Products {
     Product p[3];
     int n, items;
+    RowSums sums;
 };
 
-// C = the sum of the parts, in order; up to three products
+// C = the sum of the parts, in order; up to three products and the sums
 struct Parts {
-    const float* parts[3];
-    void* c[3];
-    int64_t n[3];        // values, a multiple of 8
-    int splits[3];
+    const float* parts[4];
+    void* c[4];
+    int64_t n[4];        // values, a multiple of 8
+    int splits[4];
+    int sums;            // which of them are the row sums, or -1
 };
 
 // Products of one launch, in the order they are added
@@ -40,6 +51,8 @@ struct Plan {
     cudaError_t e = cudaSuccess;
     explicit Plan(const TileArgs& a_, bool pairs_, uint8_t* work_) : a(a_), pairs(pairs_), work(work_) {
         all.n = all.items = 0;
+        all.sums.from = nullptr;
+        parts.sums = -1;
     }
 
     int rows_tile() const { return pairs ? 256 : 128; }
@@ -65,6 +78,25 @@ struct Plan {
             parts.n[joined] = rows * cols;
             parts.splits[joined++] = p.splits;
         }
+    }
+    // After the products are added: `out` [cols], the sums over the rows of `from`
+    void add_sums(const void* from, int64_t rows, int cols, void* out) {
+        const int ctas = grid(), blocks = ceil_div(cols, 256);
+        int phases = ctas / 16 < blocks ? ctas / 16 : blocks;
+        if (phases < 1) phases = 1;
+        all.sums = RowSums{from, rows, cols, ctas / phases, phases, (float*)work};
+        parts.parts[joined] = (float*)work;
+        parts.c[joined] = out;
+        parts.n[joined] = cols;
+        parts.sums = joined;
+        parts.splits[joined++] = ctas / phases;
+        work += (size_t)(ctas / phases) * cols * sizeof(float);
+    }
+    static size_t sums_bytes(const TileArgs& a, int cols) { return (size_t)a.num_sms * cols * sizeof(float); }
+    // CTAs of the launch
+    int grid() const {
+        const int64_t most = a.num_sms / (pairs ? 2 : 1);
+        return (int)(all.items < most ? all.items : most) * (pairs ? 2 : 1);
     }
     // Parts of a tile's sum: where the tiles leave SMs without work, at least four
     // stages each.  A sum of any length is cut below 2^16 stages, which bounds

@@ -217,8 +217,9 @@ __device__ __forceinline__ uint32_t pack16(float a, float b, bool f16) {
 // ---- tensor maps (host) ---------------------------------------------------------
 // rows x cols matrix of 16-bit elements, rows `stride` elements apart; box of 64
 // columns by box_rows rows.  Anything outside reads as zeros and is not written.
+// box_cols 32: boxes of 32 columns in the 64-byte swizzle (chunk ^ (row / 2 mod 4)).
 cudaError_t make_map(CUtensorMap* map, int type, const void* p, int64_t rows, int64_t cols, int64_t stride,
-                     int box_rows);
+                     int box_rows, int box_cols = 64);
 
 // Tile t of a grid of tiles: bands of kBand row tiles, columns outermost
 // inside a band, so that tiles that run together share operand tiles in L2.

@@ -19,7 +19,8 @@ def test_words(tmp_path):
     src, exe = tmp_path / "w.cpp", tmp_path / "w"
     src.write_text('#include <stdio.h>\n#include <stdlib.h>\n#include "philox.h"\nint main(int n, char** a) {\n'
                    "  for (int i = 1; i + 2 < n; i += 3) {\n"
-                   "    ifvs::Words w = ifvs::philox(strtoull(a[i], 0, 10), strtoull(a[i + 1], 0, 10), strtoull(a[i + 2], 0, 10));\n"
+                   "    unsigned long long b = strtoull(a[i], 0, 10), s = strtoull(a[i + 1], 0, 10);\n"
+                   "    ifvs::Words w = ifvs::philox((uint32_t)b, (uint32_t)(b >> 32), s, ifvs::round_keys(strtoull(a[i + 2], 0, 10)));\n"
                    '    printf("%08x %08x %08x %08x\\n", w.w[0], w.w[1], w.w[2], w.w[3]);\n  }\n  return 0;\n}\n')
     subprocess.check_call(["g++", "-std=c++17", "-Wall", "-Werror", "-I", CSRC, "-o", str(exe), str(src)])
     asked = [k[:3] for k in KNOWN] + [(i * 0x9E3779B97F4A7C15 % 2**64, i, 2**63 + i) for i in range(50)]
