@@ -293,12 +293,19 @@ __global__ void __launch_bounds__(256) k_attend_join(AttendArgs a, AttendOut o, 
 // How a call runs
 struct Plan {
     bool tc;             // tiles of the tensor cores
+    bool brief;          // the same for many short sequences
     int pack, log_rows, splits;
 };
 Plan plan_of(const AttendArgs& a) {
     Plan p;
     p.pack = tc_pack(a);
     p.tc = a.Tq * p.pack / a.B >= 128 && a.Tk / a.B >= 256;
+    p.brief = !p.tc && a.Tq * p.pack / a.B >= 32 && slots(a.Tq, a.B, p.pack, 7) * (a.heads / p.pack) >= 2 * a.num_sms;
+    if (p.brief) {
+        p.log_rows = 7;
+        p.splits = 1;
+        return p;
+    }
     const int group = p.tc ? p.pack : a.group, keys = p.tc ? 128 : kTileKeys;
     auto ctas = [&](int log) {
         const int64_t tiles = (a.Tq * group >> log) + 1;
@@ -342,6 +349,7 @@ cudaError_t launch_attend(const AttendArgs& a, const AttendOut& o, uint8_t* work
     }
     auto go = [&](auto t) {
         using T = decltype(t);
+        if (p.brief) return launch_attend_short(a, o, p.pack, a.Tk / a.B > 48, s);
         const cudaError_t e = p.tc           ? launch_attend_tc(a, o, p.pack, p.splits, part_out, part_lse, s)
                               : a.dh <= 32 ? run<T, 32>(a, o, p, part_out, part_lse, s)
                               : a.dh <= 64 ? run<T, 64>(a, o, p, part_out, part_lse, s)

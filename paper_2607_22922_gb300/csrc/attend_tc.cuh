@@ -22,6 +22,12 @@ __device__ __forceinline__ void tma_load_heads(uint32_t dst, const CUtensorMap* 
         : "memory");
 }
 
+__device__ __forceinline__ void tma_store_heads(const CUtensorMap* map, int d, int head, int row, uint32_t src) {
+    asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group [%0, {%1, %2, %3}], [%4];" ::"l"(map), "r"(d), "r"(head),
+                 "r"(row), "r"(src)
+                 : "memory");
+}
+
 // Operand B of a sum over the tile's rows (MN-major), 64-element blocks of 128 rows
 __device__ __forceinline__ uint64_t rows_desc(uint32_t addr) {
     return (uint64_t)((addr & 0x3FFFFu) >> 4) | ((uint64_t)(kHalfBytes >> 4) << 16) | ((uint64_t)(1024u >> 4) << 32) | (1ull << 46) |
@@ -49,6 +55,14 @@ __device__ __forceinline__ void tmem_st32(uint32_t addr, const uint32_t (&r)[32]
         "r"(r[29]), "r"(r[30]), "r"(r[31]), "r"(addr)
         : "memory");
 }
+__device__ __forceinline__ void tmem_st16(uint32_t addr, const uint32_t (&r)[16]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15};" ::"r"(r[0]),
+        "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]),
+        "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(addr)
+        : "memory");
+}
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
 // Heads of a group that share a tile of 128 rows: all, where they divide it, else one
@@ -56,6 +70,8 @@ inline int tc_pack(const AttendArgs& a) { return (a.group & (a.group - 1)) == 0 
 
 cudaError_t launch_attend_tc(const AttendArgs& a, const AttendOut& o, int pack, int splits, float* part_out, float* part_lse,
                              cudaStream_t s);
+// wide: 128 keys at a time instead of 64
+cudaError_t launch_attend_short(const AttendArgs& a, const AttendOut& o, int pack, bool wide, cudaStream_t s);
 // delta: [Tq][heads] floats of workspace
 cudaError_t launch_attend_grad_tc(const AttendArgs& a, const AttendGrads& g, int pack, int splits, float* delta, float* part_dk,
                                   float* part_dv, cudaStream_t s);

@@ -121,7 +121,8 @@ def test_padding(layers, type_, fused):
         assert not clean[1][bad].any() and not clean[2][bad].any() and not clean[0][90:99].any()
 
 
-@pytest.mark.parametrize("lengths", [([30, 31, 33], [40, 41, 43]), ([100, 131, 133], [140, 241, 143])])
+@pytest.mark.parametrize("lengths", [([30, 31, 33], [40, 41, 43]), ([100, 131, 133], [140, 241, 143]), ([200, 331, 133], [340, 541, 243]),
+                                     ([60] * 180, [30] * 180)])
 def test_sequences_do_not_see_each_other(layers, lengths):
     """Values that are not finite in one sequence stay there."""
     q, k, v, d_out, kw = _args(*lengths, 4, 2, 64, torch.bfloat16, seed=5)
@@ -172,6 +173,27 @@ def test_rows_with_gaps(layers, type_):
 ])
 def test_long(layers, type_, lq, lk, H, Hk, d):
     _check(layers, *_args(lq, lk, H, Hk, d, TYPES[type_], seed=d + H, padding=0.05))
+
+
+def _ragged(n, low, high, seed):
+    g = torch.Generator()
+    g.manual_seed(seed)
+    return torch.randint(low, high + 1, (n,), generator=g).tolist()
+
+
+# many sequences: some without queries or keys, keys of one chunk and of several, groups
+# that fill a tile of 128 rows, or do not divide it
+@pytest.mark.parametrize("type_", sorted(TYPES))
+@pytest.mark.parametrize("B,q,k,H,Hk,d", [
+    (160, (0, 130), (0, 65), 4, 1, 64),
+    (200, (20, 60), (0, 17), 8, 8, 40),
+    (150, (30, 90), (50, 140), 4, 2, 128),
+    (120, (60, 70), (40, 300), 6, 2, 72),
+    (300, (1, 3), (1, 40), 64, 1, 64),
+    (170, (120, 120), (16, 16), 8, 2, 8),
+])
+def test_many_sequences(layers, type_, B, q, k, H, Hk, d):
+    _check(layers, *_args(_ragged(B, *q, 1), _ragged(B, *k, 2), H, Hk, d, TYPES[type_], seed=B, fused=True, padding=0.04))
 
 
 def test_no_offsets_is_one_sequence(layers):
@@ -246,7 +268,7 @@ def _loss(qkv, d_out, kw):
     return total
 
 
-@pytest.mark.parametrize("lengths", [([3] * 40, [9] * 40), ([1], [9_000]), ([3_001], [65]), ([500, 400], [600, 1_000])])
+@pytest.mark.parametrize("lengths", [([3] * 40, [9] * 40), ([1], [9_000]), ([3_001], [65]), ([500, 400], [600, 1_000]), ([50] * 200, [30] * 200)])
 def test_equal_calls_give_equal_bits(layers, lengths):
     q, k, v, d_out, kw = _args(*lengths, 4, 2, 64, torch.bfloat16)
     out, lse = layers.attend(q, k, v, lse=True, **kw)
