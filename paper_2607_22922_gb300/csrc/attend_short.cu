@@ -1,11 +1,13 @@
 // Attention of many short sequences on the tensor cores (ifvs_attend).
 //
 // Persistent CTAs take units, a tile of 128 rows of one group each, whose keys are mostly one
-// chunk of KEYS.  A warp finds units by 32 at a time and loads their queries, keys and values
-// by TMA; a warp issues the MMAs; two groups of four warps take units by turns, so that one
-// group's exponentials and output run beside the other's MMAs:
-//   tensor pipe:  s_0  s_1 | o_0 s_2 | o_1 s_3 | ...
-// A thread holds a row's scores.  Sequences with more keys go on chunk by chunk as in
+// chunk of KEYS.  A warp finds units, 32 at a time, a warp loads their queries, keys and values
+// by TMA, a warp issues the MMAs, two see to keys that do not count; two or four groups of four warps take units by turns, so
+// that one group's exponentials and output run beside the others' MMAs:
+//   tensor pipe (two groups):  s_0  s_1 | o_0 s_2 | o_1 s_3 | ...
+// What bounds a unit is the chain of its waits (loads, s, weights, o, output), which four
+// groups hide better than two.  A thread takes a row's scores 32 at a time, twice: for their
+// maximum, then for the weights, which leaves registers for four groups.  Sequences with more keys go on chunk by chunk as in
 // attend_tc.cu.  Rows leave through shared memory by TMA, 32 at a time.
 #include "attend_tc.cuh"
 
@@ -13,31 +15,35 @@ namespace ifvs {
 
 namespace {
 
-constexpr int kSoftWarps = 8, kLoader = 8, kIssuer = 9, kFixer = 10, kThreads = 352;
-constexpr int kInfos = 8;
+constexpr int kBatch = 32;       // units that are found together
 
 template <int DH, int KEYS>
 struct ShortShape {
     static constexpr int kHalves = DH / 64;
+    static constexpr int kGroups = DH == 64 && KEYS == 64 ? 4 : 2;       // TMEM: KEYS + DH columns each
+    static constexpr int kSoft = 4 * kGroups, kLoader = kSoft, kIssuer = kSoft + 1, kFixer = kSoft + 2,      // warps
+                         kFixers = 2, kFinder = kFixer + kFixers, kThreads = (kFinder + 1) * 32;
     static constexpr uint32_t kQ = kHalves * kHalfBytes;                 // 128 rows
     static constexpr uint32_t kKeyHalf = KEYS * 128, kK = kHalves * kKeyHalf, kKv = 2 * kK;
-    static constexpr int kQs = DH == 128 ? 2 : (KEYS == 64 ? 5 : 4);
+    static constexpr int kQs = DH == 128 ? 2 : 4;
     static constexpr int kKvs = DH == 128 ? (KEYS == 64 ? 4 : 2) : (KEYS == 64 ? 6 : 4);
-    static constexpr uint32_t kOut = kSoftWarps * 32 * 128;              // 32 rows of 64 elements a warp
+    static constexpr uint32_t kOut = kSoft * 32 * 128;              // 32 rows of 64 elements a warp
     static constexpr size_t kSmem = 1024 + kQs * kQ + kKvs * kKv + kOut;
 };
 
-// A unit; rows = 0: there are no more
 struct Unit {
-    int64_t token, key;      // of the first row and key
-    int rows, keys, head, kv_head;
+    int token, key;          // the first row's token, the first key
+    int keys;
+    int16_t rows, head, kv_head;
+    uint8_t place, parity;   // of its first chunk in the ring of keys
 };
 
-template <int QS, int KS, int KEYS>
+template <int QS, int KS, int KEYS, int GROUPS>
 struct ShortBars {
-    uint64_t unit_full[kInfos], unit_empty[kInfos], q_full[QS], q_empty[QS], kv_full[KS], kv_empty[KS], fixed[KS], s_full[2], p_full[2],
-        o_full[2], drain;
-    Unit units[kInfos];
+    uint64_t batch_full[2], batch_empty[2], q_full[QS], q_empty[QS], kv_full[KS], kv_empty[KS], fixed[KS], s_full[GROUPS],
+        p_full[GROUPS], o_full[GROUPS], drain;
+    Unit units[2][kBatch];
+    int count[2];            // -1: there are no more
     uint32_t mask[KS][KEYS / 32];
     uint32_t tmem;
     int dead;
@@ -61,21 +67,22 @@ struct Place {
 };
 
 template <class T, int DH, int KEYS>
-__global__ void __launch_bounds__(kThreads, 1)
+__global__ void __launch_bounds__(ShortShape<DH, KEYS>::kThreads, 1)
 k_attend_short(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mv,
-               const __grid_constant__ CUtensorMap mo, AttendArgs a, AttendOut o, int pack, int64_t n_units) {
+               const __grid_constant__ CUtensorMap mo, AttendArgs a, AttendOut o, int log_pack, int64_t n_units) {
     using Sh = ShortShape<DH, KEYS>;
-    constexpr int QS = Sh::kQs, KS = Sh::kKvs, W = KEYS / 32;
+    constexpr int QS = Sh::kQs, KS = Sh::kKvs, W = KEYS / 32, GROUPS = Sh::kGroups;
+    constexpr int kLoader = Sh::kLoader, kIssuer = Sh::kIssuer, kFixer = Sh::kFixer, kFinder = Sh::kFinder;
     constexpr bool kF16 = std::is_same_v<T, __half>;
-    __shared__ __align__(16) ShortBars<QS, KS, KEYS> bars;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    __shared__ __align__(16) ShortBars<QS, KS, KEYS, GROUPS> bars;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, pack = 1 << log_pack;
     check_offsets(a.q_offsets, a.B, a.Tq, a.waits.err);
     check_offsets(a.kv_offsets, a.B, a.Tk, a.waits.err);
     const uint32_t q_at = dynamic_smem(), kv_at = q_at + QS * Sh::kQ, out_at = kv_at + KS * Sh::kKv;
     if (threadIdx.x == 0) {
-        for (int i = 0; i < kInfos; ++i) {
-            mbar_init(smem_addr(&bars.unit_full[i]), 1);
-            mbar_init(smem_addr(&bars.unit_empty[i]), kSoftWarps + 2);
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(smem_addr(&bars.batch_full[i]), 1);
+            mbar_init(smem_addr(&bars.batch_empty[i]), Sh::kSoft + 2 + Sh::kFixers);
         }
         for (int i = 0; i < QS; ++i) {
             mbar_init(smem_addr(&bars.q_full[i]), 1);
@@ -86,7 +93,7 @@ k_attend_short(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
             mbar_init(smem_addr(&bars.kv_empty[i]), 1);
             mbar_init(smem_addr(&bars.fixed[i]), 1);
         }
-        for (int i = 0; i < 2; ++i) {
+        for (int i = 0; i < GROUPS; ++i) {
             mbar_init(smem_addr(&bars.s_full[i]), 1);
             mbar_init(smem_addr(&bars.p_full[i]), 4);
             mbar_init(smem_addr(&bars.o_full[i]), 1);
@@ -102,65 +109,47 @@ k_attend_short(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
     const uint32_t tmem = bars.tmem;
     const Watch w{&bars.dead, a.waits};
     auto s_col = [](int g) { return (uint32_t)g * KEYS; };
-    auto o_col = [](int g) { return 2u * KEYS + (uint32_t)g * DH; };
+    auto o_col = [](int g) { return (uint32_t)GROUPS * KEYS + (uint32_t)g * DH; };
     int q_filled = 0, kv_filled = 0;             // by the loader's thread
 
-    // the next unit, read by this role
-    Place<kInfos> unit_at;
-    auto next_unit = [&](Unit& u, bool by_warp) {
-        const bool there = w.wait(smem_addr(&bars.unit_full[unit_at.at]), unit_at.parity);
-        if (by_warp ? !__all_sync(0xFFFFFFFFu, there) : !there) return false;
-        u = bars.units[unit_at.at];
-        if (by_warp) __syncwarp();
-        if (!by_warp || lane == 0) mbar_arrive<1>(smem_addr(&bars.unit_empty[unit_at.at]));
-        unit_at.next();
-        return u.rows > 0;
-    };
     auto chunks_of = [](int keys) { return (keys + KEYS - 1) / KEYS; };
-
-    if (warp == kLoader) {
-        const int nh = a.heads / pack;
-        Place<QS> qp;
-        Place<KS> kp;
-        bool ok = true;
-        // one unit, by the elected lane
-        auto give = [&](const Unit& u) {
-            if (!w.wait(smem_addr(&bars.unit_empty[unit_at.at]), unit_at.parity ^ 1u)) return false;
-            bars.units[unit_at.at] = u;
-            mbar_arrive<1>(smem_addr(&bars.unit_full[unit_at.at]));
-            unit_at.next();
-            const int chunks = u.rows > 0 ? chunks_of(u.keys) : 0;
-            if (chunks == 0) return true;
-            if (!w.wait(smem_addr(&bars.q_empty[qp.at]), qp.parity ^ 1u)) return false;
-            uint32_t bar = smem_addr(&bars.q_full[qp.at]);
-            mbar_arrive_expect_tx(bar, Sh::kQ + a.waits.extra);
-            for (int d = 0; d < Sh::kHalves; ++d)
-                tma_load_heads(q_at + qp.at * Sh::kQ + d * kHalfBytes, &mq, d * 64, u.head, (int)u.token, bar);
-            qp.next();
-            ++q_filled;
-            for (int j = 0; j < chunks; ++j) {
-                if (!w.wait(smem_addr(&bars.kv_empty[kp.at]), kp.parity ^ 1u)) return false;
-                bar = smem_addr(&bars.kv_full[kp.at]);
-                mbar_arrive_expect_tx(bar, Sh::kKv + a.waits.extra);
-                for (int d = 0; d < Sh::kHalves; ++d) {
-                    const uint32_t to = kv_at + kp.at * Sh::kKv + d * Sh::kKeyHalf;
-                    tma_load_heads(to, &mk, d * 64, u.kv_head, (int)(u.key + (int64_t)j * KEYS), bar);
-                    tma_load_heads(to + Sh::kK, &mv, d * 64, u.kv_head, (int)(u.key + (int64_t)j * KEYS), bar);
-                }
-                kp.next();
-                ++kv_filled;
+    // f(unit) for every step-th unit from the first-th on; by the warp, or (alone) by one of
+    // its threads
+    auto units = [&](bool alone, int first, int step, auto&& f) {
+        uint32_t b = 0, parity = 0;
+        for (;;) {
+            bool ok = w.wait(smem_addr(&bars.batch_full[b]), parity);
+            if (!alone) ok = __all_sync(0xFFFFFFFFu, ok);
+            const int n = ok ? bars.count[b] : -1;
+            if (n < 0) return ok;
+            for (; first < n; first += step) {
+                const Unit u = bars.units[b][first];
+                if (!f(u)) return false;
             }
-            return true;
-        };
-        for (int64_t u0 = blockIdx.x; u0 < n_units && ok; u0 += 32 * (int64_t)gridDim.x) {
-            const int64_t mine = u0 + lane * (int64_t)gridDim.x;
-            Unit u{0, 0, 0, 0, 0, 0};
+            first -= n;
+            if (!alone) __syncwarp();
+            if (alone || lane == 0) mbar_arrive<1>(smem_addr(&bars.batch_empty[b]));
+            b ^= 1u;
+            parity ^= b ^ 1u;
+        }
+    };
+
+    if (warp == kFinder) {
+        const int nh = a.heads >> log_pack;
+        uint32_t b = 0, parity = 1, place = 0, turn = 0;
+        // rounds of a unit per CTA; the CTAs change places from round to round, since what a
+        // sequence's slots hold may repeat with a period that divides the grid's
+        const uint32_t grid = gridDim.x;
+        for (int64_t round = 0; round * grid < n_units; round += kBatch) {
+            const uint32_t seat = (uint32_t)((blockIdx.x + 37u * (uint32_t)((round + lane) % grid)) % grid);
+            const int64_t mine = (round + lane) * grid + seat;
+            Unit u{};
             if (mine < n_units) {
                 const uint32_t slot = (uint32_t)(mine / nh), y = (uint32_t)(mine - (int64_t)slot * nh);
                 uint32_t lo = 0, n = (uint32_t)a.B;      // the sequence: the last whose slots begin there or before
                 while (n > 1) {
                     const uint32_t half = n / 2;
-                    if (first_slot(a.q_offsets, lo + half, a.B, a.Tq, pack, 7) <= slot) {
+                    if (first_slot(a.q_offsets, lo + half, a.B, a.Tq, pack, 7) <= (int64_t)slot) {
                         lo += half;
                         n -= half;
                     } else {
@@ -170,35 +159,90 @@ k_attend_short(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
                 const int64_t tile = (int64_t)slot - first_slot(a.q_offsets, lo, a.B, a.Tq, pack, 7);
                 const Span qs = span_of(a.q_offsets, lo, a.B, a.Tq), ks = span_of(a.kv_offsets, lo, a.B, a.Tk);
                 const int64_t left = qs.len * pack - tile * 128;
-                u.token = qs.at + tile * 128 / pack;
-                u.key = ks.at;
-                u.rows = tile < 0 || left <= 0 ? 0 : (left < 128 ? (int)left : 128);
+                u.token = (int)(qs.at + (tile * 128 >> log_pack));
+                u.key = (int)ks.at;
                 u.keys = (int)ks.len;
-                u.head = (int)y * pack;
-                u.kv_head = u.head / a.group;
+                u.rows = tile < 0 || left <= 0 ? 0 : (int16_t)(left < 128 ? left : 128);
+                u.head = (int16_t)(y << log_pack);
+                u.kv_head = (int16_t)((y << log_pack) / a.group);
             }
-            for (uint32_t todo = __ballot_sync(0xFFFFFFFFu, u.rows > 0); todo && ok; todo &= todo - 1) {
-                const int from = __ffs((int)todo) - 1;
-                const Unit v{__shfl_sync(0xFFFFFFFFu, u.token, from), __shfl_sync(0xFFFFFFFFu, u.key, from),
-                             __shfl_sync(0xFFFFFFFFu, u.rows, from),  __shfl_sync(0xFFFFFFFFu, u.keys, from),
-                             __shfl_sync(0xFFFFFFFFu, u.head, from),  __shfl_sync(0xFFFFFFFFu, u.kv_head, from)};
-                bool fine = true;
-                if (elect_one()) fine = give(v);
-                ok = __all_sync(0xFFFFFFFFu, fine);
+            const uint32_t there = __ballot_sync(0xFFFFFFFFu, u.rows > 0);
+            // places in the ring of keys: chunks before this unit's
+            const int mine_chunks = u.rows > 0 ? chunks_of(u.keys) : 0;
+            int before = mine_chunks;
+#pragma unroll
+            for (int x = 1; x < 32; x <<= 1) {
+                const int other = __shfl_up_sync(0xFFFFFFFFu, before, x);
+                if (lane >= x) before += other;
             }
+            const int all = __shfl_sync(0xFFFFFFFFu, before, 31);
+            const uint32_t at = place + (uint32_t)(before - mine_chunks);
+            u.place = (uint8_t)(at % KS);
+            u.parity = (uint8_t)((turn + at / KS) & 1u);
+            turn += (place + (uint32_t)all) / KS;
+            place = (place + (uint32_t)all) % KS;
+            if (!__all_sync(0xFFFFFFFFu, w.wait(smem_addr(&bars.batch_empty[b]), parity))) break;
+            if (u.rows > 0) bars.units[b][__popc(there & ((1u << lane) - 1u))] = u;
+            if (lane == 0) bars.count[b] = __popc(there);
+            __syncwarp();
+            if (lane == 0) mbar_arrive<1>(smem_addr(&bars.batch_full[b]));
+            b ^= 1u;
+            parity ^= b ^ 1u;
         }
-        if (ok && elect_one()) give(Unit{0, 0, 0, 0, 0, 0});
+        if (__all_sync(0xFFFFFFFFu, w.wait(smem_addr(&bars.batch_empty[b]), parity)) && lane == 0) {
+            bars.count[b] = -1;
+            mbar_arrive<1>(smem_addr(&bars.batch_full[b]));
+        }
+    } else if (warp == kLoader) {
+        if (elect_one()) {
+            Place<QS> qp;
+            Place<KS> kp;
+            units(true, 0, 1, [&](const Unit& u) {
+                const int chunks = chunks_of(u.keys);
+                if (chunks == 0) return true;
+                if (!w.wait(smem_addr(&bars.q_empty[qp.at]), qp.parity ^ 1u)) return false;
+                uint32_t bar = smem_addr(&bars.q_full[qp.at]);
+                mbar_arrive_expect_tx(bar, Sh::kQ + a.waits.extra);
+                for (int d = 0; d < Sh::kHalves; ++d)
+                    tma_load_heads(q_at + qp.at * Sh::kQ + d * kHalfBytes, &mq, d * 64, u.head, u.token, bar);
+                qp.next();
+                ++q_filled;
+                for (int j = 0; j < chunks; ++j) {
+                    if (!w.wait(smem_addr(&bars.kv_empty[kp.at]), kp.parity ^ 1u)) return false;
+                    bar = smem_addr(&bars.kv_full[kp.at]);
+                    mbar_arrive_expect_tx(bar, Sh::kKv + a.waits.extra);
+                    for (int d = 0; d < Sh::kHalves; ++d) {
+                        const uint32_t to = kv_at + kp.at * Sh::kKv + d * Sh::kKeyHalf;
+                        tma_load_heads(to, &mk, d * 64, u.kv_head, u.key + j * KEYS, bar);
+                        tma_load_heads(to + Sh::kK, &mv, d * 64, u.kv_head, u.key + j * KEYS, bar);
+                    }
+                    kp.next();
+                    ++kv_filled;
+                }
+                return true;
+            });
+        }
     } else if (warp == kIssuer) {
         if (elect_one()) {
             Place<QS> qp;
             Place<KS> kp;
             // what a group's weights will multiply: there, first, last, turn of p_full, parity,
             // blocks of 16 keys, stage
-            uint32_t pending[2] = {0, 0}, turns = 0;
+            uint32_t pending[GROUPS] = {}, turns = 0;
+            auto of = [&](int g) {
+                uint32_t p = 0;
+#pragma unroll
+                for (int i = 0; i < GROUPS; ++i) p = i == g ? pending[i] : p;
+                return p;
+            };
+            auto put = [&](int g, uint32_t p) {
+#pragma unroll
+                for (int i = 0; i < GROUPS; ++i) pending[i] = i == g ? p : pending[i];
+            };
             auto sums = [&](int g) {
-                const uint32_t p = g ? pending[1] : pending[0];
+                const uint32_t p = of(g);
                 if (!(p & 1u)) return true;
-                (g ? pending[1] : pending[0]) = 0;
+                put(g, 0);
                 const uint32_t stage = p >> 16, blocks = p >> 8 & 255u;
                 if (!w.wait(smem_addr(&bars.fixed[stage]), p >> 4 & 1u)) return false;
                 if (!w.wait(smem_addr(&bars.p_full[g]), p >> 3 & 1u)) return false;
@@ -211,16 +255,18 @@ k_attend_short(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
                 if (p & 4u) mma_commit<1>(smem_addr(&bars.o_full[g]));
                 return true;
             };
-            Unit u;
             int g = 0;
-            bool ok = true;
-            for (; ok && next_unit(u, false); g ^= 1) {
+            bool ok = units(true, 0, 1, [&](const Unit& u) {
                 const int chunks = chunks_of(u.keys);
+                bool ok = true;
                 for (int j = 0; j < chunks && ok; ++j, kp.next()) {
                     if (!(ok = sums(g))) break;
-                    // the other group's last may hold the place in the ring that this one needs
-                    const uint32_t other = g ? pending[0] : pending[1];
-                    if ((other & 1u) && other >> 16 == kp.at && !(ok = sums(g ^ 1))) break;
+                    // another group's last may hold the place in the ring that this one needs
+                    for (int i = 0; i < GROUPS; ++i) {
+                        const uint32_t other = of(i);
+                        if ((other & 1u) && other >> 16 == kp.at) ok = ok && sums(i);
+                    }
+                    if (!ok) break;
                     if (j == 0 && !(ok = w.wait(smem_addr(&bars.q_full[qp.at]), qp.parity))) break;
                     if (!(ok = w.wait(smem_addr(&bars.kv_full[kp.at]), kp.parity))) break;
                     fence_after_sync();
@@ -239,77 +285,71 @@ k_attend_short(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
                         mma_commit<1>(smem_addr(&bars.q_empty[qp.at]));
                         qp.next();
                     }
-                    (g ? pending[1] : pending[0]) = 1u | (j == 0 ? 2u : 0u) | (j == chunks - 1 ? 4u : 0u) | (turns >> g & 1u) << 3 |
-                                                    kp.parity << 4 | (uint32_t)blocks << 8 | kp.at << 16;
+                    put(g, 1u | (j == 0 ? 2u : 0u) | (j == chunks - 1 ? 4u : 0u) | (turns >> g & 1u) << 3 | kp.parity << 4 |
+                               (uint32_t)blocks << 8 | kp.at << 16);
                     turns ^= 1u << g;
                 }
-            }
-            // the last units', in their order
-            if (ok && (ok = sums(g))) sums(g ^ 1);
+                g = g + 1 == GROUPS ? 0 : g + 1;
+                return ok;
+            });
+            for (int i = 0; i < GROUPS && ok; ++i, g = g + 1 == GROUPS ? 0 : g + 1) ok = sums(g);
         }
-    } else if (warp == kFixer) {
+    } else if (warp >= kFixer) {
         // which keys count; values of those that do not become zeros, because 0 times what they
-        // hold may be a NaN
+        // hold may be a NaN.  The fixers take units by turns, but see every chunk arrive.
         Place<KS> kp;
-        Unit u;
-        bool ok = true;
-        while (ok && next_unit(u, true)) {
+        int it = 0;
+        units(false, 0, 1, [&](const Unit& u) {
             const int chunks = chunks_of(u.keys);
+            const bool own = it++ % Sh::kFixers == warp - kFixer;
+            bool ok = true;
             for (int j = 0; j < chunks && ok; ++j, kp.next()) {
                 const int left = u.keys - j * KEYS, blocks = ((left < KEYS ? left : KEYS) + 15) / 16;
                 uint32_t bits[W];
+                if (own)
 #pragma unroll
-                for (int i = 0; i < W; ++i) {
-                    const int key = i * 32 + lane;
-                    bits[i] = __ballot_sync(
-                        0xFFFFFFFFu, key < left && (a.kv_ids == nullptr || __ldg(a.kv_ids + u.key + (int64_t)j * KEYS + key) >= 0));
-                }
-                if (!(ok = __all_sync(0xFFFFFFFFu, w.wait(smem_addr(&bars.kv_full[kp.at]), kp.parity)))) break;
-                if (lane == 0)
-#pragma unroll
-                    for (int i = 0; i < W; ++i) bars.mask[kp.at][i] = bits[i];
+                    for (int i = 0; i < W; ++i) {
+                        const int key = i * 32 + lane;
+                        bits[i] = __ballot_sync(
+                            0xFFFFFFFFu, key < left && (a.kv_ids == nullptr || __ldg(a.kv_ids + (int64_t)u.key + (int64_t)j * KEYS + key) >= 0));
+                    }
+                ok = __all_sync(0xFFFFFFFFu, w.wait(smem_addr(&bars.kv_full[kp.at]), kp.parity));
+                if (!ok) break;
+                if (!own) continue;
                 bool any = false;
 #pragma unroll
                 for (int i = 0; i < W; ++i) {
-                    const int in = blocks * 16 - i * 32;
-                    any |= in > 0 && (~bits[i] & (in >= 32 ? 0xFFFFFFFFu : (1u << in) - 1u));
-                }
-                if (any) {
-                    const uint32_t at = kv_at + kp.at * Sh::kKv + Sh::kK;
-#pragma unroll 1
-                    for (int i = lane; i < blocks * 16 * 8; i += 32) {
-                        const int row = i >> 3;
-                        uint32_t word = bits[0];
+                    if (lane == 0) bars.mask[kp.at][i] = bits[i];
+                    // a row a lane; of a block of 16 behind the last key the MMAs read nothing
+                    if (i * 32 + lane < blocks * 16 && !((bits[i] >> lane) & 1u)) {
+                        any = true;
+                        const uint32_t at = kv_at + kp.at * Sh::kKv + Sh::kK + (uint32_t)(i * 32 + lane) * 128u;
 #pragma unroll
-                        for (int x = 1; x < W; ++x) word = (row >> 5) == x ? bits[x] : word;
-                        if (!((word >> (row & 31)) & 1u))
+                        for (int d = 0; d < Sh::kHalves; ++d)
 #pragma unroll
-                            for (int d = 0; d < Sh::kHalves; ++d)
-                                asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(at + d * Sh::kKeyHalf + (uint32_t)i * 16u), "r"(0)
+                            for (int x = 0; x < 8; ++x)
+                                asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(at + d * Sh::kKeyHalf + ((x ^ (lane & 7)) << 4)),
+                                             "r"(0)
                                              : "memory");
                     }
-                    fence_proxy_async_smem();
                 }
+                if (__any_sync(0xFFFFFFFFu, any)) fence_proxy_async_smem();
                 __syncwarp();
                 if (lane == 0) mbar_arrive<1>(smem_addr(&bars.fixed[kp.at]));
             }
-        }
-    } else if (warp < kSoftWarps) {
+            return ok;
+        });
+    } else {
         const int group = warp >> 2, quad = warp & 3;
         const uint32_t mine = tmem + ((uint32_t)quad << 21), s_at = mine + s_col(group), o_at = mine + o_col(group),
                        out = out_at + (uint32_t)warp * 32 * 128;
         const float c = a.scale * kLog2e;
         const float2 c2 = make_float2(c, c);
-        Place<KS> kp;
         uint32_t s_turn = 0, o_turn = 0;
-        Unit u;
-        bool ok = true;
-        for (int it = 0; ok && next_unit(u, true); ++it) {
+        units(false, group, GROUPS, [&](const Unit& u) {
+            bool ok = true;
             const int chunks = chunks_of(u.keys);
-            if ((it & 1) != group) {
-                for (int j = 0; j < chunks; ++j) kp.next();
-                continue;
-            }
+            Place<KS> kp{u.place, u.parity};
             float m = -INFINITY, l = 0.f;
             for (int j = 0; j < chunks && ok; ++j, kp.next(), s_turn ^= 1u) {
                 const int left = u.keys - j * KEYS, n = left < KEYS ? left : KEYS;
@@ -319,65 +359,61 @@ k_attend_short(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
                                                  w.wait(smem_addr(&bars.fixed[kp.at]), kp.parity));
                 if (!ok) break;
                 fence_after_sync();
-                // the first C times 32 keys
-                auto weigh = [&](auto count) {
-                    constexpr int C = decltype(count)::value;
-                    float s[C][32];
+                // 32 scores of this row, -infinity for keys that do not count
+                auto scores = [&](float(&s)[32], int x) {
+                    tmem_ld32(s_at + x * 32, s);
+                    const uint32_t bits = bars.mask[kp.at][x];
+                    tmem_wait(s);
+                    if (bits != 0xFFFFFFFFu)
 #pragma unroll
-                    for (int x = 0; x < C; ++x) tmem_ld32(s_at + x * 32, s[x]);
-                    uint32_t bits[C];
-#pragma unroll
-                    for (int x = 0; x < C; ++x) bits[x] = bars.mask[kp.at][x];
-#pragma unroll
-                    for (int x = 0; x < C; ++x) tmem_wait(s[x]);
-                    float high = m;
-#pragma unroll
-                    for (int x = 0; x < C; ++x) {
-                        if (bits[x] != 0xFFFFFFFFu)
-#pragma unroll
-                            for (int y = 0; y < 32; ++y)
-                                if (!((bits[x] >> y) & 1u)) s[x][y] = -INFINITY;
-                        float top = s[x][0];
-#pragma unroll
-                        for (int y = 1; y < 31; y += 2) top = fmaxf(top, fmaxf(s[x][y], s[x][y + 1]));
-                        high = fmaxf(high, fmaxf(top, s[x][31]) * c);
-                    }
-                    const float shrink = m == -INFINITY ? 0.f : ex2(m - high);
-                    m = high;
-                    if (j > 0) {       // s of this chunk came after the MMAs of o
-                        l *= shrink;
-#pragma unroll 1
-                        for (int d = 0; d < DH; d += 32) {
-                            float v[32];
-                            tmem_ld32(o_at + d, v);
-                            tmem_wait(v);
-#pragma unroll
-                            for (int y = 0; y < 32; ++y) v[y] *= shrink;
-                            tmem_st32(o_at + d, *reinterpret_cast<const uint32_t(*)[32]>(&v));
-                        }
-                    }
-                    const float base = m == -INFINITY ? 0.f : m;
-                    const float2 b2 = make_float2(-base, -base);
-                    float2 sum = make_float2(0.f, 0.f);
-                    uint32_t p[C][16];
-#pragma unroll
-                    for (int x = 0; x < C; ++x)
-#pragma unroll
-                        for (int y = 0; y < 32; y += 2) {
-                            float2 e = fma_(make_float2(s[x][y], s[x][y + 1]), c2, b2);
-                            e.x = ex2(e.x);
-                            e.y = ex2(e.y);
-                            sum = add_(sum, e);
-                            p[x][y / 2] = pack2(e, T());
-                        }
-#pragma unroll
-                    for (int x = 0; x < C; ++x) tmem_st16(s_at + x * 16, p[x]);
-                    l += total(sum);
+                        for (int y = 0; y < 32; ++y)
+                            if (!((bits >> y) & 1u)) s[y] = -INFINITY;
                 };
-                if (n <= KEYS / 2)
-                    weigh(std::integral_constant<int, W / 2>());
-                else
-                    weigh(std::integral_constant<int, W>());
+                float high = -INFINITY;
+#pragma unroll 1
+                for (int x = 0; x * 32 < n; ++x) {
+                    float s[32];
+                    scores(s, x);
+                    float top = fmaxf(high, s[0]);
+#pragma unroll
+                    for (int y = 1; y < 31; y += 2) top = fmaxf(top, fmaxf(s[y], s[y + 1]));
+                    high = fmaxf(top, s[31]);
+                }
+                high = fmaxf(high * c, m);
+                const float shrink = m == -INFINITY ? 0.f : ex2(m - high);
+                m = high;
+                if (j > 0) {       // s of this chunk came after the MMAs of o
+                    l *= shrink;
+#pragma unroll 1
+                    for (int d = 0; d < DH; d += 32) {
+                        float v[32];
+                        tmem_ld32(o_at + d, v);
+                        tmem_wait(v);
+#pragma unroll
+                        for (int y = 0; y < 32; ++y) v[y] *= shrink;
+                        tmem_st32(o_at + d, *reinterpret_cast<const uint32_t(*)[32]>(&v));
+                    }
+                }
+                const float base = m == -INFINITY ? 0.f : m;
+                const float2 b2 = make_float2(-base, -base);
+                float2 sum = make_float2(0.f, 0.f);
+                // the weights of 32 keys take 16 columns: always behind the scores still to come
+#pragma unroll 1
+                for (int x = 0; x * 32 < n; ++x) {
+                    float s[32];
+                    scores(s, x);
+                    uint32_t p[16];
+#pragma unroll
+                    for (int y = 0; y < 32; y += 2) {
+                        float2 e = fma_(make_float2(s[y], s[y + 1]), c2, b2);
+                        e.x = ex2(e.x);
+                        e.y = ex2(e.y);
+                        sum = add_(sum, e);
+                        p[y / 2] = pack2(e, T());
+                    }
+                    tmem_st16(s_at + x * 16, p);
+                }
+                l += total(sum);
                 tmem_st_wait();
                 fence_before_sync();
                 __syncwarp();
@@ -387,45 +423,42 @@ k_attend_short(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
                 ok = __all_sync(0xFFFFFFFFu, w.wait(smem_addr(&bars.o_full[group]), o_turn));
                 o_turn ^= 1u;
             }
-            if (!ok) break;
+            if (!ok) return false;
             fence_after_sync();
             const float inv = l == 0.f ? 0.f : 1.f / l;
             const int r = quad * 32 + lane;
-            const int64_t token = u.token + r / pack;
-            const int head = u.head + r % pack;
+            const int64_t token = (int64_t)u.token + (r >> log_pack);
+            const int head = u.head + (r & (pack - 1));
             const bool in = r < u.rows, whole = quad * 32 + 32 <= u.rows && pack <= 32;
             T* to = (T*)o.out + token * o.ld + (int64_t)head * a.dh;
 #pragma unroll 1
-            for (int d = 0; d < DH; d += 64) {
-                float v[2][32];
-                tmem_ld32(o_at + d, v[0]);
-                tmem_ld32(o_at + d + 32, v[1]);
-                tmem_wait(v[0]);
-                tmem_wait(v[1]);
-                if (whole) {
+            for (int d = 0; d < DH; d += 32) {
+                float v[32];
+                tmem_ld32(o_at + d, v);
+                tmem_wait(v);
+                if (whole && (d & 32) == 0) {
                     if (lane == 0) tma_wait_read<0>();
                     __syncwarp();
                 }
 #pragma unroll
-                for (int y = 0; y < 64; y += 8) {
+                for (int y = 0; y < 32; y += 8) {
                     Pack<T, 8> q;
 #pragma unroll
-                    for (int z = 0; z < 4; ++z) {
-                        const float* x = &v[y >> 5][(y & 31) + 2 * z];
-                        q.set(z, chunks > 0 ? mul_(make_float2(x[0], x[1]), make_float2(inv, inv)) : make_float2(0.f, 0.f));
-                    }
+                    for (int z = 0; z < 4; ++z)
+                        q.set(z, chunks > 0 ? mul_(make_float2(v[y + 2 * z], v[y + 2 * z + 1]), make_float2(inv, inv)) : make_float2(0.f, 0.f));
                     if (whole)
-                        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(out + lane * 128 + (((y >> 3) ^ (lane & 7)) << 4)),
+                        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(
+                                         out + lane * 128 + (((((uint32_t)d & 32u) + y) >> 3 ^ (lane & 7)) << 4)),
                                      "r"(q.w.x), "r"(q.w.y), "r"(q.w.z), "r"(q.w.w)
                                      : "memory");
                     else if (in && d + y < a.dh)
                         q.store(to + d + y);
                 }
-                if (whole) {
+                if (whole && (d & 32)) {
                     fence_proxy_async_smem();
                     __syncwarp();
                     if (lane == 0) {
-                        tma_store_heads(&mo, d, u.head, (int)(u.token + quad * 32 / pack), out);
+                        tma_store_heads(&mo, d - 32, u.head, u.token + (quad * 32 >> log_pack), out);
                         tma_commit();
                     }
                 }
@@ -433,7 +466,8 @@ k_attend_short(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
             if (in && o.lse) o.lse[token * a.heads + head] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
             // the next unit's MMAs write o once this group's weights are there
             fence_before_sync();
-        }
+            return true;
+        });
         if (lane == 0) tma_wait_all();
     }
     __syncwarp();
@@ -472,10 +506,12 @@ cudaError_t run(const AttendArgs& a, const AttendOut& o, int pack, cudaStream_t 
     if (e == cudaSuccess) e = make_head_map(&mo, a.type, o.out, a.Tq, a.heads, a.dh, o.ld, pack <= 32 ? pack : 1, pack <= 32 ? 32 / pack : 1);
     if (e == cudaSuccess) e = allow_smem(k_attend_short<T, DH, KEYS>, ShortShape<DH, KEYS>::kSmem);
     if (e != cudaSuccess) return e;
+    int log_pack = 0;
+    while (1 << log_pack < pack) ++log_pack;
     const int64_t units = slots(a.Tq, a.B, pack, 7) * (a.heads / pack);
     const dim3 grid((unsigned)(units < a.num_sms ? units : a.num_sms));
-    return launch_next(k_attend_short<T, DH, KEYS>, grid, dim3(kThreads), ShortShape<DH, KEYS>::kSmem, false, s, mq, mk, mv, mo, a, o, pack,
-                       units);
+    return launch_next(k_attend_short<T, DH, KEYS>, grid, dim3(ShortShape<DH, KEYS>::kThreads), ShortShape<DH, KEYS>::kSmem, false, s, mq, mk, mv, mo,
+                       a, o, log_pack, units);
 }
 
 }  // namespace
