@@ -397,7 +397,7 @@ template <class T, int DH>
 __global__ void __launch_bounds__(128, DH == 128 ? 2 : 3) k_attend_rows(AttendArgs a, AttendGrads g, int64_t n_slots) {
     extern __shared__ __align__(16) uint8_t raw[];
     __shared__ __align__(8) float bias[2][kTileKeys];
-    const int warp = threadIdx.x >> 5, hk = blockIdx.y;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, hk = blockIdx.y;
     const uint32_t base = smem32(raw);
     constexpr uint32_t kBytes = RowTiles<T, DH>::kBytes;
     const Rows<DH> sq{base}, sdo{base + kBytes};
@@ -405,11 +405,37 @@ __global__ void __launch_bounds__(128, DH == 128 ? 2 : 3) k_attend_rows(AttendAr
     auto v_of = [&](int stage) { return Rows<DH>{base + (3 + 2 * stage) * kBytes}; };
     const Arrays<T> at(a, g, hk);
     const float c = a.scale * kLog2e;
-    for (int64_t n = blockIdx.x; n < n_slots; n += gridDim.x) {
-        const Slot slot = slot_of(a.q_offsets, a.B, a.Tq, a.group, kTileLog, n);
+    // slots are looked at 32 at a time, one a lane
+    Slot mine{};
+    uint32_t todo = 0;
+    for (int64_t n0 = blockIdx.x; todo || n0 < n_slots;) {
+        if (!todo) {
+            const int64_t n = n0 + lane * (int64_t)gridDim.x;
+            n0 += 32 * (int64_t)gridDim.x;
+            bool some = n < n_slots;
+            if (some) {
+                uint32_t lo = 0, count = (uint32_t)a.B;
+                while (count > 1) {
+                    const uint32_t half = count / 2;
+                    if (first_slot(a.q_offsets, lo + half, a.B, a.Tq, a.group, kTileLog) <= n) {
+                        lo += half;
+                        count -= half;
+                    } else {
+                        count = half;
+                    }
+                }
+                mine = Slot{lo, n - first_slot(a.q_offsets, lo, a.B, a.Tq, a.group, kTileLog)};
+                some = mine.tile >= 0 && span_of(a.q_offsets, lo, a.B, a.Tq).len * a.group > mine.tile * kTileRows &&
+                       span_of(a.kv_offsets, lo, a.B, a.Tk).len > kTileKeys;
+            }
+            todo = __ballot_sync(0xFFFFFFFFu, some);
+            continue;
+        }
+        const int from = __ffs((int)todo) - 1;
+        todo &= todo - 1;
+        const Slot slot{__shfl_sync(0xFFFFFFFFu, mine.b, from), __shfl_sync(0xFFFFFFFFu, mine.tile, from)};
         const Span qs = span_of(a.q_offsets, slot.b, a.B, a.Tq), ks = span_of(a.kv_offsets, slot.b, a.B, a.Tk);
         const int64_t row0 = slot.tile * kTileRows, left = qs.len * a.group - row0;
-        if (slot.tile < 0 || left <= 0 || ks.len <= kTileKeys) continue;
         const int rows = left < kTileRows ? (int)left : kTileRows;
         const RowOf ro(row0, a.group);
         const RowsAt<const T> q(at.q, qs.at + ro.token, a.ld_q, a.dh), d_out(at.d_out, qs.at + ro.token, g.ld_d_out, a.dh),
@@ -466,6 +492,7 @@ __global__ void __launch_bounds__(128, DH == 128 ? 2 : 3) k_attend_rows(AttendAr
 // How a call runs
 struct Plan {
     bool tc;             // tiles of the tensor cores
+    bool brief;          // the same for many short sequences
     int pack, splits;
     size_t delta_bytes;
 };
@@ -474,6 +501,12 @@ Plan plan_of(const AttendArgs& a) {
     p.pack = tc_pack(a);
     p.tc = a.Tq * p.pack / a.B >= 128 && a.Tk / a.B >= 256;
     p.delta_bytes = p.tc ? padded((size_t)a.Tq * a.heads * 4) : 0;
+    p.brief = !p.tc && p.pack == a.group && a.Tq * a.group / a.B >= 32 && a.Tk / a.B <= kTileKeys && a.Tq * a.group <= 0x7FFFFFFF &&
+              slots(a.Tk, a.B, 1, kTileLog) * a.kv_heads >= 2 * a.num_sms;
+    if (p.brief) {
+        p.splits = 1;
+        return p;
+    }
     // Parts of the rows, where the tiles of keys leave SMs without a CTA
     const int keys = p.tc ? 128 : kTileKeys, rows = p.tc ? 128 : kTileRows;
     const int64_t tiles = a.Tk / keys > a.B ? a.Tk / keys : a.B, ctas = tiles * a.kv_heads;
@@ -486,11 +519,14 @@ Plan plan_of(const AttendArgs& a) {
 }
 
 template <class T, int DH>
-cudaError_t run(const AttendArgs& a, const AttendGrads& g, int splits, float* part_dk, float* part_dv, cudaStream_t s) {
+cudaError_t run(const AttendArgs& a, const AttendGrads& g, bool brief, int splits, float* part_dk, float* part_dv, cudaStream_t s) {
     cudaError_t e = allow_smem(k_attend_keys<T, DH>, KeyTiles<T, DH>::kSmem);
     if (e == cudaSuccess) e = allow_smem(k_attend_rows<T, DH>, RowTiles<T, DH>::kSmem);
     if (e != cudaSuccess) return e;
-    e = launch_next(k_attend_keys<T, DH>, dim3((unsigned)slots(a.Tk, a.B, 1, kTileLog), (unsigned)a.kv_heads, (unsigned)splits), dim3(128),
+    if (brief)
+        e = launch_attend_grad_short(a, g, s);
+    else
+        e = launch_next(k_attend_keys<T, DH>, dim3((unsigned)slots(a.Tk, a.B, 1, kTileLog), (unsigned)a.kv_heads, (unsigned)splits), dim3(128),
                     KeyTiles<T, DH>::kSmem, false, s, a, g, splits, part_dk, part_dv);
     if (e != cudaSuccess || a.Tk <= kTileKeys || a.Tq == 0) return e;
     const int64_t n = slots(a.Tq, a.B, a.group, kTileLog), most = (3 * a.num_sms + a.kv_heads - 1) / a.kv_heads;
@@ -513,9 +549,9 @@ cudaError_t launch_attend_grad(const AttendArgs& a, const AttendGrads& g, uint8_
     auto go = [&](auto t) {
         using T = decltype(t);
         const cudaError_t e = p.tc           ? launch_attend_grad_tc(a, g, p.pack, p.splits, delta, part_dk, part_dv, s)
-                              : a.dh <= 32 ? run<T, 32>(a, g, p.splits, part_dk, part_dv, s)
-                              : a.dh <= 64 ? run<T, 64>(a, g, p.splits, part_dk, part_dv, s)
-                                           : run<T, 128>(a, g, p.splits, part_dk, part_dv, s);
+                              : a.dh <= 32 ? run<T, 32>(a, g, p.brief, p.splits, part_dk, part_dv, s)
+                              : a.dh <= 64 ? run<T, 64>(a, g, p.brief, p.splits, part_dk, part_dv, s)
+                                           : run<T, 128>(a, g, p.brief, p.splits, part_dk, part_dv, s);
         if (e != cudaSuccess || p.splits == 1 || a.Tk == 0) return e;
         return launch_next(k_attend_keys_join<T>, dim3((unsigned)((a.Tk * a.kv_heads * a.dh + 1023) / 1024), 2u), dim3(256), 0, false, s,
                            a, g, p.splits, (const float*)part_dk, (const float*)part_dv);

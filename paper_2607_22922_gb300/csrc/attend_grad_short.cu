@@ -1,0 +1,641 @@
+// The gradient of attention of many short sequences on the tensor cores (ifvs_attend_grad).
+//
+// A unit is 64 keys of one sequence and head with all rows of their group, tiles of 128:
+//   s = q k^T, dp = do v^T; a thread makes its row's p and ds, which go to shared memory as
+//   16-bit tiles [rows][keys]; dv += p^T do, dk += ds^T q (the tiles along their rows), dq =
+//   ds k (the same tile of ds along its keys)
+// Where the unit has all of a sequence's keys, the softmax's sum and delta come from the row
+// itself and dq is complete; else from the forward call's lse and output, and k_attend_rows
+// makes dq.  Groups of four warps take one unit each and go through them tile by tile by
+// turns, so that one's exponentials run beside the other's MMAs.
+#include "attend_tc.cuh"
+
+namespace ifvs {
+
+namespace {
+
+constexpr int kBatch = 32, kKeys = 64;
+constexpr uint32_t kWeights = 128 * 128;         // a tile of p or ds
+
+template <int DH>
+struct BriefShape {
+    static constexpr int kHalves = DH / 64;
+    static constexpr int kGroups = DH == 64 ? 2 : 1;
+    static constexpr int kColumns = 64 + 3 * DH;                         // of TMEM: s, dp (then dq), dv, dk
+    static constexpr int kSoft = 4 * kGroups, kLoader = kSoft, kIssuer = kSoft + 1, kKeyFixer = kSoft + 2, kRowFixer = kSoft + 3,
+                         kFinder = kSoft + 4, kThreads = (kFinder + 1) * 32;
+    static constexpr uint32_t kQ = kHalves * kHalfBytes, kStage = 2 * kQ;            // queries and gradients
+    static constexpr uint32_t kKeyHalf = kKeys * 128, kK = kHalves * kKeyHalf, kKv = 2 * kK;
+    static constexpr int kQs = DH == 128 ? 2 : 3, kKvs = kGroups + 1;
+    // the tiles of weights first: an operand of 128 rows reaches into what follows its 64 keys
+    static constexpr size_t kSmem = 1024 + kGroups * 2 * kWeights + kQs * kStage + kKvs * kKv;
+};
+
+struct BriefUnit {
+    int token, key;          // the first row's token, the first key
+    int rows;
+    int16_t keys, kv_head;
+    uint8_t place, parity;   // in the ring of keys
+    uint8_t alone;           // whether these are all keys of the sequence
+};
+
+template <int QS, int KS, int GROUPS>
+struct BriefBars {
+    uint64_t batch_full[2], batch_empty[2], q_full[QS], q_fixed[QS], q_empty[QS], kv_full[KS], kv_fixed[KS], kv_empty[KS], s_full[GROUPS],
+        p_full[GROUPS], dq_full[GROUPS], dq_read[GROUPS], drain;
+    BriefUnit units[2][kBatch];
+    int count[2];            // -1: there are no more
+    uint32_t mask[KS][2];
+    uint32_t tmem;
+    int dead;
+};
+
+template <int N>
+struct Spot {
+    uint32_t at = 0, parity = 0;
+    __device__ __forceinline__ void next() {
+        if (++at == N) {
+            at = 0;
+            parity ^= 1u;
+        }
+    }
+};
+
+// An operand whose 64-element blocks (M or N) lie `block` bytes apart, its sum along the rows
+__device__ __forceinline__ uint64_t along_rows(uint32_t addr, uint32_t block) {
+    return (uint64_t)((addr & 0x3FFFFu) >> 4) | ((uint64_t)(block >> 4) << 16) | ((uint64_t)(1024u >> 4) << 32) | (1ull << 46) |
+           (2ull << 61);
+}
+
+template <class T, int DH>
+__global__ void __launch_bounds__(BriefShape<DH>::kThreads, 1)
+k_grad_short(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mdo, const __grid_constant__ CUtensorMap mk,
+             const __grid_constant__ CUtensorMap mv, const __grid_constant__ CUtensorMap mdq, AttendArgs a, AttendGrads g, int log_pack,
+             int64_t n_units) {
+    using Sh = BriefShape<DH>;
+    constexpr int QS = Sh::kQs, KS = Sh::kKvs, GROUPS = Sh::kGroups, H = Sh::kHalves;
+    constexpr int kLoader = Sh::kLoader, kIssuer = Sh::kIssuer, kKeyFixer = Sh::kKeyFixer, kRowFixer = Sh::kRowFixer, kFinder = Sh::kFinder;
+    constexpr bool kF16 = std::is_same_v<T, __half>;
+    __shared__ __align__(16) BriefBars<QS, KS, GROUPS> bars;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, pack = 1 << log_pack;
+    check_offsets(a.q_offsets, a.B, a.Tq, a.waits.err);
+    check_offsets(a.kv_offsets, a.B, a.Tk, a.waits.err);
+    const uint32_t w_at = dynamic_smem(), q_at = w_at + GROUPS * 2 * kWeights, kv_at = q_at + QS * Sh::kStage;
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(smem_addr(&bars.batch_full[i]), 1);
+            mbar_init(smem_addr(&bars.batch_empty[i]), Sh::kSoft + 4);
+        }
+        for (int i = 0; i < QS; ++i) {
+            mbar_init(smem_addr(&bars.q_full[i]), 1);
+            mbar_init(smem_addr(&bars.q_fixed[i]), 1);
+            mbar_init(smem_addr(&bars.q_empty[i]), 1);
+        }
+        for (int i = 0; i < KS; ++i) {
+            mbar_init(smem_addr(&bars.kv_full[i]), 1);
+            mbar_init(smem_addr(&bars.kv_fixed[i]), 1);
+            mbar_init(smem_addr(&bars.kv_empty[i]), 1);
+        }
+        for (int i = 0; i < GROUPS; ++i) {
+            mbar_init(smem_addr(&bars.s_full[i]), 1);
+            mbar_init(smem_addr(&bars.p_full[i]), 4);
+            mbar_init(smem_addr(&bars.dq_full[i]), 1);
+            mbar_init(smem_addr(&bars.dq_read[i]), 4);
+        }
+        mbar_init(smem_addr(&bars.drain), 1);
+        bars.dead = 0;
+        fence_mbar_init();
+    }
+    if (warp == kIssuer) tmem_alloc<1>(smem_addr(&bars.tmem), 512);
+    fence_before_sync();
+    __syncthreads();
+    fence_after_sync();
+    const uint32_t tmem = bars.tmem;
+    const Watch w{&bars.dead, a.waits};
+    auto s_col = [](int i) { return (uint32_t)i * Sh::kColumns; };
+    auto dp_col = [](int i) { return (uint32_t)i * Sh::kColumns + 64u; };
+    auto dv_col = [](int i) { return (uint32_t)i * Sh::kColumns + 64u + DH; };
+    auto dk_col = [](int i) { return (uint32_t)i * Sh::kColumns + 64u + 2u * DH; };
+    int q_filled = 0, kv_filled = 0;             // by the loader's thread
+
+    // tiles that take MMAs
+    auto tiles_of = [](const BriefUnit& u) { return u.keys > 0 ? (u.rows + 127) / 128 : 0; };
+    // f(units, how many) for every bundle of up to GROUPS units of a batch.  idle(): called
+    // before a batch is waited for; the finder may be waiting for a group that waits for this role.
+    auto bundles = [&](bool alone, auto&& idle, auto&& f) {
+        uint32_t b = 0, parity = 0;
+        for (;;) {
+            if (!mbar_try_wait(smem_addr(&bars.batch_full[b]), parity) && !idle()) return false;
+            bool ok = w.wait(smem_addr(&bars.batch_full[b]), parity);
+            if (!alone) ok = __all_sync(0xFFFFFFFFu, ok);
+            const int n = ok ? bars.count[b] : -1;
+            if (n < 0) return ok;
+            for (int i = 0; i < n; i += GROUPS)
+                if (!f(&bars.units[b][i], n - i < GROUPS ? n - i : GROUPS)) return false;
+            if (!alone) __syncwarp();
+            if (alone || lane == 0) mbar_arrive<1>(smem_addr(&bars.batch_empty[b]));
+            b ^= 1u;
+            parity ^= b ^ 1u;
+        }
+    };
+    // f(group, tile, unit) for a bundle's tiles, by turns
+    auto steps = [&](const BriefUnit* u, int n, auto&& f) {
+        int most = 0;
+        for (int i = 0; i < n; ++i) most = max(most, tiles_of(u[i]));
+        for (int t = 0; t < most; ++t)
+            for (int i = 0; i < n; ++i)
+                if (t < tiles_of(u[i]) && !f(i, t, u[i])) return false;
+        return true;
+    };
+
+    auto nothing = [] { return true; };
+
+    if (warp == kFinder) {
+        uint32_t b = 0, parity = 1, place = 0, turn = 0;
+        const uint32_t grid = gridDim.x;
+        for (int64_t round = 0; round * grid < n_units; round += kBatch) {
+            // the CTAs change places from round to round, since what the slots hold may repeat
+            const uint32_t seat = (uint32_t)((blockIdx.x + 37u * (uint32_t)((round + lane) % grid)) % grid);
+            const int64_t mine = (round + lane) * grid + seat;
+            BriefUnit u{};
+            bool real = false;
+            if (mine < n_units) {
+                const uint32_t slot = (uint32_t)(mine / a.kv_heads), y = (uint32_t)(mine - (int64_t)slot * a.kv_heads);
+                uint32_t lo = 0, n = (uint32_t)a.B;
+                while (n > 1) {
+                    const uint32_t half = n / 2;
+                    if (first_slot(a.kv_offsets, lo + half, a.B, a.Tk, 1, 6) <= (int64_t)slot) {
+                        lo += half;
+                        n -= half;
+                    } else {
+                        n = half;
+                    }
+                }
+                const int64_t tile = (int64_t)slot - first_slot(a.kv_offsets, lo, a.B, a.Tk, 1, 6);
+                const Span qs = span_of(a.q_offsets, lo, a.B, a.Tq), ks = span_of(a.kv_offsets, lo, a.B, a.Tk);
+                const int64_t left = ks.len - tile * kKeys;
+                u.token = (int)qs.at;
+                u.key = (int)(ks.at + tile * kKeys);
+                u.rows = (int)(qs.len << log_pack);
+                u.keys = (int16_t)(left < kKeys ? (left < 0 ? 0 : left) : kKeys);
+                u.kv_head = (int16_t)y;
+                u.alone = ks.len <= kKeys;
+                // without keys the first tile still writes dq
+                real = tile >= 0 && (left > 0 || (tile == 0 && u.rows > 0));
+            }
+            const uint32_t there = __ballot_sync(0xFFFFFFFFu, real);
+            const uint32_t loads = __ballot_sync(0xFFFFFFFFu, real && tiles_of(u) > 0), below = (1u << lane) - 1u;
+            const uint32_t at = place + (uint32_t)__popc(loads & below), all = place + (uint32_t)__popc(loads);
+            u.place = (uint8_t)(at % KS);
+            u.parity = (uint8_t)((turn + at / KS) & 1u);
+            turn += all / KS;
+            place = all % KS;
+            if (!__all_sync(0xFFFFFFFFu, w.wait(smem_addr(&bars.batch_empty[b]), parity))) break;
+            if (real) bars.units[b][__popc(there & below)] = u;
+            if (lane == 0) bars.count[b] = __popc(there);
+            __syncwarp();
+            if (lane == 0) mbar_arrive<1>(smem_addr(&bars.batch_full[b]));
+            b ^= 1u;
+            parity ^= b ^ 1u;
+        }
+        if (__all_sync(0xFFFFFFFFu, w.wait(smem_addr(&bars.batch_empty[b]), parity)) && lane == 0) {
+            bars.count[b] = -1;
+            mbar_arrive<1>(smem_addr(&bars.batch_full[b]));
+        }
+    } else if (warp == kLoader) {
+        if (elect_one()) {
+            Spot<QS> qp;
+            Spot<KS> kp;
+            bundles(true, nothing, [&](const BriefUnit* u, int n) {
+                for (int i = 0; i < n; ++i) {
+                    if (tiles_of(u[i]) == 0) continue;
+                    if (!w.wait(smem_addr(&bars.kv_empty[kp.at]), kp.parity ^ 1u)) return false;
+                    const uint32_t bar = smem_addr(&bars.kv_full[kp.at]);
+                    mbar_arrive_expect_tx(bar, Sh::kKv + a.waits.extra);
+                    for (int d = 0; d < H; ++d) {
+                        const uint32_t to = kv_at + kp.at * Sh::kKv + d * Sh::kKeyHalf;
+                        tma_load_heads(to, &mk, d * 64, u[i].kv_head, u[i].key, bar);
+                        tma_load_heads(to + Sh::kK, &mv, d * 64, u[i].kv_head, u[i].key, bar);
+                    }
+                    kp.next();
+                    ++kv_filled;
+                }
+                return steps(u, n, [&](int, int t, const BriefUnit& v) {
+                    if (!w.wait(smem_addr(&bars.q_empty[qp.at]), qp.parity ^ 1u)) return false;
+                    const uint32_t bar = smem_addr(&bars.q_full[qp.at]);
+                    mbar_arrive_expect_tx(bar, Sh::kStage + a.waits.extra);
+                    const int token = v.token + (t * 128 >> log_pack), head = v.kv_head << log_pack;
+                    for (int d = 0; d < H; ++d) {
+                        const uint32_t to = q_at + qp.at * Sh::kStage + d * kHalfBytes;
+                        tma_load_heads(to, &mq, d * 64, head, token, bar);
+                        tma_load_heads(to + Sh::kQ, &mdo, d * 64, head, token, bar);
+                    }
+                    qp.next();
+                    ++q_filled;
+                    return true;
+                });
+            });
+        }
+    } else if (warp == kIssuer) {
+        if (elect_one()) {
+            Spot<QS> qp;
+            const uint32_t id_q = mma_desc(128, DH, kF16, false, true), id_k = mma_desc(128, DH, kF16, true, true);
+            // what waits for a group's weights: there, first and last tile, parity of the unit's
+            // place, blocks of 16 keys, place in the ring of rows, place in that of keys
+            uint32_t pending[GROUPS] = {}, turns = 0, reads = 0;
+            auto of = [&](int i) { return GROUPS == 1 || i == 0 ? pending[0] : pending[GROUPS - 1]; };
+            auto put = [&](int i, uint32_t p) { (GROUPS == 1 || i == 0 ? pending[0] : pending[GROUPS - 1]) = p; };
+            auto sums = [&](int i) {
+                const uint32_t p = of(i);
+                if (!(p & 1u)) return true;
+                put(i, 0);
+                if (!w.wait(smem_addr(&bars.p_full[i]), turns >> i & 1u)) return false;
+                turns ^= 1u << i;
+                fence_after_sync();
+                const uint32_t stage = p >> 16 & 255u, keys = p >> 24, blocks = p >> 8 & 255u;
+                const uint32_t q = q_at + stage * Sh::kStage, k = kv_at + keys * Sh::kKv, weights = w_at + (uint32_t)i * 2 * kWeights;
+                const uint64_t da = along_rows(weights, kWeights), ds = along_rows(weights + kWeights, kWeights);
+                const uint64_t dd = along_rows(q + Sh::kQ, kHalfBytes), dq = along_rows(q, kHalfBytes);
+                const bool more = !(p & 2u);
+#pragma unroll
+                for (int x = 0; x < 8; ++x) {
+                    mma_f16<1>(tmem + dv_col(i), da + x * desc_step(true), dd + x * desc_step(true), id_k, more || x > 0);
+                    mma_f16<1>(tmem + dk_col(i), ds + x * desc_step(true), dq + x * desc_step(true), id_k, more || x > 0);
+                }
+                const uint64_t sa = tile_desc(weights + kWeights, false), kb = along_rows(k, Sh::kKeyHalf);
+                for (uint32_t x = 0; x < blocks; ++x)
+                    mma_f16<1>(tmem + dp_col(i), sa + x * desc_step(false), kb + x * desc_step(true), id_q, x > 0);
+                mma_commit<1>(smem_addr(&bars.dq_full[i]));
+                mma_commit<1>(smem_addr(&bars.q_empty[stage]));
+                if (p & 4u) mma_commit<1>(smem_addr(&bars.kv_empty[keys]));
+                return true;
+            };
+            auto flush = [&] {
+                for (int i = 0; i < GROUPS; ++i)
+                    if (!sums(i)) return false;
+                return true;
+            };
+            const bool ok = bundles(true, flush, [&](const BriefUnit* u, int n) {
+                // the bundle's keys are loaded before its rows: what holds a place that any of
+                // its units needs has to be done first
+                for (int i = 0; i < n; ++i)
+                    for (int x = 0; x < GROUPS; ++x)
+                        if (tiles_of(u[i]) > 0 && (of(x) & 1u) && of(x) >> 24 == u[i].place && !sums(x)) return false;
+                return steps(u, n, [&](int i, int t, const BriefUnit& v) {
+                    if (!sums(i)) return false;
+                    // and so has another group's last whose rows hold the place for these
+                    for (int x = 0; x < GROUPS; ++x)
+                        if ((of(x) & 1u) && (of(x) >> 16 & 255u) == qp.at && !sums(x)) return false;
+                    // dp takes the place of the group's last dq
+                    if (!w.wait(smem_addr(&bars.dq_read[i]), (reads >> i & 1u) ^ 1u)) return false;
+                    reads ^= 1u << i;
+                    if (t == 0 && !w.wait(smem_addr(&bars.kv_fixed[v.place]), v.parity)) return false;
+                    if (!w.wait(smem_addr(&bars.q_full[qp.at]), qp.parity)) return false;
+                    if (!w.wait(smem_addr(&bars.q_fixed[qp.at]), qp.parity)) return false;
+                    fence_after_sync();
+                    const int blocks = (v.keys + 15) / 16;
+                    const uint32_t id_s = mma_desc(128, blocks * 16, kF16, false, false);
+                    const uint32_t q = q_at + qp.at * Sh::kStage, k = kv_at + v.place * Sh::kKv;
+#pragma unroll
+                    for (int d = 0; d < H; ++d) {
+                        const uint64_t qa = tile_desc(q + d * kHalfBytes, false), kb = tile_desc(k + d * Sh::kKeyHalf, false),
+                                       da = tile_desc(q + Sh::kQ + d * kHalfBytes, false),
+                                       vb = tile_desc(k + Sh::kK + d * Sh::kKeyHalf, false);
+#pragma unroll
+                        for (int x = 0; x < 4; ++x) {
+                            mma_f16<1>(tmem + s_col(i), qa + x * desc_step(false), kb + x * desc_step(false), id_s, d + x > 0);
+                            mma_f16<1>(tmem + dp_col(i), da + x * desc_step(false), vb + x * desc_step(false), id_s, d + x > 0);
+                        }
+                    }
+                    mma_commit<1>(smem_addr(&bars.s_full[i]));
+                    put(i, 1u | (t == 0 ? 2u : 0u) | (t == tiles_of(v) - 1 ? 4u : 0u) | (uint32_t)blocks << 8 | qp.at << 16 |
+                               (uint32_t)v.place << 24);
+                    qp.next();
+                    return true;
+                });
+            });
+            if (ok) flush();
+        }
+    } else if (warp == kKeyFixer) {
+        // which keys count; keys and values of those that do not become zeros, because 0 times
+        // what they hold may be a NaN
+        Spot<KS> kp;
+        bundles(false, nothing, [&](const BriefUnit* units, int n) {
+            for (int i = 0; i < n; ++i) {
+                const BriefUnit u = units[i];
+                if (tiles_of(u) == 0) continue;
+                const int blocks = (u.keys + 15) / 16;
+                uint32_t bits[2];
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+                    const int key = x * 32 + lane;
+                    bits[x] = __ballot_sync(0xFFFFFFFFu, key < u.keys && (a.kv_ids == nullptr || __ldg(a.kv_ids + (int64_t)u.key + key) >= 0));
+                }
+                if (!__all_sync(0xFFFFFFFFu, w.wait(smem_addr(&bars.kv_full[kp.at]), kp.parity))) return false;
+                bool any = false;
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+                    if (lane == 0) bars.mask[kp.at][x] = bits[x];
+                    if (x * 32 + lane < blocks * 16 && !((bits[x] >> lane) & 1u)) {
+                        any = true;
+                        const uint32_t at = kv_at + kp.at * Sh::kKv + (uint32_t)(x * 32 + lane) * 128u;
+#pragma unroll
+                        for (int d = 0; d < 2 * H; ++d)
+#pragma unroll
+                            for (int y = 0; y < 8; ++y)
+                                asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(at + d * Sh::kKeyHalf + ((y ^ (lane & 7)) << 4)),
+                                             "r"(0)
+                                             : "memory");
+                    }
+                }
+                if (__any_sync(0xFFFFFFFFu, any)) fence_proxy_async_smem();
+                __syncwarp();
+                if (lane == 0) mbar_arrive<1>(smem_addr(&bars.kv_fixed[kp.at]));
+                kp.next();
+            }
+            return true;
+        });
+    } else if (warp == kRowFixer) {
+        // rows behind the sequence become zeros: whatever their p and ds are, they add nothing
+        Spot<QS> qp;
+        bundles(false, nothing, [&](const BriefUnit* units, int n) {
+            return steps(units, n, [&](int, int t, const BriefUnit& u) {
+                if (!__all_sync(0xFFFFFFFFu, w.wait(smem_addr(&bars.q_full[qp.at]), qp.parity))) return false;
+                const int rows = u.rows - t * 128;
+                if (rows < 128) {
+#pragma unroll 1
+                    for (int r = lane; r < 128; r += 32)
+                        if (r >= rows)
+#pragma unroll
+                            for (int d = 0; d < 2 * H; ++d)
+#pragma unroll
+                                for (int y = 0; y < 8; ++y)
+                                    asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(
+                                                     q_at + qp.at * Sh::kStage + d * kHalfBytes + (uint32_t)r * 128u + ((y ^ (lane & 7)) << 4)),
+                                                 "r"(0)
+                                                 : "memory");
+                    fence_proxy_async_smem();
+                }
+                __syncwarp();
+                if (lane == 0) mbar_arrive<1>(smem_addr(&bars.q_fixed[qp.at]));
+                qp.next();
+                return true;
+            });
+        });
+    } else {
+        const int group = warp >> 2, quad = warp & 3, r = quad * 32 + lane;
+        const uint32_t mine = tmem + ((uint32_t)quad << 21), s_at = mine + s_col(group), dp_at = mine + dp_col(group);
+        const uint32_t p_row = w_at + (uint32_t)group * 2 * kWeights + (uint32_t)r * 128u, staging = p_row - (uint32_t)lane * 128u;
+        const float c = a.scale * kLog2e;
+        const float2 c2 = make_float2(c, c);
+        uint32_t turn = 0;
+        bundles(false, nothing, [&](const BriefUnit* units, int n_units_here) {
+            if (group >= n_units_here) return true;
+            const BriefUnit u = units[group];
+            const int tiles = (u.rows + 127) / 128, head = u.kv_head << log_pack;
+            uint32_t mine_count = 0;         // the keys of this quarter that count; their place may hold others at the end
+            for (int t = 0; t < tiles; ++t) {
+                const int row = t * 128 + r;
+                const bool in = row < u.rows, whole = t * 128 + quad * 32 + 32 <= u.rows && pack <= 32;
+                const int64_t token = (int64_t)u.token + (row >> log_pack);
+                const int my_head = head + (row & (pack - 1));
+                T* to = (T*)g.dq + token * g.ld_dq + (int64_t)my_head * a.dh;
+                if (u.keys == 0) {
+                    if (in)
+                        for (int d = 0; d < a.dh; d += 8) *reinterpret_cast<uint4*>(to + d) = make_uint4(0, 0, 0, 0);
+                    continue;
+                }
+                float lse2 = INFINITY, delta = 0.f;
+                if (!u.alone && in) {
+                    const float v = __ldg(g.lse + token * a.heads + my_head);
+                    if (v != -INFINITY) lse2 = v * kLog2e;
+                    const T *x = (const T*)g.out + token * g.ld_out + (int64_t)my_head * a.dh,
+                            *y = (const T*)g.d_out + token * g.ld_d_out + (int64_t)my_head * a.dh;
+                    float2 sum = make_float2(0.f, 0.f);
+#pragma unroll 2
+                    for (int d = 0; d < a.dh; d += 8) {
+                        Pack<T, 8> p, q;
+                        p.load(x + d);
+                        q.load(y + d);
+#pragma unroll
+                        for (int z = 0; z < 4; ++z) sum = fma_(p.get(z), q.get(z), sum);
+                    }
+                    delta = total(sum);
+                }
+                if (!__all_sync(0xFFFFFFFFu, w.wait(smem_addr(&bars.s_full[group]), turn))) return false;
+                fence_after_sync();
+                const uint32_t bits[2] = {bars.mask[u.place][0], bars.mask[u.place][1]};
+                mine_count = quad ? bits[1] : bits[0];
+                auto masked = [&](float(&s)[32], int x) {
+                    if (bits[x] != 0xFFFFFFFFu)
+#pragma unroll
+                        for (int y = 0; y < 32; ++y)
+                            if (!((bits[x] >> y) & 1u)) s[y] = -INFINITY;
+                };
+                if (u.alone) {
+                    float high = -INFINITY;
+#pragma unroll
+                    for (int x = 0; x < 2; ++x) {
+                        if (x * 32 >= u.keys) break;
+                        float s[32];
+                        tmem_ld32(s_at + x * 32, s);
+                        tmem_wait(s);
+                        masked(s, x);
+                        float top = fmaxf(high, s[0]);
+#pragma unroll
+                        for (int y = 1; y < 31; y += 2) top = fmaxf(top, fmaxf(s[y], s[y + 1]));
+                        high = fmaxf(top, s[31]);
+                    }
+                    high *= c;
+                    const float base = high == -INFINITY ? 0.f : high;
+                    const float2 b2 = make_float2(-base, -base);
+                    float2 l2 = make_float2(0.f, 0.f), d2 = l2;
+#pragma unroll
+                    for (int x = 0; x < 2; ++x) {
+                        if (x * 32 >= u.keys) break;
+                        float s[32], d[32];
+                        tmem_ld32(s_at + x * 32, s);
+                        tmem_ld32(dp_at + x * 32, d);
+                        tmem_wait(s);
+                        tmem_wait(d);
+                        masked(s, x);
+#pragma unroll
+                        for (int y = 0; y < 32; y += 2) {
+                            float2 e = fma_(make_float2(s[y], s[y + 1]), c2, b2);
+                            e.x = ex2(e.x);
+                            e.y = ex2(e.y);
+                            l2 = add_(l2, e);
+                            // columns behind the last block of 16 hold what the MMAs left there
+                            const bool there = x * 32 + y < ((u.keys + 15) & ~15);
+                            d2 = fma_(e, there ? make_float2(d[y], d[y + 1]) : make_float2(0.f, 0.f), d2);
+                        }
+                    }
+                    const float l = total(l2), sum = total(d2);
+                    lse2 = l == 0.f ? INFINITY : base + log2f(l);
+                    delta = l == 0.f ? 0.f : sum / l;
+                }
+                // the tile of p may still be on its way out as the last dq
+                if (lane == 0) tma_wait_read<0>();
+                __syncwarp();
+                const float2 l2 = make_float2(-lse2, -lse2), d2 = make_float2(-delta, -delta);
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+                    if (x * 32 >= u.keys) break;
+                    float s[32], d[32];
+                    tmem_ld32(s_at + x * 32, s);
+                    tmem_ld32(dp_at + x * 32, d);
+                    tmem_wait(s);
+                    tmem_wait(d);
+                    masked(s, x);
+                    uint32_t p[16], ds[16];
+#pragma unroll
+                    for (int y = 0; y < 32; y += 2) {
+                        float2 e = fma_(make_float2(s[y], s[y + 1]), c2, l2);
+                        e.x = ex2(e.x);
+                        e.y = ex2(e.y);
+                        p[y / 2] = pack2(e, T());
+                        ds[y / 2] = pack2(mul_(e, add_(make_float2(d[y], d[y + 1]), d2)), T());
+                    }
+                    // a key that does not count has p = 0; its ds may be a NaN of a row that is not finite
+#pragma unroll
+                    for (int y = 0; y < 4; ++y) {
+                        const uint32_t at = p_row + (((x * 4 + y) ^ (lane & 7)) << 4);
+                        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(p[4 * y]), "r"(p[4 * y + 1]), "r"(p[4 * y + 2]),
+                                     "r"(p[4 * y + 3])
+                                     : "memory");
+                        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at + kWeights), "r"(ds[4 * y]), "r"(ds[4 * y + 1]),
+                                     "r"(ds[4 * y + 2]), "r"(ds[4 * y + 3])
+                                     : "memory");
+                    }
+                }
+                fence_proxy_async_smem();
+                fence_before_sync();
+                __syncwarp();
+                if (lane == 0) mbar_arrive<1>(smem_addr(&bars.p_full[group]));
+                if (!__all_sync(0xFFFFFFFFu, w.wait(smem_addr(&bars.dq_full[group]), turn))) return false;
+                turn ^= 1u;
+                fence_after_sync();
+                if (u.alone)
+#pragma unroll 1
+                    for (int d = 0; d < DH; d += 32) {
+                        float v[32];
+                        tmem_ld32(dp_at + d, v);
+                        tmem_wait(v);
+                        if (whole && (d & 32) == 0) {
+                            if (lane == 0) tma_wait_read<0>();
+                            __syncwarp();
+                        }
+#pragma unroll
+                        for (int y = 0; y < 32; y += 8) {
+                            Pack<T, 8> q;
+#pragma unroll
+                            for (int z = 0; z < 4; ++z)
+                                q.set(z, mul_(make_float2(v[y + 2 * z], v[y + 2 * z + 1]), make_float2(a.scale, a.scale)));
+                            if (whole)
+                                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(
+                                                 p_row + (((((uint32_t)d & 32u) + y) >> 3 ^ (lane & 7)) << 4)),
+                                             "r"(q.w.x), "r"(q.w.y), "r"(q.w.z), "r"(q.w.w)
+                                             : "memory");
+                            else if (in && d + y < a.dh)
+                                q.store(to + d + y);
+                        }
+                        if (whole && (d & 32)) {
+                            fence_proxy_async_smem();
+                            __syncwarp();
+                            if (lane == 0) {
+                                tma_store_heads(&mdq, d - 32, head, u.token + ((t * 128 + quad * 32) >> log_pack), staging);
+                                tma_commit();
+                            }
+                        }
+                    }
+                fence_before_sync();
+                __syncwarp();
+                if (lane == 0) mbar_arrive<1>(smem_addr(&bars.dq_read[group]));
+            }
+            // the unit's sums: a key a lane, in the first two quarters
+            if (quad < 2) {
+                const bool in = r < u.keys, sums = tiles > 0;
+                const bool counts = in && sums && ((mine_count >> lane) & 1u);
+                const int64_t key = (int64_t)u.key + r;
+                T *dk = (T*)g.dk + key * g.ld_dk + (int64_t)u.kv_head * a.dh, *dv = (T*)g.dv + key * g.ld_dv + (int64_t)u.kv_head * a.dh;
+#pragma unroll 1
+                for (int d = 0; d < 2 * DH; d += 32) {
+                    float v[32];
+                    tmem_ld32(mine + dv_col(group) + d, v);
+                    tmem_wait(v);
+                    const int at = d < DH ? d : d - DH;
+                    const float scale = d < DH ? 1.f : a.scale;
+                    if (!in) continue;
+#pragma unroll
+                    for (int y = 0; y < 32; y += 8) {
+                        if (at + y >= a.dh) break;
+                        Pack<T, 8> q;
+#pragma unroll
+                        for (int z = 0; z < 4; ++z)
+                            q.set(z, counts ? make_float2(v[y + 2 * z] * scale, v[y + 2 * z + 1] * scale) : make_float2(0.f, 0.f));
+                        q.store((d < DH ? dv : dk) + at + y);
+                    }
+                }
+            }
+            fence_before_sync();
+            return true;
+        });
+        if (lane == 0) tma_wait_all();
+    }
+    __syncwarp();
+    fence_before_sync();
+    __syncthreads();
+    fence_after_sync();
+    if (*(volatile int*)&bars.dead) {
+        // a wait ran out: wait once more, bounded, for what is in flight
+        const long long begun = clock64();
+        auto bounded = [&](uint32_t bar, uint32_t parity) {
+            while (!mbar_try_wait(bar, parity) && clock64() - begun < a.waits.cycles) {
+            }
+        };
+        if (warp == kLoader) {                   // the counts are the elected thread's
+            for (int i = q_filled > QS ? q_filled - QS : 0; i < q_filled; ++i)
+                bounded(smem_addr(&bars.q_full[i % QS]), (uint32_t)(i / QS) & 1u);
+            for (int i = kv_filled > KS ? kv_filled - KS : 0; i < kv_filled; ++i)
+                bounded(smem_addr(&bars.kv_full[i % KS]), (uint32_t)(i / KS) & 1u);
+        }
+        if (warp == kIssuer && elect_one()) {
+            mma_commit<1>(smem_addr(&bars.drain));
+            bounded(smem_addr(&bars.drain), 0);
+        }
+        __syncwarp();
+        __syncthreads();
+    }
+    if (warp == kIssuer) tmem_free<1>(tmem, 512);
+}
+
+template <class T, int DH>
+cudaError_t run(const AttendArgs& a, const AttendGrads& g, cudaStream_t s) {
+    CUtensorMap mq, mdo, mk, mv, mdq;
+    const int pack = a.group;
+    int log_pack = 0;
+    while (1 << log_pack < pack) ++log_pack;
+    cudaError_t e = make_head_map(&mq, a.type, a.q, a.Tq, a.heads, a.dh, a.ld_q, pack, 128 / pack);
+    if (e == cudaSuccess) e = make_head_map(&mdo, a.type, g.d_out, a.Tq, a.heads, a.dh, g.ld_d_out, pack, 128 / pack);
+    if (e == cudaSuccess) e = make_head_map(&mk, a.type, a.k, a.Tk, a.kv_heads, a.dh, a.ld_k, 1, kKeys);
+    if (e == cudaSuccess) e = make_head_map(&mv, a.type, a.v, a.Tk, a.kv_heads, a.dh, a.ld_v, 1, kKeys);
+    if (e == cudaSuccess) e = make_head_map(&mdq, a.type, g.dq, a.Tq, a.heads, a.dh, g.ld_dq, pack <= 32 ? pack : 1, pack <= 32 ? 32 / pack : 1);
+    if (e == cudaSuccess) e = allow_smem(k_grad_short<T, DH>, BriefShape<DH>::kSmem);
+    if (e != cudaSuccess) return e;
+    const int64_t units = slots(a.Tk, a.B, 1, 6) * a.kv_heads;
+    const dim3 grid((unsigned)(units < a.num_sms ? units : a.num_sms));
+    return launch_next(k_grad_short<T, DH>, grid, dim3(BriefShape<DH>::kThreads), BriefShape<DH>::kSmem, false, s, mq, mdo, mk, mv, mdq, a, g,
+                       log_pack, units);
+}
+
+}  // namespace
+
+cudaError_t launch_attend_grad_short(const AttendArgs& a, const AttendGrads& g, cudaStream_t s) {
+    auto go = [&](auto t) {
+        using T = decltype(t);
+        return a.dh <= 64 ? run<T, 64>(a, g, s) : run<T, 128>(a, g, s);
+    };
+    return a.type == IFVS_T_F16 ? go(__half()) : go(__nv_bfloat16());
+}
+
+}  // namespace ifvs

@@ -114,10 +114,12 @@ k_attend_short(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
 
     auto chunks_of = [](int keys) { return (keys + KEYS - 1) / KEYS; };
     // f(unit) for every step-th unit from the first-th on; by the warp, or (alone) by one of
-    // its threads
-    auto units = [&](bool alone, int first, int step, auto&& f) {
+    // its threads.  idle(): called before a batch is waited for; the finder may be waiting for
+    // a group that waits for this role.
+    auto units = [&](bool alone, int first, int step, auto&& idle, auto&& f) {
         uint32_t b = 0, parity = 0;
         for (;;) {
+            if (!mbar_try_wait(smem_addr(&bars.batch_full[b]), parity) && !idle()) return false;
             bool ok = w.wait(smem_addr(&bars.batch_full[b]), parity);
             if (!alone) ok = __all_sync(0xFFFFFFFFu, ok);
             const int n = ok ? bars.count[b] : -1;
@@ -133,6 +135,8 @@ k_attend_short(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
             parity ^= b ^ 1u;
         }
     };
+
+    auto nothing = [] { return true; };
 
     if (warp == kFinder) {
         const int nh = a.heads >> log_pack;
@@ -197,7 +201,7 @@ k_attend_short(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
         if (elect_one()) {
             Place<QS> qp;
             Place<KS> kp;
-            units(true, 0, 1, [&](const Unit& u) {
+            units(true, 0, 1, nothing, [&](const Unit& u) {
                 const int chunks = chunks_of(u.keys);
                 if (chunks == 0) return true;
                 if (!w.wait(smem_addr(&bars.q_empty[qp.at]), qp.parity ^ 1u)) return false;
@@ -256,7 +260,12 @@ k_attend_short(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
                 return true;
             };
             int g = 0;
-            bool ok = units(true, 0, 1, [&](const Unit& u) {
+            auto flush = [&] {
+                bool ok = true;
+                for (int i = 0; i < GROUPS && ok; ++i) ok = sums((g + i) % GROUPS);     // in the units' order
+                return ok;
+            };
+            const bool done = units(true, 0, 1, flush, [&](const Unit& u) {
                 const int chunks = chunks_of(u.keys);
                 bool ok = true;
                 for (int j = 0; j < chunks && ok; ++j, kp.next()) {
@@ -292,14 +301,14 @@ k_attend_short(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
                 g = g + 1 == GROUPS ? 0 : g + 1;
                 return ok;
             });
-            for (int i = 0; i < GROUPS && ok; ++i, g = g + 1 == GROUPS ? 0 : g + 1) ok = sums(g);
+            if (done) flush();
         }
     } else if (warp >= kFixer) {
         // which keys count; values of those that do not become zeros, because 0 times what they
         // hold may be a NaN.  The fixers take units by turns, but see every chunk arrive.
         Place<KS> kp;
         int it = 0;
-        units(false, 0, 1, [&](const Unit& u) {
+        units(false, 0, 1, nothing, [&](const Unit& u) {
             const int chunks = chunks_of(u.keys);
             const bool own = it++ % Sh::kFixers == warp - kFixer;
             bool ok = true;
@@ -346,7 +355,7 @@ k_attend_short(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
         const float c = a.scale * kLog2e;
         const float2 c2 = make_float2(c, c);
         uint32_t s_turn = 0, o_turn = 0;
-        units(false, group, GROUPS, [&](const Unit& u) {
+        units(false, group, GROUPS, nothing, [&](const Unit& u) {
             bool ok = true;
             const int chunks = chunks_of(u.keys);
             Place<KS> kp{u.place, u.parity};

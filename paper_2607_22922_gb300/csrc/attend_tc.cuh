@@ -72,6 +72,8 @@ cudaError_t launch_attend_tc(const AttendArgs& a, const AttendOut& o, int pack, 
                              cudaStream_t s);
 // wide: 128 keys at a time instead of 64
 cudaError_t launch_attend_short(const AttendArgs& a, const AttendOut& o, int pack, bool wide, cudaStream_t s);
+// dk and dv, and dq of sequences of up to 64 keys; groups of a power of two up to 128 heads
+cudaError_t launch_attend_grad_short(const AttendArgs& a, const AttendGrads& g, cudaStream_t s);
 // delta: [Tq][heads] floats of workspace
 cudaError_t launch_attend_grad_tc(const AttendArgs& a, const AttendGrads& g, int pack, int splits, float* delta, float* part_dk,
                                   float* part_dv, cudaStream_t s);

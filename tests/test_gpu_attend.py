@@ -191,6 +191,9 @@ def _ragged(n, low, high, seed):
     (120, (60, 70), (40, 300), 6, 2, 72),
     (300, (1, 3), (1, 40), 64, 1, 64),
     (170, (120, 120), (16, 16), 8, 2, 8),
+    (418, (64, 64), (20, 20), 8, 8, 64),      # units of a CTA: one more than are found together, in the forward pass
+    (500, (32, 40), (16, 16), 8, 8, 64),      # and in the gradient
+    (900, (0, 90), (0, 9), 1, 1, 16),
 ])
 def test_many_sequences(layers, type_, B, q, k, H, Hk, d):
     _check(layers, *_args(_ragged(B, *q, 1), _ragged(B, *k, 2), H, Hk, d, TYPES[type_], seed=B, fused=True, padding=0.04))
