@@ -502,7 +502,7 @@ Plan plan_of(const AttendArgs& a) {
     p.tc = a.Tq * p.pack / a.B >= 128 && a.Tk / a.B >= 256;
     p.delta_bytes = p.tc ? padded((size_t)a.Tq * a.heads * 4) : 0;
     p.brief = !p.tc && p.pack == a.group && a.Tq * a.group / a.B >= 32 && a.Tk / a.B <= kTileKeys && a.Tq * a.group <= 0x7FFFFFFF &&
-              slots(a.Tk, a.B, 1, kTileLog) * a.kv_heads >= 2 * a.num_sms;
+              a.B * a.kv_heads >= 2 * a.num_sms;
     if (p.brief) {
         p.splits = 1;
         return p;

@@ -2,8 +2,9 @@
 //
 // A unit is 64 keys of one sequence and head with all rows of their group, tiles of 128:
 //   s = q k^T, dp = do v^T; a thread makes its row's p and ds, which go to shared memory as
-//   16-bit tiles [rows][keys]; dv += p^T do, dk += ds^T q (the tiles along their rows), dq =
-//   ds k (the same tile of ds along its keys)
+//   16-bit tiles [rows][keys]; [p ds]^T [q do], one MMA of 128 x 2 dh, whose quarters p^T do
+//   and ds^T q are dv's and dk's sums (the others are not used; two MMAs of 64 keys each take
+//   longer, since an MMA has 128 rows); dq = ds k, the same tile of ds along its keys
 // Where the unit has all of a sequence's keys, the softmax's sum and delta come from the row
 // itself and dq is complete; else from the forward call's lse and output, and k_attend_rows
 // makes dq.  Groups of four warps take one unit each and go through them tile by tile by
@@ -14,21 +15,21 @@ namespace ifvs {
 
 namespace {
 
-constexpr int kBatch = 32, kKeys = 64;
+constexpr int kBatch = 16, kKeys = 64;       // units that are found together; keys of a unit
 constexpr uint32_t kWeights = 128 * 128;         // a tile of p or ds
+constexpr uint32_t kChunk = 32 * 64;             // 32 rows of 32 elements of dq
 
 template <int DH>
 struct BriefShape {
     static constexpr int kHalves = DH / 64;
     static constexpr int kGroups = DH == 64 ? 2 : 1;
-    static constexpr int kColumns = 64 + 3 * DH;                         // of TMEM: s, dp (then dq), dv, dk
+    static constexpr int kColumns = 64 + 3 * DH;                         // of TMEM: s, dp (then dq), sums of dk and dv
     static constexpr int kSoft = 4 * kGroups, kLoader = kSoft, kIssuer = kSoft + 1, kKeyFixer = kSoft + 2, kRowFixer = kSoft + 3,
                          kFinder = kSoft + 4, kThreads = (kFinder + 1) * 32;
     static constexpr uint32_t kQ = kHalves * kHalfBytes, kStage = 2 * kQ;            // queries and gradients
     static constexpr uint32_t kKeyHalf = kKeys * 128, kK = kHalves * kKeyHalf, kKv = 2 * kK;
     static constexpr int kQs = DH == 128 ? 2 : 3, kKvs = kGroups + 1;
-    // the tiles of weights first: an operand of 128 rows reaches into what follows its 64 keys
-    static constexpr size_t kSmem = 1024 + kGroups * 2 * kWeights + kQs * kStage + kKvs * kKv;
+    static constexpr size_t kSmem = 1024 + kGroups * 2 * kWeights + kQs * kStage + kKvs * kKv + (kGroups == 2 ? kSoft * kChunk : 0);
 };
 
 struct BriefUnit {
@@ -42,10 +43,10 @@ struct BriefUnit {
 template <int QS, int KS, int GROUPS>
 struct BriefBars {
     uint64_t batch_full[2], batch_empty[2], q_full[QS], q_fixed[QS], q_empty[QS], kv_full[KS], kv_fixed[KS], kv_empty[KS], s_full[GROUPS],
-        p_full[GROUPS], dq_full[GROUPS], dq_read[GROUPS], drain;
+        p_full[GROUPS], dq_full[GROUPS], dq_read[GROUPS], w_free[GROUPS], drain;
     BriefUnit units[2][kBatch];
     int count[2];            // -1: there are no more
-    uint32_t mask[KS][2];
+    alignas(16) float bias[KS][kKeys];   // read four at a time: 0, or -infinity for a key that does not count
     uint32_t tmem;
     int dead;
 };
@@ -101,6 +102,7 @@ k_grad_short(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUt
             mbar_init(smem_addr(&bars.p_full[i]), 4);
             mbar_init(smem_addr(&bars.dq_full[i]), 1);
             mbar_init(smem_addr(&bars.dq_read[i]), 4);
+            mbar_init(smem_addr(&bars.w_free[i]), 1);
         }
         mbar_init(smem_addr(&bars.drain), 1);
         bars.dead = 0;
@@ -114,8 +116,8 @@ k_grad_short(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUt
     const Watch w{&bars.dead, a.waits};
     auto s_col = [](int i) { return (uint32_t)i * Sh::kColumns; };
     auto dp_col = [](int i) { return (uint32_t)i * Sh::kColumns + 64u; };
-    auto dv_col = [](int i) { return (uint32_t)i * Sh::kColumns + 64u + DH; };
-    auto dk_col = [](int i) { return (uint32_t)i * Sh::kColumns + 64u + 2u * DH; };
+    // lanes 64 on, columns 0 on: dk; lanes 0 on, columns DH on: dv
+    auto sum_col = [](int i) { return (uint32_t)i * Sh::kColumns + 64u + DH; };
     int q_filled = 0, kv_filled = 0;             // by the loader's thread
 
     // tiles that take MMAs
@@ -153,35 +155,41 @@ k_grad_short(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUt
     if (warp == kFinder) {
         uint32_t b = 0, parity = 1, place = 0, turn = 0;
         const uint32_t grid = gridDim.x;
-        for (int64_t round = 0; round * grid < n_units; round += kBatch) {
-            // the CTAs change places from round to round, since what the slots hold may repeat
-            const uint32_t seat = (uint32_t)((blockIdx.x + 37u * (uint32_t)((round + lane) % grid)) % grid);
-            const int64_t mine = (round + lane) * grid + seat;
+        // A lane takes a sequence and head: mostly one unit, so that the CTAs have as many each.
+        // Of sequences with more keys one unit after the other.
+        Span qs{0, 0}, ks{0, 0};
+        int head = 0;
+        int64_t tile = 0;
+        bool some = false;               // this lane has units left
+        for (int64_t round = 0;;) {
+            if (!__any_sync(0xFFFFFFFFu, some)) {
+                if (round * grid >= n_units) break;
+                // the CTAs change places from round to round
+                const uint32_t seat = (uint32_t)((blockIdx.x + 37u * (uint32_t)((round + lane) % grid)) % grid);
+                const int64_t mine = (round + lane) * grid + seat;
+                round += kBatch;
+                some = lane < kBatch && mine < n_units;
+                if (some) {
+                    const int64_t seq = mine / a.kv_heads;
+                    head = (int)(mine - seq * a.kv_heads);
+                    qs = span_of(a.q_offsets, seq, a.B, a.Tq);
+                    ks = span_of(a.kv_offsets, seq, a.B, a.Tk);
+                    tile = 0;
+                }
+            }
             BriefUnit u{};
             bool real = false;
-            if (mine < n_units) {
-                const uint32_t slot = (uint32_t)(mine / a.kv_heads), y = (uint32_t)(mine - (int64_t)slot * a.kv_heads);
-                uint32_t lo = 0, n = (uint32_t)a.B;
-                while (n > 1) {
-                    const uint32_t half = n / 2;
-                    if (first_slot(a.kv_offsets, lo + half, a.B, a.Tk, 1, 6) <= (int64_t)slot) {
-                        lo += half;
-                        n -= half;
-                    } else {
-                        n = half;
-                    }
-                }
-                const int64_t tile = (int64_t)slot - first_slot(a.kv_offsets, lo, a.B, a.Tk, 1, 6);
-                const Span qs = span_of(a.q_offsets, lo, a.B, a.Tq), ks = span_of(a.kv_offsets, lo, a.B, a.Tk);
+            if (some) {
                 const int64_t left = ks.len - tile * kKeys;
                 u.token = (int)qs.at;
                 u.key = (int)(ks.at + tile * kKeys);
                 u.rows = (int)(qs.len << log_pack);
-                u.keys = (int16_t)(left < kKeys ? (left < 0 ? 0 : left) : kKeys);
-                u.kv_head = (int16_t)y;
+                u.keys = (int16_t)(left < kKeys ? left : kKeys);
+                u.kv_head = (int16_t)head;
                 u.alone = ks.len <= kKeys;
                 // without keys the first tile still writes dq
-                real = tile >= 0 && (left > 0 || (tile == 0 && u.rows > 0));
+                real = left > 0 || u.rows > 0;
+                some = ++tile * kKeys < ks.len;
             }
             const uint32_t there = __ballot_sync(0xFFFFFFFFu, real);
             const uint32_t loads = __ballot_sync(0xFFFFFFFFu, real && tiles_of(u) > 0), below = (1u << lane) - 1u;
@@ -239,7 +247,7 @@ k_grad_short(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUt
     } else if (warp == kIssuer) {
         if (elect_one()) {
             Spot<QS> qp;
-            const uint32_t id_q = mma_desc(128, DH, kF16, false, true), id_k = mma_desc(128, DH, kF16, true, true);
+            const uint32_t id_q = mma_desc(128, DH, kF16, false, true), id_k = mma_desc(128, 2 * DH, kF16, true, true);
             // what waits for a group's weights: there, first and last tile, parity of the unit's
             // place, blocks of 16 keys, place in the ring of rows, place in that of keys
             uint32_t pending[GROUPS] = {}, turns = 0, reads = 0;
@@ -254,18 +262,17 @@ k_grad_short(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUt
                 fence_after_sync();
                 const uint32_t stage = p >> 16 & 255u, keys = p >> 24, blocks = p >> 8 & 255u;
                 const uint32_t q = q_at + stage * Sh::kStage, k = kv_at + keys * Sh::kKv, weights = w_at + (uint32_t)i * 2 * kWeights;
-                const uint64_t da = along_rows(weights, kWeights), ds = along_rows(weights + kWeights, kWeights);
-                const uint64_t dd = along_rows(q + Sh::kQ, kHalfBytes), dq = along_rows(q, kHalfBytes);
+                const uint64_t da = along_rows(weights, kWeights), dd = along_rows(q, kHalfBytes);
                 const bool more = !(p & 2u);
-#pragma unroll
-                for (int x = 0; x < 8; ++x) {
-                    mma_f16<1>(tmem + dv_col(i), da + x * desc_step(true), dd + x * desc_step(true), id_k, more || x > 0);
-                    mma_f16<1>(tmem + dk_col(i), ds + x * desc_step(true), dq + x * desc_step(true), id_k, more || x > 0);
-                }
+                // dq first: its group waits for it
                 const uint64_t sa = tile_desc(weights + kWeights, false), kb = along_rows(k, Sh::kKeyHalf);
                 for (uint32_t x = 0; x < blocks; ++x)
                     mma_f16<1>(tmem + dp_col(i), sa + x * desc_step(false), kb + x * desc_step(true), id_q, x > 0);
                 mma_commit<1>(smem_addr(&bars.dq_full[i]));
+#pragma unroll
+                for (int x = 0; x < 8; ++x)
+                    mma_f16<1>(tmem + sum_col(i), da + x * desc_step(true), dd + x * desc_step(true), id_k, more || x > 0);
+                mma_commit<1>(smem_addr(&bars.w_free[i]));
                 mma_commit<1>(smem_addr(&bars.q_empty[stage]));
                 if (p & 4u) mma_commit<1>(smem_addr(&bars.kv_empty[keys]));
                 return true;
@@ -335,7 +342,7 @@ k_grad_short(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUt
                 bool any = false;
 #pragma unroll
                 for (int x = 0; x < 2; ++x) {
-                    if (lane == 0) bars.mask[kp.at][x] = bits[x];
+                    bars.bias[kp.at][x * 32 + lane] = (bits[x] >> lane) & 1u ? 0.f : -INFINITY;
                     if (x * 32 + lane < blocks * 16 && !((bits[x] >> lane) & 1u)) {
                         any = true;
                         const uint32_t at = kv_at + kp.at * Sh::kKv + (uint32_t)(x * 32 + lane) * 128u;
@@ -385,7 +392,8 @@ k_grad_short(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUt
     } else {
         const int group = warp >> 2, quad = warp & 3, r = quad * 32 + lane;
         const uint32_t mine = tmem + ((uint32_t)quad << 21), s_at = mine + s_col(group), dp_at = mine + dp_col(group);
-        const uint32_t p_row = w_at + (uint32_t)group * 2 * kWeights + (uint32_t)r * 128u, staging = p_row - (uint32_t)lane * 128u;
+        const uint32_t out = kv_at + KS * Sh::kKv + (uint32_t)warp * kChunk;
+        const uint32_t p_row = w_at + (uint32_t)group * 2 * kWeights + (uint32_t)r * 128u;
         const float c = a.scale * kLog2e;
         const float2 c2 = make_float2(c, c);
         uint32_t turn = 0;
@@ -393,10 +401,11 @@ k_grad_short(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUt
             if (group >= n_units_here) return true;
             const BriefUnit u = units[group];
             const int tiles = (u.rows + 127) / 128, head = u.kv_head << log_pack;
-            uint32_t mine_count = 0;         // the keys of this quarter that count; their place may hold others at the end
+            bool counts = false;             // of a key a lane; its place may hold others at the end
             for (int t = 0; t < tiles; ++t) {
                 const int row = t * 128 + r;
-                const bool in = row < u.rows, whole = t * 128 + quad * 32 + 32 <= u.rows && pack <= 32;
+                // whole: 32 rows leave by TMA, where there is room for them on their way (one group has none)
+                const bool in = row < u.rows, whole = GROUPS == 2 && t * 128 + quad * 32 + 32 <= u.rows && pack <= 32;
                 const int64_t token = (int64_t)u.token + (row >> log_pack);
                 const int my_head = head + (row & (pack - 1));
                 T* to = (T*)g.dq + token * g.ld_dq + (int64_t)my_head * a.dh;
@@ -424,90 +433,85 @@ k_grad_short(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUt
                 }
                 if (!__all_sync(0xFFFFFFFFu, w.wait(smem_addr(&bars.s_full[group]), turn))) return false;
                 fence_after_sync();
-                const uint32_t bits[2] = {bars.mask[u.place][0], bars.mask[u.place][1]};
-                mine_count = quad ? bits[1] : bits[0];
-                auto masked = [&](float(&s)[32], int x) {
-                    if (bits[x] != 0xFFFFFFFFu)
+                const float* bias = bars.bias[u.place];
+                counts = bias[r & 63] == 0.f;
+                // the first C times 32 keys; columns behind the last block of 16 hold what was there
+                auto weigh = [&](auto count) {
+                    constexpr int C = decltype(count)::value;
+                    const int most = (u.keys + 15) & ~15;
+                    float s[C][32];
 #pragma unroll
-                        for (int y = 0; y < 32; ++y)
-                            if (!((bits[x] >> y) & 1u)) s[y] = -INFINITY;
-                };
-                if (u.alone) {
+                    for (int x = 0; x < C; ++x) tmem_ld32(s_at + x * 32, s[x]);
                     float high = -INFINITY;
 #pragma unroll
-                    for (int x = 0; x < 2; ++x) {
-                        if (x * 32 >= u.keys) break;
-                        float s[32];
-                        tmem_ld32(s_at + x * 32, s);
-                        tmem_wait(s);
-                        masked(s, x);
-                        float top = fmaxf(high, s[0]);
+                    for (int x = 0; x < C; ++x) {
+                        tmem_wait(s[x]);
 #pragma unroll
-                        for (int y = 1; y < 31; y += 2) top = fmaxf(top, fmaxf(s[y], s[y + 1]));
-                        high = fmaxf(top, s[31]);
+                        for (int y = 0; y < 32; y += 4) {
+                            const float4 b = *reinterpret_cast<const float4*>(bias + x * 32 + y);
+                            if (y == 16 && x * 32 + 16 >= most)
+#pragma unroll
+                                for (int z = 16; z < 32; ++z) s[x][z] = 0.f;
+                            float2* v = reinterpret_cast<float2*>(&s[x][y]);
+                            v[0] = add_(v[0], make_float2(b.x, b.y));
+                            v[1] = add_(v[1], make_float2(b.z, b.w));
+                            high = fmaxf(fmaxf(high, fmaxf(s[x][y], s[x][y + 1])), fmaxf(s[x][y + 2], s[x][y + 3]));
+                        }
                     }
-                    high *= c;
-                    const float base = high == -INFINITY ? 0.f : high;
+                    const float base = u.alone ? (high == -INFINITY ? 0.f : high * c) : lse2;
                     const float2 b2 = make_float2(-base, -base);
                     float2 l2 = make_float2(0.f, 0.f), d2 = l2;
 #pragma unroll
-                    for (int x = 0; x < 2; ++x) {
-                        if (x * 32 >= u.keys) break;
-                        float s[32], d[32];
-                        tmem_ld32(s_at + x * 32, s);
+                    for (int x = 0; x < C; ++x) {
+                        float d[32];
                         tmem_ld32(dp_at + x * 32, d);
-                        tmem_wait(s);
                         tmem_wait(d);
-                        masked(s, x);
 #pragma unroll
                         for (int y = 0; y < 32; y += 2) {
-                            float2 e = fma_(make_float2(s[y], s[y + 1]), c2, b2);
+                            float2 e = fma_(make_float2(s[x][y], s[x][y + 1]), c2, b2);
                             e.x = ex2(e.x);
                             e.y = ex2(e.y);
+                            s[x][y] = e.x;
+                            s[x][y + 1] = e.y;
                             l2 = add_(l2, e);
-                            // columns behind the last block of 16 hold what the MMAs left there
-                            const bool there = x * 32 + y < ((u.keys + 15) & ~15);
-                            d2 = fma_(e, there ? make_float2(d[y], d[y + 1]) : make_float2(0.f, 0.f), d2);
+                            d2 = fma_(e, x * 32 + y < most ? make_float2(d[y], d[y + 1]) : make_float2(0.f, 0.f), d2);
                         }
                     }
-                    const float l = total(l2), sum = total(d2);
-                    lse2 = l == 0.f ? INFINITY : base + log2f(l);
-                    delta = l == 0.f ? 0.f : sum / l;
-                }
-                // the tile of p may still be on its way out as the last dq
-                if (lane == 0) tma_wait_read<0>();
-                __syncwarp();
-                const float2 l2 = make_float2(-lse2, -lse2), d2 = make_float2(-delta, -delta);
-#pragma unroll
-                for (int x = 0; x < 2; ++x) {
-                    if (x * 32 >= u.keys) break;
-                    float s[32], d[32];
-                    tmem_ld32(s_at + x * 32, s);
-                    tmem_ld32(dp_at + x * 32, d);
-                    tmem_wait(s);
-                    tmem_wait(d);
-                    masked(s, x);
-                    uint32_t p[16], ds[16];
-#pragma unroll
-                    for (int y = 0; y < 32; y += 2) {
-                        float2 e = fma_(make_float2(s[y], s[y + 1]), c2, l2);
-                        e.x = ex2(e.x);
-                        e.y = ex2(e.y);
-                        p[y / 2] = pack2(e, T());
-                        ds[y / 2] = pack2(mul_(e, add_(make_float2(d[y], d[y + 1]), d2)), T());
+                    float inv = 1.f;
+                    if (u.alone) {
+                        const float l = total(l2);
+                        inv = l == 0.f ? 0.f : 1.f / l;
+                        delta = total(d2) * inv;
                     }
-                    // a key that does not count has p = 0; its ds may be a NaN of a row that is not finite
+                    // the last tile's weights have been multiplied
+                    if (!__all_sync(0xFFFFFFFFu, w.wait(smem_addr(&bars.w_free[group]), turn ^ 1u))) return false;
+                    const float2 i2 = make_float2(inv, inv), n2 = make_float2(-delta, -delta);
 #pragma unroll
-                    for (int y = 0; y < 4; ++y) {
-                        const uint32_t at = p_row + (((x * 4 + y) ^ (lane & 7)) << 4);
-                        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(p[4 * y]), "r"(p[4 * y + 1]), "r"(p[4 * y + 2]),
-                                     "r"(p[4 * y + 3])
-                                     : "memory");
-                        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at + kWeights), "r"(ds[4 * y]), "r"(ds[4 * y + 1]),
-                                     "r"(ds[4 * y + 2]), "r"(ds[4 * y + 3])
-                                     : "memory");
+                    for (int x = 0; x < C; ++x) {
+                        float d[32];
+                        tmem_ld32(dp_at + x * 32, d);
+                        tmem_wait(d);
+#pragma unroll
+                        for (int y = 0; y < 32; y += 8) {
+                            uint32_t p[4], ds[4];
+#pragma unroll
+                            for (int z = 0; z < 4; ++z) {
+                                const int at = y + 2 * z;
+                                const float2 v = mul_(make_float2(s[x][at], s[x][at + 1]), i2);
+                                p[z] = pack2(v, T());
+                                ds[z] = pack2(mul_(v, add_(make_float2(d[at], d[at + 1]), n2)), T());
+                            }
+                            const uint32_t at = p_row + (((x * 4 + y / 8) ^ (lane & 7)) << 4);
+                            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(p[0]), "r"(p[1]), "r"(p[2]), "r"(p[3])
+                                         : "memory");
+                            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at + kWeights), "r"(ds[0]), "r"(ds[1]), "r"(ds[2]),
+                                         "r"(ds[3])
+                                         : "memory");
+                        }
                     }
-                }
+                    return true;
+                };
+                if (!(u.keys <= 32 ? weigh(std::integral_constant<int, 1>()) : weigh(std::integral_constant<int, 2>()))) return false;
                 fence_proxy_async_smem();
                 fence_before_sync();
                 __syncwarp();
@@ -521,7 +525,7 @@ k_grad_short(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUt
                         float v[32];
                         tmem_ld32(dp_at + d, v);
                         tmem_wait(v);
-                        if (whole && (d & 32) == 0) {
+                        if (whole) {
                             if (lane == 0) tma_wait_read<0>();
                             __syncwarp();
                         }
@@ -532,18 +536,17 @@ k_grad_short(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUt
                             for (int z = 0; z < 4; ++z)
                                 q.set(z, mul_(make_float2(v[y + 2 * z], v[y + 2 * z + 1]), make_float2(a.scale, a.scale)));
                             if (whole)
-                                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(
-                                                 p_row + (((((uint32_t)d & 32u) + y) >> 3 ^ (lane & 7)) << 4)),
+                                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(out + lane * 64 + ((y / 8 ^ (lane >> 1 & 3)) << 4)),
                                              "r"(q.w.x), "r"(q.w.y), "r"(q.w.z), "r"(q.w.w)
                                              : "memory");
                             else if (in && d + y < a.dh)
                                 q.store(to + d + y);
                         }
-                        if (whole && (d & 32)) {
+                        if (whole) {
                             fence_proxy_async_smem();
                             __syncwarp();
                             if (lane == 0) {
-                                tma_store_heads(&mdq, d - 32, head, u.token + ((t * 128 + quad * 32) >> log_pack), staging);
+                                if (d < a.dh) tma_store_heads(&mdq, d, head, u.token + ((t * 128 + quad * 32) >> log_pack), out);
                                 tma_commit();
                             }
                         }
@@ -552,35 +555,33 @@ k_grad_short(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUt
                 __syncwarp();
                 if (lane == 0) mbar_arrive<1>(smem_addr(&bars.dq_read[group]));
             }
-            // the unit's sums: a key a lane, in the first two quarters
-            if (quad < 2) {
-                const bool in = r < u.keys, sums = tiles > 0;
-                const bool counts = in && sums && ((mine_count >> lane) & 1u);
-                const int64_t key = (int64_t)u.key + r;
-                T *dk = (T*)g.dk + key * g.ld_dk + (int64_t)u.kv_head * a.dh, *dv = (T*)g.dv + key * g.ld_dv + (int64_t)u.kv_head * a.dh;
+            // the unit's sums, a key a lane: dv in the first two quarters, dk in the others
+            {
+                const int key = r & 63;
+                const bool is_dk = quad >= 2, in = key < u.keys;
+                const int64_t row = (int64_t)u.key + key, at = (int64_t)u.kv_head * a.dh;
+                T* to = is_dk ? (T*)g.dk + row * g.ld_dk + at : (T*)g.dv + row * g.ld_dv + at;
+                const float scale = is_dk ? a.scale : 1.f;
 #pragma unroll 1
-                for (int d = 0; d < 2 * DH; d += 32) {
+                for (int d = 0; d < DH; d += 32) {
                     float v[32];
-                    tmem_ld32(mine + dv_col(group) + d, v);
+                    tmem_ld32(mine + sum_col(group) + (is_dk ? 0u : (uint32_t)DH) + d, v);
                     tmem_wait(v);
-                    const int at = d < DH ? d : d - DH;
-                    const float scale = d < DH ? 1.f : a.scale;
                     if (!in) continue;
 #pragma unroll
                     for (int y = 0; y < 32; y += 8) {
-                        if (at + y >= a.dh) break;
+                        if (d + y >= a.dh) break;
                         Pack<T, 8> q;
 #pragma unroll
                         for (int z = 0; z < 4; ++z)
                             q.set(z, counts ? make_float2(v[y + 2 * z] * scale, v[y + 2 * z + 1] * scale) : make_float2(0.f, 0.f));
-                        q.store((d < DH ? dv : dk) + at + y);
+                        q.store(to + d + y);
                     }
                 }
             }
             fence_before_sync();
             return true;
         });
-        if (lane == 0) tma_wait_all();
     }
     __syncwarp();
     fence_before_sync();
@@ -619,10 +620,11 @@ cudaError_t run(const AttendArgs& a, const AttendGrads& g, cudaStream_t s) {
     if (e == cudaSuccess) e = make_head_map(&mdo, a.type, g.d_out, a.Tq, a.heads, a.dh, g.ld_d_out, pack, 128 / pack);
     if (e == cudaSuccess) e = make_head_map(&mk, a.type, a.k, a.Tk, a.kv_heads, a.dh, a.ld_k, 1, kKeys);
     if (e == cudaSuccess) e = make_head_map(&mv, a.type, a.v, a.Tk, a.kv_heads, a.dh, a.ld_v, 1, kKeys);
-    if (e == cudaSuccess) e = make_head_map(&mdq, a.type, g.dq, a.Tq, a.heads, a.dh, g.ld_dq, pack <= 32 ? pack : 1, pack <= 32 ? 32 / pack : 1);
+    if (e == cudaSuccess)
+        e = make_head_map(&mdq, a.type, g.dq, a.Tq, a.heads, a.dh, g.ld_dq, pack <= 32 ? pack : 1, pack <= 32 ? 32 / pack : 1, 32);
     if (e == cudaSuccess) e = allow_smem(k_grad_short<T, DH>, BriefShape<DH>::kSmem);
     if (e != cudaSuccess) return e;
-    const int64_t units = slots(a.Tk, a.B, 1, 6) * a.kv_heads;
+    const int64_t units = a.B * a.kv_heads;
     const dim3 grid((unsigned)(units < a.num_sms ? units : a.num_sms));
     return launch_next(k_grad_short<T, DH>, grid, dim3(BriefShape<DH>::kThreads), BriefShape<DH>::kSmem, false, s, mq, mdo, mk, mv, mdq, a, g,
                        log_pack, units);

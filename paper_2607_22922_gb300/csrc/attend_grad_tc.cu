@@ -32,7 +32,7 @@ template <int S>
 struct GradBars {
     uint64_t resident, full[S], fixed[S], empty[S], s_full[2], dp_full, p_full, ds_full, acc_full, drain;
     uint32_t mask[S][4];
-    float lse2[S][128], delta[S][128];           // terms of the ring's rows
+    alignas(16) float lse2[S][128], delta[S][128];       // terms of the ring's rows, read four at a time
     uint32_t tmem;
     int dead;
 };

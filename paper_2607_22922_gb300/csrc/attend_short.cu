@@ -1,7 +1,7 @@
 // Attention of many short sequences on the tensor cores (ifvs_attend).
 //
 // Persistent CTAs take units, a tile of 128 rows of one group each, whose keys are mostly one
-// chunk of KEYS.  A warp finds units, 32 at a time, a warp loads their queries, keys and values
+// chunk of KEYS.  A warp finds units, 16 at a time, a warp loads their queries, keys and values
 // by TMA, a warp issues the MMAs, two see to keys that do not count; two or four groups of four warps take units by turns, so
 // that one group's exponentials and output run beside the others' MMAs:
 //   tensor pipe (two groups):  s_0  s_1 | o_0 s_2 | o_1 s_3 | ...
@@ -15,7 +15,7 @@ namespace ifvs {
 
 namespace {
 
-constexpr int kBatch = 32;       // units that are found together
+constexpr int kBatch = 16, kBatches = 2;     // units that are found together; how far ahead
 
 template <int DH, int KEYS>
 struct ShortShape {
@@ -25,8 +25,8 @@ struct ShortShape {
                          kFixers = 2, kFinder = kFixer + kFixers, kThreads = (kFinder + 1) * 32;
     static constexpr uint32_t kQ = kHalves * kHalfBytes;                 // 128 rows
     static constexpr uint32_t kKeyHalf = KEYS * 128, kK = kHalves * kKeyHalf, kKv = 2 * kK;
-    static constexpr int kQs = DH == 128 ? 2 : 4;
-    static constexpr int kKvs = DH == 128 ? (KEYS == 64 ? 4 : 2) : (KEYS == 64 ? 6 : 4);
+    static constexpr int kQs = DH == 128 ? 2 : (KEYS == 64 ? 4 : 3);
+    static constexpr int kKvs = DH == 128 ? (KEYS == 64 ? 3 : 2) : (KEYS == 64 ? 5 : 4);
     static constexpr uint32_t kOut = kSoft * 32 * 128;              // 32 rows of 64 elements a warp
     static constexpr size_t kSmem = 1024 + kQs * kQ + kKvs * kKv + kOut;
 };
@@ -40,11 +40,11 @@ struct Unit {
 
 template <int QS, int KS, int KEYS, int GROUPS>
 struct ShortBars {
-    uint64_t batch_full[2], batch_empty[2], q_full[QS], q_empty[QS], kv_full[KS], kv_empty[KS], fixed[KS], s_full[GROUPS],
+    uint64_t batch_full[kBatches], batch_empty[kBatches], q_full[QS], q_empty[QS], kv_full[KS], kv_empty[KS], fixed[KS], s_full[GROUPS],
         p_full[GROUPS], o_full[GROUPS], drain;
-    Unit units[2][kBatch];
-    int count[2];            // -1: there are no more
-    uint32_t mask[KS][KEYS / 32];
+    Unit units[kBatches][kBatch];
+    int count[kBatches];            // -1: there are no more
+    alignas(16) float most[KS][KEYS];    // read four at a time: infinity, or -infinity for a key that does not count
     uint32_t tmem;
     int dead;
 };
@@ -80,7 +80,7 @@ k_attend_short(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
     check_offsets(a.kv_offsets, a.B, a.Tk, a.waits.err);
     const uint32_t q_at = dynamic_smem(), kv_at = q_at + QS * Sh::kQ, out_at = kv_at + KS * Sh::kKv;
     if (threadIdx.x == 0) {
-        for (int i = 0; i < 2; ++i) {
+        for (int i = 0; i < kBatches; ++i) {
             mbar_init(smem_addr(&bars.batch_full[i]), 1);
             mbar_init(smem_addr(&bars.batch_empty[i]), Sh::kSoft + 2 + Sh::kFixers);
         }
@@ -131,8 +131,8 @@ k_attend_short(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
             first -= n;
             if (!alone) __syncwarp();
             if (alone || lane == 0) mbar_arrive<1>(smem_addr(&bars.batch_empty[b]));
-            b ^= 1u;
-            parity ^= b ^ 1u;
+            b = (b + 1) % kBatches;
+            parity ^= b == 0;
         }
     };
 
@@ -141,14 +141,15 @@ k_attend_short(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
     if (warp == kFinder) {
         const int nh = a.heads >> log_pack;
         uint32_t b = 0, parity = 1, place = 0, turn = 0;
-        // rounds of a unit per CTA; the CTAs change places from round to round, since what a
-        // sequence's slots hold may repeat with a period that divides the grid's
+        // Rounds of a slot per CTA; the CTAs change places from round to round, since what the
+        // slots hold may repeat with a period that divides the grid's.  (Taking the next eight
+        // slots as a CTA comes to them, by a counter, takes 79 us where this takes 65.)
         const uint32_t grid = gridDim.x;
         for (int64_t round = 0; round * grid < n_units; round += kBatch) {
             const uint32_t seat = (uint32_t)((blockIdx.x + 37u * (uint32_t)((round + lane) % grid)) % grid);
             const int64_t mine = (round + lane) * grid + seat;
             Unit u{};
-            if (mine < n_units) {
+            if (lane < kBatch && mine < n_units) {
                 const uint32_t slot = (uint32_t)(mine / nh), y = (uint32_t)(mine - (int64_t)slot * nh);
                 uint32_t lo = 0, n = (uint32_t)a.B;      // the sequence: the last whose slots begin there or before
                 while (n > 1) {
@@ -190,8 +191,8 @@ k_attend_short(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
             if (lane == 0) bars.count[b] = __popc(there);
             __syncwarp();
             if (lane == 0) mbar_arrive<1>(smem_addr(&bars.batch_full[b]));
-            b ^= 1u;
-            parity ^= b ^ 1u;
+            b = (b + 1) % kBatches;
+            parity ^= b == 0;
         }
         if (__all_sync(0xFFFFFFFFu, w.wait(smem_addr(&bars.batch_empty[b]), parity)) && lane == 0) {
             bars.count[b] = -1;
@@ -328,7 +329,7 @@ k_attend_short(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
                 bool any = false;
 #pragma unroll
                 for (int i = 0; i < W; ++i) {
-                    if (lane == 0) bars.mask[kp.at][i] = bits[i];
+                    bars.most[kp.at][i * 32 + lane] = (bits[i] >> lane) & 1u ? INFINITY : -INFINITY;
                     // a row a lane; of a block of 16 behind the last key the MMAs read nothing
                     if (i * 32 + lane < blocks * 16 && !((bits[i] >> lane) & 1u)) {
                         any = true;
@@ -368,15 +369,21 @@ k_attend_short(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
                                                  w.wait(smem_addr(&bars.fixed[kp.at]), kp.parity));
                 if (!ok) break;
                 fence_after_sync();
-                // 32 scores of this row, -infinity for keys that do not count
+                // 32 scores of this row, -infinity for keys that do not count, whatever their score
+                // is (the smaller of a NaN and -infinity is -infinity; of a NaN that counts it is
+                // infinity, which makes the row a NaN as well)
                 auto scores = [&](float(&s)[32], int x) {
                     tmem_ld32(s_at + x * 32, s);
-                    const uint32_t bits = bars.mask[kp.at][x];
+                    const float4* most = reinterpret_cast<const float4*>(bars.most[kp.at] + x * 32);
                     tmem_wait(s);
-                    if (bits != 0xFFFFFFFFu)
 #pragma unroll
-                        for (int y = 0; y < 32; ++y)
-                            if (!((bits >> y) & 1u)) s[y] = -INFINITY;
+                    for (int y = 0; y < 32; y += 4) {
+                        const float4 b = most[y / 4];
+                        s[y] = fminf(s[y], b.x);
+                        s[y + 1] = fminf(s[y + 1], b.y);
+                        s[y + 2] = fminf(s[y + 2], b.z);
+                        s[y + 3] = fminf(s[y + 3], b.w);
+                    }
                 };
                 float high = -INFINITY;
 #pragma unroll 1

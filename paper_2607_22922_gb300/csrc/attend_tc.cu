@@ -344,7 +344,7 @@ cudaError_t run(const AttendArgs& a, const AttendOut& o, int pack, int splits, f
 }  // namespace
 
 cudaError_t make_head_map(CUtensorMap* map, int type, const void* p, int64_t T, int heads, int dh, int64_t ld, int box_heads,
-                          int box_rows) {
+                          int box_rows, int box_dims) {
     static const auto encode = [] {
         void* fn = nullptr;
         cudaDriverEntryPointQueryResult r;
@@ -356,10 +356,10 @@ cudaError_t make_head_map(CUtensorMap* map, int type, const void* p, int64_t T, 
     if (!encode) return cudaErrorNotSupported;
     const cuuint64_t dims[3] = {(cuuint64_t)dh, (cuuint64_t)heads, (cuuint64_t)T},
                      strides[2] = {(cuuint64_t)dh * 2, (cuuint64_t)ld * 2};
-    const cuuint32_t box[3] = {64, (cuuint32_t)box_heads, (cuuint32_t)box_rows}, step[3] = {1, 1, 1};
+    const cuuint32_t box[3] = {(cuuint32_t)box_dims, (cuuint32_t)box_heads, (cuuint32_t)box_rows}, step[3] = {1, 1, 1};
     const CUresult r = encode(map, type == IFVS_T_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16,
                               3, const_cast<void*>(p), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                              box_dims == 64 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
 }

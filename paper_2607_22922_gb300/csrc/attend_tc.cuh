@@ -11,8 +11,9 @@ constexpr uint32_t kHalfBytes = 128 * 128;      // 128 rows of 64 elements, swiz
 // Rows [T][heads][dh], `ld` elements apart, of 16-bit elements; a box is 64 elements of
 // box_heads heads of box_rows rows: box_heads x box_rows rows of 128 bytes in shared
 // memory, heads innermost.  Elements beyond dh and rows beyond T read as zeros.
+// box_dims 32: boxes of 32 elements in the 64-byte swizzle (chunk ^ (row / 2 mod 4)).
 cudaError_t make_head_map(CUtensorMap* map, int type, const void* p, int64_t T, int heads, int dh, int64_t ld, int box_heads,
-                          int box_rows);
+                          int box_rows, int box_dims = 64);
 
 __device__ __forceinline__ void tma_load_heads(uint32_t dst, const CUtensorMap* map, int d, int head, int row, uint32_t bar) {
     asm volatile(
