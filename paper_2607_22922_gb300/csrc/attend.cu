@@ -38,6 +38,9 @@ struct Running {
     __device__ __forceinline__ void begin(const Rows<DH>& from, int row) {
 #pragma unroll
         for (int d = 0; d < DH / 16; ++d) from.a(q[d], row, d * 16);
+        clear();
+    }
+    __device__ __forceinline__ void clear() {
 #pragma unroll
         for (int j = 0; j < DH / 8; ++j)
 #pragma unroll
@@ -151,12 +154,19 @@ k_attend(AttendArgs a, AttendOut o, int log_rows, int splits, float* part_out, f
         return (qs.at + ro.token + r.x) * a.heads + hk * a.group + r.y;
     };
     auto key_in = [&](int64_t key) { return key < ks.len && (a.kv_ids == nullptr || __ldg(a.kv_ids + ks.at + key) >= 0); };
-    // n keys from key0 on to row `to`, and the bias of up to 64 or all
+    // n keys from key0 on to row `to`, and the bias of up to 64 or all.  Whether one counts that
+    // this thread has seen.
     auto load_keys = [&](int64_t key0, int n, int to) {
+        bool some = false;
         const Rows<DH> dk{sm.k.addr(to, 0)}, dv{sm.v.addr(to, 0)};
         load_rows<DH, T>(dk, n, a.dh, a.q, [&](int i) { return key_in(key0 + i) ? k + (ks.at + key0 + i) * a.ld_k : nullptr; });
         load_rows<DH, T>(dv, n, a.dh, a.q, [&](int i) { return key_in(key0 + i) ? v + (ks.at + key0 + i) * a.ld_v : nullptr; });
-        for (int i = threadIdx.x; i < (n + 63) / 64 * 64; i += kWarps * 32) bias[to + i] = i < n && key_in(key0 + i) ? 0.f : -INFINITY;
+        for (int i = threadIdx.x; i < (n + 63) / 64 * 64; i += kWarps * 32) {
+            const bool in = i < n && key_in(key0 + i);
+            bias[to + i] = in ? 0.f : -INFINITY;
+            some = some || in;
+        }
+        return some;
     };
     // this warp's 16 rows from `row` on, to its buffer `to`
     auto load_queries = [&](int row, int to) {
@@ -171,9 +181,11 @@ k_attend(AttendArgs a, AttendOut o, int log_rows, int splits, float* part_out, f
     const float c = a.scale * kLog2e;
     const int g = lane >> 2, two = (lane & 3) * 2;
     Running<T, DH> run;
-    // writes the 16 rows from `row` on, through this warp's buffer `by`
-    auto put = [&](int row, int by) {
+    // writes the 16 rows from `row` on, through this warp's buffer `by`; some: whether a key counts
+    // (queries that are not finite have NaN as their scores, whatever the bias)
+    auto put = [&](int row, int by, bool some) {
         float inv[2], ln[2];
+        if (!some) run.clear();
         run.close(inv, ln);
         if (splits > 1) {
 #pragma unroll
@@ -223,11 +235,11 @@ k_attend(AttendArgs a, AttendOut o, int log_rows, int splits, float* part_out, f
     const int64_t key0 = t0 * kTileKeys, key1 = t1 * kTileKeys < ks.len ? t1 * kTileKeys : ks.len;
     if (key1 - key0 <= kResident) {
         const int n = key1 > key0 ? (int)(key1 - key0) : 0, blocks = (n + 15) / 16;
-        load_keys(key0, blocks * 16, 0);
+        const bool seen = load_keys(key0, blocks * 16, 0);
         load_queries(warp * 16, 0);
         copies_done();
         wait_copies<0>();
-        __syncthreads();
+        const bool some = __syncthreads_or(seen);
         int by = 0;
         for (int row = warp * 16; row < rows; row += kWarps * 16, by ^= 1) {
             if (row + kWarps * 16 < rows) load_queries(row + kWarps * 16, by ^ 1);
@@ -236,18 +248,18 @@ k_attend(AttendArgs a, AttendOut o, int log_rows, int splits, float* part_out, f
             __syncwarp();
             run.begin(sm.q, by * 16);
             for (int at = 0; at < blocks; at += 4) run.step(sm.k, sm.v, at * 16, min(blocks - at, 4), bias, c, at == 0);
-            put(row, by);
+            put(row, by, some);
         }
         return;
     }
     for (int row0 = 0; row0 < rows; row0 += kWarps * 16) {
         const int row = row0 + warp * 16;
         load_queries(row, 0);
-        load_keys(key0, kTileKeys, 0);
+        bool seen = load_keys(key0, kTileKeys, 0);
         copies_done();
         for (int64_t t = t0; t < t1; ++t) {
             const int stage = (int)(t - t0) & 1;
-            if (t + 1 < t1) load_keys((t + 1) * kTileKeys, kTileKeys, (stage ^ 1) * kTileKeys);
+            if (t + 1 < t1) seen |= load_keys((t + 1) * kTileKeys, kTileKeys, (stage ^ 1) * kTileKeys);
             copies_done();
             wait_copies<1>();
             __syncthreads();
@@ -255,7 +267,8 @@ k_attend(AttendArgs a, AttendOut o, int log_rows, int splits, float* part_out, f
             if (row < rows) run.step(sm.k, sm.v, stage * kTileKeys, 4, bias, c, t == t0);
             __syncthreads();
         }
-        if (row < rows) put(row, 0);
+        const bool some = __syncthreads_or(seen);
+        if (row < rows) put(row, 0, some);
     }
 }
 
@@ -300,7 +313,8 @@ Plan plan_of(const AttendArgs& a) {
     Plan p;
     p.pack = tc_pack(a);
     p.tc = a.Tq * p.pack / a.B >= 128 && a.Tk / a.B >= 256;
-    p.brief = !p.tc && a.Tq * p.pack / a.B >= 32 && slots(a.Tq, a.B, p.pack, 7) * (a.heads / p.pack) >= 2 * a.num_sms;
+    // (it counts keys and the places behind them in 32 bits)
+    p.brief = !p.tc && a.Tk <= 0x7FFFFF00 && a.Tq * p.pack / a.B >= 32 && slots(a.Tq, a.B, p.pack, 7) * (a.heads / p.pack) >= 2 * a.num_sms;
     if (p.brief) {
         p.log_rows = 7;
         p.splits = 1;

@@ -273,7 +273,10 @@ __global__ void __launch_bounds__(128, DH == 128 ? 2 : 3) k_attend_keys(AttendAr
     load_rows<DH, T>(sm.k, blocks * 16, a.dh, a.q, [&](int i) { return key_in(i) ? at.k + (ks.at + key0 + i) * a.ld_k : nullptr; });
     load_rows<DH, T>(sm.v, blocks * 16, a.dh, a.q, [&](int i) { return key_in(i) ? at.v + (ks.at + key0 + i) * a.ld_v : nullptr; });
     copies_done();
-    if (threadIdx.x < kTileKeys) bias[threadIdx.x] = key_in(threadIdx.x) ? 0.f : -INFINITY;
+    const bool seen = threadIdx.x < kTileKeys && key_in(threadIdx.x);
+    if (threadIdx.x < kTileKeys) bias[threadIdx.x] = seen ? 0.f : -INFINITY;
+    // where no key counts dq is zero, though what is not finite has NaN as its scores
+    const bool some = __syncthreads_or(seen);
     const float c = a.scale * kLog2e;
     // this warp's share of dk and dv: 16 keys, columns 16 d0 .. 16 d1 - 1
     const int shares = blocks == 1 ? 4 : blocks == 2 ? 2 : 1, block = warp / shares, d0 = warp % shares * (DH / 16) / shares,
@@ -326,7 +329,7 @@ __global__ void __launch_bounds__(128, DH == 128 ? 2 : 3) k_attend_keys(AttendAr
                 times_keys<T, DH>(dq, f, sm.k, blocks);
                 const RowsAt<T> to(at.dq, qs.at + ro.token, g.ld_dq, a.dh);
                 put_rows<T, DH>(dq, a.scale, rows - warp * 16, a.dh, 0, DH / 16, [&](int i) { return to(ro.at(warp * 16 + i)); },
-                                [](int) { return true; });
+                                [&](int) { return some; });
             }
         } else {                 // rows of zeros
             const Operands f = {};
@@ -485,7 +488,7 @@ __global__ void __launch_bounds__(128, DH == 128 ? 2 : 3) k_attend_rows(AttendAr
         }
         const RowsAt<T> to(at.dq, qs.at + ro.token, g.ld_dq, a.dh);
         put_rows<T, DH>(dq, a.scale, rows - warp * 16, a.dh, 0, DH / 16, [&](int i) { return to(ro.at(warp * 16 + i)); },
-                        [](int) { return true; });
+                        [&](int i) { return (i < 8 ? lse2[0] : lse2[1]) != INFINITY; });         // no key counts
     }
 }
 
@@ -501,7 +504,7 @@ Plan plan_of(const AttendArgs& a) {
     p.pack = tc_pack(a);
     p.tc = a.Tq * p.pack / a.B >= 128 && a.Tk / a.B >= 256;
     p.delta_bytes = p.tc ? padded((size_t)a.Tq * a.heads * 4) : 0;
-    p.brief = !p.tc && p.pack == a.group && a.Tq * a.group / a.B >= 32 && a.Tk / a.B <= kTileKeys && a.Tq * a.group <= 0x7FFFFFFF &&
+    p.brief = !p.tc && p.pack == a.group && a.Tq * a.group / a.B >= 32 && a.Tk / a.B <= kTileKeys && a.Tq * a.group <= 0x7FFFFF00 &&
               a.B * a.kv_heads >= 2 * a.num_sms;
     if (p.brief) {
         p.splits = 1;

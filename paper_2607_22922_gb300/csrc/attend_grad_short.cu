@@ -46,6 +46,7 @@ struct BriefBars {
         p_full[GROUPS], dq_full[GROUPS], dq_read[GROUPS], w_free[GROUPS], drain;
     BriefUnit units[2][kBatch];
     int count[2];            // -1: there are no more
+    int some[KS];            // whether a key counts
     alignas(16) float bias[KS][kKeys];   // read four at a time: 0, or -infinity for a key that does not count
     uint32_t tmem;
     int dead;
@@ -340,6 +341,7 @@ k_grad_short(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUt
                 }
                 if (!__all_sync(0xFFFFFFFFu, w.wait(smem_addr(&bars.kv_full[kp.at]), kp.parity))) return false;
                 bool any = false;
+                if (lane == 0) bars.some[kp.at] = (bits[0] | bits[1]) != 0;
 #pragma unroll
                 for (int x = 0; x < 2; ++x) {
                     bars.bias[kp.at][x * 32 + lane] = (bits[x] >> lane) & 1u ? 0.f : -INFINITY;
@@ -435,6 +437,7 @@ k_grad_short(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUt
                 fence_after_sync();
                 const float* bias = bars.bias[u.place];
                 counts = bias[r & 63] == 0.f;
+                const bool some = bars.some[u.place] != 0;       // else dq is zero, whatever the scores are
                 // the first C times 32 keys; columns behind the last block of 16 hold what was there
                 auto weigh = [&](auto count) {
                     constexpr int C = decltype(count)::value;
@@ -534,7 +537,7 @@ k_grad_short(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUt
                             Pack<T, 8> q;
 #pragma unroll
                             for (int z = 0; z < 4; ++z)
-                                q.set(z, mul_(make_float2(v[y + 2 * z], v[y + 2 * z + 1]), make_float2(a.scale, a.scale)));
+                                q.set(z, some ? mul_(make_float2(v[y + 2 * z], v[y + 2 * z + 1]), make_float2(a.scale, a.scale)) : make_float2(0.f, 0.f));
                             if (whole)
                                 asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(out + lane * 64 + ((y / 8 ^ (lane >> 1 & 3)) << 4)),
                                              "r"(q.w.x), "r"(q.w.y), "r"(q.w.z), "r"(q.w.w)

@@ -158,7 +158,7 @@ __global__ void __launch_bounds__(256) k_attend_delta(AttendArgs a, AttendGrads 
 template <class T, int DH>
 __global__ void __launch_bounds__(kThreads, 1)
 k_keys_tc(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mdo, const __grid_constant__ CUtensorMap mk,
-          const __grid_constant__ CUtensorMap mv, AttendArgs a, AttendGrads g, int pack, int splits, const float* __restrict__ delta,
+          const __grid_constant__ CUtensorMap mv, AttendArgs a, AttendGrads g, int log_pack, int splits, const float* __restrict__ delta,
           float* part_dk, float* part_dv) {
     using Sh = GradShape<DH>;
     constexpr int S = Sh::kStages;
@@ -172,11 +172,26 @@ k_keys_tc(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtens
     const int64_t key0 = slot.tile * 128;
     if (slot.tile < 0 || key0 >= ks.len) return;
     // tiles of rows, for every part of the group that shares tiles
-    const int64_t n_rows = qs.len * pack, per_part = (n_rows + 127) / 128, tiles = per_part * (a.group / pack);
+    const int64_t n_rows = qs.len << log_pack, per_part = (n_rows + 127) / 128, tiles = per_part * (a.group >> log_pack);
     const int64_t t0 = tiles * split / splits, t1 = tiles * (split + 1) / splits;
     const int n = (int)(t1 - t0);
-    auto head_of = [&](int64_t t) { return hk * a.group + (int)(t / per_part) * pack; };
-    auto row_of = [&](int64_t t) { return (t % per_part) * 128; };
+    // a tile's first row and its head, one tile after the other: 64-bit divisions, a tile in
+    // the warp that brings the rows' terms, take longer than the tile's MMAs
+    struct Tile {
+        int64_t row;
+        int head;
+    };
+    auto first_tile = [&] {
+        const int64_t part = n > 0 ? t0 / per_part : 0;
+        return Tile{(t0 - part * per_part) * 128, hk * a.group + (int)(part << log_pack)};
+    };
+    auto next_tile = [&](Tile& t) {
+        t.row += 128;
+        if (t.row >= n_rows) {
+            t.row = 0;
+            t.head += 1 << log_pack;
+        }
+    };
 
     const uint32_t k_at = dynamic_smem(), v_at = k_at + Sh::kTile, ring = v_at + Sh::kTile;
     auto q_of = [&](int stage) { return ring + (uint32_t)stage * 2 * Sh::kTile; };
@@ -193,10 +208,11 @@ k_keys_tc(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtens
                 tma_load_heads(v_at + d * kHalfBytes, &mv, d * 64, hk, (int)(ks.at + key0), bar);
             }
             Ring<S> r;
-            for (int j = 0; j < n; ++j, r.next(), ++filled) {
+            Tile tile = first_tile();
+            for (int j = 0; j < n; ++j, r.next(), ++filled, next_tile(tile)) {
                 if (!w.wait(smem_addr(&bars.empty[r.at]), r.parity ^ 1u)) break;
                 const uint32_t full = smem_addr(&bars.full[r.at]);
-                const int head = head_of(t0 + j), token = (int)(qs.at + row_of(t0 + j) / pack);
+                const int head = tile.head, token = (int)(qs.at + (tile.row >> log_pack));
                 mbar_arrive_expect_tx(full, 2 * Sh::kTile + a.waits.extra);
                 for (int d = 0; d < Sh::kHalves; ++d) {
                     tma_load_heads(q_of(r.at) + d * kHalfBytes, &mq, d * 64, head, token, full);
@@ -245,29 +261,33 @@ k_keys_tc(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtens
     } else if (warp == kFixer) {
         // The rows' terms; rows behind the sequence become zeros with lse infinite, so that
         // their p and ds are 0 whatever they held.  A row without keys has lse = -infinity and
-        // no key here that counts: the same.
-        for (int j = 0; j < n; ++j) {
-            const int64_t row0 = row_of(t0 + j);
-            const int head = head_of(t0 + j), rows = n_rows - row0 < 128 ? (int)(n_rows - row0) : 128;
-            float l[4], d[4];
+        // no key here that counts: the same.  The next tile's terms are on their way meanwhile.
+        float l[4], d[4];
+        auto terms = [&](const Tile& t) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const int r = i * 32 + lane;
-                l[i] = INFINITY;
+                const int64_t row = t.row + i * 32 + lane;
+                l[i] = -INFINITY;
                 d[i] = 0.f;
-                if (r < rows) {
-                    const int64_t at = (qs.at + (row0 + r) / pack) * a.heads + head + (int)((row0 + r) % pack);
-                    const float v = __ldg(g.lse + at);
-                    if (v != -INFINITY) l[i] = v * kLog2e;
+                if (row < n_rows) {
+                    const int64_t at = (qs.at + (row >> log_pack)) * a.heads + t.head + ((int)row & ((1 << log_pack) - 1));
+                    l[i] = __ldg(g.lse + at);
                     d[i] = __ldg(delta + at);
                 }
             }
+        };
+        Tile tile = first_tile();
+        if (n > 0) terms(tile);
+        for (int j = 0; j < n; ++j) {
+            const int rows = n_rows - tile.row < 128 ? (int)(n_rows - tile.row) : 128;
             if (!__all_sync(0xFFFFFFFFu, w.wait(smem_addr(&bars.full[j % S]), (uint32_t)(j / S) & 1u))) break;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                bars.lse2[j % S][i * 32 + lane] = -l[i];
+                bars.lse2[j % S][i * 32 + lane] = l[i] == -INFINITY ? -INFINITY : -l[i] * kLog2e;
                 bars.delta[j % S][i * 32 + lane] = -d[i];
             }
+            next_tile(tile);
+            if (j + 1 < n) terms(tile);
             if (rows < 128) {
                 clear_rows(q_of(j % S), Sh::kHalves, [&](int r) { return r < rows; });
                 clear_rows(q_of(j % S) + Sh::kTile, Sh::kHalves, [&](int r) { return r < rows; });
@@ -375,12 +395,12 @@ k_keys_tc(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtens
 template <class T, int DH>
 __global__ void __launch_bounds__(kThreads, 1)
 k_rows_tc(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mdo, const __grid_constant__ CUtensorMap mk,
-          const __grid_constant__ CUtensorMap mv, AttendArgs a, AttendGrads g, int pack, const float* __restrict__ delta) {
+          const __grid_constant__ CUtensorMap mv, AttendArgs a, AttendGrads g, int log_pack, const float* __restrict__ delta) {
     using Sh = GradShape<DH>;
     constexpr int S = Sh::kStages;
     constexpr bool kF16 = std::is_same_v<T, __half>;
     __shared__ __align__(16) GradBars<S> bars;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, h0 = blockIdx.y * pack, hk = h0 / a.group;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, pack = 1 << log_pack, h0 = blockIdx.y * pack, hk = h0 / a.group;
     const Slot slot = slot_of(a.q_offsets, a.B, a.Tq, pack, 7, blockIdx.x);
     const Span qs = span_of(a.q_offsets, slot.b, a.B, a.Tq), ks = span_of(a.kv_offsets, slot.b, a.B, a.Tk);
     const int64_t row0 = slot.tile * 128, left = qs.len * pack - row0;
@@ -396,7 +416,7 @@ k_rows_tc(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtens
     if (warp == kLoader) {
         if (elect_one() && n > 0) {
             const uint32_t bar = smem_addr(&bars.resident);
-            const int token = (int)(qs.at + row0 / pack);
+            const int token = (int)(qs.at + (row0 >> log_pack));
             mbar_arrive_expect_tx(bar, 2 * Sh::kTile + a.waits.extra);
             for (int d = 0; d < Sh::kHalves; ++d) {
                 tma_load_heads(q_at + d * kHalfBytes, &mq, d * 64, h0, token, bar);
@@ -470,8 +490,8 @@ k_rows_tc(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtens
         const int quad = warp & 3, half = warp >> 2, r = quad * 32 + lane;
         const uint32_t mine = tmem + ((uint32_t)quad << 21) + half * 64;
         const float2 c2 = make_float2(a.scale * kLog2e, a.scale * kLog2e);
-        const int64_t token = qs.at + (row0 + r) / pack;
-        const int head = h0 + (int)((row0 + r) % pack);
+        const int64_t token = qs.at + ((row0 + r) >> log_pack);
+        const int head = h0 + ((int)(row0 + r) & (pack - 1));
         float lse2 = -INFINITY, del = 0.f;       // negated; a row without keys: p = 0
         if (r < rows) {
             const float v = __ldg(g.lse + token * a.heads + head);
@@ -561,13 +581,15 @@ cudaError_t run(const AttendArgs& a, const AttendGrads& g, int pack, int splits,
     if (e == cudaSuccess) e = allow_smem(k_keys_tc<T, DH>, GradShape<DH>::kSmem);
     if (e == cudaSuccess) e = allow_smem(k_rows_tc<T, DH>, GradShape<DH>::kSmem);
     if (e != cudaSuccess) return e;
+    int log_pack = 0;
+    while (1 << log_pack < pack) ++log_pack;
     e = launch_next(k_attend_delta<T>, dim3((unsigned)((a.Tq * a.heads + 63) / 64)), dim3(256), 0, false, s, a, g, delta);
     if (e != cudaSuccess) return e;
     e = launch_next(k_keys_tc<T, DH>, dim3((unsigned)slots(a.Tk, a.B, 1, 7), (unsigned)a.kv_heads, (unsigned)splits), dim3(kThreads),
-                    GradShape<DH>::kSmem, false, s, mq, mdo, mk, mv, a, g, pack, splits, (const float*)delta, part_dk, part_dv);
+                    GradShape<DH>::kSmem, false, s, mq, mdo, mk, mv, a, g, log_pack, splits, (const float*)delta, part_dk, part_dv);
     if (e != cudaSuccess) return e;
     return launch_next(k_rows_tc<T, DH>, dim3((unsigned)slots(a.Tq, a.B, pack, 7), (unsigned)(a.heads / pack)), dim3(kThreads),
-                       GradShape<DH>::kSmem, false, s, mq, mdo, mk, mv, a, g, pack, (const float*)delta);
+                       GradShape<DH>::kSmem, false, s, mq, mdo, mk, mv, a, g, log_pack, (const float*)delta);
 }
 
 }  // namespace
