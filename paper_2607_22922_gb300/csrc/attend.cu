@@ -48,13 +48,14 @@ struct Running {
         m[0] = m[1] = -INFINITY;
         l[0] = l[1] = 0.f;
     }
-    // up to 64 keys from row `at` of k and v, `blocks` of 16; bias: 0, or -infinity for a key
+    // up to 16 B keys from row `at` of k and v, `blocks` of 16; bias: 0, or -infinity for a key
     // that does not count, where its score's sum begins.  first: nothing came before.
+    template <int B = kTileKeys / 16>
     __device__ __forceinline__ void step(const Rows<DH>& k, const Rows<DH>& v, int at, int blocks, const float* bias, float c, bool first) {
         const int lane = threadIdx.x & 31;
-        float2 s[kTileKeys / 8][2];
+        float2 s[2 * B][2];
 #pragma unroll
-        for (int j = 0; j < kTileKeys / 16; ++j) {
+        for (int j = 0; j < B; ++j) {
 #pragma unroll
             for (int i = 0; i < 2; ++i)
                 s[2 * j + i][0] = s[2 * j + i][1] = *reinterpret_cast<const float2*>(bias + at + (2 * j + i) * 8 + (lane & 3) * 2);
@@ -71,7 +72,7 @@ struct Running {
         for (int r = 0; r < 2; ++r) {
             float top = fmaxf(s[0][r].x, s[0][r].y);
 #pragma unroll
-            for (int j = 1; j < kTileKeys / 8; ++j) top = fmaxf(top, fmaxf(s[j][r].x, s[j][r].y));
+            for (int j = 1; j < 2 * B; ++j) top = fmaxf(top, fmaxf(s[j][r].x, s[j][r].y));
             top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
             top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
             top = fmaxf(m[r], top * c);
@@ -79,7 +80,7 @@ struct Running {
             const float2 c2 = make_float2(c, c), b2 = make_float2(-base, -base);
             float2 sum = make_float2(0.f, 0.f);
 #pragma unroll
-            for (int j = 0; j < kTileKeys / 8; ++j)
+            for (int j = 0; j < 2 * B; ++j)
                 if (j / 2 < blocks) {
                     float2 e = fma_(s[j][r], c2, b2);
                     e.x = ex2(e.x);
@@ -101,7 +102,7 @@ struct Running {
             m[r] = top;
         }
 #pragma unroll
-        for (int j = 0; j < kTileKeys / 16; ++j)
+        for (int j = 0; j < B; ++j)
             if (j < blocks) {
                 uint32_t p[4];
 #pragma unroll
@@ -272,34 +273,211 @@ k_attend(AttendArgs a, AttendOut o, int log_rows, int splits, float* part_out, f
     }
 }
 
-// Joins the splits of every row, in order: a warp per (token, head).
+// ---- a few rows and many keys ---------------------------------------------------------------
+// The call reads its keys and values once and is bound by that.  A CTA takes up to 16 rows of a
+// group, which one tile of the products holds, and the keys of one split; each of its 4 warps
+// takes every fourth chunk of 32 keys through a ring of its own, two chunks ahead, so that no
+// warp waits for another before the end, where their sums are joined in shared memory.
+// 8 sequences of one query and about 16 400 keys, 8 heads of 64 in float16: 55 us with the
+// join, where 64 keys at a time for the whole CTA take 82.
+constexpr int kFewRows = 16, kFewLog = 4, kFewKeys = 32, kFewStages = 3;
+
+template <class T, int DH>
+struct FewTiles {
+    static constexpr uint32_t kRowBytes = Rows<DH>::kLd * 2, kStage = 2 * kFewKeys * kRowBytes;
+    static constexpr uint32_t kQ = kFewRows * kRowBytes, kWarp = kFewStages * kStage;
+    static constexpr size_t kSmem = kQ + kWarps * kWarp;
+    static constexpr int kCtas = DH == 128 ? 1 : DH == 64 ? 2 : 3;       // of an SM
+};
+
+template <class T, int DH>
+__global__ void __launch_bounds__(kWarps * 32, FewTiles<T, DH>::kCtas)
+k_attend_few(AttendArgs a, AttendOut o, int splits, float* part_out, float* part_lse) {
+    using Sh = FewTiles<T, DH>;
+    constexpr int C = DH / 8;
+    extern __shared__ __align__(16) uint8_t raw[];
+    __shared__ __align__(8) float bias[kWarps][kFewStages][kFewKeys];
+    __shared__ float top[kWarps][kFewRows], sum[kWarps][kFewRows];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, hk = blockIdx.y, split = blockIdx.z;
+    if (splits > 1) start_dependents();
+    check_offsets(a.q_offsets, a.B, a.Tq, a.waits.err);
+    check_offsets(a.kv_offsets, a.B, a.Tk, a.waits.err);
+    const Slot slot = slot_of(a.q_offsets, a.B, a.Tq, a.group, kFewLog, blockIdx.x);
+    const Span qs = span_of(a.q_offsets, slot.b, a.B, a.Tq), ks = span_of(a.kv_offsets, slot.b, a.B, a.Tk);
+    const int64_t row0 = slot.tile << kFewLog, left = qs.len * a.group - row0;
+    if (slot.tile < 0 || left <= 0) return;
+    const int rows = left < kFewRows ? (int)left : kFewRows;
+    const RowOf ro(row0, a.group);
+    const int64_t chunks = (ks.len + kFewKeys - 1) / kFewKeys;
+    const int64_t t0 = chunks * split / splits + warp, t1 = chunks * (split + 1) / splits;
+    const T *k = (const T*)a.k + (int64_t)hk * a.dh, *v = (const T*)a.v + (int64_t)hk * a.dh;
+    const Rows<DH> sq{smem32(raw)};
+    uint8_t* const ring = raw + Sh::kQ;
+    const uint32_t mine = sq.at + Sh::kQ + warp * Sh::kWarp;
+    auto keys_at = [&](int stage) { return Rows<DH>{mine + stage * Sh::kStage}; };
+    auto values_at = [&](int stage) { return Rows<DH>{mine + stage * Sh::kStage + Sh::kStage / 2}; };
+    // whether this lane's key of a chunk counts, asked for one chunk before it is copied
+    auto counts = [&](int64_t t) {
+        const int64_t key = t * kFewKeys + lane;
+        return t < t1 && key < ks.len && (a.kv_ids == nullptr || __ldg(a.kv_ids + ks.at + key) >= 0);
+    };
+    bool next = counts(t0), some = false;
+    auto load = [&](int64_t t, int stage) {
+        if (t < t1) {
+            const uint32_t in = __ballot_sync(0xFFFFFFFFu, next);
+            bias[warp][stage][lane] = next ? 0.f : -INFINITY;
+            some = some || in != 0;
+            const Rows<DH> dk = keys_at(stage), dv = values_at(stage);
+            const T *ck = k + (ks.at + t * kFewKeys) * a.ld_k, *cv = v + (ks.at + t * kFewKeys) * a.ld_v;
+#pragma unroll
+            for (int i = 0; i < kFewKeys * C / 32; ++i) {
+                const int r = (i * 32 + lane) / C, d = (i * 32 + lane) % C * 8;
+                const bool there = ((in >> r) & 1u) && d < a.dh;
+                copy16(dk.addr(r, d), there ? (const void*)(ck + r * a.ld_k + d) : a.q, there);
+                copy16(dv.addr(r, d), there ? (const void*)(cv + r * a.ld_v + d) : a.q, there);
+            }
+            next = counts(t + kWarps);
+        }
+        copies_done();
+    };
+    {
+        const RowsAt<const T> q((const T*)a.q + (int64_t)hk * a.group * a.dh, qs.at + ro.token, a.ld_q, a.dh);
+#pragma unroll
+        for (int i = threadIdx.x; i < kFewRows * C; i += kWarps * 32) {
+            const int r = i / C, d = i % C * 8;
+            const bool in = r < rows && d < a.dh;
+            copy16(sq.addr(r, d), in ? (const void*)(q(ro.at(r)) + d) : a.q, in);
+        }
+        copies_done();
+    }
+    load(t0, 0);
+    load(t0 + kWarps, 1);
+    wait_copies<2>();
+    __syncthreads();
+    Running<T, DH> run;
+    run.begin(sq, 0);
+    const float c = a.scale * kLog2e;
+    int stage = 0;
+    for (int64_t t = t0; t < t1; t += kWarps) {
+        load(t + 2 * kWarps, stage == 0 ? 2 : stage - 1);
+        wait_copies<2>();
+        __syncwarp();
+        run.template step<kFewKeys / 16>(keys_at(stage), values_at(stage), 0, kFewKeys / 16, bias[warp][stage], c, t == t0);
+        __syncwarp();
+        stage = stage == 2 ? 0 : stage + 1;
+    }
+    wait_copies<0>();
+    if (!some) run.clear();          // queries that are not finite have NaN as their scores, whatever the bias
+    __syncthreads();
+    // this warp's sums over its place in shared memory: [16 rows][DH] float32
+    float* const sums = reinterpret_cast<float*>(ring + warp * Sh::kWarp);
+    const int g = lane >> 2, two = (lane & 3) * 2;
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+        float l = run.l[r];
+        l += __shfl_xor_sync(0xFFFFFFFFu, l, 1);
+        l += __shfl_xor_sync(0xFFFFFFFFu, l, 2);
+#pragma unroll
+        for (int j = 0; j < DH / 8; ++j)
+            *reinterpret_cast<float2*>(sums + (g + 8 * r) * DH + j * 8 + two) = make_float2(run.acc[j][2 * r], run.acc[j][2 * r + 1]);
+        if ((lane & 3) == 0) {
+            top[warp][g + 8 * r] = run.m[r];
+            sum[warp][g + 8 * r] = l;
+        }
+    }
+    __syncthreads();
+    // eight threads a row
+    const int row = threadIdx.x >> 3;
+    if (row >= rows) return;
+    float m = -INFINITY, l = 0.f, weight[kWarps];
+#pragma unroll
+    for (int i = 0; i < kWarps; ++i) m = fmaxf(m, top[i][row]);
+    const float base = m == -INFINITY ? 0.f : m;
+#pragma unroll
+    for (int i = 0; i < kWarps; ++i) {
+        weight[i] = ex2(top[i][row] - base);
+        l = fmaf(sum[i][row], weight[i], l);
+    }
+    const float inv = l == 0.f ? 0.f : 1.f / l, ln = l == 0.f ? -INFINITY : m + log2f(l);
+    const int2 at = ro.at(row);
+    const int64_t token = qs.at + ro.token + at.x;
+    const int head = hk * a.group + at.y;
+    const int64_t to = ((int64_t)split * a.Tq + token) * a.heads + head;
+    for (int d = (threadIdx.x & 7) * 8; d < a.dh; d += 64) {
+        float x[8] = {};
+#pragma unroll
+        for (int i = 0; i < kWarps; ++i) {
+            const float4* p = reinterpret_cast<const float4*>(ring + i * Sh::kWarp + (row * DH + d) * 4);
+            const float4 lo = p[0], hi = p[1];
+            x[0] = fmaf(lo.x, weight[i], x[0]);
+            x[1] = fmaf(lo.y, weight[i], x[1]);
+            x[2] = fmaf(lo.z, weight[i], x[2]);
+            x[3] = fmaf(lo.w, weight[i], x[3]);
+            x[4] = fmaf(hi.x, weight[i], x[4]);
+            x[5] = fmaf(hi.y, weight[i], x[5]);
+            x[6] = fmaf(hi.z, weight[i], x[6]);
+            x[7] = fmaf(hi.w, weight[i], x[7]);
+        }
+        if (splits > 1) {
+            float4* p = reinterpret_cast<float4*>(part_out + to * a.dh + d);
+            p[0] = make_float4(x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv);
+            p[1] = make_float4(x[4] * inv, x[5] * inv, x[6] * inv, x[7] * inv);
+        } else {
+            Pack<T, 8> q;
+#pragma unroll
+            for (int z = 0; z < 4; ++z) q.set(z, make_float2(x[2 * z] * inv, x[2 * z + 1] * inv));
+            q.store((T*)o.out + token * o.ld + (int64_t)head * a.dh + d);
+        }
+    }
+    if ((threadIdx.x & 7) == 0) {
+        if (splits > 1)
+            part_lse[to] = ln;
+        else if (o.lse)
+            o.lse[to] = ln * kLn2;
+    }
+}
+
+// Joins the splits of every row, in order: a warp per (token, head), a split's weight (two
+// beyond 32) in a lane.
+constexpr int kMaxSplits = 64;
 template <class T>
 __global__ void __launch_bounds__(256) k_attend_join(AttendArgs a, AttendOut o, int splits, const float* part_out, const float* part_lse) {
     wait_before();
     const int lane = threadIdx.x & 31;
     const int64_t row = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5), n = a.Tq * a.heads;
     if (row >= n) return;
-    float top = -INFINITY;
-    for (int s = 0; s < splits; ++s) top = fmaxf(top, __ldcg(part_lse + s * n + row));
+    float ln[2], top = -INFINITY, l = 0.f;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        ln[i] = i * 32 + lane < splits ? __ldcg(part_lse + (i * 32 + lane) * n + row) : -INFINITY;
+        top = fmaxf(top, ln[i]);
+    }
+#pragma unroll
+    for (int x = 16; x > 0; x >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, x));
     const float base = top == -INFINITY ? 0.f : top;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        ln[i] = ex2(ln[i] - base);
+        l += ln[i];
+    }
+    l = warp_sum(l);
+    const float inv = l == 0.f ? 0.f : 1.f / l;
     const int64_t token = row / a.heads;
     T* out = (T*)o.out + token * o.ld + (row - token * a.heads) * a.dh;
-    float l = 0.f;
-    for (int s = 0; s < splits; ++s) l += ex2(__ldcg(part_lse + s * n + row) - base);
-    const float inv = l == 0.f ? 0.f : 1.f / l;
-    for (int d = lane * 4; d < a.dh; d += 128) {
-        float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-        for (int s = 0; s < splits; ++s) {
-            const float w = ex2(__ldcg(part_lse + s * n + row) - base) * inv;
-            const float4 p = __ldcg(reinterpret_cast<const float4*>(part_out + (s * n + row) * a.dh + d));
-            sum.x = fmaf(w, p.x, sum.x);
-            sum.y = fmaf(w, p.y, sum.y);
-            sum.z = fmaf(w, p.z, sum.z);
-            sum.w = fmaf(w, p.w, sum.w);
-        }
-        *reinterpret_cast<uint2*>(out + d) = make_uint2(pack2(make_float2(sum.x, sum.y), T()), pack2(make_float2(sum.z, sum.w), T()));
+    const int d = lane * 4;      // a head has at most 128 elements
+    float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 8
+    for (int s = 0; s < splits; ++s) {
+        const float w = __shfl_sync(0xFFFFFFFFu, s < 32 ? ln[0] : ln[1], s & 31) * inv;
+        if (d >= a.dh) continue;
+        const float4 p = __ldcg(reinterpret_cast<const float4*>(part_out + (s * n + row) * a.dh + d));
+        sum.x = fmaf(w, p.x, sum.x);
+        sum.y = fmaf(w, p.y, sum.y);
+        sum.z = fmaf(w, p.z, sum.z);
+        sum.w = fmaf(w, p.w, sum.w);
     }
+    if (d < a.dh)
+        *reinterpret_cast<uint2*>(out + d) = make_uint2(pack2(make_float2(sum.x, sum.y), T()), pack2(make_float2(sum.z, sum.w), T()));
     if (o.lse && lane == 0) o.lse[row] = l == 0.f ? -INFINITY : (top + log2f(l)) * kLn2;
 }
 
@@ -307,10 +485,11 @@ __global__ void __launch_bounds__(256) k_attend_join(AttendArgs a, AttendOut o, 
 struct Plan {
     bool tc;             // tiles of the tensor cores
     bool brief;          // the same for many short sequences
+    bool few;            // a few rows and many keys
     int pack, log_rows, splits;
 };
 Plan plan_of(const AttendArgs& a) {
-    Plan p;
+    Plan p{};
     p.pack = tc_pack(a);
     p.tc = a.Tq * p.pack / a.B >= 128 && a.Tk / a.B >= 256;
     // (it counts keys and the places behind them in 32 bits)
@@ -318,6 +497,18 @@ Plan plan_of(const AttendArgs& a) {
     if (p.brief) {
         p.log_rows = 7;
         p.splits = 1;
+        return p;
+    }
+    // One tile of rows and more keys than k_attend holds.
+    p.few = !p.tc && a.Tq * a.group / a.B <= kFewRows && a.Tk / a.B > kResident;
+    if (p.few) {
+        // Parts of the keys: as many CTAs as the SMs hold at once, of two chunks a warp at least
+        const int64_t tiles = (a.Tq * a.group >> kFewLog) + 1, ctas = (tiles > a.B ? tiles : a.B) * a.kv_heads;
+        int64_t n = (int64_t)(a.dh <= 32 ? 3 : a.dh <= 64 ? 2 : 1) * a.num_sms / ctas;
+        const int64_t most = a.Tk / a.B / (2 * kWarps * kFewKeys);
+        if (n > most) n = most;
+        if (n > kMaxSplits) n = kMaxSplits;
+        p.splits = (int)(n < 1 ? 1 : n);
         return p;
     }
     const int group = p.tc ? p.pack : a.group, keys = p.tc ? 128 : kTileKeys;
@@ -333,13 +524,19 @@ Plan plan_of(const AttendArgs& a) {
     const int64_t tiles = a.Tk / a.B / keys;
     int64_t n = (p.tc ? 1 : 3) * a.num_sms / ctas(p.log_rows);
     if (n > tiles / 2) n = tiles / 2;
-    if (n > 64) n = 64;
+    if (n > kMaxSplits) n = kMaxSplits;
     p.splits = (int)(n < 1 ? 1 : n);
     return p;
 }
 
 template <class T, int DH>
 cudaError_t run(const AttendArgs& a, const AttendOut& o, const Plan& p, float* part_out, float* part_lse, cudaStream_t s) {
+    if (p.few) {
+        const cudaError_t e = allow_smem(k_attend_few<T, DH>, FewTiles<T, DH>::kSmem);
+        if (e != cudaSuccess) return e;
+        const dim3 grid((unsigned)slots(a.Tq, a.B, a.group, kFewLog), (unsigned)a.kv_heads, (unsigned)p.splits);
+        return launch_next(k_attend_few<T, DH>, grid, dim3(kWarps * 32), FewTiles<T, DH>::kSmem, false, s, a, o, p.splits, part_out, part_lse);
+    }
     constexpr size_t smem = WarpTiles<T, DH>::kSmem;
     const cudaError_t e = allow_smem(k_attend<T, DH>, smem);
     if (e != cudaSuccess) return e;

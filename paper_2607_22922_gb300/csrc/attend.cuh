@@ -102,6 +102,12 @@ struct RowsAt {
     __device__ __forceinline__ T* operator()(int2 at) const { return first + (int64_t)at.x * ld + at.y * dh; }
 };
 
+// The last CTA of a kernel that needs nothing of the one before it and may run beside it
+// waits for that one, so that what comes after them waits for both.
+__device__ __forceinline__ bool last_cta() {
+    return blockIdx.x == gridDim.x - 1 && blockIdx.y == gridDim.y - 1 && blockIdx.z == gridDim.z - 1;
+}
+
 __device__ __forceinline__ float ex2(float x) {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));

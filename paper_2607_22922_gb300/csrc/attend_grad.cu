@@ -239,6 +239,7 @@ __global__ void __launch_bounds__(128, DH == 128 ? 2 : 3) k_attend_keys(AttendAr
     extern __shared__ __align__(16) uint8_t raw[];
     __shared__ __align__(8) float bias[kTileKeys];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, hk = blockIdx.y, split = blockIdx.z;
+    start_dependents();
     check_offsets(a.q_offsets, a.B, a.Tq, a.waits.err);
     check_offsets(a.kv_offsets, a.B, a.Tk, a.waits.err);
     const Slot slot = slot_of(a.kv_offsets, a.B, a.Tk, 1, kTileLog, blockIdx.x);
@@ -389,7 +390,8 @@ __global__ void __launch_bounds__(256) k_attend_keys_join(AttendArgs a, AttendGr
 }
 
 // ---- dq of sequences with more keys than a tile ----------------------------------------------
-// A CTA takes slots of 64 rows by turns, since most may have nothing to do.
+// A CTA takes slots of 64 rows by turns, since most may have nothing to do.  It needs nothing
+// of the kernel of the keys, whose last CTAs it runs beside.
 template <class T, int DH>
 struct RowTiles {
     static constexpr uint32_t kBytes = Rows<DH>::kLd * 2 * 64;
@@ -490,6 +492,7 @@ __global__ void __launch_bounds__(128, DH == 128 ? 2 : 3) k_attend_rows(AttendAr
         put_rows<T, DH>(dq, a.scale, rows - warp * 16, a.dh, 0, DH / 16, [&](int i) { return to(ro.at(warp * 16 + i)); },
                         [&](int i) { return (i < 8 ? lse2[0] : lse2[1]) != INFINITY; });         // no key counts
     }
+    if (last_cta()) wait_before();
 }
 
 // How a call runs
@@ -534,7 +537,7 @@ cudaError_t run(const AttendArgs& a, const AttendGrads& g, bool brief, int split
     if (e != cudaSuccess || a.Tk <= kTileKeys || a.Tq == 0) return e;
     const int64_t n = slots(a.Tq, a.B, a.group, kTileLog), most = (3 * a.num_sms + a.kv_heads - 1) / a.kv_heads;
     return launch_next(k_attend_rows<T, DH>, dim3((unsigned)(n < most ? n : most), (unsigned)a.kv_heads), dim3(128),
-                       RowTiles<T, DH>::kSmem, false, s, a, g, n);
+                       RowTiles<T, DH>::kSmem, true, s, a, g, n);
 }
 
 }  // namespace

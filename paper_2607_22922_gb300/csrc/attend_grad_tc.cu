@@ -10,6 +10,8 @@
 // the columns each.  While they take exponentials the tensor pipe makes the other scores:
 //   k_keys_tc:  .. dk dp' | dv' s'' | dk' dp'' ..     p' beside dk dp', ds' beside dv' s''
 //   k_rows_tc:  .. dq dp' s'' | dq' dp'' s''' ..      p' beside dq dp'
+// k_rows_tc starts first, since its CTAs mostly have more to do; k_keys_tc's fill the SMs as
+// it runs out.
 #include "attend_tc.cuh"
 
 namespace ifvs {
@@ -136,6 +138,7 @@ template <class T>
 __global__ void __launch_bounds__(256) k_attend_delta(AttendArgs a, AttendGrads g, float* delta) {
     const int64_t row = (int64_t)blockIdx.x * 64 + (threadIdx.x >> 2), n = a.Tq * a.heads;
     const int l = threadIdx.x & 3;
+    start_dependents();
     float2 sum = make_float2(0.f, 0.f);
     if (row < n) {
         const int64_t token = row / a.heads, at = (row - token * a.heads) * a.dh;
@@ -170,7 +173,10 @@ k_keys_tc(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtens
     const Slot slot = slot_of(a.kv_offsets, a.B, a.Tk, 1, 7, blockIdx.x);
     const Span qs = span_of(a.q_offsets, slot.b, a.B, a.Tq), ks = span_of(a.kv_offsets, slot.b, a.B, a.Tk);
     const int64_t key0 = slot.tile * 128;
-    if (slot.tile < 0 || key0 >= ks.len) return;
+    if (slot.tile < 0 || key0 >= ks.len) {
+        if (last_cta()) wait_before();
+        return;
+    }
     // tiles of rows, for every part of the group that shares tiles
     const int64_t n_rows = qs.len << log_pack, per_part = (n_rows + 127) / 128, tiles = per_part * (a.group >> log_pack);
     const int64_t t0 = tiles * split / splits, t1 = tiles * (split + 1) / splits;
@@ -272,7 +278,7 @@ k_keys_tc(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtens
                 if (row < n_rows) {
                     const int64_t at = (qs.at + (row >> log_pack)) * a.heads + t.head + ((int)row & ((1 << log_pack) - 1));
                     l[i] = __ldg(g.lse + at);
-                    d[i] = __ldg(delta + at);
+                    d[i] = __ldcg(delta + at);
                 }
             }
         };
@@ -388,6 +394,7 @@ k_keys_tc(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtens
         }
     }
     end(bars, tmem, filled, filled > 0, a.waits);
+    if (last_cta()) wait_before();
 }
 
 // ---- dq ----------------------------------------------------------------------------------------
@@ -404,12 +411,17 @@ k_rows_tc(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtens
     const Slot slot = slot_of(a.q_offsets, a.B, a.Tq, pack, 7, blockIdx.x);
     const Span qs = span_of(a.q_offsets, slot.b, a.B, a.Tq), ks = span_of(a.kv_offsets, slot.b, a.B, a.Tk);
     const int64_t row0 = slot.tile * 128, left = qs.len * pack - row0;
-    if (slot.tile < 0 || left <= 0) return;
+    if (slot.tile < 0 || left <= 0) {
+        if (last_cta()) wait_before();
+        return;
+    }
     const int rows = left < 128 ? (int)left : 128, n = (int)((ks.len + 127) / 128);
 
     const uint32_t q_at = dynamic_smem(), do_at = q_at + Sh::kTile, ring = do_at + Sh::kTile;
     auto k_of = [&](int stage) { return ring + (uint32_t)stage * 2 * Sh::kTile; };
     const uint32_t tmem = begin(bars);
+    wait_before();           // delta; with it there k_keys_tc may start
+    start_dependents();
     const Watch w{&bars.dead, a.waits};
     int filled = 0;
 
@@ -496,7 +508,7 @@ k_rows_tc(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtens
         if (r < rows) {
             const float v = __ldg(g.lse + token * a.heads + head);
             if (v != -INFINITY) lse2 = -v * kLog2e;
-            del = -__ldg(delta + token * a.heads + head);
+            del = -__ldcg(delta + token * a.heads + head);
         }
         const float2 l2 = make_float2(lse2, lse2), d2 = make_float2(del, del);
         bool ok = true;
@@ -585,11 +597,11 @@ cudaError_t run(const AttendArgs& a, const AttendGrads& g, int pack, int splits,
     while (1 << log_pack < pack) ++log_pack;
     e = launch_next(k_attend_delta<T>, dim3((unsigned)((a.Tq * a.heads + 63) / 64)), dim3(256), 0, false, s, a, g, delta);
     if (e != cudaSuccess) return e;
-    e = launch_next(k_keys_tc<T, DH>, dim3((unsigned)slots(a.Tk, a.B, 1, 7), (unsigned)a.kv_heads, (unsigned)splits), dim3(kThreads),
-                    GradShape<DH>::kSmem, false, s, mq, mdo, mk, mv, a, g, log_pack, splits, (const float*)delta, part_dk, part_dv);
+    e = launch_next(k_rows_tc<T, DH>, dim3((unsigned)slots(a.Tq, a.B, pack, 7), (unsigned)(a.heads / pack)), dim3(kThreads),
+                    GradShape<DH>::kSmem, true, s, mq, mdo, mk, mv, a, g, log_pack, (const float*)delta);
     if (e != cudaSuccess) return e;
-    return launch_next(k_rows_tc<T, DH>, dim3((unsigned)slots(a.Tq, a.B, pack, 7), (unsigned)(a.heads / pack)), dim3(kThreads),
-                       GradShape<DH>::kSmem, false, s, mq, mdo, mk, mv, a, g, log_pack, (const float*)delta);
+    return launch_next(k_keys_tc<T, DH>, dim3((unsigned)slots(a.Tk, a.B, 1, 7), (unsigned)a.kv_heads, (unsigned)splits), dim3(kThreads),
+                       GradShape<DH>::kSmem, true, s, mq, mdo, mk, mv, a, g, log_pack, splits, (const float*)delta, part_dk, part_dv);
 }
 
 }  // namespace
