@@ -9,6 +9,12 @@
 // itself and dq is complete; else from the forward call's lse and output, and k_attend_rows
 // makes dq.  Groups of four warps take one unit each and go through them tile by tile by
 // turns, so that one's exponentials run beside the other's MMAs.
+//
+// What bounds a tile is the chain of its waits (rows, s and dp, weights, dq, its rows on their
+// way), two of them at a time: 1000 sequences of 60 to 68 queries and up to 65 keys, 8 heads of
+// 64 over 2, take 108 us with k_attend_rows, 2.8 TB/s.  The issuing warp takes whichever group's
+// weights come first; in the order of the tiles, with a warp more (128 registers, which spill)
+// and all keys of a bundle before its rows it takes 137.
 #include "attend_tc.cuh"
 
 namespace ifvs {
@@ -24,8 +30,8 @@ struct BriefShape {
     static constexpr int kHalves = DH / 64;
     static constexpr int kGroups = DH == 64 ? 2 : 1;
     static constexpr int kColumns = 64 + 3 * DH;                         // of TMEM: s, dp (then dq), sums of dk and dv
-    static constexpr int kSoft = 4 * kGroups, kLoader = kSoft, kIssuer = kSoft + 1, kKeyFixer = kSoft + 2, kRowFixer = kSoft + 3,
-                         kFinder = kSoft + 4, kThreads = (kFinder + 1) * 32;
+    static constexpr int kSoft = 4 * kGroups, kLoader = kSoft, kIssuer = kSoft + 1, kFixer = kSoft + 2, kFinder = kSoft + 3,
+                         kThreads = (kFinder + 1) * 32;
     static constexpr uint32_t kQ = kHalves * kHalfBytes, kStage = 2 * kQ;            // queries and gradients
     static constexpr uint32_t kKeyHalf = kKeys * 128, kK = kHalves * kKeyHalf, kKv = 2 * kK;
     static constexpr int kQs = DH == 128 ? 2 : 3, kKvs = kGroups + 1;
@@ -52,6 +58,16 @@ struct BriefBars {
     int dead;
 };
 
+// whether a phase has ended, without waiting
+__device__ __forceinline__ bool mbar_test(uint32_t bar, uint32_t parity) {
+    uint32_t ok;
+    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+                 : "=r"(ok)
+                 : "r"(bar), "r"(parity)
+                 : "memory");
+    return ok != 0;
+}
+
 template <int N>
 struct Spot {
     uint32_t at = 0, parity = 0;
@@ -76,17 +92,18 @@ k_grad_short(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUt
              int64_t n_units) {
     using Sh = BriefShape<DH>;
     constexpr int QS = Sh::kQs, KS = Sh::kKvs, GROUPS = Sh::kGroups, H = Sh::kHalves;
-    constexpr int kLoader = Sh::kLoader, kIssuer = Sh::kIssuer, kKeyFixer = Sh::kKeyFixer, kRowFixer = Sh::kRowFixer, kFinder = Sh::kFinder;
+    constexpr int kLoader = Sh::kLoader, kIssuer = Sh::kIssuer, kFixer = Sh::kFixer, kFinder = Sh::kFinder;
     constexpr bool kF16 = std::is_same_v<T, __half>;
     __shared__ __align__(16) BriefBars<QS, KS, GROUPS> bars;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, pack = 1 << log_pack;
     check_offsets(a.q_offsets, a.B, a.Tq, a.waits.err);
     check_offsets(a.kv_offsets, a.B, a.Tk, a.waits.err);
+    start_dependents();
     const uint32_t w_at = dynamic_smem(), q_at = w_at + GROUPS * 2 * kWeights, kv_at = q_at + QS * Sh::kStage;
     if (threadIdx.x == 0) {
         for (int i = 0; i < 2; ++i) {
             mbar_init(smem_addr(&bars.batch_full[i]), 1);
-            mbar_init(smem_addr(&bars.batch_empty[i]), Sh::kSoft + 4);
+            mbar_init(smem_addr(&bars.batch_empty[i]), Sh::kSoft + 3);
         }
         for (int i = 0; i < QS; ++i) {
             mbar_init(smem_addr(&bars.q_full[i]), 1);
@@ -215,21 +232,21 @@ k_grad_short(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUt
         if (elect_one()) {
             Spot<QS> qp;
             Spot<KS> kp;
+            // a unit's keys before its first rows: the other roles go by the same order
             bundles(true, nothing, [&](const BriefUnit* u, int n) {
-                for (int i = 0; i < n; ++i) {
-                    if (tiles_of(u[i]) == 0) continue;
-                    if (!w.wait(smem_addr(&bars.kv_empty[kp.at]), kp.parity ^ 1u)) return false;
-                    const uint32_t bar = smem_addr(&bars.kv_full[kp.at]);
-                    mbar_arrive_expect_tx(bar, Sh::kKv + a.waits.extra);
-                    for (int d = 0; d < H; ++d) {
-                        const uint32_t to = kv_at + kp.at * Sh::kKv + d * Sh::kKeyHalf;
-                        tma_load_heads(to, &mk, d * 64, u[i].kv_head, u[i].key, bar);
-                        tma_load_heads(to + Sh::kK, &mv, d * 64, u[i].kv_head, u[i].key, bar);
-                    }
-                    kp.next();
-                    ++kv_filled;
-                }
                 return steps(u, n, [&](int, int t, const BriefUnit& v) {
+                    if (t == 0) {
+                        if (!w.wait(smem_addr(&bars.kv_empty[kp.at]), kp.parity ^ 1u)) return false;
+                        const uint32_t bar = smem_addr(&bars.kv_full[kp.at]);
+                        mbar_arrive_expect_tx(bar, Sh::kKv + a.waits.extra);
+                        for (int d = 0; d < H; ++d) {
+                            const uint32_t to = kv_at + kp.at * Sh::kKv + d * Sh::kKeyHalf;
+                            tma_load_heads(to, &mk, d * 64, v.kv_head, v.key, bar);
+                            tma_load_heads(to + Sh::kK, &mv, d * 64, v.kv_head, v.key, bar);
+                        }
+                        kp.next();
+                        ++kv_filled;
+                    }
                     if (!w.wait(smem_addr(&bars.q_empty[qp.at]), qp.parity ^ 1u)) return false;
                     const uint32_t bar = smem_addr(&bars.q_full[qp.at]);
                     mbar_arrive_expect_tx(bar, Sh::kStage + a.waits.extra);
@@ -254,11 +271,9 @@ k_grad_short(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUt
             uint32_t pending[GROUPS] = {}, turns = 0, reads = 0;
             auto of = [&](int i) { return GROUPS == 1 || i == 0 ? pending[0] : pending[GROUPS - 1]; };
             auto put = [&](int i, uint32_t p) { (GROUPS == 1 || i == 0 ? pending[0] : pending[GROUPS - 1]) = p; };
-            auto sums = [&](int i) {
+            auto multiply = [&](int i) {         // group i's weights are there
                 const uint32_t p = of(i);
-                if (!(p & 1u)) return true;
                 put(i, 0);
-                if (!w.wait(smem_addr(&bars.p_full[i]), turns >> i & 1u)) return false;
                 turns ^= 1u << i;
                 fence_after_sync();
                 const uint32_t stage = p >> 16 & 255u, keys = p >> 24, blocks = p >> 8 & 255u;
@@ -276,6 +291,26 @@ k_grad_short(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUt
                 mma_commit<1>(smem_addr(&bars.w_free[i]));
                 mma_commit<1>(smem_addr(&bars.q_empty[stage]));
                 if (p & 4u) mma_commit<1>(smem_addr(&bars.kv_empty[keys]));
+            };
+            // waits for what group i needs; the other group's weights may be there first
+            auto wait = [&](int i, uint64_t& barrier, uint32_t parity) {
+                const uint32_t bar = smem_addr(&barrier);
+                const long long begun = clock64();
+                for (;;) {
+                    if (mbar_test(bar, parity)) return true;
+                    bool other = false;
+                    for (int x = 0; x < GROUPS; ++x)
+                        if (x != i && (of(x) & 1u)) {
+                            other = true;
+                            if (mbar_test(smem_addr(&bars.p_full[x]), turns >> x & 1u)) multiply(x);
+                        }
+                    if (!other || clock64() - begun > a.waits.cycles) return w.wait(bar, parity);
+                }
+            };
+            auto sums = [&](int i) {
+                if (!(of(i) & 1u)) return true;
+                if (!wait(i, bars.p_full[i], turns >> i & 1u)) return false;
+                multiply(i);
                 return true;
             };
             auto flush = [&] {
@@ -284,22 +319,17 @@ k_grad_short(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUt
                 return true;
             };
             const bool ok = bundles(true, flush, [&](const BriefUnit* u, int n) {
-                // the bundle's keys are loaded before its rows: what holds a place that any of
-                // its units needs has to be done first
-                for (int i = 0; i < n; ++i)
-                    for (int x = 0; x < GROUPS; ++x)
-                        if (tiles_of(u[i]) > 0 && (of(x) & 1u) && of(x) >> 24 == u[i].place && !sums(x)) return false;
                 return steps(u, n, [&](int i, int t, const BriefUnit& v) {
                     if (!sums(i)) return false;
-                    // and so has another group's last whose rows hold the place for these
+                    // and another group's last that holds the place for these keys or rows
                     for (int x = 0; x < GROUPS; ++x)
-                        if ((of(x) & 1u) && (of(x) >> 16 & 255u) == qp.at && !sums(x)) return false;
+                        if ((of(x) & 1u) && ((t == 0 && of(x) >> 24 == v.place) || (of(x) >> 16 & 255u) == qp.at) && !sums(x)) return false;
                     // dp takes the place of the group's last dq
-                    if (!w.wait(smem_addr(&bars.dq_read[i]), (reads >> i & 1u) ^ 1u)) return false;
+                    if (!wait(i, bars.dq_read[i], (reads >> i & 1u) ^ 1u)) return false;
                     reads ^= 1u << i;
-                    if (t == 0 && !w.wait(smem_addr(&bars.kv_fixed[v.place]), v.parity)) return false;
-                    if (!w.wait(smem_addr(&bars.q_full[qp.at]), qp.parity)) return false;
-                    if (!w.wait(smem_addr(&bars.q_fixed[qp.at]), qp.parity)) return false;
+                    if (t == 0 && !wait(i, bars.kv_fixed[v.place], v.parity)) return false;
+                    if (!wait(i, bars.q_full[qp.at], qp.parity)) return false;
+                    if (!wait(i, bars.q_fixed[qp.at], qp.parity)) return false;
                     fence_after_sync();
                     const int blocks = (v.keys + 15) / 16;
                     const uint32_t id_s = mma_desc(128, blocks * 16, kF16, false, false);
@@ -324,51 +354,48 @@ k_grad_short(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUt
             });
             if (ok) flush();
         }
-    } else if (warp == kKeyFixer) {
-        // which keys count; keys and values of those that do not become zeros, because 0 times
-        // what they hold may be a NaN
-        Spot<KS> kp;
-        bundles(false, nothing, [&](const BriefUnit* units, int n) {
-            for (int i = 0; i < n; ++i) {
-                const BriefUnit u = units[i];
-                if (tiles_of(u) == 0) continue;
-                const int blocks = (u.keys + 15) / 16;
-                uint32_t bits[2];
-#pragma unroll
-                for (int x = 0; x < 2; ++x) {
-                    const int key = x * 32 + lane;
-                    bits[x] = __ballot_sync(0xFFFFFFFFu, key < u.keys && (a.kv_ids == nullptr || __ldg(a.kv_ids + (int64_t)u.key + key) >= 0));
-                }
-                if (!__all_sync(0xFFFFFFFFu, w.wait(smem_addr(&bars.kv_full[kp.at]), kp.parity))) return false;
-                bool any = false;
-                if (lane == 0) bars.some[kp.at] = (bits[0] | bits[1]) != 0;
-#pragma unroll
-                for (int x = 0; x < 2; ++x) {
-                    bars.bias[kp.at][x * 32 + lane] = (bits[x] >> lane) & 1u ? 0.f : -INFINITY;
-                    if (x * 32 + lane < blocks * 16 && !((bits[x] >> lane) & 1u)) {
-                        any = true;
-                        const uint32_t at = kv_at + kp.at * Sh::kKv + (uint32_t)(x * 32 + lane) * 128u;
-#pragma unroll
-                        for (int d = 0; d < 2 * H; ++d)
-#pragma unroll
-                            for (int y = 0; y < 8; ++y)
-                                asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(at + d * Sh::kKeyHalf + ((y ^ (lane & 7)) << 4)),
-                                             "r"(0)
-                                             : "memory");
-                    }
-                }
-                if (__any_sync(0xFFFFFFFFu, any)) fence_proxy_async_smem();
-                __syncwarp();
-                if (lane == 0) mbar_arrive<1>(smem_addr(&bars.kv_fixed[kp.at]));
-                kp.next();
-            }
-            return true;
-        });
-    } else if (warp == kRowFixer) {
-        // rows behind the sequence become zeros: whatever their p and ds are, they add nothing
+    } else if (warp == kFixer) {
+        // Which keys count; keys and values of those that do not become zeros, because 0 times
+        // what they hold may be a NaN.  Rows behind the sequence become zeros: whatever their p
+        // and ds are, they add nothing.  (One warp for both: a thirteenth would leave 128
+        // registers a thread, with which the others spill.)
         Spot<QS> qp;
+        Spot<KS> kp;
+        auto fix_keys = [&](const BriefUnit& u) {
+            const int blocks = (u.keys + 15) / 16;
+            uint32_t bits[2];
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                const int key = x * 32 + lane;
+                bits[x] = __ballot_sync(0xFFFFFFFFu, key < u.keys && (a.kv_ids == nullptr || __ldg(a.kv_ids + (int64_t)u.key + key) >= 0));
+            }
+            if (!__all_sync(0xFFFFFFFFu, w.wait(smem_addr(&bars.kv_full[kp.at]), kp.parity))) return false;
+            bool any = false;
+            if (lane == 0) bars.some[kp.at] = (bits[0] | bits[1]) != 0;
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                bars.bias[kp.at][x * 32 + lane] = (bits[x] >> lane) & 1u ? 0.f : -INFINITY;
+                if (x * 32 + lane < blocks * 16 && !((bits[x] >> lane) & 1u)) {
+                    any = true;
+                    const uint32_t at = kv_at + kp.at * Sh::kKv + (uint32_t)(x * 32 + lane) * 128u;
+#pragma unroll
+                    for (int d = 0; d < 2 * H; ++d)
+#pragma unroll
+                        for (int y = 0; y < 8; ++y)
+                            asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(at + d * Sh::kKeyHalf + ((y ^ (lane & 7)) << 4)),
+                                         "r"(0)
+                                         : "memory");
+                }
+            }
+            if (__any_sync(0xFFFFFFFFu, any)) fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) mbar_arrive<1>(smem_addr(&bars.kv_fixed[kp.at]));
+            kp.next();
+            return true;
+        };
         bundles(false, nothing, [&](const BriefUnit* units, int n) {
             return steps(units, n, [&](int, int t, const BriefUnit& u) {
+                if (t == 0 && !fix_keys(u)) return false;
                 if (!__all_sync(0xFFFFFFFFu, w.wait(smem_addr(&bars.q_full[qp.at]), qp.parity))) return false;
                 const int rows = u.rows - t * 128;
                 if (rows < 128) {
@@ -558,7 +585,10 @@ k_grad_short(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUt
                 __syncwarp();
                 if (lane == 0) mbar_arrive<1>(smem_addr(&bars.dq_read[group]));
             }
-            // the unit's sums, a key a lane: dv in the first two quarters, dk in the others
+            // the unit's sums, a key a lane: dv in the first two quarters, dk in the others; their
+            // MMAs came after dq's
+            if (!__all_sync(0xFFFFFFFFu, w.wait(smem_addr(&bars.w_free[group]), turn ^ 1u))) return false;
+            fence_after_sync();
             {
                 const int key = r & 63;
                 const bool is_dk = quad >= 2, in = key < u.keys;

@@ -42,11 +42,6 @@ __device__ __forceinline__ float2 pair_ex2(float2 x) {
     return y;
 }
 
-// a box into L2
-__device__ __forceinline__ void tma_prefetch(const CUtensorMap* map, int x, int y) {
-    asm volatile("cp.async.bulk.prefetch.tensor.2d.L2.global.tile [%0, {%1, %2}];" ::"l"(map), "r"(x), "r"(y) : "memory");
-}
-
 // act and act' of two values, two float32 operations per instruction: the epilogue of 17408 x
 // 960 -> 2560 with GELU takes 16 instructions a value one by one, 10 so.
 template <int ACT>
@@ -87,7 +82,10 @@ __device__ __forceinline__ float2 finish_two(float2 z, float2 other) {
 // BN columns of the output per tile; 8 epilogue warps, each 32 rows x BN / 2 columns, 32
 // columns at a time.  A warp's two buffers of 32 x 32 hold the residual (or dy), brought by
 // TMA, then the output in its place.  More room there would take a stage of the ring: with
-// five instead of six 17408 x 960 -> 2560 takes 101 us instead of 94.
+// five instead of six 17408 x 960 -> 2560 takes 7 us more.  Without residual and activation that
+// takes 53 us, with GELU 67, with the residual 67, with both 81; a residual through registers
+// (83), or asked of L2 a tile ahead (82), takes no less: the operands alone take 64 bytes a
+// clock of an SM's way to L2.
 constexpr uint32_t kChunkBytes = 32 * 64;
 template <int CG, int BN>
 struct LinearShape {
@@ -170,16 +168,6 @@ k_linear(const __grid_constant__ CUtensorMap mx, const __grid_constant__ CUtenso
             }
             ++asked;
         };
-        // the next tile's into L2: a buffer's copy is asked for one chunk ahead, which covers
-        // L2's latency but not the memory's
-        auto prefetch = [&](int i) {
-            if (lane != 0 || i >= items) return;
-            const int2 mn = tile_of(i, g.m_tiles, g.n_tiles);
-            const int row = row_of(mn);
-            for (int c = 0; c < BN / 2; c += 32)
-                if (row < g.rows && mn.y * BN + part + c < g.cols) tma_prefetch(&mo, mn.y * BN + part + c, row);
-        };
-        if (fetches) prefetch(first);
         if (fetches && first < items) fetch(tile_of(first, g.m_tiles, g.n_tiles), 0);
         Ring<2> acc;
         bool ok = true;
@@ -187,7 +175,6 @@ k_linear(const __grid_constant__ CUtensorMap mx, const __grid_constant__ CUtenso
         for (int i = first; i < items && ok; i += step, acc.next()) {
             const int2 mn = tile_of(i / splits, g.m_tiles, g.n_tiles);
             const int row = row_of(mn), col0 = mn.y * BN + part;
-            if (fetches) prefetch(i + step);
             if (!(ok = __all_sync(0xFFFFFFFFu, w.wait(smem_addr(&bars.acc_full[acc.at]), acc.parity)))) break;
             fence_after_sync();
             const uint32_t tm = tmem + acc.at * 256 + part + ((uint32_t)quad << 21);
