@@ -15,7 +15,9 @@ namespace {
 // ---- tiles of warps: any lengths ---------------------------------------------------------
 // A CTA of 4 warps takes up to 2^log_rows rows of one group and the keys of one split.  Up to 128
 // keys stay in shared memory, and the warps go through tiles of 16 rows by themselves, the
-// next tile's queries on their way; more keys pass 64 at a time, for 64 rows at a time.
+// next tile's queries on their way; more keys pass 64 at a time, for 64 rows at a time.  200
+// sequences of 32 queries and 40 keys, 8 heads of 64, take 18 us (1.6 TB/s): the chain of a
+// CTA's loads, products and stores, of which an SM has four at a time.
 constexpr int kWarps = 4, kResident = 128;
 
 template <class T, int DH>
@@ -491,19 +493,33 @@ struct Plan {
 Plan plan_of(const AttendArgs& a) {
     Plan p{};
     p.pack = tc_pack(a);
+    // Both sides in us, 8 heads with keys of their own, bfloat16, one call after the other:
+    // 128 queries x 256 keys, heads of 64 (of 128): 1 sequence 8.0 against k_attend's 10.1 (9.3
+    // and 12.1), 8 sequences 8.4 against 14.4 (9.5 and 16.2); 4 of 1024 x 1024 18.9 against 50.8.
     p.tc = a.Tq * p.pack / a.B >= 128 && a.Tk / a.B >= 256;
-    // (it counts keys and the places behind them in 32 bits)
-    p.brief = !p.tc && a.Tk <= 0x7FFFFF00 && a.Tq * p.pack / a.B >= 32 && slots(a.Tq, a.B, p.pack, 7) * (a.heads / p.pack) >= 2 * a.num_sms;
+    // Many sequences, each with a good part of a tile of 128 rows, whose keys mostly are one
+    // chunk.  200 sequences of 120 x 60, heads of 64: 24.2 against k_attend's 34.8; of 32 x 40
+    // 18.7 and 18.4; 40 of 64 x 64 10.5 and 9.1: below about three tiles' worth of rows an SM it
+    // is the longer.  Heads of 128: 40.4 and 66.1, 23.6 and 36.8, 12.5 and 14.9.  (It counts keys and
+    // the places behind them in 32 bits.)
+    p.brief = !p.tc && a.Tk <= 0x7FFFFF00 && a.Tq * p.pack / a.B >= 32 &&
+              (a.dh > 64 ? slots(a.Tq, a.B, p.pack, 7) * (a.heads / p.pack) >= 2 * a.num_sms
+                         : a.Tq * a.heads / 128 >= 3 * a.num_sms);
     if (p.brief) {
         p.log_rows = 7;
         p.splits = 1;
         return p;
     }
-    // One tile of rows and more keys than k_attend holds.
-    p.few = !p.tc && a.Tq * a.group / a.B <= kFewRows && a.Tk / a.B > kResident;
+    // One tile of rows and more keys than k_attend holds; a few more keys only where there are few
+    // CTAs.  One query, 8 heads of 64 (of 128), 300 sequences: 130 keys 40.7 against k_attend's 38.9
+    // (103 and 88), 512 keys 64.4 and 84.7 (146 and 206), 4096 keys 376 and 547 (748 and 1476);
+    // 1 sequence of 130 keys, heads of 128, 7.2 and 11.1; 8 heads sharing 4096 keys of 300, 55
+    // and 128.
+    const int64_t few_tiles = (a.Tq * a.group >> kFewLog) + 1, few_ctas = (few_tiles > a.B ? few_tiles : a.B) * a.kv_heads;
+    p.few = !p.tc && a.Tq * a.group / a.B <= kFewRows && a.Tk / a.B > (few_ctas <= a.num_sms ? kResident : 2 * kResident);
     if (p.few) {
         // Parts of the keys: as many CTAs as the SMs hold at once, of two chunks a warp at least
-        const int64_t tiles = (a.Tq * a.group >> kFewLog) + 1, ctas = (tiles > a.B ? tiles : a.B) * a.kv_heads;
+        const int64_t ctas = few_ctas;
         int64_t n = (int64_t)(a.dh <= 32 ? 3 : a.dh <= 64 ? 2 : 1) * a.num_sms / ctas;
         const int64_t most = a.Tk / a.B / (2 * kWarps * kFewKeys);
         if (n > most) n = most;
@@ -521,8 +537,8 @@ Plan plan_of(const AttendArgs& a) {
     while (!p.tc && p.log_rows > 6 && ctas(p.log_rows) < 4 * a.num_sms) --p.log_rows;
     // Parts of the keys, where the rows leave SMs without a CTA: at least two tiles of the
     // average sequence each.  (4099 queries x 17 403 keys, 8 heads of 128, are 128 CTAs and 8 of
-    // 3 rows.  Cut 1 : 0.19 they fill the SMs, and the kernel takes 249 us instead of 246: the
-    // clock falls as more tensor cores run.)
+    // 3 rows.  Cut 1 : 0.19 they leave SMs idle at the end instead, and take 249 us and the join
+    // instead of 246.)
     const int64_t tiles = a.Tk / a.B / keys;
     int64_t n = (p.tc ? 1 : 3) * a.num_sms / ctas(p.log_rows);
     if (n > tiles / 2) n = tiles / 2;

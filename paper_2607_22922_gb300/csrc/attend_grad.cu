@@ -225,7 +225,8 @@ struct Arrays {
 // A CTA takes 64 keys and one part of the rows of their group, 64 at a time with the next
 // on their way: each of its 4 warps makes p and ds of 16 rows, then adds 16 keys' sums over
 // the 64 rows (a share of the columns for fewer keys).  Blocks of 16 keys behind the last are
-// left out.
+// left out.  40 sequences of 40 queries and 16 keys, 8 heads of 64, take 11 us: one round of
+// CTAs, bound by the chain of a CTA's loads, products and stores.
 template <class T, int DH>
 struct KeyTiles {
     Rows<DH> k, v, q[2], d_out[2];
@@ -505,10 +506,16 @@ struct Plan {
 Plan plan_of(const AttendArgs& a) {
     Plan p;
     p.pack = tc_pack(a);
+    // Both sides in us, 8 heads with keys of their own, bfloat16, one call after the other: 1
+    // sequence of 128 queries x 256 keys, heads of 64 (of 128), 9.7 against k_attend_keys and _rows'
+    // 17.8 (12.9 and 24.5), 64 of them 76 and 179 (112 and 446), 4 of 1024 x 1024 53 and 253.
     p.tc = a.Tq * p.pack / a.B >= 128 && a.Tk / a.B >= 256;
     p.delta_bytes = p.tc ? padded((size_t)a.Tq * a.heads * 4) : 0;
+    // Sequences whose keys mostly are one chunk: 200 of 32 x 40, heads of 64, 35 against
+    // k_attend_keys' 47, of 120 x 60 47 and 92; 40 of 40 x 16 14.0 and 11.1, of 64 x 64 15.9 and
+    // 15.4; heads of 128 64 and 249, 14.9 and 31.  (It counts rows in 32 bits.)
     p.brief = !p.tc && p.pack == a.group && a.Tq * a.group / a.B >= 32 && a.Tk / a.B <= kTileKeys && a.Tq * a.group <= 0x7FFFFF00 &&
-              a.B * a.kv_heads >= 2 * a.num_sms;
+              a.B * a.kv_heads >= (a.dh > 64 ? 2 : 4) * a.num_sms;
     if (p.brief) {
         p.splits = 1;
         return p;

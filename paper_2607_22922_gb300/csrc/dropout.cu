@@ -19,6 +19,8 @@ struct DropArgs {
     float scale;
 };
 
+// Ten rounds of two 32 x 32-bit products make four words; at 16 bits an element they bound
+// the call, not memory: 163 847 x 960 in bfloat16 take 125 us, 5.0 TB/s, where their bytes take 93.
 // A thread takes CH chunks of 16 bytes of x, a grid's width apart.  WIDE: all arrays
 // begin on 16 bytes; else elements come one by one.
 template <class T, bool RES, bool WIDE, int CH>

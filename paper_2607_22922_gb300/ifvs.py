@@ -748,6 +748,8 @@ def ifvs_attend(L, q, k, v, q_offsets=None, kv_offsets=None, kv_ids=None, scale=
     if lse is True:
         import torch
         lse = _like(q, stream, *sq[:2], dtype=torch.float32)
+    elif lse is False:
+        lse = None
     to, p.ld_out = _heads(out, sq, dt, "out", at)
     _check(_lib.ifvs_attend(L, C.byref(p), *ptr, to, _lse(lse, sq[:2], at)))
     return out, lse

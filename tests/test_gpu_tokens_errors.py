@@ -73,7 +73,7 @@ def test_linear_wait_runs_out(ifvs, layers, monkeypatch, T, D_in, D_out, act, dt
 
 # long sequences, whole and in parts; many short ones, of one chunk of keys and of several
 @pytest.mark.parametrize("lq,lk,H,Hk,d,dtype", [([300, 200], [400, 700], 2, 1, 128, torch.bfloat16), ([130], [3_000], 2, 2, 64, torch.float16),
-                                                ([50] * 200, [30] * 200, 4, 2, 64, torch.bfloat16),
+                                                ([50] * 400, [30] * 400, 8, 4, 64, torch.bfloat16),
                                                 ([40] * 200, [60] * 200, 4, 4, 128, torch.float16)])
 def test_attend_wait_runs_out(ifvs, layers, monkeypatch, lq, lk, H, Hk, d, dtype):
     for call in _attend(layers, lq, lk, H, Hk, d, dtype):
