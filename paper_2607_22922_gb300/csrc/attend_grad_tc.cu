@@ -9,14 +9,16 @@
 // to TMEM as the 16-bit operands of the next MMAs.  Two halves of the threads take half of
 // the columns each.  While they take exponentials the tensor pipe makes the other scores:
 //   k_keys_tc:  .. dk dp' | dv' s'' | dk' dp'' ..     p' beside dk dp', ds' beside dv' s''
-//   k_rows_tc:  .. dq dp' s'' | dq' dp'' s''' ..      p' beside dq dp'
+//      DH = 64: .. dk | dv' s'' dp'' | dk' | dv'' ..  TMEM has room for a second dp
+//   k_rows_tc:  .. dq s'' | dp'' | dq' s''' ..        p' beside dq s'', ds' beside dp''
 // k_rows_tc starts first, since its CTAs mostly have more to do; k_keys_tc's fill the SMs as
 // it runs out.
 //
-// Four sequences of about 1500 x 4250, 8 heads of 64: 242 us, of seven products 760 TFLOP/s;
-// apart k_keys_tc takes 150 us and k_rows_tc 116, their tensor pipes active 31 % of the time: the
-// waits between MMAs and exponentials, since TMEM has room for one tile's scores on their way.
-// Sixteen warps for the exponentials, 32 scores a thread, take 155 and 125.
+// Four sequences of about 1500 x 4250, 8 heads of 64: 223 us, of seven products 820 TFLOP/s;
+// apart k_keys_tc takes 143 us and k_rows_tc 102, their tensor pipes active a third of the time:
+// the waits between MMAs and exponentials, and a CTA's start and end, which nothing hides since
+// it holds all of TMEM.  With one place of dp, made again once ds is there, they take 150 and
+// 116, and then with sixteen warps for the exponentials, 32 scores a thread, 155 and 125.
 #include "attend_tc.cuh"
 
 namespace ifvs {
@@ -37,7 +39,7 @@ struct GradShape {
 
 template <int S>
 struct GradBars {
-    uint64_t resident, full[S], fixed[S], empty[S], s_full[2], dp_full, p_full, ds_full, acc_full, drain;
+    uint64_t resident, full[S], fixed[S], empty[S], s_full[2], dp_full[2], dp_read, p_full, ds_full, acc_full, drain;
     uint32_t mask[S][4];
     alignas(16) float lse2[S][128], delta[S][128];       // terms of the ring's rows, read four at a time
     uint32_t tmem;
@@ -54,8 +56,11 @@ __device__ __forceinline__ uint32_t begin(GradBars<S>& b) {
             mbar_init(smem_addr(&b.fixed[i]), 1);
             mbar_init(smem_addr(&b.empty[i]), 1);
         }
-        for (int i = 0; i < 2; ++i) mbar_init(smem_addr(&b.s_full[i]), 1);
-        mbar_init(smem_addr(&b.dp_full), 1);
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(smem_addr(&b.s_full[i]), 1);
+            mbar_init(smem_addr(&b.dp_full[i]), 1);
+        }
+        mbar_init(smem_addr(&b.dp_read), kSoftWarps);
         mbar_init(smem_addr(&b.p_full), kSoftWarps);
         mbar_init(smem_addr(&b.ds_full), kSoftWarps);
         mbar_init(smem_addr(&b.acc_full), 1);
@@ -162,17 +167,19 @@ __global__ void __launch_bounds__(256) k_attend_delta(AttendArgs a, AttendGrads 
 }
 
 // ---- dk, dv ------------------------------------------------------------------------------------
-// TMEM: s^T (then p^T) 0, dp^T (then ds^T) 128, dv 256, dk 256 + DH
+// TMEM: s^T (then p^T) 0, dp^T (then ds^T) 128, dv 256, dk 256 + DH; for DH = 64 dp^T of odd
+// tiles 384
 template <class T, int DH>
 __global__ void __launch_bounds__(kThreads, 1)
 k_keys_tc(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mdo, const __grid_constant__ CUtensorMap mk,
           const __grid_constant__ CUtensorMap mv, AttendArgs a, AttendGrads g, int log_pack, int splits, const float* __restrict__ delta,
           float* part_dk, float* part_dv) {
     using Sh = GradShape<DH>;
-    constexpr int S = Sh::kStages;
+    constexpr int S = Sh::kStages, DPS = DH == 64 ? 2 : 1;       // places of dp^T
     constexpr bool kF16 = std::is_same_v<T, __half>;
     __shared__ __align__(16) GradBars<S> bars;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, hk = blockIdx.y, split = blockIdx.z;
+    auto dp_col = [](int j) { return DPS == 2 && (j & 1) ? 384u : 128u; };
     check_offsets(a.q_offsets, a.B, a.Tq, a.waits.err);
     check_offsets(a.kv_offsets, a.B, a.Tk, a.waits.err);
     const Slot slot = slot_of(a.kv_offsets, a.B, a.Tk, 1, 7, blockIdx.x);
@@ -246,8 +253,8 @@ k_keys_tc(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtens
                 mma_commit<1>(smem_addr(&bars.s_full[0]));
             };
             auto dp_of = [&](int j) {
-                mma_rows<DH>(tmem + 128, v_at, q_of(j % S) + Sh::kTile, id_s);
-                mma_commit<1>(smem_addr(&bars.dp_full));
+                mma_rows<DH>(tmem + dp_col(j), v_at, q_of(j % S) + Sh::kTile, id_s);
+                mma_commit<1>(smem_addr(&bars.dp_full[j % DPS]));
             };
             if (ok && (ok = there(0))) {
                 s_of(0);
@@ -260,12 +267,13 @@ k_keys_tc(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtens
                 if (j + 1 < n) {
                     if (!(ok = there(j + 1))) break;
                     s_of(j + 1);
+                    if (DPS == 2) dp_of(j + 1);
                 }
                 if (!(ok = w.wait(smem_addr(&bars.ds_full), (uint32_t)j & 1u))) break;
                 fence_after_sync();
-                mma_sums(tmem + 256 + DH, tmem + 128, q_of(j % S), id_o, j > 0);
+                mma_sums(tmem + 256 + DH, tmem + dp_col(j), q_of(j % S), id_o, j > 0);
                 mma_commit<1>(smem_addr(&bars.empty[j % S]));
-                if (j + 1 < n) dp_of(j + 1);
+                if (DPS == 1 && j + 1 < n) dp_of(j + 1);
             }
             if (ok) mma_commit<1>(smem_addr(&bars.acc_full));
         }
@@ -342,10 +350,10 @@ k_keys_tc(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtens
             fence_before_sync();
             __syncwarp();
             if (lane == 0) mbar_arrive<1>(smem_addr(&bars.p_full));
-            ok = __all_sync(0xFFFFFFFFu, w.wait(smem_addr(&bars.dp_full), turn));
+            ok = __all_sync(0xFFFFFFFFu, w.wait(smem_addr(&bars.dp_full[j % DPS]), (uint32_t)(j / DPS) & 1u));
             if (!ok) break;
             fence_after_sync();
-            load64(mine + 128, d);
+            load64(mine + dp_col(j), d);
             wait64(d);
 #pragma unroll
             for (int y = 0; y < 64; y += 4) {
@@ -354,7 +362,7 @@ k_keys_tc(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtens
                 w16[y / 2] = pack2(mul_(make_float2(s[0], s[1]), add_(make_float2(x[0], x[1]), make_float2(t.x, t.y))), T());
                 w16[y / 2 + 1] = pack2(mul_(make_float2(s[2], s[3]), add_(make_float2(x[2], x[3]), make_float2(t.z, t.w))), T());
             }
-            tmem_st32(mine + 128, w16);
+            tmem_st32(mine + dp_col(j), w16);
             tmem_st_wait();
             fence_before_sync();
             __syncwarp();
@@ -464,18 +472,22 @@ k_rows_tc(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtens
             };
             auto dp_of = [&](int j) {
                 mma_rows<DH>(tmem + 256, do_at, k_of(j % S) + Sh::kTile, id_s);
-                mma_commit<1>(smem_addr(&bars.dp_full));
+                mma_commit<1>(smem_addr(&bars.dp_full[0]));
             };
             if (ok && (ok = s_of(0))) {
                 dp_of(0);
                 if (n > 1) ok = s_of(1);
             }
             for (int j = 0; j < n && ok; ++j) {
+                if (j + 1 < n) {         // as soon as dp is in registers
+                    if (!(ok = w.wait(smem_addr(&bars.dp_read), (uint32_t)j & 1u))) break;
+                    fence_after_sync();
+                    dp_of(j + 1);
+                }
                 if (!(ok = w.wait(smem_addr(&bars.ds_full), (uint32_t)j & 1u))) break;
                 fence_after_sync();
                 mma_sums(tmem + 384, tmem + (j & 1) * 128, k_of(j % S), id_o, j > 0);
                 mma_commit<1>(smem_addr(&bars.empty[j % S]));
-                if (j + 1 < n) dp_of(j + 1);
                 if (j + 2 < n) ok = s_of(j + 2);
             }
             if (ok) mma_commit<1>(smem_addr(&bars.acc_full));
@@ -534,11 +546,14 @@ k_rows_tc(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtens
                 s[0] = ex2(e.x);
                 s[1] = ex2(e.y);
             }
-            ok = __all_sync(0xFFFFFFFFu, w.wait(smem_addr(&bars.dp_full), (uint32_t)j & 1u));
+            ok = __all_sync(0xFFFFFFFFu, w.wait(smem_addr(&bars.dp_full[0]), (uint32_t)j & 1u));
             if (!ok) break;
             fence_after_sync();
             load64(mine + 256, d);
             wait64(d);
+            fence_before_sync();
+            __syncwarp();
+            if (lane == 0) mbar_arrive<1>(smem_addr(&bars.dp_read));
 #pragma unroll
             for (int y = 0; y < 64; y += 2) {
                 float *x = &d[y >> 5][y & 31], *s = &p[y >> 5][y & 31];
