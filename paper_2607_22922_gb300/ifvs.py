@@ -703,9 +703,12 @@ def _heads(a, shape, dtype, name, at):
 def _offsets(a, name, at):
     if a is None:
         return 1, None
-    if not _is_vector(a, "int64") or a.shape[0] < 2:
+    n = a.shape[0] if _is_vector(a, "int64") else 0
+    if n < 2:
         raise ValueError("%s must be a vector of B + 1 int64" % name)
-    return a.shape[0] - 1, _dev(a, (a.shape[0],), a.dtype, name, at)
+    if a.get_device() != at or not a.is_contiguous():
+        raise ValueError("%s must be a contiguous tensor on cuda:%d" % (name, at))
+    return n - 1, a.data_ptr()
 
 
 def _attend_params(q, k, v, q_offsets, kv_offsets, kv_ids, scale, stream, at):
@@ -732,6 +735,8 @@ def _attend_params(q, k, v, q_offsets, kv_offsets, kv_ids, scale, stream, at):
 
 
 def _lse(lse, shape, at):
+    if lse is None:
+        return None
     import torch
     return _dev(lse, shape, torch.float32, "lse", at)
 
