@@ -537,8 +537,8 @@ Plan plan_of(const AttendArgs& a) {
     while (!p.tc && p.log_rows > 6 && ctas(p.log_rows) < 4 * a.num_sms) --p.log_rows;
     // Parts of the keys, where the rows leave SMs without a CTA: at least two tiles of the
     // average sequence each.  (4099 queries x 17 403 keys, 8 heads of 128, are 128 CTAs and 8 of
-    // 3 rows.  Cut 1 : 0.19 they leave SMs idle at the end instead, and take 249 us and the join
-    // instead of 246.)
+    // 3 rows.  Cut 1 : 0.19 they leave SMs idle at the end instead, and take 3 us more, and the
+    // join.)
     const int64_t tiles = a.Tk / a.B / keys;
     int64_t n = (p.tc ? 1 : 3) * a.num_sms / ctas(p.log_rows);
     if (n > tiles / 2) n = tiles / 2;

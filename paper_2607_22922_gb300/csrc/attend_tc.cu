@@ -9,10 +9,11 @@
 // The running maximum is raised, and o rescaled by the threads that hold its rows, only
 // where a score exceeds it by 2^8: until then the weights are at most 2^8 and as exact.
 //
-// 4099 queries x 17 403 keys, 8 heads of 128 in bfloat16: 246 us, 1.18 PFLOP/s, on 128 of the
+// 4099 queries x 17 403 keys, 8 heads of 128 in bfloat16: 232 us, 1.26 PFLOP/s, on 128 of the
 // 152 SMs (plan_of in attend.cu); the tensor pipe is active half of the time, the rest are the
-// waits between the MMAs and the exponentials of one tile.  Twice the warps, half of a row's
-// scores a thread and the maximum by way of shared memory, take 354 us.
+// waits between the MMAs and the exponentials of one tile.  With all weights of a tile at once
+// for their MMAs it takes 246, and then with twice the warps, half of a row's scores a thread and
+// the maximum by way of shared memory, 354.
 #include "attend_tc.cuh"
 
 namespace ifvs {
@@ -33,7 +34,7 @@ struct TcShapes {
 
 template <int S>
 struct TcBars {
-    uint64_t full[S], empty[S], fixed[S], mask_ready[kMasks], q_full, s_full[2], p_full[2], o_full[2], drain;
+    uint64_t full[S], empty[S], fixed[S], mask_ready[kMasks], q_full, s_full[2], p_full[2][2], o_full[2], drain;
     uint32_t mask[kMasks][4];
     uint32_t tmem;
     int dead;
@@ -77,7 +78,7 @@ k_attend_tc(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUte
         mbar_init(smem_addr(&bars.q_full), 1);
         for (int i = 0; i < 2; ++i) {
             mbar_init(smem_addr(&bars.s_full[i]), 1);
-            mbar_init(smem_addr(&bars.p_full[i]), 4);
+            for (int x = 0; x < 2; ++x) mbar_init(smem_addr(&bars.p_full[i][x]), 4);
             mbar_init(smem_addr(&bars.o_full[i]), 1);
         }
         mbar_init(smem_addr(&bars.drain), 1);
@@ -149,11 +150,15 @@ k_attend_tc(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUte
                 if (j + 1 < n && !(ok = keys_there(j + 1))) break;
                 const uint64_t dv = rows_desc(ring + slot_at(v) * Sh::kTile);
                 for (int i = 0; i < n_tiles && ok; ++i) {
-                    if (!(ok = w.wait(smem_addr(&bars.p_full[i]), (uint32_t)j & 1u))) break;
-                    fence_after_sync();
+                    for (int x = 0; x < 2; ++x) {
+                        if (!(ok = w.wait(smem_addr(&bars.p_full[i][x]), (uint32_t)j & 1u))) break;
+                        fence_after_sync();
 #pragma unroll
-                    for (int k = 0; k < 8; ++k)
-                        mma_f16_tmem_a(tmem + o_col(i), tmem + s_col(i) + k * 8, dv + k * desc_step(true), id_o, j > 0 || k > 0);
+                        for (int k = 0; k < 4; ++k)
+                            mma_f16_tmem_a(tmem + o_col(i), tmem + s_col(i) + (4 * x + k) * 8, dv + (4 * x + k) * desc_step(true), id_o,
+                                           j > 0 || x + k > 0);
+                    }
+                    if (!ok) break;
                     if (i == n_tiles - 1) mma_commit<1>(smem_addr(&bars.empty[slot_at(v)]));
                     if (j + 1 < n)
                         scores(i, j + 1);
@@ -261,12 +266,13 @@ k_attend_tc(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUte
                     p[y / 2] = pack2(e, T());
                 }
                 tmem_st32(s_at + x * 16, p);
+                // half of the weights: their MMAs run beside the other half's exponentials
+                tmem_st_wait();
+                fence_before_sync();
+                __syncwarp();
+                if (lane == 0) mbar_arrive<1>(smem_addr(&bars.p_full[i][x / 2]));
             }
             l += total(add_(sum[0], sum[1]));
-            tmem_st_wait();
-            fence_before_sync();
-            __syncwarp();
-            if (lane == 0) mbar_arrive<1>(smem_addr(&bars.p_full[i]));
         }
         if (ok && n > 0) ok = __all_sync(0xFFFFFFFFu, w.wait(smem_addr(&bars.o_full[i]), 0));
         if (ok) {
