@@ -501,8 +501,8 @@ Plan plan_of(const AttendArgs& a) {
     // chunk.  200 sequences of 120 x 60, heads of 64: 24.2 against k_attend's 34.8; of 32 x 40
     // 18.7 and 18.4; 40 of 64 x 64 10.5 and 9.1: below about three tiles' worth of rows an SM it
     // is the longer.  Heads of 128: 40.4 and 66.1, 23.6 and 36.8, 12.5 and 14.9.  (It counts keys and
-    // the places behind them in 32 bits.)
-    p.brief = !p.tc && a.Tk <= 0x7FFFFF00 && a.Tq * p.pack / a.B >= 32 &&
+    // the places behind them in 32 bits.  Its copies need a key: a tensor map has no empty side.)
+    p.brief = !p.tc && a.Tk > 0 && a.Tk <= 0x7FFFFF00 && a.Tq * p.pack / a.B >= 32 &&
               (a.dh > 64 ? slots(a.Tq, a.B, p.pack, 7) * (a.heads / p.pack) >= 2 * a.num_sms
                          : a.Tq * a.heads / 128 >= 3 * a.num_sms);
     if (p.brief) {

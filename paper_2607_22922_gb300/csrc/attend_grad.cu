@@ -513,8 +513,9 @@ Plan plan_of(const AttendArgs& a) {
     p.delta_bytes = p.tc ? padded((size_t)a.Tq * a.heads * 4) : 0;
     // Sequences whose keys mostly are one chunk: 200 of 32 x 40, heads of 64, 35 against
     // k_attend_keys' 47, of 120 x 60 47 and 92; 40 of 40 x 16 14.0 and 11.1, of 64 x 64 15.9 and
-    // 15.4; heads of 128 64 and 249, 14.9 and 31.  (It counts rows in 32 bits.)
-    p.brief = !p.tc && p.pack == a.group && a.Tq * a.group / a.B >= 32 && a.Tk / a.B <= kTileKeys && a.Tq * a.group <= 0x7FFFFF00 &&
+    // 15.4; heads of 128 64 and 249, 14.9 and 31.  (It counts rows in 32 bits, and its tensor
+    // maps need a key.)
+    p.brief = !p.tc && a.Tk > 0 && p.pack == a.group && a.Tq * a.group / a.B >= 32 && a.Tk / a.B <= kTileKeys && a.Tq * a.group <= 0x7FFFFF00 &&
               a.B * a.kv_heads >= (a.dh > 64 ? 2 : 4) * a.num_sms;
     if (p.brief) {
         p.splits = 1;
