@@ -615,6 +615,8 @@ k_grad_short(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUt
             fence_before_sync();
             return true;
         });
+        // the last rows of dq are read from shared memory until then
+        if (lane == 0) tma_wait_all();
     }
     __syncwarp();
     fence_before_sync();
