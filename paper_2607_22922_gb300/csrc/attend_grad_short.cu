@@ -460,7 +460,11 @@ k_grad_short(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUt
                     }
                     delta = total(sum);
                 }
-                if (!__all_sync(0xFFFFFFFFu, w.wait(smem_addr(&bars.s_full[group]), turn))) return false;
+                // the second wait, over by then, is for the fixer's own stores of what counts.  In this order: the
+                // place cannot be filled again before this tile's weights are there
+                if (!__all_sync(0xFFFFFFFFu, w.wait(smem_addr(&bars.s_full[group]), turn) &&
+                                                 w.wait(smem_addr(&bars.kv_fixed[u.place]), u.parity)))
+                    return false;
                 fence_after_sync();
                 const float* bias = bars.bias[u.place];
                 counts = bias[r & 63] == 0.f;
