@@ -55,7 +55,7 @@ struct BriefBars {
     int some[KS];            // whether a key counts
     alignas(16) float bias[KS][kKeys];   // read four at a time: 0, or -infinity for a key that does not count
     uint32_t tmem;
-    int dead;
+    Pulse pulse;
 };
 
 // whether a phase has ended, without waiting
@@ -123,7 +123,8 @@ k_grad_short(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUt
             mbar_init(smem_addr(&bars.w_free[i]), 1);
         }
         mbar_init(smem_addr(&bars.drain), 1);
-        bars.dead = 0;
+        bars.pulse.dead = 0;
+        bars.pulse.last = (uint32_t)clock();
         fence_mbar_init();
     }
     if (warp == kIssuer) tmem_alloc<1>(smem_addr(&bars.tmem), 512);
@@ -131,7 +132,7 @@ k_grad_short(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUt
     __syncthreads();
     fence_after_sync();
     const uint32_t tmem = bars.tmem;
-    const Watch w{&bars.dead, a.waits};
+    const UnitWatch w{&bars.pulse, a.waits};
     auto s_col = [](int i) { return (uint32_t)i * Sh::kColumns; };
     auto dp_col = [](int i) { return (uint32_t)i * Sh::kColumns + 64u; };
     // lanes 64 on, columns 0 on: dk; lanes 0 on, columns DH on: dv
@@ -220,7 +221,10 @@ k_grad_short(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUt
             if (real) bars.units[b][__popc(there & below)] = u;
             if (lane == 0) bars.count[b] = __popc(there);
             __syncwarp();
-            if (lane == 0) mbar_arrive<1>(smem_addr(&bars.batch_full[b]));
+            if (lane == 0) {
+                w.further();
+                mbar_arrive<1>(smem_addr(&bars.batch_full[b]));
+            }
             b ^= 1u;
             parity ^= b ^ 1u;
         }
@@ -432,6 +436,7 @@ k_grad_short(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUt
             const int tiles = (u.rows + 127) / 128, head = u.kv_head << log_pack;
             bool counts = false;             // of a key a lane; its place may hold others at the end
             for (int t = 0; t < tiles; ++t) {
+                if (lane == 0 && (t & 63) == 63) w.further();
                 const int row = t * 128 + r;
                 // whole: 32 rows leave by TMA, where there is room for them on their way (one group has none)
                 const bool in = row < u.rows, whole = GROUPS == 2 && t * 128 + quad * 32 + 32 <= u.rows && pack <= 32;
@@ -626,7 +631,7 @@ k_grad_short(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUt
     fence_before_sync();
     __syncthreads();
     fence_after_sync();
-    if (*(volatile int*)&bars.dead) {
+    if (*(volatile int*)&bars.pulse.dead) {
         // a wait ran out: wait once more, bounded, for what is in flight
         const long long begun = clock64();
         auto bounded = [&](uint32_t bar, uint32_t parity) {

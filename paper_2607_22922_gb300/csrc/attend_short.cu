@@ -51,7 +51,7 @@ struct ShortBars {
     int count[kBatches];            // -1: there are no more
     alignas(16) float most[KS][KEYS];    // read four at a time: infinity, or -infinity for a key that does not count
     uint32_t tmem;
-    int dead;
+    Pulse pulse;
 };
 
 __device__ __forceinline__ uint64_t keys_rows_desc(uint32_t addr, uint32_t half_bytes) {
@@ -104,7 +104,8 @@ k_attend_short(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
             mbar_init(smem_addr(&bars.o_full[i]), 1);
         }
         mbar_init(smem_addr(&bars.drain), 1);
-        bars.dead = 0;
+        bars.pulse.dead = 0;
+        bars.pulse.last = (uint32_t)clock();
         fence_mbar_init();
     }
     if (warp == kIssuer) tmem_alloc<1>(smem_addr(&bars.tmem), 512);
@@ -112,7 +113,10 @@ k_attend_short(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
     __syncthreads();
     fence_after_sync();
     const uint32_t tmem = bars.tmem;
-    const Watch w{&bars.dead, a.waits};
+    // within a unit, and behind other units.  (With the second for all of them the 1024 sequences
+    // above take 78 us.)
+    const Watch w{&bars.pulse.dead, a.waits};
+    const UnitWatch far{&bars.pulse, a.waits};
     auto s_col = [](int g) { return (uint32_t)g * KEYS; };
     auto o_col = [](int g) { return (uint32_t)GROUPS * KEYS + (uint32_t)g * DH; };
     int q_filled = 0, kv_filled = 0;             // by the loader's thread
@@ -125,7 +129,7 @@ k_attend_short(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
         uint32_t b = 0, parity = 0;
         for (;;) {
             if (!mbar_try_wait(smem_addr(&bars.batch_full[b]), parity) && !idle()) return false;
-            bool ok = w.wait(smem_addr(&bars.batch_full[b]), parity);
+            bool ok = far.wait(smem_addr(&bars.batch_full[b]), parity);
             if (!alone) ok = __all_sync(0xFFFFFFFFu, ok);
             const int n = ok ? bars.count[b] : -1;
             if (n < 0) return ok;
@@ -191,15 +195,18 @@ k_attend_short(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
             u.parity = (uint8_t)((turn + at / KS) & 1u);
             turn += (place + (uint32_t)all) / KS;
             place = (place + (uint32_t)all) % KS;
-            if (!__all_sync(0xFFFFFFFFu, w.wait(smem_addr(&bars.batch_empty[b]), parity))) break;
+            if (!__all_sync(0xFFFFFFFFu, far.wait(smem_addr(&bars.batch_empty[b]), parity))) break;
             if (u.rows > 0) bars.units[b][__popc(there & ((1u << lane) - 1u))] = u;
             if (lane == 0) bars.count[b] = __popc(there);
             __syncwarp();
-            if (lane == 0) mbar_arrive<1>(smem_addr(&bars.batch_full[b]));
+            if (lane == 0) {
+                far.further();
+                mbar_arrive<1>(smem_addr(&bars.batch_full[b]));
+            }
             b = (b + 1) % kBatches;
             parity ^= b == 0;
         }
-        if (__all_sync(0xFFFFFFFFu, w.wait(smem_addr(&bars.batch_empty[b]), parity)) && lane == 0) {
+        if (__all_sync(0xFFFFFFFFu, far.wait(smem_addr(&bars.batch_empty[b]), parity)) && lane == 0) {
             bars.count[b] = -1;
             mbar_arrive<1>(smem_addr(&bars.batch_full[b]));
         }
@@ -370,7 +377,7 @@ k_attend_short(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
                 const int left = u.keys - j * KEYS, n = left < KEYS ? left : KEYS;
                 // in this order: a wait for `fixed` may not be two fills ahead, and the group sees
                 // those of its own units alone; s there means that the fill before was used
-                ok = __all_sync(0xFFFFFFFFu, w.wait(smem_addr(&bars.s_full[group]), s_turn) &&
+                ok = __all_sync(0xFFFFFFFFu, far.wait(smem_addr(&bars.s_full[group]), s_turn) &&
                                                  w.wait(smem_addr(&bars.fixed[kp.at]), kp.parity));
                 if (!ok) break;
                 fence_after_sync();
@@ -439,6 +446,7 @@ k_attend_short(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
                 fence_before_sync();
                 __syncwarp();
                 if (lane == 0) mbar_arrive<1>(smem_addr(&bars.p_full[group]));
+                if (lane == 0 && (j & 63) == 63) far.further();
             }
             if (ok && chunks > 0) {
                 ok = __all_sync(0xFFFFFFFFu, w.wait(smem_addr(&bars.o_full[group]), o_turn));
@@ -495,7 +503,7 @@ k_attend_short(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
     fence_before_sync();
     __syncthreads();
     fence_after_sync();
-    if (*(volatile int*)&bars.dead) {
+    if (*(volatile int*)&bars.pulse.dead) {
         // a wait ran out: wait once more, bounded, for what is in flight
         const long long begun = clock64();
         auto bounded = [&](uint32_t bar, uint32_t parity) {

@@ -66,6 +66,36 @@ __device__ __forceinline__ void tmem_st16(uint32_t addr, const uint32_t (&r)[16]
 }
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
+// The waits of a kernel whose units may be of any size, so that one may last as long as another
+// unit's tiles: it has run out when the CTA has got no further for its bound.  A poll is one load of
+// both words: the gradient of 1000 short sequences takes 104 us so, 112 with a bound of the wait's
+// own before the second word is looked at.
+struct Pulse {
+    alignas(8) int dead;             // as Watch's
+    uint32_t last;                   // clock() when the CTA last got further
+};
+struct UnitWatch {
+    Pulse* pulse;                    // shared memory
+    Waits by;
+    __device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity) const {
+        while (!mbar_try_wait(bar, parity)) {
+            uint32_t dead, last;
+            asm volatile("ld.volatile.shared.v2.u32 {%0, %1}, [%2];" : "=r"(dead), "=r"(last) : "r"(smem_addr(pulse)) : "memory");
+            if (dead) return false;
+            // (2^32 cycles are four bounds and two seconds: polls are more frequent)
+            if ((uint32_t)clock() - last > (uint32_t)by.cycles) {
+                *(volatile int*)&pulse->dead = 1;
+                by.err[kErrWait] = 1;
+                return false;
+            }
+        }
+        return true;
+    }
+    // by the warp that finds units, for every batch, and by one thread of those that weigh, for
+    // every 64th tile of a unit: far more often than a bound, and never in a short unit
+    __device__ __forceinline__ void further() const { *(volatile uint32_t*)&pulse->last = (uint32_t)clock(); }
+};
+
 // Heads of a group that share a tile of 128 rows: all, where they divide it, else one
 inline int tc_pack(const AttendArgs& a) { return (a.group & (a.group - 1)) == 0 && a.group <= 128 ? a.group : 1; }
 
