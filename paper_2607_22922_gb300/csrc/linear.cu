@@ -44,30 +44,30 @@ __device__ __forceinline__ float2 pair_ex2(float2 x) {
 
 // g Phi(g) and its slope, two values at a time.  The lower tail is a product, so that it keeps
 // its leading digits however small it is:
-//   Phi(-x) = e^(-x^2 / 2) R(x), R(x) = erfcx(x / sqrt(2)) / 2 = t P(t), t = 1 / (1 + 0.35 x)
-// and P, of degree 6, was fitted to R over 0 <= x <= 14: within 5e-8 of Phi where it is large,
-// within 5e-6 of its own value where it is small, down to the exponential's 2^-126.  (Phi as 1/2 + (1/2 - tail) loses all digits
-// from -5 down.  17408 x 960 -> 2560 with the residual takes 80.9 us where that takes 79.6; 1 - tail
-// as a pair 82.0, by a sign that multiplies 82.5.)
+//   Phi(-x) = e^(-x^2 / 2) R(x), R(x) = erfcx(x / sqrt(2)) / 2 = Q(t), t = 1 / (1 + 0.29 x)
+// and Q, of degree 6, was fitted to R over 0 <= x <= 13.4, where the exponential vanishes: within
+// 8.3e-8 of Phi where it is large, within 1.2e-5 of its own value where it is small.  (Phi as 1/2 +
+// (1/2 - tail) loses all digits from -5 down.  17408 x 960 -> 2560 with the residual takes 80.3 us,
+// with that 80.5; with t P(t), P of degree 6, 81.9.)
 __device__ __forceinline__ void gelu(float2 g, float2& v, float2& slope) {
     auto both2 = [](float c) { return make_float2(c, c); };
     const float2 e = pair_ex2(mul_(mul_(g, g), both2(-0.5f * 1.44269504f)));
-    const float2 d = fma_(make_float2(fabsf(g.x), fabsf(g.y)), both2(0.35f), both2(1.f));
+    const float2 d = fma_(make_float2(fabsf(g.x), fabsf(g.y)), both2(0.29f), both2(1.f));
     const float2 t = make_float2(rcp(d.x), rcp(d.y));
-    float2 q = fma_(t, both2(0.0442778468f), both2(-0.183066979f));
-    q = fma_(t, q, both2(0.208882123f));
-    q = fma_(t, q, both2(0.0107296752f));
-    q = fma_(t, q, both2(0.142377868f));
-    q = fma_(t, q, both2(0.137036189f));
-    q = fma_(t, q, both2(0.139763325f));
-    const float2 tail = mul_(mul_(t, e), q);
+    float2 q = fma_(t, both2(-0.0930059254f), both2(0.301860571f));
+    q = fma_(t, q, both2(-0.120859757f));
+    q = fma_(t, q, both2(0.202541292f));
+    q = fma_(t, q, both2(0.0905459449f));
+    q = fma_(t, q, both2(0.119104102f));
+    q = fma_(t, q, both2(-0.000186309364f));
+    const float2 tail = mul_(e, q);
     const float2 p = make_float2(g.x < 0.f ? tail.x : 1.f - tail.x, g.y < 0.f ? tail.y : 1.f - tail.y);
     v = mul_(g, p);
     slope = fma_(mul_(g, both2(0.39894228f)), e, p);
 }
 
 // act and act' of two values, two float32 operations per instruction: the epilogue of 17408 x
-// 960 -> 2560 with GELU takes 16 instructions a value one by one, 11 to 12 so.
+// 960 -> 2560 with GELU takes 16 instructions a value one by one, 11 so.
 template <int ACT>
 __device__ __forceinline__ void activations(float2 g, float2& v, float2& slope) {
     auto both2 = [](float c) { return make_float2(c, c); };

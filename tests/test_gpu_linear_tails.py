@@ -4,8 +4,8 @@ digits, and a token's row is the same whichever of the layer's kernels makes it.
 The inputs make x w^T one exact product, so that the activation alone is off.  Its terms,
 for -13 <= z <= 0, with U = 2^-24: the exponent z^2 / 2 log2(e), at most 122, is rounded
 three times, the constant among them (122 ln(2) 3 U < 1.6e-5 of the exponential); the
-polynomial is within 1e-5 of the tail's own value; the exponential, the reciprocal and ten
-operations are within 20 U (1.2e-6).  In all below 2.8e-5 < 2^-15 of each term."""
+polynomial is within 1.2e-5 of the tail's own value; the exponential, the reciprocal and ten
+operations are within 20 U (1.2e-6).  In all below 3e-5 < 2^-15 of each term."""
 import math
 
 import pytest
