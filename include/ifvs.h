@@ -694,7 +694,8 @@ int ifvs_attend(ifvs_layers* L, const ifvs_attend_params* p, const void* q, cons
  *              are computed again instead
  *   d_out, dq as q; dk, dv as k: for heads that share keys their sum
  * Zeros for queries without keys, keys without queries and padding.  p and its gradient
- * are rounded to `type` before the products that sum them.  Errors as ifvs_attend.
+ * are rounded to `type` before the products that sum them (in IFVS_T_F16 a gradient of p
+ * times p beyond 65504 becomes infinite).  Errors as ifvs_attend.
  */
 int ifvs_attend_grad(ifvs_layers* L, const ifvs_attend_params* p, const void* q, const void* k, const void* v,
                      const void* out, const float* lse, const void* d_out, void* dq, void* dk, void* dv);

@@ -496,6 +496,8 @@ Plan plan_of(const AttendArgs& a) {
     // Both sides in us, 8 heads with keys of their own, bfloat16, one call after the other:
     // 128 queries x 256 keys, heads of 64 (of 128): 1 sequence 8.0 against k_attend's 10.1 (9.3
     // and 12.1), 8 sequences 8.4 against 14.4 (9.5 and 16.2); 4 of 1024 x 1024 18.9 against 50.8.
+    // (The bound on the rows is not moved for many keys, where it costs: of 16 000 keys 127 queries take
+    // 39 in k_attend, 128 here 25 (78 and 27).)
     p.tc = a.Tq * p.pack / a.B >= 128 && a.Tk / a.B >= 256;
     // Many sequences, each with a good part of a tile of 128 rows, whose keys mostly are one
     // chunk.  200 sequences of 120 x 60, heads of 64: 24.2 against k_attend's 34.8; of 32 x 40

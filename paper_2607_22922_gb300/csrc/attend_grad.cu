@@ -509,6 +509,8 @@ Plan plan_of(const AttendArgs& a) {
     // Both sides in us, 8 heads with keys of their own, bfloat16, one call after the other: 1
     // sequence of 128 queries x 256 keys, heads of 64 (of 128), 9.7 against k_attend_keys and _rows'
     // 17.8 (12.9 and 24.5), 64 of them 76 and 179 (112 and 446), 4 of 1024 x 1024 53 and 253.
+    // (The bound on the rows is not moved for many keys, where it costs: of 16 000 keys 127 queries take
+    // 859 in k_attend_rows, whose CTAs walk all of the keys, 128 here 108 (1255 and 259).)
     p.tc = a.Tq * p.pack / a.B >= 128 && a.Tk / a.B >= 256;
     p.delta_bytes = p.tc ? padded((size_t)a.Tq * a.heads * 4) : 0;
     // Sequences whose keys mostly are one chunk: 200 of 32 x 40, heads of 64, 35 against

@@ -12,7 +12,7 @@
 //
 // What bounds a tile is the chain of its waits (rows, s and dp, weights, dq, its rows on their
 // way), two of them at a time: 1000 sequences of 60 to 68 queries and up to 65 keys, 8 heads of
-// 64 over 2, take 108 to 114 us with k_attend_rows, 2.7 TB/s.  The issuing warp takes whichever group's
+// 64 over 2, take 104 to 112 us with k_attend_rows, 2.8 TB/s.  The issuing warp takes whichever group's
 // weights come first; in the order of the tiles, with a warp more (128 registers, which spill)
 // and all keys of a bundle before its rows it takes 137.
 #include "attend_tc.cuh"

@@ -10,7 +10,7 @@
 // maximum, then for the weights, which leaves registers for four groups.  Sequences with more keys go on chunk by chunk as in
 // attend_tc.cu.  Rows leave through shared memory by TMA, 32 at a time.
 //
-// 1024 sequences of 120 queries and 0 to 65 keys, 8 heads of 64 over 2: 67 us, 4.0 TB/s.  With
+// 1024 sequences of 120 queries and 0 to 65 keys, 8 heads of 64 over 2: 68 us, 4.0 TB/s.  With
 // three stages of queries and six of keys (four and five here) and the MMAs of whichever
 // group's weights come first it takes 80: the issuing warp's polls cost the others more than
 // they save.

@@ -10,8 +10,8 @@
 // where a score exceeds it by 2^8: until then the weights are at most 2^8 and as exact.
 //
 // 4099 queries x 17 403 keys, 8 heads of 128 in bfloat16: 232 us, 1.26 PFLOP/s, on 128 of the
-// 152 SMs (plan_of in attend.cu); the tensor pipe is active half of the time, the rest are the
-// waits between the MMAs and the exponentials of one tile.  With all weights of a tile at once
+// 152 SMs (plan_of in attend.cu); their tensor pipes are active 64 % of the time, the rest are
+// the waits between the MMAs and the exponentials of one tile.  With all weights of a tile at once
 // for their MMAs it takes 246, with a quarter at a time 245; with all and twice the warps, half of a row's scores a thread and
 // the maximum by way of shared memory, 354.
 #include "attend_tc.cuh"
